@@ -221,6 +221,80 @@ int dl_append_step_tiled_noalloc(const dl_desc* desc, const dl_state* state,
                                  const dl_token* tok, float* o, const int32_t* slots,
                                  int32_t n, int32_t value_tiles, hipStream_t stream);
 
+/* ---------------------------------------------------------------- whole sequences
+ * The recurrence over ragged batches of sequences (prompts, training documents): token
+ * rows of all sequences packed one after the other, [N, H, ...], sequence i with its own
+ * initial and final state (a slot of a [B,H,dk,dv] buffer).  Lengths live in device memory;
+ * the host knows n (sequences) and N (token rows the buffers hold) only.  Sequences may be
+ * empty: their state passes through.  Rows behind the last sequence belong to nobody: they
+ * are never used, and output rows there stay as they were. */
+#define DL_CHUNK 32   /* tokens of a chunk of the tables below */
+
+/* Chunk rows the tables of n sequences with up to `tokens` token rows have. */
+#define DL_MAX_CHUNKS(n, tokens) ((tokens) / DL_CHUNK + (n))
+
+/* Chunk tables and slot maps of a ragged batch (device memory, owned by the caller). */
+typedef struct {
+  int32_t* cu_tokens; /* [n+1] first token row of each sequence; [n] = rows in use         */
+  int32_t* cu_chunks; /* [n+1] first chunk of each sequence; [n] = chunks in use           */
+  int32_t* chunks;    /* [DL_MAX_CHUNKS(n,N), 4], 16-byte aligned: (sequence, first token  */
+                      /*       row, tokens, slot); (-1, 0, 0, -1) past the chunks in use   */
+  int32_t* row_slot;  /* [N]   slot of every token row; -1 past the rows in use            */
+  int32_t* seq_slot;  /* [n]   slot of every sequence                                      */
+} dl_tables;
+
+/* Build the tables from lens [n] (device) and slots (device int32 [n], or NULL: sequence i
+ * has slot i, which requires n <= num_slots).  What only the device can see is ORed into
+ * *err (device, may be NULL): 1 = a slot id outside [0, num_slots) (the sequence's slot
+ * becomes -1, and dl_prefill and dl_prefill_backward skip it), 4 = a length below 0 (taken
+ * as 0) or past the N token rows (cut there).  n == 0 is a no-op. */
+int dl_chunk_tables(const int32_t* lens, const int32_t* slots, int32_t n, int32_t tokens,
+                    int32_t num_slots, const dl_tables* tables, int32_t* err,
+                    hipStream_t stream);
+
+/* Bytes of workspace dl_prefill (backward == 0) or dl_prefill and dl_prefill_backward
+ * (backward != 0) need for n sequences and N token rows.  Writes *bytes. */
+int dl_prefill_workspace_bytes(const dl_desc* desc, int32_t n, int32_t tokens,
+                               int32_t backward, size_t* bytes);
+
+/* The recurrence over whole sequences (Eq. 3, token by token in exact arithmetic): for
+ * every sequence of the tables, from S_in[slot] (S_in == NULL: zero) to S_out[slot] (both
+ * [B,H,dk,dv] of state_dtype; S_out may be S_in), with o [N,H,dv] in in_dtype -- a prompt's
+ * outputs go on to products in that type, and a state read back in it would not gain from
+ * wider ones.  tok holds N rows.  All arithmetic keeps fp32 accuracy; S_out is rounded once.
+ * The log of a DeltaLog state is not looked at: flush it first (dl_merge without a token)
+ * where S_in is the base of a state with a log, and reset len where S_out is.
+ * tables: as dl_chunk_tables left them for the same n and N (row_slot is not read).
+ * workspace: at least dl_prefill_workspace_bytes(desc, n, N, 0, ..) bytes, 256-byte
+ * aligned; scratch, never read across calls; calls that share one must not overlap.
+ * desc->merge_interval is validated but otherwise ignored.  n == 0 is a no-op. */
+int dl_prefill(const dl_desc* desc, const void* S_in, void* S_out, const dl_token* tok, void* o,
+               const dl_tables* tables, int32_t n, int32_t tokens, void* workspace,
+               size_t workspace_bytes, hipStream_t stream);
+
+/* Gradients, shaped as what they belong to; dq, dk, dv in in_dtype, dS in state_dtype. */
+typedef struct {
+  void*  dq;    /* [N,H,dk]                                                              */
+  void*  dk;    /* [N,H,dk]                                                              */
+  void*  dv;    /* [N,H,dv]                                                              */
+  float* dbeta; /* [N,H] (GDN/KDA; else ignored)                                         */
+  float* dlam;  /* [N,H,dl] (ignored for LINATTN)                                        */
+  float* du;    /* [H,dk] (RWKV6; else ignored)                                          */
+  void*  dS;    /* [B,H,dk,dv] of the initial states; may be NULL.  Slots that no        */
+                /* sequence has stay as they were.                                       */
+} dl_grads;
+
+/* Backward pass of dl_prefill: from d_o [N,H,dv] (in_dtype) and dS_out [B,H,dk,dv] (of the
+ * final states, state_dtype; NULL: zero) to every gradient, for the same S_in, tok and
+ * tables as the forward call.  Nothing is kept from the forward call: the states are
+ * computed again.  S_in is read, so a forward call that wrote its states in place has
+ * destroyed what this call needs.  dS must not alias S_in; it may alias dS_out.
+ * workspace: dl_prefill_workspace_bytes(desc, n, N, 1, ..) bytes, 256-byte aligned. */
+int dl_prefill_backward(const dl_desc* desc, const void* S_in, const dl_token* tok,
+                        const void* d_o, const void* dS_out, const dl_grads* grads,
+                        const dl_tables* tables, int32_t n, int32_t tokens, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+
 /* Human-readable name of a dl_status value (static storage). */
 const char* dl_status_str(int status);
 

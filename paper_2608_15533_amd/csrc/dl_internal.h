@@ -74,4 +74,14 @@ int tiled_launch(const dl_desc* desc, const dl_state* state, const dl_token* tok
                  const int32_t* slots, int32_t n, int32_t value_tiles, bool split, float* coef,
                  hipStream_t stream);
 
+// Whole sequences: argument checks that the front end shares, and the launches.
+int check_sequences(const dl_desc* desc, const dl_token* tok, const dl_tables* tables, int32_t n,
+                    int32_t tokens, const void* workspace, size_t workspace_bytes, bool backward);
+hipError_t launch_tables(const int32_t* lens, const int32_t* slots, int32_t n, int32_t tokens,
+                         int32_t num_slots, const dl_tables& t, int32_t* err, int32_t max_chunks,
+                         hipStream_t s);
+struct SeqParams;
+hipError_t launch_forward(const dl_desc* desc, const SeqParams& p, hipStream_t s);
+hipError_t launch_backward(const dl_desc* desc, const SeqParams& p, hipStream_t s);
+
 }  // namespace dl

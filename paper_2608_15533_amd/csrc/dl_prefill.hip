@@ -1,0 +1,168 @@
+// Whole sequences: entry points (checks, then launches) and the forward pass.
+#include "dl_prep.hpp"
+#include "dl_seq.hpp"
+
+namespace dl {
+namespace {
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+template <typename K>
+hipError_t start(K* kernel, int64_t grid, int block, const SeqParams& p, hipStream_t s) {
+  SeqParams q = p;
+  void* args[] = {&q};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(unsigned(grid)), dim3(block),
+                         args, 0, s);
+}
+
+template <int DC, int DK, typename TIN>
+hipError_t launch_prep(const SeqParams& p, hipStream_t s) {
+  return start(&prep_kernel<DC, DK, TIN>, int64_t(p.max_chunks) * p.H, 256, p, s);
+}
+
+template <int DK, typename TIN>
+hipError_t launch_forward_shape(int op, const SeqParams& p, hipStream_t s) {
+  hipError_t e;
+  if (op == DL_OP_RWKV6) e = launch_prep<DC_BONUS, DK, TIN>(p, s);
+  else if (op == DL_OP_KDA || op == DL_OP_GLA) e = launch_prep<DC_KEY, DK, TIN>(p, s);
+  else e = launch_prep<DC_SCALAR, DK, TIN>(p, s);
+  if (e != hipSuccess) return e;
+  const int64_t grid = int64_t(p.n) * p.H * (p.dv / 16);
+  return p.delta ? start(&forward_kernel<DK, 1, true, TIN>, grid, 64, p, s)
+                 : start(&forward_kernel<DK, 1, false, TIN>, grid, 64, p, s);
+}
+
+}  // namespace
+
+hipError_t launch_forward(const dl_desc* d, const SeqParams& p, hipStream_t s) {
+  if (d->in_dtype == DL_BF16)
+    return d->dk == 128 ? launch_forward_shape<128, uint16_t>(d->op, p, s)
+                        : launch_forward_shape<64, uint16_t>(d->op, p, s);
+  return d->dk == 128 ? launch_forward_shape<128, float>(d->op, p, s)
+                      : launch_forward_shape<64, float>(d->op, p, s);
+}
+
+namespace {
+
+int check_counts(const dl_desc* d, int32_t n, int32_t tokens) {
+  if (n < 0 || tokens < 0 || n > d->num_slots) return DL_E_SHAPE;
+  // Grids of one workgroup per (chunk, head) and per (sequence, head, 16 value columns).
+  const int64_t chunks = int64_t(tokens) / DL_CHUNK + n;
+  if (chunks * d->heads > int64_t(0x7fffffff)) return DL_E_SHAPE;
+  if (int64_t(n) * d->heads * (d->dv / 16) > int64_t(0x7fffffff)) return DL_E_SHAPE;
+  return DL_OK;
+}
+
+// The descriptor's own checks are those of a call that drives no rows.
+int check_desc_only(const dl_desc* d) { return dl_readout(d, nullptr, nullptr, nullptr, nullptr, 0, nullptr); }
+
+SeqParams params(const dl_desc* d, const void* S_in, const dl_token* tok, const dl_tables* t,
+                 int32_t n, int32_t tokens, void* ws) {
+  SeqParams p{};
+  p.S_in = S_in;
+  p.q = tok->q;
+  p.k = tok->k;
+  p.v = tok->v;
+  p.delta = d->op == DL_OP_GDN || d->op == DL_OP_KDA;
+  p.beta = p.delta ? tok->beta : nullptr;
+  p.lam = d->op == DL_OP_LINATTN ? nullptr : tok->lam;
+  p.u = d->op == DL_OP_RWKV6 ? tok->u : nullptr;
+  p.cu_tokens = t->cu_tokens;
+  p.cu_chunks = t->cu_chunks;
+  p.chunks = t->chunks;
+  p.seq_slot = t->seq_slot;
+  p.ws = static_cast<unsigned char*>(ws);
+  p.n = n;
+  p.N = tokens;
+  p.B = d->num_slots;
+  p.H = d->heads;
+  p.dv = d->dv;
+  p.max_chunks = tokens / DL_CHUNK + n;
+  p.state_bf16 = d->state_dtype == DL_BF16;
+  return p;
+}
+
+}  // namespace
+}  // namespace dl
+
+#define DL_TRY(x)                 \
+  do {                            \
+    const int rc_ = (x);          \
+    if (rc_ != DL_OK) return rc_; \
+  } while (0)
+
+extern "C" {
+
+int dl_chunk_tables(const int32_t* lens, const int32_t* slots, int32_t n, int32_t tokens,
+                    int32_t num_slots, const dl_tables* t, int32_t* err, hipStream_t stream) {
+  if (n < 0 || tokens < 0 || num_slots < 1) return DL_E_SHAPE;
+  if (int64_t(tokens) / DL_CHUNK + n > int64_t(0x7fffffff)) return DL_E_SHAPE;
+  if (n == 0) return DL_OK;
+  if (!slots && n > num_slots) return DL_E_SHAPE;
+  if (!lens || !t || !t->cu_tokens || !t->cu_chunks || !t->chunks || !t->seq_slot) return DL_E_NULL;
+  if (tokens > 0 && !t->row_slot) return DL_E_NULL;
+  if (!dl::aligned(lens, 4) || !dl::aligned(slots, 4) || !dl::aligned(t->cu_tokens, 4) ||
+      !dl::aligned(t->cu_chunks, 4) || !dl::aligned(t->chunks, 16) ||
+      !dl::aligned(t->row_slot, 4) || !dl::aligned(t->seq_slot, 4) || !dl::aligned(err, 4))
+    return DL_E_ALIGN;
+  const hipError_t e = dl::launch_tables(lens, slots, n, tokens, num_slots, *t, err,
+                                         tokens / DL_CHUNK + n, stream);
+  return e == hipSuccess ? DL_OK : DL_E_HIP;
+}
+
+int dl_prefill_workspace_bytes(const dl_desc* desc, int32_t n, int32_t tokens, int32_t backward,
+                               size_t* bytes) {
+  DL_TRY(dl::check_desc_only(desc));
+  DL_TRY(dl::check_counts(desc, n, tokens));
+  if (!bytes) return DL_E_NULL;
+  const dl::WsLayout w{desc->dk, desc->dv, backward != 0};
+  *bytes = size_t(w.block()) * size_t(tokens / DL_CHUNK + n) * size_t(desc->heads);
+  return DL_OK;
+}
+
+int dl_prefill(const dl_desc* desc, const void* S_in, void* S_out, const dl_token* tok, void* o,
+               const dl_tables* tables, int32_t n, int32_t tokens, void* workspace,
+               size_t workspace_bytes, hipStream_t stream) {
+  DL_TRY(dl::check_desc_only(desc));
+  DL_TRY(dl::check_counts(desc, n, tokens));
+  if (n == 0) return DL_OK;               // nothing to do, whatever the other pointers are
+  DL_TRY(dl::check_sequences(desc, tok, tables, n, tokens, workspace, workspace_bytes, false));
+  if (!S_out || !o) return DL_E_NULL;
+  if (!dl::aligned(S_in, 16) || !dl::aligned(S_out, 16) || !dl::aligned(o, 16)) return DL_E_ALIGN;
+  dl::SeqParams p = dl::params(desc, S_in, tok, tables, n, tokens, workspace);
+  p.S_out = S_out;
+  p.o = o;
+  return dl::launch_forward(desc, p, stream) == hipSuccess ? DL_OK : DL_E_HIP;
+}
+
+int dl_prefill_backward(const dl_desc* desc, const void* S_in, const dl_token* tok,
+                        const void* d_o, const void* dS_out, const dl_grads* g,
+                        const dl_tables* tables, int32_t n, int32_t tokens, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream) {
+  DL_TRY(dl::check_desc_only(desc));
+  DL_TRY(dl::check_counts(desc, n, tokens));
+  if (n == 0) return DL_OK;               // nothing to do, whatever the other pointers are
+  DL_TRY(dl::check_sequences(desc, tok, tables, n, tokens, workspace, workspace_bytes, true));
+  if (!d_o || !g || !g->dq || !g->dk || !g->dv) return DL_E_NULL;
+  dl::SeqParams p = dl::params(desc, S_in, tok, tables, n, tokens, workspace);
+  if ((p.delta && !g->dbeta) || (p.lam && !g->dlam) || (p.u && !g->du)) return DL_E_NULL;
+  if (!dl::aligned(S_in, 16) || !dl::aligned(d_o, 16) || !dl::aligned(dS_out, 16) ||
+      !dl::aligned(g->dq, 16) || !dl::aligned(g->dk, 16) || !dl::aligned(g->dv, 16) ||
+      !dl::aligned(g->dS, 16) || !dl::aligned(g->dbeta, 4) || !dl::aligned(g->dlam, 4) ||
+      !dl::aligned(g->du, 4))
+    return DL_E_ALIGN;
+  p.bwd = true;
+  if (dl::launch_forward(desc, p, stream) != hipSuccess) return DL_E_HIP;   // states and E again
+  p.d_o = d_o;
+  p.dS_out = dS_out;
+  p.S_out = g->dS;
+  p.dq = g->dq;
+  p.dk_ = g->dk;
+  p.dv_ = g->dv;
+  p.dbeta = p.delta ? g->dbeta : nullptr;
+  p.dlam = p.lam ? g->dlam : nullptr;
+  p.du = p.u ? g->du : nullptr;
+  return dl::launch_backward(desc, p, stream) == hipSuccess ? DL_OK : DL_E_HIP;
+}
+
+}  // extern "C"

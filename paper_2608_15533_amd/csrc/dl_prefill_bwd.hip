@@ -1,0 +1,44 @@
+// Whole sequences: the backward pass's launches.
+#include "dl_grad.hpp"
+#include "dl_seq.hpp"
+
+namespace dl {
+namespace {
+
+template <typename K>
+hipError_t start(K* kernel, int64_t grid, int block, const SeqParams& p, hipStream_t s) {
+  SeqParams q = p;
+  void* args[] = {&q};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(unsigned(grid)), dim3(block),
+                         args, 0, s);
+}
+
+template <int DC, int DK, typename TIN>
+hipError_t launch_grad(const SeqParams& p, hipStream_t s) {
+  hipError_t e = start(&grad_kernel<DC, DK, TIN>, int64_t(p.max_chunks) * p.H, 256, p, s);
+  if (DC == DC_BONUS && e == hipSuccess) e = start(&bonus_grad_kernel<DK>, p.H, 1024, p, s);
+  return e;
+}
+
+template <int DK, typename TIN>
+hipError_t launch_backward_shape(int op, const SeqParams& p, hipStream_t s) {
+  const int64_t grid = int64_t(p.n) * p.H * (p.dv / 16);
+  const hipError_t e = p.delta ? start(&backward_kernel<DK, 1, true, TIN>, grid, 64, p, s)
+                               : start(&backward_kernel<DK, 1, false, TIN>, grid, 64, p, s);
+  if (e != hipSuccess) return e;
+  if (op == DL_OP_RWKV6) return launch_grad<DC_BONUS, DK, TIN>(p, s);
+  if (op == DL_OP_KDA || op == DL_OP_GLA) return launch_grad<DC_KEY, DK, TIN>(p, s);
+  return launch_grad<DC_SCALAR, DK, TIN>(p, s);
+}
+
+}  // namespace
+
+hipError_t launch_backward(const dl_desc* d, const SeqParams& p, hipStream_t s) {
+  if (d->in_dtype == DL_BF16)
+    return d->dk == 128 ? launch_backward_shape<128, uint16_t>(d->op, p, s)
+                        : launch_backward_shape<64, uint16_t>(d->op, p, s);
+  return d->dk == 128 ? launch_backward_shape<128, float>(d->op, p, s)
+                      : launch_backward_shape<64, float>(d->op, p, s);
+}
+
+}  // namespace dl

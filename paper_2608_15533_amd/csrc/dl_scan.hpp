@@ -1,0 +1,163 @@
+// Shared pieces of the sequence kernels (prefill and its backward pass): fp32 values on the
+// bf16 matrix cores, the workspace's layout, chunk bookkeeping.
+//
+// The recurrence of Eq. 3 over a chunk of T = 32 tokens, with l_i the log-decay summed from
+// the chunk's start through token i (per key, or the same for all keys; 0 without decay), S
+// the state before the chunk, and (x)_i a row of a token matrix:
+//
+//   Kh_i = k_i e^{l_i}     Qh_i = q_i e^{l_i}     Kb_i = k_i e^{l_T - l_i}
+//   G_ij = sum_r k_ir k_jr e^{l_ir - l_jr}  (i > j)
+//   P_ij = sum_r q_ir k_jr e^{l_ir - l_jr}  (i >= j)
+//   U = V                                        (pair (k, v))
+//   U = beta E,  (I + G beta) E = V - Kh S       (delta rule: E = N (V - Kh S))
+//   O = Qh S + P U           S <- e^{l_T} S + Kb^T U
+//
+// RWKV6 reads the state before its token: q_i takes l_{i-1}, and P_ii = sum_r q u k.
+// Every exponent that is taken is of a sum of log-decays over a stretch of tokens, so with
+// log-decays <= 0 nothing overflows.  log-decays below -104 (e^-104 is 0 in fp32) count as
+// -104: a gate of exactly 0 (log -inf) forgets exactly, with no inf - inf.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "deltalog.h"
+#include "dl_internal.h"
+
+namespace dl {
+
+constexpr int CT = DL_CHUNK;   // tokens of a chunk
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+// An fp32 operand as two bf16 numbers: hi the nearest bf16, lo the nearest bf16 to what hi
+// leaves.  hi + lo is within 2^-18 of the value (half a bf16 step, twice), and of the
+// product of two such operands the three terms hi hi, hi lo and lo hi are kept: what is left
+// out is another 2^-18.  Three bf16 MFMAs of 32 terms take 48 cycles, eight fp32 ones 256.
+struct Split {
+  bf16x8 hi, lo;
+};
+
+__device__ __forceinline__ Split split8(const float* x) {
+  Split s;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s.hi[e] = (__bf16)x[e];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s.lo[e] = (__bf16)(x[e] - (float)s.hi[e]);
+  return s;
+}
+
+// acc += a b over 32 terms.  Lane l holds of the 16x16 result rows 4(l/16)+r, column l%16;
+// of a row l%16, of b column l%16, and of both the same eight terms: which eight is free as
+// long as a and b agree.  Natural order: terms 8(l/16)+e.  State order: terms
+// 16(e/4)+4(l/16)+e%4, which makes two 16x16 results of an earlier product, side by side, an
+// operand without any exchange between lanes.
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 acc) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma3(const Split& a, const Split& b, f32x4 acc) {
+  acc = mma(a.lo, b.hi, acc);
+  acc = mma(a.hi, b.lo, acc);
+  return mma(a.hi, b.hi, acc);
+}
+__device__ __forceinline__ int state_term(int lane, int e) {
+  return 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3);
+}
+
+__device__ __forceinline__ Split load_split(const uint16_t* hi, const uint16_t* lo) {
+  Split s;
+  s.hi = *reinterpret_cast<const bf16x8*>(hi);
+  s.lo = *reinterpret_cast<const bf16x8*>(lo);
+  return s;
+}
+
+__device__ __forceinline__ float widen(float x) { return x; }
+__device__ __forceinline__ float widen(uint16_t x) { return __uint_as_float(uint32_t(x) << 16); }
+__device__ __forceinline__ void narrow(float* p, float x) { *p = x; }
+__device__ __forceinline__ void narrow(uint16_t* p, float x) {
+  const __bf16 b = (__bf16)x;             // nearest even
+  *p = __builtin_bit_cast(uint16_t, b);
+}
+
+// A state or state gradient of either dtype.
+__device__ __forceinline__ float load_state(const void* S, bool bf16, int64_t i) {
+  return bf16 ? widen(static_cast<const uint16_t*>(S)[i]) : static_cast<const float*>(S)[i];
+}
+__device__ __forceinline__ void store_state(void* S, bool bf16, int64_t i, float x) {
+  if (bf16) narrow(static_cast<uint16_t*>(S) + i, x);
+  else static_cast<float*>(S)[i] = x;
+}
+
+// ------------------------------------------------------------------ workspace
+// One block per (chunk, head), chunk-major.  Operand planes are bf16 in fragment order: the
+// eight terms a lane feeds one MFMA are 16 consecutive bytes, a wave's load 1 KiB.
+//   rows   token x key   [token tile 2][key step dk/32][lane 64][8]   (state order of keys)
+//   cols   key x token   [key tile dk/16][lane 64][8]                 (state order of tokens)
+//   square token x token [token tile 2][lane 64][8]                   (state order of tokens)
+struct WsLayout {
+  int dk, dv;
+  bool bwd;
+  // offsets in bytes into a block
+  __host__ __device__ int plane() const { return CT * dk * 2; }
+  __host__ __device__ int sq() const { return CT * CT * 2; }
+  __host__ __device__ int kh() const { return 0; }                       // rows, hi then lo
+  __host__ __device__ int qh() const { return 2 * plane(); }             // rows
+  __host__ __device__ int kbt() const { return 4 * plane(); }            // cols
+  __host__ __device__ int n() const { return 6 * plane(); }              // square
+  __host__ __device__ int p() const { return n() + 2 * sq(); }           // square
+  __host__ __device__ int dec() const { return p() + 2 * sq(); }         // fp32 [dk] e^{l_T}
+  __host__ __device__ int beta() const { return dec() + dk * 4; }        // fp32 [CT]
+  __host__ __device__ int fwd_end() const { return beta() + CT * 4; }
+  // backward only
+  __host__ __device__ int kb() const { return fwd_end(); }               // rows
+  __host__ __device__ int qht() const { return kb() + 2 * plane(); }     // cols
+  __host__ __device__ int kht() const { return qht() + 2 * plane(); }    // cols
+  __host__ __device__ int mt() const { return kht() + 2 * plane(); }     // square
+  __host__ __device__ int pt() const { return mt() + 2 * sq(); }         // square
+  __host__ __device__ int s0() const { return pt() + 2 * sq(); }         // fp32 [dk][dv]
+  __host__ __device__ int ds() const { return s0() + dk * dv * 4; }      // fp32 [dk][dv]
+  __host__ __device__ int e() const { return ds() + dk * dv * 4; }       // fp32 [CT][dv]
+  __host__ __device__ int z() const { return e() + CT * dv * 4; }        // fp32 [CT][dv]
+  __host__ __device__ int du() const { return z() + CT * dv * 4; }       // fp32 [dk]
+  __host__ __device__ int bwd_end() const { return du() + dk * 4; }
+  __host__ __device__ int64_t block() const { return bwd ? bwd_end() : fwd_end(); }
+};
+
+// Everything the sequence kernels need, passed by value (all pointers are device pointers).
+struct SeqParams {
+  const void* S_in;      // [B,H,dk,dv] or null (zero states)
+  void* S_out;           // [B,H,dk,dv] (backward: gradient of S_in, or null)
+  const void* dS_out;    // [B,H,dk,dv] or null (backward: gradient of the final states)
+  const void* q;         // [N,H,dk]
+  const void* k;         // [N,H,dk]
+  const void* v;         // [N,H,dv]
+  const void* d_o;       // [N,H,dv] (backward)
+  const float* beta;     // [N,H]
+  const float* lam;      // [N,H,dl]
+  const float* u;        // [H,dk]
+  void* o;               // [N,H,dv]
+  void *dq, *dk_, *dv_;  // gradients
+  float *dbeta, *dlam, *du;
+  const int32_t *cu_tokens, *cu_chunks, *chunks, *seq_slot;
+  unsigned char* ws;
+  int32_t n, N, B, H, dv, max_chunks;
+  bool delta, state_bf16, bwd;
+};
+
+struct ChunkRow {
+  int seq, first, count, slot;
+};
+// The chunk's row of the tables, or a count of 0 where there is nothing to do: no such
+// chunk, or a slot or token range that does not fit the buffers of this call.
+__device__ __forceinline__ ChunkRow chunk_row(const SeqParams& p, int c) {
+  const int32_t* t = p.chunks + 4 * int64_t(c);
+  ChunkRow r{t[0], t[1], t[2], t[3]};
+  const bool ok = r.seq >= 0 && r.seq < p.n && r.slot >= 0 && r.slot < p.B && r.first >= 0 &&
+                  r.count > 0 && r.count <= CT && r.first <= p.N - r.count;
+  if (!ok) r.count = 0;
+  return r;
+}
+
+}  // namespace dl

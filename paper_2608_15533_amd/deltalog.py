@@ -33,6 +33,7 @@ DL_OK, DL_E_NULL, DL_E_SHAPE, DL_E_DTYPE, DL_E_ALIGN, DL_E_UNSUPPORTED, DL_E_HIP
     0, -1, -2, -3, -4, -5, -6, -7)
 DL_E_SCRATCH = -8
 DL_NOALLOC_SCRATCH_BYTES = 4 << 20
+DL_CHUNK = 32
 DL_OP_GDN, DL_OP_KDA, DL_OP_RWKV6, DL_OP_LINATTN, DL_OP_RETNET, DL_OP_GLA = 0, 1, 2, 3, 4, 5
 DL_F32, DL_BF16 = 0, 1
 OP_IDS = {"gdn": DL_OP_GDN, "kda": DL_OP_KDA, "rwkv6": DL_OP_RWKV6, "linattn": DL_OP_LINATTN,
@@ -44,7 +45,9 @@ TORCH_DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 EXPORTED = ("dl_eager_step", "dl_append_step", "dl_merge", "dl_readout",
             "dl_append_step_tiled", "dl_tiled_workspace_bytes", "dl_status_str",
-            "dl_abi_version", "dl_build_flags", "dl_append_step_tiled_noalloc")
+            "dl_abi_version", "dl_build_flags", "dl_append_step_tiled_noalloc",
+            "dl_chunk_tables", "dl_prefill_workspace_bytes", "dl_prefill",
+            "dl_prefill_backward")
 
 
 class dl_desc(ctypes.Structure):
@@ -66,6 +69,18 @@ class dl_token(ctypes.Structure):
                 ("beta", ctypes.c_void_p), ("lam", ctypes.c_void_p), ("u", ctypes.c_void_p)]
 
 
+class dl_tables(ctypes.Structure):
+    _fields_ = [("cu_tokens", ctypes.c_void_p), ("cu_chunks", ctypes.c_void_p),
+                ("chunks", ctypes.c_void_p), ("row_slot", ctypes.c_void_p),
+                ("seq_slot", ctypes.c_void_p)]
+
+
+class dl_grads(ctypes.Structure):
+    _fields_ = [("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p),
+                ("dbeta", ctypes.c_void_p), ("dlam", ctypes.c_void_p), ("du", ctypes.c_void_p),
+                ("dS", ctypes.c_void_p)]
+
+
 _P = ctypes.c_void_p
 _lib.dl_eager_step.argtypes = [ctypes.POINTER(dl_desc), _P, ctypes.POINTER(dl_token), _P, _P,
                                ctypes.c_int32, _P]
@@ -83,8 +98,21 @@ _lib.dl_tiled_workspace_bytes.argtypes = [ctypes.POINTER(dl_desc), ctypes.c_int3
 _lib.dl_append_step_tiled_noalloc.argtypes = [ctypes.POINTER(dl_desc), ctypes.POINTER(dl_state),
                                               ctypes.POINTER(dl_token), _P, _P, ctypes.c_int32,
                                               ctypes.c_int32, _P]
+_lib.dl_chunk_tables.argtypes = [_P, _P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                 ctypes.POINTER(dl_tables), _P, _P]
+_lib.dl_prefill_workspace_bytes.argtypes = [ctypes.POINTER(dl_desc), ctypes.c_int32,
+                                            ctypes.c_int32, ctypes.c_int32,
+                                            ctypes.POINTER(ctypes.c_size_t)]
+_lib.dl_prefill.argtypes = [ctypes.POINTER(dl_desc), _P, _P, ctypes.POINTER(dl_token), _P,
+                            ctypes.POINTER(dl_tables), ctypes.c_int32, ctypes.c_int32, _P,
+                            ctypes.c_size_t, _P]
+_lib.dl_prefill_backward.argtypes = [ctypes.POINTER(dl_desc), _P, ctypes.POINTER(dl_token), _P,
+                                     _P, ctypes.POINTER(dl_grads), ctypes.POINTER(dl_tables),
+                                     ctypes.c_int32, ctypes.c_int32, _P, ctypes.c_size_t, _P]
 for _f in ("dl_eager_step", "dl_append_step", "dl_merge", "dl_readout", "dl_append_step_tiled",
-           "dl_tiled_workspace_bytes", "dl_abi_version", "dl_append_step_tiled_noalloc"):
+           "dl_tiled_workspace_bytes", "dl_abi_version", "dl_append_step_tiled_noalloc",
+           "dl_chunk_tables", "dl_prefill_workspace_bytes", "dl_prefill",
+           "dl_prefill_backward"):
     getattr(_lib, _f).restype = ctypes.c_int
 _lib.dl_status_str.argtypes = [ctypes.c_int]
 _lib.dl_status_str.restype = ctypes.c_char_p
@@ -334,3 +362,101 @@ def dl_append_step_tiled_noalloc(desc, state, tok, o, slots=None, value_tiles=4,
                                              ctypes.byref(tok.struct), _ptr(o), sp, n,
                                              int(value_tiles), _stream(stream)),
            "dl_append_step_tiled_noalloc")
+
+
+# ----------------------------------------------------------------- whole sequences
+class ChunkTables:
+    """Device buffers of the chunk tables and slot maps of ``n`` sequences whose token rows
+    are packed into buffers of ``tokens`` rows (dl_tables).  ``num_slots`` bounds the slot
+    ids (default n); ``err`` is the device error word (1 = bad slot id, 4 = bad length)."""
+
+    def __init__(self, n, tokens, num_slots=None, device="cuda"):
+        i32 = dict(dtype=torch.int32, device=device)
+        self.n, self.tokens = int(n), int(tokens)
+        self.num_slots = self.n if num_slots is None else int(num_slots)
+        self.cu_tokens = torch.zeros((self.n + 1,), **i32)
+        self.cu_chunks = torch.zeros((self.n + 1,), **i32)
+        self.chunks = torch.zeros((self.tokens // DL_CHUNK + self.n, 4), **i32)
+        self.row_slot = torch.zeros((self.tokens,), **i32)
+        self.seq_slot = torch.zeros((self.n,), **i32)
+        self.err = torch.zeros((1,), **i32)
+        self.struct = dl_tables(_ptr(self.cu_tokens), _ptr(self.cu_chunks), _ptr(self.chunks),
+                                _ptr(self.row_slot), _ptr(self.seq_slot))
+
+
+class Grads:
+    """Device buffers for the gradients of one dl_prefill call (dl_grads), shaped as the
+    token's tensors and the state buffer ``S`` (None: no gradient of the initial states)."""
+
+    def __init__(self, desc, tok, S=None):
+        q, k, v, lam, beta, u = tok.tensors
+        like = lambda t: None if t is None else torch.zeros_like(t)  # noqa: E731
+        self.dq, self.dk, self.dv = like(q), like(k), like(v)
+        self.dlam, self.dbeta, self.du = like(lam), like(beta), like(u)
+        if S is not None:
+            _need(S, "S", state_torch_dtype(desc),
+                  (desc.num_slots, desc.heads, desc.dk, desc.dv))
+        self.dS = like(S)
+        self.struct = dl_grads(_ptr(self.dq), _ptr(self.dk), _ptr(self.dv), _ptr(self.dbeta),
+                               _ptr(self.dlam), _ptr(self.du), _ptr(self.dS))
+
+
+def dl_chunk_tables(lens, tables, slots=None, stream=None):
+    """Build ``tables`` from the sequences' lengths, lens [n] int32 on the device (slots [n]
+    int32, or None: sequence i has slot i)."""
+    _need(lens, "lens", torch.int32, (tables.n,))
+    if slots is not None:
+        _need(slots, "slots", torch.int32, (tables.n,))
+    _check(_lib.dl_chunk_tables(_ptr(lens), _ptr(slots), tables.n, tables.tokens,
+                                tables.num_slots, ctypes.byref(tables.struct),
+                                _ptr(tables.err), _stream(stream)), "dl_chunk_tables")
+
+
+def dl_prefill_workspace_bytes(desc, n, tokens, backward=False):
+    """Bytes of workspace dl_prefill needs (with ``backward``: it and dl_prefill_backward)."""
+    out = ctypes.c_size_t(0)
+    _check(_lib.dl_prefill_workspace_bytes(ctypes.byref(desc), int(n), int(tokens),
+                                           int(bool(backward)), ctypes.byref(out)),
+           "dl_prefill_workspace_bytes")
+    return out.value
+
+
+def prefill_workspace(desc, n, tokens, backward=False, device="cuda"):
+    """A device buffer of the size dl_prefill_workspace_bytes names."""
+    return torch.empty((dl_prefill_workspace_bytes(desc, n, tokens, backward),),
+                       dtype=torch.uint8, device=device)
+
+
+def _sequences(desc, tok, tables, workspace, S_in):
+    if tok.n != tables.tokens:
+        raise ValueError(f"the token holds {tok.n} rows but the tables are for {tables.tokens}")
+    if S_in is not None:
+        _need(S_in, "S_in", state_torch_dtype(desc),
+              (desc.num_slots, desc.heads, desc.dk, desc.dv))
+    return (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def dl_prefill(desc, S_in, S_out, tok, o, tables, workspace, stream=None):
+    """The recurrence over the whole sequences of ``tables``: from S_in[slot] (None: zero) to
+    S_out[slot] (may be S_in), o [N,H,dv] in the input dtype."""
+    wp, wn = _sequences(desc, tok, tables, workspace, S_in)
+    _need(S_out, "S_out", state_torch_dtype(desc),
+          (desc.num_slots, desc.heads, desc.dk, desc.dv))
+    _need(o, "o", tok.tensors[2].dtype, (tok.n, desc.heads, desc.dv))
+    _check(_lib.dl_prefill(ctypes.byref(desc), _ptr(S_in), _ptr(S_out), ctypes.byref(tok.struct),
+                           _ptr(o), ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,
+                           _stream(stream)), "dl_prefill")
+
+
+def dl_prefill_backward(desc, S_in, tok, d_o, dS_out, grads, tables, workspace, stream=None):
+    """Gradients of dl_prefill into ``grads`` (``Grads``) from d_o [N,H,dv] and dS_out
+    [B,H,dk,dv] (None: zero).  The forward call must have left S_in as it was."""
+    wp, wn = _sequences(desc, tok, tables, workspace, S_in)
+    _need(d_o, "d_o", tok.tensors[2].dtype, (tok.n, desc.heads, desc.dv))
+    if dS_out is not None:
+        _need(dS_out, "dS_out", state_torch_dtype(desc),
+              (desc.num_slots, desc.heads, desc.dk, desc.dv))
+    _check(_lib.dl_prefill_backward(ctypes.byref(desc), _ptr(S_in), ctypes.byref(tok.struct),
+                                    _ptr(d_o), _ptr(dS_out), ctypes.byref(grads.struct),
+                                    ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,
+                                    _stream(stream)), "dl_prefill_backward")
