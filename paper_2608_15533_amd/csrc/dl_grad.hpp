@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
   const int tid = threadIdx.x, nt = 256, lane = tid & 63, wave = tid >> 6;
   const int c16 = lane & 15, g = lane >> 4;
   const int h = blockIdx.x % p.H, c = blockIdx.x / p.H;
-  const WsLayout w{DK, p.dv, true};
+  const WsLayout w{DK, p.dv, p.raw, true};
   unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
   float* du = reinterpret_cast<float*>(blk + w.du());
   const ChunkRow row = chunk_row(p, c);
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(1024) void bonus_grad_kernel(SeqParams p) {
   constexpr int PARTS = 1024 / DK;
   __shared__ float sum[PARTS][DK];
   const int h = blockIdx.x, r = threadIdx.x % DK, part = threadIdx.x / DK;
-  const WsLayout w{DK, p.dv, true};
+  const WsLayout w{DK, p.dv, p.raw, true};
   const int last = min(p.cu_chunks[p.n], p.max_chunks);
   float s = 0.f;
   for (int c = part; c < last; c += PARTS)

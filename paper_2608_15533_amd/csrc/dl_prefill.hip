@@ -15,21 +15,32 @@ hipError_t start(K* kernel, int64_t grid, int block, const SeqParams& p, hipStre
                          args, 0, s);
 }
 
-template <int DC, int DK, typename TIN>
-hipError_t launch_prep(const SeqParams& p, hipStream_t s) {
-  return start(&prep_kernel<DC, DK, TIN>, int64_t(p.max_chunks) * p.H, 256, p, s);
+template <int DK, typename TIN>
+hipError_t launch_prep(int op, const SeqParams& p, hipStream_t s) {
+  const int64_t grid = int64_t(p.max_chunks) * p.H;
+  if (p.raw) return start(&raw_prep_kernel<DK>, grid, 64, p, s);
+  if (op == DL_OP_RWKV6) return start(&prep_kernel<DC_BONUS, DK, TIN>, grid, 256, p, s);
+  if (op == DL_OP_KDA || op == DL_OP_GLA) return start(&prep_kernel<DC_KEY, DK, TIN>, grid, 256, p, s);
+  return start(&prep_kernel<DC_SCALAR, DK, TIN>, grid, 256, p, s);
+}
+
+template <int DK, bool RAW, bool DELTA, typename TIN>
+hipError_t launch_scan(const SeqParams& p, hipStream_t s) {
+  const int64_t heads = int64_t(p.n) * p.H;
+  if (wide_walk(heads, p.dv)) {
+    if (p.dv == 128) return start(&forward_kernel<DK, 2, 4, RAW, DELTA, TIN>, heads, 256, p, s);
+    return start(&forward_kernel<DK, 2, 2, RAW, DELTA, TIN>, heads, 128, p, s);
+  }
+  return start(&forward_kernel<DK, 1, 2, RAW, DELTA, TIN>, heads * (p.dv / 32), 128, p, s);
 }
 
 template <int DK, typename TIN>
 hipError_t launch_forward_shape(int op, const SeqParams& p, hipStream_t s) {
-  hipError_t e;
-  if (op == DL_OP_RWKV6) e = launch_prep<DC_BONUS, DK, TIN>(p, s);
-  else if (op == DL_OP_KDA || op == DL_OP_GLA) e = launch_prep<DC_KEY, DK, TIN>(p, s);
-  else e = launch_prep<DC_SCALAR, DK, TIN>(p, s);
+  const hipError_t e = launch_prep<DK, TIN>(op, p, s);
   if (e != hipSuccess) return e;
-  const int64_t grid = int64_t(p.n) * p.H * (p.dv / 16);
-  return p.delta ? start(&forward_kernel<DK, 1, true, TIN>, grid, 64, p, s)
-                 : start(&forward_kernel<DK, 1, false, TIN>, grid, 64, p, s);
+  if constexpr (sizeof(TIN) == 2)
+    if (p.raw) return p.delta ? launch_scan<DK, true, true, TIN>(p, s) : launch_scan<DK, true, false, TIN>(p, s);
+  return p.delta ? launch_scan<DK, false, true, TIN>(p, s) : launch_scan<DK, false, false, TIN>(p, s);
 }
 
 }  // namespace
@@ -51,6 +62,12 @@ int check_counts(const dl_desc* d, int32_t n, int32_t tokens) {
   if (chunks * d->heads > int64_t(0x7fffffff)) return DL_E_SHAPE;
   if (int64_t(n) * d->heads * (d->dv / 16) > int64_t(0x7fffffff)) return DL_E_SHAPE;
   return DL_OK;
+}
+
+// bf16 keys and queries with one log-decay per head or none are operands as they are.
+bool raw_planes(const dl_desc* d) {
+  return d->in_dtype == DL_BF16 &&
+         (d->op == DL_OP_GDN || d->op == DL_OP_RETNET || d->op == DL_OP_LINATTN);
 }
 
 // The descriptor's own checks are those of a call that drives no rows.
@@ -79,6 +96,7 @@ SeqParams params(const dl_desc* d, const void* S_in, const dl_token* tok, const 
   p.dv = d->dv;
   p.max_chunks = tokens / DL_CHUNK + n;
   p.state_bf16 = d->state_dtype == DL_BF16;
+  p.raw = raw_planes(d);
   return p;
 }
 
@@ -115,7 +133,7 @@ int dl_prefill_workspace_bytes(const dl_desc* desc, int32_t n, int32_t tokens, i
   DL_TRY(dl::check_desc_only(desc));
   DL_TRY(dl::check_counts(desc, n, tokens));
   if (!bytes) return DL_E_NULL;
-  const dl::WsLayout w{desc->dk, desc->dv, backward != 0};
+  const dl::WsLayout w{desc->dk, desc->dv, dl::raw_planes(desc), backward != 0};
   *bytes = size_t(w.block()) * size_t(tokens / DL_CHUNK + n) * size_t(desc->heads);
   return DL_OK;
 }

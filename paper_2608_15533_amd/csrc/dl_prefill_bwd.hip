@@ -20,11 +20,22 @@ hipError_t launch_grad(const SeqParams& p, hipStream_t s) {
   return e;
 }
 
+template <int DK, bool RAW, bool DELTA, typename TIN>
+hipError_t launch_scan(const SeqParams& p, hipStream_t s) {
+  const int64_t heads = int64_t(p.n) * p.H;
+  if (wide_walk(heads, p.dv)) {
+    if (p.dv == 128) return start(&backward_kernel<DK, 2, 4, RAW, DELTA, TIN>, heads, 256, p, s);
+    return start(&backward_kernel<DK, 2, 2, RAW, DELTA, TIN>, heads, 128, p, s);
+  }
+  return start(&backward_kernel<DK, 1, 2, RAW, DELTA, TIN>, heads * (p.dv / 32), 128, p, s);
+}
+
 template <int DK, typename TIN>
 hipError_t launch_backward_shape(int op, const SeqParams& p, hipStream_t s) {
-  const int64_t grid = int64_t(p.n) * p.H * (p.dv / 16);
-  const hipError_t e = p.delta ? start(&backward_kernel<DK, 1, true, TIN>, grid, 64, p, s)
-                               : start(&backward_kernel<DK, 1, false, TIN>, grid, 64, p, s);
+  hipError_t e = hipErrorInvalidValue;
+  if constexpr (sizeof(TIN) == 2)
+    if (p.raw) e = p.delta ? launch_scan<DK, true, true, TIN>(p, s) : launch_scan<DK, true, false, TIN>(p, s);
+  if (!p.raw) e = p.delta ? launch_scan<DK, false, true, TIN>(p, s) : launch_scan<DK, false, false, TIN>(p, s);
   if (e != hipSuccess) return e;
   if (op == DL_OP_RWKV6) return launch_grad<DC_BONUS, DK, TIN>(p, s);
   if (op == DL_OP_KDA || op == DL_OP_GLA) return launch_grad<DC_KEY, DK, TIN>(p, s);

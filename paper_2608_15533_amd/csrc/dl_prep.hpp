@@ -179,10 +179,39 @@ __device__ __forceinline__ float prep_lq(const PrepShared<DK>& sh, int t, int r)
   else return sh.lq[t][r];
 }
 
-__device__ __forceinline__ void put(unsigned char* base, int plane, int unit, const float* x) {
+__device__ __forceinline__ void put(unsigned char* base, int half, int unit, const float* x) {
   const Split s = split8(x);
   *reinterpret_cast<bf16x8*>(base + 16 * unit) = s.hi;
-  *reinterpret_cast<bf16x8*>(base + plane + 16 * unit) = s.lo;
+  *reinterpret_cast<bf16x8*>(base + half + 16 * unit) = s.lo;
+}
+
+// The squares from LDS matrices, by NTH threads.
+template <int NTH, int LD>
+__device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& w, const SeqParams& p,
+                                            const float (*P)[LD], const float (*Nm)[LD],
+                                            const float (*Mm)[LD], int tid) {
+  for (int x = tid; x < CT * CT / 8; x += NTH) {
+    const int lane = x & 63, i = 16 * (x >> 6) + (lane & 15);
+    float a[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a[e] = P[i][state_term(lane, e)];
+    put(blk + w.p(), WsLayout::SQ, x, a);
+    if (p.delta) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) a[e] = Nm[i][state_term(lane, e)];
+      put(blk + w.n(), WsLayout::SQ, x, a);
+    }
+    if (p.bwd) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) a[e] = P[state_term(lane, e)][i];
+      put(blk + w.pt(), WsLayout::SQ, x, a);
+      if (p.delta) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = Mm[state_term(lane, e)][i];
+        put(blk + w.mt(), WsLayout::SQ, x, a);
+      }
+    }
+  }
 }
 
 template <int DC, int DK, typename TIN>
@@ -192,7 +221,7 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
   const int h = blockIdx.x % p.H, c = blockIdx.x / p.H;
   const ChunkRow row = chunk_row(p, c);
   if (row.count == 0) return;
-  const WsLayout w{DK, p.dv, p.bwd};
+  const WsLayout w{DK, p.dv, false, p.bwd};
   unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
 
   load_chunk<DC, DK, TIN>(sh, p, row, h, tid, nt);
@@ -206,61 +235,113 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
   for (int r = tid; r < DK; r += nt) dec[r] = __expf(prep_l<DC>(sh, CT - 1, r));
   if (tid < CT) beta[tid] = sh.beta[tid];
 
-  // token x key and key x token planes
-  constexpr int UNITS = CT * DK / 8;
-  for (int x = tid; x < UNITS; x += nt) {
-    const int lane = x & 63, c16 = lane & 15, f = x >> 6;
+  constexpr int NP = DK / 8;
+  for (int x = tid; x < CT * NP; x += nt) {
+    const int t = x / NP, k0 = 8 * (x % NP), at = piece_at<NP>(t, x % NP);
     float a[8], b[8], d[8];
-    {                                       // rows: f = tile * (DK / 32) + step
-      const int t = 16 * (f / (DK / 32)) + c16, s = f % (DK / 32);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int r = 32 * s + state_term(lane, e);
-        const float l = prep_l<DC>(sh, t, r);
-        a[e] = sh.k[t][r] * __expf(l);
-        b[e] = sh.q[t][r] * __expf(prep_lq<DC>(sh, t, r));
-        d[e] = sh.k[t][r] * __expf(prep_l<DC>(sh, CT - 1, r) - l);
-      }
-      put(blk + w.kh(), w.plane(), x, a);
-      put(blk + w.qh(), w.plane(), x, b);
-      if (p.bwd) put(blk + w.kb(), w.plane(), x, d);
-    }
-    {                                       // cols: f = key tile
-      const int r = 16 * f + c16;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int t = state_term(lane, e);
-        const float l = prep_l<DC>(sh, t, r);
-        a[e] = sh.k[t][r] * __expf(prep_l<DC>(sh, CT - 1, r) - l);
-        b[e] = sh.q[t][r] * __expf(prep_lq<DC>(sh, t, r));
-        d[e] = sh.k[t][r] * __expf(l);
-      }
-      put(blk + w.kbt(), w.plane(), x, a);
-      if (p.bwd) {
-        put(blk + w.qht(), w.plane(), x, b);
-        put(blk + w.kht(), w.plane(), x, d);
-      }
-    }
-  }
-  // token x token planes
-  for (int x = tid; x < CT * CT / 8; x += nt) {
-    const int lane = x & 63, i = 16 * (x >> 6) + (lane & 15);
-    float a[8], b[8], d[8], f[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int j = state_term(lane, e);
-      a[e] = sh.P[i][j];
-      b[e] = sh.P[j][i];
-      d[e] = p.delta ? sh.Nm[i][j] : 0.f;
-      f[e] = p.delta ? sh.Mm[j][i] : 0.f;
+      const int r = k0 + e;
+      const float l = prep_l<DC>(sh, t, r);
+      a[e] = sh.k[t][r] * __expf(l);
+      b[e] = sh.q[t][r] * __expf(prep_lq<DC>(sh, t, r));
+      d[e] = sh.k[t][r] * __expf(prep_l<DC>(sh, CT - 1, r) - l);
     }
-    put(blk + w.p(), w.sq(), x, a);
-    put(blk + w.n(), w.sq(), x, d);
-    if (p.bwd) {
-      put(blk + w.pt(), w.sq(), x, b);
-      put(blk + w.mt(), w.sq(), x, f);
+    if (p.delta) put(blk + w.kh(), w.plane(), at, a);
+    put(blk + w.qh(), w.plane(), at, b);
+    put(blk + w.kb(), w.plane(), at, d);
+  }
+  put_squares<256>(blk, w, p, sh.P, sh.Nm, sh.Mm, tid);
+}
+
+// The same for bf16 keys and queries with one log-decay per head or none, one wave per
+// (chunk, head): the operands of k k^T and q k^T come straight from memory, exact in bf16, and
+// only the squares and the row factors are written.
+template <int DK>
+__global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
+  constexpr int NKS = DK / 32;
+  __shared__ float G[CT][CT + 1], P[CT][CT + 1], Mm[CT][CT + 1];
+  const int lane = threadIdx.x, c16 = lane & 15, g = lane >> 4;
+  const int h = blockIdx.x % p.H, c = blockIdx.x / p.H;
+  const ChunkRow row = chunk_row(p, c);
+  if (row.count == 0) return;
+  const WsLayout w{DK, p.dv, true, p.bwd};
+  unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
+
+  bf16x8 kf[2][NKS], qf[2][NKS];
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt) {
+    const int t = 16 * tt + c16;
+    const int64_t at = (int64_t(row.first + min(t, row.count - 1)) * p.H + h) * DK + 8 * g;
+#pragma unroll
+    for (int s = 0; s < NKS; ++s) {
+      kf[tt][s] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.k) + at + 32 * s);
+      qf[tt][s] = *reinterpret_cast<const bf16x8*>(static_cast<const uint16_t*>(p.q) + at + 32 * s);
+    }
+    if (t >= row.count) {
+      const u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < NKS; ++s) kf[tt][s] = qf[tt][s] = __builtin_bit_cast(bf16x8, zero);
     }
   }
+  const bool live = lane < row.count;
+  const int64_t tok = int64_t(row.first + (live ? lane : 0)) * p.H + h;
+  float l = live && p.lam ? fmaxf(p.lam[tok], LOG_FLOOR) : 0.f;
+  const float beta = live && p.delta ? p.beta[tok] : 0.f;
+#pragma unroll
+  for (int d = 1; d < CT; d *= 2) {
+    const float y = __shfl_up(l, d);
+    if (lane >= d) l += y;
+  }
+  const float lT = __shfl(l, CT - 1);
+  if (lane < CT) {
+    float* fac = reinterpret_cast<float*>(blk + w.beta());
+    fac[lane] = beta;
+    fac[CT + lane] = __expf(l);
+    fac[2 * CT + lane] = __expf(lT - l);
+  }
+#pragma unroll
+  for (int b = 0; b < 3; ++b) {                 // (0,0), (1,1), (1,0)
+    const int bi = b == 0 ? 0 : 1, bj = b == 1 ? 1 : 0;
+    f32x4 ag = {0.f, 0.f, 0.f, 0.f}, ap = ag;
+#pragma unroll
+    for (int s = 0; s < NKS; ++s) {
+      if (p.delta) ag = mma(kf[bi][s], kf[bj][s], ag);
+      ap = mma(qf[bi][s], kf[bj][s], ap);
+    }
+    const int j = 16 * bj + c16;
+    const float lj = __shfl(l, j);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = 16 * bi + 4 * g + r;
+      const float x = __expf(fminf(__shfl(l, i) - lj, 0.f));
+      P[i][j] = i >= j ? ap[r] * x : 0.f;
+      G[i][j] = i > j ? ag[r] * x : 0.f;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) G[4 * g + r][16 + c16] = P[4 * g + r][16 + c16] = 0.f;
+  __syncthreads();
+  if (p.delta) {
+    // as solve(): row i of G is used at step i alone, and N's row i replaces it
+    const int j = lane & 31;
+    const bool second = lane >= 32;
+    float y[CT];
+#pragma unroll
+    for (int i = 0; i < CT; ++i) {
+      float s = 0.f;
+#pragma unroll
+      for (int m = 0; m < i; ++m) s += G[i][m] * y[m];
+      const float b = __shfl(beta, i), d = i == j ? 1.f : 0.f;
+      const float x = d - (second ? b * s : s);
+      y[i] = second ? x : b * x;
+      __syncthreads();
+      if (second) Mm[i][j] = x;
+      else G[i][j] = x;
+    }
+    __syncthreads();
+  }
+  put_squares<64>(blk, w, p, P, G, Mm, lane);
 }
 
 }  // namespace dl

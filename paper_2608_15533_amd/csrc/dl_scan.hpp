@@ -90,39 +90,81 @@ __device__ __forceinline__ void store_state(void* S, bool bf16, int64_t i, float
   else static_cast<float*>(S)[i] = x;
 }
 
+// ------------------------------------------------------------------ operands in LDS
+// A token x key plane: 32 rows of 16-byte pieces (8 bf16), piece x of row r at
+// piece_at(r, x).  The exchange of pieces within a row spreads the 16 rows that an operand
+// read touches over all banks.  NP: pieces in a row.
+template <int NP>
+__host__ __device__ constexpr int piece_swap(int r) {
+  return NP >= 16 ? (r & 15) : NP == 8 ? ((r >> 1) & 7) : NP == 4 ? ((r >> 1) & 2) : 0;
+}
+template <int NP>
+__host__ __device__ constexpr int piece_at(int r, int x) {
+  return r * NP + (x ^ piece_swap<NP>(r));
+}
+
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+__device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) {
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// Four rows of one column: of each 16 lanes, lane i gives the address of 8 bytes of row i/4
+// (columns 4(i%4)..) and receives column i of the four rows.
+__device__ __forceinline__ bf16x4 read_column(const unsigned char* lds) {
+  typedef __attribute__((address_space(3))) s16x4 lds_t;
+  return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)lds));
+}
+
+// Tokens 16 tt + l%16, terms: keys 32 s + (state order).
+template <int NP>
+__device__ __forceinline__ bf16x8 rows_operand(const unsigned char* plane, int tt, int s, int lane) {
+  const int r = 16 * tt + (lane & 15), g = lane >> 4;
+  const unsigned char* at = plane + 8 * (g & 1);
+  const bf16x4 a = *reinterpret_cast<const bf16x4*>(at + 16 * piece_at<NP>(r, 4 * s + (g >> 1)));
+  const bf16x4 b = *reinterpret_cast<const bf16x4*>(at + 16 * piece_at<NP>(r, 4 * s + 2 + (g >> 1)));
+  return join(a, b);
+}
+// Keys 16 f + l%16, terms: the chunk's tokens (state order).
+template <int NP>
+__device__ __forceinline__ bf16x8 cols_operand(const unsigned char* plane, int f, int lane) {
+  const int i = lane & 15, r = 4 * (lane >> 4) + (i >> 2);
+  const unsigned char* at = plane + 8 * (i & 1);
+  const bf16x4 a = read_column(at + 16 * piece_at<NP>(r, 2 * f + ((i >> 1) & 1)));
+  const bf16x4 b = read_column(at + 16 * piece_at<NP>(r + 16, 2 * f + ((i >> 1) & 1)));
+  return join(a, b);
+}
+
 // ------------------------------------------------------------------ workspace
-// One block per (chunk, head), chunk-major.  Operand planes are bf16 in fragment order: the
-// eight terms a lane feeds one MFMA are 16 consecutive bytes, a wave's load 1 KiB.
-//   rows   token x key   [token tile 2][key step dk/32][lane 64][8]   (state order of keys)
-//   cols   key x token   [key tile dk/16][lane 64][8]                 (state order of tokens)
-//   square token x token [token tile 2][lane 64][8]                   (state order of tokens)
+// One block per (chunk, head), chunk-major:
+//   planes  Kh, Qh, Kb: token x key, hi then lo, as they lie in LDS.  Not there ("raw") for
+//           bf16 keys and queries with one log-decay per head or none: the keys and queries
+//           themselves are the planes, exact in bf16, and e^{l_i} (f) and e^{l_T-l_i} (g)
+//           scale token rows of fp32 products instead.
+//   squares N, P and (backward) P^T, M^T: token x token, hi then lo, in fragment order: the
+//           eight terms (state order) a lane feeds one MFMA are 16 consecutive bytes.
 struct WsLayout {
   int dk, dv;
-  bool bwd;
-  // offsets in bytes into a block
-  __host__ __device__ int plane() const { return CT * dk * 2; }
-  __host__ __device__ int sq() const { return CT * CT * 2; }
-  __host__ __device__ int kh() const { return 0; }                       // rows, hi then lo
-  __host__ __device__ int qh() const { return 2 * plane(); }             // rows
-  __host__ __device__ int kbt() const { return 4 * plane(); }            // cols
-  __host__ __device__ int n() const { return 6 * plane(); }              // square
-  __host__ __device__ int p() const { return n() + 2 * sq(); }           // square
-  __host__ __device__ int dec() const { return p() + 2 * sq(); }         // fp32 [dk] e^{l_T}
+  bool raw, bwd;
+  static constexpr int SQ = CT * CT * 2;                                 // one square, one half
+  __host__ __device__ int plane() const { return CT * dk * 2; }          // one plane, one half
+  __host__ __device__ int p() const { return 0; }
+  __host__ __device__ int n() const { return 2 * SQ; }
+  __host__ __device__ int kh() const { return 4 * SQ; }
+  __host__ __device__ int qh() const { return kh() + (raw ? 0 : 2 * plane()); }
+  __host__ __device__ int kb() const { return qh() + (raw ? 0 : 2 * plane()); }
+  __host__ __device__ int dec() const { return kb() + (raw ? 0 : 2 * plane()); }  // fp32 [dk] e^{l_T} (not raw)
   __host__ __device__ int beta() const { return dec() + dk * 4; }        // fp32 [CT]
-  __host__ __device__ int fwd_end() const { return beta() + CT * 4; }
-  // backward only
-  __host__ __device__ int kb() const { return fwd_end(); }               // rows
-  __host__ __device__ int qht() const { return kb() + 2 * plane(); }     // cols
-  __host__ __device__ int kht() const { return qht() + 2 * plane(); }    // cols
-  __host__ __device__ int mt() const { return kht() + 2 * plane(); }     // square
-  __host__ __device__ int pt() const { return mt() + 2 * sq(); }         // square
-  __host__ __device__ int s0() const { return pt() + 2 * sq(); }         // fp32 [dk][dv]
-  __host__ __device__ int ds() const { return s0() + dk * dv * 4; }      // fp32 [dk][dv]
+  __host__ __device__ int f() const { return beta() + CT * 4; }          // fp32 [CT] (raw)
+  __host__ __device__ int g() const { return f() + CT * 4; }             // fp32 [CT] (raw)
+  __host__ __device__ int pt() const { return g() + CT * 4; }
+  __host__ __device__ int mt() const { return pt() + 2 * SQ; }
+  __host__ __device__ int s0() const { return mt() + 2 * SQ; }           // fp32 [dk][dv] S
+  __host__ __device__ int ds() const { return s0() + dk * dv * 4; }      // fp32 [dk][dv] D
   __host__ __device__ int e() const { return ds() + dk * dv * 4; }       // fp32 [CT][dv]
   __host__ __device__ int z() const { return e() + CT * dv * 4; }        // fp32 [CT][dv]
   __host__ __device__ int du() const { return z() + CT * dv * 4; }       // fp32 [dk]
-  __host__ __device__ int bwd_end() const { return du() + dk * 4; }
-  __host__ __device__ int64_t block() const { return bwd ? bwd_end() : fwd_end(); }
+  __host__ __device__ int64_t block() const { return bwd ? du() + dk * 4 : pt(); }
 };
 
 // Everything the sequence kernels need, passed by value (all pointers are device pointers).
@@ -143,8 +185,11 @@ struct SeqParams {
   const int32_t *cu_tokens, *cu_chunks, *chunks, *seq_slot;
   unsigned char* ws;
   int32_t n, N, B, H, dv, max_chunks;
-  bool delta, state_bf16, bwd;
+  bool delta, state_bf16, bwd, raw;
 };
+
+// Whether a workgroup walks whole heads with 32 columns a wave, or 32 columns with 16 a wave.
+inline bool wide_walk(int64_t heads, int dv) { return heads * (dv / 32) >= 1024; }
 
 struct ChunkRow {
   int seq, first, count, slot;

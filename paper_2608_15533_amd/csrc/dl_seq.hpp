@@ -1,19 +1,22 @@
 // The serial passes over a sequence's chunks: forward (states and outputs) and backward
-// (state gradients and value gradients).  One wave owns VT = 16 NT value columns of one
-// (sequence, head) and keeps its dk x VT piece of the state (or of its gradient) in registers
-// as MFMA results; columns do not meet, so waves never wait for each other.
+// (state gradients and value gradients).
 //
-// Column j of tile t of a wave is v0 + NT * (j) + t: a lane's NT values are adjacent in memory.
+// A workgroup of NW waves walks the chunks of one (sequence, head); each wave owns NT tiles of
+// 16 value columns and keeps its dk x 16 NT piece of the state (or of the state's gradient) in
+// registers as MFMA results.  Columns never meet, so the waves share nothing but the chunk's
+// operands, which go through LDS: each chunk's are loaded into registers while the chunk before
+// is computed, and written to LDS between two barriers.  Inside a chunk every product's result
+// is the next product's operand as it stands (state order), without a trip through LDS.
 #pragma once
 
 #include "dl_scan.hpp"
 
 namespace dl {
 
-template <int NT, typename T>
-__device__ __forceinline__ void load_cols(const T* p, float* x) {
-#pragma unroll
-  for (int t = 0; t < NT; ++t) x[t] = widen(p[t]);
+__device__ __forceinline__ Split square_at(const unsigned char* lds, int tt, int lane) {
+  const unsigned char* at = lds + 16 * (tt * 64 + lane);
+  return Split{*reinterpret_cast<const bf16x8*>(at),
+               *reinterpret_cast<const bf16x8*>(at + WsLayout::SQ)};
 }
 
 // Result tiles [2][NT] (tokens 16 tt + 4 g + r) as operands over the chunk's tokens.
@@ -32,67 +35,232 @@ __device__ __forceinline__ Split state_operand(const f32x4 (&S)[NKT][NT], int s,
   return split8(a);
 }
 
-__device__ __forceinline__ Split plane_at(const unsigned char* base, int plane, int unit) {
-  return load_split(reinterpret_cast<const uint16_t*>(base + 16 * unit),
-                    reinterpret_cast<const uint16_t*>(base + plane + 16 * unit));
+// acc += a b with a plane operand that has a second half (LO) or is exact in bf16.
+template <bool LO>
+__device__ __forceinline__ f32x4 mma_plane(const Split& a, const Split& b, f32x4 acc) {
+  if constexpr (LO) acc = mma(a.lo, b.hi, acc);
+  acc = mma(a.hi, b.lo, acc);
+  return mma(a.hi, b.hi, acc);
 }
 
-template <int DK, int NT, bool DELTA, typename TIN>
-__global__ __launch_bounds__(64) void forward_kernel(SeqParams p) {
-  constexpr int NKT = DK / 16, NKS = DK / 32;
-  const int lane = threadIdx.x, c16 = lane & 15, g = lane >> 4;
-  const int nvt = p.dv / (16 * NT);
-  const int b = blockIdx.x, vt = b % nvt, h = (b / nvt) % p.H, seq = b / nvt / p.H;
-  const int slot = p.seq_slot[seq];
-  if (slot < 0 || slot >= p.B) return;
-  const int v = 16 * NT * vt + NT * c16;
-  const WsLayout w{DK, p.dv, p.bwd};
-  const int64_t state_at = (int64_t(slot) * p.H + h) * DK * p.dv + v;
+// One chunk's operands on their way from memory to LDS.
+template <int DK, int NT, int NW, bool RAW, bool DELTA, bool BWD, typename TIN>
+struct Stage {
+  static constexpr int T = 64 * NW, VC = 16 * NT * NW, NP = DK / 8;
+  static constexpr int HALF = CT * DK * 2;                     // bytes of half a plane
+  static constexpr int SQ2 = 2 * WsLayout::SQ;
+  static constexpr int FAC = 4 * DK + 12 * CT;
+  // LDS offsets.  Forward: P, N, planes, factors; backward: planes, factors, P^T, M^T.
+  static constexpr int A_P = 0;
+  static constexpr int A_N = BWD ? 0 : SQ2;
+  static constexpr int A_KH = A_N + (!BWD && DELTA ? SQ2 : 0);
+  static constexpr int A_QH = A_KH + (!RAW && DELTA ? 2 * HALF : 0);
+  static constexpr int A_KB = A_QH + (RAW ? 0 : 2 * HALF);
+  static constexpr int A_DEC = A_KB + (RAW ? 0 : 2 * HALF);
+  static constexpr int A_BETA = A_DEC + 4 * DK, A_F = A_BETA + 4 * CT, A_G = A_F + 4 * CT;
+  static constexpr int A_PT = A_DEC + FAC;
+  static constexpr int A_MT = A_PT + (BWD ? SQ2 : 0);
+  static constexpr int LINEAR = A_MT + (BWD && DELTA ? SQ2 : 0);
+  static constexpr int A_K = LINEAR, A_Q = A_K + (RAW ? HALF : 0);
+  static constexpr int A_V = A_Q + (RAW ? HALF : 0);
+  static constexpr int VNP = VC * int(sizeof(TIN)) / 16;       // pieces of a value row
+  static constexpr int VROW = sizeof(TIN) == 2 ? VC * 2 : VC * 4 + 16;
+  static constexpr int BYTES = A_V + CT * VROW;
 
-  f32x4 S[NKT][NT];
+  static constexpr int NLIN = (LINEAR / 16 + T - 1) / T;
+  static constexpr int NKQ = RAW ? CT * NP / T : 0;
+  static constexpr int NV = (CT * VNP + T - 1) / T;
+  u32x4 lin[NLIN], kk[NKQ ? NKQ : 1], qq[NKQ ? NKQ : 1], vv[NV];
+
+  // vals: row 0, this workgroup's first column, of this head's value rows (stride H dv).
+  __device__ __forceinline__ void load(const SeqParams& p, const unsigned char* blk, int first,
+                                       int count, int h, const TIN* vals, int tid) {
+    const WsLayout w{DK, p.dv, RAW, p.bwd};
+    const unsigned char* rest = blk + (DELTA ? (BWD ? w.kh() : w.n()) : RAW ? w.dec() : w.qh());
+    constexpr int HEAD = BWD ? 0 : SQ2;                        // P comes first in the block
+    const u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < NLIN; ++i) {
+      const int x = 16 * (i * T + tid);
+      if (x < LINEAR)
+        lin[i] = *reinterpret_cast<const u32x4*>(x < HEAD ? blk + w.p() + x : rest + (x - HEAD));
+    }
+    if constexpr (RAW) {
+#pragma unroll
+      for (int i = 0; i < NKQ; ++i) {
+        const int x = i * T + tid, r = x / NP, pc = (x % NP) ^ piece_swap<NP>(r);
+        const int64_t at = (int64_t(first + min(r, count - 1)) * p.H + h) * DK + 8 * pc;
+        kk[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.k) + at);
+        qq[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + at);
+        if (r >= count) kk[i] = qq[i] = zero;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int x = i * T + tid, r = x / VNP;
+      if (x < CT * VNP) {
+        const TIN* at = vals + int64_t(first + min(r, count - 1)) * p.H * p.dv;
+        vv[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(at) +
+                                                16 * (x % VNP));
+        if (r >= count) vv[i] = zero;
+      }
+    }
+  }
+  __device__ __forceinline__ void store(unsigned char* lds, int tid) const {
+#pragma unroll
+    for (int i = 0; i < NLIN; ++i) {
+      const int x = 16 * (i * T + tid);
+      if (x < LINEAR) *reinterpret_cast<u32x4*>(lds + x) = lin[i];
+    }
+    if constexpr (RAW) {
+#pragma unroll
+      for (int i = 0; i < NKQ; ++i) {
+        *reinterpret_cast<u32x4*>(lds + A_K + 16 * (i * T + tid)) = kk[i];
+        *reinterpret_cast<u32x4*>(lds + A_Q + 16 * (i * T + tid)) = qq[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int x = i * T + tid, r = x / VNP;
+      if (x < CT * VNP) {
+        if constexpr (sizeof(TIN) == 2)
+          *reinterpret_cast<u32x4*>(lds + A_V + 16 * piece_at<VNP>(r, x % VNP)) = vv[i];
+        else
+          *reinterpret_cast<u32x4*>(lds + A_V + r * VROW + 16 * (x % VNP)) = vv[i];
+      }
+    }
+  }
+  // Value rows as result tiles: tokens 16 tt + 4 g + r, column 16 ct + l%16.
+  static __device__ __forceinline__ f32x4 values(const unsigned char* lds, int tt, int ct, int lane) {
+    f32x4 x;
+    if constexpr (sizeof(TIN) == 2) {
+      const int i = lane & 15, r = 16 * tt + 4 * (lane >> 4) + (i >> 2);
+      const bf16x4 a =
+          read_column(lds + A_V + 8 * (i & 1) + 16 * piece_at<VNP>(r, 2 * ct + ((i >> 1) & 1)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (float)a[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        x[e] = *reinterpret_cast<const float*>(lds + A_V + (16 * tt + 4 * (lane >> 4) + e) * VROW +
+                                               4 * (16 * ct + (lane & 15)));
+    }
+    return x;
+  }
+  static __device__ __forceinline__ f32x4 factor(const unsigned char* lds, int at, int tt, int lane) {
+    return *reinterpret_cast<const f32x4*>(lds + at + 4 * (16 * tt + 4 * (lane >> 4)));
+  }
+  // Operands from the planes; raw ones have no second half.
+  static __device__ __forceinline__ Split rows(const unsigned char* lds, int raw_at, int at, int tt,
+                                               int s, int lane) {
+    Split o;
+    o.hi = rows_operand<NP>(lds + (RAW ? raw_at : at), tt, s, lane);
+    if constexpr (!RAW) o.lo = rows_operand<NP>(lds + at + HALF, tt, s, lane);
+    return o;
+  }
+  static __device__ __forceinline__ Split cols(const unsigned char* lds, int raw_at, int at, int f,
+                                               int lane) {
+    Split o;
+    o.hi = cols_operand<NP>(lds + (RAW ? raw_at : at), f, lane);
+    if constexpr (!RAW) o.lo = cols_operand<NP>(lds + at + HALF, f, lane);
+    return o;
+  }
+  // e^{l_T} for keys 16 f + 4 g + r
+  static __device__ __forceinline__ f32x4 decay(const unsigned char* lds, int f, int lane) {
+    if constexpr (RAW) {
+      const float d = *reinterpret_cast<const float*>(lds + A_F + 4 * (CT - 1));
+      return f32x4{d, d, d, d};
+    } else {
+      return *reinterpret_cast<const f32x4*>(lds + A_DEC + 4 * (16 * f + 4 * (lane >> 4)));
+    }
+  }
+};
+
+// Where a workgroup stands: (sequence, head, first value column).
+struct Walk {
+  int seq, h, slot, v0, c0, c1, first, end;
+};
+template <int VC>
+__device__ __forceinline__ bool start_walk(const SeqParams& p, Walk& k) {
+  const int nvt = p.dv / VC, b = blockIdx.x;
+  k.v0 = VC * (b % nvt);
+  k.h = (b / nvt) % p.H;
+  k.seq = b / nvt / p.H;
+  k.slot = p.seq_slot[k.seq];
+  if (k.slot < 0 || k.slot >= p.B) return false;
+  k.c0 = max(p.cu_chunks[k.seq], 0);
+  k.c1 = min(p.cu_chunks[k.seq + 1], p.max_chunks);
+  k.first = max(p.cu_tokens[k.seq], 0);
+  k.end = min(p.cu_tokens[k.seq + 1], p.N);
+  k.c1 = min(k.c1, k.c0 + (max(k.end - k.first, 0) + CT - 1) / CT);
+  return true;
+}
+
+template <int NKT, int NT>
+__device__ __forceinline__ void read_state(f32x4 (&S)[NKT][NT], const void* base, const SeqParams& p,
+                                           int64_t at, int lane) {
 #pragma unroll
   for (int f = 0; f < NKT; ++f)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int t = 0; t < NT; ++t)
-        S[f][t][r] = p.S_in ? load_state(p.S_in, p.state_bf16,
-                                         state_at + int64_t(16 * f + 4 * g + r) * p.dv + t)
-                            : 0.f;
+        S[f][t][r] = base ? load_state(base, p.state_bf16,
+                                       at + int64_t(16 * f + 4 * (lane >> 4) + r) * p.dv + 16 * t)
+                          : 0.f;
+}
+template <int NKT, int NT>
+__device__ __forceinline__ void write_state(const f32x4 (&S)[NKT][NT], void* base, bool bf16, int dv,
+                                            int64_t at, int lane) {
+#pragma unroll
+  for (int f = 0; f < NKT; ++f)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        store_state(base, bf16, at + int64_t(16 * f + 4 * (lane >> 4) + r) * dv + 16 * t, S[f][t][r]);
+}
 
-  const int c0 = max(p.cu_chunks[seq], 0), c1 = min(p.cu_chunks[seq + 1], p.max_chunks);
-  for (int c = c0; c < c1; ++c) {
-    const ChunkRow row = chunk_row(p, c);
-    if (row.count == 0) continue;
-    unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
-    const TIN* vp = static_cast<const TIN*>(p.v) + (int64_t(row.first) * p.H + h) * p.dv + v;
-    f32x4 U[2][NT], O[2][NT];
-    // V, rows past the chunk's end as 0
+template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
+__global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
+  using St = Stage<DK, NT, NW, RAW, DELTA, false, TIN>;
+  constexpr int NKT = DK / 16, NKS = DK / 32;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[St::BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
+  Walk k;
+  if (!start_walk<St::VC>(p, k)) return;
+  const WsLayout w{DK, p.dv, RAW, p.bwd};
+  const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;        // this lane's first column
+  const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
+  const TIN* vals = static_cast<const TIN*>(p.v) + int64_t(k.h) * p.dv + k.v0;
+  unsigned char* blk = p.ws + (int64_t(k.c0) * p.H + k.h) * w.block();
+
+  St st;
+  if (k.c0 < k.c1) st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
+  f32x4 S[NKT][NT];
+  read_state(S, p.S_in, p, state_at, lane);
+
+  for (int c = k.c0; c < k.c1; ++c) {
+    const int first = k.first, count = min(CT, k.end - first);
+    unsigned char* cur = blk;
+    __syncthreads();
+    st.store(lds, tid);
+    __syncthreads();
+    k.first += CT;
+    blk += int64_t(p.H) * w.block();
+    if (c + 1 < k.c1) st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
+
+    if (p.bwd)
+      write_state(S, cur + w.s0(), false, p.dv, v, lane);
+    f32x4 U[2][NT], O[2][NT], X[2][NT];
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int tok = 16 * tt + 4 * g + r;
-        float x[NT];
-        load_cols<NT>(vp + int64_t(min(tok, row.count - 1)) * p.H * p.dv, x);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) U[tt][t][r] = tok < row.count ? x[t] : 0.f;
+      for (int t = 0; t < NT; ++t) {
+        U[tt][t] = St::values(lds, tt, ct0 + t, lane);
+        O[tt][t] = X[tt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
-    if (p.bwd) {
-      float* s0 = reinterpret_cast<float*>(blk + w.s0()) + v;
-#pragma unroll
-      for (int f = 0; f < NKT; ++f)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int t = 0; t < NT; ++t) s0[(16 * f + 4 * g + r) * p.dv + t] = S[f][t][r];
-    }
     // Kh S and Qh S
-    f32x4 X[2][NT];
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) O[tt][t] = X[tt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < NKS; ++s) {
       Split sb[NT];
@@ -100,15 +268,25 @@ __global__ __launch_bounds__(64) void forward_kernel(SeqParams p) {
       for (int t = 0; t < NT; ++t) sb[t] = state_operand<NKT, NT>(S, s, t);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        const int unit = (tt * NKS + s) * 64 + lane;
         if constexpr (DELTA) {
-          const Split a = plane_at(blk + w.kh(), w.plane(), unit);
+          const Split a = St::rows(lds, St::A_K, St::A_KH, tt, s, lane);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) X[tt][t] = mma3(a, sb[t], X[tt][t]);
+          for (int t = 0; t < NT; ++t) X[tt][t] = mma_plane<!RAW>(a, sb[t], X[tt][t]);
         }
-        const Split a = plane_at(blk + w.qh(), w.plane(), unit);
+        const Split a = St::rows(lds, St::A_Q, St::A_QH, tt, s, lane);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) O[tt][t] = mma3(a, sb[t], O[tt][t]);
+        for (int t = 0; t < NT; ++t) O[tt][t] = mma_plane<!RAW>(a, sb[t], O[tt][t]);
+      }
+    }
+    if constexpr (RAW) {
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const f32x4 f = St::factor(lds, St::A_F, tt, lane);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          O[tt][t] *= f;
+          X[tt][t] *= f;
+        }
       }
     }
     if constexpr (DELTA) {
@@ -119,140 +297,118 @@ __global__ __launch_bounds__(64) void forward_kernel(SeqParams p) {
         for (int tt = 0; tt < 2; ++tt) U[tt][t] -= X[tt][t];
         rb[t] = tokens_operand<NT>(U, t);
       }
-      const float* beta = reinterpret_cast<const float*>(blk + w.beta());
-      float* eo = reinterpret_cast<float*>(blk + w.e()) + v;
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        const Split a = plane_at(blk + w.n(), w.sq(), tt * 64 + lane);
+        const Split a = square_at(lds + St::A_N, tt, lane);
 #pragma unroll
         for (int t = 0; t < NT; ++t) U[tt][t] = mma3(a, rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int tok = 16 * tt + 4 * g + r;
-          const float be = beta[tok];
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            if (p.bwd) eo[tok * p.dv + t] = U[tt][t][r];
-            U[tt][t][r] *= be;
-          }
-        }
       }
-    } else if (p.bwd) {
-      float* eo = reinterpret_cast<float*>(blk + w.e()) + v;
+    }
+    if (p.bwd) {
+      float* eo = reinterpret_cast<float*>(cur + w.e()) + v;
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int t = 0; t < NT; ++t) eo[(16 * tt + 4 * g + r) * p.dv + t] = U[tt][t][r];
+          for (int t = 0; t < NT; ++t) eo[(16 * tt + 4 * g + r) * p.dv + 16 * t] = U[tt][t][r];
     }
-    Split ub[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) ub[t] = tokens_operand<NT>(U, t);
-    // S <- e^{l_T} S + Kb^T U
-    const float* dec = reinterpret_cast<const float*>(blk + w.dec());
-#pragma unroll
-    for (int f = 0; f < NKT; ++f) {
-      const f32x4 d = *reinterpret_cast<const f32x4*>(dec + 16 * f + 4 * g);
-      const Split a = plane_at(blk + w.kbt(), w.plane(), f * 64 + lane);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[f][t][r] *= d[r];
-        S[f][t] = mma3(a, ub[t], S[f][t]);
-      }
-    }
-    if (p.o) {
-      TIN* op = static_cast<TIN*>(p.o) + (int64_t(row.first) * p.H + h) * p.dv + v;
+    if constexpr (DELTA) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        const Split a = plane_at(blk + w.p(), w.sq(), tt * 64 + lane);
+        const f32x4 be = St::factor(lds, St::A_BETA, tt, lane);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) U[tt][t] *= be;
+      }
+    }
+    Split ub[NT], gb[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) ub[t] = tokens_operand<NT>(U, t);
+    if constexpr (RAW) {
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const f32x4 gf = St::factor(lds, St::A_G, tt, lane);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) U[tt][t] *= gf;
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) gb[t] = tokens_operand<NT>(U, t);
+    } else {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) gb[t] = ub[t];
+    }
+    // S <- e^{l_T} S + Kb^T U
+#pragma unroll
+    for (int f = 0; f < NKT; ++f) {
+      const f32x4 d = St::decay(lds, f, lane);
+      const Split a = St::cols(lds, St::A_K, St::A_KB, f, lane);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) S[f][t] = mma_plane<!RAW>(a, gb[t], S[f][t] * d);
+    }
+    if (p.o) {
+      TIN* op = static_cast<TIN*>(p.o) + (int64_t(first) * p.H + k.h) * p.dv + v;
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const Split a = square_at(lds + St::A_P, tt, lane);
 #pragma unroll
         for (int t = 0; t < NT; ++t) O[tt][t] = mma3(a, ub[t], O[tt][t]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int tok = 16 * tt + 4 * g + r;
-          if (tok < row.count)
+          if (tok < count)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) narrow(op + int64_t(tok) * p.H * p.dv + t, O[tt][t][r]);
+            for (int t = 0; t < NT; ++t)
+              narrow(op + int64_t(tok) * p.H * p.dv + 16 * t, O[tt][t][r]);
         }
       }
     }
   }
-  if (p.S_out) {
-#pragma unroll
-    for (int f = 0; f < NKT; ++f)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-          store_state(p.S_out, p.state_bf16, state_at + int64_t(16 * f + 4 * g + r) * p.dv + t,
-                      S[f][t][r]);
-  }
+  if (p.S_out) write_state(S, p.S_out, p.state_bf16, p.dv, state_at, lane);
 }
 
 // Backward over the chunks, last to first, with D the gradient of the state after a chunk:
 //   dU = P^T dO + Kb D      Z = M^T dU,  Y = beta Z   (no delta rule: Y = dU)
 //   dV = Y                  D <- e^{l_T} D + Qh^T dO - Kh^T Y
-template <int DK, int NT, bool DELTA, typename TIN>
-__global__ __launch_bounds__(64) void backward_kernel(SeqParams p) {
+template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
+__global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
+  using St = Stage<DK, NT, NW, RAW, DELTA, true, TIN>;
   constexpr int NKT = DK / 16, NKS = DK / 32;
-  const int lane = threadIdx.x, c16 = lane & 15, g = lane >> 4;
-  const int nvt = p.dv / (16 * NT);
-  const int b = blockIdx.x, vt = b % nvt, h = (b / nvt) % p.H, seq = b / nvt / p.H;
-  const int slot = p.seq_slot[seq];
-  if (slot < 0 || slot >= p.B) return;
-  const int v = 16 * NT * vt + NT * c16;
-  const WsLayout w{DK, p.dv, true};
-  const int64_t state_at = (int64_t(slot) * p.H + h) * DK * p.dv + v;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[St::BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
+  Walk k;
+  if (!start_walk<St::VC>(p, k)) return;
+  const WsLayout w{DK, p.dv, RAW, true};
+  const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;
+  const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
+  const TIN* vals = static_cast<const TIN*>(p.d_o) + int64_t(k.h) * p.dv + k.v0;
+  unsigned char* blk = p.ws + (int64_t(k.c1 - 1) * p.H + k.h) * w.block();
+  k.first += CT * (k.c1 - 1 - k.c0);
 
+  St st;
+  if (k.c0 < k.c1) st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
   f32x4 D[NKT][NT];
-#pragma unroll
-  for (int f = 0; f < NKT; ++f)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        D[f][t][r] = p.dS_out ? load_state(p.dS_out, p.state_bf16,
-                                           state_at + int64_t(16 * f + 4 * g + r) * p.dv + t)
-                              : 0.f;
+  read_state(D, p.dS_out, p, state_at, lane);
 
-  const int c0 = max(p.cu_chunks[seq], 0), c1 = min(p.cu_chunks[seq + 1], p.max_chunks);
-  for (int c = c1 - 1; c >= c0; --c) {
-    const ChunkRow row = chunk_row(p, c);
-    if (row.count == 0) continue;
-    unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
-    const int64_t at = (int64_t(row.first) * p.H + h) * p.dv + v;
-    const TIN* dop = static_cast<const TIN*>(p.d_o) + at;
-    f32x4 G[2][NT];                        // dO
+  for (int c = k.c1 - 1; c >= k.c0; --c) {
+    const int first = k.first, count = min(CT, k.end - first);
+    unsigned char* cur = blk;
+    __syncthreads();
+    st.store(lds, tid);
+    __syncthreads();
+    k.first -= CT;
+    blk -= int64_t(p.H) * w.block();
+    if (c > k.c0) st.load(p, blk, k.first, CT, k.h, vals, tid);
+
+    write_state(D, cur + w.ds(), false, p.dv, v, lane);
+    f32x4 G[2][NT], Y[2][NT];
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int tok = 16 * tt + 4 * g + r;
-        float x[NT];
-        load_cols<NT>(dop + int64_t(min(tok, row.count - 1)) * p.H * p.dv, x);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) G[tt][t][r] = tok < row.count ? x[t] : 0.f;
+      for (int t = 0; t < NT; ++t) {
+        G[tt][t] = St::values(lds, tt, ct0 + t, lane);         // dO
+        Y[tt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
-    float* ds = reinterpret_cast<float*>(blk + w.ds()) + v;
-#pragma unroll
-    for (int f = 0; f < NKT; ++f)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) ds[(16 * f + 4 * g + r) * p.dv + t] = D[f][t][r];
-
-    Split gb[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) gb[t] = tokens_operand<NT>(G, t);
-    f32x4 Y[2][NT];
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const Split a = plane_at(blk + w.pt(), w.sq(), tt * 64 + lane);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) Y[tt][t] = mma3(a, gb[t], f32x4{0.f, 0.f, 0.f, 0.f});
-    }
+    // dU
 #pragma unroll
     for (int s = 0; s < NKS; ++s) {
       Split sb[NT];
@@ -260,10 +416,20 @@ __global__ __launch_bounds__(64) void backward_kernel(SeqParams p) {
       for (int t = 0; t < NT; ++t) sb[t] = state_operand<NKT, NT>(D, s, t);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        const Split a = plane_at(blk + w.kb(), w.plane(), (tt * NKS + s) * 64 + lane);
+        const Split a = St::rows(lds, St::A_K, St::A_KB, tt, s, lane);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) Y[tt][t] = mma3(a, sb[t], Y[tt][t]);
+        for (int t = 0; t < NT; ++t) Y[tt][t] = mma_plane<!RAW>(a, sb[t], Y[tt][t]);
       }
+    }
+    Split gb[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) gb[t] = tokens_operand<NT>(G, t);
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const Split a = square_at(lds + St::A_PT, tt, lane);
+      const f32x4 gf = RAW ? St::factor(lds, St::A_G, tt, lane) : f32x4{1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+      for (int t = 0; t < NT; ++t) Y[tt][t] = mma3(a, gb[t], RAW ? Y[tt][t] * gf : Y[tt][t]);
     }
     if constexpr (DELTA) {
       Split rb[NT];
@@ -271,64 +437,53 @@ __global__ __launch_bounds__(64) void backward_kernel(SeqParams p) {
       for (int t = 0; t < NT; ++t) rb[t] = tokens_operand<NT>(Y, t);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        const Split a = plane_at(blk + w.mt(), w.sq(), tt * 64 + lane);
+        const Split a = square_at(lds + St::A_MT, tt, lane);
 #pragma unroll
         for (int t = 0; t < NT; ++t) Y[tt][t] = mma3(a, rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
       }
     }
-    const float* beta = reinterpret_cast<const float*>(blk + w.beta());
-    float* zo = reinterpret_cast<float*>(blk + w.z()) + v;
-    TIN* dvp = static_cast<TIN*>(p.dv_) + at;
+    float* zo = reinterpret_cast<float*>(cur + w.z()) + v;
+    TIN* dvp = static_cast<TIN*>(p.dv_) + (int64_t(first) * p.H + k.h) * p.dv + v;
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int tok = 16 * tt + 4 * g + r;
-        const float be = DELTA ? beta[tok] : 1.f;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          zo[tok * p.dv + t] = Y[tt][t][r];
-          Y[tt][t][r] *= be;
-          if (tok < row.count) narrow(dvp + int64_t(tok) * p.H * p.dv + t, Y[tt][t][r]);
-        }
-      }
-    Split yb[NT];
-    if constexpr (DELTA) {
+    for (int tt = 0; tt < 2; ++tt) {
+      const f32x4 be = DELTA ? St::factor(lds, St::A_BETA, tt, lane) : f32x4{1.f, 1.f, 1.f, 1.f};
+      const f32x4 f = RAW ? St::factor(lds, St::A_F, tt, lane) : f32x4{1.f, 1.f, 1.f, 1.f};
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) Y[tt][t] = -Y[tt][t];
-        yb[t] = tokens_operand<NT>(Y, t);
+        for (int r = 0; r < 4; ++r) {
+          const int tok = 16 * tt + 4 * g + r;
+          zo[tok * p.dv + 16 * t] = Y[tt][t][r];
+          if (DELTA) Y[tt][t][r] *= be[r];
+          if (tok < count) narrow(dvp + int64_t(tok) * p.H * p.dv + 16 * t, Y[tt][t][r]);
+        }
+        if constexpr (RAW) {
+          G[tt][t] *= f;
+          Y[tt][t] *= f;
+        }
+        Y[tt][t] = -Y[tt][t];
       }
     }
-    const float* dec = reinterpret_cast<const float*>(blk + w.dec());
+    Split yb[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if constexpr (RAW) gb[t] = tokens_operand<NT>(G, t);
+      if constexpr (DELTA) yb[t] = tokens_operand<NT>(Y, t);
+    }
 #pragma unroll
     for (int f = 0; f < NKT; ++f) {
-      const f32x4 d = *reinterpret_cast<const f32x4*>(dec + 16 * f + 4 * g);
-      const Split a = plane_at(blk + w.qht(), w.plane(), f * 64 + lane);
+      const f32x4 d = St::decay(lds, f, lane);
+      const Split a = St::cols(lds, St::A_Q, St::A_QH, f, lane);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) D[f][t][r] *= d[r];
-        D[f][t] = mma3(a, gb[t], D[f][t]);
-      }
+      for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(a, gb[t], D[f][t] * d);
       if constexpr (DELTA) {
-        const Split ak = plane_at(blk + w.kht(), w.plane(), f * 64 + lane);
+        const Split ak = St::cols(lds, St::A_K, St::A_KH, f, lane);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) D[f][t] = mma3(ak, yb[t], D[f][t]);
+        for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(ak, yb[t], D[f][t]);
       }
     }
   }
-  if (p.S_out) {
-#pragma unroll
-    for (int f = 0; f < NKT; ++f)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-          store_state(p.S_out, p.state_bf16, state_at + int64_t(16 * f + 4 * g + r) * p.dv + t,
-                      D[f][t][r]);
-  }
+  if (p.S_out) write_state(D, p.S_out, p.state_bf16, p.dv, state_at, lane);
 }
 
 }  // namespace dl
