@@ -12,40 +12,65 @@
 //   dl_i = q_i dq_i + k_i dk'_i - k_i dk''_i,   dlam_t = sum_{s>=t} dl_s + sum_v (S' D)
 // with S' the state after the chunk: sum_v S' D = e^{l_T} sum_v S D + sum_j Kb_j dKb_j.
 // RWKV6: q_i dq_i counts towards l_{i-1}, and its bonus pair (dP_ii) goes to q, k and u alone.
+//
+// Each wave owns dk/64 tiles of 16 keys and all tokens, as MFMA results: a lane has one key
+// and the eight tokens 16 tt + 4 g + r, which are also the terms (state order) that it feeds a
+// product over tokens, so keys, queries and decay factors are fetched once for both uses.
 #pragma once
 
 #include "dl_prep.hpp"
 
 namespace dl {
 
-template <int DK>
-struct GradShared {
-  PrepShared<DK> in;
-  float dq[CT][DK + 1], dkr[CT][DK + 1], dkc[CT][DK + 1];
-  float dP[CT][CT + 1], dG[CT][CT + 1];
-  float bnd[DK];
-  float tok_sum[CT];
-};
-
-__device__ __forceinline__ void load8(const float* p, float* x) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+// One key's eight tokens of a lane, in state order.
+template <int LD>
+__device__ __forceinline__ void lane_tokens(const uint16_t (*m)[LD], int f, int lane, float* x) {
+  const int i = lane & 15, r = 4 * (lane >> 4) + (i >> 2);
+  const bf16x4 a = read_column(reinterpret_cast<const unsigned char*>(&m[r][16 * f + 4 * (i & 3)]));
+  const bf16x4 b = read_column(reinterpret_cast<const unsigned char*>(&m[r + 16][16 * f + 4 * (i & 3)]));
 #pragma unroll
-  for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
+  for (int e = 0; e < 4; ++e) { x[e] = (float)a[e]; x[4 + e] = (float)b[e]; }
 }
-__device__ __forceinline__ void load8(const uint16_t* p, float* x) {
-  const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+template <int LD>
+__device__ __forceinline__ void lane_tokens(const float (*m)[LD], int f, int lane, float* x) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    x[2 * e] = __uint_as_float(a[e] << 16);
-    x[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
-  }
+  for (int e = 0; e < 8; ++e) x[e] = m[state_term(lane, e)][16 * f + (lane & 15)];
+}
+
+// A token x token matrix (or its transpose) as an operand over tokens.
+template <bool TR>
+__device__ __forceinline__ Split square_operand(const float (*m)[CT + 1], int tt, int lane) {
+  float a[8];
+  const int i = 16 * tt + (lane & 15);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) a[e] = TR ? m[state_term(lane, e)][i] : m[i][state_term(lane, e)];
+  return split8(a);
+}
+
+// A token row's eight values as an operand over values; bf16 ones are exact (lo unused).
+__device__ __forceinline__ Split value_operand(const uint16_t* at, bool live) {
+  Split s;
+  u32x4 x = *reinterpret_cast<const u32x4*>(at);
+  const u32x4 zero = {0, 0, 0, 0};
+  if (!live) x = zero;
+  s.hi = __builtin_bit_cast(bf16x8, x);
+  return s;
+}
+__device__ __forceinline__ Split value_operand(const float* at, bool live) {
+  float x[8];
+  load8(at, x);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = live ? x[e] : 0.f;
+  return split8(x);
 }
 
 template <int DC, int DK, typename TIN>
 __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
-  __shared__ GradShared<DK> sh;
-  PrepShared<DK>& in = sh.in;
-  const int tid = threadIdx.x, nt = 256, lane = tid & 63, wave = tid >> 6;
+  constexpr int KT = DK / 64;                  // key tiles of a wave
+  constexpr bool LO = sizeof(TIN) == 4;        // dO has a second half
+  __shared__ ChunkIn<DC, DK, TIN> in;
+  __shared__ float dP[CT][CT + 1], dG[CT][CT + 1], tok_sum[4][CT + 1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int c16 = lane & 15, g = lane >> 4;
   const int h = blockIdx.x % p.H, c = blockIdx.x / p.H;
   const WsLayout w{DK, p.dv, p.raw, true};
@@ -53,8 +78,7 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
   float* du = reinterpret_cast<float*>(blk + w.du());
   const ChunkRow row = chunk_row(p, c);
   if (row.count == 0) {
-    if (DC == DC_BONUS)
-      for (int r = tid; r < DK; r += nt) du[r] = 0.f;
+    if (DC == DC_BONUS && tid < DK) du[tid] = 0.f;
     return;
   }
   const float* S = reinterpret_cast<const float*>(blk + w.s0());
@@ -62,175 +86,317 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
   const float* E = reinterpret_cast<const float*>(blk + w.e());
   const float* Z = reinterpret_cast<const float*>(blk + w.z());
   const TIN* dop = static_cast<const TIN*>(p.d_o) + (int64_t(row.first) * p.H + h) * p.dv;
+  const int64_t do_row = int64_t(p.H) * p.dv;
 
-  load_chunk<DC, DK, TIN>(in, p, row, h, tid, nt);
+  in.template load<256>(p, row, h, tid);
 
-  auto do_row = [&](int t, int v, float* x) {
-    load8(dop + int64_t(min(t, row.count - 1)) * p.H * p.dv + v, x);
+  // Products over the value columns: token x key ...
+  f32x4 aq[KT][2], ar[KT][2], ac[KT][2];
+  float dot[KT];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = t < row.count ? x[e] : 0.f;
-  };
-  auto scaled = [&](const float* m, int t, int v, float f, float* x) {
-    load8(m + t * p.dv + v, x);
+  for (int x = 0; x < KT; ++x) {
+    dot[x] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= f;
-  };
-
-  // token x key products over the value columns
-  for (int kt = wave; kt < DK / 16; kt += 4) {
-    const int key = 16 * kt + c16;
-    f32x4 aq[2], ar[2], ac[2];
+    for (int tt = 0; tt < 2; ++tt) aq[x][tt] = ar[x][tt] = ac[x][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  for (int s = 0; s < p.dv / 32; ++s) {
+    const int v = 32 * s + 8 * g;
+    Split od[2], oz[2], oe[2];
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) aq[tt] = ar[tt] = ac[tt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float dot = 0.f;
-    for (int s = 0; s < p.dv / 32; ++s) {
-      const int v = 32 * s + 8 * g;
-      float xs[8], xd[8], x[8];
+    for (int tt = 0; tt < 2; ++tt) {
+      const int t = 16 * tt + c16;
+      float x[8];
+      od[tt] = value_operand(dop + min(t, row.count - 1) * do_row + v, t < row.count);
+      if (p.delta) {
+        load8(Z + t * p.dv + v, x);
+        oz[tt] = split8(x);
+      }
+      load8(E + t * p.dv + v, x);
+      oe[tt] = split8(x);
+    }
+#pragma unroll
+    for (int x = 0; x < KT; ++x) {
+      const int key = 16 * (wave * KT + x) + c16;
+      float xs[8], xd[8];
       load8(S + key * p.dv + v, xs);
       load8(D + key * p.dv + v, xd);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) dot += xs[e] * xd[e];
+      for (int e = 0; e < 8; ++e) dot[x] += xs[e] * xd[e];
       const Split bs = split8(xs), bd = split8(xd);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        const int t = 16 * tt + c16;
-        const float be = p.delta ? in.beta[t] : 1.f;
-        do_row(t, v, x);
-        aq[tt] = mma3(split8(x), bs, aq[tt]);
-        if (p.delta) {
-          scaled(Z, t, v, -be, x);
-          ar[tt] = mma3(split8(x), bs, ar[tt]);
-        }
-        scaled(E, t, v, be, x);
-        ac[tt] = mma3(split8(x), bd, ac[tt]);
+        aq[x][tt] = mma(od[tt].hi, bs.lo, aq[x][tt]);
+        if constexpr (LO) aq[x][tt] = mma(od[tt].lo, bs.hi, aq[x][tt]);
+        aq[x][tt] = mma(od[tt].hi, bs.hi, aq[x][tt]);
+        if (p.delta) ar[x][tt] = mma3(oz[tt], bs, ar[x][tt]);
+        ac[x][tt] = mma3(oe[tt], bd, ac[x][tt]);
       }
     }
-    float share = 0.f;                       // sum_j Kb_j dKb_j
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = 16 * tt + 4 * g + r;
-        const float l = prep_l<DC>(in, t, key);
-        const float dkb = ac[tt][r] * __expf(prep_l<DC>(in, CT - 1, key) - l);
-        share += in.k[t][key] * dkb;
-        sh.dq[t][key] = aq[tt][r] * __expf(prep_lq<DC>(in, t, key));
-        sh.dkr[t][key] = ar[tt][r] * __expf(l);
-        sh.dkc[t][key] = dkb;
-      }
-    dot = dot * __expf(prep_l<DC>(in, CT - 1, key)) + share;
-    dot += __shfl_xor(dot, 16);
-    dot += __shfl_xor(dot, 32);
-    if (g == 0) sh.bnd[key] = dot;
   }
-  // token x token products
-  for (int task = wave; task < 8; task += 4) {
-    const bool isP = task & 1;
-    const int bi = task >> 2, bj = (task >> 1) & 1;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    if (bi >= bj && (isP || p.delta)) {
-      for (int s = 0; s < p.dv / 32; ++s) {
-        const int v = 32 * s + 8 * g, i = 16 * bi + c16, j = 16 * bj + c16;
-        float a[8], b[8];
-        if (isP) do_row(i, v, a);
-        else scaled(Z, i, v, -in.beta[i], a);
-        scaled(E, j, v, p.delta ? in.beta[j] : 1.f, b);
-        acc = mma3(split8(a), split8(b), acc);
+  // ... and token x token: a block of dP and dG per wave; the last wave has dbeta.
+  if (wave < 3) {
+    const int bi = wave == 0 ? 0 : 1, bj = wave == 1 ? 1 : 0;   // (0,0), (1,1), (1,0)
+    const int i = 16 * bi + c16, j = 16 * bj + c16;
+    f32x4 ap = {0.f, 0.f, 0.f, 0.f}, ag = ap;
+    for (int s = 0; s < p.dv / 32; ++s) {
+      const int v = 32 * s + 8 * g;
+      float x[8];
+      load8(E + j * p.dv + v, x);
+      const Split b = split8(x);
+      const Split a = value_operand(dop + min(i, row.count - 1) * do_row + v, i < row.count);
+      ap = mma(a.hi, b.lo, ap);
+      if constexpr (LO) ap = mma(a.lo, b.hi, ap);
+      ap = mma(a.hi, b.hi, ap);
+      if (p.delta) {
+        load8(Z + i * p.dv + v, x);
+        ag = mma3(split8(x), b, ag);
       }
     }
+    const float bj_ = p.delta ? in.beta[j] : 1.f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int i = 16 * bi + 4 * g + r, j = 16 * bj + c16;
-      if (isP) sh.dP[i][j] = i >= j ? acc[r] : 0.f;
-      else sh.dG[i][j] = i > j ? acc[r] : 0.f;
+      const int ri = 16 * bi + 4 * g + r;
+      float f = bj_;
+      if (DC == DC_SCALAR) f *= exp2_of(fminf(in.l[ri][0] - in.l[j][0], 0.f));
+      if constexpr (DC == DC_BONUS) {
+        if (ri == j) tok_sum[0][j] = ap[r];      // the bonus pair, apart from the others
+        dP[ri][j] = ri > j ? ap[r] * f : 0.f;
+      } else {
+        dP[ri][j] = ri >= j ? ap[r] * f : 0.f;
+      }
+      dG[ri][j] = ri > j ? -ag[r] * f * in.beta[ri] : 0.f;
     }
-  }
-  // dbeta
-  if (p.delta) {
-    const int t = tid >> 3, part = tid & 7;      // eight lanes per token
-    float s = 0.f;
-    for (int v = part; v < p.dv; v += 8) s += E[t * p.dv + v] * Z[t * p.dv + v];
-    s += __shfl_xor(s, 1);
-    s += __shfl_xor(s, 2);
-    s += __shfl_xor(s, 4);
-    if (part == 0 && t < row.count) p.dbeta[int64_t(row.first + t) * p.H + h] = s;
+  } else {
+    for (int x = lane; x < 256; x += 64) dP[x >> 4][16 + (x & 15)] = dG[x >> 4][16 + (x & 15)] = 0.f;
+    if (p.delta) {
+      const int t = lane >> 1;                 // two lanes a token
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+      for (int v = 4 * (lane & 1); v < p.dv; v += 8)
+        sum += *reinterpret_cast<const f32x4*>(E + t * p.dv + v) *
+               *reinterpret_cast<const f32x4*>(Z + t * p.dv + v);
+      float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      s += __shfl_xor(s, 1);
+      if (!(lane & 1) && t < row.count) p.dbeta[int64_t(row.first + t) * p.H + h] = s;
+    }
   }
   __syncthreads();
 
-  // pairs inside the chunk, a key per thread and the tokens split over the rest
-  constexpr int PER = 256 / DK;
-  const int r = tid % DK, part = tid / DK;
-  for (int i = part; i < CT; i += PER) {
-    float aq = 0.f, ar = 0.f, ac = 0.f;
-    const float li = prep_l<DC>(in, i, r), lqi = prep_lq<DC>(in, i, r);
-    for (int j = 0; j < i; ++j) {
-      const float lj = prep_l<DC>(in, j, r), kj = in.k[j][r];
-      aq += sh.dP[i][j] * kj * __expf(fminf(lqi - lj, 0.f));
-      ar += sh.dG[i][j] * kj * __expf(li - lj);
-    }
-    if (DC != DC_BONUS) aq += sh.dP[i][i] * in.k[i][r];
-    for (int m = i + 1; m < CT; ++m) {
-      const float lm = prep_l<DC>(in, m, r), lqm = prep_lq<DC>(in, m, r);
-      ac += sh.dP[m][i] * in.q[m][r] * __expf(fminf(lqm - li, 0.f)) +
-            sh.dG[m][i] * in.k[m][r] * __expf(lm - li);
-    }
-    if (DC != DC_BONUS) ac += sh.dP[i][i] * in.q[i][r];
-    sh.dq[i][r] += aq;
-    sh.dkr[i][r] += ar;
-    sh.dkc[i][r] += ac;
-  }
-  __syncthreads();
+  f32x4 be[2];
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt)
+    be[tt] = p.delta ? *reinterpret_cast<const f32x4*>(&in.beta[16 * tt + 4 * g])
+                     : f32x4{1.f, 1.f, 1.f, 1.f};
+  float ck[8], cq[8];                          // scalar log-decay: sums over this wave's keys
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ck[e] = cq[e] = 0.f;
+  float bnd_all = 0.f;
 
-  // log-decays: suffix sums over the chunk's tokens
-  if constexpr (DC == DC_SCALAR) {
-    if (p.dlam) {
-      const int t = tid >> 3, sub = tid & 7;       // eight lanes per token
-      float s = 0.f, bs = 0.f;
-      for (int x = sub; x < DK; x += 8) {
-        s += in.q[t][x] * sh.dq[t][x] + in.k[t][x] * (sh.dkr[t][x] - sh.dkc[t][x]);
-        bs += sh.bnd[x];
+#pragma unroll
+  for (int x = 0; x < KT; ++x) {
+    const int f = wave * KT + x, key = 16 * f + c16;
+    float k[8], q[8], l[8], lq[8];
+    lane_tokens(in.k, f, lane, k);
+    lane_tokens(in.q, f, lane, q);
+    const float lT = in.at(CT - 1, key);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      l[e] = in.at(state_term(lane, e), key);
+      lq[e] = DC == DC_BONUS ? in.at_q(state_term(lane, e), key) : l[e];
+    }
+    float share = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int tt = e >> 2, r = e & 3;
+      const float fl = exp2_of(l[e]), fr = exp2_of(lT - l[e]) * be[tt][r];
+      aq[x][tt][r] *= DC == DC_BONUS ? exp2_of(lq[e]) : fl;
+      ar[x][tt][r] *= -fl * be[tt][r];
+      ac[x][tt][r] *= fr;
+      share += k[e] * ac[x][tt][r];
+    }
+    float bnd = dot[x] * exp2_of(lT) + share;
+    bnd += __shfl_xor(bnd, 16);
+    bnd += __shfl_xor(bnd, 32);
+
+    // pairs inside the chunk
+    if constexpr (DC == DC_SCALAR) {
+      const Split bk = split8(k), bq = split8(q);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const Split a = square_operand<false>(dP, tt, lane), at = square_operand<true>(dP, tt, lane);
+        aq[x][tt] = mma3(a, bk, aq[x][tt]);
+        ac[x][tt] = mma3(at, bq, ac[x][tt]);
+        if (p.delta) {
+          const Split b = square_operand<false>(dG, tt, lane), bt = square_operand<true>(dG, tt, lane);
+          ar[x][tt] = mma3(b, bk, ar[x][tt]);
+          ac[x][tt] = mma3(bt, bk, ac[x][tt]);
+        }
+      }
+    } else if (!in.wide) {
+      // Rows of the first half against m = l_7, of the second against m = l_23: e^{l_i - m}
+      // outside the product, e^{m - l_j} inside.  The first half's rows use no token of the
+      // second (0 there: its factor could overflow); the second half's factors of earlier
+      // tokens are at most 1.  For dk'' the two change places.
+      const float m0 = in.at(7, key), m1 = in.at(23, key);
+      float kin0[8], kin1[8], s0[8], s1[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        kin0[e] = e < 4 ? k[e] * exp2_of(m0 - l[e]) : 0.f;
+        kin1[e] = k[e] * exp2_of(m1 - l[e]);
+      }
+      const Split bk0 = split8(kin0), bk1 = split8(kin1);
+      f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+      f32x4 pq[2], pr[2], pc[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const Split a = square_operand<false>(dP, tt, lane);
+        const Split ax = square_operand<false>(dG, tt, lane);
+        pq[tt] = mma3(a, tt ? bk1 : bk0, zero);
+        pr[tt] = p.delta ? mma3(ax, tt ? bk1 : bk0, zero) : zero;
       }
 #pragma unroll
-      for (int d = 1; d < 8; d *= 2) {
-        s += __shfl_xor(s, d);
-        bs += __shfl_xor(bs, d);
+      for (int e = 0; e < 8; ++e) {
+        s0[e] = q[e] * exp2_of(lq[e] - m0);
+        s1[e] = e < 4 ? 0.f : q[e] * exp2_of(lq[e] - m1);
       }
-      if (sub == 0) sh.tok_sum[t] = s;
-      __syncthreads();
-      if (sub == 0 && t < row.count) {
-        float acc = bs;
-        for (int m = CT - 1; m >= t; --m) acc += sh.tok_sum[m];
-        p.dlam[int64_t(row.first + t) * p.H + h] = acc;
+      const Split bq0 = split8(s0), bq1 = split8(s1);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+        pc[tt] = mma3(square_operand<true>(dP, tt, lane), tt ? bq1 : bq0, zero);
+      if (p.delta) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          s0[e] = k[e] * exp2_of(l[e] - m0);
+          s1[e] = e < 4 ? 0.f : k[e] * exp2_of(l[e] - m1);
+        }
+        const Split c0 = split8(s0), c1 = split8(s1);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+          pc[tt] = mma3(square_operand<true>(dG, tt, lane), tt ? c1 : c0, pc[tt]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int tt = e >> 2, r = e & 3;
+        const float m = tt ? m1 : m0;
+        const float out = exp2_of(l[e] - m);
+        aq[x][tt][r] += pq[tt][r] * (DC == DC_BONUS ? exp2_of(lq[e] - m) : out);
+        ar[x][tt][r] += pr[tt][r] * out;
+        ac[x][tt][r] += pc[tt][r] * exp2_of(m - l[e]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int tt = e >> 2, r = e & 3, i = state_term(lane, e);
+        float sq = 0.f, sr = 0.f, sc = 0.f;
+#pragma unroll 1
+        for (int j = 0; j < CT; ++j) {
+          const float kj = widen(in.k[j][key]), qj = widen(in.q[j][key]);
+          const float lj = in.at(j, key), lqj = in.at_q(j, key);
+          if (j < i || (j == i && DC == DC_KEY)) {
+            sq += dP[i][j] * kj * exp2_of(fminf(lq[e] - lj, 0.f));
+            sr += dG[i][j] * kj * exp2_of(l[e] - lj);
+          }
+          if (j > i || (j == i && DC == DC_KEY))
+            sc += dP[j][i] * qj * exp2_of(fminf(lqj - l[e], 0.f)) + dG[j][i] * kj * exp2_of(lj - l[e]);
+        }
+        aq[x][tt][r] += sq;
+        ar[x][tt][r] += sr;
+        ac[x][tt][r] += sc;
       }
     }
-  } else if (tid < DK) {
-    float acc = sh.bnd[tid];
-    for (int t = CT - 1; t >= 0; --t) {
-      const float fromq = in.q[t][tid] * sh.dq[t][tid];
-      acc += in.k[t][tid] * (sh.dkr[t][tid] - sh.dkc[t][tid]);
-      if (DC == DC_KEY) acc += fromq;
-      if (t < row.count) p.dlam[(int64_t(row.first + t) * p.H + h) * DK + tid] = acc;
-      if (DC == DC_BONUS) acc += fromq;
+
+    // log-decays
+    if constexpr (DC == DC_SCALAR) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        ck[e] += q[e] * aq[x][e >> 2][e & 3] + k[e] * (ar[x][e >> 2][e & 3] - ac[x][e >> 2][e & 3]);
+      bnd_all += bnd;
+    } else {
+      // suffix sums over tokens: over r in the lane, over g across lanes, then the halves
+      float sum[2], after[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        float s = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          ck[4 * tt + r] = k[4 * tt + r] * (ar[x][tt][r] - ac[x][tt][r]);
+          cq[4 * tt + r] = q[4 * tt + r] * aq[x][tt][r];
+          s += ck[4 * tt + r] + cq[4 * tt + r];
+        }
+        float y = __shfl_down(s, 16);
+        float t = s + (g < 3 ? y : 0.f);
+        y = __shfl_down(t, 32);
+        t += g < 2 ? y : 0.f;
+        sum[tt] = __shfl(t, c16);
+        y = __shfl_down(t, 16);
+        after[tt] = g < 3 ? y : 0.f;
+      }
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        float acc = bnd + (tt ? 0.f : sum[1]) + after[tt];
+#pragma unroll
+        for (int r = 3; r >= 0; --r) {
+          const int t = 16 * tt + 4 * g + r;
+          acc += ck[4 * tt + r];
+          if (DC == DC_KEY) acc += cq[4 * tt + r];
+          if (t < row.count) p.dlam[(int64_t(row.first + t) * p.H + h) * DK + key] = acc;
+          if (DC == DC_BONUS) acc += cq[4 * tt + r];
+        }
+      }
+    }
+
+    // queries and keys
+    TIN* dqp = static_cast<TIN*>(p.dq) + (int64_t(row.first) * p.H + h) * DK + key;
+    TIN* dkp = static_cast<TIN*>(p.dk_) + (int64_t(row.first) * p.H + h) * DK + key;
+    const float u = DC == DC_BONUS ? p.u[int64_t(h) * DK + key] : 0.f;
+    float dus = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int tt = e >> 2, r = e & 3, t = 16 * tt + 4 * g + r;
+      float xq = aq[x][tt][r], xk = ar[x][tt][r] + ac[x][tt][r];
+      if constexpr (DC == DC_BONUS) {
+        const float own_pair = tok_sum[0][t];
+        xq += own_pair * u * k[e];
+        xk += own_pair * u * q[e];
+        dus += own_pair * q[e] * k[e];
+      }
+      if (t < row.count) {
+        narrow(dqp + int64_t(t) * p.H * DK, xq);
+        narrow(dkp + int64_t(t) * p.H * DK, xk);
+      }
+    }
+    if constexpr (DC == DC_BONUS) {
+      dus += __shfl_xor(dus, 16);
+      dus += __shfl_xor(dus, 32);
+      if (g == 0) du[key] = dus;
     }
   }
 
-  // queries and keys
-  TIN* dqp = static_cast<TIN*>(p.dq) + (int64_t(row.first) * p.H + h) * DK;
-  TIN* dkp = static_cast<TIN*>(p.dk_) + (int64_t(row.first) * p.H + h) * DK;
-  const float ur = DC == DC_BONUS ? p.u[int64_t(h) * DK + r] : 0.f;
-  for (int t = part; t < row.count; t += PER) {
-    float xq = sh.dq[t][r], xk = sh.dkr[t][r] + sh.dkc[t][r];
-    if (DC == DC_BONUS) {
-      xq += sh.dP[t][t] * ur * in.k[t][r];
-      xk += sh.dP[t][t] * ur * in.q[t][r];
+  if constexpr (DC == DC_SCALAR) {
+    if (p.dlam) {
+#pragma unroll
+      for (int d = 1; d < 16; d *= 2) {
+        bnd_all += __shfl_xor(bnd_all, d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ck[e] += __shfl_xor(ck[e], d);
+      }
+      if (c16 == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tok_sum[wave][state_term(lane, e)] = ck[e];
+        if (g == 0) tok_sum[wave][CT] = bnd_all;
+      }
+      __syncthreads();
+      if (tid < 64) {
+        float s = 0.f;
+        if (tid <= CT) s = tok_sum[0][tid] + tok_sum[1][tid] + tok_sum[2][tid] + tok_sum[3][tid];
+#pragma unroll
+        for (int d = 1; d <= CT; d *= 2) {         // suffix sums over lanes 0..CT
+          const float y = __shfl_down(s, d);
+          if (tid + d <= CT) s += y;
+        }
+        if (tid < row.count) p.dlam[int64_t(row.first + tid) * p.H + h] = s;
+      }
     }
-    narrow(dqp + int64_t(t) * p.H * DK + r, xq);
-    narrow(dkp + int64_t(t) * p.H * DK + r, xk);
-  }
-  if (DC == DC_BONUS && tid < DK) {
-    float s = 0.f;
-    for (int t = 0; t < CT; ++t) s += sh.dP[t][t] * in.q[t][tid] * in.k[t][tid];
-    du[tid] = s;
   }
 }
 

@@ -18,10 +18,11 @@ hipError_t start(K* kernel, int64_t grid, int block, const SeqParams& p, hipStre
 template <int DK, typename TIN>
 hipError_t launch_prep(int op, const SeqParams& p, hipStream_t s) {
   const int64_t grid = int64_t(p.max_chunks) * p.H;
-  if (p.raw) return start(&raw_prep_kernel<DK>, grid, 64, p, s);
+  if (p.raw) return start(&raw_prep_kernel<DK>, grid, 64, p, s);   // bf16, head-wise decay
   if (op == DL_OP_RWKV6) return start(&prep_kernel<DC_BONUS, DK, TIN>, grid, 256, p, s);
   if (op == DL_OP_KDA || op == DL_OP_GLA) return start(&prep_kernel<DC_KEY, DK, TIN>, grid, 256, p, s);
-  return start(&prep_kernel<DC_SCALAR, DK, TIN>, grid, 256, p, s);
+  if constexpr (sizeof(TIN) == 4) return start(&prep_kernel<DC_SCALAR, DK, TIN>, grid, 256, p, s);
+  return hipErrorInvalidValue;
 }
 
 template <int DK, bool RAW, bool DELTA, typename TIN>

@@ -6,177 +6,279 @@
 
 namespace dl {
 
-enum DecayClass { DC_SCALAR = 0, DC_KEY = 1, DC_BONUS = 2 };  // one per head (or none) | per key | per key, RWKV6
+// One log-decay per head (or none) | per key | per key, read before the token (RWKV6).
+enum DecayClass { DC_SCALAR = 0, DC_KEY = 1, DC_BONUS = 2 };
 
+constexpr float LOG2E = 1.44269504088896341f;
 constexpr float LOG_FLOOR = -104.f;   // e^-104 rounds to 0 in fp32
 // A diagonal 16 x 16 block of G and P factors through e^{l_i - m} e^{m - l_j} with m the
-// log-decay at its middle; both factors stay below e^60 unless the block decays by more.
-constexpr float WIDE = 60.f;
+// log-decay at its middle; both factors stay below 2^WIDE unless the block decays by more.
+constexpr float WIDE = 80.f;
 
-// LDS of one (chunk, head): inputs widened to fp32, cumulative log-decays, G and P.
-template <int DK>
-struct PrepShared {
-  float k[CT][DK + 4], q[CT][DK + 4];
-  float l[CT][DK + 4];              // l_i (per key)
-  float lq[CT][DK + 4];             // what q_i takes: l_i, or l_{i-1} for RWKV6 (per key)
-  float sl[CT];                     // l_i (one per head)
-  float beta[CT];
-  float G[CT][CT + 1], P[CT][CT + 1], Nm[CT][CT + 1], Mm[CT][CT + 1];
-  float diag[CT];
-  int wide;
-};
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <int DC, int DK, typename TIN>
-__device__ void load_chunk(PrepShared<DK>& sh, const SeqParams& p, const ChunkRow& row, int h,
-                           int tid, int nt) {
-  const TIN* k = static_cast<const TIN*>(p.k);
-  const TIN* q = static_cast<const TIN*>(p.q);
-  for (int i = tid; i < CT * DK; i += nt) {
-    const int t = i / DK, r = i % DK;
-    const bool live = t < row.count;
-    const int64_t at = (int64_t(row.first + (live ? t : 0)) * p.H + h) * DK + r;
-    const float kv = widen(k[at]), qv = widen(q[at]);
-    sh.k[t][r] = live ? kv : 0.f;
-    sh.q[t][r] = live ? qv : 0.f;
-  }
-  if (tid < CT) {
-    const bool live = tid < row.count && p.delta;
-    sh.beta[tid] = live ? p.beta[int64_t(row.first + tid) * p.H + h] : 0.f;
-  }
-  if (tid == 0) sh.wide = 0;
-  if constexpr (DC == DC_SCALAR) {
-    if (tid < 64) {
-      float x = 0.f;
-      if (tid < row.count && p.lam)
-        x = fmaxf(p.lam[int64_t(row.first + tid) * p.H + h], LOG_FLOOR);
+__device__ __forceinline__ void load8(const float* p, float* x) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
 #pragma unroll
-      for (int d = 1; d < CT; d *= 2) {
-        const float y = __shfl_up(x, d);
-        if (tid >= d) x += y;
-      }
-      if (tid < CT) sh.sl[tid] = x;
-    }
-  } else {
-    __syncthreads();               // wide is cleared
-    for (int r = tid; r < DK; r += nt) {
-      const float* lam = p.lam + (int64_t(row.first) * p.H + h) * DK + r;
-      float acc = 0.f, half = 0.f;
-#pragma unroll 8
-      for (int t = 0; t < CT; ++t) {
-        if (t == CT / 2) half = acc;
-        sh.lq[t][r] = acc;
-        if (t < row.count) acc += fmaxf(lam[int64_t(t) * p.H * DK], LOG_FLOOR);
-        if (DC == DC_KEY) sh.lq[t][r] = acc;
-        sh.l[t][r] = acc;
-      }
-      if (-half > WIDE || half - acc > WIDE) atomicOr(&sh.wide, 1);
-    }
+  for (int e = 0; e < 4; ++e) { x[e] = a[e]; x[4 + e] = b[e]; }
+}
+__device__ __forceinline__ void load8(const uint16_t* p, float* x) {
+  const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[2 * e] = __uint_as_float(a[e] << 16);
+    x[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
   }
-  __syncthreads();
 }
 
-// G (strictly lower) and P (lower; RWKV6 strictly, plus its bonus diagonal) into LDS.
-template <int DC, int DK>
-__device__ void pair_products(PrepShared<DK>& sh, const SeqParams& p, int h, int tid, int nt) {
-  const int lane = tid & 63, wave = tid >> 6, nw = nt >> 6;
-  const int c16 = lane & 15, g = lane >> 4;
-  const bool wide = DC != DC_SCALAR && sh.wide != 0;
-  // Upper blocks are zero; the products below write the three lower ones.
-  for (int i = tid; i < 16 * 16; i += nt) sh.G[i / 16][16 + i % 16] = sh.P[i / 16][16 + i % 16] = 0.f;
-  if constexpr (DC == DC_BONUS) {
-    for (int t = wave; t < CT; t += nw) {
-      float s = 0.f;
-      for (int r = lane; r < DK; r += 64) s += sh.q[t][r] * p.u[int64_t(h) * DK + r] * sh.k[t][r];
+// A chunk's inputs in LDS, rows past its end as zero (log-decays: as no decay).  l holds
+// cumulative log-decays in powers of two (l log2 e).
+template <int DC, int DK, typename TIN>
+struct ChunkIn {
+  static constexpr int LD = DK + 16 / int(sizeof(TIN)), LL = DC == DC_SCALAR ? 4 : DK + 4;
+  __attribute__((aligned(16))) TIN k[CT][LD], q[CT][LD];
+  __attribute__((aligned(16))) float l[CT][LL];      // scalar: l[t][0]
+  float beta[CT];
+  int wide;
+
+  __device__ __forceinline__ float at(int t, int r) const { return l[t][DC == DC_SCALAR ? 0 : r]; }
+  // what q_i takes: l_i, or l_{i-1} for RWKV6
+  __device__ __forceinline__ float at_q(int t, int r) const {
+    if constexpr (DC == DC_BONUS) return t ? l[t - 1][r] : 0.f;
+    else return at(t, r);
+  }
+  __device__ __forceinline__ void at8(int t, int r, float* x) const {
+    if constexpr (DC == DC_SCALAR) {
 #pragma unroll
-      for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);
-      if (lane == 0) sh.diag[t] = s;
+      for (int e = 0; e < 8; ++e) x[e] = l[t][0];
+    } else {
+      load8(&l[t][r], x);
+    }
+  }
+  __device__ __forceinline__ void at_q8(int t, int r, float* x) const {
+    if constexpr (DC == DC_BONUS) {
+      load8(&l[t ? t - 1 : 0][r], x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = t ? x[e] : 0.f;
+    } else {
+      at8(t, r, x);
+    }
+  }
+
+  template <int NT>
+  __device__ void load(const SeqParams& p, const ChunkRow& row, int h, int tid) {
+    constexpr int PER = 16 / int(sizeof(TIN)), NPC = DK / PER, NI = CT * NPC / NT;
+    u32x4 kk[NI], qq[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int x = i * NT + tid, t = x / NPC;
+      const int64_t a = (int64_t(row.first + min(t, row.count - 1)) * p.H + h) * DK + PER * (x % NPC);
+      kk[i] = *reinterpret_cast<const u32x4*>(static_cast<const TIN*>(p.k) + a);
+      qq[i] = *reinterpret_cast<const u32x4*>(static_cast<const TIN*>(p.q) + a);
+    }
+    f32x4 lam[DC == DC_SCALAR ? 1 : CT * DK / 4 / NT];
+    float one = 0.f;
+    if constexpr (DC == DC_SCALAR) {
+      if (tid < row.count && p.lam) one = p.lam[int64_t(row.first + tid) * p.H + h];
+    } else {
+      constexpr int LP = DK / 4;
+#pragma unroll
+      for (int i = 0; i < CT * LP / NT; ++i) {
+        const int x = i * NT + tid, t = x / LP;
+        // lam is 4-byte aligned only
+        typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;
+        lam[i] = *reinterpret_cast<const f32x4_any*>(
+            p.lam + (int64_t(row.first + min(t, row.count - 1)) * p.H + h) * DK + 4 * (x % LP));
+      }
+    }
+    float b = 0.f;
+    if (tid < CT) {
+      if (tid < row.count && p.delta) b = p.beta[int64_t(row.first + tid) * p.H + h];
+      beta[tid] = b;
+    }
+    if (tid == 0) wide = 0;
+    const u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int x = i * NT + tid, t = x / NPC;
+      *reinterpret_cast<u32x4*>(&k[t][PER * (x % NPC)]) = t < row.count ? kk[i] : zero;
+      *reinterpret_cast<u32x4*>(&q[t][PER * (x % NPC)]) = t < row.count ? qq[i] : zero;
+    }
+    if constexpr (DC == DC_SCALAR) {
+      if (tid < 64) {
+        float x = tid < row.count ? fmaxf(one, LOG_FLOOR) * LOG2E : 0.f;
+#pragma unroll
+        for (int d = 1; d < CT; d *= 2) {
+          const float y = __shfl_up(x, d);
+          if (tid >= d) x += y;
+        }
+        if (tid < CT) l[tid][0] = x;
+      }
+    } else {
+      constexpr int LP = DK / 4;
+#pragma unroll
+      for (int i = 0; i < CT * LP / NT; ++i) {
+        const int x = i * NT + tid, t = x / LP;
+        f32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = t < row.count ? fmaxf(lam[i][e], LOG_FLOOR) * LOG2E : 0.f;
+        *reinterpret_cast<f32x4*>(&l[t][4 * (x % LP)]) = y;
+      }
+      __syncthreads();
+      if (tid < DK) {
+        float x[CT];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) x[t] = l[t][tid];
+#pragma unroll
+        for (int t = 1; t < CT; ++t) {
+          x[t] += x[t - 1];
+          l[t][tid] = x[t];
+        }
+        if (x[CT / 2 - 1] < -WIDE || x[CT - 1] - x[CT / 2 - 1] < -WIDE) wide = 1;
+      }
     }
     __syncthreads();
   }
-  for (int task = wave; task < 6; task += nw) {
-    const bool isP = task & 1;
-    const int blk = task >> 1;              // (0,0), (1,1), (1,0)
-    const int bi = blk == 0 ? 0 : 1, bj = blk == 1 ? 1 : 0;
-    if (wide && blk != 2) continue;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    const int i = 16 * bi + c16, j = 16 * bj + c16;
-    const int ref = blk == 0 ? 7 : blk == 1 ? 23 : 15;
-    for (int s = 0; s < DK / 32; ++s) {
+};
+
+// G (strictly lower) and P (lower; RWKV6: strictly, and its bonus on the diagonal), by three
+// of the workgroup's waves; by all of them, pair by pair, where a block decays too far.
+template <int DC, int DK, typename TIN>
+__device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[CT + 1], float (*P)[CT + 1],
+                              float* diag, const SeqParams& p, int h, int tid) {
+  const int lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
+  if constexpr (DC == DC_BONUS) {
+    // eight lanes per token
+    const int t = tid >> 3;
+    float s = 0.f;
+    for (int r = 8 * (tid & 7); r < DK; r += 64) {
       float a[8], b[8];
+      load8(&in.q[t][r], a);
+      load8(&in.k[t][r], b);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int r = 32 * s + 8 * g + e;
-        a[e] = isP ? sh.q[i][r] : sh.k[i][r];
-        b[e] = sh.k[j][r];
-        if constexpr (DC != DC_SCALAR) {
-          const float m = sh.l[ref][r];
-          a[e] *= __expf((isP ? sh.lq[i][r] : sh.l[i][r]) - m);
-          b[e] *= __expf(m - sh.l[j][r]);
+      for (int e = 0; e < 8; ++e) s += a[e] * p.u[int64_t(h) * DK + r + e] * b[e];
+    }
+    s += __shfl_xor(s, 1);
+    s += __shfl_xor(s, 2);
+    s += __shfl_xor(s, 4);
+    if ((tid & 7) == 0) diag[t] = s;
+    __syncthreads();
+  }
+  const bool wide = DC != DC_SCALAR && in.wide != 0;
+  if (wave == 3) {
+    for (int i = lane; i < 16 * 16; i += 64) G[i / 16][16 + i % 16] = P[i / 16][16 + i % 16] = 0.f;
+  } else if (!(wide && wave < 2)) {
+    const int bi = wave == 0 ? 0 : 1, bj = wave == 1 ? 1 : 0;   // (0,0), (1,1), (1,0)
+    const int ref = wave == 0 ? 7 : wave == 1 ? 23 : 15;
+    const int i = 16 * bi + c16, j = 16 * bj + c16;
+    f32x4 ag = {0.f, 0.f, 0.f, 0.f}, ap = ag;
+#pragma unroll
+    for (int s = 0; s < DK / 32; ++s) {
+      const int r = 32 * s + 8 * g;
+      float ak[8], aq[8], b[8];
+      load8(&in.k[i][r], ak);
+      load8(&in.q[i][r], aq);
+      load8(&in.k[j][r], b);
+      if constexpr (DC != DC_SCALAR) {
+        float m[8], li[8], lq[8], lj[8];
+        in.at8(ref, r, m);
+        in.at8(i, r, li);
+        in.at8(j, r, lj);
+        if (DC == DC_BONUS) in.at_q8(i, r, lq);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float f = exp2_of(li[e] - m[e]);
+          ak[e] *= f;
+          aq[e] *= DC == DC_BONUS ? exp2_of(lq[e] - m[e]) : f;
+          b[e] *= exp2_of(m[e] - lj[e]);
         }
       }
-      acc = mma3(split8(a), split8(b), acc);
+      const Split sb = split8(b);
+      if (p.delta) ag = mma3(split8(ak), sb, ag);
+      ap = mma3(split8(aq), sb, ap);
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int ri = 16 * bi + 4 * g + r, cj = j;
-      float x = acc[r];
-      if constexpr (DC == DC_SCALAR) x *= __expf(fminf(sh.sl[ri] - sh.sl[cj], 0.f));
-      if (isP) {
-        if constexpr (DC == DC_BONUS) x = ri > cj ? x : ri == cj ? sh.diag[ri] : 0.f;
-        else x = ri >= cj ? x : 0.f;
-        sh.P[ri][cj] = x;
-      } else {
-        sh.G[ri][cj] = ri > cj ? x : 0.f;
+      const int ri = 16 * bi + 4 * g + r;
+      float x = ap[r], y = ag[r];
+      if constexpr (DC == DC_SCALAR) {
+        const float f = exp2_of(fminf(in.l[ri][0] - in.l[j][0], 0.f));
+        x *= f;
+        y *= f;
       }
+      if constexpr (DC == DC_BONUS) P[ri][j] = ri > j ? x : ri == j ? diag[ri] : 0.f;
+      else P[ri][j] = ri >= j ? x : 0.f;
+      G[ri][j] = ri > j ? y : 0.f;
     }
   }
-  if (wide) {                               // pair by pair, the exponent of the difference
-    for (int x = tid; x < 2 * 256; x += nt) {
+  if (wide) {
+    for (int x = tid; x < 2 * 256; x += 256) {
       const int b = x >> 8, i = 16 * b + ((x >> 4) & 15), j = 16 * b + (x & 15);
       float sg = 0.f, sp = 0.f;
       if (i >= j) {
+#pragma unroll 1
         for (int r = 0; r < DK; ++r) {
-          const float kj = sh.k[j][r];
-          sg += sh.k[i][r] * kj * __expf(sh.l[i][r] - sh.l[j][r]);
-          if (DC == DC_KEY || i > j) sp += sh.q[i][r] * kj * __expf(fminf(sh.lq[i][r] - sh.l[j][r], 0.f));
+          const float kj = widen(in.k[j][r]), lj = in.at(j, r);
+          sg += widen(in.k[i][r]) * kj * exp2_of(in.at(i, r) - lj);
+          if (DC == DC_KEY || i > j)
+            sp += widen(in.q[i][r]) * kj * exp2_of(fminf(in.at_q(i, r) - lj, 0.f));
         }
       }
-      sh.G[i][j] = i > j ? sg : 0.f;
-      sh.P[i][j] = (DC == DC_BONUS && i == j) ? sh.diag[i] : sp;
+      G[i][j] = i > j ? sg : 0.f;
+      P[i][j] = (DC == DC_BONUS && i == j) ? diag[i] : sp;
     }
   }
   __syncthreads();
 }
 
-// N = (I + G beta)^-1 in lanes 0-31, M = (I + beta G)^-1 in lanes 32-63 of one wave, a
-// column per lane by forward substitution.
-template <int DK>
-__device__ void solve(PrepShared<DK>& sh, int lane) {
-  const int j = lane & 31;
+// N = (I + G beta)^-1 over G, and M = (I + beta G)^-1, by one wave.  The two diagonal 16 x 16
+// blocks of each by forward substitution, a column per lane (G's row is read before N's takes
+// its place); then the lower left block, N21 = -N22 (G21 beta) N11 and M21 = -M22 (beta G21)
+// M11, by fp32 MFMA: 120 dependent steps instead of 496.
+__device__ __forceinline__ void solve(float (*G)[CT + 1], float (*M)[CT + 1], const float* beta,
+                                      int lane) {
+  const int c16 = lane & 15, g = lane >> 4, o = lane & 16;
   const bool second = lane >= 32;
-  float y[CT];
+  float y[16];
 #pragma unroll
-  for (int i = 0; i < CT; ++i) {
-    float s = 0.f;
+  for (int i = 0; i < 16; ++i) {
+    float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int m = 0; m < i; ++m) s += sh.G[i][m] * y[m];
-    const float b = sh.beta[i], d = i == j ? 1.f : 0.f;
+    for (int m = 0; m < i; ++m) {
+      if (m & 1) s1 += G[o + i][o + m] * y[m];
+      else s0 += G[o + i][o + m] * y[m];
+    }
+    const float b = beta[o + i], s = s0 + s1, d = i == c16 ? 1.f : 0.f;
     const float x = d - (second ? b * s : s);
     y[i] = second ? x : b * x;
-    if (second) sh.Mm[i][j] = x;
-    else sh.Nm[i][j] = x;
+    __builtin_amdgcn_wave_barrier();
+    if (second) {
+      M[o + i][o + c16] = x;
+      if (!o) M[i][16 + c16] = 0.f;
+    } else {
+      G[o + i][o + c16] = x;
+    }
+    __builtin_amdgcn_wave_barrier();
   }
-}
-
-template <int DC, int DK>
-__device__ __forceinline__ float prep_l(const PrepShared<DK>& sh, int t, int r) {
-  if constexpr (DC == DC_SCALAR) return sh.sl[t];
-  else return sh.l[t][r];
-}
-template <int DC, int DK>
-__device__ __forceinline__ float prep_lq(const PrepShared<DK>& sh, int t, int r) {
-  if constexpr (DC == DC_SCALAR) return sh.sl[t];
-  else return sh.lq[t][r];
+  f32x4 tn = {0.f, 0.f, 0.f, 0.f}, tm = tn;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const float a = G[16 + c16][4 * s + g];
+    tn = __builtin_amdgcn_mfma_f32_16x16x4f32(a * beta[4 * s + g], G[4 * s + g][c16], tn, 0, 0, 0);
+    tm = __builtin_amdgcn_mfma_f32_16x16x4f32(a * beta[16 + c16], M[4 * s + g][c16], tm, 0, 0, 0);
+  }
+  f32x4 rn = {0.f, 0.f, 0.f, 0.f}, rm = rn;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    rn = __builtin_amdgcn_mfma_f32_16x16x4f32(G[16 + c16][16 + 4 * g + r], tn[r], rn, 0, 0, 0);
+    rm = __builtin_amdgcn_mfma_f32_16x16x4f32(M[16 + c16][16 + 4 * g + r], tm[r], rm, 0, 0, 0);
+  }
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    G[16 + 4 * g + r][c16] = -rn[r];
+    M[16 + 4 * g + r][c16] = -rm[r];
+  }
 }
 
 __device__ __forceinline__ void put(unsigned char* base, int half, int unit, const float* x) {
@@ -186,10 +288,10 @@ __device__ __forceinline__ void put(unsigned char* base, int half, int unit, con
 }
 
 // The squares from LDS matrices, by NTH threads.
-template <int NTH, int LD>
+template <int NTH>
 __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& w, const SeqParams& p,
-                                            const float (*P)[LD], const float (*Nm)[LD],
-                                            const float (*Mm)[LD], int tid) {
+                                            const float (*P)[CT + 1], const float (*N)[CT + 1],
+                                            const float (*M)[CT + 1], int tid) {
   for (int x = tid; x < CT * CT / 8; x += NTH) {
     const int lane = x & 63, i = 16 * (x >> 6) + (lane & 15);
     float a[8];
@@ -198,7 +300,7 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
     put(blk + w.p(), WsLayout::SQ, x, a);
     if (p.delta) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) a[e] = Nm[i][state_term(lane, e)];
+      for (int e = 0; e < 8; ++e) a[e] = N[i][state_term(lane, e)];
       put(blk + w.n(), WsLayout::SQ, x, a);
     }
     if (p.bwd) {
@@ -207,7 +309,7 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
       put(blk + w.pt(), WsLayout::SQ, x, a);
       if (p.delta) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] = Mm[state_term(lane, e)][i];
+        for (int e = 0; e < 8; ++e) a[e] = M[state_term(lane, e)][i];
         put(blk + w.mt(), WsLayout::SQ, x, a);
       }
     }
@@ -216,42 +318,46 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
 
 template <int DC, int DK, typename TIN>
 __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
-  __shared__ PrepShared<DK> sh;
-  const int tid = threadIdx.x, nt = 256;
+  __shared__ ChunkIn<DC, DK, TIN> in;
+  __shared__ float G[CT][CT + 1], P[CT][CT + 1], M[CT][CT + 1], diag[CT];
+  const int tid = threadIdx.x;
   const int h = blockIdx.x % p.H, c = blockIdx.x / p.H;
   const ChunkRow row = chunk_row(p, c);
   if (row.count == 0) return;
   const WsLayout w{DK, p.dv, false, p.bwd};
   unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
 
-  load_chunk<DC, DK, TIN>(sh, p, row, h, tid, nt);
-  pair_products<DC, DK>(sh, p, h, tid, nt);
-  if (p.delta) {
-    if (tid < 64) solve(sh, tid);
-    __syncthreads();
-  }
+  in.template load<256>(p, row, h, tid);
+  pair_products<DC, DK, TIN>(in, G, P, diag, p, h, tid);
+  // One wave solves while the others go on to the planes.
+  if (p.delta && tid < 64) solve(G, M, in.beta, tid);
+
   float* dec = reinterpret_cast<float*>(blk + w.dec());
   float* beta = reinterpret_cast<float*>(blk + w.beta());
-  for (int r = tid; r < DK; r += nt) dec[r] = __expf(prep_l<DC>(sh, CT - 1, r));
-  if (tid < CT) beta[tid] = sh.beta[tid];
-
+  if (tid < DK) dec[tid] = exp2_of(in.at(CT - 1, tid));
+  if (tid < CT) beta[tid] = in.beta[tid];
   constexpr int NP = DK / 8;
-  for (int x = tid; x < CT * NP; x += nt) {
-    const int t = x / NP, k0 = 8 * (x % NP), at = piece_at<NP>(t, x % NP);
-    float a[8], b[8], d[8];
+  for (int x = tid; x < CT * NP; x += 256) {
+    const int t = x / NP, r = 8 * (x % NP), at = piece_at<NP>(t, x % NP);
+    float k[8], q[8], l[8], lq[8], lT[8], f[8];
+    load8(&in.k[t][r], k);
+    load8(&in.q[t][r], q);
+    in.at8(t, r, l);
+    in.at8(CT - 1, r, lT);
+    if (DC == DC_BONUS) in.at_q8(t, r, lq);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int r = k0 + e;
-      const float l = prep_l<DC>(sh, t, r);
-      a[e] = sh.k[t][r] * __expf(l);
-      b[e] = sh.q[t][r] * __expf(prep_lq<DC>(sh, t, r));
-      d[e] = sh.k[t][r] * __expf(prep_l<DC>(sh, CT - 1, r) - l);
+      f[e] = exp2_of(l[e]);
+      q[e] *= DC == DC_BONUS ? exp2_of(lq[e]) : f[e];
+      lT[e] = k[e] * exp2_of(lT[e] - l[e]);
+      k[e] *= f[e];
     }
-    if (p.delta) put(blk + w.kh(), w.plane(), at, a);
-    put(blk + w.qh(), w.plane(), at, b);
-    put(blk + w.kb(), w.plane(), at, d);
+    if (p.delta) put(blk + w.kh(), w.plane(), at, k);
+    put(blk + w.qh(), w.plane(), at, q);
+    put(blk + w.kb(), w.plane(), at, lT);
   }
-  put_squares<256>(blk, w, p, sh.P, sh.Nm, sh.Mm, tid);
+  __syncthreads();
+  put_squares<256>(blk, w, p, P, G, M, tid);
 }
 
 // The same for bf16 keys and queries with one log-decay per head or none, one wave per
@@ -260,7 +366,7 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
 template <int DK>
 __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   constexpr int NKS = DK / 32;
-  __shared__ float G[CT][CT + 1], P[CT][CT + 1], Mm[CT][CT + 1];
+  __shared__ float G[CT][CT + 1], P[CT][CT + 1], M[CT][CT + 1], betas[CT];
   const int lane = threadIdx.x, c16 = lane & 15, g = lane >> 4;
   const int h = blockIdx.x % p.H, c = blockIdx.x / p.H;
   const ChunkRow row = chunk_row(p, c);
@@ -286,7 +392,7 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   }
   const bool live = lane < row.count;
   const int64_t tok = int64_t(row.first + (live ? lane : 0)) * p.H + h;
-  float l = live && p.lam ? fmaxf(p.lam[tok], LOG_FLOOR) : 0.f;
+  float l = live && p.lam ? fmaxf(p.lam[tok], LOG_FLOOR) * LOG2E : 0.f;
   const float beta = live && p.delta ? p.beta[tok] : 0.f;
 #pragma unroll
   for (int d = 1; d < CT; d *= 2) {
@@ -296,9 +402,9 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   const float lT = __shfl(l, CT - 1);
   if (lane < CT) {
     float* fac = reinterpret_cast<float*>(blk + w.beta());
-    fac[lane] = beta;
-    fac[CT + lane] = __expf(l);
-    fac[2 * CT + lane] = __expf(lT - l);
+    fac[lane] = betas[lane] = beta;
+    fac[CT + lane] = exp2_of(l);
+    fac[2 * CT + lane] = exp2_of(lT - l);
   }
 #pragma unroll
   for (int b = 0; b < 3; ++b) {                 // (0,0), (1,1), (1,0)
@@ -314,7 +420,7 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = 16 * bi + 4 * g + r;
-      const float x = __expf(fminf(__shfl(l, i) - lj, 0.f));
+      const float x = exp2_of(fminf(__shfl(l, i) - lj, 0.f));
       P[i][j] = i >= j ? ap[r] * x : 0.f;
       G[i][j] = i > j ? ag[r] * x : 0.f;
     }
@@ -322,26 +428,9 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) G[4 * g + r][16 + c16] = P[4 * g + r][16 + c16] = 0.f;
   __syncthreads();
-  if (p.delta) {
-    // as solve(): row i of G is used at step i alone, and N's row i replaces it
-    const int j = lane & 31;
-    const bool second = lane >= 32;
-    float y[CT];
-#pragma unroll
-    for (int i = 0; i < CT; ++i) {
-      float s = 0.f;
-#pragma unroll
-      for (int m = 0; m < i; ++m) s += G[i][m] * y[m];
-      const float b = __shfl(beta, i), d = i == j ? 1.f : 0.f;
-      const float x = d - (second ? b * s : s);
-      y[i] = second ? x : b * x;
-      __syncthreads();
-      if (second) Mm[i][j] = x;
-      else G[i][j] = x;
-    }
-    __syncthreads();
-  }
-  put_squares<64>(blk, w, p, P, G, Mm, lane);
+  if (p.delta) solve(G, M, betas, lane);
+  __syncthreads();
+  put_squares<64>(blk, w, p, P, G, M, lane);
 }
 
 }  // namespace dl
