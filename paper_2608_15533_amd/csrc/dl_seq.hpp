@@ -69,7 +69,8 @@ struct Stage {
 
   static constexpr int NLIN = (LINEAR / 16 + T - 1) / T;
   static constexpr int NKQ = RAW ? CT * NP / T : 0;
-  static constexpr int NV = (CT * VNP + T - 1) / T;
+  static constexpr int NV = CT * VNP / T;
+  static_assert(CT * VNP % T == 0, "whole rounds of value pieces");
   u32x4 lin[NLIN], kk[NKQ ? NKQ : 1], qq[NKQ ? NKQ : 1], vv[NV];
 
   // vals: row 0, this workgroup's first column, of this head's value rows (stride H dv).
@@ -78,12 +79,10 @@ struct Stage {
     const WsLayout w{DK, p.dv, RAW, p.bwd};
     const unsigned char* rest = blk + (DELTA ? (BWD ? w.kh() : w.n()) : RAW ? w.dec() : w.qh());
     constexpr int HEAD = BWD ? 0 : SQ2;                        // P comes first in the block
-    const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < NLIN; ++i) {
-      const int x = 16 * (i * T + tid);
-      if (x < LINEAR)
-        lin[i] = *reinterpret_cast<const u32x4*>(x < HEAD ? blk + w.p() + x : rest + (x - HEAD));
+      const int x = min(16 * (i * T + tid), LINEAR - 16);
+      lin[i] = *reinterpret_cast<const u32x4*>(x < HEAD ? blk + w.p() + x : rest + (x - HEAD));
     }
     if constexpr (RAW) {
 #pragma unroll
@@ -92,21 +91,19 @@ struct Stage {
         const int64_t at = (int64_t(first + min(r, count - 1)) * p.H + h) * DK + 8 * pc;
         kk[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.k) + at);
         qq[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + at);
-        if (r >= count) kk[i] = qq[i] = zero;
       }
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int x = i * T + tid, r = x / VNP;
-      if (x < CT * VNP) {
-        const TIN* at = vals + int64_t(first + min(r, count - 1)) * p.H * p.dv;
-        vv[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(at) +
-                                                16 * (x % VNP));
-        if (r >= count) vv[i] = zero;
-      }
+      const TIN* at = vals + int64_t(first + min(r, count - 1)) * p.H * p.dv;
+      vv[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(at) +
+                                              16 * (x % VNP));
     }
   }
-  __device__ __forceinline__ void store(unsigned char* lds, int tid) const {
+  // Rows past the chunk's end become zero here: a test in load() would wait for the data.
+  __device__ __forceinline__ void store(unsigned char* lds, int count, int tid) const {
+    const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < NLIN; ++i) {
       const int x = 16 * (i * T + tid);
@@ -115,19 +112,43 @@ struct Stage {
     if constexpr (RAW) {
 #pragma unroll
       for (int i = 0; i < NKQ; ++i) {
-        *reinterpret_cast<u32x4*>(lds + A_K + 16 * (i * T + tid)) = kk[i];
-        *reinterpret_cast<u32x4*>(lds + A_Q + 16 * (i * T + tid)) = qq[i];
+        const bool live = (i * T + tid) / NP < count;
+        *reinterpret_cast<u32x4*>(lds + A_K + 16 * (i * T + tid)) = live ? kk[i] : zero;
+        *reinterpret_cast<u32x4*>(lds + A_Q + 16 * (i * T + tid)) = live ? qq[i] : zero;
       }
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int x = i * T + tid, r = x / VNP;
-      if (x < CT * VNP) {
-        if constexpr (sizeof(TIN) == 2)
-          *reinterpret_cast<u32x4*>(lds + A_V + 16 * piece_at<VNP>(r, x % VNP)) = vv[i];
-        else
-          *reinterpret_cast<u32x4*>(lds + A_V + r * VROW + 16 * (x % VNP)) = vv[i];
-      }
+      *reinterpret_cast<u32x4*>(lds + value_piece(r, x % VNP)) = r < count ? vv[i] : zero;
+    }
+  }
+  static __device__ __forceinline__ int value_piece(int r, int x) {
+    return A_V + (sizeof(TIN) == 2 ? 16 * piece_at<VNP>(r, x) : r * VROW + 16 * x);
+  }
+  // A wave's result tiles over its own value columns, which it has read, and from there to
+  // memory in 16-byte pieces (rows below count): out points to row 0, the wave's first column.
+  static __device__ __forceinline__ void results(unsigned char* lds, const f32x4 (&x)[2][NT], int ct0,
+                                                 TIN* out, int64_t stride, int count, int lane) {
+    const int c16 = lane & 15, g = lane >> 4;
+    constexpr int PER = 16 / int(sizeof(TIN));
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int col = 16 * (ct0 + t) + c16;
+          narrow(reinterpret_cast<TIN*>(lds + value_piece(16 * tt + 4 * g + r, col / PER)) + col % PER,
+                 x[tt][t][r]);
+        }
+    __builtin_amdgcn_wave_barrier();
+    constexpr int WP = 16 * NT / PER;                        // pieces of a row
+#pragma unroll
+    for (int i = 0; i < CT * WP / 64; ++i) {
+      const int y = i * 64 + lane, r = y / WP, pc = y % WP;
+      const u32x4 z = *reinterpret_cast<const u32x4*>(lds + value_piece(r, 16 * ct0 / PER + pc));
+      if (r < count) *reinterpret_cast<u32x4*>(out + r * stride + PER * pc) = z;
     }
   }
   // Value rows as result tiles: tokens 16 tt + 4 g + r, column 16 ct + l%16.
@@ -221,7 +242,13 @@ __device__ __forceinline__ void write_state(const f32x4 (&S)[NKT][NT], void* bas
         store_state(base, bf16, at + int64_t(16 * f + 4 * (lane >> 4) + r) * dv + 16 * t, S[f][t][r]);
 }
 
-template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
+// Operand reads are issued ahead of the arithmetic that hides their latency; the scheduler
+// must not move them back to their uses.
+__device__ __forceinline__ void issued() { __builtin_amdgcn_sched_barrier(0); }
+
+// SAVE: the backward pass's states before each chunk and E go to the workspace; otherwise
+// outputs and final states are written.
+template <int DK, int NT, int NW, bool RAW, bool DELTA, bool SAVE, typename TIN>
 __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
   using St = Stage<DK, NT, NW, RAW, DELTA, false, TIN>;
   constexpr int NKT = DK / 16, NKS = DK / 32;
@@ -229,9 +256,10 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
   Walk k;
   if (!start_walk<St::VC>(p, k)) return;
-  const WsLayout w{DK, p.dv, RAW, p.bwd};
+  const WsLayout w{DK, p.dv, RAW, SAVE};
   const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;        // this lane's first column
   const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
+  const int64_t row_stride = int64_t(p.H) * p.dv, step = int64_t(p.H) * w.block();
   const TIN* vals = static_cast<const TIN*>(p.v) + int64_t(k.h) * p.dv + k.v0;
   unsigned char* blk = p.ws + (int64_t(k.c0) * p.H + k.h) * w.block();
 
@@ -244,22 +272,42 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
     const int first = k.first, count = min(CT, k.end - first);
     unsigned char* cur = blk;
     __syncthreads();
-    st.store(lds, tid);
+    st.store(lds, count, tid);
     __syncthreads();
-    k.first += CT;
-    blk += int64_t(p.H) * w.block();
-    if (c + 1 < k.c1) st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
+    if (c + 1 < k.c1) {                       // after the last chunk that one again, unused
+      k.first += CT;
+      blk += step;
+    }
+    st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
+    issued();
 
-    if (p.bwd)
-      write_state(S, cur + w.s0(), false, p.dv, v, lane);
     f32x4 U[2][NT], O[2][NT], X[2][NT];
+    Split ak[2][NKS], aq[2][NKS], an[2], ap[2];
+    f32x4 ff[2];
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
+    for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+      for (int s = 0; s < NKS; ++s) {
+        if constexpr (DELTA) ak[tt][s] = St::rows(lds, St::A_K, St::A_KH, tt, s, lane);
+      }
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         U[tt][t] = St::values(lds, tt, ct0 + t, lane);
         O[tt][t] = X[tt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
+      if constexpr (RAW) ff[tt] = St::factor(lds, St::A_F, tt, lane);
+      if constexpr (DELTA) an[tt] = square_at(lds + St::A_N, tt, lane);
+    }
+    if constexpr (!SAVE) {
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+        for (int s = 0; s < NKS; ++s) aq[tt][s] = St::rows(lds, St::A_Q, St::A_QH, tt, s, lane);
+        ap[tt] = square_at(lds + St::A_P, tt, lane);
+      }
+    }
+    issued();
+    if constexpr (SAVE) write_state(S, cur + w.s0(), false, p.dv, v, lane);
     // Kh S and Qh S
 #pragma unroll
     for (int s = 0; s < NKS; ++s) {
@@ -267,44 +315,38 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) sb[t] = state_operand<NKT, NT>(S, s, t);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        if constexpr (DELTA) {
-          const Split a = St::rows(lds, St::A_K, St::A_KH, tt, s, lane);
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int t = 0; t < NT; ++t) X[tt][t] = mma_plane<!RAW>(a, sb[t], X[tt][t]);
+        for (int tt = 0; tt < 2; ++tt) {
+          if constexpr (DELTA) X[tt][t] = mma_plane<!RAW>(ak[tt][s], sb[t], X[tt][t]);
+          if constexpr (!SAVE) O[tt][t] = mma_plane<!RAW>(aq[tt][s], sb[t], O[tt][t]);
         }
-        const Split a = St::rows(lds, St::A_Q, St::A_QH, tt, s, lane);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) O[tt][t] = mma_plane<!RAW>(a, sb[t], O[tt][t]);
-      }
     }
-    if constexpr (RAW) {
+    issued();
+    Split ac[NKT];
+    f32x4 gf[2], be[2];
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const f32x4 f = St::factor(lds, St::A_F, tt, lane);
+    for (int f = 0; f < NKT; ++f) ac[f] = St::cols(lds, St::A_K, St::A_KB, f, lane);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          O[tt][t] *= f;
-          X[tt][t] *= f;
-        }
-      }
+    for (int tt = 0; tt < 2; ++tt) {
+      if constexpr (RAW) gf[tt] = St::factor(lds, St::A_G, tt, lane);
+      if constexpr (DELTA) be[tt] = St::factor(lds, St::A_BETA, tt, lane);
     }
+    issued();
     if constexpr (DELTA) {
       Split rb[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) U[tt][t] -= X[tt][t];
+        for (int tt = 0; tt < 2; ++tt) U[tt][t] -= RAW ? X[tt][t] * ff[tt] : X[tt][t];
         rb[t] = tokens_operand<NT>(U, t);
       }
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const Split a = square_at(lds + St::A_N, tt, lane);
+      for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) U[tt][t] = mma3(a, rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
-      }
+        for (int t = 0; t < NT; ++t) U[tt][t] = mma3(an[tt], rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
     }
-    if (p.bwd) {
+    if constexpr (SAVE) {
       float* eo = reinterpret_cast<float*>(cur + w.e()) + v;
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
@@ -315,55 +357,41 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
     }
     if constexpr (DELTA) {
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const f32x4 be = St::factor(lds, St::A_BETA, tt, lane);
+      for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) U[tt][t] *= be;
-      }
+        for (int t = 0; t < NT; ++t) U[tt][t] *= be[tt];
     }
     Split ub[NT], gb[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) ub[t] = tokens_operand<NT>(U, t);
-    if constexpr (RAW) {
+    for (int t = 0; t < NT; ++t) {
+      if constexpr (!SAVE || !RAW) ub[t] = tokens_operand<NT>(U, t);
+      if constexpr (RAW) {
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const f32x4 gf = St::factor(lds, St::A_G, tt, lane);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) U[tt][t] *= gf;
+        for (int tt = 0; tt < 2; ++tt) U[tt][t] *= gf[tt];
+        gb[t] = tokens_operand<NT>(U, t);
+      } else {
+        gb[t] = ub[t];
       }
-#pragma unroll
-      for (int t = 0; t < NT; ++t) gb[t] = tokens_operand<NT>(U, t);
-    } else {
-#pragma unroll
-      for (int t = 0; t < NT; ++t) gb[t] = ub[t];
     }
     // S <- e^{l_T} S + Kb^T U
 #pragma unroll
     for (int f = 0; f < NKT; ++f) {
       const f32x4 d = St::decay(lds, f, lane);
-      const Split a = St::cols(lds, St::A_K, St::A_KB, f, lane);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) S[f][t] = mma_plane<!RAW>(a, gb[t], S[f][t] * d);
+      for (int t = 0; t < NT; ++t) S[f][t] = mma_plane<!RAW>(ac[f], gb[t], S[f][t] * d);
     }
-    if (p.o) {
-      TIN* op = static_cast<TIN*>(p.o) + (int64_t(first) * p.H + k.h) * p.dv + v;
+    if constexpr (!SAVE) {
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const Split a = square_at(lds + St::A_P, tt, lane);
+      for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) O[tt][t] = mma3(a, ub[t], O[tt][t]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int tok = 16 * tt + 4 * g + r;
-          if (tok < count)
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-              narrow(op + int64_t(tok) * p.H * p.dv + 16 * t, O[tt][t][r]);
-        }
-      }
+        for (int t = 0; t < NT; ++t) O[tt][t] = mma3(ap[tt], ub[t], RAW ? O[tt][t] * ff[tt] : O[tt][t]);
+      St::results(lds, O, ct0,
+                  static_cast<TIN*>(p.o) + int64_t(first) * row_stride + int64_t(k.h) * p.dv + k.v0 +
+                      16 * ct0,
+                  row_stride, count, lane);
     }
   }
-  if (p.S_out) write_state(S, p.S_out, p.state_bf16, p.dv, state_at, lane);
+  if constexpr (!SAVE) write_state(S, p.S_out, p.state_bf16, p.dv, state_at, lane);
 }
 
 // Backward over the chunks, last to first, with D the gradient of the state after a chunk:
@@ -380,6 +408,7 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
   const WsLayout w{DK, p.dv, RAW, true};
   const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;
   const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
+  const int64_t row_stride = int64_t(p.H) * p.dv, step = int64_t(p.H) * w.block();
   const TIN* vals = static_cast<const TIN*>(p.d_o) + int64_t(k.h) * p.dv + k.v0;
   unsigned char* blk = p.ws + (int64_t(k.c1 - 1) * p.H + k.h) * w.block();
   k.first += CT * (k.c1 - 1 - k.c0);
@@ -393,21 +422,35 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
     const int first = k.first, count = min(CT, k.end - first);
     unsigned char* cur = blk;
     __syncthreads();
-    st.store(lds, tid);
+    st.store(lds, count, tid);
     __syncthreads();
-    k.first -= CT;
-    blk -= int64_t(p.H) * w.block();
-    if (c > k.c0) st.load(p, blk, k.first, CT, k.h, vals, tid);
+    if (c > k.c0) {
+      k.first -= CT;
+      blk -= step;
+    }
+    st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
+    issued();
 
-    write_state(D, cur + w.ds(), false, p.dv, v, lane);
     f32x4 G[2][NT], Y[2][NT];
+    Split ar[2][NKS], apt[2];
+    f32x4 gf[2], ff[2];
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
+    for (int tt = 0; tt < 2; ++tt) {
+#pragma unroll
+      for (int s = 0; s < NKS; ++s) ar[tt][s] = St::rows(lds, St::A_K, St::A_KB, tt, s, lane);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         G[tt][t] = St::values(lds, tt, ct0 + t, lane);         // dO
         Y[tt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
+      apt[tt] = square_at(lds + St::A_PT, tt, lane);
+      if constexpr (RAW) {
+        gf[tt] = St::factor(lds, St::A_G, tt, lane);
+        ff[tt] = St::factor(lds, St::A_F, tt, lane);
+      }
+    }
+    issued();
+    write_state(D, cur + w.ds(), false, p.dv, v, lane);
     // dU
 #pragma unroll
     for (int s = 0; s < NKS; ++s) {
@@ -415,73 +458,87 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) sb[t] = state_operand<NKT, NT>(D, s, t);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const Split a = St::rows(lds, St::A_K, St::A_KB, tt, s, lane);
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) Y[tt][t] = mma_plane<!RAW>(a, sb[t], Y[tt][t]);
-      }
+        for (int tt = 0; tt < 2; ++tt) Y[tt][t] = mma_plane<!RAW>(ar[tt][s], sb[t], Y[tt][t]);
     }
+    issued();
+    Split ac[NKT];
+#pragma unroll
+    for (int f = 0; f < NKT; ++f) ac[f] = St::cols(lds, St::A_Q, St::A_QH, f, lane);
+    issued();
     Split gb[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) gb[t] = tokens_operand<NT>(G, t);
 #pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const Split a = square_at(lds + St::A_PT, tt, lane);
-      const f32x4 gf = RAW ? St::factor(lds, St::A_G, tt, lane) : f32x4{1.f, 1.f, 1.f, 1.f};
+    for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) Y[tt][t] = mma3(a, gb[t], RAW ? Y[tt][t] * gf : Y[tt][t]);
-    }
-    if constexpr (DELTA) {
-      Split rb[NT];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) rb[t] = tokens_operand<NT>(Y, t);
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const Split a = square_at(lds + St::A_MT, tt, lane);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) Y[tt][t] = mma3(a, rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
-      }
-    }
-    float* zo = reinterpret_cast<float*>(cur + w.z()) + v;
-    TIN* dvp = static_cast<TIN*>(p.dv_) + (int64_t(first) * p.H + k.h) * p.dv + v;
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      const f32x4 be = DELTA ? St::factor(lds, St::A_BETA, tt, lane) : f32x4{1.f, 1.f, 1.f, 1.f};
-      const f32x4 f = RAW ? St::factor(lds, St::A_F, tt, lane) : f32x4{1.f, 1.f, 1.f, 1.f};
+      for (int t = 0; t < NT; ++t)
+        Y[tt][t] = mma3(apt[tt], gb[t], RAW ? Y[tt][t] * gf[tt] : Y[tt][t]);
+    // D's share of the outputs needs nothing of Y
+    if constexpr (RAW) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int tok = 16 * tt + 4 * g + r;
-          zo[tok * p.dv + 16 * t] = Y[tt][t][r];
-          if (DELTA) Y[tt][t][r] *= be[r];
-          if (tok < count) narrow(dvp + int64_t(tok) * p.H * p.dv + 16 * t, Y[tt][t][r]);
-        }
-        if constexpr (RAW) {
-          G[tt][t] *= f;
-          Y[tt][t] *= f;
-        }
-        Y[tt][t] = -Y[tt][t];
+        for (int tt = 0; tt < 2; ++tt) G[tt][t] *= ff[tt];
+        gb[t] = tokens_operand<NT>(G, t);
       }
-    }
-    Split yb[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      if constexpr (RAW) gb[t] = tokens_operand<NT>(G, t);
-      if constexpr (DELTA) yb[t] = tokens_operand<NT>(Y, t);
     }
 #pragma unroll
     for (int f = 0; f < NKT; ++f) {
       const f32x4 d = St::decay(lds, f, lane);
-      const Split a = St::cols(lds, St::A_Q, St::A_QH, f, lane);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(a, gb[t], D[f][t] * d);
-      if constexpr (DELTA) {
-        const Split ak = St::cols(lds, St::A_K, St::A_KH, f, lane);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(ak, yb[t], D[f][t]);
-      }
+      for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(ac[f], gb[t], D[f][t] * d);
     }
+    float* zo = reinterpret_cast<float*>(cur + w.z()) + v;
+    if constexpr (DELTA) {
+      issued();
+      Split amt[2];
+      f32x4 be[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        amt[tt] = square_at(lds + St::A_MT, tt, lane);
+        be[tt] = St::factor(lds, St::A_BETA, tt, lane);
+      }
+#pragma unroll
+      for (int f = 0; f < NKT; ++f) ac[f] = St::cols(lds, St::A_K, St::A_KH, f, lane);
+      issued();
+      Split rb[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) rb[t] = tokens_operand<NT>(Y, t);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          Y[tt][t] = mma3(amt[tt], rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int r = 0; r < 4; ++r) zo[(16 * tt + 4 * g + r) * p.dv + 16 * t] = Y[tt][t][r];
+          Y[tt][t] *= be[tt];
+        }
+      Split yb[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        f32x4 m[2][1];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) m[tt][0] = RAW ? -Y[tt][t] * ff[tt] : -Y[tt][t];
+        yb[t] = tokens_operand<1>(m, 0);
+      }
+#pragma unroll
+      for (int f = 0; f < NKT; ++f)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(ac[f], yb[t], D[f][t]);
+    } else {
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) zo[(16 * tt + 4 * g + r) * p.dv + 16 * t] = Y[tt][t][r];
+    }
+    St::results(lds, Y, ct0,
+                static_cast<TIN*>(p.dv_) + int64_t(first) * row_stride + int64_t(k.h) * p.dv + k.v0 +
+                    16 * ct0,
+                row_stride, count, lane);
   }
   if (p.S_out) write_state(D, p.S_out, p.state_bf16, p.dv, state_at, lane);
 }
