@@ -90,6 +90,11 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
 
   in.template load<256>(p, row, h, tid);
 
+  // Row x, values v..v+7 of what the serial passes saved ([value tile][row][16]).
+  auto saved = [](const float* m, int rows, int x, int v, float* out) {
+    load8(m + ((v >> 4) * rows + x) * 16 + (v & 15), out);
+  };
+
   // Products over the value columns: token x key ...
   f32x4 aq[KT][2], ar[KT][2], ac[KT][2];
   float dot[KT];
@@ -108,18 +113,18 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
       float x[8];
       od[tt] = value_operand(dop + min(t, row.count - 1) * do_row + v, t < row.count);
       if (p.delta) {
-        load8(Z + t * p.dv + v, x);
+        saved(Z, CT, t, v, x);
         oz[tt] = split8(x);
       }
-      load8(E + t * p.dv + v, x);
+      saved(E, CT, t, v, x);
       oe[tt] = split8(x);
     }
 #pragma unroll
     for (int x = 0; x < KT; ++x) {
       const int key = 16 * (wave * KT + x) + c16;
       float xs[8], xd[8];
-      load8(S + key * p.dv + v, xs);
-      load8(D + key * p.dv + v, xd);
+      saved(S, DK, key, v, xs);
+      saved(D, DK, key, v, xd);
 #pragma unroll
       for (int e = 0; e < 8; ++e) dot[x] += xs[e] * xd[e];
       const Split bs = split8(xs), bd = split8(xd);
@@ -141,14 +146,14 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
     for (int s = 0; s < p.dv / 32; ++s) {
       const int v = 32 * s + 8 * g;
       float x[8];
-      load8(E + j * p.dv + v, x);
+      saved(E, CT, j, v, x);
       const Split b = split8(x);
       const Split a = value_operand(dop + min(i, row.count - 1) * do_row + v, i < row.count);
       ap = mma(a.hi, b.lo, ap);
       if constexpr (LO) ap = mma(a.lo, b.hi, ap);
       ap = mma(a.hi, b.hi, ap);
       if (p.delta) {
-        load8(Z + i * p.dv + v, x);
+        saved(Z, CT, i, v, x);
         ag = mma3(split8(x), b, ag);
       }
     }
@@ -171,10 +176,13 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
     if (p.delta) {
       const int t = lane >> 1;                 // two lanes a token
       f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-      for (int v = 4 * (lane & 1); v < p.dv; v += 8)
-        sum += *reinterpret_cast<const f32x4*>(E + t * p.dv + v) *
-               *reinterpret_cast<const f32x4*>(Z + t * p.dv + v);
+#pragma unroll 4
+      for (int v = 8 * (lane & 1); v < p.dv; v += 16) {
+        const int at = ((v >> 4) * CT + t) * 16 + (v & 15);
+#pragma unroll
+        for (int y = 0; y < 8; y += 4)
+          sum += *reinterpret_cast<const f32x4*>(E + at + y) * *reinterpret_cast<const f32x4*>(Z + at + y);
+      }
       float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
       s += __shfl_xor(s, 1);
       if (!(lane & 1) && t < row.count) p.dbeta[int64_t(row.first + t) * p.H + h] = s;

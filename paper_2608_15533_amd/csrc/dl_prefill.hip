@@ -29,7 +29,7 @@ template <int DK, bool RAW, bool DELTA, bool SAVE, typename TIN>
 hipError_t launch_walk(const SeqParams& p, hipStream_t s) {
   const int64_t heads = int64_t(p.n) * p.H;
   if (wide_walk(heads, p.dv)) {
-    if (p.dv == 128) return start(&forward_kernel<DK, 2, 4, RAW, DELTA, SAVE, TIN>, heads, 256, p, s);
+    if (p.dv == 128) return start(&forward_kernel<DK, 1, 8, RAW, DELTA, SAVE, TIN>, heads, 512, p, s);
     return start(&forward_kernel<DK, 1, 4, RAW, DELTA, SAVE, TIN>, heads, 256, p, s);
   }
   return start(&forward_kernel<DK, 1, 2, RAW, DELTA, SAVE, TIN>, heads * (p.dv / 32), 128, p, s);

@@ -291,7 +291,7 @@ __device__ __forceinline__ void put(unsigned char* base, int half, int unit, con
 template <int NTH>
 __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& w, const SeqParams& p,
                                             const float (*P)[CT + 1], const float (*N)[CT + 1],
-                                            const float (*M)[CT + 1], int tid) {
+                                            const float (*M)[CT + 1], const float* beta, int tid) {
   for (int x = tid; x < CT * CT / 8; x += NTH) {
     const int lane = x & 63, i = 16 * (x >> 6) + (lane & 15);
     float a[8];
@@ -300,7 +300,7 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
     put(blk + w.p(), WsLayout::SQ, x, a);
     if (p.delta) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) a[e] = N[i][state_term(lane, e)];
+      for (int e = 0; e < 8; ++e) a[e] = N[i][state_term(lane, e)] * (p.bwd ? 1.f : beta[i]);
       put(blk + w.n(), WsLayout::SQ, x, a);
     }
     if (p.bwd) {
@@ -357,7 +357,7 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
     put(blk + w.kb(), w.plane(), at, lT);
   }
   __syncthreads();
-  put_squares<256>(blk, w, p, P, G, M, tid);
+  put_squares<256>(blk, w, p, P, G, M, in.beta, tid);
 }
 
 // The same for bf16 keys and queries with one log-decay per head or none, one wave per
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   __syncthreads();
   if (p.delta) solve(G, M, betas, lane);
   __syncthreads();
-  put_squares<64>(blk, w, p, P, G, M, lane);
+  put_squares<64>(blk, w, p, P, G, M, betas, lane);
 }
 
 }  // namespace dl

@@ -40,13 +40,21 @@ struct Split {
   bf16x8 hi, lo;
 };
 
+// 24 VALU instructions: two conversions a pair, hi widened again, the difference.
 __device__ __forceinline__ Split split8(const float* x) {
-  Split s;
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  u32x4 hi, lo;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s.hi[e] = (__bf16)x[e];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) s.lo[e] = (__bf16)(x[e] - (float)s.hi[e]);
-  return s;
+  for (int e = 0; e < 4; ++e) {
+    const f32x2 v = {x[2 * e], x[2 * e + 1]};
+    const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+    const f32x2 d = {x[2 * e] - __uint_as_float(h << 16),
+                     x[2 * e + 1] - __uint_as_float(h & 0xffff0000u)};
+    hi[e] = h;
+    lo[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(d, bf16x2));
+  }
+  return Split{__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, lo)};
 }
 
 // acc += a b over 32 terms.  Lane l holds of the 16x16 result rows 4(l/16)+r, column l%16;
@@ -141,7 +149,7 @@ __device__ __forceinline__ bf16x8 cols_operand(const unsigned char* plane, int f
 //           bf16 keys and queries with one log-decay per head or none: the keys and queries
 //           themselves are the planes, exact in bf16, and e^{l_i} (f) and e^{l_T-l_i} (g)
 //           scale token rows of fp32 products instead.
-//   squares N, P and (backward) P^T, M^T: token x token, hi then lo, in fragment order: the
+//   squares N (beta N where no backward pass asks for E), P and (backward) P^T, M^T: token x token, hi then lo, in fragment order: the
 //           eight terms (state order) a lane feeds one MFMA are 16 consecutive bytes.
 struct WsLayout {
   int dk, dv;
@@ -159,10 +167,10 @@ struct WsLayout {
   __host__ __device__ int g() const { return f() + CT * 4; }             // fp32 [CT] (raw)
   __host__ __device__ int pt() const { return g() + CT * 4; }
   __host__ __device__ int mt() const { return pt() + 2 * SQ; }
-  __host__ __device__ int s0() const { return mt() + 2 * SQ; }           // fp32 [dk][dv] S
-  __host__ __device__ int ds() const { return s0() + dk * dv * 4; }      // fp32 [dk][dv] D
+  __host__ __device__ int s0() const { return mt() + 2 * SQ; }           // fp32 S, [dv/16][dk][16]
+  __host__ __device__ int ds() const { return s0() + dk * dv * 4; }      // fp32 D, [dv/16][dk][16]
   __host__ __device__ int e() const { return ds() + dk * dv * 4; }       // fp32 [CT][dv]
-  __host__ __device__ int z() const { return e() + CT * dv * 4; }        // fp32 [CT][dv]
+  __host__ __device__ int z() const { return e() + CT * dv * 4; }        // fp32 Z, [dv/16][CT][16]
   __host__ __device__ int du() const { return z() + CT * dv * 4; }       // fp32 [dk]
   __host__ __device__ int64_t block() const { return bwd ? du() + dk * 4 : pt(); }
 };

@@ -73,54 +73,72 @@ struct Stage {
   static_assert(CT * VNP % T == 0, "whole rounds of value pieces");
   u32x4 lin[NLIN], kk[NKQ ? NKQ : 1], qq[NKQ ? NKQ : 1], vv[NV];
 
-  // vals: row 0, this workgroup's first column, of this head's value rows (stride H dv).
+  // Everything but the thread's own 32-bit offsets is the same for all lanes.  vals: row 0,
+  // this workgroup's first column, of this head's value rows (stride H dv).
   __device__ __forceinline__ void load(const SeqParams& p, const unsigned char* blk, int first,
                                        int count, int h, const TIN* vals, int tid) {
     const WsLayout w{DK, p.dv, RAW, p.bwd};
     const unsigned char* rest = blk + (DELTA ? (BWD ? w.kh() : w.n()) : RAW ? w.dec() : w.qh());
     constexpr int HEAD = BWD ? 0 : SQ2;                        // P comes first in the block
+    const uint32_t gap = uint32_t(rest - blk) - HEAD;
 #pragma unroll
     for (int i = 0; i < NLIN; ++i) {
-      const int x = min(16 * (i * T + tid), LINEAR - 16);
-      lin[i] = *reinterpret_cast<const u32x4*>(x < HEAD ? blk + w.p() + x : rest + (x - HEAD));
+      uint32_t x = 16 * (i * T + tid);
+      if ((i + 1) * 16 * T > LINEAR) x = min(x, uint32_t(LINEAR - 16));
+      if (i * 16 * T >= HEAD) x += gap;
+      else if ((i + 1) * 16 * T > HEAD) x += x >= uint32_t(HEAD) ? gap : 0u;
+      lin[i] = *reinterpret_cast<const u32x4*>(blk + x);
     }
     if constexpr (RAW) {
+      const uint32_t stride = uint32_t(p.H) * DK * 2, last = uint32_t(count - 1) * stride;
+      const int64_t at = (int64_t(first) * p.H + h) * DK * 2;
+      const unsigned char* kb = static_cast<const unsigned char*>(p.k) + at;
+      const unsigned char* qb = static_cast<const unsigned char*>(p.q) + at;
 #pragma unroll
       for (int i = 0; i < NKQ; ++i) {
         const int x = i * T + tid, r = x / NP, pc = (x % NP) ^ piece_swap<NP>(r);
-        const int64_t at = (int64_t(first + min(r, count - 1)) * p.H + h) * DK + 8 * pc;
-        kk[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.k) + at);
-        qq[i] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + at);
+        const uint32_t o = min(r * stride, last) + 16 * pc;
+        kk[i] = *reinterpret_cast<const u32x4*>(kb + o);
+        qq[i] = *reinterpret_cast<const u32x4*>(qb + o);
       }
     }
+    const uint32_t stride = uint32_t(p.H) * uint32_t(p.dv) * sizeof(TIN);
+    const uint32_t last = uint32_t(count - 1) * stride;
+    const unsigned char* vb = reinterpret_cast<const unsigned char*>(vals + int64_t(first) * p.H * p.dv);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int x = i * T + tid, r = x / VNP;
-      const TIN* at = vals + int64_t(first + min(r, count - 1)) * p.H * p.dv;
-      vv[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(at) +
-                                              16 * (x % VNP));
+      vv[i] = *reinterpret_cast<const u32x4*>(vb + (min(r * stride, last) + 16 * (x % VNP)));
     }
   }
   // Rows past the chunk's end become zero here: a test in load() would wait for the data.
-  __device__ __forceinline__ void store(unsigned char* lds, int count, int tid) const {
-    const u32x4 zero = {0, 0, 0, 0};
+  __device__ __forceinline__ void store(unsigned char* lds, int count, int tid) {
+    if (count < CT) {
+      const u32x4 zero = {0, 0, 0, 0};
+      if constexpr (RAW)
+#pragma unroll
+        for (int i = 0; i < NKQ; ++i)
+          if ((i * T + tid) / NP >= count) kk[i] = qq[i] = zero;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if ((i * T + tid) / VNP >= count) vv[i] = zero;
+    }
 #pragma unroll
     for (int i = 0; i < NLIN; ++i) {
       const int x = 16 * (i * T + tid);
-      if (x < LINEAR) *reinterpret_cast<u32x4*>(lds + x) = lin[i];
+      if ((i + 1) * 16 * T <= LINEAR || x < LINEAR) *reinterpret_cast<u32x4*>(lds + x) = lin[i];
     }
     if constexpr (RAW) {
 #pragma unroll
       for (int i = 0; i < NKQ; ++i) {
-        const bool live = (i * T + tid) / NP < count;
-        *reinterpret_cast<u32x4*>(lds + A_K + 16 * (i * T + tid)) = live ? kk[i] : zero;
-        *reinterpret_cast<u32x4*>(lds + A_Q + 16 * (i * T + tid)) = live ? qq[i] : zero;
+        *reinterpret_cast<u32x4*>(lds + A_K + 16 * (i * T + tid)) = kk[i];
+        *reinterpret_cast<u32x4*>(lds + A_Q + 16 * (i * T + tid)) = qq[i];
       }
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int x = i * T + tid, r = x / VNP;
-      *reinterpret_cast<u32x4*>(lds + value_piece(r, x % VNP)) = r < count ? vv[i] : zero;
+      const int x = i * T + tid;
+      *reinterpret_cast<u32x4*>(lds + value_piece(x / VNP, x % VNP)) = vv[i];
     }
   }
   static __device__ __forceinline__ int value_piece(int r, int x) {
@@ -242,12 +260,30 @@ __device__ __forceinline__ void write_state(const f32x4 (&S)[NKT][NT], void* bas
         store_state(base, bf16, at + int64_t(16 * f + 4 * (lane >> 4) + r) * dv + 16 * t, S[f][t][r]);
 }
 
-// Operand reads are issued ahead of the arithmetic that hides their latency; the scheduler
-// must not move them back to their uses.
-__device__ __forceinline__ void issued() { __builtin_amdgcn_sched_barrier(0); }
+// A wave that has its SIMD to itself (NW <= 2) issues operand reads ahead of the arithmetic
+// that hides their latency, and the scheduler must not move them back to their uses; with two
+// waves to a SIMD the other wave hides it, and the registers are worth more.
+template <int NW>
+__device__ __forceinline__ void issued() {
+  if constexpr (NW <= 2) __builtin_amdgcn_sched_barrier(0);
+}
 
 // SAVE: the backward pass's states before each chunk and E go to the workspace; otherwise
 // outputs and final states are written.
+// Results into the workspace, [column tile][row][16] (rows: keys, or tokens).
+template <int NR, int NT>
+__device__ __forceinline__ void save_tiles(const f32x4 (&x)[NR][NT], unsigned char* base, int tile,
+                                           int lane) {
+  float* at = reinterpret_cast<float*>(base) + tile * NR * 256;
+  const uint32_t o = 64 * (lane >> 4) + (lane & 15);
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int f = 0; f < NR; ++f)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) at[o + (t * NR + f) * 256 + 16 * r] = x[f][t][r];
+}
+
 template <int DK, int NT, int NW, bool RAW, bool DELTA, bool SAVE, typename TIN>
 __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
   using St = Stage<DK, NT, NW, RAW, DELTA, false, TIN>;
@@ -279,7 +315,7 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
       blk += step;
     }
     st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
-    issued();
+    issued<NW>();
 
     f32x4 U[2][NT], O[2][NT], X[2][NT];
     Split ak[2][NKS], aq[2][NKS], an[2], ap[2];
@@ -306,8 +342,8 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
         ap[tt] = square_at(lds + St::A_P, tt, lane);
       }
     }
-    issued();
-    if constexpr (SAVE) write_state(S, cur + w.s0(), false, p.dv, v, lane);
+    issued<NW>();
+    if constexpr (SAVE) save_tiles(S, cur + w.s0(), k.v0 / 16 + ct0, lane);
     // Kh S and Qh S
 #pragma unroll
     for (int s = 0; s < NKS; ++s) {
@@ -322,7 +358,7 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
           if constexpr (!SAVE) O[tt][t] = mma_plane<!RAW>(aq[tt][s], sb[t], O[tt][t]);
         }
     }
-    issued();
+    issued<NW>();
     Split ac[NKT];
     f32x4 gf[2], be[2];
 #pragma unroll
@@ -330,9 +366,9 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
       if constexpr (RAW) gf[tt] = St::factor(lds, St::A_G, tt, lane);
-      if constexpr (DELTA) be[tt] = St::factor(lds, St::A_BETA, tt, lane);
+      if constexpr (DELTA && SAVE) be[tt] = St::factor(lds, St::A_BETA, tt, lane);
     }
-    issued();
+    issued<NW>();
     if constexpr (DELTA) {
       Split rb[NT];
 #pragma unroll
@@ -346,16 +382,8 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) U[tt][t] = mma3(an[tt], rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
     }
-    if constexpr (SAVE) {
-      float* eo = reinterpret_cast<float*>(cur + w.e()) + v;
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int t = 0; t < NT; ++t) eo[(16 * tt + 4 * g + r) * p.dv + 16 * t] = U[tt][t][r];
-    }
-    if constexpr (DELTA) {
+    if constexpr (SAVE) save_tiles(U, cur + w.e(), k.v0 / 16 + ct0, lane);
+    if constexpr (DELTA && SAVE) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
@@ -429,7 +457,7 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
       blk -= step;
     }
     st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
-    issued();
+    issued<NW>();
 
     f32x4 G[2][NT], Y[2][NT];
     Split ar[2][NKS], apt[2];
@@ -449,8 +477,8 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
         ff[tt] = St::factor(lds, St::A_F, tt, lane);
       }
     }
-    issued();
-    write_state(D, cur + w.ds(), false, p.dv, v, lane);
+    issued<NW>();
+    save_tiles(D, cur + w.ds(), k.v0 / 16 + ct0, lane);
     // dU
 #pragma unroll
     for (int s = 0; s < NKS; ++s) {
@@ -462,11 +490,11 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) Y[tt][t] = mma_plane<!RAW>(ar[tt][s], sb[t], Y[tt][t]);
     }
-    issued();
+    issued<NW>();
     Split ac[NKT];
 #pragma unroll
     for (int f = 0; f < NKT; ++f) ac[f] = St::cols(lds, St::A_Q, St::A_QH, f, lane);
-    issued();
+    issued<NW>();
     Split gb[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) gb[t] = tokens_operand<NT>(G, t);
@@ -490,9 +518,8 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(ac[f], gb[t], D[f][t] * d);
     }
-    float* zo = reinterpret_cast<float*>(cur + w.z()) + v;
     if constexpr (DELTA) {
-      issued();
+      issued<NW>();
       Split amt[2];
       f32x4 be[2];
 #pragma unroll
@@ -502,7 +529,7 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
       }
 #pragma unroll
       for (int f = 0; f < NKT; ++f) ac[f] = St::cols(lds, St::A_K, St::A_KH, f, lane);
-      issued();
+      issued<NW>();
       Split rb[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) rb[t] = tokens_operand<NT>(Y, t);
@@ -511,10 +538,12 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           Y[tt][t] = mma3(amt[tt], rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-          for (int r = 0; r < 4; ++r) zo[(16 * tt + 4 * g + r) * p.dv + 16 * t] = Y[tt][t][r];
-          Y[tt][t] *= be[tt];
         }
+      save_tiles(Y, cur + w.z(), k.v0 / 16 + ct0, lane);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) Y[tt][t] *= be[tt];
       Split yb[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -528,12 +557,7 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(ac[f], yb[t], D[f][t]);
     } else {
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) zo[(16 * tt + 4 * g + r) * p.dv + 16 * t] = Y[tt][t][r];
+      save_tiles(Y, cur + w.z(), k.v0 / 16 + ct0, lane);
     }
     St::results(lds, Y, ct0,
                 static_cast<TIN*>(p.dv_) + int64_t(first) * row_stride + int64_t(k.h) * p.dv + k.v0 +

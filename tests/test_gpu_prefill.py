@@ -70,3 +70,11 @@ def test_zero_start(op):
 def test_decays_from_none_to_everything(op, decay):
     """Log-decays scaled up to sums far past what a factor e^(l_i) e^(-l_j) could hold."""
     run(op, [70, 20], 2, 64, 64, backward=True, seed=8, decay=decay)
+
+
+@pytest.mark.parametrize("op", R.OPS)
+@pytest.mark.parametrize("dk,dv", SHAPES)
+def test_many_heads(op, dk, dv):
+    """Enough (sequence, head) pairs for workgroups that walk whole heads."""
+    dtype = BF16 if dk == dv else F32
+    run(op, [37, 5, 64], 1024 // (dv // 32) // 3 + 1, dk, dv, dtype, backward=True, seed=9)
