@@ -218,6 +218,8 @@ struct Stage {
 // Where a workgroup stands: (sequence, head, first value column).
 struct Walk {
   int seq, h, slot, v0, c0, c1, first, end;
+  __device__ __forceinline__ int row(int c) const { return first + CT * (c - c0); }
+  __device__ __forceinline__ int count(int c) const { return min(CT, end - row(c)); }
 };
 template <int VC>
 __device__ __forceinline__ bool start_walk(const SeqParams& p, Walk& k) {
@@ -288,87 +290,77 @@ template <int DK, int NT, int NW, bool RAW, bool DELTA, bool SAVE, typename TIN>
 __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
   using St = Stage<DK, NT, NW, RAW, DELTA, false, TIN>;
   constexpr int NKT = DK / 16, NKS = DK / 32;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[St::BYTES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][St::BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15;
   Walk k;
   if (!start_walk<St::VC>(p, k)) return;
   const WsLayout w{DK, p.dv, RAW, SAVE};
   const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;        // this lane's first column
   const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
-  const int64_t row_stride = int64_t(p.H) * p.dv, step = int64_t(p.H) * w.block();
+  const int64_t row_stride = int64_t(p.H) * p.dv;
   const TIN* vals = static_cast<const TIN*>(p.v) + int64_t(k.h) * p.dv + k.v0;
-  unsigned char* blk = p.ws + (int64_t(k.c0) * p.H + k.h) * w.block();
-
   St st;
-  if (k.c0 < k.c1) st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
-  f32x4 S[NKT][NT];
-  read_state(S, p.S_in, p, state_at, lane);
+  auto fetch = [&](int c) {
+    c = min(c, k.c1 - 1);
+    st.load(p, p.ws + (int64_t(c) * p.H + k.h) * w.block(), k.row(c), k.count(c), k.h, vals, tid);
+  };
 
-  for (int c = k.c0; c < k.c1; ++c) {
-    const int first = k.first, count = min(CT, k.end - first);
-    unsigned char* cur = blk;
-    __syncthreads();
-    st.store(lds, count, tid);
-    __syncthreads();
-    if (c + 1 < k.c1) {                       // after the last chunk that one again, unused
-      k.first += CT;
-      blk += step;
-    }
-    st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
-    issued<NW>();
-
-    f32x4 U[2][NT], O[2][NT], X[2][NT];
-    Split ak[2][NKS], aq[2][NKS], an[2], ap[2];
-    f32x4 ff[2];
+  f32x4 U[2][NT], S[NKT][NT], ff[2];
+  Split ak[2][NKS], an[2];
+  auto ahead = [&](const unsigned char* l) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
 #pragma unroll
-      for (int s = 0; s < NKS; ++s) {
-        if constexpr (DELTA) ak[tt][s] = St::rows(lds, St::A_K, St::A_KH, tt, s, lane);
-      }
+      for (int t = 0; t < NT; ++t) U[tt][t] = St::values(l, tt, ct0 + t, lane);
+      if constexpr (RAW) ff[tt] = St::factor(l, St::A_F, tt, lane);
+      if constexpr (DELTA) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        U[tt][t] = St::values(lds, tt, ct0 + t, lane);
-        O[tt][t] = X[tt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-      if constexpr (RAW) ff[tt] = St::factor(lds, St::A_F, tt, lane);
-      if constexpr (DELTA) an[tt] = square_at(lds + St::A_N, tt, lane);
-    }
-    if constexpr (!SAVE) {
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-#pragma unroll
-        for (int s = 0; s < NKS; ++s) aq[tt][s] = St::rows(lds, St::A_Q, St::A_QH, tt, s, lane);
-        ap[tt] = square_at(lds + St::A_P, tt, lane);
+        for (int s = 0; s < NKS; ++s) ak[tt][s] = St::rows(l, St::A_K, St::A_KH, tt, s, lane);
+        an[tt] = square_at(l + St::A_N, tt, lane);
       }
     }
-    issued<NW>();
-    if constexpr (SAVE) save_tiles(S, cur + w.s0(), k.v0 / 16 + ct0, lane);
-    // Kh S and Qh S
+  };
+  if (k.c0 < k.c1) fetch(k.c0);
+  read_state(S, p.S_in, p, state_at, lane);
+  if (k.c0 < k.c1) {
+    st.store(lds[0], k.count(k.c0), tid);
+    fetch(k.c0 + 1);
+    __syncthreads();
+    ahead(lds[0]);
+  }
+  for (int c = k.c0; c < k.c1; ++c) {
+    unsigned char* cur = lds[(c - k.c0) & 1];
+    unsigned char* nxt = lds[(c - k.c0 + 1) & 1];
+    __syncthreads();
+    st.store(nxt, k.count(min(c + 1, k.c1 - 1)), tid);
+    fetch(c + 2);
+    unsigned char* blk = p.ws + (int64_t(c) * p.H + k.h) * w.block();
+    if constexpr (SAVE) save_tiles(S, blk + w.s0(), k.v0 / 16 + ct0, lane);
+
+    // Kh S, R = V - Kh S, E = N R
+    Split sb[NKS][NT];
+    f32x4 X[2][NT];
 #pragma unroll
     for (int s = 0; s < NKS; ++s) {
-      Split sb[NT];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) sb[t] = state_operand<NKT, NT>(S, s, t);
+      for (int t = 0; t < NT; ++t) {
+        if constexpr (DELTA || !SAVE) sb[s][t] = state_operand<NKT, NT>(S, s, t);
+        if constexpr (DELTA) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          if constexpr (DELTA) X[tt][t] = mma_plane<!RAW>(ak[tt][s], sb[t], X[tt][t]);
-          if constexpr (!SAVE) O[tt][t] = mma_plane<!RAW>(aq[tt][s], sb[t], O[tt][t]);
+          for (int tt = 0; tt < 2; ++tt)
+            X[tt][t] = mma_plane<!RAW>(ak[tt][s], sb[s][t], s ? X[tt][t] : f32x4{0.f, 0.f, 0.f, 0.f});
         }
+      }
     }
-    issued<NW>();
     Split ac[NKT];
     f32x4 gf[2], be[2];
 #pragma unroll
-    for (int f = 0; f < NKT; ++f) ac[f] = St::cols(lds, St::A_K, St::A_KB, f, lane);
+    for (int f = 0; f < NKT; ++f) ac[f] = St::cols(cur, St::A_K, St::A_KB, f, lane);
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      if constexpr (RAW) gf[tt] = St::factor(lds, St::A_G, tt, lane);
-      if constexpr (DELTA && SAVE) be[tt] = St::factor(lds, St::A_BETA, tt, lane);
+      if constexpr (RAW) gf[tt] = St::factor(cur, St::A_G, tt, lane);
+      if constexpr (DELTA && SAVE) be[tt] = St::factor(cur, St::A_BETA, tt, lane);
     }
-    issued<NW>();
     if constexpr (DELTA) {
       Split rb[NT];
 #pragma unroll
@@ -382,7 +374,7 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) U[tt][t] = mma3(an[tt], rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
     }
-    if constexpr (SAVE) save_tiles(U, cur + w.e(), k.v0 / 16 + ct0, lane);
+    if constexpr (SAVE) save_tiles(U, blk + w.e(), k.v0 / 16 + ct0, lane);
     if constexpr (DELTA && SAVE) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
@@ -404,19 +396,37 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
     // S <- e^{l_T} S + Kb^T U
 #pragma unroll
     for (int f = 0; f < NKT; ++f) {
-      const f32x4 d = St::decay(lds, f, lane);
+      const f32x4 d = St::decay(cur, f, lane);
 #pragma unroll
       for (int t = 0; t < NT; ++t) S[f][t] = mma_plane<!RAW>(ac[f], gb[t], S[f][t] * d);
     }
+    __syncthreads();
     if constexpr (!SAVE) {
+      f32x4 O[2][NT], fo[2];
+      Split ap[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        fo[tt] = ff[tt];
+        ap[tt] = square_at(cur + St::A_P, tt, lane);
+#pragma unroll
+        for (int s = 0; s < NKS; ++s) {
+          const Split aq = St::rows(cur, St::A_Q, St::A_QH, tt, s, lane);
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            O[tt][t] = mma_plane<!RAW>(aq, sb[s][t], s ? O[tt][t] : f32x4{0.f, 0.f, 0.f, 0.f});
+        }
+      }
+      ahead(nxt);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) O[tt][t] = mma3(ap[tt], ub[t], RAW ? O[tt][t] * ff[tt] : O[tt][t]);
-      St::results(lds, O, ct0,
-                  static_cast<TIN*>(p.o) + int64_t(first) * row_stride + int64_t(k.h) * p.dv + k.v0 +
-                      16 * ct0,
-                  row_stride, count, lane);
+        for (int t = 0; t < NT; ++t) O[tt][t] = mma3(ap[tt], ub[t], RAW ? O[tt][t] * fo[tt] : O[tt][t]);
+      St::results(cur, O, ct0,
+                  static_cast<TIN*>(p.o) + int64_t(k.row(c)) * row_stride + int64_t(k.h) * p.dv +
+                      k.v0 + 16 * ct0,
+                  row_stride, k.count(c), lane);
+    } else {
+      ahead(nxt);
     }
   }
   if constexpr (!SAVE) write_state(S, p.S_out, p.state_bf16, p.dv, state_at, lane);
