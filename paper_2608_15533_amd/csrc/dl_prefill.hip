@@ -25,18 +25,18 @@ hipError_t launch_prep(int op, const SeqParams& p, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 
-template <int DK, bool RAW, bool DELTA, bool SAVE, typename TIN>
+template <int DK, bool RAW, bool DELTA, int PASS, typename TIN>
 hipError_t launch_walk(const SeqParams& p, hipStream_t s) {
   const int64_t heads = int64_t(p.n) * p.H;
   if (wide_walk(heads, p.dv)) {
-    if (p.dv == 128) return start(&forward_kernel<DK, 1, 8, RAW, DELTA, SAVE, TIN>, heads, 512, p, s);
-    return start(&forward_kernel<DK, 1, 4, RAW, DELTA, SAVE, TIN>, heads, 256, p, s);
+    if (p.dv == 128) return start(&forward_kernel<DK, 1, 8, RAW, DELTA, PASS, TIN>, heads, 512, p, s);
+    return start(&forward_kernel<DK, 1, 4, RAW, DELTA, PASS, TIN>, heads, 256, p, s);
   }
-  return start(&forward_kernel<DK, 1, 2, RAW, DELTA, SAVE, TIN>, heads * (p.dv / 32), 128, p, s);
+  return start(&forward_kernel<DK, 1, 2, RAW, DELTA, PASS, TIN>, heads * (p.dv / 32), 128, p, s);
 }
 template <int DK, bool RAW, bool DELTA, typename TIN>
 hipError_t launch_scan(const SeqParams& p, hipStream_t s) {
-  return p.bwd ? launch_walk<DK, RAW, DELTA, true, TIN>(p, s) : launch_walk<DK, RAW, DELTA, false, TIN>(p, s);
+  return p.bwd ? launch_walk<DK, RAW, DELTA, PASS_SAVE, TIN>(p, s) : launch_walk<DK, RAW, DELTA, PASS_OUT, TIN>(p, s);
 }
 
 template <int DK, typename TIN>

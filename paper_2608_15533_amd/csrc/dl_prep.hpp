@@ -297,7 +297,7 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
     float a[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) a[e] = P[i][state_term(lane, e)];
-    put(blk + w.p(), WsLayout::SQ, x, a);
+    put(blk + w.p(), -WsLayout::SQ, x, a);
     if (p.delta) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) a[e] = N[i][state_term(lane, e)] * (p.bwd ? 1.f : beta[i]);
@@ -353,7 +353,7 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
       k[e] *= f[e];
     }
     if (p.delta) put(blk + w.kh(), w.plane(), at, k);
-    put(blk + w.qh(), w.plane(), at, q);
+    put(blk + w.qh(), -w.plane(), at, q);
     put(blk + w.kb(), w.plane(), at, lT);
   }
   __syncthreads();

@@ -13,10 +13,14 @@
 
 namespace dl {
 
+// A square's operand; LO: bytes from the first half to the second, or 0 for the first alone.
+template <int LO = WsLayout::SQ>
 __device__ __forceinline__ Split square_at(const unsigned char* lds, int tt, int lane) {
   const unsigned char* at = lds + 16 * (tt * 64 + lane);
-  return Split{*reinterpret_cast<const bf16x8*>(at),
-               *reinterpret_cast<const bf16x8*>(at + WsLayout::SQ)};
+  Split s;
+  s.hi = *reinterpret_cast<const bf16x8*>(at);
+  if constexpr (LO != 0) s.lo = *reinterpret_cast<const bf16x8*>(at + LO);
+  return s;
 }
 
 // Result tiles [2][NT] (tokens 16 tt + 4 g + r) as operands over the chunk's tokens.
@@ -43,26 +47,38 @@ __device__ __forceinline__ f32x4 mma_plane(const Split& a, const Split& b, f32x4
   return mma(a.hi, b.hi, acc);
 }
 
+enum PassId { PASS_OUT = 0, PASS_SAVE = 1, PASS_BACK = 2 };
+
 // One chunk's operands on their way from memory to LDS.
-template <int DK, int NT, int NW, bool RAW, bool DELTA, bool BWD, typename TIN>
+template <int DK, int NT, int NW, bool RAW, bool DELTA, int PASS, typename TIN>
 struct Stage {
   static constexpr int T = 64 * NW, VC = 16 * NT * NW, NP = DK / 8;
   static constexpr int HALF = CT * DK * 2;                     // bytes of half a plane
-  static constexpr int SQ2 = 2 * WsLayout::SQ;
+  static constexpr int PL = RAW ? 0 : HALF, SQ = WsLayout::SQ, SQ2 = 2 * SQ;
   static constexpr int FAC = 4 * DK + 12 * CT;
-  // LDS offsets.  Forward: P, N, planes, factors; backward: planes, factors, P^T, M^T.
-  static constexpr int A_P = 0;
-  static constexpr int A_N = BWD ? 0 : SQ2;
-  static constexpr int A_KH = A_N + (!BWD && DELTA ? SQ2 : 0);
-  static constexpr int A_QH = A_KH + (!RAW && DELTA ? 2 * HALF : 0);
-  static constexpr int A_KB = A_QH + (RAW ? 0 : 2 * HALF);
-  static constexpr int A_DEC = A_KB + (RAW ? 0 : 2 * HALF);
+  static constexpr bool BACK = PASS == PASS_BACK, OUT = PASS == PASS_OUT;
+  // Outputs that are rounded to bf16 take Qh S and P U with the second halves of all four left
+  // out: each rounding is at most 2^-9 of its factor, as the output's own is.
+  static constexpr bool BRIEF = OUT && sizeof(TIN) == 2;
+  // LDS offsets, of the workspace block: first P, N, Kh (what of them the pass needs), then Qh,
+  // Kb, the factors, and backward P^T, M^T.  A_P and A_QH are the first halves; the second lie
+  // before them.
+  static constexpr int P_LEN = OUT ? (BRIEF ? SQ : SQ2) : 0;
+  static constexpr int A_P = P_LEN - SQ;
+  static constexpr int A_N = P_LEN;
+  static constexpr int A_KH = A_N + (!BACK && DELTA ? SQ2 : 0);
+  static constexpr int HEAD = A_KH + (DELTA ? 2 * PL : 0);
+  static constexpr int Q_LEN = PASS == PASS_SAVE ? 0 : BRIEF ? PL : 2 * PL;
+  static constexpr int A_QH = HEAD + Q_LEN - PL;
+  static constexpr int A_KB = HEAD + Q_LEN;
+  static constexpr int A_DEC = A_KB + 2 * PL;
   static constexpr int A_BETA = A_DEC + 4 * DK, A_F = A_BETA + 4 * CT, A_G = A_F + 4 * CT;
   static constexpr int A_PT = A_DEC + FAC;
-  static constexpr int A_MT = A_PT + (BWD ? SQ2 : 0);
-  static constexpr int LINEAR = A_MT + (BWD && DELTA ? SQ2 : 0);
+  static constexpr int A_MT = A_PT + (BACK ? SQ2 : 0);
+  static constexpr int LINEAR = A_MT + (BACK && DELTA ? SQ2 : 0);
+  static constexpr bool WITH_Q = PASS != PASS_SAVE;
   static constexpr int A_K = LINEAR, A_Q = A_K + (RAW ? HALF : 0);
-  static constexpr int A_V = A_Q + (RAW ? HALF : 0);
+  static constexpr int A_V = A_Q + (RAW && WITH_Q ? HALF : 0);
   static constexpr int VNP = VC * int(sizeof(TIN)) / 16;       // pieces of a value row
   static constexpr int VROW = sizeof(TIN) == 2 ? VC * 2 : VC * 4 + 16;
   static constexpr int BYTES = A_V + CT * VROW;
@@ -78,15 +94,15 @@ struct Stage {
   __device__ __forceinline__ void load(const SeqParams& p, const unsigned char* blk, int first,
                                        int count, int h, const TIN* vals, int tid) {
     const WsLayout w{DK, p.dv, RAW, p.bwd};
-    const unsigned char* rest = blk + (DELTA ? (BWD ? w.kh() : w.n()) : RAW ? w.dec() : w.qh());
-    constexpr int HEAD = BWD ? 0 : SQ2;                        // P comes first in the block
-    const uint32_t gap = uint32_t(rest - blk) - HEAD;
+    const uint32_t from = BACK ? w.kh() : OUT ? w.p() + SQ - P_LEN : w.n();
+    const uint32_t gap = (BACK || OUT ? w.qh() + PL - Q_LEN : w.kb()) - HEAD;
 #pragma unroll
     for (int i = 0; i < NLIN; ++i) {
       uint32_t x = 16 * (i * T + tid);
       if ((i + 1) * 16 * T > LINEAR) x = min(x, uint32_t(LINEAR - 16));
       if (i * 16 * T >= HEAD) x += gap;
-      else if ((i + 1) * 16 * T > HEAD) x += x >= uint32_t(HEAD) ? gap : 0u;
+      else if ((i + 1) * 16 * T <= HEAD) x += from;
+      else x += x >= uint32_t(HEAD) ? gap : from;
       lin[i] = *reinterpret_cast<const u32x4*>(blk + x);
     }
     if constexpr (RAW) {
@@ -99,7 +115,7 @@ struct Stage {
         const int x = i * T + tid, r = x / NP, pc = (x % NP) ^ piece_swap<NP>(r);
         const uint32_t o = min(r * stride, last) + 16 * pc;
         kk[i] = *reinterpret_cast<const u32x4*>(kb + o);
-        qq[i] = *reinterpret_cast<const u32x4*>(qb + o);
+        if constexpr (WITH_Q) qq[i] = *reinterpret_cast<const u32x4*>(qb + o);
       }
     }
     const uint32_t stride = uint32_t(p.H) * uint32_t(p.dv) * sizeof(TIN);
@@ -132,7 +148,7 @@ struct Stage {
 #pragma unroll
       for (int i = 0; i < NKQ; ++i) {
         *reinterpret_cast<u32x4*>(lds + A_K + 16 * (i * T + tid)) = kk[i];
-        *reinterpret_cast<u32x4*>(lds + A_Q + 16 * (i * T + tid)) = qq[i];
+        if constexpr (WITH_Q) *reinterpret_cast<u32x4*>(lds + A_Q + 16 * (i * T + tid)) = qq[i];
       }
     }
 #pragma unroll
@@ -145,7 +161,9 @@ struct Stage {
     return A_V + (sizeof(TIN) == 2 ? 16 * piece_at<VNP>(r, x) : r * VROW + 16 * x);
   }
   // A wave's result tiles over its own value columns, which it has read, and from there to
-  // memory in 16-byte pieces (rows below count): out points to row 0, the wave's first column.
+  // memory in 16-byte pieces: out points to row 0, the wave's first column.  Rows from count on
+  // write the last row once more: with a store that some lanes or chunks skip, the wait for
+  // the next chunk's loads would have to be one for every store as well.
   static __device__ __forceinline__ void results(unsigned char* lds, const f32x4 (&x)[2][NT], int ct0,
                                                  TIN* out, int64_t stride, int count, int lane) {
     const int c16 = lane & 15, g = lane >> 4;
@@ -164,9 +182,9 @@ struct Stage {
     constexpr int WP = 16 * NT / PER;                        // pieces of a row
 #pragma unroll
     for (int i = 0; i < CT * WP / 64; ++i) {
-      const int y = i * 64 + lane, r = y / WP, pc = y % WP;
+      const int y = i * 64 + lane, r = min(y / WP, count - 1), pc = y % WP;
       const u32x4 z = *reinterpret_cast<const u32x4*>(lds + value_piece(r, 16 * ct0 / PER + pc));
-      if (r < count) *reinterpret_cast<u32x4*>(out + r * stride + PER * pc) = z;
+      *reinterpret_cast<u32x4*>(out + r * stride + PER * pc) = z;
     }
   }
   // Value rows as result tiles: tokens 16 tt + 4 g + r, column 16 ct + l%16.
@@ -189,19 +207,22 @@ struct Stage {
   static __device__ __forceinline__ f32x4 factor(const unsigned char* lds, int at, int tt, int lane) {
     return *reinterpret_cast<const f32x4*>(lds + at + 4 * (16 * tt + 4 * (lane >> 4)));
   }
-  // Operands from the planes; raw ones have no second half.
+  // Operands from the planes; raw ones have no second half.  LO: bytes from the first half to
+  // the second, or 0 for the first alone.
+  template <int LO = HALF>
   static __device__ __forceinline__ Split rows(const unsigned char* lds, int raw_at, int at, int tt,
                                                int s, int lane) {
     Split o;
     o.hi = rows_operand<NP>(lds + (RAW ? raw_at : at), tt, s, lane);
-    if constexpr (!RAW) o.lo = rows_operand<NP>(lds + at + HALF, tt, s, lane);
+    if constexpr (!RAW && LO != 0) o.lo = rows_operand<NP>(lds + at + LO, tt, s, lane);
     return o;
   }
+  template <int LO = HALF>
   static __device__ __forceinline__ Split cols(const unsigned char* lds, int raw_at, int at, int f,
                                                int lane) {
     Split o;
     o.hi = cols_operand<NP>(lds + (RAW ? raw_at : at), f, lane);
-    if constexpr (!RAW) o.lo = cols_operand<NP>(lds + at + HALF, f, lane);
+    if constexpr (!RAW && LO != 0) o.lo = cols_operand<NP>(lds + at + LO, f, lane);
     return o;
   }
   // e^{l_T} for keys 16 f + 4 g + r
@@ -262,16 +283,6 @@ __device__ __forceinline__ void write_state(const f32x4 (&S)[NKT][NT], void* bas
         store_state(base, bf16, at + int64_t(16 * f + 4 * (lane >> 4) + r) * dv + 16 * t, S[f][t][r]);
 }
 
-// A wave that has its SIMD to itself (NW <= 2) issues operand reads ahead of the arithmetic
-// that hides their latency, and the scheduler must not move them back to their uses; with two
-// waves to a SIMD the other wave hides it, and the registers are worth more.
-template <int NW>
-__device__ __forceinline__ void issued() {
-  if constexpr (NW <= 2) __builtin_amdgcn_sched_barrier(0);
-}
-
-// SAVE: the backward pass's states before each chunk and E go to the workspace; otherwise
-// outputs and final states are written.
 // Results into the workspace, [column tile][row][16] (rows: keys, or tokens).
 template <int NR, int NT>
 __device__ __forceinline__ void save_tiles(const f32x4 (&x)[NR][NT], unsigned char* base, int tile,
@@ -286,23 +297,32 @@ __device__ __forceinline__ void save_tiles(const f32x4 (&x)[NR][NT], unsigned ch
       for (int r = 0; r < 4; ++r) at[o + (t * NR + f) * 256 + 16 * r] = x[f][t][r];
 }
 
-template <int DK, int NT, int NW, bool RAW, bool DELTA, bool SAVE, typename TIN>
+// PASS_OUT writes outputs and final states; PASS_SAVE the states before each chunk and E, for
+// the backward pass.
+//
+// Two LDS buffers: while chunk c is computed from one, chunk c + 1 goes from registers to the
+// other and c + 2 from memory to registers, and at its end the wave reads what chunk c + 1
+// starts with.  What the state needs comes first, outputs follow.
+template <int DK, int NT, int NW, bool RAW, bool DELTA, int PASS, typename TIN>
 __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
-  using St = Stage<DK, NT, NW, RAW, DELTA, false, TIN>;
+  using St = Stage<DK, NT, NW, RAW, DELTA, PASS, TIN>;
   constexpr int NKT = DK / 16, NKS = DK / 32;
+  constexpr bool OUT = PASS == PASS_OUT;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   __shared__ __attribute__((aligned(16))) unsigned char lds[2][St::BYTES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15;
   Walk k;
   if (!start_walk<St::VC>(p, k)) return;
-  const WsLayout w{DK, p.dv, RAW, SAVE};
+  const WsLayout w{DK, p.dv, RAW, p.bwd};
   const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;        // this lane's first column
   const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
   const int64_t row_stride = int64_t(p.H) * p.dv;
   const TIN* vals = static_cast<const TIN*>(p.v) + int64_t(k.h) * p.dv + k.v0;
   St st;
+  auto block = [&](int c) { return p.ws + (int64_t(c) * p.H + k.h) * w.block(); };
   auto fetch = [&](int c) {
     c = min(c, k.c1 - 1);
-    st.load(p, p.ws + (int64_t(c) * p.H + k.h) * w.block(), k.row(c), k.count(c), k.h, vals, tid);
+    st.load(p, block(c), k.row(c), k.count(c), k.h, vals, tid);
   };
 
   f32x4 U[2][NT], S[NKT][NT], ff[2];
@@ -320,38 +340,26 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
       }
     }
   };
-  if (k.c0 < k.c1) fetch(k.c0);
-  read_state(S, p.S_in, p, state_at, lane);
-  if (k.c0 < k.c1) {
-    st.store(lds[0], k.count(k.c0), tid);
-    fetch(k.c0 + 1);
-    __syncthreads();
-    ahead(lds[0]);
-  }
-  for (int c = k.c0; c < k.c1; ++c) {
-    unsigned char* cur = lds[(c - k.c0) & 1];
-    unsigned char* nxt = lds[(c - k.c0 + 1) & 1];
+  auto chunk = [&](int c, unsigned char* cur, unsigned char* nxt) __attribute__((always_inline)) {
     __syncthreads();
     st.store(nxt, k.count(min(c + 1, k.c1 - 1)), tid);
     fetch(c + 2);
-    unsigned char* blk = p.ws + (int64_t(c) * p.H + k.h) * w.block();
-    if constexpr (SAVE) save_tiles(S, blk + w.s0(), k.v0 / 16 + ct0, lane);
+    if constexpr (!OUT) save_tiles(S, block(c) + w.s0(), k.v0 / 16 + ct0, lane);
 
-    // Kh S, R = V - Kh S, E = N R
+    // Kh S, R = V - Kh S, E = N R (PASS_OUT: N holds beta N, and U comes at once)
     Split sb[NKS][NT];
     f32x4 X[2][NT];
 #pragma unroll
-    for (int s = 0; s < NKS; ++s) {
+    for (int s = 0; s < NKS; ++s)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        if constexpr (DELTA || !SAVE) sb[s][t] = state_operand<NKT, NT>(S, s, t);
+        if constexpr (DELTA || OUT) sb[s][t] = state_operand<NKT, NT>(S, s, t);
         if constexpr (DELTA) {
 #pragma unroll
           for (int tt = 0; tt < 2; ++tt)
-            X[tt][t] = mma_plane<!RAW>(ak[tt][s], sb[s][t], s ? X[tt][t] : f32x4{0.f, 0.f, 0.f, 0.f});
+            X[tt][t] = mma_plane<!RAW>(ak[tt][s], sb[s][t], s ? X[tt][t] : zero);
         }
       }
-    }
     Split ac[NKT];
     f32x4 gf[2], be[2];
 #pragma unroll
@@ -359,7 +367,7 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
       if constexpr (RAW) gf[tt] = St::factor(cur, St::A_G, tt, lane);
-      if constexpr (DELTA && SAVE) be[tt] = St::factor(cur, St::A_BETA, tt, lane);
+      if constexpr (DELTA && !OUT) be[tt] = St::factor(cur, St::A_BETA, tt, lane);
     }
     if constexpr (DELTA) {
       Split rb[NT];
@@ -372,19 +380,21 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) U[tt][t] = mma3(an[tt], rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
+        for (int t = 0; t < NT; ++t) U[tt][t] = mma3(an[tt], rb[t], zero);
     }
-    if constexpr (SAVE) save_tiles(U, blk + w.e(), k.v0 / 16 + ct0, lane);
-    if constexpr (DELTA && SAVE) {
+    if constexpr (!OUT) {
+      save_tiles(U, block(c) + w.e(), k.v0 / 16 + ct0, lane);
+      if constexpr (DELTA) {
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
+        for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) U[tt][t] *= be[tt];
+          for (int t = 0; t < NT; ++t) U[tt][t] *= be[tt];
+      }
     }
     Split ub[NT], gb[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      if constexpr (!SAVE || !RAW) ub[t] = tokens_operand<NT>(U, t);
+      if constexpr (OUT || !RAW) ub[t] = tokens_operand<NT>(U, t);
       if constexpr (RAW) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) U[tt][t] *= gf[tt];
@@ -401,26 +411,32 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
       for (int t = 0; t < NT; ++t) S[f][t] = mma_plane<!RAW>(ac[f], gb[t], S[f][t] * d);
     }
     __syncthreads();
-    if constexpr (!SAVE) {
+    if constexpr (OUT) {
       f32x4 O[2][NT], fo[2];
       Split ap[2];
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         fo[tt] = ff[tt];
-        ap[tt] = square_at(cur + St::A_P, tt, lane);
+        ap[tt] = square_at<St::BRIEF ? 0 : -St::SQ>(cur + St::A_P, tt, lane);
 #pragma unroll
         for (int s = 0; s < NKS; ++s) {
-          const Split aq = St::rows(cur, St::A_Q, St::A_QH, tt, s, lane);
+          const Split aq = St::template rows<St::BRIEF ? 0 : -St::HALF>(cur, St::A_Q, St::A_QH, tt, s, lane);
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
-            O[tt][t] = mma_plane<!RAW>(aq, sb[s][t], s ? O[tt][t] : f32x4{0.f, 0.f, 0.f, 0.f});
+          for (int t = 0; t < NT; ++t) {
+            if constexpr (St::BRIEF) O[tt][t] = mma(aq.hi, sb[s][t].hi, s ? O[tt][t] : zero);
+            else O[tt][t] = mma_plane<!RAW>(aq, sb[s][t], s ? O[tt][t] : zero);
+          }
         }
       }
       ahead(nxt);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) O[tt][t] = mma3(ap[tt], ub[t], RAW ? O[tt][t] * fo[tt] : O[tt][t]);
+        for (int t = 0; t < NT; ++t) {
+          if constexpr (RAW) O[tt][t] *= fo[tt];
+          if constexpr (St::BRIEF) O[tt][t] = mma(ap[tt].hi, ub[t].hi, O[tt][t]);
+          else O[tt][t] = mma3(ap[tt], ub[t], O[tt][t]);
+        }
       St::results(cur, O, ct0,
                   static_cast<TIN*>(p.o) + int64_t(k.row(c)) * row_stride + int64_t(k.h) * p.dv +
                       k.v0 + 16 * ct0,
@@ -428,151 +444,170 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
     } else {
       ahead(nxt);
     }
+  };
+
+  if (k.c0 < k.c1) fetch(k.c0);
+  read_state(S, p.S_in, p, state_at, lane);
+  if (k.c0 < k.c1) {
+    st.store(lds[0], k.count(k.c0), tid);
+    fetch(k.c0 + 1);
+    __syncthreads();
+    ahead(lds[0]);
+    // Two chunks a round while both buffers are within an LDS instruction's offset (64 KiB):
+    // their addresses are then the same registers.
+    if constexpr (OUT && sizeof(lds) <= 65536) {
+      for (int c = k.c0;;) {
+        chunk(c, lds[0], lds[1]);
+        if (++c == k.c1) break;
+        chunk(c, lds[1], lds[0]);
+        if (++c == k.c1) break;
+      }
+    } else {
+      for (int c = k.c0; c < k.c1; ++c) chunk(c, lds[(c - k.c0) & 1], lds[(c - k.c0 + 1) & 1]);
+    }
   }
-  if constexpr (!SAVE) write_state(S, p.S_out, p.state_bf16, p.dv, state_at, lane);
+  if constexpr (OUT) write_state(S, p.S_out, p.state_bf16, p.dv, state_at, lane);
 }
 
 // Backward over the chunks, last to first, with D the gradient of the state after a chunk:
 //   dU = P^T dO + Kb D      Z = M^T dU,  Y = beta Z   (no delta rule: Y = dU)
 //   dV = Y                  D <- e^{l_T} D + Qh^T dO - Kh^T Y
+// LDS as in the forward pass.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
 __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
-  using St = Stage<DK, NT, NW, RAW, DELTA, true, TIN>;
+  using St = Stage<DK, NT, NW, RAW, DELTA, PASS_BACK, TIN>;
   constexpr int NKT = DK / 16, NKS = DK / 32;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[St::BYTES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][St::BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15;
   Walk k;
   if (!start_walk<St::VC>(p, k)) return;
   const WsLayout w{DK, p.dv, RAW, true};
   const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;
   const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
-  const int64_t row_stride = int64_t(p.H) * p.dv, step = int64_t(p.H) * w.block();
+  const int64_t row_stride = int64_t(p.H) * p.dv;
   const TIN* vals = static_cast<const TIN*>(p.d_o) + int64_t(k.h) * p.dv + k.v0;
-  unsigned char* blk = p.ws + (int64_t(k.c1 - 1) * p.H + k.h) * w.block();
-  k.first += CT * (k.c1 - 1 - k.c0);
-
   St st;
-  if (k.c0 < k.c1) st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
-  f32x4 D[NKT][NT];
-  read_state(D, p.dS_out, p, state_at, lane);
+  auto block = [&](int c) { return p.ws + (int64_t(c) * p.H + k.h) * w.block(); };
+  auto fetch = [&](int c) {
+    c = max(c, k.c0);
+    st.load(p, block(c), k.row(c), k.count(c), k.h, vals, tid);
+  };
 
-  for (int c = k.c1 - 1; c >= k.c0; --c) {
-    const int first = k.first, count = min(CT, k.end - first);
-    unsigned char* cur = blk;
-    __syncthreads();
-    st.store(lds, count, tid);
-    __syncthreads();
-    if (c > k.c0) {
-      k.first -= CT;
-      blk -= step;
-    }
-    st.load(p, blk, k.first, min(CT, k.end - k.first), k.h, vals, tid);
-    issued<NW>();
-
-    f32x4 G[2][NT], Y[2][NT];
-    Split ar[2][NKS], apt[2];
-    f32x4 gf[2], ff[2];
+  f32x4 G[2][NT], D[NKT][NT];
+  Split ar[2][NKS], apt[2];
+  auto ahead = [&](const unsigned char* l) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
 #pragma unroll
-      for (int s = 0; s < NKS; ++s) ar[tt][s] = St::rows(lds, St::A_K, St::A_KB, tt, s, lane);
+      for (int t = 0; t < NT; ++t) G[tt][t] = St::values(l, tt, ct0 + t, lane);    // dO
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        G[tt][t] = St::values(lds, tt, ct0 + t, lane);         // dO
-        Y[tt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-      apt[tt] = square_at(lds + St::A_PT, tt, lane);
+      for (int s = 0; s < NKS; ++s) ar[tt][s] = St::rows(l, St::A_K, St::A_KB, tt, s, lane);
+      apt[tt] = square_at(l + St::A_PT, tt, lane);
+    }
+  };
+  auto chunk = [&](int c, unsigned char* cur, unsigned char* nxt) __attribute__((always_inline)) {
+    __syncthreads();
+    st.store(nxt, k.count(max(c - 1, k.c0)), tid);
+    fetch(c - 2);
+    save_tiles(D, block(c) + w.ds(), k.v0 / 16 + ct0, lane);
+
+    f32x4 Y[2][NT], gf[2], ff[2], be[2];
+    Split ac[NKT], amt[2];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
       if constexpr (RAW) {
-        gf[tt] = St::factor(lds, St::A_G, tt, lane);
-        ff[tt] = St::factor(lds, St::A_F, tt, lane);
+        gf[tt] = St::factor(cur, St::A_G, tt, lane);
+        ff[tt] = St::factor(cur, St::A_F, tt, lane);
+      }
+      if constexpr (DELTA) {
+        be[tt] = St::factor(cur, St::A_BETA, tt, lane);
+        amt[tt] = square_at(cur + St::A_MT, tt, lane);
       }
     }
-    issued<NW>();
-    save_tiles(D, cur + w.ds(), k.v0 / 16 + ct0, lane);
     // dU
 #pragma unroll
-    for (int s = 0; s < NKS; ++s) {
-      Split sb[NT];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) sb[t] = state_operand<NKT, NT>(D, s, t);
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) Y[tt][t] = mma_plane<!RAW>(ar[tt][s], sb[t], Y[tt][t]);
-    }
-    issued<NW>();
-    Split ac[NKT];
-#pragma unroll
-    for (int f = 0; f < NKT; ++f) ac[f] = St::cols(lds, St::A_Q, St::A_QH, f, lane);
-    issued<NW>();
-    Split gb[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) gb[t] = tokens_operand<NT>(G, t);
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        Y[tt][t] = mma3(apt[tt], gb[t], RAW ? Y[tt][t] * gf[tt] : Y[tt][t]);
-    // D's share of the outputs needs nothing of Y
-    if constexpr (RAW) {
+    for (int s = 0; s < NKS; ++s)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
+        const Split sb = state_operand<NKT, NT>(D, s, t);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) Y[tt][t] = mma_plane<!RAW>(ar[tt][s], sb, s ? Y[tt][t] : zero);
+      }
+#pragma unroll
+    for (int f = 0; f < NKT; ++f)
+      ac[f] = St::template cols<-St::HALF>(cur, St::A_Q, St::A_QH, f, lane);
+    Split gb[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      gb[t] = tokens_operand<NT>(G, t);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+        Y[tt][t] = mma3(apt[tt], gb[t], RAW ? Y[tt][t] * gf[tt] : Y[tt][t]);
+      if constexpr (RAW) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) G[tt][t] *= ff[tt];
         gb[t] = tokens_operand<NT>(G, t);
       }
     }
+    // the outputs' share of D needs nothing of Y
 #pragma unroll
     for (int f = 0; f < NKT; ++f) {
-      const f32x4 d = St::decay(lds, f, lane);
+      const f32x4 d = St::decay(cur, f, lane);
 #pragma unroll
       for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(ac[f], gb[t], D[f][t] * d);
     }
     if constexpr (DELTA) {
-      issued<NW>();
-      Split amt[2];
-      f32x4 be[2];
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        amt[tt] = square_at(lds + St::A_MT, tt, lane);
-        be[tt] = St::factor(lds, St::A_BETA, tt, lane);
-      }
-#pragma unroll
-      for (int f = 0; f < NKT; ++f) ac[f] = St::cols(lds, St::A_K, St::A_KH, f, lane);
-      issued<NW>();
       Split rb[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) rb[t] = tokens_operand<NT>(Y, t);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          Y[tt][t] = mma3(amt[tt], rb[t], f32x4{0.f, 0.f, 0.f, 0.f});
-        }
-      save_tiles(Y, cur + w.z(), k.v0 / 16 + ct0, lane);
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) Y[tt][t] *= be[tt];
-      Split yb[NT];
+        for (int t = 0; t < NT; ++t) Y[tt][t] = mma3(amt[tt], rb[t], zero);
+    }
+    save_tiles(Y, block(c) + w.z(), k.v0 / 16 + ct0, lane);
+    if constexpr (DELTA) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         f32x4 m[2][1];
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) m[tt][0] = RAW ? -Y[tt][t] * ff[tt] : -Y[tt][t];
-        yb[t] = tokens_operand<1>(m, 0);
+        for (int tt = 0; tt < 2; ++tt) {
+          Y[tt][t] *= be[tt];
+          m[tt][0] = RAW ? -Y[tt][t] * ff[tt] : -Y[tt][t];
+        }
+        const Split yb = tokens_operand<1>(m, 0);
+#pragma unroll
+        for (int f = 0; f < NKT; ++f)
+          D[f][t] = mma_plane<!RAW>(St::cols(cur, St::A_K, St::A_KH, f, lane), yb, D[f][t]);
       }
-#pragma unroll
-      for (int f = 0; f < NKT; ++f)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(ac[f], yb[t], D[f][t]);
-    } else {
-      save_tiles(Y, cur + w.z(), k.v0 / 16 + ct0, lane);
     }
-    St::results(lds, Y, ct0,
-                static_cast<TIN*>(p.dv_) + int64_t(first) * row_stride + int64_t(k.h) * p.dv + k.v0 +
-                    16 * ct0,
-                row_stride, count, lane);
+    __syncthreads();
+    ahead(nxt);
+    St::results(cur, Y, ct0,
+                static_cast<TIN*>(p.dv_) + int64_t(k.row(c)) * row_stride + int64_t(k.h) * p.dv +
+                    k.v0 + 16 * ct0,
+                row_stride, k.count(c), lane);
+  };
+
+  if (k.c0 < k.c1) fetch(k.c1 - 1);
+  read_state(D, p.dS_out, p, state_at, lane);
+  if (k.c0 < k.c1) {
+    st.store(lds[0], k.count(k.c1 - 1), tid);
+    fetch(k.c1 - 2);
+    __syncthreads();
+    ahead(lds[0]);
+    if constexpr (sizeof(lds) <= 65536) {
+      for (int c = k.c1 - 1;;) {
+        chunk(c, lds[0], lds[1]);
+        if (--c < k.c0) break;
+        chunk(c, lds[1], lds[0]);
+        if (--c < k.c0) break;
+      }
+    } else {
+      for (int c = k.c1 - 1; c >= k.c0; --c)
+        chunk(c, lds[(k.c1 - 1 - c) & 1], lds[(k.c1 - c) & 1]);
+    }
   }
   if (p.S_out) write_state(D, p.S_out, p.state_bf16, p.dv, state_at, lane);
 }
