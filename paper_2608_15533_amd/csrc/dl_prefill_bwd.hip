@@ -23,11 +23,13 @@ hipError_t launch_grad(const SeqParams& p, hipStream_t s) {
 template <int DK, bool RAW, bool DELTA, typename TIN>
 hipError_t launch_scan(const SeqParams& p, hipStream_t s) {
   const int64_t heads = int64_t(p.n) * p.H;
-  if (wide_walk(heads, p.dv)) {
-    if (p.dv == 128) return start(&backward_kernel<DK, 1, 8, RAW, DELTA, TIN>, heads, 512, p, s);
-    return start(&backward_kernel<DK, 1, 4, RAW, DELTA, TIN>, heads, 256, p, s);
+  const int waves = walk_waves(heads, p.dv, RAW);
+  const int64_t grid = heads * (p.dv / 16 / waves);
+  switch (waves) {
+    case 2: return start(&backward_kernel<DK, 1, 2, RAW, DELTA, TIN>, grid, 128, p, s);
+    case 4: return start(&backward_kernel<DK, 1, 4, RAW, DELTA, TIN>, grid, 256, p, s);
+    default: return start(&backward_kernel<DK, 1, 8, RAW, DELTA, TIN>, grid, 512, p, s);
   }
-  return start(&backward_kernel<DK, 1, 2, RAW, DELTA, TIN>, heads * (p.dv / 32), 128, p, s);
 }
 
 template <int DK, typename TIN>

@@ -59,9 +59,11 @@ __device__ __forceinline__ Split split8(const float* x) {
 
 // acc += a b over 32 terms.  Lane l holds of the 16x16 result rows 4(l/16)+r, column l%16;
 // of a row l%16, of b column l%16, and of both the same eight terms: which eight is free as
-// long as a and b agree.  Natural order: terms 8(l/16)+e.  State order: terms
-// 16(e/4)+4(l/16)+e%4, which makes two 16x16 results of an earlier product, side by side, an
-// operand without any exchange between lanes.
+// long as a and b agree.  With the terms chosen as a lane's own rows of two 16x16 results side
+// by side, those results are an operand of the next product without any exchange between lanes.
+// Terms that are tokens: 16(e/4)+4(l/16)+e%4, results' rows being tokens in their order ("state
+// order").  Terms that are keys: 8(l/16)+e, in their order, with row 4g+r of result f standing
+// for key state_key(f, g, r).
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 acc) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
 }
@@ -69,6 +71,9 @@ __device__ __forceinline__ f32x4 mma3(const Split& a, const Split& b, f32x4 acc)
   acc = mma(a.lo, b.hi, acc);
   acc = mma(a.hi, b.lo, acc);
   return mma(a.hi, b.hi, acc);
+}
+__host__ __device__ constexpr int state_key(int f, int g, int r) {
+  return 32 * (f >> 1) + 8 * g + 4 * (f & 1) + r;
 }
 __device__ __forceinline__ int state_term(int lane, int e) {
   return 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3);
@@ -100,11 +105,15 @@ __device__ __forceinline__ void store_state(void* S, bool bf16, int64_t i, float
 
 // ------------------------------------------------------------------ operands in LDS
 // A token x key plane: 32 rows of 16-byte pieces (8 bf16), piece x of row r at
-// piece_at(r, x).  The exchange of pieces within a row spreads the 16 rows that an operand
-// read touches over all banks.  NP: pieces in a row.
+// piece_at(r, x).  The exchange of pieces within a row lets 16 rows of one piece (an operand
+// over keys) and four pieces of four rows (one over tokens) each lie in different banks.
+// NP: pieces in a row.
 template <int NP>
 __host__ __device__ constexpr int piece_swap(int r) {
-  return NP >= 16 ? (r & 15) : NP == 8 ? ((r >> 1) & 7) : NP == 4 ? ((r >> 1) & 2) : 0;
+  return NP >= 16  ? ((r & 3) << 2) | ((r >> 2) & 3)
+         : NP == 8 ? ((r & 2) << 1) | ((r >> 2) & 3)
+         : NP == 4 ? (r >> 1) & 2
+                   : 0;
 }
 template <int NP>
 __host__ __device__ constexpr int piece_at(int r, int x) {
@@ -117,30 +126,24 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 __device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
-// Four rows of one column: of each 16 lanes, lane i gives the address of 8 bytes of row i/4
-// (columns 4(i%4)..) and receives column i of the four rows.
+// Four rows of one column: of each 16 lanes, lane i gives the address of four columns of row
+// i/4, the (i%4)-th such four, and receives column i of the four rows.
 __device__ __forceinline__ bf16x4 read_column(const unsigned char* lds) {
   typedef __attribute__((address_space(3))) s16x4 lds_t;
   return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)lds));
 }
 
-// Tokens 16 tt + l%16, terms: keys 32 s + (state order).
+// Tokens 16 tt + l%16, terms: keys 32 s + 8 (l/16) + e.
 template <int NP>
 __device__ __forceinline__ bf16x8 rows_operand(const unsigned char* plane, int tt, int s, int lane) {
-  const int r = 16 * tt + (lane & 15), g = lane >> 4;
-  const unsigned char* at = plane + 8 * (g & 1);
-  const bf16x4 a = *reinterpret_cast<const bf16x4*>(at + 16 * piece_at<NP>(r, 4 * s + (g >> 1)));
-  const bf16x4 b = *reinterpret_cast<const bf16x4*>(at + 16 * piece_at<NP>(r, 4 * s + 2 + (g >> 1)));
-  return join(a, b);
+  return *reinterpret_cast<const bf16x8*>(plane + 16 * piece_at<NP>(16 * tt + (lane & 15), 4 * s + (lane >> 4)));
 }
-// Keys 16 f + l%16, terms: the chunk's tokens (state order).
+// Keys state_key(f, ., .) in the place of l%16, terms: the chunk's tokens (state order).
 template <int NP>
 __device__ __forceinline__ bf16x8 cols_operand(const unsigned char* plane, int f, int lane) {
-  const int i = lane & 15, r = 4 * (lane >> 4) + (i >> 2);
-  const unsigned char* at = plane + 8 * (i & 1);
-  const bf16x4 a = read_column(at + 16 * piece_at<NP>(r, 2 * f + ((i >> 1) & 1)));
-  const bf16x4 b = read_column(at + 16 * piece_at<NP>(r + 16, 2 * f + ((i >> 1) & 1)));
-  return join(a, b);
+  const int i = lane & 15, r = 4 * (lane >> 4) + (i >> 2), x = 4 * (f >> 1) + (i & 3);
+  const unsigned char* at = plane + 8 * (f & 1);
+  return join(read_column(at + 16 * piece_at<NP>(r, x)), read_column(at + 16 * piece_at<NP>(r + 16, x)));
 }
 
 // ------------------------------------------------------------------ workspace
@@ -198,8 +201,14 @@ struct SeqParams {
   bool delta, state_bf16, bwd, raw;
 };
 
-// Whether a workgroup walks whole heads with 32 columns a wave, or 32 columns with 16 a wave.
-inline bool wide_walk(int64_t heads, int dv) { return heads * (dv / 32) >= 1024; }
+// Waves of a workgroup that walks chunks, 16 value columns each.  While there are few waves for
+// the 256 CUs, few to a workgroup spread them (a wave alone on its SIMD is at its fastest);
+// where planes from the workspace fill a CU's LDS with one workgroup, four as soon as two would
+// leave workgroups waiting; with more waves than that, whole heads, which share the operands.
+inline int walk_waves(int64_t heads, int dv, bool raw) {
+  const int64_t waves = heads * (dv / 16);
+  return waves <= 512 || (raw && waves <= 1024) ? 2 : waves <= 1024 ? 4 : dv / 16;
+}
 
 struct ChunkRow {
   int seq, first, count, slot;

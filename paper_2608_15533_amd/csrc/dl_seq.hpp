@@ -225,13 +225,13 @@ struct Stage {
     if constexpr (!RAW && LO != 0) o.lo = cols_operand<NP>(lds + at + LO, f, lane);
     return o;
   }
-  // e^{l_T} for keys 16 f + 4 g + r
+  // e^{l_T} for keys state_key(f, g, r)
   static __device__ __forceinline__ f32x4 decay(const unsigned char* lds, int f, int lane) {
     if constexpr (RAW) {
       const float d = *reinterpret_cast<const float*>(lds + A_F + 4 * (CT - 1));
       return f32x4{d, d, d, d};
     } else {
-      return *reinterpret_cast<const f32x4*>(lds + A_DEC + 4 * (16 * f + 4 * (lane >> 4)));
+      return *reinterpret_cast<const f32x4*>(lds + A_DEC + 4 * state_key(f, lane >> 4, 0));
     }
   }
 };
@@ -268,7 +268,7 @@ __device__ __forceinline__ void read_state(f32x4 (&S)[NKT][NT], const void* base
 #pragma unroll
       for (int t = 0; t < NT; ++t)
         S[f][t][r] = base ? load_state(base, p.state_bf16,
-                                       at + int64_t(16 * f + 4 * (lane >> 4) + r) * p.dv + 16 * t)
+                                       at + int64_t(state_key(f, lane >> 4, r)) * p.dv + 16 * t)
                           : 0.f;
 }
 template <int NKT, int NT>
@@ -280,21 +280,22 @@ __device__ __forceinline__ void write_state(const f32x4 (&S)[NKT][NT], void* bas
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int t = 0; t < NT; ++t)
-        store_state(base, bf16, at + int64_t(16 * f + 4 * (lane >> 4) + r) * dv + 16 * t, S[f][t][r]);
+        store_state(base, bf16, at + int64_t(state_key(f, lane >> 4, r)) * dv + 16 * t, S[f][t][r]);
 }
 
-// Results into the workspace, [column tile][row][16] (rows: keys, or tokens).
-template <int NR, int NT>
+// Results into the workspace, [column tile][row][16]; rows: KEYS (of a state), or tokens.
+template <bool KEYS, int NR, int NT>
 __device__ __forceinline__ void save_tiles(const f32x4 (&x)[NR][NT], unsigned char* base, int tile,
                                            int lane) {
   float* at = reinterpret_cast<float*>(base) + tile * NR * 256;
-  const uint32_t o = 64 * (lane >> 4) + (lane & 15);
+  const uint32_t o = (KEYS ? 128 : 64) * (lane >> 4) + (lane & 15);
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int f = 0; f < NR; ++f)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) at[o + (t * NR + f) * 256 + 16 * r] = x[f][t][r];
+      for (int r = 0; r < 4; ++r)
+        at[o + t * NR * 256 + 16 * (KEYS ? state_key(f, 0, r) : 16 * f + r)] = x[f][t][r];
 }
 
 // PASS_OUT writes outputs and final states; PASS_SAVE the states before each chunk and E, for
@@ -344,7 +345,7 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
     __syncthreads();
     st.store(nxt, k.count(min(c + 1, k.c1 - 1)), tid);
     fetch(c + 2);
-    if constexpr (!OUT) save_tiles(S, block(c) + w.s0(), k.v0 / 16 + ct0, lane);
+    if constexpr (!OUT) save_tiles<true>(S, block(c) + w.s0(), k.v0 / 16 + ct0, lane);
 
     // Kh S, R = V - Kh S, E = N R (PASS_OUT: N holds beta N, and U comes at once)
     Split sb[NKS][NT];
@@ -383,7 +384,7 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
         for (int t = 0; t < NT; ++t) U[tt][t] = mma3(an[tt], rb[t], zero);
     }
     if constexpr (!OUT) {
-      save_tiles(U, block(c) + w.e(), k.v0 / 16 + ct0, lane);
+      save_tiles<false>(U, block(c) + w.e(), k.v0 / 16 + ct0, lane);
       if constexpr (DELTA) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
@@ -495,7 +496,7 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
   };
 
   f32x4 G[2][NT], D[NKT][NT];
-  Split ar[2][NKS], apt[2];
+  Split ar[2][NKS];
   auto ahead = [&](const unsigned char* l) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
@@ -503,19 +504,19 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
       for (int t = 0; t < NT; ++t) G[tt][t] = St::values(l, tt, ct0 + t, lane);    // dO
 #pragma unroll
       for (int s = 0; s < NKS; ++s) ar[tt][s] = St::rows(l, St::A_K, St::A_KB, tt, s, lane);
-      apt[tt] = square_at(l + St::A_PT, tt, lane);
     }
   };
   auto chunk = [&](int c, unsigned char* cur, unsigned char* nxt) __attribute__((always_inline)) {
     __syncthreads();
     st.store(nxt, k.count(max(c - 1, k.c0)), tid);
     fetch(c - 2);
-    save_tiles(D, block(c) + w.ds(), k.v0 / 16 + ct0, lane);
+    save_tiles<true>(D, block(c) + w.ds(), k.v0 / 16 + ct0, lane);
 
     f32x4 Y[2][NT], gf[2], ff[2], be[2];
-    Split ac[NKT], amt[2];
+    Split ac[NKT], amt[2], apt[2];
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
+      apt[tt] = square_at(cur + St::A_PT, tt, lane);
       if constexpr (RAW) {
         gf[tt] = St::factor(cur, St::A_G, tt, lane);
         ff[tt] = St::factor(cur, St::A_F, tt, lane);
@@ -566,7 +567,7 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) Y[tt][t] = mma3(amt[tt], rb[t], zero);
     }
-    save_tiles(Y, block(c) + w.z(), k.v0 / 16 + ct0, lane);
+    save_tiles<false>(Y, block(c) + w.z(), k.v0 / 16 + ct0, lane);
     if constexpr (DELTA) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
