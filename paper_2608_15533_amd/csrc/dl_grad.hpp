@@ -39,7 +39,7 @@ __device__ __forceinline__ void lane_tokens(const float (*m)[LD], int f, int lan
 
 // A token x token matrix (or its transpose) as an operand over tokens.
 template <bool TR>
-__device__ __forceinline__ Split square_operand(const float (*m)[CT + 1], int tt, int lane) {
+__device__ __forceinline__ Split square_operand(const float (*m)[SL], int tt, int lane) {
   float a[8];
   const int i = 16 * tt + (lane & 15);
 #pragma unroll
@@ -69,7 +69,8 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
   constexpr int KT = DK / 64;                  // key tiles of a wave
   constexpr bool LO = sizeof(TIN) == 4;        // dO has a second half
   __shared__ ChunkIn<DC, DK, TIN> in;
-  __shared__ float dP[CT][CT + 1], dG[CT][CT + 1], tok_sum[4][CT + 1];
+  __shared__ __attribute__((aligned(16))) float dP[CT][SL], dG[CT][SL];
+  __shared__ float tok_sum[4][CT + 1];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int c16 = lane & 15, g = lane >> 4;
   const int h = blockIdx.x % p.H, c = blockIdx.x / p.H;

@@ -15,20 +15,24 @@ hipError_t start(K* kernel, int64_t grid, int block, const SeqParams& p, hipStre
                          args, 0, s);
 }
 
+template <int DK, bool BWD, typename TIN>
+hipError_t launch_prep_pass(int op, const SeqParams& p, hipStream_t s) {
+  const int64_t grid = int64_t(p.max_chunks) * p.H;
+  if (p.raw) return start(&raw_prep_kernel<DK, BWD>, grid, 64, p, s);   // bf16, head-wise decay
+  if (op == DL_OP_RWKV6) return start(&prep_kernel<DC_BONUS, DK, BWD, TIN>, grid, 256, p, s);
+  if (op == DL_OP_KDA || op == DL_OP_GLA) return start(&prep_kernel<DC_KEY, DK, BWD, TIN>, grid, 256, p, s);
+  if constexpr (sizeof(TIN) == 4) return start(&prep_kernel<DC_SCALAR, DK, BWD, TIN>, grid, 256, p, s);
+  return hipErrorInvalidValue;
+}
 template <int DK, typename TIN>
 hipError_t launch_prep(int op, const SeqParams& p, hipStream_t s) {
-  const int64_t grid = int64_t(p.max_chunks) * p.H;
-  if (p.raw) return start(&raw_prep_kernel<DK>, grid, 64, p, s);   // bf16, head-wise decay
-  if (op == DL_OP_RWKV6) return start(&prep_kernel<DC_BONUS, DK, TIN>, grid, 256, p, s);
-  if (op == DL_OP_KDA || op == DL_OP_GLA) return start(&prep_kernel<DC_KEY, DK, TIN>, grid, 256, p, s);
-  if constexpr (sizeof(TIN) == 4) return start(&prep_kernel<DC_SCALAR, DK, TIN>, grid, 256, p, s);
-  return hipErrorInvalidValue;
+  return p.bwd ? launch_prep_pass<DK, true, TIN>(op, p, s) : launch_prep_pass<DK, false, TIN>(op, p, s);
 }
 
 template <int DK, bool RAW, bool DELTA, int PASS, typename TIN>
 hipError_t launch_walk(const SeqParams& p, hipStream_t s) {
   const int64_t heads = int64_t(p.n) * p.H;
-  const int waves = walk_waves(heads, p.dv, RAW);
+  const int waves = walk_waves(heads, DK, p.dv, RAW);
   const int64_t grid = heads * (p.dv / 16 / waves);
   switch (waves) {
     case 2: return start(&forward_kernel<DK, 1, 2, RAW, DELTA, PASS, TIN>, grid, 128, p, s);

@@ -23,7 +23,7 @@ hipError_t launch_grad(const SeqParams& p, hipStream_t s) {
 template <int DK, bool RAW, bool DELTA, typename TIN>
 hipError_t launch_scan(const SeqParams& p, hipStream_t s) {
   const int64_t heads = int64_t(p.n) * p.H;
-  const int waves = walk_waves(heads, p.dv, RAW);
+  const int waves = walk_waves(heads, DK, p.dv, RAW);
   const int64_t grid = heads * (p.dv / 16 / waves);
   switch (waves) {
     case 2: return start(&backward_kernel<DK, 1, 2, RAW, DELTA, TIN>, grid, 128, p, s);

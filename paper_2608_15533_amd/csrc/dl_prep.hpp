@@ -7,6 +7,8 @@
 namespace dl {
 
 // One log-decay per head (or none) | per key | per key, read before the token (RWKV6).
+constexpr int SL = CT + 4;             // row of a token x token matrix in LDS (16-byte rows)
+
 enum DecayClass { DC_SCALAR = 0, DC_KEY = 1, DC_BONUS = 2 };
 
 constexpr float LOG2E = 1.44269504088896341f;
@@ -142,9 +144,11 @@ struct ChunkIn {
 };
 
 // G (strictly lower) and P (lower; RWKV6: strictly, and its bonus on the diagonal), by three
-// of the workgroup's waves; by all of them, pair by pair, where a block decays too far.
+// of the workgroup's waves; by all of them, pair by pair, where a block decays too far.  On
+// fp32 MFMA: the operands are used once, so splitting them (24 instructions for eight values)
+// would cost more than the matrix cores' slower fp32 rate, which nothing else here waits for.
 template <int DC, int DK, typename TIN>
-__device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[CT + 1], float (*P)[CT + 1],
+__device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[SL], float (*P)[SL],
                               float* diag, const SeqParams& p, int h, int tid) {
   const int lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
   if constexpr (DC == DC_BONUS) {
@@ -171,7 +175,9 @@ __device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[CT + 1]
     const int bi = wave == 0 ? 0 : 1, bj = wave == 1 ? 1 : 0;   // (0,0), (1,1), (1,0)
     const int ref = wave == 0 ? 7 : wave == 1 ? 23 : 15;
     const int i = 16 * bi + c16, j = 16 * bj + c16;
-    f32x4 ag = {0.f, 0.f, 0.f, 0.f}, ap = ag;
+    f32x4 ag[2], ap[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) ag[x] = ap[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < DK / 32; ++s) {
       const int r = 32 * s + 8 * g;
@@ -187,20 +193,27 @@ __device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[CT + 1]
         if (DC == DC_BONUS) in.at_q8(i, r, lq);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float f = exp2_of(li[e] - m[e]);
-          ak[e] *= f;
-          aq[e] *= DC == DC_BONUS ? exp2_of(lq[e] - m[e]) : f;
+          if (DC == DC_BONUS) {
+            aq[e] *= exp2_of(lq[e] - m[e]);
+          } else {
+            const float f = exp2_of(li[e] - m[e]);
+            aq[e] *= f;
+            ak[e] *= f;
+          }
           b[e] *= exp2_of(m[e] - lj[e]);
         }
       }
-      const Split sb = split8(b);
-      if (p.delta) ag = mma3(split8(ak), sb, ag);
-      ap = mma3(split8(aq), sb, ap);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (DC != DC_BONUS && p.delta)
+          ag[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(ak[e], b[e], ag[e & 1], 0, 0, 0);
+        ap[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(aq[e], b[e], ap[e & 1], 0, 0, 0);
+      }
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int ri = 16 * bi + 4 * g + r;
-      float x = ap[r], y = ag[r];
+      float x = ap[0][r] + ap[1][r], y = ag[0][r] + ag[1][r];
       if constexpr (DC == DC_SCALAR) {
         const float f = exp2_of(fminf(in.l[ri][0] - in.l[j][0], 0.f));
         x *= f;
@@ -231,83 +244,95 @@ __device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[CT + 1]
   __syncthreads();
 }
 
-// N = (I + G beta)^-1 over G, and M = (I + beta G)^-1, by one wave.  The two diagonal 16 x 16
-// blocks of each by forward substitution, a column per lane (G's row is read before N's takes
-// its place); then the lower left block, N21 = -N22 (G21 beta) N11 and M21 = -M22 (beta G21)
-// M11, by fp32 MFMA: 120 dependent steps instead of 496.
-__device__ __forceinline__ void solve(float (*G)[CT + 1], float (*M)[CT + 1], const float* beta,
-                                      int lane) {
+// N = (I + G beta)^-1 over G, and (BWD) M = (I + beta G)^-1, by one wave.  The two diagonal
+// 16 x 16 blocks of each by forward substitution, a column per lane in registers; then the
+// lower left block, N21 = -N22 (G21 beta) N11 and M21 = -M22 (beta G21) M11, by fp32 MFMA:
+// 120 multiplications a lane instead of 496.
+template <bool BWD>
+__device__ __forceinline__ void solve(float (*G)[SL], float (*M)[SL], const float* beta, int lane) {
   const int c16 = lane & 15, g = lane >> 4, o = lane & 16;
-  const bool second = lane >= 32;
-  float y[16];
+  const bool second = BWD && lane >= 32;
+  float x[16], y[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    float s0 = 0.f, s1 = 0.f;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int m = 0; m < i; ++m) {
-      if (m & 1) s1 += G[o + i][o + m] * y[m];
-      else s0 += G[o + i][o + m] * y[m];
+    for (int m = 0; m < i; m += 4) {
+      const f32x4 row = *reinterpret_cast<const f32x4*>(&G[o + i][o + m]);   // 0 from column i on
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (m + e < i) s[e] += row[e] * y[m + e];
     }
-    const float b = beta[o + i], s = s0 + s1, d = i == c16 ? 1.f : 0.f;
-    const float x = d - (second ? b * s : s);
-    y[i] = second ? x : b * x;
-    __builtin_amdgcn_wave_barrier();
-    if (second) {
-      M[o + i][o + c16] = x;
-      if (!o) M[i][16 + c16] = 0.f;
-    } else {
-      G[o + i][o + c16] = x;
-    }
-    __builtin_amdgcn_wave_barrier();
+    const float b = beta[o + i], t = (s[0] + s[1]) + (s[2] + s[3]), d = i == c16 ? 1.f : 0.f;
+    x[i] = d - (second ? b * t : t);
+    y[i] = second ? x[i] : b * x[i];
   }
+  float (*out)[SL] = second ? M : G;
+  if (BWD || lane < 32) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      out[o + i][o + c16] = x[i];
+      if (second && !o) M[i][16 + c16] = 0.f;
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
   f32x4 tn = {0.f, 0.f, 0.f, 0.f}, tm = tn;
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
     const float a = G[16 + c16][4 * s + g];
     tn = __builtin_amdgcn_mfma_f32_16x16x4f32(a * beta[4 * s + g], G[4 * s + g][c16], tn, 0, 0, 0);
-    tm = __builtin_amdgcn_mfma_f32_16x16x4f32(a * beta[16 + c16], M[4 * s + g][c16], tm, 0, 0, 0);
+    if (BWD) tm = __builtin_amdgcn_mfma_f32_16x16x4f32(a * beta[16 + c16], M[4 * s + g][c16], tm, 0, 0, 0);
   }
   f32x4 rn = {0.f, 0.f, 0.f, 0.f}, rm = rn;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     rn = __builtin_amdgcn_mfma_f32_16x16x4f32(G[16 + c16][16 + 4 * g + r], tn[r], rn, 0, 0, 0);
-    rm = __builtin_amdgcn_mfma_f32_16x16x4f32(M[16 + c16][16 + 4 * g + r], tm[r], rm, 0, 0, 0);
+    if (BWD) rm = __builtin_amdgcn_mfma_f32_16x16x4f32(M[16 + c16][16 + 4 * g + r], tm[r], rm, 0, 0, 0);
   }
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     G[16 + 4 * g + r][c16] = -rn[r];
-    M[16 + 4 * g + r][c16] = -rm[r];
+    if (BWD) M[16 + 4 * g + r][c16] = -rm[r];
   }
 }
 
+// Eight values as two bf16 halves, or the first alone.
+template <bool LO = true>
 __device__ __forceinline__ void put(unsigned char* base, int half, int unit, const float* x) {
   const Split s = split8(x);
   *reinterpret_cast<bf16x8*>(base + 16 * unit) = s.hi;
-  *reinterpret_cast<bf16x8*>(base + half + 16 * unit) = s.lo;
+  if constexpr (LO) *reinterpret_cast<bf16x8*>(base + half + 16 * unit) = s.lo;
 }
 
-// The squares from LDS matrices, by NTH threads.
-template <int NTH>
-__device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& w, const SeqParams& p,
-                                            const float (*P)[CT + 1], const float (*N)[CT + 1],
-                                            const float (*M)[CT + 1], const float* beta, int tid) {
+// The squares from LDS matrices, by NTH threads.  BRIEF: P's second half is not wanted.
+template <int NTH, bool BWD, bool BRIEF>
+__device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& w, bool delta,
+                                            const float (*P)[SL], const float (*N)[SL],
+                                            const float (*M)[SL], const float* beta, int tid) {
+#pragma unroll
   for (int x = tid; x < CT * CT / 8; x += NTH) {
-    const int lane = x & 63, i = 16 * (x >> 6) + (lane & 15);
+    const int lane = x & 63, i = 16 * (x >> 6) + (lane & 15), t0 = 4 * (lane >> 4);
     float a[8];
+    auto row = [&](const float (*m)[SL], float f) {
+      const f32x4 u = *reinterpret_cast<const f32x4*>(&m[i][t0]);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(&m[i][16 + t0]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) a[e] = P[i][state_term(lane, e)];
-    put(blk + w.p(), -WsLayout::SQ, x, a);
-    if (p.delta) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) a[e] = N[i][state_term(lane, e)] * (p.bwd ? 1.f : beta[i]);
+      for (int e = 0; e < 4; ++e) { a[e] = f * u[e]; a[4 + e] = f * v[e]; }
+    };
+    if constexpr (!BWD) {
+      row(P, 1.f);
+      put<!BRIEF>(blk + w.p(), -WsLayout::SQ, x, a);
+    }
+    if (delta) {
+      row(N, BWD ? 1.f : beta[i]);
       put(blk + w.n(), WsLayout::SQ, x, a);
     }
-    if (p.bwd) {
+    if constexpr (BWD) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) a[e] = P[state_term(lane, e)][i];
       put(blk + w.pt(), WsLayout::SQ, x, a);
-      if (p.delta) {
+      if (delta) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] = M[state_term(lane, e)][i];
         put(blk + w.mt(), WsLayout::SQ, x, a);
@@ -316,21 +341,24 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
   }
 }
 
-template <int DC, int DK, typename TIN>
+// BWD: for the backward pass.
+template <int DC, int DK, bool BWD, typename TIN>
 __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
+  constexpr bool BRIEF = !BWD && sizeof(TIN) == 2;
   __shared__ ChunkIn<DC, DK, TIN> in;
-  __shared__ float G[CT][CT + 1], P[CT][CT + 1], M[CT][CT + 1], diag[CT];
+  __shared__ __attribute__((aligned(16))) float G[CT][SL], P[CT][SL], M[BWD ? CT : 1][SL];
+  __shared__ float diag[CT];
   const int tid = threadIdx.x;
   const int h = blockIdx.x % p.H, c = blockIdx.x / p.H;
   const ChunkRow row = chunk_row(p, c);
   if (row.count == 0) return;
-  const WsLayout w{DK, p.dv, false, p.bwd};
+  const WsLayout w{DK, p.dv, false, BWD};
   unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
 
   in.template load<256>(p, row, h, tid);
   pair_products<DC, DK, TIN>(in, G, P, diag, p, h, tid);
   // One wave solves while the others go on to the planes.
-  if (p.delta && tid < 64) solve(G, M, in.beta, tid);
+  if (p.delta && tid < 64) solve<BWD>(G, M, in.beta, tid);
 
   float* dec = reinterpret_cast<float*>(blk + w.dec());
   float* beta = reinterpret_cast<float*>(blk + w.beta());
@@ -353,25 +381,25 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
       k[e] *= f[e];
     }
     if (p.delta) put(blk + w.kh(), w.plane(), at, k);
-    put(blk + w.qh(), -w.plane(), at, q);
+    put<!BRIEF>(blk + w.qh(), -w.plane(), at, q);
     put(blk + w.kb(), w.plane(), at, lT);
   }
   __syncthreads();
-  put_squares<256>(blk, w, p, P, G, M, in.beta, tid);
+  put_squares<256, BWD, BRIEF>(blk, w, p.delta, P, G, M, in.beta, tid);
 }
 
 // The same for bf16 keys and queries with one log-decay per head or none, one wave per
 // (chunk, head): the operands of k k^T and q k^T come straight from memory, exact in bf16, and
 // only the squares and the row factors are written.
-template <int DK>
+template <int DK, bool BWD>
 __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   constexpr int NKS = DK / 32;
-  __shared__ float G[CT][CT + 1], P[CT][CT + 1], M[CT][CT + 1], betas[CT];
+  __shared__ __attribute__((aligned(16))) float G[CT][SL], P[CT][SL], M[BWD ? CT : 1][SL], betas[CT];
   const int lane = threadIdx.x, c16 = lane & 15, g = lane >> 4;
   const int h = blockIdx.x % p.H, c = blockIdx.x / p.H;
   const ChunkRow row = chunk_row(p, c);
   if (row.count == 0) return;
-  const WsLayout w{DK, p.dv, true, p.bwd};
+  const WsLayout w{DK, p.dv, true, BWD};
   unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
 
   bf16x8 kf[2][NKS], qf[2][NKS];
@@ -428,9 +456,9 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) G[4 * g + r][16 + c16] = P[4 * g + r][16 + c16] = 0.f;
   __syncthreads();
-  if (p.delta) solve(G, M, betas, lane);
+  if (p.delta) solve<BWD>(G, M, betas, lane);
   __syncthreads();
-  put_squares<64>(blk, w, p, P, G, M, betas, lane);
+  put_squares<64, BWD, true>(blk, w, p.delta, P, G, M, betas, lane);
 }
 
 }  // namespace dl

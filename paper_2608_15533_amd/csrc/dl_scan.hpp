@@ -202,12 +202,14 @@ struct SeqParams {
 };
 
 // Waves of a workgroup that walks chunks, 16 value columns each.  While there are few waves for
-// the 256 CUs, few to a workgroup spread them (a wave alone on its SIMD is at its fastest);
-// where planes from the workspace fill a CU's LDS with one workgroup, four as soon as two would
-// leave workgroups waiting; with more waves than that, whole heads, which share the operands.
-inline int walk_waves(int64_t heads, int dv, bool raw) {
+// the 256 CUs, workgroups of two spread them (a wave alone on its SIMD is at its fastest), as
+// long as all run at once: LDS and registers hold four of them on a CU for 64 keys, two for 128
+// with raw operands, one with planes from the workspace.  Then four waves, then whole heads,
+// which share their operands.
+inline int walk_waves(int64_t heads, int dk, int dv, bool raw) {
   const int64_t waves = heads * (dv / 16);
-  return waves <= 512 || (raw && waves <= 1024) ? 2 : waves <= 1024 ? 4 : dv / 16;
+  const int64_t two = dk == 64 ? 2048 : raw ? 1024 : 512;   // what workgroups of two keep running
+  return waves <= two ? 2 : waves <= 1024 ? 4 : dv / 16;
 }
 
 struct ChunkRow {
