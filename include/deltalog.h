@@ -230,6 +230,8 @@ int dl_append_step_tiled_noalloc(const dl_desc* desc, const dl_state* state,
  * are never used, and output rows there stay as they were. */
 #define DL_CHUNK 32   /* tokens of a chunk of the tables below */
 
+#define DL_MAX_HEADS 65536   /* of whole-sequence calls */
+
 /* Chunk rows the tables of n sequences with up to `tokens` token rows have. */
 #define DL_MAX_CHUNKS(n, tokens) ((tokens) / DL_CHUNK + (n))
 
@@ -241,6 +243,8 @@ typedef struct {
                       /*       row, tokens, slot); (-1, 0, 0, -1) past the chunks in use   */
   int32_t* row_slot;  /* [N]   slot of every token row; -1 past the rows in use            */
   int32_t* seq_slot;  /* [n]   slot of every sequence                                      */
+  int32_t* order;     /* [n]   the sequences, longest first up to 1024 of them (dl_prefill */
+                      /*       starts them in this order), as they come with more          */
 } dl_tables;
 
 /* Build the tables from lens [n] (device) and slots (device int32 [n], or NULL: sequence i
@@ -267,7 +271,11 @@ int dl_prefill_workspace_bytes(const dl_desc* desc, int32_t n, int32_t tokens,
  * tables: as dl_chunk_tables left them for the same n and N (row_slot is not read).
  * workspace: at least dl_prefill_workspace_bytes(desc, n, N, 0, ..) bytes, 256-byte
  * aligned; scratch, never read across calls; calls that share one must not overlap.
- * desc->merge_interval is validated but otherwise ignored.  n == 0 is a no-op. */
+ * With no token rows (N == 0) the pointers to rows may be NULL.
+ * desc->merge_interval is validated but otherwise ignored.  At most DL_MAX_HEADS heads
+ * (else DL_E_SHAPE).  n == 0 is a no-op.
+ * A value that is infinite or NaN stays within its sequence and head, but may reach outputs
+ * of up to 31 tokens before its own (its chunk's). */
 int dl_prefill(const dl_desc* desc, const void* S_in, void* S_out, const dl_token* tok, void* o,
                const dl_tables* tables, int32_t n, int32_t tokens, void* workspace,
                size_t workspace_bytes, hipStream_t stream);

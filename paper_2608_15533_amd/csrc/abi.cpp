@@ -172,10 +172,12 @@ int tiled_launch(const dl_desc* desc, const dl_state* state, const dl_token* tok
 int check_sequences(const dl_desc* desc, const dl_token* tok, const dl_tables* t, int32_t n,
                     int32_t tokens, const void* workspace, size_t workspace_bytes,
                     bool backward) {
-  DL_TRY(check_token(desc, tok));
-  if (!t || !t->cu_tokens || !t->cu_chunks || !t->chunks || !t->seq_slot) return DL_E_NULL;
+  if (!tok) return DL_E_NULL;
+  if (tokens > 0) DL_TRY(check_token(desc, tok));   // no rows: no pointers to rows
+  if (!t || !t->cu_tokens || !t->cu_chunks || !t->chunks || !t->seq_slot || !t->order)
+    return DL_E_NULL;
   if (!aligned(t->cu_tokens, 4) || !aligned(t->cu_chunks, 4) || !aligned(t->chunks, 16) ||
-      !aligned(t->seq_slot, 4))
+      !aligned(t->seq_slot, 4) || !aligned(t->order, 4))
     return DL_E_ALIGN;
   size_t need = 0;
   DL_TRY(dl_prefill_workspace_bytes(desc, n, tokens, backward, &need));

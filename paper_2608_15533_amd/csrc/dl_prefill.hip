@@ -68,6 +68,7 @@ namespace {
 
 int check_counts(const dl_desc* d, int32_t n, int32_t tokens) {
   if (n < 0 || tokens < 0 || n > d->num_slots) return DL_E_SHAPE;
+  if (d->heads > DL_MAX_HEADS) return DL_E_SHAPE;   // a chunk's rows lie within 32-bit offsets
   // Grids of one workgroup per (chunk, head) and per (sequence, head, 16 value columns).
   const int64_t chunks = int64_t(tokens) / DL_CHUNK + n;
   if (chunks * d->heads > int64_t(0x7fffffff)) return DL_E_SHAPE;
@@ -99,6 +100,7 @@ SeqParams params(const dl_desc* d, const void* S_in, const dl_token* tok, const 
   p.cu_chunks = t->cu_chunks;
   p.chunks = t->chunks;
   p.seq_slot = t->seq_slot;
+  p.order = t->order;
   p.ws = static_cast<unsigned char*>(ws);
   p.n = n;
   p.N = tokens;
@@ -128,11 +130,13 @@ int dl_chunk_tables(const int32_t* lens, const int32_t* slots, int32_t n, int32_
   if (int64_t(tokens) / DL_CHUNK + n > int64_t(0x7fffffff)) return DL_E_SHAPE;
   if (n == 0) return DL_OK;
   if (!slots && n > num_slots) return DL_E_SHAPE;
-  if (!lens || !t || !t->cu_tokens || !t->cu_chunks || !t->chunks || !t->seq_slot) return DL_E_NULL;
+  if (!lens || !t || !t->cu_tokens || !t->cu_chunks || !t->chunks || !t->seq_slot || !t->order)
+    return DL_E_NULL;
   if (tokens > 0 && !t->row_slot) return DL_E_NULL;
   if (!dl::aligned(lens, 4) || !dl::aligned(slots, 4) || !dl::aligned(t->cu_tokens, 4) ||
       !dl::aligned(t->cu_chunks, 4) || !dl::aligned(t->chunks, 16) ||
-      !dl::aligned(t->row_slot, 4) || !dl::aligned(t->seq_slot, 4) || !dl::aligned(err, 4))
+      !dl::aligned(t->row_slot, 4) || !dl::aligned(t->seq_slot, 4) || !dl::aligned(t->order, 4) ||
+      !dl::aligned(err, 4))
     return DL_E_ALIGN;
   const hipError_t e = dl::launch_tables(lens, slots, n, tokens, num_slots, *t, err,
                                          tokens / DL_CHUNK + n, stream);
@@ -156,7 +160,7 @@ int dl_prefill(const dl_desc* desc, const void* S_in, void* S_out, const dl_toke
   DL_TRY(dl::check_counts(desc, n, tokens));
   if (n == 0) return DL_OK;               // nothing to do, whatever the other pointers are
   DL_TRY(dl::check_sequences(desc, tok, tables, n, tokens, workspace, workspace_bytes, false));
-  if (!S_out || !o) return DL_E_NULL;
+  if (!S_out || (tokens > 0 && !o)) return DL_E_NULL;
   if (!dl::aligned(S_in, 16) || !dl::aligned(S_out, 16) || !dl::aligned(o, 16)) return DL_E_ALIGN;
   dl::SeqParams p = dl::params(desc, S_in, tok, tables, n, tokens, workspace);
   p.S_out = S_out;
@@ -172,9 +176,10 @@ int dl_prefill_backward(const dl_desc* desc, const void* S_in, const dl_token* t
   DL_TRY(dl::check_counts(desc, n, tokens));
   if (n == 0) return DL_OK;               // nothing to do, whatever the other pointers are
   DL_TRY(dl::check_sequences(desc, tok, tables, n, tokens, workspace, workspace_bytes, true));
-  if (!d_o || !g || !g->dq || !g->dk || !g->dv) return DL_E_NULL;
+  if (!g || (tokens > 0 && (!d_o || !g->dq || !g->dk || !g->dv))) return DL_E_NULL;
   dl::SeqParams p = dl::params(desc, S_in, tok, tables, n, tokens, workspace);
-  if ((p.delta && !g->dbeta) || (p.lam && !g->dlam) || (p.u && !g->du)) return DL_E_NULL;
+  if (tokens > 0 && ((p.delta && !g->dbeta) || (p.lam && !g->dlam))) return DL_E_NULL;
+  if (p.u && !g->du) return DL_E_NULL;
   if (!dl::aligned(S_in, 16) || !dl::aligned(d_o, 16) || !dl::aligned(dS_out, 16) ||
       !dl::aligned(g->dq, 16) || !dl::aligned(g->dk, 16) || !dl::aligned(g->dv, 16) ||
       !dl::aligned(g->dS, 16) || !dl::aligned(g->dbeta, 4) || !dl::aligned(g->dlam, 4) ||

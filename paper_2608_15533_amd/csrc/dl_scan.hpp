@@ -195,7 +195,7 @@ struct SeqParams {
   void* o;               // [N,H,dv]
   void *dq, *dk_, *dv_;  // gradients
   float *dbeta, *dlam, *du;
-  const int32_t *cu_tokens, *cu_chunks, *chunks, *seq_slot;
+  const int32_t *cu_tokens, *cu_chunks, *chunks, *seq_slot, *order;
   unsigned char* ws;
   int32_t n, N, B, H, dv, max_chunks;
   bool delta, state_bf16, bwd, raw;

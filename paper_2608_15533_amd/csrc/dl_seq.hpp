@@ -247,7 +247,8 @@ __device__ __forceinline__ bool start_walk(const SeqParams& p, Walk& k) {
   const int nvt = p.dv / VC, b = blockIdx.x;
   k.v0 = VC * (b % nvt);
   k.h = (b / nvt) % p.H;
-  k.seq = b / nvt / p.H;
+  k.seq = p.order[b / nvt / p.H];              // longest first: none starts when the rest is done
+  if (k.seq < 0 || k.seq >= p.n) return false;
   k.slot = p.seq_slot[k.seq];
   if (k.slot < 0 || k.slot >= p.B) return false;
   k.c0 = max(p.cu_chunks[k.seq], 0);

@@ -23,6 +23,7 @@ constexpr int SCAN_NT = 1024;
 __global__ __launch_bounds__(SCAN_NT) void table_scan_kernel(TableParams p) {
   __shared__ int64_t part_t[SCAN_NT / 64];
   __shared__ int part_c[SCAN_NT / 64];
+  __shared__ __attribute__((aligned(16))) int count[SCAN_NT];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int64_t base_t = 0;
   int base_c = 0, bad = 0;
@@ -74,7 +75,20 @@ __global__ __launch_bounds__(SCAN_NT) void table_scan_kernel(TableParams p) {
     }
     base_t = all;
     base_c = call;
+    if (p.n > SCAN_NT && i < p.n) p.t.order[i] = i;
+    count[tid] = i < p.n ? mine : -1;
     __syncthreads();
+  }
+  if (p.n <= SCAN_NT && tid < p.n) {
+    // place of a sequence: how many are longer, or as long and before it
+    const int mine = count[tid];
+    int place = 0;
+    for (int j = 0; j < p.n; j += 4) {
+      const int4 c = *reinterpret_cast<const int4*>(&count[j]);     // past n: -1
+      place += (c.x > mine || (c.x == mine && j < tid)) + (c.y > mine || (c.y == mine && j + 1 < tid)) +
+               (c.z > mine || (c.z == mine && j + 2 < tid)) + (c.w > mine || (c.w == mine && j + 3 < tid));
+    }
+    p.t.order[place] = tid;
   }
   if (bad && p.err) atomicOr(p.err, bad);
 }

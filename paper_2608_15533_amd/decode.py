@@ -46,7 +46,9 @@ host-to-device copy, outside the graph, when the plan's row order changes.
 
 Slot lifecycle (Sec. 4): ``admit`` writes the prefill state into the slot's dense base
 and resets only the slot's live length (which also restarts the cumulative log-decay;
-log rows past the live length are never read).  ``release`` frees the slot, optionally
+log rows past the live length are never read).  ``prefill`` admits prompts and runs them
+through every layer, straight into the slots' bases; called again with those slots it
+continues them (a prompt in parts, a later turn).  ``release`` frees the slot, optionally
 flushing its log into the base first so the materialised state can be saved.
 """
 
@@ -121,6 +123,7 @@ class DecodeEngine:
         self._graph_cache = {}
         self._side = torch.cuda.Stream(device=device) if mode == "phased_concurrent" else None
         self.plan = None
+        self._prefill_ws = None
         self.replays = 0
         self.direct_steps = 0
 
@@ -143,6 +146,63 @@ class DecodeEngine:
             st.len[slot].zero_()
         self.plan = None
         return slot
+
+    def prefill(self, lens, tokens, slots=None):
+        """Run prompts through every layer (``dl_prefill``).  ``lens`` (host integers) are the
+        prompts' lengths, their token rows packed one after the other; ``tokens`` has one
+        (q, k, v, lam, beta) per layer, [sum(lens), H, ...] (RWKV6's bonus is the layer's).
+        Without ``slots`` every prompt takes a free slot and starts from a zero state; with it,
+        a list of distinct active slots, prompt i goes on from the state of slots[i], whose log
+        is flushed first.  Returns (slots, outputs), one output [sum(lens), H, dv] per layer in
+        the input dtype."""
+        lens = [int(n) for n in lens]
+        if any(n < 0 for n in lens):
+            raise ValueError("a prompt's length is negative")
+        if len(tokens) != self.layers:
+            raise ValueError("prefill needs one set of tokens per layer")
+        N, desc = sum(lens), self.desc
+        layer_tokens = [D.Token(desc, N, q, k, v, lam, beta, inp.u)
+                        for (q, k, v, lam, beta), inp in zip(tokens, self.inputs)]
+        fresh = slots is None
+        if fresh:
+            if len(lens) > self.sched.free_slots:
+                raise SlotError(f"{len(lens)} prompts, {self.sched.free_slots} free slots")
+            slots = [self.sched.admit() for _ in lens]
+        else:
+            slots = list(slots)
+            if len(slots) != len(lens) or len(set(slots)) != len(slots):
+                raise ValueError("one slot per prompt, each slot once")
+            for s in slots:
+                if s not in self.sched.active:
+                    raise SlotError(f"slot {s} is not active")
+        self.plan = None
+        outs = [torch.empty_like(t.tensors[2]) for t in layer_tokens]
+        try:
+            if lens:
+                self._run_prompts(lens, slots, layer_tokens, outs, fresh)
+        except Exception:
+            for s in slots if fresh else ():
+                self.sched.release(s)
+            raise
+        return slots, outs
+
+    def _run_prompts(self, lens, slots, layer_tokens, outs, fresh):
+        desc, N = self.desc, sum(lens)
+        host = torch.tensor([lens, slots], dtype=torch.int32).to(self.device)
+        tables = D.ChunkTables(len(lens), N, num_slots=desc.num_slots, device=self.device)
+        D.dl_chunk_tables(host[0], tables, slots=host[1])
+        need = D.dl_prefill_workspace_bytes(desc, len(lens), N)
+        if self._prefill_ws is None or self._prefill_ws.numel() < need:
+            self._prefill_ws = None                   # let go before taking the larger one
+            self._prefill_ws = D.prefill_workspace(desc, len(lens), N, device=self.device)
+        rows = host[1].long()
+        for st, tok, o in zip(self.states, layer_tokens, outs):
+            if not fresh:
+                D.dl_merge(desc, st, slots=host[1])
+            D.dl_prefill(desc, None if fresh else st.S, st.S, tok, o, tables, self._prefill_ws)
+            st.len[rows] = 0
+        for s in slots:
+            self.sched.flushed(s)
 
     def release(self, slot, flush=False):
         """Free an active slot; with ``flush`` fold its log into the base first and

@@ -33,7 +33,7 @@ DL_OK, DL_E_NULL, DL_E_SHAPE, DL_E_DTYPE, DL_E_ALIGN, DL_E_UNSUPPORTED, DL_E_HIP
     0, -1, -2, -3, -4, -5, -6, -7)
 DL_E_SCRATCH = -8
 DL_NOALLOC_SCRATCH_BYTES = 4 << 20
-DL_CHUNK = 32
+DL_CHUNK, DL_MAX_HEADS = 32, 65536
 DL_OP_GDN, DL_OP_KDA, DL_OP_RWKV6, DL_OP_LINATTN, DL_OP_RETNET, DL_OP_GLA = 0, 1, 2, 3, 4, 5
 DL_F32, DL_BF16 = 0, 1
 OP_IDS = {"gdn": DL_OP_GDN, "kda": DL_OP_KDA, "rwkv6": DL_OP_RWKV6, "linattn": DL_OP_LINATTN,
@@ -72,7 +72,7 @@ class dl_token(ctypes.Structure):
 class dl_tables(ctypes.Structure):
     _fields_ = [("cu_tokens", ctypes.c_void_p), ("cu_chunks", ctypes.c_void_p),
                 ("chunks", ctypes.c_void_p), ("row_slot", ctypes.c_void_p),
-                ("seq_slot", ctypes.c_void_p)]
+                ("seq_slot", ctypes.c_void_p), ("order", ctypes.c_void_p)]
 
 
 class dl_grads(ctypes.Structure):
@@ -379,9 +379,10 @@ class ChunkTables:
         self.chunks = torch.zeros((self.tokens // DL_CHUNK + self.n, 4), **i32)
         self.row_slot = torch.zeros((self.tokens,), **i32)
         self.seq_slot = torch.zeros((self.n,), **i32)
+        self.order = torch.zeros((self.n,), **i32)
         self.err = torch.zeros((1,), **i32)
         self.struct = dl_tables(_ptr(self.cu_tokens), _ptr(self.cu_chunks), _ptr(self.chunks),
-                                _ptr(self.row_slot), _ptr(self.seq_slot))
+                                _ptr(self.row_slot), _ptr(self.seq_slot), _ptr(self.order))
 
 
 class Grads:
@@ -401,12 +402,21 @@ class Grads:
                                _ptr(self.dlam), _ptr(self.du), _ptr(self.dS))
 
 
+def _on_current_device(*tensors):
+    """Every tensor on the current device, whose stream the call goes to."""
+    cur = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != cur:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{cur}")
+
+
 def dl_chunk_tables(lens, tables, slots=None, stream=None):
     """Build ``tables`` from the sequences' lengths, lens [n] int32 on the device (slots [n]
     int32, or None: sequence i has slot i)."""
     _need(lens, "lens", torch.int32, (tables.n,))
     if slots is not None:
         _need(slots, "slots", torch.int32, (tables.n,))
+    _on_current_device(lens, slots, tables.err)
     _check(_lib.dl_chunk_tables(_ptr(lens), _ptr(slots), tables.n, tables.tokens,
                                 tables.num_slots, ctypes.byref(tables.struct),
                                 _ptr(tables.err), _stream(stream)), "dl_chunk_tables")
@@ -428,6 +438,9 @@ def prefill_workspace(desc, n, tokens, backward=False, device="cuda"):
 
 
 def _sequences(desc, tok, tables, workspace, S_in):
+    if workspace is None or not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous device tensor (see prefill_workspace)")
+    _on_current_device(tok.tensors[0], tables.err, workspace, S_in)
     if tok.n != tables.tokens:
         raise ValueError(f"the token holds {tok.n} rows but the tables are for {tables.tokens}")
     if S_in is not None:
