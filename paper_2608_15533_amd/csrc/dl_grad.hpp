@@ -64,7 +64,7 @@ __device__ __forceinline__ Split value_operand(const float* at, bool live) {
   return split8(x);
 }
 
-template <int DC, int DK, typename TIN>
+template <int DC, int DK, int DV, typename TIN>
 __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
   constexpr int KT = DK / 64;                  // key tiles of a wave
   constexpr bool LO = sizeof(TIN) == 4;        // dO has a second half
@@ -105,7 +105,8 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) aq[x][tt] = ar[x][tt] = ac[x][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  for (int s = 0; s < p.dv / 32; ++s) {
+#pragma unroll
+  for (int s = 0; s < DV / 32; ++s) {
     const int v = 32 * s + 8 * g;
     Split od[2], oz[2], oe[2];
 #pragma unroll
@@ -144,7 +145,8 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
     const int bi = wave == 0 ? 0 : 1, bj = wave == 1 ? 1 : 0;   // (0,0), (1,1), (1,0)
     const int i = 16 * bi + c16, j = 16 * bj + c16;
     f32x4 ap = {0.f, 0.f, 0.f, 0.f}, ag = ap;
-    for (int s = 0; s < p.dv / 32; ++s) {
+#pragma unroll
+    for (int s = 0; s < DV / 32; ++s) {
       const int v = 32 * s + 8 * g;
       float x[8];
       saved(E, CT, j, v, x);
@@ -177,8 +179,8 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
     if (p.delta) {
       const int t = lane >> 1;                 // two lanes a token
       f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-      for (int v = 8 * (lane & 1); v < p.dv; v += 16) {
+#pragma unroll
+      for (int v = 8 * (lane & 1); v < DV; v += 16) {
         const int at = ((v >> 4) * CT + t) * 16 + (v & 15);
 #pragma unroll
         for (int y = 0; y < 8; y += 4)

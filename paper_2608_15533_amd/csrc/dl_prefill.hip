@@ -29,29 +29,25 @@ hipError_t launch_prep(int op, const SeqParams& p, hipStream_t s) {
   return p.bwd ? launch_prep_pass<DK, true, TIN>(op, p, s) : launch_prep_pass<DK, false, TIN>(op, p, s);
 }
 
-template <int DK, bool RAW, bool DELTA, int PASS, typename TIN>
+template <int DK, bool RAW, bool DELTA, typename TIN>
 hipError_t launch_walk(const SeqParams& p, hipStream_t s) {
   const int64_t heads = int64_t(p.n) * p.H;
   const int waves = walk_waves(heads, DK, p.dv, RAW);
   const int64_t grid = heads * (p.dv / 16 / waves);
   switch (waves) {
-    case 2: return start(&forward_kernel<DK, 1, 2, RAW, DELTA, PASS, TIN>, grid, 128, p, s);
-    case 4: return start(&forward_kernel<DK, 1, 4, RAW, DELTA, PASS, TIN>, grid, 256, p, s);
-    default: return start(&forward_kernel<DK, 1, 8, RAW, DELTA, PASS, TIN>, grid, 512, p, s);
+    case 2: return start(&forward_kernel<DK, 1, 2, RAW, DELTA, TIN>, grid, 128, p, s);
+    case 4: return start(&forward_kernel<DK, 1, 4, RAW, DELTA, TIN>, grid, 256, p, s);
+    default: return start(&forward_kernel<DK, 1, 8, RAW, DELTA, TIN>, grid, 512, p, s);
   }
-}
-template <int DK, bool RAW, bool DELTA, typename TIN>
-hipError_t launch_scan(const SeqParams& p, hipStream_t s) {
-  return p.bwd ? launch_walk<DK, RAW, DELTA, PASS_SAVE, TIN>(p, s) : launch_walk<DK, RAW, DELTA, PASS_OUT, TIN>(p, s);
 }
 
 template <int DK, typename TIN>
 hipError_t launch_forward_shape(int op, const SeqParams& p, hipStream_t s) {
   const hipError_t e = launch_prep<DK, TIN>(op, p, s);
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || p.bwd) return e;         // the backward pass has its walks elsewhere
   if constexpr (sizeof(TIN) == 2)
-    if (p.raw) return p.delta ? launch_scan<DK, true, true, TIN>(p, s) : launch_scan<DK, true, false, TIN>(p, s);
-  return p.delta ? launch_scan<DK, false, true, TIN>(p, s) : launch_scan<DK, false, false, TIN>(p, s);
+    if (p.raw) return p.delta ? launch_walk<DK, true, true, TIN>(p, s) : launch_walk<DK, true, false, TIN>(p, s);
+  return p.delta ? launch_walk<DK, false, true, TIN>(p, s) : launch_walk<DK, false, false, TIN>(p, s);
 }
 
 }  // namespace
@@ -186,7 +182,6 @@ int dl_prefill_backward(const dl_desc* desc, const void* S_in, const dl_token* t
       !dl::aligned(g->du, 4))
     return DL_E_ALIGN;
   p.bwd = true;
-  if (dl::launch_forward(desc, p, stream) != hipSuccess) return DL_E_HIP;   // states and E again
   p.d_o = d_o;
   p.dS_out = dS_out;
   p.S_out = g->dS;
@@ -196,6 +191,7 @@ int dl_prefill_backward(const dl_desc* desc, const void* S_in, const dl_token* t
   p.dbeta = p.delta ? g->dbeta : nullptr;
   p.dlam = p.lam ? g->dlam : nullptr;
   p.du = p.u ? g->du : nullptr;
+  if (dl::launch_forward(desc, p, stream) != hipSuccess) return DL_E_HIP;   // the operands
   return dl::launch_backward(desc, p, stream) == hipSuccess ? DL_OK : DL_E_HIP;
 }
 

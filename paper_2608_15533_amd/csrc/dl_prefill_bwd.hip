@@ -15,20 +15,22 @@ hipError_t start(K* kernel, int64_t grid, int block, const SeqParams& p, hipStre
 
 template <int DC, int DK, typename TIN>
 hipError_t launch_grad(const SeqParams& p, hipStream_t s) {
-  hipError_t e = start(&grad_kernel<DC, DK, TIN>, int64_t(p.max_chunks) * p.H, 256, p, s);
+  const int64_t grid = int64_t(p.max_chunks) * p.H;
+  hipError_t e = p.dv == 128 ? start(&grad_kernel<DC, DK, 128, TIN>, grid, 256, p, s)
+                             : start(&grad_kernel<DC, DK, 64, TIN>, grid, 256, p, s);
   if (DC == DC_BONUS && e == hipSuccess) e = start(&bonus_grad_kernel<DK>, p.H, 1024, p, s);
   return e;
 }
 
 template <int DK, bool RAW, bool DELTA, typename TIN>
-hipError_t launch_scan(const SeqParams& p, hipStream_t s) {
+hipError_t launch_walks(const SeqParams& p, hipStream_t s) {
   const int64_t heads = int64_t(p.n) * p.H;
-  const int waves = walk_waves(heads, DK, p.dv, RAW);
-  const int64_t grid = heads * (p.dv / 16 / waves);
+  const int waves = walk_waves(2 * heads, DK, p.dv, RAW);
+  const int64_t grid = 2 * heads * (p.dv / 16 / waves);
   switch (waves) {
-    case 2: return start(&backward_kernel<DK, 1, 2, RAW, DELTA, TIN>, grid, 128, p, s);
-    case 4: return start(&backward_kernel<DK, 1, 4, RAW, DELTA, TIN>, grid, 256, p, s);
-    default: return start(&backward_kernel<DK, 1, 8, RAW, DELTA, TIN>, grid, 512, p, s);
+    case 2: return start(&both_kernel<DK, 1, 2, RAW, DELTA, TIN>, grid, 128, p, s);
+    case 4: return start(&both_kernel<DK, 1, 4, RAW, DELTA, TIN>, grid, 256, p, s);
+    default: return start(&both_kernel<DK, 1, 8, RAW, DELTA, TIN>, grid, 512, p, s);
   }
 }
 
@@ -36,8 +38,8 @@ template <int DK, typename TIN>
 hipError_t launch_backward_shape(int op, const SeqParams& p, hipStream_t s) {
   hipError_t e = hipErrorInvalidValue;
   if constexpr (sizeof(TIN) == 2)
-    if (p.raw) e = p.delta ? launch_scan<DK, true, true, TIN>(p, s) : launch_scan<DK, true, false, TIN>(p, s);
-  if (!p.raw) e = p.delta ? launch_scan<DK, false, true, TIN>(p, s) : launch_scan<DK, false, false, TIN>(p, s);
+    if (p.raw) e = p.delta ? launch_walks<DK, true, true, TIN>(p, s) : launch_walks<DK, true, false, TIN>(p, s);
+  if (!p.raw) e = p.delta ? launch_walks<DK, false, true, TIN>(p, s) : launch_walks<DK, false, false, TIN>(p, s);
   if (e != hipSuccess) return e;
   if (op == DL_OP_RWKV6) return launch_grad<DC_BONUS, DK, TIN>(p, s);
   if (op == DL_OP_KDA || op == DL_OP_GLA) return launch_grad<DC_KEY, DK, TIN>(p, s);

@@ -243,8 +243,8 @@ struct Walk {
   __device__ __forceinline__ int count(int c) const { return min(CT, end - row(c)); }
 };
 template <int VC>
-__device__ __forceinline__ bool start_walk(const SeqParams& p, Walk& k) {
-  const int nvt = p.dv / VC, b = blockIdx.x;
+__device__ __forceinline__ bool start_walk(const SeqParams& p, int b, Walk& k) {
+  const int nvt = p.dv / VC;
   k.v0 = VC * (b % nvt);
   k.h = (b / nvt) % p.H;
   k.seq = p.order[b / nvt / p.H];              // longest first: none starts when the rest is done
@@ -306,15 +306,16 @@ __device__ __forceinline__ void save_tiles(const f32x4 (&x)[NR][NT], unsigned ch
 // other and c + 2 from memory to registers, and at its end the wave reads what chunk c + 1
 // starts with.  What the state needs comes first, outputs follow.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, int PASS, typename TIN>
-__global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
+__device__ __forceinline__ void walk_forward(
+    const SeqParams& p, int group,
+    unsigned char (&lds)[2][Stage<DK, NT, NW, RAW, DELTA, PASS, TIN>::BYTES]) {
   using St = Stage<DK, NT, NW, RAW, DELTA, PASS, TIN>;
   constexpr int NKT = DK / 16, NKS = DK / 32;
   constexpr bool OUT = PASS == PASS_OUT;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][St::BYTES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15;
   Walk k;
-  if (!start_walk<St::VC>(p, k)) return;
+  if (!start_walk<St::VC>(p, group, k)) return;
   const WsLayout w{DK, p.dv, RAW, p.bwd};
   const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;        // this lane's first column
   const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
@@ -476,14 +477,15 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
 //   dV = Y                  D <- e^{l_T} D + Qh^T dO - Kh^T Y
 // LDS as in the forward pass.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
-__global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
+__device__ __forceinline__ void walk_backward(
+    const SeqParams& p, int group,
+    unsigned char (&lds)[2][Stage<DK, NT, NW, RAW, DELTA, PASS_BACK, TIN>::BYTES]) {
   using St = Stage<DK, NT, NW, RAW, DELTA, PASS_BACK, TIN>;
   constexpr int NKT = DK / 16, NKS = DK / 32;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][St::BYTES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15;
   Walk k;
-  if (!start_walk<St::VC>(p, k)) return;
+  if (!start_walk<St::VC>(p, group, k)) return;
   const WsLayout w{DK, p.dv, RAW, true};
   const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;
   const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
@@ -612,6 +614,30 @@ __global__ __launch_bounds__(64 * NW) void backward_kernel(SeqParams p) {
     }
   }
   if (p.S_out) write_state(D, p.S_out, p.state_bf16, p.dv, state_at, lane);
+}
+
+template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
+__global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
+  __shared__ __attribute__((aligned(16))) unsigned char
+      lds[2][Stage<DK, NT, NW, RAW, DELTA, PASS_OUT, TIN>::BYTES];
+  walk_forward<DK, NT, NW, RAW, DELTA, PASS_OUT, TIN>(p, blockIdx.x, lds);
+}
+
+// The backward pass's two walks in one launch: neither needs the other, and each alone leaves
+// most of the chip waiting while sequences and heads are few (64 heads of 2048 tokens, 128 x 128:
+// 139 + 186 us one after the other).  Even workgroups go backward, odd ones forward.
+template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
+__global__ __launch_bounds__(64 * NW) void both_kernel(SeqParams p) {
+  using Save = Stage<DK, NT, NW, RAW, DELTA, PASS_SAVE, TIN>;
+  using Back = Stage<DK, NT, NW, RAW, DELTA, PASS_BACK, TIN>;
+  constexpr int BYTES = 2 * (Save::BYTES > Back::BYTES ? Save::BYTES : Back::BYTES);
+  __shared__ __attribute__((aligned(16))) unsigned char lds[BYTES];
+  if (blockIdx.x & 1)
+    walk_forward<DK, NT, NW, RAW, DELTA, PASS_SAVE, TIN>(
+        p, blockIdx.x >> 1, *reinterpret_cast<unsigned char(*)[2][Save::BYTES]>(&lds));
+  else
+    walk_backward<DK, NT, NW, RAW, DELTA, TIN>(
+        p, blockIdx.x >> 1, *reinterpret_cast<unsigned char(*)[2][Back::BYTES]>(&lds));
 }
 
 }  // namespace dl
