@@ -13,9 +13,11 @@
 // with S' the state after the chunk: sum_v S' D = e^{l_T} sum_v S D + sum_j Kb_j dKb_j.
 // RWKV6: q_i dq_i counts towards l_{i-1}, and its bonus pair (dP_ii) goes to q, k and u alone.
 //
-// Each wave owns dk/64 tiles of 16 keys and all tokens, as MFMA results: a lane has one key
-// and the eight tokens 16 tt + 4 g + r, which are also the terms (state order) that it feeds a
-// product over tokens, so keys, queries and decay factors are fetched once for both uses.
+// Each wave owns 16 keys and all tokens, as MFMA results: a lane has one key and the eight tokens
+// 16 tt + 4 g + r, which are also the terms (state order) that it feeds a product over tokens, so
+// keys, queries and decay factors are fetched once for both uses.  dO, E and Z are split once by
+// the workgroup into planes in LDS, from which every wave reads its operands; S and D, which
+// no two waves share, go from memory to registers.
 #pragma once
 
 #include "dl_prep.hpp"
@@ -47,34 +49,87 @@ __device__ __forceinline__ Split square_operand(const float (*m)[SL], int tt, in
   return split8(a);
 }
 
-// A token row's eight values as an operand over values; bf16 ones are exact (lo unused).
-__device__ __forceinline__ Split value_operand(const uint16_t* at, bool live) {
-  Split s;
-  u32x4 x = *reinterpret_cast<const u32x4*>(at);
-  const u32x4 zero = {0, 0, 0, 0};
-  if (!live) x = zero;
-  s.hi = __builtin_bit_cast(bf16x8, x);
-  return s;
-}
-__device__ __forceinline__ Split value_operand(const float* at, bool live) {
-  float x[8];
-  load8(at, x);
+template <int DC, int DK, int DV, typename TIN>
+struct GradShared {
+  static constexpr bool LO = sizeof(TIN) == 4;           // dO has a second half
+  static constexpr int NP = DV / 8, HALF = CT * DV * 2;
+  static constexpr int A_E = 0, A_Z = 2 * HALF, A_DO = 4 * HALF;
+  ChunkIn<DC, DK, TIN> in;
+  union {
+    __attribute__((aligned(16))) unsigned char planes[(LO ? 6 : 5) * HALF];
+    struct {
+      __attribute__((aligned(16))) float dP[CT][SL], dG[CT][SL];
+    };
+  };
+  float tok_sum[DK / 16][CT + 1];
+};
+
+// The planes' rows: dO (rows past the chunk's end as 0), E and Z, and dbeta on the way.
+template <int DC, int DK, int DV, int NTH, bool DELTA, typename TIN>
+__device__ __forceinline__ void load_planes(GradShared<DC, DK, DV, TIN>& sh, const SeqParams& p,
+                                            const ChunkRow& row, int h, const float* E,
+                                            const float* Z, int tid) {
+  using Sh = GradShared<DC, DK, DV, TIN>;
+  constexpr int NP = Sh::NP;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = live ? x[e] : 0.f;
-  return split8(x);
+  for (int x = tid; x < CT * NP; x += NTH) {
+    const int t = x / NP, pc = x % NP, at = 16 * piece_at<NP>(t, pc);
+    const int from = ((pc >> 1) * CT + t) * 16 + 8 * (pc & 1);      // [value tile][token][16]
+    float e[8], z[8];
+    load8(E + from, e);
+    if constexpr (DELTA) load8(Z + from, z);
+    const TIN* d = static_cast<const TIN*>(p.d_o) +
+                   (int64_t(row.first + min(t, row.count - 1)) * p.H + h) * DV + 8 * pc;
+    const bool live = t < row.count;
+    if constexpr (Sh::LO) {
+      float o[8];
+      load8(d, o);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = live ? o[i] : 0.f;
+      const Split s = split8(o);
+      *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_DO + at) = s.hi;
+      *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_DO + Sh::HALF + at) = s.lo;
+    } else {
+      const u32x4 zero = {0, 0, 0, 0}, o = *reinterpret_cast<const u32x4*>(d);
+      *reinterpret_cast<u32x4*>(sh.planes + Sh::A_DO + at) = live ? o : zero;
+    }
+    const Split se = split8(e);
+    *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_E + at) = se.hi;
+    *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_E + Sh::HALF + at) = se.lo;
+    if constexpr (DELTA) {
+      const Split sz = split8(z);
+      *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_Z + at) = sz.hi;
+      *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_Z + Sh::HALF + at) = sz.lo;
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += e[i] * z[i];
+#pragma unroll
+      for (int i = 1; i < NP; i *= 2) s += __shfl_xor(s, i);
+      if (pc == 0 && live) p.dbeta[int64_t(row.first + t) * p.H + h] = s;
+    }
+  }
 }
 
-template <int DC, int DK, int DV, typename TIN>
-__global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
-  constexpr int KT = DK / 64;                  // key tiles of a wave
-  constexpr bool LO = sizeof(TIN) == 4;        // dO has a second half
-  __shared__ ChunkIn<DC, DK, TIN> in;
-  __shared__ __attribute__((aligned(16))) float dP[CT][SL], dG[CT][SL];
-  __shared__ float tok_sum[4][CT + 1];
+// Waves to a SIMD: two workgroups on a CU for 128 keys (128 registers), where that spills none.
+template <int DC, int DK, typename TIN>
+constexpr int grad_waves() {
+  return DK == 64 ? 3 : DC == DC_BONUS || sizeof(TIN) == 4 ? 2 : 4;
+}
+
+template <int DC, int DK, int DV, bool DELTA, typename TIN>
+__global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kernel(SeqParams p) {
+  using Sh = GradShared<DC, DK, DV, TIN>;
+  constexpr int NTH = 4 * DK, NW = DK / 16, KT = 1, HALF = Sh::HALF, NP = Sh::NP;
+  constexpr bool LO = Sh::LO;
+  __shared__ Sh sh;
+  ChunkIn<DC, DK, TIN>& in = sh.in;
+  auto& dP = sh.dP;
+  auto& dG = sh.dG;
+  auto& tok_sum = sh.tok_sum;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int c16 = lane & 15, g = lane >> 4;
   const int h = blockIdx.x % p.H, c = blockIdx.x / p.H;
-  const WsLayout w{DK, p.dv, p.raw, true};
+  const WsLayout w{DK, DV, p.raw, true};
   unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
   float* du = reinterpret_cast<float*>(blk + w.du());
   const ChunkRow row = chunk_row(p, c);
@@ -84,83 +139,62 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
   }
   const float* S = reinterpret_cast<const float*>(blk + w.s0());
   const float* D = reinterpret_cast<const float*>(blk + w.ds());
-  const float* E = reinterpret_cast<const float*>(blk + w.e());
-  const float* Z = reinterpret_cast<const float*>(blk + w.z());
-  const TIN* dop = static_cast<const TIN*>(p.d_o) + (int64_t(row.first) * p.H + h) * p.dv;
-  const int64_t do_row = int64_t(p.H) * p.dv;
 
-  in.template load<256>(p, row, h, tid);
-
-  // Row x, values v..v+7 of what the serial passes saved ([value tile][row][16]).
-  auto saved = [](const float* m, int rows, int x, int v, float* out) {
-    load8(m + ((v >> 4) * rows + x) * 16 + (v & 15), out);
-  };
-
-  // Products over the value columns: token x key ...
-  f32x4 aq[KT][2], ar[KT][2], ac[KT][2];
-  float dot[KT];
-#pragma unroll
-  for (int x = 0; x < KT; ++x) {
-    dot[x] = 0.f;
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) aq[x][tt] = ar[x][tt] = ac[x][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  // S and D of this lane's key, ahead of everything that is waited for
+  const int mine = (((g >> 1) * DK) + 16 * wave + c16) * 16 + 8 * (g & 1);
+  float xs[DV / 32][8], xd[DV / 32][8];
 #pragma unroll
   for (int s = 0; s < DV / 32; ++s) {
-    const int v = 32 * s + 8 * g;
-    Split od[2], oz[2], oe[2];
+    load8(S + mine + 2 * s * DK * 16, xs[s]);
+    load8(D + mine + 2 * s * DK * 16, xd[s]);
+  }
+  load_planes<DC, DK, DV, NTH, DELTA, TIN>(sh, p, row, h, reinterpret_cast<const float*>(blk + w.e()),
+                                    reinterpret_cast<const float*>(blk + w.z()), tid);
+  in.template load<NTH, DELTA>(p, row, h, tid);   // and every thread past this point
+
+  auto operand = [&](int at, bool lo, int tt, int s) {
+    Split o;
+    o.hi = rows_operand<NP>(sh.planes + at, tt, s, lane);
+    if (lo) o.lo = rows_operand<NP>(sh.planes + at + HALF, tt, s, lane);
+    return o;
+  };
+  // Products over the value columns: token x key ...
+  f32x4 aq[KT][2], ar[KT][2], ac[KT][2];
+  float dot[KT] = {0.f};
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt) aq[0][tt] = ar[0][tt] = ac[0][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < DV / 32; ++s) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dot[0] += xs[s][e] * xd[s][e];
+    const Split bs = split8(xs[s]), bd = split8(xd[s]);
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      const int t = 16 * tt + c16;
-      float x[8];
-      od[tt] = value_operand(dop + min(t, row.count - 1) * do_row + v, t < row.count);
-      if (p.delta) {
-        saved(Z, CT, t, v, x);
-        oz[tt] = split8(x);
-      }
-      saved(E, CT, t, v, x);
-      oe[tt] = split8(x);
-    }
-#pragma unroll
-    for (int x = 0; x < KT; ++x) {
-      const int key = 16 * (wave * KT + x) + c16;
-      float xs[8], xd[8];
-      saved(S, DK, key, v, xs);
-      saved(D, DK, key, v, xd);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) dot[x] += xs[e] * xd[e];
-      const Split bs = split8(xs), bd = split8(xd);
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        aq[x][tt] = mma(od[tt].hi, bs.lo, aq[x][tt]);
-        if constexpr (LO) aq[x][tt] = mma(od[tt].lo, bs.hi, aq[x][tt]);
-        aq[x][tt] = mma(od[tt].hi, bs.hi, aq[x][tt]);
-        if (p.delta) ar[x][tt] = mma3(oz[tt], bs, ar[x][tt]);
-        ac[x][tt] = mma3(oe[tt], bd, ac[x][tt]);
-      }
+      const Split od = operand(Sh::A_DO, LO, tt, s);
+      aq[0][tt] = mma(od.hi, bs.lo, aq[0][tt]);
+      if constexpr (LO) aq[0][tt] = mma(od.lo, bs.hi, aq[0][tt]);
+      aq[0][tt] = mma(od.hi, bs.hi, aq[0][tt]);
+      if constexpr (DELTA) ar[0][tt] = mma3(operand(Sh::A_Z, true, tt, s), bs, ar[0][tt]);
+      ac[0][tt] = mma3(operand(Sh::A_E, true, tt, s), bd, ac[0][tt]);
     }
   }
-  // ... and token x token: a block of dP and dG per wave; the last wave has dbeta.
+  // ... and token x token: block (0,0), (1,1) or (1,0) of dP and dG by one wave each.
+  f32x4 ap = {0.f, 0.f, 0.f, 0.f}, ag = ap;
+  const int bi = wave == 0 ? 0 : 1, bj = wave == 1 ? 1 : 0;
   if (wave < 3) {
-    const int bi = wave == 0 ? 0 : 1, bj = wave == 1 ? 1 : 0;   // (0,0), (1,1), (1,0)
-    const int i = 16 * bi + c16, j = 16 * bj + c16;
-    f32x4 ap = {0.f, 0.f, 0.f, 0.f}, ag = ap;
 #pragma unroll
     for (int s = 0; s < DV / 32; ++s) {
-      const int v = 32 * s + 8 * g;
-      float x[8];
-      saved(E, CT, j, v, x);
-      const Split b = split8(x);
-      const Split a = value_operand(dop + min(i, row.count - 1) * do_row + v, i < row.count);
+      const Split b = operand(Sh::A_E, true, bj, s), a = operand(Sh::A_DO, LO, bi, s);
       ap = mma(a.hi, b.lo, ap);
       if constexpr (LO) ap = mma(a.lo, b.hi, ap);
       ap = mma(a.hi, b.hi, ap);
-      if (p.delta) {
-        saved(Z, CT, i, v, x);
-        ag = mma3(split8(x), b, ag);
-      }
+      if constexpr (DELTA) ag = mma3(operand(Sh::A_Z, true, bi, s), b, ag);
     }
-    const float bj_ = p.delta ? in.beta[j] : 1.f;
+  }
+  __syncthreads();                                // the squares take the planes' place
+  if (wave < 3) {
+    const int j = 16 * bj + c16;
+    const float bj_ = DELTA ? in.beta[j] : 1.f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int ri = 16 * bi + 4 * g + r;
@@ -174,29 +208,15 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
       }
       dG[ri][j] = ri > j ? -ag[r] * f * in.beta[ri] : 0.f;
     }
-  } else {
+  } else if (wave == 3) {
     for (int x = lane; x < 256; x += 64) dP[x >> 4][16 + (x & 15)] = dG[x >> 4][16 + (x & 15)] = 0.f;
-    if (p.delta) {
-      const int t = lane >> 1;                 // two lanes a token
-      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int v = 8 * (lane & 1); v < DV; v += 16) {
-        const int at = ((v >> 4) * CT + t) * 16 + (v & 15);
-#pragma unroll
-        for (int y = 0; y < 8; y += 4)
-          sum += *reinterpret_cast<const f32x4*>(E + at + y) * *reinterpret_cast<const f32x4*>(Z + at + y);
-      }
-      float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      s += __shfl_xor(s, 1);
-      if (!(lane & 1) && t < row.count) p.dbeta[int64_t(row.first + t) * p.H + h] = s;
-    }
   }
   __syncthreads();
 
   f32x4 be[2];
 #pragma unroll
   for (int tt = 0; tt < 2; ++tt)
-    be[tt] = p.delta ? *reinterpret_cast<const f32x4*>(&in.beta[16 * tt + 4 * g])
+    be[tt] = DELTA ? *reinterpret_cast<const f32x4*>(&in.beta[16 * tt + 4 * g])
                      : f32x4{1.f, 1.f, 1.f, 1.f};
   float ck[8], cq[8];                          // scalar log-decay: sums over this wave's keys
 #pragma unroll
@@ -237,7 +257,7 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
         const Split a = square_operand<false>(dP, tt, lane), at = square_operand<true>(dP, tt, lane);
         aq[x][tt] = mma3(a, bk, aq[x][tt]);
         ac[x][tt] = mma3(at, bq, ac[x][tt]);
-        if (p.delta) {
+        if constexpr (DELTA) {
           const Split b = square_operand<false>(dG, tt, lane), bt = square_operand<true>(dG, tt, lane);
           ar[x][tt] = mma3(b, bk, ar[x][tt]);
           ac[x][tt] = mma3(bt, bk, ac[x][tt]);
@@ -261,12 +281,16 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         const Split a = square_operand<false>(dP, tt, lane);
-        const Split ax = square_operand<false>(dG, tt, lane);
         pq[tt] = mma3(a, tt ? bk1 : bk0, zero);
-        pr[tt] = p.delta ? mma3(ax, tt ? bk1 : bk0, zero) : zero;
+        if constexpr (DELTA) pr[tt] = mma3(square_operand<false>(dG, tt, lane), tt ? bk1 : bk0, zero);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
+        const int tt = e >> 2, r = e & 3;
+        const float m = tt ? m1 : m0;
+        const float out = exp2_of(l[e] - m);
+        aq[x][tt][r] += pq[tt][r] * (DC == DC_BONUS ? exp2_of(lq[e] - m) : out);
+        if constexpr (DELTA) ar[x][tt][r] += pr[tt][r] * out;
         s0[e] = q[e] * exp2_of(lq[e] - m0);
         s1[e] = e < 4 ? 0.f : q[e] * exp2_of(lq[e] - m1);
       }
@@ -274,7 +298,7 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
         pc[tt] = mma3(square_operand<true>(dP, tt, lane), tt ? bq1 : bq0, zero);
-      if (p.delta) {
+      if constexpr (DELTA) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           s0[e] = k[e] * exp2_of(l[e] - m0);
@@ -286,14 +310,8 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
           pc[tt] = mma3(square_operand<true>(dG, tt, lane), tt ? c1 : c0, pc[tt]);
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int tt = e >> 2, r = e & 3;
-        const float m = tt ? m1 : m0;
-        const float out = exp2_of(l[e] - m);
-        aq[x][tt][r] += pq[tt][r] * (DC == DC_BONUS ? exp2_of(lq[e] - m) : out);
-        ar[x][tt][r] += pr[tt][r] * out;
-        ac[x][tt][r] += pc[tt][r] * exp2_of(m - l[e]);
-      }
+      for (int e = 0; e < 8; ++e)
+        ac[x][e >> 2][e & 3] += pc[e >> 2][e & 3] * exp2_of((e < 4 ? m0 : m1) - l[e]);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -322,6 +340,10 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
       for (int e = 0; e < 8; ++e)
         ck[e] += q[e] * aq[x][e >> 2][e & 3] + k[e] * (ar[x][e >> 2][e & 3] - ac[x][e >> 2][e & 3]);
       bnd_all += bnd;
+      // Every product is read here, ahead of the branches around the stores below (see SL's
+      // note on branches and accumulators): the sums may not move past them.
+#pragma unroll
+      for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(ck[e]));
     } else {
       // suffix sums over tokens: over r in the lane, over g across lanes, then the halves
       float sum[2], after[2];
@@ -384,29 +406,31 @@ __global__ __launch_bounds__(256) void grad_kernel(SeqParams p) {
   }
 
   if constexpr (DC == DC_SCALAR) {
-    if (p.dlam) {
+    // without a log-decay too: only the store is left out (what follows the products directly
+    // is the same for every call)
 #pragma unroll
-      for (int d = 1; d < 16; d *= 2) {
-        bnd_all += __shfl_xor(bnd_all, d);
+    for (int d = 1; d < 16; d *= 2) {
+      bnd_all += __shfl_xor(bnd_all, d);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ck[e] += __shfl_xor(ck[e], d);
+      for (int e = 0; e < 8; ++e) ck[e] += __shfl_xor(ck[e], d);
+    }
+    if (c16 == 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tok_sum[wave][state_term(lane, e)] = ck[e];
+      if (g == 0) tok_sum[wave][CT] = bnd_all;
+    }
+    __syncthreads();
+    if (tid < 64) {
+      float s = 0.f;
+      if (tid <= CT)
+#pragma unroll
+        for (int x = 0; x < NW; ++x) s += tok_sum[x][tid];
+#pragma unroll
+      for (int d = 1; d <= CT; d *= 2) {           // suffix sums over lanes 0..CT
+        const float y = __shfl_down(s, d);
+        if (tid + d <= CT) s += y;
       }
-      if (c16 == 0) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) tok_sum[wave][state_term(lane, e)] = ck[e];
-        if (g == 0) tok_sum[wave][CT] = bnd_all;
-      }
-      __syncthreads();
-      if (tid < 64) {
-        float s = 0.f;
-        if (tid <= CT) s = tok_sum[0][tid] + tok_sum[1][tid] + tok_sum[2][tid] + tok_sum[3][tid];
-#pragma unroll
-        for (int d = 1; d <= CT; d *= 2) {         // suffix sums over lanes 0..CT
-          const float y = __shfl_down(s, d);
-          if (tid + d <= CT) s += y;
-        }
-        if (tid < row.count) p.dlam[int64_t(row.first + tid) * p.H + h] = s;
-      }
+      if (p.dlam && tid < row.count) p.dlam[int64_t(row.first + tid) * p.H + h] = s;
     }
   }
 }

@@ -18,11 +18,17 @@ hipError_t start(K* kernel, int64_t grid, int block, const SeqParams& p, hipStre
 template <int DK, bool BWD, typename TIN>
 hipError_t launch_prep_pass(int op, const SeqParams& p, hipStream_t s) {
   const int64_t grid = int64_t(p.max_chunks) * p.H;
-  if (p.raw) return start(&raw_prep_kernel<DK, BWD>, grid, 64, p, s);   // bf16, head-wise decay
-  if (op == DL_OP_RWKV6) return start(&prep_kernel<DC_BONUS, DK, BWD, TIN>, grid, 256, p, s);
-  if (op == DL_OP_KDA || op == DL_OP_GLA) return start(&prep_kernel<DC_KEY, DK, BWD, TIN>, grid, 256, p, s);
-  if constexpr (sizeof(TIN) == 4) return start(&prep_kernel<DC_SCALAR, DK, BWD, TIN>, grid, 256, p, s);
-  return hipErrorInvalidValue;
+  if constexpr (sizeof(TIN) == 2) {
+    if (p.raw && p.delta) return start(&raw_prep_kernel<DK, true, BWD>, grid, 64, p, s);
+    if (p.raw) return start(&raw_prep_kernel<DK, false, BWD>, grid, 64, p, s);
+  } else {
+    if (op == DL_OP_GDN) return start(&prep_kernel<DC_SCALAR, DK, true, BWD, TIN>, grid, 256, p, s);
+    if (op == DL_OP_RETNET || op == DL_OP_LINATTN)
+      return start(&prep_kernel<DC_SCALAR, DK, false, BWD, TIN>, grid, 256, p, s);
+  }
+  if (op == DL_OP_KDA) return start(&prep_kernel<DC_KEY, DK, true, BWD, TIN>, grid, 256, p, s);
+  if (op == DL_OP_GLA) return start(&prep_kernel<DC_KEY, DK, false, BWD, TIN>, grid, 256, p, s);
+  return start(&prep_kernel<DC_BONUS, DK, false, BWD, TIN>, grid, 256, p, s);
 }
 template <int DK, typename TIN>
 hipError_t launch_prep(int op, const SeqParams& p, hipStream_t s) {

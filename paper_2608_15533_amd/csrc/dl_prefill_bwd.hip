@@ -13,13 +13,11 @@ hipError_t start(K* kernel, int64_t grid, int block, const SeqParams& p, hipStre
                          args, 0, s);
 }
 
-template <int DC, int DK, typename TIN>
+template <int DC, int DK, bool DELTA, typename TIN>
 hipError_t launch_grad(const SeqParams& p, hipStream_t s) {
   const int64_t grid = int64_t(p.max_chunks) * p.H;
-  hipError_t e = p.dv == 128 ? start(&grad_kernel<DC, DK, 128, TIN>, grid, 256, p, s)
-                             : start(&grad_kernel<DC, DK, 64, TIN>, grid, 256, p, s);
-  if (DC == DC_BONUS && e == hipSuccess) e = start(&bonus_grad_kernel<DK>, p.H, 1024, p, s);
-  return e;
+  return p.dv == 128 ? start(&grad_kernel<DC, DK, 128, DELTA, TIN>, grid, 4 * DK, p, s)
+                     : start(&grad_kernel<DC, DK, 64, DELTA, TIN>, grid, 4 * DK, p, s);
 }
 
 template <int DK, bool RAW, bool DELTA, typename TIN>
@@ -41,9 +39,15 @@ hipError_t launch_backward_shape(int op, const SeqParams& p, hipStream_t s) {
     if (p.raw) e = p.delta ? launch_walks<DK, true, true, TIN>(p, s) : launch_walks<DK, true, false, TIN>(p, s);
   if (!p.raw) e = p.delta ? launch_walks<DK, false, true, TIN>(p, s) : launch_walks<DK, false, false, TIN>(p, s);
   if (e != hipSuccess) return e;
-  if (op == DL_OP_RWKV6) return launch_grad<DC_BONUS, DK, TIN>(p, s);
-  if (op == DL_OP_KDA || op == DL_OP_GLA) return launch_grad<DC_KEY, DK, TIN>(p, s);
-  return launch_grad<DC_SCALAR, DK, TIN>(p, s);
+  switch (op) {
+    case DL_OP_GDN: return launch_grad<DC_SCALAR, DK, true, TIN>(p, s);
+    case DL_OP_KDA: return launch_grad<DC_KEY, DK, true, TIN>(p, s);
+    case DL_OP_GLA: return launch_grad<DC_KEY, DK, false, TIN>(p, s);
+    case DL_OP_RWKV6:
+      e = launch_grad<DC_BONUS, DK, false, TIN>(p, s);
+      return e != hipSuccess ? e : start(&bonus_grad_kernel<DK>, p.H, 1024, p, s);
+  }
+  return launch_grad<DC_SCALAR, DK, false, TIN>(p, s);   // RetNet, linear attention
 }
 
 }  // namespace

@@ -67,9 +67,10 @@ struct ChunkIn {
     }
   }
 
-  template <int NT>
+  template <int NT, bool DELTA>
   __device__ void load(const SeqParams& p, const ChunkRow& row, int h, int tid) {
     constexpr int PER = 16 / int(sizeof(TIN)), NPC = DK / PER, NI = CT * NPC / NT;
+    static_assert(CT * NPC % NT == 0 && CT * DK / 4 % NT == 0, "whole rounds");
     u32x4 kk[NI], qq[NI];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -95,7 +96,7 @@ struct ChunkIn {
     }
     float b = 0.f;
     if (tid < CT) {
-      if (tid < row.count && p.delta) b = p.beta[int64_t(row.first + tid) * p.H + h];
+      if (DELTA && tid < row.count) b = p.beta[int64_t(row.first + tid) * p.H + h];
       beta[tid] = b;
     }
     if (tid == 0) wide = 0;
@@ -147,7 +148,7 @@ struct ChunkIn {
 // of the workgroup's waves; by all of them, pair by pair, where a block decays too far.  On
 // fp32 MFMA: the operands are used once, so splitting them (24 instructions for eight values)
 // would cost more than the matrix cores' slower fp32 rate, which nothing else here waits for.
-template <int DC, int DK, typename TIN>
+template <int DC, int DK, bool DELTA, typename TIN>
 __device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[SL], float (*P)[SL],
                               float* diag, const SeqParams& p, int h, int tid) {
   const int lane = tid & 63, wave = tid >> 6, c16 = lane & 15, g = lane >> 4;
@@ -205,7 +206,7 @@ __device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[SL], fl
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if (DC != DC_BONUS && p.delta)
+        if constexpr (DELTA)
           ag[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(ak[e], b[e], ag[e & 1], 0, 0, 0);
         ap[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(aq[e], b[e], ap[e & 1], 0, 0, 0);
       }
@@ -306,8 +307,8 @@ __device__ __forceinline__ void put(unsigned char* base, int half, int unit, con
 }
 
 // The squares from LDS matrices, by NTH threads.  BRIEF: P's second half is not wanted.
-template <int NTH, bool BWD, bool BRIEF>
-__device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& w, bool delta,
+template <int NTH, bool DELTA, bool BWD, bool BRIEF>
+__device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& w,
                                             const float (*P)[SL], const float (*N)[SL],
                                             const float (*M)[SL], const float* beta, int tid) {
 #pragma unroll
@@ -324,7 +325,7 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
       row(P, 1.f);
       put<!BRIEF>(blk + w.p(), -WsLayout::SQ, x, a);
     }
-    if (delta) {
+    if constexpr (DELTA) {
       row(N, BWD ? 1.f : beta[i]);
       put(blk + w.n(), WsLayout::SQ, x, a);
     }
@@ -332,7 +333,7 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
 #pragma unroll
       for (int e = 0; e < 8; ++e) a[e] = P[state_term(lane, e)][i];
       put(blk + w.pt(), WsLayout::SQ, x, a);
-      if (delta) {
+      if constexpr (DELTA) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] = M[state_term(lane, e)][i];
         put(blk + w.mt(), WsLayout::SQ, x, a);
@@ -342,7 +343,7 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
 }
 
 // BWD: for the backward pass.
-template <int DC, int DK, bool BWD, typename TIN>
+template <int DC, int DK, bool DELTA, bool BWD, typename TIN>
 __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
   constexpr bool BRIEF = !BWD && sizeof(TIN) == 2;
   __shared__ ChunkIn<DC, DK, TIN> in;
@@ -355,10 +356,10 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
   const WsLayout w{DK, p.dv, false, BWD};
   unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
 
-  in.template load<256>(p, row, h, tid);
-  pair_products<DC, DK, TIN>(in, G, P, diag, p, h, tid);
+  in.template load<256, DELTA>(p, row, h, tid);
+  pair_products<DC, DK, DELTA, TIN>(in, G, P, diag, p, h, tid);
   // One wave solves while the others go on to the planes.
-  if (p.delta && tid < 64) solve<BWD>(G, M, in.beta, tid);
+  if (DELTA && tid < 64) solve<BWD>(G, M, in.beta, tid);
 
   float* dec = reinterpret_cast<float*>(blk + w.dec());
   float* beta = reinterpret_cast<float*>(blk + w.beta());
@@ -380,18 +381,18 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
       lT[e] = k[e] * exp2_of(lT[e] - l[e]);
       k[e] *= f[e];
     }
-    if (p.delta) put(blk + w.kh(), w.plane(), at, k);
+    if constexpr (DELTA) put(blk + w.kh(), w.plane(), at, k);
     put<!BRIEF>(blk + w.qh(), -w.plane(), at, q);
     put(blk + w.kb(), w.plane(), at, lT);
   }
   __syncthreads();
-  put_squares<256, BWD, BRIEF>(blk, w, p.delta, P, G, M, in.beta, tid);
+  put_squares<256, DELTA, BWD, BRIEF>(blk, w, P, G, M, in.beta, tid);
 }
 
 // The same for bf16 keys and queries with one log-decay per head or none, one wave per
 // (chunk, head): the operands of k k^T and q k^T come straight from memory, exact in bf16, and
 // only the squares and the row factors are written.
-template <int DK, bool BWD>
+template <int DK, bool DELTA, bool BWD>
 __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   constexpr int NKS = DK / 32;
   __shared__ __attribute__((aligned(16))) float G[CT][SL], P[CT][SL], M[BWD ? CT : 1][SL], betas[CT];
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   const bool live = lane < row.count;
   const int64_t tok = int64_t(row.first + (live ? lane : 0)) * p.H + h;
   float l = live && p.lam ? fmaxf(p.lam[tok], LOG_FLOOR) * LOG2E : 0.f;
-  const float beta = live && p.delta ? p.beta[tok] : 0.f;
+  const float beta = DELTA && live ? p.beta[tok] : 0.f;
 #pragma unroll
   for (int d = 1; d < CT; d *= 2) {
     const float y = __shfl_up(l, d);
@@ -440,7 +441,7 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
     f32x4 ag = {0.f, 0.f, 0.f, 0.f}, ap = ag;
 #pragma unroll
     for (int s = 0; s < NKS; ++s) {
-      if (p.delta) ag = mma(kf[bi][s], kf[bj][s], ag);
+      if constexpr (DELTA) ag = mma(kf[bi][s], kf[bj][s], ag);
       ap = mma(qf[bi][s], kf[bj][s], ap);
     }
     const int j = 16 * bj + c16;
@@ -456,9 +457,9 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) G[4 * g + r][16 + c16] = P[4 * g + r][16 + c16] = 0.f;
   __syncthreads();
-  if (p.delta) solve<BWD>(G, M, betas, lane);
+  if constexpr (DELTA) solve<BWD>(G, M, betas, lane);
   __syncthreads();
-  put_squares<64, BWD, true>(blk, w, p.delta, P, G, M, betas, lane);
+  put_squares<64, DELTA, BWD, true>(blk, w, P, G, M, betas, lane);
 }
 
 }  // namespace dl
