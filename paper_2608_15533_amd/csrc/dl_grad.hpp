@@ -39,14 +39,30 @@ __device__ __forceinline__ void lane_tokens(const float (*m)[LD], int f, int lan
   for (int e = 0; e < 8; ++e) x[e] = m[state_term(lane, e)][16 * f + (lane & 15)];
 }
 
-// A token x token matrix (or its transpose) as an operand over tokens.
+// acc += m b (TR: m^T b) for the result tile of tokens 16 tt.., m lower triangular token x token,
+// b a lane's eight tokens of its key.  On fp32 MFMA: what a pair gives to q_i dq_i it takes from
+// k_j dk''_j, and dlam's suffix sums keep the difference, so both must see the same product (with
+// operands in two bf16 halves dlam of RWKV6 came out 3e-5 off instead of 1e-6).  Four terms an
+// instruction and no splitting: 32 x 24 vector instructions less, 32 slower MFMAs more.
 template <bool TR>
-__device__ __forceinline__ Split square_operand(const float (*m)[SL], int tt, int lane) {
-  float a[8];
-  const int i = 16 * tt + (lane & 15);
+__device__ __forceinline__ f32x4 pair_mma(const float (*m)[SL], int tt, const float* b, f32x4 acc,
+                                          int lane) {
+  const int i = 16 * tt + (lane & 15), t0 = 4 * (lane >> 4);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) a[e] = TR ? m[state_term(lane, e)][i] : m[i][state_term(lane, e)];
-  return split8(a);
+  for (int half = 0; half < 2; ++half) {
+    if (TR ? half < tt : half > tt) continue;     // blocks that are zero
+    f32x4 a;
+    if constexpr (TR) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[e] = m[16 * half + t0 + e][i];
+    } else {
+      a = *reinterpret_cast<const f32x4*>(&m[i][16 * half + t0]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[4 * half + e], acc, 0, 0, 0);
+  }
+  return acc;
 }
 
 template <int DC, int DK, int DV, typename TIN>
@@ -251,16 +267,13 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
 
     // pairs inside the chunk
     if constexpr (DC == DC_SCALAR) {
-      const Split bk = split8(k), bq = split8(q);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        const Split a = square_operand<false>(dP, tt, lane), at = square_operand<true>(dP, tt, lane);
-        aq[x][tt] = mma3(a, bk, aq[x][tt]);
-        ac[x][tt] = mma3(at, bq, ac[x][tt]);
+        aq[x][tt] = pair_mma<false>(dP, tt, k, aq[x][tt], lane);
+        ac[x][tt] = pair_mma<true>(dP, tt, q, ac[x][tt], lane);
         if constexpr (DELTA) {
-          const Split b = square_operand<false>(dG, tt, lane), bt = square_operand<true>(dG, tt, lane);
-          ar[x][tt] = mma3(b, bk, ar[x][tt]);
-          ac[x][tt] = mma3(bt, bk, ac[x][tt]);
+          ar[x][tt] = pair_mma<false>(dG, tt, k, ar[x][tt], lane);
+          ac[x][tt] = pair_mma<true>(dG, tt, k, ac[x][tt], lane);
         }
       }
     } else if (!in.wide) {
@@ -269,20 +282,18 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
       // second (0 there: its factor could overflow); the second half's factors of earlier
       // tokens are at most 1.  For dk'' the two change places.
       const float m0 = in.at(7, key), m1 = in.at(23, key);
-      float kin0[8], kin1[8], s0[8], s1[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        kin0[e] = e < 4 ? k[e] * exp2_of(m0 - l[e]) : 0.f;
-        kin1[e] = k[e] * exp2_of(m1 - l[e]);
-      }
-      const Split bk0 = split8(kin0), bk1 = split8(kin1);
-      f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+      float s0[8], s1[8];
       f32x4 pq[2], pr[2], pc[2];
 #pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        s0[e] = e < 4 ? k[e] * exp2_of(m0 - l[e]) : 0.f;
+        s1[e] = k[e] * exp2_of(m1 - l[e]);
+      }
+#pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
-        const Split a = square_operand<false>(dP, tt, lane);
-        pq[tt] = mma3(a, tt ? bk1 : bk0, zero);
-        if constexpr (DELTA) pr[tt] = mma3(square_operand<false>(dG, tt, lane), tt ? bk1 : bk0, zero);
+        pq[tt] = pair_mma<false>(dP, tt, tt ? s1 : s0, zero, lane);
+        if constexpr (DELTA) pr[tt] = pair_mma<false>(dG, tt, tt ? s1 : s0, zero, lane);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -294,20 +305,16 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
         s0[e] = q[e] * exp2_of(lq[e] - m0);
         s1[e] = e < 4 ? 0.f : q[e] * exp2_of(lq[e] - m1);
       }
-      const Split bq0 = split8(s0), bq1 = split8(s1);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
-        pc[tt] = mma3(square_operand<true>(dP, tt, lane), tt ? bq1 : bq0, zero);
+      for (int tt = 0; tt < 2; ++tt) pc[tt] = pair_mma<true>(dP, tt, tt ? s1 : s0, zero, lane);
       if constexpr (DELTA) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           s0[e] = k[e] * exp2_of(l[e] - m0);
           s1[e] = e < 4 ? 0.f : k[e] * exp2_of(l[e] - m1);
         }
-        const Split c0 = split8(s0), c1 = split8(s1);
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-          pc[tt] = mma3(square_operand<true>(dG, tt, lane), tt ? c1 : c0, pc[tt]);
+        for (int tt = 0; tt < 2; ++tt) pc[tt] = pair_mma<true>(dG, tt, tt ? s1 : s0, pc[tt], lane);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e)

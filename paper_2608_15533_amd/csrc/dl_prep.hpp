@@ -306,7 +306,8 @@ __device__ __forceinline__ void put(unsigned char* base, int half, int unit, con
   if constexpr (LO) *reinterpret_cast<bf16x8*>(base + half + 16 * unit) = s.lo;
 }
 
-// The squares from LDS matrices, by NTH threads.  BRIEF: P's second half is not wanted.
+// The squares from LDS matrices, by NTH threads.  BRIEF: outputs in bf16 (P's second half is then
+// not wanted without the delta rule).
 template <int NTH, bool DELTA, bool BWD, bool BRIEF>
 __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& w,
                                             const float (*P)[SL], const float (*N)[SL],
@@ -323,7 +324,7 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
     };
     if constexpr (!BWD) {
       row(P, 1.f);
-      put<!BRIEF>(blk + w.p(), -WsLayout::SQ, x, a);
+      put<DELTA || !BRIEF>(blk + w.p(), -WsLayout::SQ, x, a);
     }
     if constexpr (DELTA) {
       row(N, BWD ? 1.f : beta[i]);
