@@ -70,7 +70,7 @@ def test_tables(lens, spare):
     check_tables(lens, list(range(len(lens)))[::-1], sum(lens) + spare, len(lens) + 2)
 
 
-@pytest.mark.parametrize("n", [1023, 1024, 1025, 2049, 5000])
+@pytest.mark.parametrize("n", [1023, 1024, 1025, 2049, 4096, 4097, 5000])
 def test_tables_of_many_sequences(n):
     g = np.random.default_rng(n)
     lens = g.integers(0, 70, n).tolist()
