@@ -1,4 +1,6 @@
 // Whole sequences: entry points (checks, then launches) and the forward pass.
+#include <algorithm>
+
 #include "dl_prep.hpp"
 #include "dl_seq.hpp"
 
@@ -37,13 +39,21 @@ hipError_t launch_prep(int op, const SeqParams& p, hipStream_t s) {
 
 template <int DK, bool RAW, bool DELTA, typename TIN>
 hipError_t launch_walk(const SeqParams& p, hipStream_t s) {
-  const int64_t heads = int64_t(p.n) * p.H;
+  const int64_t heads = int64_t(p.n) * p.H, tiles = p.dv / 16;
+  if (p.seg_len) {
+    // columns of values and of M, four tiles a workgroup: one workgroup is of one kind
+    const int64_t segs = int64_t(p.segs) * p.H, cols = tiles + (DELTA ? DK / 16 : 0);
+    hipError_t e = start(&forward_kernel<DK, 1, 4, RAW, DELTA, PASS_SEG, TIN>, segs * (cols / 4), 256, p, s);
+    if (e == hipSuccess) e = start(&join_kernel<DK, RAW, DELTA>, heads * tiles, 4 * DK, p, s);
+    if (e != hipSuccess) return e;
+    return start(&forward_kernel<DK, 1, 4, RAW, DELTA, PASS_OUT, TIN>, segs * (tiles / 4), 256, p, s);
+  }
   const int waves = walk_waves(heads, DK, p.dv, RAW);
-  const int64_t grid = heads * (p.dv / 16 / waves);
+  const int64_t grid = heads * (tiles / waves);
   switch (waves) {
-    case 2: return start(&forward_kernel<DK, 1, 2, RAW, DELTA, TIN>, grid, 128, p, s);
-    case 4: return start(&forward_kernel<DK, 1, 4, RAW, DELTA, TIN>, grid, 256, p, s);
-    default: return start(&forward_kernel<DK, 1, 8, RAW, DELTA, TIN>, grid, 512, p, s);
+    case 2: return start(&forward_kernel<DK, 1, 2, RAW, DELTA, PASS_OUT, TIN>, grid, 128, p, s);
+    case 4: return start(&forward_kernel<DK, 1, 4, RAW, DELTA, PASS_OUT, TIN>, grid, 256, p, s);
+    default: return start(&forward_kernel<DK, 1, 8, RAW, DELTA, PASS_OUT, TIN>, grid, 512, p, s);
   }
 }
 
@@ -87,6 +97,18 @@ bool raw_planes(const dl_desc* d) {
 // The descriptor's own checks are those of a call that drives no rows.
 int check_desc_only(const dl_desc* d) { return dl_readout(d, nullptr, nullptr, nullptr, nullptr, 0, nullptr); }
 
+bool is_delta(const dl_desc* d) { return d->op == DL_OP_GDN || d->op == DL_OP_KDA; }
+
+// Workspace: the chunk blocks, then the segment states.
+size_t block_bytes(const dl_desc* d, int32_t n, int32_t tokens, bool backward) {
+  const WsLayout w{d->dk, d->dv, raw_planes(d), backward};
+  return size_t(w.block()) * size_t(tokens / DL_CHUNK + n) * size_t(d->heads);
+}
+size_t seg_bytes(const dl_desc* d, int32_t n, int32_t tokens) {
+  const SegPlan s = seg_plan(n, tokens, d->heads, d->dv, is_delta(d));
+  return s.len ? size_t(s.segs) * d->heads * seg_floats(d->dk, d->dv, is_delta(d)) * sizeof(float) : 0;
+}
+
 SeqParams params(const dl_desc* d, const void* S_in, const dl_token* tok, const dl_tables* t,
                  int32_t n, int32_t tokens, void* ws) {
   SeqParams p{};
@@ -94,7 +116,7 @@ SeqParams params(const dl_desc* d, const void* S_in, const dl_token* tok, const 
   p.q = tok->q;
   p.k = tok->k;
   p.v = tok->v;
-  p.delta = d->op == DL_OP_GDN || d->op == DL_OP_KDA;
+  p.delta = is_delta(d);
   p.beta = p.delta ? tok->beta : nullptr;
   p.lam = d->op == DL_OP_LINATTN ? nullptr : tok->lam;
   p.u = d->op == DL_OP_RWKV6 ? tok->u : nullptr;
@@ -150,8 +172,9 @@ int dl_prefill_workspace_bytes(const dl_desc* desc, int32_t n, int32_t tokens, i
   DL_TRY(dl::check_desc_only(desc));
   DL_TRY(dl::check_counts(desc, n, tokens));
   if (!bytes) return DL_E_NULL;
-  const dl::WsLayout w{desc->dk, desc->dv, dl::raw_planes(desc), backward != 0};
-  *bytes = size_t(w.block()) * size_t(tokens / DL_CHUNK + n) * size_t(desc->heads);
+  size_t most = dl::block_bytes(desc, n, tokens, false) + dl::seg_bytes(desc, n, tokens);
+  if (backward) most = std::max(most, dl::block_bytes(desc, n, tokens, true));
+  *bytes = most;
   return DL_OK;
 }
 
@@ -167,6 +190,10 @@ int dl_prefill(const dl_desc* desc, const void* S_in, void* S_out, const dl_toke
   dl::SeqParams p = dl::params(desc, S_in, tok, tables, n, tokens, workspace);
   p.S_out = S_out;
   p.o = o;
+  const dl::SegPlan seg = dl::seg_plan(n, tokens, desc->heads, desc->dv, p.delta);
+  p.seg_len = seg.len;
+  p.segs = seg.segs;
+  p.seg = reinterpret_cast<float*>(p.ws + dl::block_bytes(desc, n, tokens, false));
   return dl::launch_forward(desc, p, stream) == hipSuccess ? DL_OK : DL_E_HIP;
 }
 

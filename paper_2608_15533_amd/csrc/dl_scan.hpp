@@ -197,7 +197,9 @@ struct SeqParams {
   float *dbeta, *dlam, *du;
   const int32_t *cu_tokens, *cu_chunks, *chunks, *seq_slot, *order;
   unsigned char* ws;
+  float* seg;            // segment states (seg_len > 0)
   int32_t n, N, B, H, dv, max_chunks;
+  int32_t seg_len, segs;      // chunks of a segment (0: sequences are walked whole), segments
   bool delta, state_bf16, bwd, raw;
 };
 
@@ -210,6 +212,38 @@ inline int walk_waves(int64_t heads, int dk, int dv, bool raw) {
   const int64_t waves = heads * (dv / 16);
   const int64_t two = dk == 64 ? 2048 : raw ? 1024 : 512;   // what workgroups of two keep running
   return waves <= two ? 2 : waves <= 1024 ? 4 : dv / 16;
+}
+
+// Long sequences on few heads: the walk is one chain per sequence and head, and most of the chip
+// has nothing to do.  The state after a segment of chunks is M S + L, S the state before it; so
+// all segments but the last are walked at once for L (from a zero state) and, with the delta
+// rule, for M (from the identity, without values: dk more columns), the states between segments
+// follow by one product each, and then all segments are walked at once for the outputs.  Without
+// the delta rule M is the decay.  That is about 2.3 times the work (1.5 without the delta rule) in
+// as many parallel parts as there is room for, and worth it up to 320 waves (then there are three
+// parts at least) and from 48 chunks a sequence on average.  Workgroups of four waves.
+// Measured, one bf16 sequence, whole call, whole -> in segments, us: GDN 128 x 128, 8 heads of
+// 8192 tokens 337 -> 116, 32 of 3200 152 -> 132, 32 of 1536 81 -> 78, 64 of 2048 (512 waves) 116 ->
+// 130; KDA, the same, 478 -> 188, 240 -> 238, 124 -> 118, 228 -> 238; RWKV6 64 x 64, 40 heads of
+// 4096 129 -> 87.  32 GDN heads of 8192: walk whole 330; in four segments 120 for L and M, 12 for
+// the states, 112 for the outputs; in three 113 + 9 + 140, in five 110 + 15 + 127.
+struct SegPlan {
+  int len, segs;          // chunks of a segment (0: none), room for segments
+};
+inline SegPlan seg_plan(int64_t n, int64_t tokens, int64_t H, int dv, bool delta) {
+  const int64_t waves = n * H * (dv / 16);
+  if (n == 0 || waves > 320) return {0, 0};
+  const int64_t avg = tokens / DL_CHUNK / n;
+  if (avg < 48) return {0, 0};
+  int64_t parts = (delta ? 1024 : 2048) / waves;
+  if (parts > 16) parts = 16;
+  int64_t len = (avg + parts - 1) / parts;
+  if (len < 16) len = 16;
+  return {int(len), int((tokens / DL_CHUNK + n) / len + n)};
+}
+// Floats of one (sequence, segment, head): L (later the segment's first state) and M.
+__host__ __device__ inline int64_t seg_floats(int dk, int dv, bool delta) {
+  return int64_t(dk) * (dv + (delta ? dk : 0));
 }
 
 struct ChunkRow {

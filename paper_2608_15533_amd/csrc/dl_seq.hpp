@@ -47,7 +47,7 @@ __device__ __forceinline__ f32x4 mma_plane(const Split& a, const Split& b, f32x4
   return mma(a.hi, b.hi, acc);
 }
 
-enum PassId { PASS_OUT = 0, PASS_SAVE = 1, PASS_BACK = 2 };
+enum PassId { PASS_OUT = 0, PASS_SAVE = 1, PASS_BACK = 2, PASS_SEG = 3 };
 
 // One chunk's operands on their way from memory to LDS.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, int PASS, typename TIN>
@@ -71,7 +71,7 @@ struct Stage {
   static constexpr int A_N = P_LEN;
   static constexpr int A_KH = A_N + (!BACK && DELTA ? SQ2 : 0);
   static constexpr int HEAD = A_KH + (DELTA ? 2 * PL : 0);
-  static constexpr int Q_LEN = PASS == PASS_SAVE ? 0 : BRIEF ? PL : 2 * PL;
+  static constexpr int Q_LEN = !BACK && !OUT ? 0 : BRIEF ? PL : 2 * PL;
   static constexpr int A_QH = HEAD + Q_LEN - PL;
   static constexpr int A_KB = HEAD + Q_LEN;
   static constexpr int A_DEC = A_KB + 2 * PL;
@@ -79,7 +79,7 @@ struct Stage {
   static constexpr int A_PT = A_DEC + FAC;
   static constexpr int A_MT = A_PT + (BACK ? SQ2 : 0);
   static constexpr int LINEAR = A_MT + (BACK && DELTA ? SQ2 : 0);
-  static constexpr bool WITH_Q = PASS != PASS_SAVE;
+  static constexpr bool WITH_Q = BACK || OUT;
   static constexpr int A_K = LINEAR, A_Q = A_K + (RAW ? HALF : 0);
   static constexpr int A_V = A_Q + (RAW && WITH_Q ? HALF : 0);
   static constexpr int VNP = VC * int(sizeof(TIN)) / 16;       // pieces of a value row
@@ -239,18 +239,42 @@ struct Stage {
   }
 };
 
-// Where a workgroup stands: (sequence, head, first value column).
+// Where a workgroup stands: (sequence, segment, head, first value column) and its chunks.
 struct Walk {
-  int seq, h, slot, v0, c0, c1, first, end;
+  int seq, h, slot, v0, j, c0, c1, first, end;
+  bool last;               // the sequence ends here
+  int64_t seg_at;          // floats into the segment states
   __device__ __forceinline__ int row(int c) const { return first + CT * (c - c0); }
   __device__ __forceinline__ int count(int c) const { return min(CT, end - row(c)); }
 };
+// Segments stand one after the other, sequence by sequence: those of sequence s from here on, room
+// for cu_chunks[s + 1] - cu_chunks[s] chunks, and for one segment at least.
+__device__ __forceinline__ int seg_base(const SeqParams& p, int s) {
+  return max(p.cu_chunks[s], 0) / p.seg_len + s;
+}
+// cols: the columns walked, dv or (segments of a delta rule) dv + dk.  segments: p.seg_len counts,
+// else sequences are walked whole.
 template <int VC>
-__device__ __forceinline__ bool start_walk(const SeqParams& p, int b, Walk& k) {
-  const int nvt = p.dv / VC;
+__device__ __forceinline__ bool start_walk(const SeqParams& p, int b, int cols, bool segments,
+                                           int64_t seg_size, Walk& k) {
+  const int nvt = cols / VC;
   k.v0 = VC * (b % nvt);
   k.h = (b / nvt) % p.H;
-  k.seq = p.order[b / nvt / p.H];              // longest first: none starts when the rest is done
+  const int i = b / nvt / p.H;
+  k.j = 0;
+  if (segments) {                              // the last sequence that starts at i or before
+    int lo = 0, hi = p.n - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (seg_base(p, mid) <= i) lo = mid;
+      else hi = mid - 1;
+    }
+    k.seq = lo;
+    k.j = i - seg_base(p, lo);
+    if (k.j < 0) return false;
+  } else {
+    k.seq = p.order[i];                        // longest first: none starts when the rest is done
+  }
   if (k.seq < 0 || k.seq >= p.n) return false;
   k.slot = p.seq_slot[k.seq];
   if (k.slot < 0 || k.slot >= p.B) return false;
@@ -259,6 +283,17 @@ __device__ __forceinline__ bool start_walk(const SeqParams& p, int b, Walk& k) {
   k.first = max(p.cu_tokens[k.seq], 0);
   k.end = min(p.cu_tokens[k.seq + 1], p.N);
   k.c1 = min(k.c1, k.c0 + (max(k.end - k.first, 0) + CT - 1) / CT);
+  k.last = true;
+  k.seg_at = 0;
+  if (segments) {
+    const int from = k.c0 + k.j * p.seg_len;   // seg_base: at most cu_chunks[seq] + i * seg_len
+    if (k.j > 0 && from >= k.c1) return false;
+    k.first += CT * (from - k.c0);
+    k.c0 = from;
+    k.last = k.c1 - from <= p.seg_len;
+    if (!k.last) k.c1 = from + p.seg_len;
+    k.seg_at = (int64_t(i) * p.H + k.h) * seg_size;
+  }
   return true;
 }
 
@@ -274,6 +309,17 @@ __device__ __forceinline__ void read_state(f32x4 (&S)[NKT][NT], const void* base
         S[f][t][r] = base ? load_state(base, p.state_bf16,
                                        at + int64_t(state_key(f, lane >> 4, r)) * p.dv + 16 * t)
                           : 0.f;
+}
+template <int NKT, int NT>
+__device__ __forceinline__ void read_floats(f32x4 (&S)[NKT][NT], const float* base, int dv, int v,
+                                            int lane) {
+#pragma unroll
+  for (int f = 0; f < NKT; ++f)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        S[f][t][r] = base[int64_t(state_key(f, lane >> 4, r)) * dv + v + 16 * t];
 }
 template <int NKT, int NT>
 __device__ __forceinline__ void write_state(const f32x4 (&S)[NKT][NT], void* base, bool bf16, int dv,
@@ -318,12 +364,17 @@ __device__ __forceinline__ void walk_forward(
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15;
   Walk k;
-  if (!start_walk<St::VC>(p, group, k)) return;
+  constexpr bool SEG = PASS == PASS_SEG;
+  const int cols = p.dv + (SEG && DELTA ? DK : 0);
+  const bool segments = SEG || (OUT && p.seg_len);
+  if (!start_walk<St::VC>(p, group, cols, segments, seg_floats(DK, p.dv, DELTA), k)) return;
+  const bool unit = SEG && DELTA && k.v0 >= p.dv;              // columns of M
+  if (SEG && (k.last || (unit && k.j == 0))) return;           // nobody asks for these
   const WsLayout w{DK, p.dv, RAW, p.bwd};
   const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;        // this lane's first column
   const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
   const int64_t row_stride = int64_t(p.H) * p.dv;
-  const TIN* vals = static_cast<const TIN*>(p.v) + int64_t(k.h) * p.dv + k.v0;
+  const TIN* vals = static_cast<const TIN*>(p.v) + int64_t(k.h) * p.dv + (unit ? 0 : k.v0);
   St st;
   auto block = [&](int c) { return p.ws + (int64_t(c) * p.H + k.h) * w.block(); };
   auto fetch = [&](int c) {
@@ -337,7 +388,10 @@ __device__ __forceinline__ void walk_forward(
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) U[tt][t] = St::values(l, tt, ct0 + t, lane);
+      for (int t = 0; t < NT; ++t) {
+        U[tt][t] = St::values(l, tt, ct0 + t, lane);
+        if (SEG && DELTA && unit) U[tt][t] = zero;             // no values
+      }
       if constexpr (RAW) ff[tt] = St::factor(l, St::A_F, tt, lane);
       if constexpr (DELTA) {
 #pragma unroll
@@ -350,9 +404,9 @@ __device__ __forceinline__ void walk_forward(
     __syncthreads();
     st.store(nxt, k.count(min(c + 1, k.c1 - 1)), tid);
     fetch(c + 2);
-    if constexpr (!OUT) save_tiles<true>(S, block(c) + w.s0(), k.v0 / 16 + ct0, lane);
+    if constexpr (PASS == PASS_SAVE) save_tiles<true>(S, block(c) + w.s0(), k.v0 / 16 + ct0, lane);
 
-    // Kh S, R = V - Kh S, E = N R (PASS_OUT: N holds beta N, and U comes at once)
+    // Kh S, R = V - Kh S, E = N R (but for PASS_SAVE N holds beta N, and U comes at once)
     Split sb[NKS][NT];
     f32x4 X[2][NT];
 #pragma unroll
@@ -373,7 +427,7 @@ __device__ __forceinline__ void walk_forward(
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
       if constexpr (RAW) gf[tt] = St::factor(cur, St::A_G, tt, lane);
-      if constexpr (DELTA && !OUT) be[tt] = St::factor(cur, St::A_BETA, tt, lane);
+      if constexpr (DELTA && PASS == PASS_SAVE) be[tt] = St::factor(cur, St::A_BETA, tt, lane);
     }
     if constexpr (DELTA) {
       Split rb[NT];
@@ -388,7 +442,7 @@ __device__ __forceinline__ void walk_forward(
 #pragma unroll
         for (int t = 0; t < NT; ++t) U[tt][t] = mma3(an[tt], rb[t], zero);
     }
-    if constexpr (!OUT) {
+    if constexpr (PASS == PASS_SAVE) {
       save_tiles<false>(U, block(c) + w.e(), k.v0 / 16 + ct0, lane);
       if constexpr (DELTA) {
 #pragma unroll
@@ -455,7 +509,18 @@ __device__ __forceinline__ void walk_forward(
   };
 
   if (k.c0 < k.c1) fetch(k.c0);
-  read_state(S, p.S_in, p, state_at, lane);
+  float* seg = p.seg + k.seg_at;               // L, then the segment's first state: [dk][dv]; M
+  if (PASS == PASS_SAVE || (SEG ? k.j == 0 : k.j == 0 && k.last))
+    read_state(S, p.S_in, p, state_at, lane);
+  else if constexpr (OUT) read_floats(S, seg, p.dv, v, lane);
+  else if constexpr (SEG)
+#pragma unroll
+    for (int f = 0; f < NKT; ++f)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          S[f][t][r] = unit && state_key(f, lane >> 4, r) == v + 16 * t - p.dv ? 1.f : 0.f;
   if (k.c0 < k.c1) {
     st.store(lds[0], k.count(k.c0), tid);
     fetch(k.c0 + 1);
@@ -471,10 +536,17 @@ __device__ __forceinline__ void walk_forward(
         if (++c == k.c1) break;
       }
     } else {
+#pragma unroll 1
       for (int c = k.c0; c < k.c1; ++c) chunk(c, lds[(c - k.c0) & 1], lds[(c - k.c0 + 1) & 1]);
     }
   }
-  if constexpr (OUT) write_state(S, p.S_out, p.state_bf16, p.dv, state_at, lane);
+  if constexpr (OUT) {
+    if (k.last) write_state(S, p.S_out, p.state_bf16, p.dv, state_at, lane);
+  }
+  if constexpr (SEG) {
+    if (unit) write_state(S, seg + DK * p.dv, false, DK, v - p.dv, lane);
+    else write_state(S, seg, false, p.dv, v, lane);
+  }
 }
 
 // Backward over the chunks, last to first, with D the gradient of the state after a chunk:
@@ -490,7 +562,7 @@ __device__ __forceinline__ void walk_backward(
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15;
   Walk k;
-  if (!start_walk<St::VC>(p, group, k)) return;
+  if (!start_walk<St::VC>(p, group, p.dv, false, 0, k)) return;
   const WsLayout w{DK, p.dv, RAW, true};
   const int ct0 = wave * NT, v = k.v0 + 16 * ct0 + c16;
   const int64_t state_at = (int64_t(k.slot) * p.H + k.h) * DK * p.dv + v;
@@ -614,6 +686,7 @@ __device__ __forceinline__ void walk_backward(
         if (--c < k.c0) break;
       }
     } else {
+#pragma unroll 1
       for (int c = k.c1 - 1; c >= k.c0; --c)
         chunk(c, lds[(k.c1 - 1 - c) & 1], lds[(k.c1 - c) & 1]);
     }
@@ -621,11 +694,100 @@ __device__ __forceinline__ void walk_backward(
   if (p.S_out) write_state(D, p.S_out, p.state_bf16, p.dv, state_at, lane);
 }
 
-template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
+template <int DK, int NT, int NW, bool RAW, bool DELTA, int PASS, typename TIN>
 __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
   __shared__ __attribute__((aligned(16))) unsigned char
-      lds[2][Stage<DK, NT, NW, RAW, DELTA, PASS_OUT, TIN>::BYTES];
-  walk_forward<DK, NT, NW, RAW, DELTA, PASS_OUT, TIN>(p, blockIdx.x, lds);
+      lds[2][Stage<DK, NT, NW, RAW, DELTA, PASS, TIN>::BYTES];
+  walk_forward<DK, NT, NW, RAW, DELTA, PASS, TIN>(p, blockIdx.x, lds);
+}
+
+// The states between a sequence's segments, one after the other, a workgroup for 16 columns and a
+// wave for 16 keys of them: S_1 = L_0 (segment 0 started from the initial state), S_j+1 = M_j S_j +
+// L_j; S_j takes L_j's place, and the initial state that of L_0: where S_out is S_in, the last
+// segment writes it while the first one may not have started.  Without the delta rule M_j is the decay over the segment.  A step is
+// a chain of one load, one product and one exchange of S through LDS; M_j and L_j do not depend on
+// S and are fetched a step ahead.
+template <int DK, bool RAW, bool DELTA>
+__global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
+  constexpr int NKS = DK / 32, PITCH = 18;     // 8 rows further: 16 banks further
+  __shared__ float sh[2][DK * PITCH];
+  const int lane = threadIdx.x & 63, f = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
+  const int nvt = p.dv / 16, b = blockIdx.x, v = 16 * (b % nvt) + c16, h = b / nvt % p.H;
+  const int seq = b / nvt / p.H, slot = p.seq_slot[seq];
+  if (slot < 0 || slot >= p.B) return;
+  const int c0 = max(p.cu_chunks[seq], 0), c1 = min(p.cu_chunks[seq + 1], p.max_chunks);
+  const int parts = (c1 - c0 + p.seg_len - 1) / p.seg_len, base = seg_base(p, seq);
+  if (parts <= 1) return;
+  const int64_t size = seg_floats(DK, p.dv, DELTA);
+  auto at = [&](int j) { return p.seg + (int64_t(base + j) * p.H + h) * size; };
+  auto column = [&](int j) {                   // this lane's keys of L_j or S_j
+    const float* x = at(j) + int64_t(state_key(f, g, 0)) * p.dv + v;
+    return f32x4{x[0], x[p.dv], x[2 * p.dv], x[3 * p.dv]};
+  };
+  auto place = [&](int j, f32x4 S) {
+    float* x = at(j) + int64_t(state_key(f, g, 0)) * p.dv + v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) x[r * p.dv] = S[r];
+  };
+
+  f32x4 S = column(0), L = column(1), first = {0.f, 0.f, 0.f, 0.f};
+  if (p.S_in) {
+    const int64_t x = ((int64_t(slot) * p.H + h) * DK + state_key(f, g, 0)) * p.dv + v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) first[r] = load_state(p.S_in, p.state_bf16, x + r * p.dv);
+  }
+  place(0, first);
+  if constexpr (DELTA) {
+    auto rows = [&](int j, f32x4 (&m)[2 * NKS]) {
+      const float* M = at(j) + DK * p.dv + state_key(f, c16 >> 2, c16 & 3) * DK + 8 * g;
+#pragma unroll
+      for (int s = 0; s < 2 * NKS; ++s)
+        m[s] = *reinterpret_cast<const f32x4*>(M + 32 * (s >> 1) + 4 * (s & 1));
+    };
+    f32x4 m[2 * NKS];
+    rows(1, m);
+    for (int j = 1; j + 1 < parts; ++j) {
+      float* x = sh[j & 1];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[(state_key(f, g, 0) + r) * PITCH + c16] = S[r];
+      place(j, S);
+      Split am[NKS];
+#pragma unroll
+      for (int s = 0; s < NKS; ++s) {
+        float a[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = m[2 * s + (e >> 2)][e & 3];
+        am[s] = split8(a);
+      }
+      S = L;
+      const int next = min(j + 1, parts - 2);  // the last one's M is never made
+      L = column(next);
+      rows(next, m);
+      __syncthreads();
+#pragma unroll
+      for (int s = 0; s < NKS; ++s) {
+        float a[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = x[(32 * s + 8 * g + e) * PITCH + c16];
+        S = mma3(am[s], split8(a), S);
+      }
+    }
+  } else {
+    const WsLayout w{DK, p.dv, RAW, false};
+    for (int j = 1; j + 1 < parts; ++j) {
+      f32x4 d = {1.f, 1.f, 1.f, 1.f};
+#pragma unroll 8
+      for (int c = c0 + j * p.seg_len; c < c0 + (j + 1) * p.seg_len; ++c) {
+        const unsigned char* blk = p.ws + (int64_t(c) * p.H + h) * w.block();
+        if constexpr (RAW) d *= *reinterpret_cast<const float*>(blk + w.f() + 4 * (CT - 1));
+        else d *= *reinterpret_cast<const f32x4*>(blk + w.dec() + 4 * state_key(f, g, 0));
+      }
+      place(j, S);
+      S = d * S + L;
+      L = column(min(j + 1, parts - 2));
+    }
+  }
+  place(parts - 1, S);
 }
 
 // The backward pass's two walks in one launch: neither needs the other, and each alone leaves
