@@ -248,7 +248,8 @@ typedef struct {
 } dl_tables;
 
 /* Build the tables from lens [n] (device) and slots (device int32 [n], or NULL: sequence i
- * has slot i, which requires n <= num_slots).  What only the device can see is ORed into
+ * has slot i, which requires n <= num_slots; ids of sequences that run are distinct, two on
+ * one slot race on its final state).  What only the device can see is ORed into
  * *err (device, may be NULL): 1 = a slot id outside [0, num_slots) (the sequence's slot
  * becomes -1, and dl_prefill and dl_prefill_backward skip it), 4 = a length below 0 (taken
  * as 0) or past the N token rows (cut there).  n == 0 is a no-op. */
@@ -265,7 +266,10 @@ int dl_prefill_workspace_bytes(const dl_desc* desc, int32_t n, int32_t tokens,
  * every sequence of the tables, from S_in[slot] (S_in == NULL: zero) to S_out[slot] (both
  * [B,H,dk,dv] of state_dtype; S_out may be S_in), with o [N,H,dv] in in_dtype -- a prompt's
  * outputs go on to products in that type, and a state read back in it would not gain from
- * wider ones.  tok holds N rows.  All arithmetic keeps fp32 accuracy; S_out is rounded once.
+ * wider ones.  tok holds N rows.  Sums, decays and states are fp32; products of fp32 factors
+ * take each as a sum of two bf16 numbers, good to 2^-17, so that fp32 results are within some
+ * 1e-5 of the exact ones, relative to their norm; S_out is rounded once.  Outputs must not
+ * overlap inputs, S_out = S_in apart.
  * The log of a DeltaLog state is not looked at: flush it first (dl_merge without a token)
  * where S_in is the base of a state with a log, and reset len where S_out is.
  * tables: as dl_chunk_tables left them for the same n and N (row_slot is not read).
@@ -296,7 +300,8 @@ typedef struct {
  * final states, state_dtype; NULL: zero) to every gradient, for the same S_in, tok and
  * tables as the forward call.  Nothing is kept from the forward call: the states are
  * computed again.  S_in is read, so a forward call that wrote its states in place has
- * destroyed what this call needs.  dS must not alias S_in; it may alias dS_out.
+ * destroyed what this call needs.  dS may be dS_out; no other gradient may overlap an input or
+ * another gradient (dv is written while v is still read).
  * workspace: dl_prefill_workspace_bytes(desc, n, N, 1, ..) bytes, 256-byte aligned. */
 int dl_prefill_backward(const dl_desc* desc, const void* S_in, const dl_token* tok,
                         const void* d_o, const void* dS_out, const dl_grads* grads,

@@ -1,7 +1,8 @@
 """ctypes binding of libdeltalog.so -- argument marshalling only.
 
 The entry points keep the C names (``dl_eager_step``, ``dl_append_step``, ``dl_merge``,
-``dl_readout``) and take torch CUDA tensors; each call checks layouts, builds the C
+``dl_readout``; for whole sequences ``dl_chunk_tables``, ``dl_prefill``,
+``dl_prefill_backward``) and take torch CUDA tensors; each call checks layouts, builds the C
 structs and calls the library, which launches the HIP kernels on the current (or the
 given) stream.  No arithmetic of the method happens here.  PyTorch is used only to
 own device memory and to name the stream.
@@ -437,25 +438,24 @@ def prefill_workspace(desc, n, tokens, backward=False, device="cuda"):
                        dtype=torch.uint8, device=device)
 
 
-def _sequences(desc, tok, tables, workspace, S_in):
+def _sequences(desc, tok, tables, workspace, *others):
     if workspace is None or not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous device tensor (see prefill_workspace)")
-    _on_current_device(tok.tensors[0], tables.err, workspace, S_in)
+    _on_current_device(*tok.tensors, tables.err, workspace, *others)
     if tok.n != tables.tokens:
         raise ValueError(f"the token holds {tok.n} rows but the tables are for {tables.tokens}")
-    if S_in is not None:
-        _need(S_in, "S_in", state_torch_dtype(desc),
-              (desc.num_slots, desc.heads, desc.dk, desc.dv))
     return (workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
 
 def dl_prefill(desc, S_in, S_out, tok, o, tables, workspace, stream=None):
     """The recurrence over the whole sequences of ``tables``: from S_in[slot] (None: zero) to
     S_out[slot] (may be S_in), o [N,H,dv] in the input dtype."""
-    wp, wn = _sequences(desc, tok, tables, workspace, S_in)
-    _need(S_out, "S_out", state_torch_dtype(desc),
-          (desc.num_slots, desc.heads, desc.dk, desc.dv))
+    state = (state_torch_dtype(desc), (desc.num_slots, desc.heads, desc.dk, desc.dv))
+    if S_in is not None:
+        _need(S_in, "S_in", *state)
+    _need(S_out, "S_out", *state)
     _need(o, "o", tok.tensors[2].dtype, (tok.n, desc.heads, desc.dv))
+    wp, wn = _sequences(desc, tok, tables, workspace, S_in, S_out, o)
     _check(_lib.dl_prefill(ctypes.byref(desc), _ptr(S_in), _ptr(S_out), ctypes.byref(tok.struct),
                            _ptr(o), ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,
                            _stream(stream)), "dl_prefill")
@@ -464,11 +464,12 @@ def dl_prefill(desc, S_in, S_out, tok, o, tables, workspace, stream=None):
 def dl_prefill_backward(desc, S_in, tok, d_o, dS_out, grads, tables, workspace, stream=None):
     """Gradients of dl_prefill into ``grads`` (``Grads``) from d_o [N,H,dv] and dS_out
     [B,H,dk,dv] (None: zero).  The forward call must have left S_in as it was."""
-    wp, wn = _sequences(desc, tok, tables, workspace, S_in)
+    state = (state_torch_dtype(desc), (desc.num_slots, desc.heads, desc.dk, desc.dv))
     _need(d_o, "d_o", tok.tensors[2].dtype, (tok.n, desc.heads, desc.dv))
-    if dS_out is not None:
-        _need(dS_out, "dS_out", state_torch_dtype(desc),
-              (desc.num_slots, desc.heads, desc.dk, desc.dv))
+    for name, t in (("S_in", S_in), ("dS_out", dS_out)):
+        if t is not None:
+            _need(t, name, *state)
+    wp, wn = _sequences(desc, tok, tables, workspace, S_in, d_o, dS_out, grads.dq)
     _check(_lib.dl_prefill_backward(ctypes.byref(desc), _ptr(S_in), ctypes.byref(tok.struct),
                                     _ptr(d_o), _ptr(dS_out), ctypes.byref(grads.struct),
                                     ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,

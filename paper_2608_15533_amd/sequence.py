@@ -42,7 +42,7 @@ def delta_scan(op, q, k, v, lam=None, beta=None, u=None, S0=None, lens=None, sta
     the operator needs them (fp32); lens [n] int32 on the device (None: one sequence of N
     tokens); S0 [n,H,dk,dv] initial states in ``state_dtype`` (None: zero).  Returns (o
     [N,H,dv], final states [n,H,dk,dv]); o and every gradient are 0 in rows behind the last
-    sequence.  All tensors contiguous.  Gradients once; the states are computed again for
+    sequence; lengths that run past the N rows are cut there.  All tensors contiguous.  Gradients once; the states are computed again for
     them, so a call keeps its inputs and nothing else."""
     N, H, dk = q.shape
     if lens is None:
