@@ -694,11 +694,23 @@ __device__ __forceinline__ void walk_backward(
   if (p.S_out) write_state(D, p.S_out, p.state_bf16, p.dv, state_at, lane);
 }
 
+// Workgroups go round the chip's eight XCDs, each with an L2 of its own.  The `share` workgroups of
+// one head read the same operands, chunk by chunk at about the same time, so they are placed on
+// one XCD: of `groups` workgroups, of which every ROUND-th lands on the same one, which one this is.
+template <int ROUND>
+__device__ __forceinline__ int xcd_place(int b, int groups, int share) {
+  const int block = ROUND * share;
+  if (b >= groups / block * block) return b;
+  const int in = b % block;
+  return b - in + in % ROUND * share + in / ROUND;
+}
+
 template <int DK, int NT, int NW, bool RAW, bool DELTA, int PASS, typename TIN>
 __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
   __shared__ __attribute__((aligned(16))) unsigned char
       lds[2][Stage<DK, NT, NW, RAW, DELTA, PASS, TIN>::BYTES];
-  walk_forward<DK, NT, NW, RAW, DELTA, PASS, TIN>(p, blockIdx.x, lds);
+  const int share = (p.dv + (PASS == PASS_SEG && DELTA ? DK : 0)) / (16 * NT * NW);
+  walk_forward<DK, NT, NW, RAW, DELTA, PASS, TIN>(p, xcd_place<8>(blockIdx.x, gridDim.x, share), lds);
 }
 
 // The states between a sequence's segments, one after the other, a workgroup for 16 columns and a
@@ -799,12 +811,13 @@ __global__ __launch_bounds__(64 * NW) void both_kernel(SeqParams p) {
   using Back = Stage<DK, NT, NW, RAW, DELTA, PASS_BACK, TIN>;
   constexpr int BYTES = 2 * (Save::BYTES > Back::BYTES ? Save::BYTES : Back::BYTES);
   __shared__ __attribute__((aligned(16))) unsigned char lds[BYTES];
+  const int group = xcd_place<4>(blockIdx.x >> 1, gridDim.x >> 1, p.dv / (16 * NT * NW));
   if (blockIdx.x & 1)
     walk_forward<DK, NT, NW, RAW, DELTA, PASS_SAVE, TIN>(
-        p, blockIdx.x >> 1, *reinterpret_cast<unsigned char(*)[2][Save::BYTES]>(&lds));
+        p, group, *reinterpret_cast<unsigned char(*)[2][Save::BYTES]>(&lds));
   else
     walk_backward<DK, NT, NW, RAW, DELTA, TIN>(
-        p, blockIdx.x >> 1, *reinterpret_cast<unsigned char(*)[2][Back::BYTES]>(&lds));
+        p, group, *reinterpret_cast<unsigned char(*)[2][Back::BYTES]>(&lds));
 }
 
 }  // namespace dl
