@@ -344,6 +344,8 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
 }
 
 // BWD: for the backward pass.
+// Bound by memory: 12345 tokens, 32 heads of 128 keys (KDA, bf16) 180 us for 417 MB read and
+// 621 MB written (the planes), 5.8 TB/s, where a large copy reaches 5.55.
 template <int DC, int DK, bool DELTA, bool BWD, typename TIN>
 __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
   constexpr bool BRIEF = !BWD && sizeof(TIN) == 2;
@@ -392,7 +394,8 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
 
 // The same for bf16 keys and queries with one log-decay per head or none, one wave per
 // (chunk, head): the operands of k k^T and q k^T come straight from memory, exact in bf16, and
-// only the squares and the row factors are written.
+// only the squares and the row factors are written.  Bound by memory: 32768 tokens, 32 heads of
+// 128 keys (GDN) 150 us for 613 MB read and 281 MB written, 6 TB/s.
 template <int DK, bool DELTA, bool BWD>
 __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   constexpr int NKS = DK / 32;
