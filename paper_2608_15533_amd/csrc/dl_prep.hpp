@@ -298,17 +298,15 @@ __device__ __forceinline__ void solve(float (*G)[SL], float (*M)[SL], const floa
   }
 }
 
-// Eight values as two bf16 halves, or the first alone.
-template <bool LO = true>
+// Eight values as two bf16 halves.
 __device__ __forceinline__ void put(unsigned char* base, int half, int unit, const float* x) {
   const Split s = split8(x);
   *reinterpret_cast<bf16x8*>(base + 16 * unit) = s.hi;
-  if constexpr (LO) *reinterpret_cast<bf16x8*>(base + half + 16 * unit) = s.lo;
+  *reinterpret_cast<bf16x8*>(base + half + 16 * unit) = s.lo;
 }
 
-// The squares from LDS matrices, by NTH threads.  BRIEF: outputs in bf16 (P's second half is then
-// not wanted without the delta rule).
-template <int NTH, bool DELTA, bool BWD, bool BRIEF>
+// The squares from LDS matrices, by NTH threads.
+template <int NTH, bool DELTA, bool BWD>
 __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& w,
                                             const float (*P)[SL], const float (*N)[SL],
                                             const float (*M)[SL], const float* beta, int tid) {
@@ -324,7 +322,7 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
     };
     if constexpr (!BWD) {
       row(P, 1.f);
-      put<DELTA || !BRIEF>(blk + w.p(), -WsLayout::SQ, x, a);
+      put(blk + w.p(), WsLayout::SQ, x, a);
     }
     if constexpr (DELTA) {
       row(N, BWD ? 1.f : beta[i]);
@@ -348,7 +346,6 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
 // 621 MB written (the planes), 5.8 TB/s, where a large copy reaches 5.55.
 template <int DC, int DK, bool DELTA, bool BWD, typename TIN>
 __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
-  constexpr bool BRIEF = !BWD && sizeof(TIN) == 2;
   __shared__ ChunkIn<DC, DK, TIN> in;
   __shared__ __attribute__((aligned(16))) float G[CT][SL], P[CT][SL], M[BWD ? CT : 1][SL];
   __shared__ float diag[CT];
@@ -385,11 +382,11 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
       k[e] *= f[e];
     }
     if constexpr (DELTA) put(blk + w.kh(), w.plane(), at, k);
-    put<!BRIEF>(blk + w.qh(), -w.plane(), at, q);
+    put(blk + w.qh(), w.plane(), at, q);
     put(blk + w.kb(), w.plane(), at, lT);
   }
   __syncthreads();
-  put_squares<256, DELTA, BWD, BRIEF>(blk, w, P, G, M, in.beta, tid);
+  put_squares<256, DELTA, BWD>(blk, w, P, G, M, in.beta, tid);
 }
 
 // The same for bf16 keys and queries with one log-decay per head or none, one wave per
@@ -463,7 +460,7 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   __syncthreads();
   if constexpr (DELTA) solve<BWD>(G, M, betas, lane);
   __syncthreads();
-  put_squares<64, DELTA, BWD, true>(blk, w, P, G, M, betas, lane);
+  put_squares<64, DELTA, BWD>(blk, w, P, G, M, betas, lane);
 }
 
 }  // namespace dl

@@ -154,18 +154,18 @@ __device__ __forceinline__ bf16x8 cols_operand(const unsigned char* plane, int f
 //           scale token rows of fp32 products instead.
 //   squares N (beta N where no backward pass asks for E), P and (backward) P^T, M^T: token x token, two halves, in fragment order: the
 //           eight terms (state order) a lane feeds one MFMA are 16 consecutive bytes.
-// The order makes what one pass reads of a block two runs of bytes: outputs of bf16 take the
-// first halves of P and Qh alone, a pass without outputs neither.
+// The first half lies before the second.  The order makes what one pass reads of a block two runs
+// of bytes (a pass without outputs takes neither P nor Qh).
 struct WsLayout {
   int dk, dv;
   bool raw, bwd;
   static constexpr int SQ = CT * CT * 2;                                 // one square, one half
   __host__ __device__ int plane() const { return CT * dk * 2; }          // one plane, one half
-  __host__ __device__ int p() const { return SQ; }                       // lo before hi
+  __host__ __device__ int p() const { return 0; }
   __host__ __device__ int n() const { return 2 * SQ; }
   __host__ __device__ int kh() const { return 4 * SQ; }
-  __host__ __device__ int qh() const { return kh() + (raw ? 0 : 3 * plane()); }   // lo before hi
-  __host__ __device__ int kb() const { return qh() + (raw ? 0 : plane()); }
+  __host__ __device__ int qh() const { return kh() + (raw ? 0 : 2 * plane()); }
+  __host__ __device__ int kb() const { return qh() + (raw ? 0 : 2 * plane()); }
   __host__ __device__ int dec() const { return kb() + (raw ? 0 : 2 * plane()); }  // fp32 [dk] e^{l_T} (not raw)
   __host__ __device__ int beta() const { return dec() + dk * 4; }        // fp32 [CT]
   __host__ __device__ int f() const { return beta() + CT * 4; }          // fp32 [CT] (raw)

@@ -13,13 +13,12 @@
 
 namespace dl {
 
-// A square's operand; LO: bytes from the first half to the second, or 0 for the first alone.
-template <int LO = WsLayout::SQ>
+// A square's operand.
 __device__ __forceinline__ Split square_at(const unsigned char* lds, int tt, int lane) {
   const unsigned char* at = lds + 16 * (tt * 64 + lane);
   Split s;
   s.hi = *reinterpret_cast<const bf16x8*>(at);
-  if constexpr (LO != 0) s.lo = *reinterpret_cast<const bf16x8*>(at + LO);
+  s.lo = *reinterpret_cast<const bf16x8*>(at + WsLayout::SQ);
   return s;
 }
 
@@ -57,29 +56,20 @@ struct Stage {
   static constexpr int PL = RAW ? 0 : HALF, SQ = WsLayout::SQ, SQ2 = 2 * SQ;
   static constexpr int FAC = 4 * DK + 12 * CT;
   static constexpr bool BACK = PASS == PASS_BACK, OUT = PASS == PASS_OUT;
-  // Outputs that are rounded to bf16 take Qh S and P U with second halves left out: Qh's, S's, U's
-  // where nothing else needs it (raw planes), and P's without the delta rule (U is V then, exact
-  // in bf16).  Each rounding is at most 2^-9 of its factor, as the output's own is; measured
-  // against 64 bits the outputs are 2.1e-3 to 2.4e-3 off with them and 1.7e-3 without, for 5 to 8%
-  // of the walk's time.
-  static constexpr bool BRIEF = OUT && sizeof(TIN) == 2;
+  static constexpr bool WITH_Q = BACK || OUT;
   // LDS offsets, of the workspace block: first P, N, Kh (what of them the pass needs), then Qh,
-  // Kb, the factors, and backward P^T, M^T.  A_P and A_QH are the first halves; the second lie
-  // before them.
-  static constexpr int P_LEN = OUT ? (BRIEF && !DELTA ? SQ : SQ2) : 0;
-  static constexpr int A_P = P_LEN - SQ;
-  static constexpr int A_N = P_LEN;
+  // Kb, the factors, and backward P^T, M^T.
+  static constexpr int A_P = 0;
+  static constexpr int A_N = OUT ? SQ2 : 0;
   static constexpr int A_KH = A_N + (!BACK && DELTA ? SQ2 : 0);
   static constexpr int HEAD = A_KH + (DELTA ? 2 * PL : 0);
-  static constexpr int Q_LEN = !BACK && !OUT ? 0 : BRIEF ? PL : 2 * PL;
-  static constexpr int A_QH = HEAD + Q_LEN - PL;
-  static constexpr int A_KB = HEAD + Q_LEN;
+  static constexpr int A_QH = HEAD;
+  static constexpr int A_KB = A_QH + (WITH_Q ? 2 * PL : 0);
   static constexpr int A_DEC = A_KB + 2 * PL;
   static constexpr int A_BETA = A_DEC + 4 * DK, A_F = A_BETA + 4 * CT, A_G = A_F + 4 * CT;
   static constexpr int A_PT = A_DEC + FAC;
   static constexpr int A_MT = A_PT + (BACK ? SQ2 : 0);
   static constexpr int LINEAR = A_MT + (BACK && DELTA ? SQ2 : 0);
-  static constexpr bool WITH_Q = BACK || OUT;
   static constexpr int A_K = LINEAR, A_Q = A_K + (RAW ? HALF : 0);
   static constexpr int A_V = A_Q + (RAW && WITH_Q ? HALF : 0);
   static constexpr int VNP = VC * int(sizeof(TIN)) / 16;       // pieces of a value row
@@ -97,8 +87,8 @@ struct Stage {
   __device__ __forceinline__ void load(const SeqParams& p, const unsigned char* blk, int first,
                                        int count, int h, const TIN* vals, int tid) {
     const WsLayout w{DK, p.dv, RAW, p.bwd};
-    const uint32_t from = BACK ? w.kh() : OUT ? w.p() + SQ - P_LEN : w.n();
-    const uint32_t gap = (BACK || OUT ? w.qh() + PL - Q_LEN : w.kb()) - HEAD;
+    const uint32_t from = BACK ? w.kh() : OUT ? w.p() : w.n();
+    const uint32_t gap = (WITH_Q ? w.qh() : w.kb()) - HEAD;
 #pragma unroll
     for (int i = 0; i < NLIN; ++i) {
       uint32_t x = 16 * (i * T + tid);
@@ -210,22 +200,19 @@ struct Stage {
   static __device__ __forceinline__ f32x4 factor(const unsigned char* lds, int at, int tt, int lane) {
     return *reinterpret_cast<const f32x4*>(lds + at + 4 * (16 * tt + 4 * (lane >> 4)));
   }
-  // Operands from the planes; raw ones have no second half.  LO: bytes from the first half to
-  // the second, or 0 for the first alone.
-  template <int LO = HALF>
+  // Operands from the planes; raw ones have no second half.
   static __device__ __forceinline__ Split rows(const unsigned char* lds, int raw_at, int at, int tt,
                                                int s, int lane) {
     Split o;
     o.hi = rows_operand<NP>(lds + (RAW ? raw_at : at), tt, s, lane);
-    if constexpr (!RAW && LO != 0) o.lo = rows_operand<NP>(lds + at + LO, tt, s, lane);
+    if constexpr (!RAW) o.lo = rows_operand<NP>(lds + at + HALF, tt, s, lane);
     return o;
   }
-  template <int LO = HALF>
   static __device__ __forceinline__ Split cols(const unsigned char* lds, int raw_at, int at, int f,
                                                int lane) {
     Split o;
     o.hi = cols_operand<NP>(lds + (RAW ? raw_at : at), f, lane);
-    if constexpr (!RAW && LO != 0) o.lo = cols_operand<NP>(lds + at + LO, f, lane);
+    if constexpr (!RAW) o.lo = cols_operand<NP>(lds + at + HALF, f, lane);
     return o;
   }
   // e^{l_T} for keys state_key(f, g, r)
@@ -481,15 +468,12 @@ __device__ __forceinline__ void walk_forward(
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         fo[tt] = ff[tt];
-        ap[tt] = square_at<St::P_LEN == St::SQ ? 0 : -St::SQ>(cur + St::A_P, tt, lane);
+        ap[tt] = square_at(cur + St::A_P, tt, lane);
 #pragma unroll
         for (int s = 0; s < NKS; ++s) {
-          const Split aq = St::template rows<St::BRIEF ? 0 : -St::HALF>(cur, St::A_Q, St::A_QH, tt, s, lane);
+          const Split aq = St::rows(cur, St::A_Q, St::A_QH, tt, s, lane);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            if constexpr (St::BRIEF) O[tt][t] = mma(aq.hi, sb[s][t].hi, s ? O[tt][t] : zero);
-            else O[tt][t] = mma_plane<!RAW>(aq, sb[s][t], s ? O[tt][t] : zero);
-          }
+          for (int t = 0; t < NT; ++t) O[tt][t] = mma_plane<!RAW>(aq, sb[s][t], s ? O[tt][t] : zero);
         }
       }
       ahead(nxt);
@@ -498,10 +482,12 @@ __device__ __forceinline__ void walk_forward(
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           if constexpr (RAW) O[tt][t] *= fo[tt];
-          if constexpr (St::BRIEF && (RAW || !DELTA)) {
-            if constexpr (DELTA) O[tt][t] = mma(ap[tt].lo, ub[t].hi, O[tt][t]);
+          if constexpr (!DELTA && sizeof(TIN) == 2) {          // U is V: no second half
+            O[tt][t] = mma(ap[tt].lo, ub[t].hi, O[tt][t]);
             O[tt][t] = mma(ap[tt].hi, ub[t].hi, O[tt][t]);
-          } else O[tt][t] = mma3(ap[tt], ub[t], O[tt][t]);
+          } else {
+            O[tt][t] = mma3(ap[tt], ub[t], O[tt][t]);
+          }
         }
       St::results(cur, O, ct0,
                   static_cast<TIN*>(p.o) + int64_t(k.row(c)) * row_stride + int64_t(k.h) * p.dv +
@@ -621,7 +607,7 @@ __device__ __forceinline__ void walk_backward(
       }
 #pragma unroll
     for (int f = 0; f < NKT; ++f)
-      ac[f] = St::template cols<-St::HALF>(cur, St::A_Q, St::A_QH, f, lane);
+      ac[f] = St::cols(cur, St::A_Q, St::A_QH, f, lane);
     Split gb[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
