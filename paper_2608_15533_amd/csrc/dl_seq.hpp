@@ -77,8 +77,12 @@ struct Stage {
   static constexpr int BYTES = A_V + CT * VROW;
 
   static constexpr int NLIN = (LINEAR / 16 + T - 1) / T;
-  static constexpr int NKQ = RAW ? CT * NP / T : 0;
+  // Rounds of a plane's pieces and of the values'.  Eight waves have twice as many threads as a plane
+  // of 64 keys has pieces: those past the last load it once more and store nothing.
+  static constexpr int KQ = CT * NP;
+  static constexpr int NKQ = RAW ? (KQ + T - 1) / T : 0;
   static constexpr int NV = CT * VNP / T;
+  static_assert(!RAW || NKQ * T >= KQ, "every key piece has a thread");
   static_assert(CT * VNP % T == 0, "whole rounds of value pieces");
   u32x4 lin[NLIN], kk[NKQ ? NKQ : 1], qq[NKQ ? NKQ : 1], vv[NV];
 
@@ -105,7 +109,9 @@ struct Stage {
       const unsigned char* qb = static_cast<const unsigned char*>(p.q) + at;
 #pragma unroll
       for (int i = 0; i < NKQ; ++i) {
-        const int x = i * T + tid, r = x / NP, pc = (x % NP) ^ piece_swap<NP>(r);
+        int x = i * T + tid;
+        if ((i + 1) * T > KQ) x = min(x, KQ - 1);
+        const int r = x / NP, pc = (x % NP) ^ piece_swap<NP>(r);
         const uint32_t o = min(r * stride, last) + 16 * pc;
         kk[i] = *reinterpret_cast<const u32x4*>(kb + o);
         if constexpr (WITH_Q) qq[i] = *reinterpret_cast<const u32x4*>(qb + o);
@@ -140,8 +146,10 @@ struct Stage {
     if constexpr (RAW) {
 #pragma unroll
       for (int i = 0; i < NKQ; ++i) {
-        *reinterpret_cast<u32x4*>(lds + A_K + 16 * (i * T + tid)) = kk[i];
-        if constexpr (WITH_Q) *reinterpret_cast<u32x4*>(lds + A_Q + 16 * (i * T + tid)) = qq[i];
+        const int x = i * T + tid;
+        if ((i + 1) * T > KQ && x >= KQ) continue;
+        *reinterpret_cast<u32x4*>(lds + A_K + 16 * x) = kk[i];
+        if constexpr (WITH_Q) *reinterpret_cast<u32x4*>(lds + A_Q + 16 * x) = qq[i];
       }
     }
 #pragma unroll
