@@ -13,6 +13,8 @@ enum DecayClass { DC_SCALAR = 0, DC_KEY = 1, DC_BONUS = 2 };
 
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr float LOG_FLOOR = -104.f;   // e^-104 rounds to 0 in fp32
+// The log-decay that counts, in powers of two.  Not fmaxf, which would make a NaN the floor.
+__device__ __forceinline__ float log2_decay(float x) { return (x < LOG_FLOOR ? LOG_FLOOR : x) * LOG2E; }
 // A diagonal 16 x 16 block of G and P factors through e^{l_i - m} e^{m - l_j} with m the
 // log-decay at its middle; both factors stay below 2^WIDE unless the block decays by more.
 constexpr float WIDE = 80.f;
@@ -109,7 +111,7 @@ struct ChunkIn {
     }
     if constexpr (DC == DC_SCALAR) {
       if (tid < 64) {
-        float x = tid < row.count ? fmaxf(one, LOG_FLOOR) * LOG2E : 0.f;
+        float x = tid < row.count ? log2_decay(one) : 0.f;
 #pragma unroll
         for (int d = 1; d < CT; d *= 2) {
           const float y = __shfl_up(x, d);
@@ -124,7 +126,7 @@ struct ChunkIn {
         const int x = i * NT + tid, t = x / LP;
         f32x4 y;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = t < row.count ? fmaxf(lam[i][e], LOG_FLOOR) * LOG2E : 0.f;
+        for (int e = 0; e < 4; ++e) y[e] = t < row.count ? log2_decay(lam[i][e]) : 0.f;
         *reinterpret_cast<f32x4*>(&l[t][4 * (x % LP)]) = y;
       }
       __syncthreads();
@@ -422,7 +424,7 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   }
   const bool live = lane < row.count;
   const int64_t tok = int64_t(row.first + (live ? lane : 0)) * p.H + h;
-  float l = live && p.lam ? fmaxf(p.lam[tok], LOG_FLOOR) * LOG2E : 0.f;
+  float l = live && p.lam ? log2_decay(p.lam[tok]) : 0.f;
   const float beta = DELTA && live ? p.beta[tok] : 0.f;
 #pragma unroll
   for (int d = 1; d < CT; d *= 2) {

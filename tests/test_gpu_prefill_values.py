@@ -1,5 +1,5 @@
 """What whole-sequence calls make of values that a program has by choice or by accident: outputs
-rounded once."""
+rounded once, log-decays that are not a number."""
 
 import pytest
 import torch
@@ -28,3 +28,43 @@ def test_bf16_outputs_are_rounded_once(op, dk, dv, lens):
     size = (want ** 2).mean(-1, keepdim=True).sqrt()
     slack = (c.o.double().cpu() - want).abs() - torch.finfo(BF16).eps / 2 * want.abs()
     assert (slack / size).max().item() <= 4 * R.TOL_F32
+
+
+@pytest.mark.parametrize("op", [o for o in R.OPS if o != "linattn"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("at", [0, 7, 20, 31, 32, 39])
+def test_a_log_decay_that_is_not_a_number(op, dtype, at):
+    """It makes its head's state one from its token on: the sequence's later outputs, its final state
+    and what flows back through it; other heads and sequences keep their bits."""
+    lens, H = [40, 40, 40], 3
+    x = R.inputs(op, lens, H, 64, 64, dtype, seed=2)
+    c = P.Call(op, x, backward=True)
+    c.build()
+    c.forward()
+    c.backward()
+    results = lambda: [t for t in (c.o, c.S_out, c.grads.dq, c.grads.dk, c.grads.dv,  # noqa: E731
+                                   c.grads.dlam, c.grads.dS) if t is not None]
+    clean = [t.clone() for t in results()]
+    per_key = c.x["lam"].dim() == 3
+    if per_key:
+        c.x["lam"][40 + at, 1, 5] = float("nan")
+    else:
+        c.x["lam"][40 + at, 1] = float("nan")
+    c.forward()
+    c.backward()
+    mid = x["slots"][1]
+    first = 40 + at + (op == "rwkv6")                # reads the state before its token
+    assert torch.isnan(c.o[first:80, 1]).all()
+    row = c.S_out[mid, 1, 5] if per_key else c.S_out[mid, 1]
+    assert torch.isnan(row).all()
+    row = c.grads.dS[mid, 1, 5] if per_key else c.grads.dS[mid, 1]
+    assert torch.isnan(row).all()
+    lam = c.grads.dlam[40:40 + at + 1, 1]
+    assert torch.isnan(lam[..., 5] if per_key else lam).all()
+    for a, b in zip(clean, results()):
+        a, b = a.clone(), b.clone()
+        if a.dim() == 4:
+            a[mid, 1] = b[mid, 1] = 0
+        else:
+            a[40:80, 1] = b[40:80, 1] = 0
+        assert torch.equal(a, b)
