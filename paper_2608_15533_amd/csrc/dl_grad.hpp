@@ -218,7 +218,7 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
     for (int r = 0; r < 4; ++r) {
       const int ri = 16 * bi + 4 * g + r;
       float f = bj_;
-      if (DC == DC_SCALAR) f *= exp2_of(fminf(in.l[ri][0] - in.l[j][0], 0.f));
+      if (DC == DC_SCALAR) f *= exp2_of(in.l[ri][0] - in.l[j][0]);
       if constexpr (DC == DC_BONUS) {
         if (ri == j) tok_sum[0][j] = ap[r];      // the bonus pair, apart from the others
         dP[ri][j] = ri > j ? ap[r] * f : 0.f;
@@ -332,11 +332,11 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
           const float kj = widen(in.k[j][key]), qj = widen(in.q[j][key]);
           const float lj = in.at(j, key), lqj = in.at_q(j, key);
           if (j < i || (j == i && DC == DC_KEY)) {
-            sq += dP[i][j] * kj * exp2_of(fminf(lq[e] - lj, 0.f));
+            sq += dP[i][j] * kj * exp2_of(lq[e] - lj);
             sr += dG[i][j] * kj * exp2_of(l[e] - lj);
           }
           if (j > i || (j == i && DC == DC_KEY))
-            sc += dP[j][i] * qj * exp2_of(fminf(lqj - l[e], 0.f)) + dG[j][i] * kj * exp2_of(lj - l[e]);
+            sc += dP[j][i] * qj * exp2_of(lqj - l[e]) + dG[j][i] * kj * exp2_of(lj - l[e]);
         }
         aq[x][tt][r] += sq;
         ar[x][tt][r] += sr;

@@ -218,7 +218,7 @@ __device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[SL], fl
       const int ri = 16 * bi + 4 * g + r;
       float x = ap[0][r] + ap[1][r], y = ag[0][r] + ag[1][r];
       if constexpr (DC == DC_SCALAR) {
-        const float f = exp2_of(fminf(in.l[ri][0] - in.l[j][0], 0.f));
+        const float f = exp2_of(in.l[ri][0] - in.l[j][0]);
         x *= f;
         y *= f;
       }
@@ -237,7 +237,7 @@ __device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[SL], fl
           const float kj = widen(in.k[j][r]), lj = in.at(j, r);
           sg += widen(in.k[i][r]) * kj * exp2_of(in.at(i, r) - lj);
           if (DC == DC_KEY || i > j)
-            sp += widen(in.q[i][r]) * kj * exp2_of(fminf(in.at_q(i, r) - lj, 0.f));
+            sp += widen(in.q[i][r]) * kj * exp2_of(in.at_q(i, r) - lj);
         }
       }
       G[i][j] = i > j ? sg : 0.f;
@@ -452,7 +452,7 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = 16 * bi + 4 * g + r;
-      const float x = exp2_of(fminf(__shfl(l, i) - lj, 0.f));
+      const float x = exp2_of(__shfl(l, i) - lj);
       P[i][j] = i >= j ? ap[r] * x : 0.f;
       G[i][j] = i > j ? ag[r] * x : 0.f;
     }

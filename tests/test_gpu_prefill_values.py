@@ -1,5 +1,5 @@
 """What whole-sequence calls make of values that a program has by choice or by accident: outputs
-rounded once, log-decays that are not a number."""
+rounded once, log-decays that are not a number or above zero."""
 
 import pytest
 import torch
@@ -68,3 +68,19 @@ def test_a_log_decay_that_is_not_a_number(op, dtype, at):
         else:
             a[40:80, 1] = b[40:80, 1] = 0
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("op", [o for o in R.OPS if o != "linattn"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_log_decays_above_zero(op, dtype):
+    """Outside the domain, as for the decode step, which takes them at their value: so do these."""
+    x = R.inputs(op, [70, 20], 2, 64, 64, dtype, seed=3)
+    x["lam"] = x["lam"].clone()
+    x["lam"][::3] = 0.125
+    want = R.expected(op, x, grads=True)
+    c = P.Call(op, x, backward=True)
+    c.build()
+    c.forward()
+    c.backward()
+    P.check_forward(c, want)
+    P.check_grads(c, want)
