@@ -124,6 +124,7 @@ class DecodeEngine:
         self._side = torch.cuda.Stream(device=device) if mode == "phased_concurrent" else None
         self.plan = None
         self._prefill_ws = None
+        self._prefill_done = torch.cuda.Event()       # behind the workspace's last use
         self.replays = 0
         self.direct_steps = 0
 
@@ -154,7 +155,7 @@ class DecodeEngine:
         Without ``slots`` every prompt takes a free slot and starts from a zero state; with it,
         a list of distinct active slots, prompt i goes on from the state of slots[i], whose log
         is flushed first.  Returns (slots, outputs), one output [sum(lens), H, dv] per layer in
-        the input dtype."""
+        the input dtype.  Calls share one workspace: one on another stream waits for the last."""
         lens = [int(n) for n in lens]
         if any(n < 0 for n in lens):
             raise ValueError("a prompt's length is negative")
@@ -196,11 +197,17 @@ class DecodeEngine:
             self._prefill_ws = None                   # let go before taking the larger one
             self._prefill_ws = D.prefill_workspace(desc, len(lens), N, device=self.device)
         rows = host[1].long()
-        for st, tok, o in zip(self.states, layer_tokens, outs):
-            if not fresh:
-                D.dl_merge(desc, st, slots=host[1])
-            D.dl_prefill(desc, None if fresh else st.S, st.S, tok, o, tables, self._prefill_ws)
-            st.len[rows] = 0
+        stream = torch.cuda.current_stream(self.device)
+        stream.wait_event(self._prefill_done)
+        self._prefill_ws.record_stream(stream)        # its memory outlives this stream's use of it
+        try:
+            for st, tok, o in zip(self.states, layer_tokens, outs):
+                if not fresh:
+                    D.dl_merge(desc, st, slots=host[1])
+                D.dl_prefill(desc, None if fresh else st.S, st.S, tok, o, tables, self._prefill_ws)
+                st.len[rows] = 0
+        finally:
+            self._prefill_done.record(stream)
         for s in slots:
             self.sched.flushed(s)
 
