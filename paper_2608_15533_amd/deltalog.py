@@ -224,6 +224,11 @@ class DeltaLogState:
                     lam_log=self.lam_log, len=self.len, err=self.err)
 
 
+def _row_sizes(desc):
+    """What of a descriptor the arrays over token rows go by."""
+    return (desc.op, desc.heads, desc.dk, desc.dv, desc.in_dtype)
+
+
 class Token:
     """Device tensors of one decode step's inputs plus the dl_token struct over them."""
 
@@ -247,6 +252,7 @@ class Token:
         else:
             beta = None
         self.n = n
+        self.sizes = _row_sizes(desc)
         self.tensors = (q, k, v, lam, beta, u)
         self.struct = dl_token(_ptr(q), _ptr(k), _ptr(v), _ptr(beta), _ptr(lam), _ptr(u))
 
@@ -399,6 +405,8 @@ class Grads:
             _need(S, "S", state_torch_dtype(desc),
                   (desc.num_slots, desc.heads, desc.dk, desc.dv))
         self.dS = like(S)
+        self.n, self.sizes = tok.n, tok.sizes
+        self.state = None if S is None else (desc.num_slots, desc.state_dtype)
         self.struct = dl_grads(_ptr(self.dq), _ptr(self.dk), _ptr(self.dv), _ptr(self.dbeta),
                                _ptr(self.dlam), _ptr(self.du), _ptr(self.dS))
 
@@ -441,9 +449,11 @@ def prefill_workspace(desc, n, tokens, backward=False, device="cuda"):
 def _sequences(desc, tok, tables, workspace, *others):
     if workspace is None or not workspace.is_cuda or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous device tensor (see prefill_workspace)")
-    _on_current_device(*tok.tensors, tables.err, workspace, *others)
+    if tok.sizes != _row_sizes(desc):
+        raise ValueError("the token was made for another descriptor")
     if tok.n != tables.tokens:
         raise ValueError(f"the token holds {tok.n} rows but the tables are for {tables.tokens}")
+    _on_current_device(*tok.tensors, tables.err, workspace, *others)
     return (workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
 
@@ -469,7 +479,11 @@ def dl_prefill_backward(desc, S_in, tok, d_o, dS_out, grads, tables, workspace, 
     for name, t in (("S_in", S_in), ("dS_out", dS_out)):
         if t is not None:
             _need(t, name, *state)
-    wp, wn = _sequences(desc, tok, tables, workspace, S_in, d_o, dS_out, grads.dq)
+    if grads.n != tok.n or grads.sizes != _row_sizes(desc):
+        raise ValueError("the gradients were made for another token or descriptor")
+    if grads.state not in (None, (desc.num_slots, desc.state_dtype)):
+        raise ValueError("the gradient of the states was made for another descriptor")
+    wp, wn = _sequences(desc, tok, tables, workspace, S_in, d_o, dS_out, grads.dq, grads.dS)
     _check(_lib.dl_prefill_backward(ctypes.byref(desc), _ptr(S_in), ctypes.byref(tok.struct),
                                     _ptr(d_o), _ptr(dS_out), ctypes.byref(grads.struct),
                                     ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,
