@@ -278,7 +278,7 @@ __device__ __forceinline__ void solve(float (*G)[SL], float (*M)[SL], const floa
       if (second && !o) M[i][16 + c16] = 0.f;
     }
   }
-  __builtin_amdgcn_wave_barrier();
+  wave_sync();
   f32x4 tn = {0.f, 0.f, 0.f, 0.f}, tm = tn;
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
@@ -292,7 +292,7 @@ __device__ __forceinline__ void solve(float (*G)[SL], float (*M)[SL], const floa
     rn = __builtin_amdgcn_mfma_f32_16x16x4f32(G[16 + c16][16 + 4 * g + r], tn[r], rn, 0, 0, 0);
     if (BWD) rm = __builtin_amdgcn_mfma_f32_16x16x4f32(M[16 + c16][16 + 4 * g + r], tm[r], rm, 0, 0, 0);
   }
-  __builtin_amdgcn_wave_barrier();
+  wave_sync();
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     G[16 + 4 * g + r][c16] = -rn[r];

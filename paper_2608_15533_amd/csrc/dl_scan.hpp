@@ -86,6 +86,14 @@ __device__ __forceinline__ Split load_split(const uint16_t* hi, const uint16_t* 
   return s;
 }
 
+// What a wave's lanes have written to LDS, its other lanes may read: a wave's LDS accesses happen in
+// order, so this only keeps the compiler from moving them across.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 __device__ __forceinline__ float widen(float x) { return x; }
 __device__ __forceinline__ float widen(uint16_t x) { return __uint_as_float(uint32_t(x) << 16); }
 __device__ __forceinline__ void narrow(float* p, float x) { *p = x; }

@@ -179,7 +179,7 @@ struct Stage {
           narrow(reinterpret_cast<TIN*>(lds + value_piece(16 * tt + 4 * g + r, col / PER)) + col % PER,
                  x[tt][t][r]);
         }
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     constexpr int WP = 16 * NT / PER;                        // pieces of a row
 #pragma unroll
     for (int i = 0; i < CT * WP / 64; ++i) {
