@@ -92,7 +92,7 @@ __device__ __forceinline__ void load_planes(GradShared<DC, DK, DV, TIN>& sh, con
   constexpr int NP = Sh::NP;
 #pragma unroll
   for (int x = tid; x < CT * NP; x += NTH) {
-    const int t = x / NP, pc = x % NP, at = 16 * piece_at<NP>(t, pc);
+    const int t = x / NP, pc = x % NP, at = piece_at<NP>(t, pc);
     const int from = ((pc >> 1) * CT + t) * 16 + 8 * (pc & 1);      // [value tile][token][16]
     float e[8], z[8];
     load8(E + from, e);
@@ -105,20 +105,14 @@ __device__ __forceinline__ void load_planes(GradShared<DC, DK, DV, TIN>& sh, con
       load8(d, o);
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i] = live ? o[i] : 0.f;
-      const Split s = split8(o);
-      *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_DO + at) = s.hi;
-      *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_DO + Sh::HALF + at) = s.lo;
+      put<TIN>(sh.planes + Sh::A_DO, Sh::HALF, at, o);
     } else {
       const u32x4 zero = {0, 0, 0, 0}, o = *reinterpret_cast<const u32x4*>(d);
-      *reinterpret_cast<u32x4*>(sh.planes + Sh::A_DO + at) = live ? o : zero;
+      *reinterpret_cast<u32x4*>(sh.planes + Sh::A_DO + 16 * at) = live ? o : zero;
     }
-    const Split se = split8(e);
-    *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_E + at) = se.hi;
-    *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_E + Sh::HALF + at) = se.lo;
+    put<TIN>(sh.planes + Sh::A_E, Sh::HALF, at, e);
     if constexpr (DELTA) {
-      const Split sz = split8(z);
-      *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_Z + at) = sz.hi;
-      *reinterpret_cast<bf16x8*>(sh.planes + Sh::A_Z + Sh::HALF + at) = sz.lo;
+      put<TIN>(sh.planes + Sh::A_Z, Sh::HALF, at, z);
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += e[i] * z[i];
@@ -138,6 +132,7 @@ constexpr int grad_waves() {
 template <int DC, int DK, int DV, bool DELTA, typename TIN>
 __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kernel(SeqParams p) {
   using Sh = GradShared<DC, DK, DV, TIN>;
+  using Op = Operand<TIN>;
   constexpr int NTH = 4 * DK, NW = DK / 16, KT = 1, HALF = Sh::HALF, NP = Sh::NP;
   constexpr bool LO = Sh::LO;
   __shared__ Sh sh;
@@ -172,10 +167,7 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
   in.template load<NTH, DELTA>(p, row, h, tid);   // and every thread past this point
 
   auto operand = [&](int at, bool lo, int tt, int s) {
-    Split o;
-    o.hi = rows_operand<NP>(sh.planes + at, tt, s, lane);
-    if (lo) o.lo = rows_operand<NP>(sh.planes + at + HALF, tt, s, lane);
-    return o;
+    return rows_operand<Op, NP>(sh.planes + at, lo ? HALF : 0, tt, s, lane);
   };
   // Products over the value columns: token x key ...
   f32x4 aq[KT][2], ar[KT][2], ac[KT][2];
@@ -186,13 +178,10 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
   for (int s = 0; s < DV / 32; ++s) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) dot[0] += xs[s][e] * xd[s][e];
-    const Split bs = split8(xs[s]), bd = split8(xd[s]);
+    const Op bs = operand8<Op>(xs[s]), bd = operand8<Op>(xd[s]);
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      const Split od = operand(Sh::A_DO, LO, tt, s);
-      aq[0][tt] = mma(od.hi, bs.lo, aq[0][tt]);
-      if constexpr (LO) aq[0][tt] = mma(od.lo, bs.hi, aq[0][tt]);
-      aq[0][tt] = mma(od.hi, bs.hi, aq[0][tt]);
+      aq[0][tt] = mma_plane<LO>(operand(Sh::A_DO, LO, tt, s), bs, aq[0][tt]);
       if constexpr (DELTA) ar[0][tt] = mma3(operand(Sh::A_Z, true, tt, s), bs, ar[0][tt]);
       ac[0][tt] = mma3(operand(Sh::A_E, true, tt, s), bd, ac[0][tt]);
     }
@@ -203,10 +192,8 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
   if (wave < 3) {
 #pragma unroll
     for (int s = 0; s < DV / 32; ++s) {
-      const Split b = operand(Sh::A_E, true, bj, s), a = operand(Sh::A_DO, LO, bi, s);
-      ap = mma(a.hi, b.lo, ap);
-      if constexpr (LO) ap = mma(a.lo, b.hi, ap);
-      ap = mma(a.hi, b.hi, ap);
+      const Op b = operand(Sh::A_E, true, bj, s);
+      ap = mma_plane<LO>(operand(Sh::A_DO, LO, bi, s), b, ap);
       if constexpr (DELTA) ag = mma3(operand(Sh::A_Z, true, bi, s), b, ag);
     }
   }

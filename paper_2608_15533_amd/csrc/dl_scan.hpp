@@ -1,5 +1,5 @@
 // Shared pieces of the sequence kernels (prefill and its backward pass): fp32 values on the
-// bf16 matrix cores, the workspace's layout, chunk bookkeeping.
+// matrix cores, the workspace's layout, chunk bookkeeping.
 //
 // The recurrence of Eq. 3 over a chunk of T = 32 tokens, with l_i the log-decay summed from
 // the chunk's start through token i (per key, or the same for all keys; 0 without decay), S
@@ -21,6 +21,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "deltalog.h"
 #include "dl_internal.h"
 
@@ -32,13 +34,21 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-// An fp32 operand as two bf16 numbers: hi the nearest bf16, lo the nearest bf16 to what hi
-// leaves.  hi + lo is within 2^-18 of the value (half a bf16 step, twice), and of the
-// product of two such operands the three terms hi hi, hi lo and lo hi are kept: what is left
-// out is another 2^-18.  Three bf16 MFMAs of 32 terms take 48 cycles, eight fp32 ones 256.
+// Eight terms of an fp32 operand, for calls with bf16 inputs: two bf16 numbers each, hi the nearest
+// bf16, lo the nearest bf16 to what hi leaves.  hi + lo is within 2^-18 of the value (half a bf16
+// step, twice), and of the product of two such operands the three terms hi hi, hi lo and lo hi are
+// kept: what is left out is another 2^-18, where the inputs' own rounding was 2^-9.  Three bf16
+// MFMAs of 32 terms take 48 cycles, eight fp32 ones 256.
 struct Split {
   bf16x8 hi, lo;
 };
+// For calls with fp32 inputs: as they are, terms 0 to 3 in hi and 4 to 7 in lo.  The same bytes, in
+// the same places of memory and LDS, as a Split.
+struct Full {
+  f32x4 hi, lo;
+};
+template <typename TIN>
+using Operand = std::conditional_t<sizeof(TIN) == 4, Full, Split>;
 
 // 24 VALU instructions: two conversions a pair, hi widened again, the difference.
 __device__ __forceinline__ Split split8(const float* x) {
@@ -56,6 +66,11 @@ __device__ __forceinline__ Split split8(const float* x) {
   }
   return Split{__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, lo)};
 }
+template <typename OP>
+__device__ __forceinline__ OP operand8(const float* x) {
+  if constexpr (std::is_same_v<OP, Split>) return split8(x);
+  else return Full{{x[0], x[1], x[2], x[3]}, {x[4], x[5], x[6], x[7]}};
+}
 
 // acc += a b over 32 terms.  Lane l holds of the 16x16 result rows 4(l/16)+r, column l%16;
 // of a row l%16, of b column l%16, and of both the same eight terms: which eight is free as
@@ -72,18 +87,29 @@ __device__ __forceinline__ f32x4 mma3(const Split& a, const Split& b, f32x4 acc)
   acc = mma(a.hi, b.lo, acc);
   return mma(a.hi, b.hi, acc);
 }
+// Four terms an instruction, one of each lane of a row or column.
+__device__ __forceinline__ f32x4 mma3(const Full& a, const Full& b, f32x4 acc) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.hi[e], b.hi[e], acc, 0, 0, 0);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.lo[e], b.lo[e], acc, 0, 0, 0);
+  return acc;
+}
+// acc += a b with an operand a that has a second half (LO) or is exact in bf16.
+template <bool LO, typename OP>
+__device__ __forceinline__ f32x4 mma_plane(const OP& a, const OP& b, f32x4 acc) {
+  if constexpr (LO) {
+    return mma3(a, b, acc);
+  } else {
+    acc = mma(a.hi, b.lo, acc);
+    return mma(a.hi, b.hi, acc);
+  }
+}
 __host__ __device__ constexpr int state_key(int f, int g, int r) {
   return 32 * (f >> 1) + 8 * g + 4 * (f & 1) + r;
 }
 __device__ __forceinline__ int state_term(int lane, int e) {
   return 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3);
-}
-
-__device__ __forceinline__ Split load_split(const uint16_t* hi, const uint16_t* lo) {
-  Split s;
-  s.hi = *reinterpret_cast<const bf16x8*>(hi);
-  s.lo = *reinterpret_cast<const bf16x8*>(lo);
-  return s;
 }
 
 // What a wave's lanes have written to LDS, its other lanes may read: a wave's LDS accesses happen in
@@ -112,8 +138,8 @@ __device__ __forceinline__ void store_state(void* S, bool bf16, int64_t i, float
 }
 
 // ------------------------------------------------------------------ operands in LDS
-// A token x key plane: 32 rows of 16-byte pieces (8 bf16), piece x of row r at
-// piece_at(r, x).  The exchange of pieces within a row lets 16 rows of one piece (an operand
+// A token x key plane: 32 rows of 16-byte pieces (8 bf16; of Full planes four fp32, the other four in
+// the second half), piece x of row r at piece_at(r, x).  The exchange of pieces within a row lets 16 rows of one piece (an operand
 // over keys) and four pieces of four rows (one over tokens) each lie in different banks.
 // NP: pieces in a row.
 template <int NP>
@@ -141,17 +167,39 @@ __device__ __forceinline__ bf16x4 read_column(const unsigned char* lds) {
   return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)lds));
 }
 
-// Tokens 16 tt + l%16, terms: keys 32 s + 8 (l/16) + e.
-template <int NP>
-__device__ __forceinline__ bf16x8 rows_operand(const unsigned char* plane, int tt, int s, int lane) {
-  return *reinterpret_cast<const bf16x8*>(plane + 16 * piece_at<NP>(16 * tt + (lane & 15), 4 * s + (lane >> 4)));
+// Tokens 16 tt + l%16, terms: keys 32 s + 8 (l/16) + e.  half: bytes to the second half, or 0: none.
+template <typename OP, int NP>
+__device__ __forceinline__ OP rows_operand(const unsigned char* plane, int half, int tt, int s, int lane) {
+  const unsigned char* at = plane + 16 * piece_at<NP>(16 * tt + (lane & 15), 4 * s + (lane >> 4));
+  OP o;
+  o.hi = *reinterpret_cast<const decltype(o.hi)*>(at);
+  if (half) o.lo = *reinterpret_cast<const decltype(o.lo)*>(at + half);
+  return o;
 }
 // Keys state_key(f, ., .) in the place of l%16, terms: the chunk's tokens (state order).
-template <int NP>
-__device__ __forceinline__ bf16x8 cols_operand(const unsigned char* plane, int f, int lane) {
-  const int i = lane & 15, r = 4 * (lane >> 4) + (i >> 2), x = 4 * (f >> 1) + (i & 3);
-  const unsigned char* at = plane + 8 * (f & 1);
-  return join(read_column(at + 16 * piece_at<NP>(r, x)), read_column(at + 16 * piece_at<NP>(r + 16, x)));
+template <typename OP, int NP>
+__device__ __forceinline__ OP cols_operand(const unsigned char* plane, int half, int f, int lane) {
+  const int i = lane & 15;
+  OP o;
+  if constexpr (std::is_same_v<OP, Split>) {
+    const int r = 4 * (lane >> 4) + (i >> 2), x = 4 * (f >> 1) + (i & 3);
+    const int a = 8 * (f & 1) + 16 * piece_at<NP>(r, x), b = 8 * (f & 1) + 16 * piece_at<NP>(r + 16, x);
+    o.hi = join(read_column(plane + a), read_column(plane + b));
+    if (half) o.lo = join(read_column(plane + half + a), read_column(plane + half + b));
+  } else {
+    // Key i is in piece i / 4 of these 32 keys' eight, half f & 1.  Rows 4 g + e and 16 + 4 g + e; their
+    // exchange of pieces is g's with e's, so one address serves all e.
+    static_assert(NP >= 8 && piece_swap<NP>(4 + 1) == (piece_swap<NP>(4) ^ piece_swap<NP>(1)), "see above");
+    const int g = lane >> 4;
+    const unsigned char* at = plane + half * (f & 1) + 16 * (4 * g * NP + ((i >> 2) ^ g)) + 4 * (i & 3);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int to = 16 * (e * NP + ((4 * (f >> 1)) ^ piece_swap<NP>(e)));
+      o.hi[e] = *reinterpret_cast<const float*>(at + to);
+      o.lo[e] = *reinterpret_cast<const float*>(at + to + 256 * NP);
+    }
+  }
+  return o;
 }
 
 // ------------------------------------------------------------------ workspace
@@ -213,9 +261,10 @@ struct SeqParams {
 
 // Waves of a workgroup that walks chunks, 16 value columns each.  While there are few waves for
 // the 256 CUs, workgroups of two spread them (a wave alone on its SIMD is at its fastest), as
-// long as all run at once: LDS and registers hold four of them on a CU for 64 keys, two for 128
-// with raw operands, one with planes from the workspace.  Then four waves, then whole heads,
-// which share their operands.
+// long as all run at once: with raw operands LDS and registers hold four of them on a CU for 64 keys
+// and two for 128; with planes from the workspace two or three for 64 (taken as four: the last ones
+// start when the first are done) and one for 128.  Then four waves, then whole heads, which share
+// their operands.
 inline int walk_waves(int64_t heads, int dk, int dv, bool raw) {
   const int64_t waves = heads * (dv / 16);
   const int64_t two = dk == 64 ? 2048 : raw ? 1024 : 512;   // what workgroups of two keep running

@@ -14,36 +14,29 @@
 namespace dl {
 
 // A square's operand.
-__device__ __forceinline__ Split square_at(const unsigned char* lds, int tt, int lane) {
+template <typename OP>
+__device__ __forceinline__ OP square_at(const unsigned char* lds, int tt, int lane) {
   const unsigned char* at = lds + 16 * (tt * 64 + lane);
-  Split s;
-  s.hi = *reinterpret_cast<const bf16x8*>(at);
-  s.lo = *reinterpret_cast<const bf16x8*>(at + WsLayout::SQ);
+  OP s;
+  s.hi = *reinterpret_cast<const decltype(s.hi)*>(at);
+  s.lo = *reinterpret_cast<const decltype(s.lo)*>(at + WsLayout::SQ);
   return s;
 }
 
 // Result tiles [2][NT] (tokens 16 tt + 4 g + r) as operands over the chunk's tokens.
-template <int NT>
-__device__ __forceinline__ Split tokens_operand(const f32x4 (&x)[2][NT], int t) {
+template <typename OP, int NT>
+__device__ __forceinline__ OP tokens_operand(const f32x4 (&x)[2][NT], int t) {
   float a[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) a[e] = x[e >> 2][t][e & 3];
-  return split8(a);
+  return operand8<OP>(a);
 }
-template <int NKT, int NT>
-__device__ __forceinline__ Split state_operand(const f32x4 (&S)[NKT][NT], int s, int t) {
+template <typename OP, int NKT, int NT>
+__device__ __forceinline__ OP state_operand(const f32x4 (&S)[NKT][NT], int s, int t) {
   float a[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) a[e] = S[2 * s + (e >> 2)][t][e & 3];
-  return split8(a);
-}
-
-// acc += a b with a plane operand that has a second half (LO) or is exact in bf16.
-template <bool LO>
-__device__ __forceinline__ f32x4 mma_plane(const Split& a, const Split& b, f32x4 acc) {
-  if constexpr (LO) acc = mma(a.lo, b.hi, acc);
-  acc = mma(a.hi, b.lo, acc);
-  return mma(a.hi, b.hi, acc);
+  return operand8<OP>(a);
 }
 
 enum PassId { PASS_OUT = 0, PASS_SAVE = 1, PASS_BACK = 2, PASS_SEG = 3 };
@@ -51,12 +44,16 @@ enum PassId { PASS_OUT = 0, PASS_SAVE = 1, PASS_BACK = 2, PASS_SEG = 3 };
 // One chunk's operands on their way from memory to LDS.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, int PASS, typename TIN>
 struct Stage {
+  using Op = Operand<TIN>;
   static constexpr int T = 64 * NW, VC = 16 * NT * NW, NP = DK / 8;
   static constexpr int HALF = CT * DK * 2;                     // bytes of half a plane
   static constexpr int PL = RAW ? 0 : HALF, SQ = WsLayout::SQ, SQ2 = 2 * SQ;
   static constexpr int FAC = 4 * DK + 12 * CT;
   static constexpr bool BACK = PASS == PASS_BACK, OUT = PASS == PASS_OUT;
   static constexpr bool WITH_Q = BACK || OUT;
+  // Plane operands are read ahead of the products before theirs; with fp32 inputs, whose products take
+  // five times as long, one by one: registers would not do for all.
+  static constexpr bool AHEAD = sizeof(TIN) == 2;
   // LDS offsets, of the workspace block: first P, N, Kh (what of them the pass needs), then Qh,
   // Kb, the factors, and backward P^T, M^T.
   static constexpr int A_P = 0;
@@ -209,19 +206,12 @@ struct Stage {
     return *reinterpret_cast<const f32x4*>(lds + at + 4 * (16 * tt + 4 * (lane >> 4)));
   }
   // Operands from the planes; raw ones have no second half.
-  static __device__ __forceinline__ Split rows(const unsigned char* lds, int raw_at, int at, int tt,
-                                               int s, int lane) {
-    Split o;
-    o.hi = rows_operand<NP>(lds + (RAW ? raw_at : at), tt, s, lane);
-    if constexpr (!RAW) o.lo = rows_operand<NP>(lds + at + HALF, tt, s, lane);
-    return o;
+  static __device__ __forceinline__ Op rows(const unsigned char* lds, int raw_at, int at, int tt, int s,
+                                            int lane) {
+    return rows_operand<Op, NP>(lds + (RAW ? raw_at : at), RAW ? 0 : HALF, tt, s, lane);
   }
-  static __device__ __forceinline__ Split cols(const unsigned char* lds, int raw_at, int at, int f,
-                                               int lane) {
-    Split o;
-    o.hi = cols_operand<NP>(lds + (RAW ? raw_at : at), f, lane);
-    if constexpr (!RAW) o.lo = cols_operand<NP>(lds + at + HALF, f, lane);
-    return o;
+  static __device__ __forceinline__ Op cols(const unsigned char* lds, int raw_at, int at, int f, int lane) {
+    return cols_operand<Op, NP>(lds + (RAW ? raw_at : at), RAW ? 0 : HALF, f, lane);
   }
   // e^{l_T} for keys state_key(f, g, r)
   static __device__ __forceinline__ f32x4 decay(const unsigned char* lds, int f, int lane) {
@@ -358,6 +348,7 @@ __device__ __forceinline__ void walk_forward(
     const SeqParams& p, int group,
     unsigned char (&lds)[2][Stage<DK, NT, NW, RAW, DELTA, PASS, TIN>::BYTES]) {
   using St = Stage<DK, NT, NW, RAW, DELTA, PASS, TIN>;
+  using Op = typename St::Op;
   constexpr int NKT = DK / 16, NKS = DK / 32;
   constexpr bool OUT = PASS == PASS_OUT;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -382,7 +373,7 @@ __device__ __forceinline__ void walk_forward(
   };
 
   f32x4 U[2][NT], S[NKT][NT], ff[2];
-  Split ak[2][NKS], an[2];
+  Op ak[2][NKS], an[2];
   auto ahead = [&](const unsigned char* l) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
@@ -394,8 +385,9 @@ __device__ __forceinline__ void walk_forward(
       if constexpr (RAW) ff[tt] = St::factor(l, St::A_F, tt, lane);
       if constexpr (DELTA) {
 #pragma unroll
-        for (int s = 0; s < NKS; ++s) ak[tt][s] = St::rows(l, St::A_K, St::A_KH, tt, s, lane);
-        an[tt] = square_at(l + St::A_N, tt, lane);
+        for (int s = 0; s < NKS; ++s)
+          if constexpr (St::AHEAD) ak[tt][s] = St::rows(l, St::A_K, St::A_KH, tt, s, lane);
+        an[tt] = square_at<Op>(l + St::A_N, tt, lane);
       }
     }
   };
@@ -406,35 +398,38 @@ __device__ __forceinline__ void walk_forward(
     if constexpr (PASS == PASS_SAVE) save_tiles<true>(S, block(c) + w.s0(), k.v0 / 16 + ct0, lane);
 
     // Kh S, R = V - Kh S, E = N R (but for PASS_SAVE N holds beta N, and U comes at once)
-    Split sb[NKS][NT];
+    Op sb[NKS][NT];
     f32x4 X[2][NT];
 #pragma unroll
     for (int s = 0; s < NKS; ++s)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        if constexpr (DELTA || OUT) sb[s][t] = state_operand<NKT, NT>(S, s, t);
+        if constexpr (DELTA || OUT) sb[s][t] = state_operand<Op, NKT, NT>(S, s, t);
         if constexpr (DELTA) {
 #pragma unroll
-          for (int tt = 0; tt < 2; ++tt)
+          for (int tt = 0; tt < 2; ++tt) {
+            if constexpr (!St::AHEAD) ak[tt][s] = St::rows(cur, St::A_K, St::A_KH, tt, s, lane);
             X[tt][t] = mma_plane<!RAW>(ak[tt][s], sb[s][t], s ? X[tt][t] : zero);
+          }
         }
       }
-    Split ac[NKT];
+    Op ac[NKT];
     f32x4 gf[2], be[2];
 #pragma unroll
-    for (int f = 0; f < NKT; ++f) ac[f] = St::cols(cur, St::A_K, St::A_KB, f, lane);
+    for (int f = 0; f < NKT; ++f)
+      if constexpr (St::AHEAD) ac[f] = St::cols(cur, St::A_K, St::A_KB, f, lane);
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
       if constexpr (RAW) gf[tt] = St::factor(cur, St::A_G, tt, lane);
       if constexpr (DELTA && PASS == PASS_SAVE) be[tt] = St::factor(cur, St::A_BETA, tt, lane);
     }
     if constexpr (DELTA) {
-      Split rb[NT];
+      Op rb[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) U[tt][t] -= RAW ? X[tt][t] * ff[tt] : X[tt][t];
-        rb[t] = tokens_operand<NT>(U, t);
+        rb[t] = tokens_operand<Op, NT>(U, t);
       }
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
@@ -450,14 +445,14 @@ __device__ __forceinline__ void walk_forward(
           for (int t = 0; t < NT; ++t) U[tt][t] *= be[tt];
       }
     }
-    Split ub[NT], gb[NT];
+    Op ub[NT], gb[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      if constexpr (OUT || !RAW) ub[t] = tokens_operand<NT>(U, t);
+      if constexpr (OUT || !RAW) ub[t] = tokens_operand<Op, NT>(U, t);
       if constexpr (RAW) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) U[tt][t] *= gf[tt];
-        gb[t] = tokens_operand<NT>(U, t);
+        gb[t] = tokens_operand<Op, NT>(U, t);
       } else {
         gb[t] = ub[t];
       }
@@ -466,20 +461,21 @@ __device__ __forceinline__ void walk_forward(
 #pragma unroll
     for (int f = 0; f < NKT; ++f) {
       const f32x4 d = St::decay(cur, f, lane);
+      if constexpr (!St::AHEAD) ac[f] = St::cols(cur, St::A_K, St::A_KB, f, lane);
 #pragma unroll
       for (int t = 0; t < NT; ++t) S[f][t] = mma_plane<!RAW>(ac[f], gb[t], S[f][t] * d);
     }
     __syncthreads();
     if constexpr (OUT) {
       f32x4 O[2][NT], fo[2];
-      Split ap[2];
+      Op ap[2];
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         fo[tt] = ff[tt];
-        ap[tt] = square_at(cur + St::A_P, tt, lane);
+        ap[tt] = square_at<Op>(cur + St::A_P, tt, lane);
 #pragma unroll
         for (int s = 0; s < NKS; ++s) {
-          const Split aq = St::rows(cur, St::A_Q, St::A_QH, tt, s, lane);
+          const Op aq = St::rows(cur, St::A_Q, St::A_QH, tt, s, lane);
 #pragma unroll
           for (int t = 0; t < NT; ++t) O[tt][t] = mma_plane<!RAW>(aq, sb[s][t], s ? O[tt][t] : zero);
         }
@@ -556,6 +552,7 @@ __device__ __forceinline__ void walk_backward(
     const SeqParams& p, int group,
     unsigned char (&lds)[2][Stage<DK, NT, NW, RAW, DELTA, PASS_BACK, TIN>::BYTES]) {
   using St = Stage<DK, NT, NW, RAW, DELTA, PASS_BACK, TIN>;
+  using Op = typename St::Op;
   constexpr int NKT = DK / 16, NKS = DK / 32;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15;
@@ -574,14 +571,15 @@ __device__ __forceinline__ void walk_backward(
   };
 
   f32x4 G[2][NT], D[NKT][NT];
-  Split ar[2][NKS];
+  Op ar[2][NKS];
   auto ahead = [&](const unsigned char* l) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) G[tt][t] = St::values(l, tt, ct0 + t, lane);    // dO
 #pragma unroll
-      for (int s = 0; s < NKS; ++s) ar[tt][s] = St::rows(l, St::A_K, St::A_KB, tt, s, lane);
+      for (int s = 0; s < NKS; ++s)
+        if constexpr (St::AHEAD) ar[tt][s] = St::rows(l, St::A_K, St::A_KB, tt, s, lane);
     }
   };
   auto chunk = [&](int c, unsigned char* cur, unsigned char* nxt) __attribute__((always_inline)) {
@@ -591,17 +589,17 @@ __device__ __forceinline__ void walk_backward(
     save_tiles<true>(D, block(c) + w.ds(), k.v0 / 16 + ct0, lane);
 
     f32x4 Y[2][NT], gf[2], ff[2], be[2];
-    Split ac[NKT], amt[2], apt[2];
+    Op ac[NKT], amt[2], apt[2];
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      apt[tt] = square_at(cur + St::A_PT, tt, lane);
+      apt[tt] = square_at<Op>(cur + St::A_PT, tt, lane);
       if constexpr (RAW) {
         gf[tt] = St::factor(cur, St::A_G, tt, lane);
         ff[tt] = St::factor(cur, St::A_F, tt, lane);
       }
       if constexpr (DELTA) {
         be[tt] = St::factor(cur, St::A_BETA, tt, lane);
-        amt[tt] = square_at(cur + St::A_MT, tt, lane);
+        amt[tt] = square_at<Op>(cur + St::A_MT, tt, lane);
       }
     }
     // dU
@@ -609,37 +607,41 @@ __device__ __forceinline__ void walk_backward(
     for (int s = 0; s < NKS; ++s)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const Split sb = state_operand<NKT, NT>(D, s, t);
+        const Op sb = state_operand<Op, NKT, NT>(D, s, t);
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) Y[tt][t] = mma_plane<!RAW>(ar[tt][s], sb, s ? Y[tt][t] : zero);
+        for (int tt = 0; tt < 2; ++tt) {
+          if constexpr (!St::AHEAD) ar[tt][s] = St::rows(cur, St::A_K, St::A_KB, tt, s, lane);
+          Y[tt][t] = mma_plane<!RAW>(ar[tt][s], sb, s ? Y[tt][t] : zero);
+        }
       }
 #pragma unroll
     for (int f = 0; f < NKT; ++f)
-      ac[f] = St::cols(cur, St::A_Q, St::A_QH, f, lane);
-    Split gb[NT];
+      if constexpr (St::AHEAD) ac[f] = St::cols(cur, St::A_Q, St::A_QH, f, lane);
+    Op gb[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      gb[t] = tokens_operand<NT>(G, t);
+      gb[t] = tokens_operand<Op, NT>(G, t);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
         Y[tt][t] = mma3(apt[tt], gb[t], RAW ? Y[tt][t] * gf[tt] : Y[tt][t]);
       if constexpr (RAW) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) G[tt][t] *= ff[tt];
-        gb[t] = tokens_operand<NT>(G, t);
+        gb[t] = tokens_operand<Op, NT>(G, t);
       }
     }
     // the outputs' share of D needs nothing of Y
 #pragma unroll
     for (int f = 0; f < NKT; ++f) {
       const f32x4 d = St::decay(cur, f, lane);
+      if constexpr (!St::AHEAD) ac[f] = St::cols(cur, St::A_Q, St::A_QH, f, lane);
 #pragma unroll
       for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(ac[f], gb[t], D[f][t] * d);
     }
     if constexpr (DELTA) {
-      Split rb[NT];
+      Op rb[NT];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) rb[t] = tokens_operand<NT>(Y, t);
+      for (int t = 0; t < NT; ++t) rb[t] = tokens_operand<Op, NT>(Y, t);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
@@ -655,7 +657,7 @@ __device__ __forceinline__ void walk_backward(
           Y[tt][t] *= be[tt];
           m[tt][0] = RAW ? -Y[tt][t] * ff[tt] : -Y[tt][t];
         }
-        const Split yb = tokens_operand<1>(m, 0);
+        const Op yb = tokens_operand<Op, 1>(m, 0);
 #pragma unroll
         for (int f = 0; f < NKT; ++f)
           D[f][t] = mma_plane<!RAW>(St::cols(cur, St::A_K, St::A_KH, f, lane), yb, D[f][t]);
@@ -722,8 +724,9 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
 // segment writes it while the first one may not have started.  Without the delta rule M_j is the decay over the segment.  A step is
 // a chain of one load, one product and one exchange of S through LDS; M_j and L_j do not depend on
 // S and are fetched a step ahead.
-template <int DK, bool RAW, bool DELTA>
+template <int DK, bool RAW, bool DELTA, typename TIN>
 __global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
+  using Op = Operand<TIN>;
   constexpr int NKS = DK / 32, PITCH = 18;     // 8 rows further: 16 banks further
   __shared__ float sh[2][DK * PITCH];
   const int lane = threadIdx.x & 63, f = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
@@ -766,13 +769,13 @@ __global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[(state_key(f, g, 0) + r) * PITCH + c16] = S[r];
       place(j, S);
-      Split am[NKS];
+      Op am[NKS];
 #pragma unroll
       for (int s = 0; s < NKS; ++s) {
         float a[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] = m[2 * s + (e >> 2)][e & 3];
-        am[s] = split8(a);
+        am[s] = operand8<Op>(a);
       }
       S = L;
       const int next = min(j + 1, parts - 2);  // the last one's M is never made
@@ -784,7 +787,7 @@ __global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
         float a[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] = x[(32 * s + 8 * g + e) * PITCH + c16];
-        S = mma3(am[s], split8(a), S);
+        S = mma3(am[s], operand8<Op>(a), S);
       }
     }
   } else {

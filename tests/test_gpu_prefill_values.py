@@ -1,5 +1,5 @@
-"""What whole-sequence calls make of values that a program has by choice or by accident: outputs
-rounded once, log-decays that are not a number or above zero."""
+"""What whole-sequence calls make of values that a program has by choice or by accident: fp32
+inputs, bf16 outputs rounded once, log-decays that are not a number or above zero."""
 
 import pytest
 import torch
@@ -28,6 +28,48 @@ def test_bf16_outputs_are_rounded_once(op, dk, dv, lens):
     size = (want ** 2).mean(-1, keepdim=True).sqrt()
     slack = (c.o.double().cpu() - want).abs() - torch.finfo(BF16).eps / 2 * want.abs()
     assert (slack / size).max().item() <= 4 * R.TOL_F32
+
+
+# fp32 all the way: a sum of up to 128 + 32 terms rounds as often, each time by 2^-24 / sqrt(3) of what
+# it holds (root mean square), so it is off by sqrt(160) of that, 4.4e-7; five such products in a row by
+# sqrt(5) times as much, 1e-6; an exponential adds 2^-23 (its last bit).  Twice that.
+FULL = 2e-6
+
+
+def check_full(c, want, backward):
+    lens, slots = sum(c.x["lens"]), c.x["slots"]
+    pairs = [("o", c.o[:lens], want["o"]), ("S", c.S_out[slots], want["S"][slots])]
+    for name, ref in want.get("grads", {}).items() if backward else ():
+        got = getattr(c.grads, name)
+        if name == "dS":
+            got, ref = got[slots], ref[slots]
+        elif name != "du":
+            got = got[:lens]
+        pairs.append((name, got, ref))
+    errors = {name: R.rel(got, ref) for name, got, ref in pairs}
+    assert max(errors.values()) <= FULL, errors
+
+
+@pytest.mark.parametrize("op", R.OPS)
+@pytest.mark.parametrize("dk,dv", SHAPES)
+def test_fp32_inputs_keep_fp32(op, dk, dv):
+    x = R.inputs(op, [150, 0, 33], 3, dk, dv, F32, F32, seed=4)
+    want = R.expected(op, x, grads=True)
+    c = P.Call(op, x, backward=True)
+    c.build()
+    c.forward()
+    c.backward()
+    check_full(c, want, True)
+
+
+@pytest.mark.parametrize("op", R.OPS)
+def test_fp32_inputs_keep_fp32_over_segments(op):
+    x = R.inputs(op, [1700, 40], 2, 128, 64, F32, F32, seed=5)
+    want = R.expected(op, x)
+    c = P.Call(op, x)
+    c.build()
+    c.forward()
+    check_full(c, want, False)
 
 
 @pytest.mark.parametrize("op", [o for o in R.OPS if o != "linattn"])
