@@ -133,7 +133,7 @@ template <int DC, int DK, int DV, bool DELTA, typename TIN>
 __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kernel(SeqParams p) {
   using Sh = GradShared<DC, DK, DV, TIN>;
   using Op = Operand<TIN>;
-  constexpr int NTH = 4 * DK, NW = DK / 16, KT = 1, HALF = Sh::HALF, NP = Sh::NP;
+  constexpr int NTH = 4 * DK, NW = DK / 16, HALF = Sh::HALF, NP = Sh::NP;
   constexpr bool LO = Sh::LO;
   __shared__ Sh sh;
   ChunkIn<DC, DK, TIN>& in = sh.in;
@@ -170,20 +170,20 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
     return rows_operand<Op, NP>(sh.planes + at, lo ? HALF : 0, tt, s, lane);
   };
   // Products over the value columns: token x key ...
-  f32x4 aq[KT][2], ar[KT][2], ac[KT][2];
-  float dot[KT] = {0.f};
+  f32x4 aq[2], ar[2], ac[2];
+  float dot = 0.f;
 #pragma unroll
-  for (int tt = 0; tt < 2; ++tt) aq[0][tt] = ar[0][tt] = ac[0][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int tt = 0; tt < 2; ++tt) aq[tt] = ar[tt] = ac[tt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int s = 0; s < DV / 32; ++s) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dot[0] += xs[s][e] * xd[s][e];
+    for (int e = 0; e < 8; ++e) dot += xs[s][e] * xd[s][e];
     const Op bs = operand8<Op>(xs[s]), bd = operand8<Op>(xd[s]);
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      aq[0][tt] = mma_plane<LO>(operand(Sh::A_DO, LO, tt, s), bs, aq[0][tt]);
-      if constexpr (DELTA) ar[0][tt] = mma3(operand(Sh::A_Z, true, tt, s), bs, ar[0][tt]);
-      ac[0][tt] = mma3(operand(Sh::A_E, true, tt, s), bd, ac[0][tt]);
+      aq[tt] = mma_plane<LO>(operand(Sh::A_DO, LO, tt, s), bs, aq[tt]);
+      if constexpr (DELTA) ar[tt] = mma3(operand(Sh::A_Z, true, tt, s), bs, ar[tt]);
+      ac[tt] = mma3(operand(Sh::A_E, true, tt, s), bd, ac[tt]);
     }
   }
   // ... and token x token: block (0,0), (1,1) or (1,0) of dP and dG by one wave each.
@@ -229,177 +229,175 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
   for (int e = 0; e < 8; ++e) ck[e] = cq[e] = 0.f;
   float bnd_all = 0.f;
 
+  const int key = 16 * wave + c16;
+  float k[8], q[8], l[8], lq[8];
+  lane_tokens(in.k, wave, lane, k);
+  lane_tokens(in.q, wave, lane, q);
+  const float lT = in.at(CT - 1, key);
 #pragma unroll
-  for (int x = 0; x < KT; ++x) {
-    const int f = wave * KT + x, key = 16 * f + c16;
-    float k[8], q[8], l[8], lq[8];
-    lane_tokens(in.k, f, lane, k);
-    lane_tokens(in.q, f, lane, q);
-    const float lT = in.at(CT - 1, key);
+  for (int e = 0; e < 8; ++e) {
+    l[e] = in.at(state_term(lane, e), key);
+    lq[e] = DC == DC_BONUS ? in.at_q(state_term(lane, e), key) : l[e];
+  }
+  float share = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int tt = e >> 2, r = e & 3;
+    const float fl = exp2_of(l[e]), fr = exp2_of(lT - l[e]) * be[tt][r];
+    aq[tt][r] *= DC == DC_BONUS ? exp2_of(lq[e]) : fl;
+    ar[tt][r] *= -fl * be[tt][r];
+    ac[tt][r] *= fr;
+    share += k[e] * ac[tt][r];
+  }
+  float bnd = dot * exp2_of(lT) + share;
+  bnd += __shfl_xor(bnd, 16);
+  bnd += __shfl_xor(bnd, 32);
+
+  // pairs inside the chunk
+  if constexpr (DC == DC_SCALAR) {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      aq[tt] = pair_mma<false>(dP, tt, k, aq[tt], lane);
+      ac[tt] = pair_mma<true>(dP, tt, q, ac[tt], lane);
+      if constexpr (DELTA) {
+        ar[tt] = pair_mma<false>(dG, tt, k, ar[tt], lane);
+        ac[tt] = pair_mma<true>(dG, tt, k, ac[tt], lane);
+      }
+    }
+  } else if (!in.wide) {
+    // Rows of the first half against m = l_7, of the second against m = l_23: e^{l_i - m}
+    // outside the product, e^{m - l_j} inside.  The first half's rows use no token of the
+    // second (0 there: its factor could overflow); the second half's factors of earlier
+    // tokens are at most 1.  For dk'' the two change places.
+    const float m0 = in.at(7, key), m1 = in.at(23, key);
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    float s0[8], s1[8];
+    f32x4 pq[2], pr[2], pc[2];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      l[e] = in.at(state_term(lane, e), key);
-      lq[e] = DC == DC_BONUS ? in.at_q(state_term(lane, e), key) : l[e];
+      s0[e] = e < 4 ? k[e] * exp2_of(m0 - l[e]) : 0.f;
+      s1[e] = k[e] * exp2_of(m1 - l[e]);
     }
-    float share = 0.f;
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      pq[tt] = pair_mma<false>(dP, tt, tt ? s1 : s0, zero, lane);
+      if constexpr (DELTA) pr[tt] = pair_mma<false>(dG, tt, tt ? s1 : s0, zero, lane);
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int tt = e >> 2, r = e & 3;
-      const float fl = exp2_of(l[e]), fr = exp2_of(lT - l[e]) * be[tt][r];
-      aq[x][tt][r] *= DC == DC_BONUS ? exp2_of(lq[e]) : fl;
-      ar[x][tt][r] *= -fl * be[tt][r];
-      ac[x][tt][r] *= fr;
-      share += k[e] * ac[x][tt][r];
+      const float m = tt ? m1 : m0;
+      const float out = exp2_of(l[e] - m);
+      aq[tt][r] += pq[tt][r] * (DC == DC_BONUS ? exp2_of(lq[e] - m) : out);
+      if constexpr (DELTA) ar[tt][r] += pr[tt][r] * out;
+      s0[e] = q[e] * exp2_of(lq[e] - m0);
+      s1[e] = e < 4 ? 0.f : q[e] * exp2_of(lq[e] - m1);
     }
-    float bnd = dot[x] * exp2_of(lT) + share;
-    bnd += __shfl_xor(bnd, 16);
-    bnd += __shfl_xor(bnd, 32);
-
-    // pairs inside the chunk
-    if constexpr (DC == DC_SCALAR) {
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        aq[x][tt] = pair_mma<false>(dP, tt, k, aq[x][tt], lane);
-        ac[x][tt] = pair_mma<true>(dP, tt, q, ac[x][tt], lane);
-        if constexpr (DELTA) {
-          ar[x][tt] = pair_mma<false>(dG, tt, k, ar[x][tt], lane);
-          ac[x][tt] = pair_mma<true>(dG, tt, k, ac[x][tt], lane);
-        }
-      }
-    } else if (!in.wide) {
-      // Rows of the first half against m = l_7, of the second against m = l_23: e^{l_i - m}
-      // outside the product, e^{m - l_j} inside.  The first half's rows use no token of the
-      // second (0 there: its factor could overflow); the second half's factors of earlier
-      // tokens are at most 1.  For dk'' the two change places.
-      const float m0 = in.at(7, key), m1 = in.at(23, key);
-      const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-      float s0[8], s1[8];
-      f32x4 pq[2], pr[2], pc[2];
+    for (int tt = 0; tt < 2; ++tt) pc[tt] = pair_mma<true>(dP, tt, tt ? s1 : s0, zero, lane);
+    if constexpr (DELTA) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        s0[e] = e < 4 ? k[e] * exp2_of(m0 - l[e]) : 0.f;
-        s1[e] = k[e] * exp2_of(m1 - l[e]);
+        s0[e] = k[e] * exp2_of(l[e] - m0);
+        s1[e] = e < 4 ? 0.f : k[e] * exp2_of(l[e] - m1);
       }
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        pq[tt] = pair_mma<false>(dP, tt, tt ? s1 : s0, zero, lane);
-        if constexpr (DELTA) pr[tt] = pair_mma<false>(dG, tt, tt ? s1 : s0, zero, lane);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int tt = e >> 2, r = e & 3;
-        const float m = tt ? m1 : m0;
-        const float out = exp2_of(l[e] - m);
-        aq[x][tt][r] += pq[tt][r] * (DC == DC_BONUS ? exp2_of(lq[e] - m) : out);
-        if constexpr (DELTA) ar[x][tt][r] += pr[tt][r] * out;
-        s0[e] = q[e] * exp2_of(lq[e] - m0);
-        s1[e] = e < 4 ? 0.f : q[e] * exp2_of(lq[e] - m1);
-      }
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) pc[tt] = pair_mma<true>(dP, tt, tt ? s1 : s0, zero, lane);
-      if constexpr (DELTA) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          s0[e] = k[e] * exp2_of(l[e] - m0);
-          s1[e] = e < 4 ? 0.f : k[e] * exp2_of(l[e] - m1);
-        }
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) pc[tt] = pair_mma<true>(dG, tt, tt ? s1 : s0, pc[tt], lane);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        ac[x][e >> 2][e & 3] += pc[e >> 2][e & 3] * exp2_of((e < 4 ? m0 : m1) - l[e]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int tt = e >> 2, r = e & 3, i = state_term(lane, e);
-        float sq = 0.f, sr = 0.f, sc = 0.f;
-#pragma unroll 1
-        for (int j = 0; j < CT; ++j) {
-          const float kj = widen(in.k[j][key]), qj = widen(in.q[j][key]);
-          const float lj = in.at(j, key), lqj = in.at_q(j, key);
-          if (j < i || (j == i && DC == DC_KEY)) {
-            sq += dP[i][j] * kj * exp2_of(lq[e] - lj);
-            sr += dG[i][j] * kj * exp2_of(l[e] - lj);
-          }
-          if (j > i || (j == i && DC == DC_KEY))
-            sc += dP[j][i] * qj * exp2_of(lqj - l[e]) + dG[j][i] * kj * exp2_of(lj - l[e]);
-        }
-        aq[x][tt][r] += sq;
-        ar[x][tt][r] += sr;
-        ac[x][tt][r] += sc;
-      }
+      for (int tt = 0; tt < 2; ++tt) pc[tt] = pair_mma<true>(dG, tt, tt ? s1 : s0, pc[tt], lane);
     }
-
-    // log-decays
-    if constexpr (DC == DC_SCALAR) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        ck[e] += q[e] * aq[x][e >> 2][e & 3] + k[e] * (ar[x][e >> 2][e & 3] - ac[x][e >> 2][e & 3]);
-      bnd_all += bnd;
-      // Every product is read here, ahead of the branches around the stores below (see SL's
-      // note on branches and accumulators): the sums may not move past them.
-#pragma unroll
-      for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(ck[e]));
-    } else {
-      // suffix sums over tokens: over r in the lane, over g across lanes, then the halves
-      float sum[2], after[2];
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        float s = 0.f;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          ck[4 * tt + r] = k[4 * tt + r] * (ar[x][tt][r] - ac[x][tt][r]);
-          cq[4 * tt + r] = q[4 * tt + r] * aq[x][tt][r];
-          s += ck[4 * tt + r] + cq[4 * tt + r];
-        }
-        float y = __shfl_down(s, 16);
-        float t = s + (g < 3 ? y : 0.f);
-        y = __shfl_down(t, 32);
-        t += g < 2 ? y : 0.f;
-        sum[tt] = __shfl(t, c16);
-        y = __shfl_down(t, 16);
-        after[tt] = g < 3 ? y : 0.f;
-      }
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        float acc = bnd + (tt ? 0.f : sum[1]) + after[tt];
-#pragma unroll
-        for (int r = 3; r >= 0; --r) {
-          const int t = 16 * tt + 4 * g + r;
-          acc += ck[4 * tt + r];
-          if (DC == DC_KEY) acc += cq[4 * tt + r];
-          if (t < row.count) p.dlam[(int64_t(row.first + t) * p.H + h) * DK + key] = acc;
-          if (DC == DC_BONUS) acc += cq[4 * tt + r];
-        }
-      }
-    }
-
-    // queries and keys
-    TIN* dqp = static_cast<TIN*>(p.dq) + (int64_t(row.first) * p.H + h) * DK + key;
-    TIN* dkp = static_cast<TIN*>(p.dk_) + (int64_t(row.first) * p.H + h) * DK + key;
-    const float u = DC == DC_BONUS ? p.u[int64_t(h) * DK + key] : 0.f;
-    float dus = 0.f;
+    for (int e = 0; e < 8; ++e)
+      ac[e >> 2][e & 3] += pc[e >> 2][e & 3] * exp2_of((e < 4 ? m0 : m1) - l[e]);
+  } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int tt = e >> 2, r = e & 3, t = 16 * tt + 4 * g + r;
-      float xq = aq[x][tt][r], xk = ar[x][tt][r] + ac[x][tt][r];
-      if constexpr (DC == DC_BONUS) {
-        const float own_pair = tok_sum[0][t];
-        xq += own_pair * u * k[e];
-        xk += own_pair * u * q[e];
-        dus += own_pair * q[e] * k[e];
+      const int tt = e >> 2, r = e & 3, i = state_term(lane, e);
+      float sq = 0.f, sr = 0.f, sc = 0.f;
+#pragma unroll 1
+      for (int j = 0; j < CT; ++j) {
+        const float kj = widen(in.k[j][key]), qj = widen(in.q[j][key]);
+        const float lj = in.at(j, key), lqj = in.at_q(j, key);
+        if (j < i || (j == i && DC == DC_KEY)) {
+          sq += dP[i][j] * kj * exp2_of(lq[e] - lj);
+          sr += dG[i][j] * kj * exp2_of(l[e] - lj);
+        }
+        if (j > i || (j == i && DC == DC_KEY))
+          sc += dP[j][i] * qj * exp2_of(lqj - l[e]) + dG[j][i] * kj * exp2_of(lj - l[e]);
       }
-      if (t < row.count) {
-        narrow(dqp + int64_t(t) * p.H * DK, xq);
-        narrow(dkp + int64_t(t) * p.H * DK, xk);
+      aq[tt][r] += sq;
+      ar[tt][r] += sr;
+      ac[tt][r] += sc;
+    }
+  }
+
+  // log-decays
+  if constexpr (DC == DC_SCALAR) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      ck[e] += q[e] * aq[e >> 2][e & 3] + k[e] * (ar[e >> 2][e & 3] - ac[e >> 2][e & 3]);
+    bnd_all += bnd;
+    // Every product is read here, ahead of the branches around the stores below: behind a taken
+    // branch the compiler has let other instructions overwrite the addend of an MFMA that was
+    // still running.  So the sums may not move past them.
+#pragma unroll
+    for (int e = 0; e < 8; ++e) asm volatile("" : "+v"(ck[e]));
+  } else {
+    // suffix sums over tokens: over r in the lane, over g across lanes, then the halves
+    float sum[2], after[2];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      float s = 0.f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        ck[4 * tt + r] = k[4 * tt + r] * (ar[tt][r] - ac[tt][r]);
+        cq[4 * tt + r] = q[4 * tt + r] * aq[tt][r];
+        s += ck[4 * tt + r] + cq[4 * tt + r];
+      }
+      float y = __shfl_down(s, 16);
+      float t = s + (g < 3 ? y : 0.f);
+      y = __shfl_down(t, 32);
+      t += g < 2 ? y : 0.f;
+      sum[tt] = __shfl(t, c16);
+      y = __shfl_down(t, 16);
+      after[tt] = g < 3 ? y : 0.f;
+    }
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      float acc = bnd + (tt ? 0.f : sum[1]) + after[tt];
+#pragma unroll
+      for (int r = 3; r >= 0; --r) {
+        const int t = 16 * tt + 4 * g + r;
+        acc += ck[4 * tt + r];
+        if (DC == DC_KEY) acc += cq[4 * tt + r];
+        if (t < row.count) p.dlam[(int64_t(row.first + t) * p.H + h) * DK + key] = acc;
+        if (DC == DC_BONUS) acc += cq[4 * tt + r];
       }
     }
+  }
+
+  // queries and keys
+  TIN* dqp = static_cast<TIN*>(p.dq) + (int64_t(row.first) * p.H + h) * DK + key;
+  TIN* dkp = static_cast<TIN*>(p.dk_) + (int64_t(row.first) * p.H + h) * DK + key;
+  const float u = DC == DC_BONUS ? p.u[int64_t(h) * DK + key] : 0.f;
+  float dus = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int tt = e >> 2, r = e & 3, t = 16 * tt + 4 * g + r;
+    float xq = aq[tt][r], xk = ar[tt][r] + ac[tt][r];
     if constexpr (DC == DC_BONUS) {
-      dus += __shfl_xor(dus, 16);
-      dus += __shfl_xor(dus, 32);
-      if (g == 0) du[key] = dus;
+      const float own_pair = tok_sum[0][t];
+      xq += own_pair * u * k[e];
+      xk += own_pair * u * q[e];
+      dus += own_pair * q[e] * k[e];
     }
+    if (t < row.count) {
+      narrow(dqp + int64_t(t) * p.H * DK, xq);
+      narrow(dkp + int64_t(t) * p.H * DK, xk);
+    }
+  }
+  if constexpr (DC == DC_BONUS) {
+    dus += __shfl_xor(dus, 16);
+    dus += __shfl_xor(dus, 32);
+    if (g == 0) du[key] = dus;
   }
 
   if constexpr (DC == DC_SCALAR) {
