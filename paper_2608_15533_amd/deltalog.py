@@ -380,7 +380,7 @@ class ChunkTables:
     def __init__(self, n, tokens, num_slots=None, device="cuda"):
         i32 = dict(dtype=torch.int32, device=device)
         self.n, self.tokens = int(n), int(tokens)
-        self.num_slots = self.n if num_slots is None else int(num_slots)
+        self.num_slots = max(self.n, 1) if num_slots is None else int(num_slots)
         self.cu_tokens = torch.zeros((self.n + 1,), **i32)
         self.cu_chunks = torch.zeros((self.n + 1,), **i32)
         self.chunks = torch.zeros((self.tokens // DL_CHUNK + self.n, 4), **i32)

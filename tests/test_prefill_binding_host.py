@@ -2,6 +2,8 @@
 another descriptor or row count are refused before the library is called (the kernels would read or
 write past them).  Stand-ins for device tensors: only what the checks look at."""
 
+import types
+
 import pytest
 import torch
 
@@ -96,3 +98,14 @@ def test_rows_that_do_not_add_up():
         forward(desc, tok, S, o, n=41)
     with pytest.raises(ValueError, match="40 rows but the tables are for 41"):
         backward(desc, tok, S, o, grads, n=41)
+
+
+def test_no_sequences_are_no_work(monkeypatch):
+    monkeypatch.setattr(D, "_on_current_device", lambda *a: None)
+    desc, tok, S, o, grads = case()
+    tables = D.ChunkTables(0, 40, device="cpu")
+    D.dl_chunk_tables(Device(torch.int32, 0), tables, stream=0)
+    ws = types.SimpleNamespace(is_cuda=True, is_contiguous=lambda: True, data_ptr=lambda: 0,
+                               numel=lambda: 0, element_size=lambda: 1)
+    D.dl_prefill(desc, S, S, tok, o, tables, ws, stream=0)
+    D.dl_prefill_backward(desc, S, tok, o, None, grads, tables, ws, stream=0)
