@@ -19,8 +19,8 @@
 // the workgroup into planes in LDS, from which every wave reads its operands; S and D, which
 // no two waves share, go from memory to registers.
 //
-// Bound by the saved states: 2 x 2048 tokens, 32 heads of 128 x 128 (GDN, bf16) 177 us for 780 MB
-// read and 76 MB written, 4.8 TB/s; waves wait for them half of their time.
+// Bound by the saved states: 2 x 2048 tokens, 32 heads of 128 x 128 (GDN, bf16) 176 us for 780 MB
+// read and 76 MB written, 4.9 TB/s; waves wait for them half of their time.
 #pragma once
 
 #include "dl_prep.hpp"

@@ -345,8 +345,8 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
 }
 
 // BWD: for the backward pass.
-// Bound by memory: 12345 tokens, 32 heads of 128 keys (KDA, bf16) 180 us for 417 MB read and
-// 621 MB written (the planes), 5.8 TB/s, where a large copy reaches 5.55.
+// Bound by memory: 12345 tokens, 32 heads of 128 keys (KDA, bf16) 188 us for 417 MB read and
+// 724 MB written (the planes), 6.1 TB/s, where a large copy reaches 5.55.
 template <int DC, int DK, bool DELTA, bool BWD, typename TIN>
 __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
   __shared__ ChunkIn<DC, DK, TIN> in;

@@ -139,9 +139,9 @@ __device__ __forceinline__ void store_state(void* S, bool bf16, int64_t i, float
 
 // ------------------------------------------------------------------ operands in LDS
 // A token x key plane: 32 rows of 16-byte pieces (8 bf16; of Full planes four fp32, the other four in
-// the second half), piece x of row r at piece_at(r, x).  The exchange of pieces within a row lets 16 rows of one piece (an operand
-// over keys) and four pieces of four rows (one over tokens) each lie in different banks.
-// NP: pieces in a row.
+// the second half), piece x of row r at piece_at(r, x).  The exchange of pieces within a row lets 16
+// rows of one piece (an operand over keys) and four pieces of four rows (one over tokens) each lie in
+// different banks.  NP: pieces in a row.
 template <int NP>
 __host__ __device__ constexpr int piece_swap(int r) {
   return NP >= 16  ? ((r & 3) << 2) | ((r >> 2) & 3)
@@ -208,8 +208,9 @@ __device__ __forceinline__ OP cols_operand(const unsigned char* plane, int half,
 //           bf16 keys and queries with one log-decay per head or none: the keys and queries
 //           themselves are the planes, exact in bf16, and e^{l_i} (f) and e^{l_T-l_i} (g)
 //           scale token rows of fp32 products instead.
-//   squares N (beta N where no backward pass asks for E), P and (backward) P^T, M^T: token x token, two halves, in fragment order: the
-//           eight terms (state order) a lane feeds one MFMA are 16 consecutive bytes.
+//   squares N (beta N where no backward pass asks for E), P and (backward) P^T, M^T: token x token,
+//           two halves, in fragment order: a half of the eight terms (state order) that a lane feeds
+//           a product is 16 consecutive bytes.
 // The first half lies before the second.  The order makes what one pass reads of a block two runs
 // of bytes (a pass without outputs takes neither P nor Qh).
 struct WsLayout {
@@ -279,11 +280,12 @@ inline int walk_waves(int64_t heads, int dk, int dv, bool raw) {
 // the delta rule M is the decay.  That is about 2.3 times the work (1.5 without the delta rule) in
 // as many parallel parts as there is room for, and worth it up to 320 waves (then there are three
 // parts at least) and from 48 chunks a sequence on average.  Workgroups of four waves.
-// Measured, one bf16 sequence, whole call, whole -> in segments, us: GDN 128 x 128, 8 heads of
-// 8192 tokens 337 -> 116, 32 of 3200 152 -> 132, 32 of 1536 81 -> 78, 64 of 2048 (512 waves) 116 ->
-// 130; KDA, the same, 478 -> 188, 240 -> 238, 124 -> 118, 228 -> 238; RWKV6 64 x 64, 40 heads of
-// 4096 129 -> 87.  32 GDN heads of 8192: walk whole 330; in four segments 120 for L and M, 12 for
-// the states, 112 for the outputs; in three 113 + 9 + 140, in five 110 + 15 + 127.
+// Measured, one bf16 sequence, whole call with its tables, whole -> in segments, us: GDN 128 x 128, 8
+// heads of 8192 tokens 375 -> 114, 32 of 3200 165 -> 121, 32 of 1536 89 -> 77, 64 of 2048 (512 waves)
+// 120 -> 127; KDA, the same, 591 -> 180, 278 -> 221, 144 -> 120, 228 -> 227; RWKV6 64 x 64, 40 heads of
+// 4096 174 -> 106; fp32 GDN 1235 -> 269, 542 -> 361, 263 -> 180.  32 GDN heads of 8192: whole 400; in
+// four segments 268, of which 118 for L and M, 14 for the states, 116 for the outputs; in three 282, in
+// five 271.
 struct SegPlan {
   int len, segs;          // chunks of a segment (0: none), room for segments
 };

@@ -706,10 +706,10 @@ __device__ __forceinline__ int xcd_place(int b, int groups, int share) {
   return b - in + in % ROUND * share + in / ROUND;
 }
 
-// One wave to a SIMD (64 heads of 2048 tokens, 128 x 128, GDN, bf16): 100 us, 1.6 a chunk; the wave
-// issues in 61% of its cycles (vector instructions 35%, matrix cores busy 23%) and waits for its
-// own results in the rest: it is one chain.  Two (256 heads of 4096): 345 us, vector 53% and matrix 30%
-// of a SIMD's cycles, 1.4 GB moved, 4.1 TB/s.
+// One wave to a SIMD (64 heads of 2048 tokens, 128 x 128, GDN, bf16): 107 us, 1.7 a chunk; the wave
+// issues in 61% of its cycles (vector instructions 36%, matrix cores busy 26%) and waits for its
+// own results in the rest: it is one chain.  Two (256 heads of 4096): 359 us, vector 55% and matrix 35%
+// of a SIMD's cycles, 1.4 GB moved, 3.9 TB/s.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, int PASS, typename TIN>
 __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
   __shared__ __attribute__((aligned(16))) unsigned char
@@ -721,9 +721,9 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
 // The states between a sequence's segments, one after the other, a workgroup for 16 columns and a
 // wave for 16 keys of them: S_1 = L_0 (segment 0 started from the initial state), S_j+1 = M_j S_j +
 // L_j; S_j takes L_j's place, and the initial state that of L_0: where S_out is S_in, the last
-// segment writes it while the first one may not have started.  Without the delta rule M_j is the decay over the segment.  A step is
-// a chain of one load, one product and one exchange of S through LDS; M_j and L_j do not depend on
-// S and are fetched a step ahead.
+// segment writes it while the first one may not have started.  Without the delta rule M_j is the
+// decay over the segment.  A step is a chain of one load, one product and one exchange of S through
+// LDS; M_j and L_j do not depend on S and are fetched a step ahead.
 template <int DK, bool RAW, bool DELTA, typename TIN>
 __global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
   using Op = Operand<TIN>;
@@ -810,7 +810,7 @@ __global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
 
 // The backward pass's two walks in one launch: neither needs the other, and each alone leaves
 // most of the chip waiting while sequences and heads are few (64 heads of 2048 tokens, 128 x 128:
-// 139 + 186 us one after the other, 260 in one launch: 235 MB read and 732 MB written, of which
+// 139 + 186 us one after the other, 256 in one launch: 234 MB read and 732 MB written, of which
 // the states before and the state gradients after every chunk are 537).  Even workgroups go
 // backward, odd ones forward.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
