@@ -105,14 +105,14 @@ __device__ __forceinline__ void load_planes(GradShared<DC, DK, DV, TIN>& sh, con
       load8(d, o);
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i] = live ? o[i] : 0.f;
-      put<TIN>(sh.planes + Sh::A_DO, Sh::HALF, at, o);
+      put(sh.planes + Sh::A_DO, Sh::HALF, at, o);
     } else {
       const u32x4 zero = {0, 0, 0, 0}, o = *reinterpret_cast<const u32x4*>(d);
       *reinterpret_cast<u32x4*>(sh.planes + Sh::A_DO + 16 * at) = live ? o : zero;
     }
-    put<TIN>(sh.planes + Sh::A_E, Sh::HALF, at, e);
+    put(sh.planes + Sh::A_E, Sh::HALF, at, e);
     if constexpr (DELTA) {
-      put<TIN>(sh.planes + Sh::A_Z, Sh::HALF, at, z);
+      put(sh.planes + Sh::A_Z, Sh::HALF, at, z);
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += e[i] * z[i];
@@ -132,9 +132,10 @@ constexpr int grad_waves() {
 template <int DC, int DK, int DV, bool DELTA, typename TIN>
 __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kernel(SeqParams p) {
   using Sh = GradShared<DC, DK, DV, TIN>;
-  using Op = Operand<TIN>;
   constexpr int NTH = 4 * DK, NW = DK / 16, HALF = Sh::HALF, NP = Sh::NP;
   constexpr bool LO = Sh::LO;
+  using Out = std::conditional_t<LO, Full, bf16x8>;      // dO's rows, and what they are multiplied with
+  using By = std::conditional_t<LO, Full, Three>;
   __shared__ Sh sh;
   ChunkIn<DC, DK, TIN>& in = sh.in;
   auto& dP = sh.dP;
@@ -166,8 +167,8 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
                                     reinterpret_cast<const float*>(blk + w.z()), tid);
   in.template load<NTH, DELTA>(p, row, h, tid);   // and every thread past this point
 
-  auto operand = [&](int at, bool lo, int tt, int s) {
-    return rows_operand<Op, NP>(sh.planes + at, lo ? HALF : 0, tt, s, lane);
+  auto operand = [&](int at, int tt, int s) {
+    return rows_operand<Full, NP>(sh.planes + at, HALF, tt, s, lane);
   };
   // Products over the value columns: token x key ...
   f32x4 aq[2], ar[2], ac[2];
@@ -178,13 +179,16 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
   for (int s = 0; s < DV / 32; ++s) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) dot += xs[s][e] * xd[s][e];
-    const Op bs = operand8<Op>(xs[s]), bd = operand8<Op>(xd[s]);
+    const Full bs = full8(xs[s]), bd = full8(xd[s]);
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      aq[tt] = mma_plane<LO>(operand(Sh::A_DO, LO, tt, s), bs, aq[tt]);
-      if constexpr (DELTA) ar[tt] = mma3(operand(Sh::A_Z, true, tt, s), bs, ar[tt]);
-      ac[tt] = mma3(operand(Sh::A_E, true, tt, s), bd, ac[tt]);
+      if constexpr (DELTA) ar[tt] = mma(operand(Sh::A_Z, tt, s), bs, ar[tt]);
+      ac[tt] = mma(operand(Sh::A_E, tt, s), bd, ac[tt]);
     }
+    const By bo = operand8<By>(xs[s]);
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+      aq[tt] = mma(rows_operand<Out, NP>(sh.planes + Sh::A_DO, HALF, tt, s, lane), bo, aq[tt]);
   }
   // ... and token x token: block (0,0), (1,1) or (1,0) of dP and dG by one wave each.
   f32x4 ap = {0.f, 0.f, 0.f, 0.f}, ag = ap;
@@ -192,9 +196,17 @@ __global__ __launch_bounds__(4 * DK, (grad_waves<DC, DK, TIN>())) void grad_kern
   if (wave < 3) {
 #pragma unroll
     for (int s = 0; s < DV / 32; ++s) {
-      const Op b = operand(Sh::A_E, true, bj, s);
-      ap = mma_plane<LO>(operand(Sh::A_DO, LO, bi, s), b, ap);
-      if constexpr (DELTA) ag = mma3(operand(Sh::A_Z, true, bi, s), b, ag);
+      const Full b = operand(Sh::A_E, bj, s);
+      if constexpr (LO) {
+        ap = mma(operand(Sh::A_DO, bi, s), b, ap);
+      } else {
+        const bf16x8 o = rows_operand<bf16x8, NP>(sh.planes + Sh::A_DO, 0, bi, s, lane);
+        float a[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] = (float)o[e];
+        ap = mma(full8(a), b, ap);
+      }
+      if constexpr (DELTA) ag = mma(operand(Sh::A_Z, bi, s), b, ag);
     }
   }
   __syncthreads();                                // the squares take the planes' place

@@ -44,14 +44,14 @@ hipError_t launch_walk(const SeqParams& p, hipStream_t s) {
     // columns of values and of M, four tiles a workgroup: one workgroup is of one kind
     const int64_t segs = int64_t(p.segs) * p.H, cols = tiles + (DELTA ? DK / 16 : 0);
     hipError_t e = start(&forward_kernel<DK, 1, 4, RAW, DELTA, PASS_SEG, TIN>, segs * (cols / 4), 256, p, s);
-    if (e == hipSuccess) e = start(&join_kernel<DK, RAW, DELTA, TIN>, heads * tiles, 4 * DK, p, s);
+    if (e == hipSuccess) e = start(&join_kernel<DK, RAW, DELTA>, heads * tiles, 4 * DK, p, s);
     if (e != hipSuccess) return e;
     return start(&forward_kernel<DK, 1, 4, RAW, DELTA, PASS_OUT, TIN>, segs * (tiles / 4), 256, p, s);
   }
   int waves = walk_waves(heads, DK, p.dv, RAW);
-  // fp32 delta-rule heads of 128 keys: two waves' registers do not hold a chunk on its way to LDS
-  // beside what they compute with, and four take the same time (1 to 128 heads of 1024 tokens).
-  constexpr bool TWO = !(DK == 128 && DELTA && sizeof(TIN) == 4);
+  // Delta-rule heads of 128 keys with planes: two waves' registers do not hold a chunk on its way to LDS
+  // beside what they compute with, and four take the same time (fp32, 2 to 64 heads of 1024 tokens).
+  constexpr bool TWO = !(DK == 128 && DELTA && !RAW);
   if (!TWO && waves == 2) waves = 4;
   const int64_t grid = heads * (tiles / waves);
   switch (waves) {

@@ -301,15 +301,19 @@ __device__ __forceinline__ void solve(float (*G)[SL], float (*M)[SL], const floa
 }
 
 // Eight values as the two halves of an operand.
-template <typename TIN>
 __device__ __forceinline__ void put(unsigned char* base, int half, int unit, const float* x) {
-  const Operand<TIN> s = operand8<Operand<TIN>>(x);
-  *reinterpret_cast<decltype(s.hi)*>(base + 16 * unit) = s.hi;
-  *reinterpret_cast<decltype(s.lo)*>(base + half + 16 * unit) = s.lo;
+  const Full s = full8(x);
+  *reinterpret_cast<f32x4*>(base + 16 * unit) = s.hi;
+  *reinterpret_cast<f32x4*>(base + half + 16 * unit) = s.lo;
+}
+__device__ __forceinline__ void put_pair(unsigned char* base, int half, int unit, const float* x) {
+  const Pair s = operand8<Pair>(x);
+  *reinterpret_cast<bf16x8*>(base + 16 * unit) = s.a;
+  *reinterpret_cast<bf16x8*>(base + half + 16 * unit) = s.b;
 }
 
 // The squares from LDS matrices, by NTH threads.
-template <int NTH, bool DELTA, bool BWD, typename TIN>
+template <int NTH, bool DELTA, bool BWD>
 __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& w,
                                             const float (*P)[SL], const float (*N)[SL],
                                             const float (*M)[SL], const float* beta, int tid) {
@@ -325,20 +329,20 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
     };
     if constexpr (!BWD) {
       row(P, 1.f);
-      put<TIN>(blk + w.p(), WsLayout::SQ, x, a);
+      put(blk + w.p(), WsLayout::SQ, x, a);
     }
     if constexpr (DELTA) {
       row(N, BWD ? 1.f : beta[i]);
-      put<TIN>(blk + w.n(), WsLayout::SQ, x, a);
+      put(blk + w.n(), WsLayout::SQ, x, a);
     }
     if constexpr (BWD) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) a[e] = P[state_term(lane, e)][i];
-      put<TIN>(blk + w.pt(), WsLayout::SQ, x, a);
+      put(blk + w.pt(), WsLayout::SQ, x, a);
       if constexpr (DELTA) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] = M[state_term(lane, e)][i];
-        put<TIN>(blk + w.mt(), WsLayout::SQ, x, a);
+        put(blk + w.mt(), WsLayout::SQ, x, a);
       }
     }
   }
@@ -384,12 +388,13 @@ __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
       lT[e] = k[e] * exp2_of(lT[e] - l[e]);
       k[e] *= f[e];
     }
-    if constexpr (DELTA) put<TIN>(blk + w.kh(), w.plane(), at, k);
-    put<TIN>(blk + w.qh(), w.plane(), at, q);
-    put<TIN>(blk + w.kb(), w.plane(), at, lT);
+    if constexpr (DELTA) put(blk + w.kh(), w.plane(), at, k);
+    if constexpr (!BWD && sizeof(TIN) == 2) put_pair(blk + w.qh(), w.plane(), at, q);
+    else put(blk + w.qh(), w.plane(), at, q);
+    put(blk + w.kb(), w.plane(), at, lT);
   }
   __syncthreads();
-  put_squares<256, DELTA, BWD, TIN>(blk, w, P, G, M, in.beta, tid);
+  put_squares<256, DELTA, BWD>(blk, w, P, G, M, in.beta, tid);
 }
 
 // The same for bf16 keys and queries with one log-decay per head or none, one wave per
@@ -463,7 +468,7 @@ __global__ __launch_bounds__(64) void raw_prep_kernel(SeqParams p) {
   __syncthreads();
   if constexpr (DELTA) solve<BWD>(G, M, betas, lane);
   __syncthreads();
-  put_squares<64, DELTA, BWD, uint16_t>(blk, w, P, G, M, betas, lane);
+  put_squares<64, DELTA, BWD>(blk, w, P, G, M, betas, lane);
 }
 
 }  // namespace dl

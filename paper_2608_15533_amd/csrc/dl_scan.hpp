@@ -34,42 +34,54 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-// Eight terms of an fp32 operand, for calls with bf16 inputs: two bf16 numbers each, hi the nearest
-// bf16, lo the nearest bf16 to what hi leaves.  hi + lo is within 2^-18 of the value (half a bf16
-// step, twice), and of the product of two such operands the three terms hi hi, hi lo and lo hi are
-// kept: what is left out is another 2^-18, where the inputs' own rounding was 2^-9.  Three bf16
-// MFMAs of 32 terms take 48 cycles, eight fp32 ones 256.
-struct Split {
-  bf16x8 hi, lo;
-};
-// For calls with fp32 inputs: as they are, terms 0 to 3 in hi and 4 to 7 in lo.  The same bytes, in
-// the same places of memory and LDS, as a Split.
+// Eight terms of an fp32 operand of fp32 MFMAs, terms 0 to 3 in hi and 4 to 7 in lo.
 struct Full {
   f32x4 hi, lo;
 };
-template <typename TIN>
-using Operand = std::conditional_t<sizeof(TIN) == 4, Full, Split>;
+// Eight terms of an fp32 factor of bf16 keys, queries or output gradients, which are exact in bf16: three
+// bf16 numbers each, every one the nearest to what those before it leave.  That is all 24 bits, so the
+// products are exact.  Three bf16 MFMAs of 32 terms take 48 cycles, eight fp32 ones 256.  (Two numbers are
+// off by up to 2^-17: states then came out 5e-6 from 64 bits instead of 1e-7.)
+struct Three {
+  bf16x8 a, b, c;
+};
+// The first two of them, good to 2^-17: for outputs in bf16, which are good to 2^-8.  Of a product of two
+// such operands b b is left out, 2^-16 at the most.
+struct Pair {
+  bf16x8 a, b;
+};
 
-// 24 VALU instructions: two conversions a pair, hi widened again, the difference.
-__device__ __forceinline__ Split split8(const float* x) {
+__device__ __forceinline__ Full full8(const float* x) {
+  return Full{{x[0], x[1], x[2], x[3]}, {x[4], x[5], x[6], x[7]}};
+}
+// 44 VALU instructions: three conversions a pair, two of them widened again, the differences.
+__device__ __forceinline__ Three three8(const float* x) {
   typedef __attribute__((ext_vector_type(2))) float f32x2;
   typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-  u32x4 hi, lo;
+  u32x4 a, b, c;
+  auto narrowed = [](f32x2 v) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2)); };
+  auto left = [](f32x2 v, uint32_t n) {
+    return f32x2{v[0] - __uint_as_float(n << 16), v[1] - __uint_as_float(n & 0xffff0000u)};
+  };
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const f32x2 v = {x[2 * e], x[2 * e + 1]};
-    const uint32_t h = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-    const f32x2 d = {x[2 * e] - __uint_as_float(h << 16),
-                     x[2 * e + 1] - __uint_as_float(h & 0xffff0000u)};
-    hi[e] = h;
-    lo[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(d, bf16x2));
+    f32x2 v = {x[2 * e], x[2 * e + 1]};
+    a[e] = narrowed(v);
+    v = left(v, a[e]);
+    b[e] = narrowed(v);
+    c[e] = narrowed(left(v, b[e]));
   }
-  return Split{__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, lo)};
+  return Three{__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, c)};
 }
 template <typename OP>
 __device__ __forceinline__ OP operand8(const float* x) {
-  if constexpr (std::is_same_v<OP, Split>) return split8(x);
-  else return Full{{x[0], x[1], x[2], x[3]}, {x[4], x[5], x[6], x[7]}};
+  if constexpr (std::is_same_v<OP, Full>) {
+    return full8(x);
+  } else {
+    const Three t = three8(x);
+    if constexpr (std::is_same_v<OP, Pair>) return Pair{t.a, t.b};
+    else return t;
+  }
 }
 
 // acc += a b over 32 terms.  Lane l holds of the 16x16 result rows 4(l/16)+r, column l%16;
@@ -82,28 +94,47 @@ __device__ __forceinline__ OP operand8(const float* x) {
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 acc) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
 }
-__device__ __forceinline__ f32x4 mma3(const Split& a, const Split& b, f32x4 acc) {
-  acc = mma(a.lo, b.hi, acc);
-  acc = mma(a.hi, b.lo, acc);
-  return mma(a.hi, b.hi, acc);
+// Four terms, one of each lane of a row or column.
+__device__ __forceinline__ f32x4 mma(float a, float b, f32x4 acc) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, acc, 0, 0, 0);
 }
-// Four terms an instruction, one of each lane of a row or column.
-__device__ __forceinline__ f32x4 mma3(const Full& a, const Full& b, f32x4 acc) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.hi[e], b.hi[e], acc, 0, 0, 0);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a.lo[e], b.lo[e], acc, 0, 0, 0);
-  return acc;
+// acc + low += a b: two sums, so that fewer instructions wait for the one before.
+__device__ __forceinline__ void mma(bf16x8 a, const Three& b, f32x4& acc, f32x4& low) {
+  low = mma(a, b.c, low);
+  acc = mma(a, b.a, acc);
+  low = mma(a, b.b, low);
 }
-// acc += a b with an operand a that has a second half (LO) or is exact in bf16.
-template <bool LO, typename OP>
-__device__ __forceinline__ f32x4 mma_plane(const OP& a, const OP& b, f32x4 acc) {
-  if constexpr (LO) {
-    return mma3(a, b, acc);
-  } else {
-    acc = mma(a.hi, b.lo, acc);
-    return mma(a.hi, b.hi, acc);
+__device__ __forceinline__ void mma(const Full& a, const Full& b, f32x4& acc, f32x4& low) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    acc = mma(a.hi[e], b.hi[e], acc);
+    low = mma(a.lo[e], b.lo[e], low);
   }
+}
+// For outputs: without b's last part where they are bf16.
+__device__ __forceinline__ void mma_out(bf16x8 a, const Three& b, f32x4& acc, f32x4& low) {
+  acc = mma(a, b.a, acc);
+  low = mma(a, b.b, low);
+}
+__device__ __forceinline__ void mma_out(const Pair& a, const Pair& b, f32x4& acc, f32x4& low) {
+  low = mma(a.b, b.a, low);
+  acc = mma(a.a, b.a, acc);
+  low = mma(a.a, b.b, low);
+}
+__device__ __forceinline__ void mma_out(const Full& a, const Full& b, f32x4& acc, f32x4& low) {
+  mma(a, b, acc, low);
+}
+__device__ __forceinline__ f32x4 mma(bf16x8 a, const Three& b, f32x4 acc) {
+  acc = mma(a, b.c, acc);
+  acc = mma(a, b.b, acc);
+  return mma(a, b.a, acc);
+}
+__device__ __forceinline__ f32x4 mma(const Full& a, const Full& b, f32x4 acc) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc = mma(a.hi[e], b.hi[e], acc);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) acc = mma(a.lo[e], b.lo[e], acc);
+  return acc;
 }
 __host__ __device__ constexpr int state_key(int f, int g, int r) {
   return 32 * (f >> 1) + 8 * g + 4 * (f & 1) + r;
@@ -138,10 +169,10 @@ __device__ __forceinline__ void store_state(void* S, bool bf16, int64_t i, float
 }
 
 // ------------------------------------------------------------------ operands in LDS
-// A token x key plane: 32 rows of 16-byte pieces (8 bf16; of Full planes four fp32, the other four in
-// the second half), piece x of row r at piece_at(r, x).  The exchange of pieces within a row lets 16
-// rows of one piece (an operand over keys) and four pieces of four rows (one over tokens) each lie in
-// different banks.  NP: pieces in a row.
+// A token x key plane: 32 rows of 16-byte pieces (8 bf16; or four fp32, of eight keys the others in the
+// same piece of the second half), piece x of row r at piece_at(r, x).  The exchange of pieces within a
+// row lets 16 rows of one piece (an operand over keys) and four pieces of four rows (one over tokens)
+// each lie in different banks.  NP: pieces in a row.
 template <int NP>
 __host__ __device__ constexpr int piece_swap(int r) {
   return NP >= 16  ? ((r & 3) << 2) | ((r >> 2) & 3)
@@ -167,39 +198,40 @@ __device__ __forceinline__ bf16x4 read_column(const unsigned char* lds) {
   return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)lds));
 }
 
-// Tokens 16 tt + l%16, terms: keys 32 s + 8 (l/16) + e.  half: bytes to the second half, or 0: none.
+// Operands from a plane, exact in bf16 (bf16x8), Full or Pair, its second half `half` bytes on.
+// Tokens 16 tt + l%16, terms: keys 32 s + 8 (l/16) + e.
 template <typename OP, int NP>
 __device__ __forceinline__ OP rows_operand(const unsigned char* plane, int half, int tt, int s, int lane) {
   const unsigned char* at = plane + 16 * piece_at<NP>(16 * tt + (lane & 15), 4 * s + (lane >> 4));
-  OP o;
-  o.hi = *reinterpret_cast<const decltype(o.hi)*>(at);
-  if (half) o.lo = *reinterpret_cast<const decltype(o.lo)*>(at + half);
-  return o;
+  if constexpr (std::is_same_v<OP, bf16x8>)
+    return *reinterpret_cast<const bf16x8*>(at);
+  else if constexpr (std::is_same_v<OP, Pair>)
+    return Pair{*reinterpret_cast<const bf16x8*>(at), *reinterpret_cast<const bf16x8*>(at + half)};
+  else
+    return Full{*reinterpret_cast<const f32x4*>(at), *reinterpret_cast<const f32x4*>(at + half)};
 }
 // Keys state_key(f, ., .) in the place of l%16, terms: the chunk's tokens (state order).
 template <typename OP, int NP>
 __device__ __forceinline__ OP cols_operand(const unsigned char* plane, int half, int f, int lane) {
-  const int i = lane & 15;
-  OP o;
-  if constexpr (std::is_same_v<OP, Split>) {
-    const int r = 4 * (lane >> 4) + (i >> 2), x = 4 * (f >> 1) + (i & 3);
-    const int a = 8 * (f & 1) + 16 * piece_at<NP>(r, x), b = 8 * (f & 1) + 16 * piece_at<NP>(r + 16, x);
-    o.hi = join(read_column(plane + a), read_column(plane + b));
-    if (half) o.lo = join(read_column(plane + half + a), read_column(plane + half + b));
+  const int i = lane & 15, g = lane >> 4;
+  if constexpr (std::is_same_v<OP, bf16x8>) {
+    const int r = 4 * g + (i >> 2), x = 4 * (f >> 1) + (i & 3);
+    const unsigned char* at = plane + 8 * (f & 1);
+    return join(read_column(at + 16 * piece_at<NP>(r, x)), read_column(at + 16 * piece_at<NP>(r + 16, x)));
   } else {
     // Key i is in piece i / 4 of these 32 keys' eight, half f & 1.  Rows 4 g + e and 16 + 4 g + e; their
     // exchange of pieces is g's with e's, so one address serves all e.
     static_assert(NP >= 8 && piece_swap<NP>(4 + 1) == (piece_swap<NP>(4) ^ piece_swap<NP>(1)), "see above");
-    const int g = lane >> 4;
     const unsigned char* at = plane + half * (f & 1) + 16 * (4 * g * NP + ((i >> 2) ^ g)) + 4 * (i & 3);
+    Full o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int to = 16 * (e * NP + ((4 * (f >> 1)) ^ piece_swap<NP>(e)));
       o.hi[e] = *reinterpret_cast<const float*>(at + to);
       o.lo[e] = *reinterpret_cast<const float*>(at + to + 256 * NP);
     }
+    return o;
   }
-  return o;
 }
 
 // ------------------------------------------------------------------ workspace

@@ -13,14 +13,29 @@
 
 namespace dl {
 
-// A square's operand.
-template <typename OP>
-__device__ __forceinline__ OP square_at(const unsigned char* lds, int tt, int lane) {
-  const unsigned char* at = lds + 16 * (tt * 64 + lane);
-  OP s;
-  s.hi = *reinterpret_cast<const decltype(s.hi)*>(at);
-  s.lo = *reinterpret_cast<const decltype(s.lo)*>(at + WsLayout::SQ);
-  return s;
+// A triangular square's three 16 x 16 blocks that are not zero, (0, 0), (1, 0) and (1, 1) of a LOWER
+// one, (0, 0), (0, 1) and (1, 1) of an upper one, as operands over the tokens of their columns.
+struct Square {
+  f32x4 m[3];
+};
+template <bool LOWER>
+__device__ __forceinline__ Square square_at(const unsigned char* lds, int lane) {
+  auto block = [&](int i, int j) {
+    return *reinterpret_cast<const f32x4*>(lds + 16 * (64 * i + lane) + j * WsLayout::SQ);
+  };
+  return Square{{block(0, 0), LOWER ? block(1, 0) : block(0, 1), block(1, 1)}};
+}
+// r += m b over the chunk's tokens.
+template <bool LOWER>
+__device__ __forceinline__ void square_mma(const Square& m, const Full& b, f32x4& r0, f32x4& r1) {
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    r0 = mma(m.m[0][e], b.hi[e], r0);
+    x = mma(m.m[1][e], LOWER ? b.hi[e] : b.lo[e], x);
+    r1 = mma(m.m[2][e], b.lo[e], r1);
+  }
+  (LOWER ? r1 : r0) += x;
 }
 
 // Result tiles [2][NT] (tokens 16 tt + 4 g + r) as operands over the chunk's tokens.
@@ -44,16 +59,20 @@ enum PassId { PASS_OUT = 0, PASS_SAVE = 1, PASS_BACK = 2, PASS_SEG = 3 };
 // One chunk's operands on their way from memory to LDS.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, int PASS, typename TIN>
 struct Stage {
-  using Op = Operand<TIN>;
+  using Op = std::conditional_t<RAW, bf16x8, Full>;    // an operand from a plane,
+  using By = std::conditional_t<RAW, Three, Full>;     // and what it is multiplied with;
+  // the same for outputs
+  using OutOp = std::conditional_t<RAW, bf16x8, std::conditional_t<sizeof(TIN) == 2, Pair, Full>>;
+  using OutBy = std::conditional_t<RAW, Three, std::conditional_t<sizeof(TIN) == 2, Pair, Full>>;
   static constexpr int T = 64 * NW, VC = 16 * NT * NW, NP = DK / 8;
   static constexpr int HALF = CT * DK * 2;                     // bytes of half a plane
   static constexpr int PL = RAW ? 0 : HALF, SQ = WsLayout::SQ, SQ2 = 2 * SQ;
   static constexpr int FAC = 4 * DK + 12 * CT;
   static constexpr bool BACK = PASS == PASS_BACK, OUT = PASS == PASS_OUT;
   static constexpr bool WITH_Q = BACK || OUT;
-  // Plane operands are read ahead of the products before theirs; with fp32 inputs, whose products take
+  // Raw planes' operands are read ahead of the products before theirs; fp32 ones, whose products take
   // five times as long, one by one: registers would not do for all.
-  static constexpr bool AHEAD = sizeof(TIN) == 2;
+  static constexpr bool AHEAD = RAW;
   // LDS offsets, of the workspace block: first P, N, Kh (what of them the pass needs), then Qh,
   // Kb, the factors, and backward P^T, M^T.
   static constexpr int A_P = 0;
@@ -206,9 +225,10 @@ struct Stage {
     return *reinterpret_cast<const f32x4*>(lds + at + 4 * (16 * tt + 4 * (lane >> 4)));
   }
   // Operands from the planes; raw ones have no second half.
-  static __device__ __forceinline__ Op rows(const unsigned char* lds, int raw_at, int at, int tt, int s,
+  template <typename OP = Op>
+  static __device__ __forceinline__ OP rows(const unsigned char* lds, int raw_at, int at, int tt, int s,
                                             int lane) {
-    return rows_operand<Op, NP>(lds + (RAW ? raw_at : at), RAW ? 0 : HALF, tt, s, lane);
+    return rows_operand<OP, NP>(lds + (RAW ? raw_at : at), RAW ? 0 : HALF, tt, s, lane);
   }
   static __device__ __forceinline__ Op cols(const unsigned char* lds, int raw_at, int at, int f, int lane) {
     return cols_operand<Op, NP>(lds + (RAW ? raw_at : at), RAW ? 0 : HALF, f, lane);
@@ -349,6 +369,7 @@ __device__ __forceinline__ void walk_forward(
     unsigned char (&lds)[2][Stage<DK, NT, NW, RAW, DELTA, PASS, TIN>::BYTES]) {
   using St = Stage<DK, NT, NW, RAW, DELTA, PASS, TIN>;
   using Op = typename St::Op;
+  using By = typename St::By;
   constexpr int NKT = DK / 16, NKS = DK / 32;
   constexpr bool OUT = PASS == PASS_OUT;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -373,7 +394,8 @@ __device__ __forceinline__ void walk_forward(
   };
 
   f32x4 U[2][NT], S[NKT][NT], ff[2];
-  Op ak[2][NKS], an[2];
+  Op ak[2][NKS];
+  Square an;
   auto ahead = [&](const unsigned char* l) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
@@ -387,9 +409,9 @@ __device__ __forceinline__ void walk_forward(
 #pragma unroll
         for (int s = 0; s < NKS; ++s)
           if constexpr (St::AHEAD) ak[tt][s] = St::rows(l, St::A_K, St::A_KH, tt, s, lane);
-        an[tt] = square_at<Op>(l + St::A_N, tt, lane);
       }
     }
+    if constexpr (DELTA) an = square_at<true>(l + St::A_N, lane);
   };
   auto chunk = [&](int c, unsigned char* cur, unsigned char* nxt) __attribute__((always_inline)) {
     __syncthreads();
@@ -398,19 +420,29 @@ __device__ __forceinline__ void walk_forward(
     if constexpr (PASS == PASS_SAVE) save_tiles<true>(S, block(c) + w.s0(), k.v0 / 16 + ct0, lane);
 
     // Kh S, R = V - Kh S, E = N R (but for PASS_SAVE N holds beta N, and U comes at once)
-    Op sb[NKS][NT];
-    f32x4 X[2][NT];
+    using OutBy = typename St::OutBy;
+    By sb[NKS][NT];
+    OutBy so[NKS][NT];
+    f32x4 X[2][NT], XL[2][NT];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) X[tt][t] = XL[tt][t] = zero;
 #pragma unroll
     for (int s = 0; s < NKS; ++s)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        if constexpr (DELTA || OUT) sb[s][t] = state_operand<Op, NKT, NT>(S, s, t);
         if constexpr (DELTA) {
+          sb[s][t] = state_operand<By, NKT, NT>(S, s, t);
 #pragma unroll
           for (int tt = 0; tt < 2; ++tt) {
             if constexpr (!St::AHEAD) ak[tt][s] = St::rows(cur, St::A_K, St::A_KH, tt, s, lane);
-            X[tt][t] = mma_plane<!RAW>(ak[tt][s], sb[s][t], s ? X[tt][t] : zero);
+            mma(ak[tt][s], sb[s][t], X[tt][t], XL[tt][t]);
           }
+        }
+        if constexpr (OUT) {
+          if constexpr (DELTA && std::is_same_v<By, OutBy>) so[s][t] = sb[s][t];
+          else so[s][t] = state_operand<OutBy, NKT, NT>(S, s, t);
         }
       }
     Op ac[NKT];
@@ -424,17 +456,18 @@ __device__ __forceinline__ void walk_forward(
       if constexpr (DELTA && PASS == PASS_SAVE) be[tt] = St::factor(cur, St::A_BETA, tt, lane);
     }
     if constexpr (DELTA) {
-      Op rb[NT];
+      Full rb[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int tt = 0; tt < 2; ++tt) U[tt][t] -= RAW ? X[tt][t] * ff[tt] : X[tt][t];
-        rb[t] = tokens_operand<Op, NT>(U, t);
+        for (int tt = 0; tt < 2; ++tt) {
+          X[tt][t] += XL[tt][t];
+          U[tt][t] -= RAW ? X[tt][t] * ff[tt] : X[tt][t];
+        }
+        rb[t] = tokens_operand<Full, NT>(U, t);
+        U[0][t] = U[1][t] = zero;
+        square_mma<true>(an, rb[t], U[0][t], U[1][t]);
       }
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) U[tt][t] = mma3(an[tt], rb[t], zero);
     }
     if constexpr (PASS == PASS_SAVE) {
       save_tiles<false>(U, block(c) + w.e(), k.v0 / 16 + ct0, lane);
@@ -445,14 +478,15 @@ __device__ __forceinline__ void walk_forward(
           for (int t = 0; t < NT; ++t) U[tt][t] *= be[tt];
       }
     }
-    Op ub[NT], gb[NT];
+    Full ub[NT];
+    By gb[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      if constexpr (OUT || !RAW) ub[t] = tokens_operand<Op, NT>(U, t);
+      if constexpr (OUT || !RAW) ub[t] = tokens_operand<Full, NT>(U, t);
       if constexpr (RAW) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) U[tt][t] *= gf[tt];
-        gb[t] = tokens_operand<Op, NT>(U, t);
+        gb[t] = tokens_operand<By, NT>(U, t);
       } else {
         gb[t] = ub[t];
       }
@@ -463,36 +497,36 @@ __device__ __forceinline__ void walk_forward(
       const f32x4 d = St::decay(cur, f, lane);
       if constexpr (!St::AHEAD) ac[f] = St::cols(cur, St::A_K, St::A_KB, f, lane);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) S[f][t] = mma_plane<!RAW>(ac[f], gb[t], S[f][t] * d);
+      for (int t = 0; t < NT; ++t) S[f][t] = mma(ac[f], gb[t], S[f][t] * d);
     }
     __syncthreads();
     if constexpr (OUT) {
-      f32x4 O[2][NT], fo[2];
-      Op ap[2];
+      f32x4 O[2][NT], OL[2][NT], fo[2];
+      const Square ap = square_at<true>(cur + St::A_P, lane);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         fo[tt] = ff[tt];
-        ap[tt] = square_at<Op>(cur + St::A_P, tt, lane);
 #pragma unroll
-        for (int s = 0; s < NKS; ++s) {
-          const Op aq = St::rows(cur, St::A_Q, St::A_QH, tt, s, lane);
-#pragma unroll
-          for (int t = 0; t < NT; ++t) O[tt][t] = mma_plane<!RAW>(aq, sb[s][t], s ? O[tt][t] : zero);
-        }
+        for (int t = 0; t < NT; ++t) O[tt][t] = OL[tt][t] = zero;
       }
+#pragma unroll
+      for (int s = 0; s < NKS; ++s)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+          const auto aq = St::template rows<typename St::OutOp>(cur, St::A_Q, St::A_QH, tt, s, lane);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) mma_out(aq, so[s][t], O[tt][t], OL[tt][t]);
+        }
       ahead(nxt);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
+      for (int t = 0; t < NT; ++t) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int tt = 0; tt < 2; ++tt) {
+          O[tt][t] += OL[tt][t];
           if constexpr (RAW) O[tt][t] *= fo[tt];
-          if constexpr (!DELTA && sizeof(TIN) == 2) {          // U is V: no second half
-            O[tt][t] = mma(ap[tt].lo, ub[t].hi, O[tt][t]);
-            O[tt][t] = mma(ap[tt].hi, ub[t].hi, O[tt][t]);
-          } else {
-            O[tt][t] = mma3(ap[tt], ub[t], O[tt][t]);
-          }
         }
+        square_mma<true>(ap, ub[t], O[0][t], O[1][t]);
+      }
       St::results(cur, O, ct0,
                   static_cast<TIN*>(p.o) + int64_t(k.row(c)) * row_stride + int64_t(k.h) * p.dv +
                       k.v0 + 16 * ct0,
@@ -553,6 +587,7 @@ __device__ __forceinline__ void walk_backward(
     unsigned char (&lds)[2][Stage<DK, NT, NW, RAW, DELTA, PASS_BACK, TIN>::BYTES]) {
   using St = Stage<DK, NT, NW, RAW, DELTA, PASS_BACK, TIN>;
   using Op = typename St::Op;
+  using By = typename St::By;
   constexpr int NKT = DK / 16, NKS = DK / 32;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, c16 = lane & 15;
@@ -589,46 +624,55 @@ __device__ __forceinline__ void walk_backward(
     save_tiles<true>(D, block(c) + w.ds(), k.v0 / 16 + ct0, lane);
 
     f32x4 Y[2][NT], gf[2], ff[2], be[2];
-    Op ac[NKT], amt[2], apt[2];
+    Op ac[NKT];
+    const Square apt = square_at<false>(cur + St::A_PT, lane);
+    Square amt;
+    if constexpr (DELTA) amt = square_at<false>(cur + St::A_MT, lane);
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      apt[tt] = square_at<Op>(cur + St::A_PT, tt, lane);
       if constexpr (RAW) {
         gf[tt] = St::factor(cur, St::A_G, tt, lane);
         ff[tt] = St::factor(cur, St::A_F, tt, lane);
       }
       if constexpr (DELTA) {
         be[tt] = St::factor(cur, St::A_BETA, tt, lane);
-        amt[tt] = square_at<Op>(cur + St::A_MT, tt, lane);
       }
     }
     // dU
+    f32x4 YL[2][NT];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) Y[tt][t] = YL[tt][t] = zero;
 #pragma unroll
     for (int s = 0; s < NKS; ++s)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const Op sb = state_operand<Op, NKT, NT>(D, s, t);
+        const By sb = state_operand<By, NKT, NT>(D, s, t);
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
           if constexpr (!St::AHEAD) ar[tt][s] = St::rows(cur, St::A_K, St::A_KB, tt, s, lane);
-          Y[tt][t] = mma_plane<!RAW>(ar[tt][s], sb, s ? Y[tt][t] : zero);
+          mma(ar[tt][s], sb, Y[tt][t], YL[tt][t]);
         }
       }
 #pragma unroll
     for (int f = 0; f < NKT; ++f)
       if constexpr (St::AHEAD) ac[f] = St::cols(cur, St::A_Q, St::A_QH, f, lane);
-    Op gb[NT];
+    By gb[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      gb[t] = tokens_operand<Op, NT>(G, t);
+      const Full o = tokens_operand<Full, NT>(G, t);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
-        Y[tt][t] = mma3(apt[tt], gb[t], RAW ? Y[tt][t] * gf[tt] : Y[tt][t]);
+      for (int tt = 0; tt < 2; ++tt) {
+        Y[tt][t] += YL[tt][t];
+        if constexpr (RAW) Y[tt][t] *= gf[tt];
+      }
+      square_mma<false>(apt, o, Y[0][t], Y[1][t]);
       if constexpr (RAW) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) G[tt][t] *= ff[tt];
-        gb[t] = tokens_operand<Op, NT>(G, t);
       }
+      gb[t] = tokens_operand<By, NT>(G, t);
     }
     // the outputs' share of D needs nothing of Y
 #pragma unroll
@@ -636,16 +680,15 @@ __device__ __forceinline__ void walk_backward(
       const f32x4 d = St::decay(cur, f, lane);
       if constexpr (!St::AHEAD) ac[f] = St::cols(cur, St::A_Q, St::A_QH, f, lane);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) D[f][t] = mma_plane<!RAW>(ac[f], gb[t], D[f][t] * d);
+      for (int t = 0; t < NT; ++t) D[f][t] = mma(ac[f], gb[t], D[f][t] * d);
     }
     if constexpr (DELTA) {
-      Op rb[NT];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) rb[t] = tokens_operand<Op, NT>(Y, t);
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) Y[tt][t] = mma3(amt[tt], rb[t], zero);
+      for (int t = 0; t < NT; ++t) {
+        const Full rb = tokens_operand<Full, NT>(Y, t);
+        Y[0][t] = Y[1][t] = zero;
+        square_mma<false>(amt, rb, Y[0][t], Y[1][t]);
+      }
     }
     save_tiles<false>(Y, block(c) + w.z(), k.v0 / 16 + ct0, lane);
     if constexpr (DELTA) {
@@ -657,10 +700,10 @@ __device__ __forceinline__ void walk_backward(
           Y[tt][t] *= be[tt];
           m[tt][0] = RAW ? -Y[tt][t] * ff[tt] : -Y[tt][t];
         }
-        const Op yb = tokens_operand<Op, 1>(m, 0);
+        const By yb = tokens_operand<By, 1>(m, 0);
 #pragma unroll
         for (int f = 0; f < NKT; ++f)
-          D[f][t] = mma_plane<!RAW>(St::cols(cur, St::A_K, St::A_KH, f, lane), yb, D[f][t]);
+          D[f][t] = mma(St::cols(cur, St::A_K, St::A_KH, f, lane), yb, D[f][t]);
       }
     }
     __syncthreads();
@@ -724,9 +767,8 @@ __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
 // segment writes it while the first one may not have started.  Without the delta rule M_j is the
 // decay over the segment.  A step is a chain of one load, one product and one exchange of S through
 // LDS; M_j and L_j do not depend on S and are fetched a step ahead.
-template <int DK, bool RAW, bool DELTA, typename TIN>
+template <int DK, bool RAW, bool DELTA>
 __global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
-  using Op = Operand<TIN>;
   constexpr int NKS = DK / 32, PITCH = 18;     // 8 rows further: 16 banks further
   __shared__ float sh[2][DK * PITCH];
   const int lane = threadIdx.x & 63, f = threadIdx.x >> 6, c16 = lane & 15, g = lane >> 4;
@@ -769,13 +811,13 @@ __global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[(state_key(f, g, 0) + r) * PITCH + c16] = S[r];
       place(j, S);
-      Op am[NKS];
+      Full am[NKS];
 #pragma unroll
       for (int s = 0; s < NKS; ++s) {
         float a[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] = m[2 * s + (e >> 2)][e & 3];
-        am[s] = operand8<Op>(a);
+        am[s] = full8(a);
       }
       S = L;
       const int next = min(j + 1, parts - 2);  // the last one's M is never made
@@ -787,7 +829,7 @@ __global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
         float a[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] = x[(32 * s + 8 * g + e) * PITCH + c16];
-        S = mma3(am[s], operand8<Op>(a), S);
+        S = mma(am[s], full8(a), S);
       }
     }
   } else {

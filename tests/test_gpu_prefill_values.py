@@ -63,6 +63,28 @@ def test_fp32_inputs_keep_fp32(op, dk, dv):
 
 
 @pytest.mark.parametrize("op", R.OPS)
+@pytest.mark.parametrize("dk,dv", SHAPES)
+def test_bf16_inputs_have_fp32_states_and_gate_gradients(op, dk, dv):
+    """What is fp32 of a call with bf16 inputs is as good as with fp32 ones."""
+    for lens, H, backward in (([150, 0, 33], 3, True), ([1650, 40], 2, False), ([33, 40], 130, True)):
+        x = R.inputs(op, lens, H, dk, dv, BF16, F32, seed=6)
+        want = R.expected(op, x, grads=backward)
+        c = P.Call(op, x, backward=backward)
+        c.build()
+        c.forward()
+        slots = x["slots"]
+        errors = {"S": R.rel(c.S_out[slots], want["S"][slots])}
+        if backward:
+            c.backward()
+            errors["dS"] = R.rel(c.grads.dS[slots], want["grads"]["dS"][slots])
+            for name in ("dlam", "dbeta", "du"):
+                if name in want["grads"]:
+                    got = getattr(c.grads, name)
+                    errors[name] = R.rel(got, want["grads"][name])
+        assert max(errors.values()) <= FULL, errors
+
+
+@pytest.mark.parametrize("op", R.OPS)
 def test_fp32_inputs_keep_fp32_over_segments(op):
     x = R.inputs(op, [1700, 40], 2, 128, 64, F32, F32, seed=5)
     want = R.expected(op, x)
