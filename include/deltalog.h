@@ -266,13 +266,11 @@ int dl_prefill_workspace_bytes(const dl_desc* desc, int32_t n, int32_t tokens,
  * every sequence of the tables, from S_in[slot] (S_in == NULL: zero) to S_out[slot] (both
  * [B,H,dk,dv] of state_dtype; S_out may be S_in), with o [N,H,dv] in in_dtype -- a prompt's
  * outputs go on to products in that type, and a state read back in it would not gain from
- * wider ones.  tok holds N rows.  Sums, decays and states are fp32, and o and S_out are rounded
- * once.  With fp32 inputs products are fp32 too: results are within some 4e-7 of the exact ones,
- * relative to their norm.  With bf16 inputs products of fp32 factors take each as a sum of two
- * bf16 numbers, good to 2^-17 where the inputs' own rounding was 2^-9: fp32 results are within
- * some 1e-5.  Log-decays are summed in fp32 from a chunk's start, so what two tokens behind a gate
- * of 0 (a sum of -104 or less) in the same chunk share is good to some 1e-5 as well.  Outputs must
- * not overlap inputs, S_out = S_in apart.
+ * wider ones.  tok holds N rows.  Products, sums, decays and states are fp32 (fp32 results are
+ * within some 4e-7 of the exact ones, relative to their norm), and o and S_out are rounded once;
+ * only factors that go into a bf16 o alone are good to 2^-17.  Log-decays are summed in fp32 from a
+ * chunk's start, so the decay between two tokens behind a gate of 0 (which counts as -104) in the
+ * same chunk is good to some 1e-5.  Outputs must not overlap inputs, S_out = S_in apart.
  * The log of a DeltaLog state is not looked at: flush it first (dl_merge without a token)
  * where S_in is the base of a state with a log, and reset len where S_out is.
  * tables: as dl_chunk_tables left them for the same n and N (row_slot is not read).

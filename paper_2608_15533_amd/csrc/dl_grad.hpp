@@ -15,12 +15,13 @@
 //
 // Each wave owns 16 keys and all tokens, as MFMA results: a lane has one key and the eight tokens
 // 16 tt + 4 g + r, which are also the terms (state order) that it feeds a product over tokens, so
-// keys, queries and decay factors are fetched once for both uses.  dO, E and Z are split once by
-// the workgroup into planes in LDS, from which every wave reads its operands; S and D, which
-// no two waves share, go from memory to registers.
+// keys, queries and decay factors are fetched once for both uses.  dO, E and Z go once through
+// planes in LDS, from which every wave reads its operands; S and D, which no two waves share, go
+// from memory to registers.
 //
-// Bound by the saved states: 2 x 2048 tokens, 32 heads of 128 x 128 (GDN, bf16) 176 us for 780 MB
-// read and 76 MB written, 4.9 TB/s; waves wait for them half of their time.
+// Bound by the saved states and, half of the time, by the fp32 products with them: 2 x 2048 tokens,
+// 32 heads of 128 x 128 (GDN, bf16) 219 us for 780 MB read and 76 MB written, 3.9 TB/s, the matrix
+// cores busy in 41% of the cycles.
 #pragma once
 
 #include "dl_prep.hpp"
@@ -45,8 +46,7 @@ __device__ __forceinline__ void lane_tokens(const float (*m)[LD], int f, int lan
 // acc += m b (TR: m^T b) for the result tile of tokens 16 tt.., m lower triangular token x token,
 // b a lane's eight tokens of its key.  On fp32 MFMA: what a pair gives to q_i dq_i it takes from
 // k_j dk''_j, and dlam's suffix sums keep the difference, so both must see the same product (with
-// operands in two bf16 halves dlam of RWKV6 came out 3e-5 off instead of 1e-6).  Four terms an
-// instruction and no splitting: 32 x 24 vector instructions less, 32 slower MFMAs more.
+// operands in two bf16 halves dlam of RWKV6 came out 3e-5 off instead of 1e-6).
 template <bool TR>
 __device__ __forceinline__ f32x4 pair_mma(const float (*m)[SL], int tt, const float* b, f32x4 acc,
                                           int lane) {

@@ -148,7 +148,7 @@ struct ChunkIn {
 
 // G (strictly lower) and P (lower; RWKV6: strictly, and its bonus on the diagonal), by three
 // of the workgroup's waves; by all of them, pair by pair, where a block decays too far.  On
-// fp32 MFMA: the operands are used once, so splitting them (24 instructions for eight values)
+// fp32 MFMA: the operands are used once, so splitting them (44 instructions for eight values)
 // would cost more than the matrix cores' slower fp32 rate, which nothing else here waits for.
 template <int DC, int DK, bool DELTA, typename TIN>
 __device__ void pair_products(const ChunkIn<DC, DK, TIN>& in, float (*G)[SL], float (*P)[SL],
@@ -349,8 +349,8 @@ __device__ __forceinline__ void put_squares(unsigned char* blk, const WsLayout& 
 }
 
 // BWD: for the backward pass.
-// Bound by memory: 12345 tokens, 32 heads of 128 keys (KDA, bf16) 188 us for 417 MB read and
-// 724 MB written (the planes), 6.1 TB/s, where a large copy reaches 5.55.
+// Bound by memory: 12345 tokens, 32 heads of 128 keys (KDA, bf16) 184 us for 417 MB read and
+// 724 MB written (the planes), 6.2 TB/s, where a large copy reaches 5.55.
 template <int DC, int DK, bool DELTA, bool BWD, typename TIN>
 __global__ __launch_bounds__(256) void prep_kernel(SeqParams p) {
   __shared__ ChunkIn<DC, DK, TIN> in;

@@ -313,11 +313,11 @@ inline int walk_waves(int64_t heads, int dk, int dv, bool raw) {
 // as many parallel parts as there is room for, and worth it up to 320 waves (then there are three
 // parts at least) and from 48 chunks a sequence on average.  Workgroups of four waves.
 // Measured, one bf16 sequence, whole call with its tables, whole -> in segments, us: GDN 128 x 128, 8
-// heads of 8192 tokens 375 -> 114, 32 of 3200 165 -> 121, 32 of 1536 89 -> 77, 64 of 2048 (512 waves)
-// 120 -> 127; KDA, the same, 591 -> 180, 278 -> 221, 144 -> 120, 228 -> 227; RWKV6 64 x 64, 40 heads of
-// 4096 174 -> 106; fp32 GDN 1235 -> 269, 542 -> 361, 263 -> 180.  32 GDN heads of 8192: whole 400; in
-// four segments 268, of which 118 for L and M, 14 for the states, 116 for the outputs; in three 282, in
-// five 271.
+// heads of 8192 tokens 556 -> 143, 32 of 3200 237 -> 157, 32 of 1536 123 -> 95, 64 of 2048 (512 waves)
+// 165 -> 163; KDA, the same, 1055 -> 252, 462 -> 338, 232 -> 169, 347 -> 330; RWKV6 64 x 64, 40 heads of
+// 4096 239 -> 131; fp32 GDN 1231 -> 269, 542 -> 363, 263 -> 179.  32 GDN heads of 8192: whole 582; in
+// four segments 360, of which 171 for L and M, 14 for the states, 163 for the outputs; in three 379, in
+// five 360.
 struct SegPlan {
   int len, segs;          // chunks of a segment (0: none), room for segments
 };

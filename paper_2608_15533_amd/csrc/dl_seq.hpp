@@ -341,7 +341,7 @@ __device__ __forceinline__ void write_state(const f32x4 (&S)[NKT][NT], void* bas
 // Results into the workspace, [column tile][row][16]; rows: KEYS (of a state), or tokens.  They are
 // read once, by a later kernel, and there are more of them than caches hold: stored past the
 // caches, what follows finds its operands there (a GDN training step of 2 x 2048 tokens, 32 heads
-// of 128 x 128: 613 -> 577 us, of which the gradients 199 -> 176).
+// of 128 x 128: 613 -> 577 us, of which the gradients 199 -> 176, when its products were shorter).
 template <bool KEYS, int NR, int NT>
 __device__ __forceinline__ void save_tiles(const f32x4 (&x)[NR][NT], unsigned char* base, int tile,
                                            int lane) {
@@ -749,10 +749,11 @@ __device__ __forceinline__ int xcd_place(int b, int groups, int share) {
   return b - in + in % ROUND * share + in / ROUND;
 }
 
-// One wave to a SIMD (64 heads of 2048 tokens, 128 x 128, GDN, bf16): 107 us, 1.7 a chunk; the wave
-// issues in 61% of its cycles (vector instructions 36%, matrix cores busy 26%) and waits for its
-// own results in the rest: it is one chain.  Two (256 heads of 4096): 359 us, vector 55% and matrix 35%
-// of a SIMD's cycles, 1.4 GB moved, 3.9 TB/s.
+// One wave to a SIMD (64 heads of 2048 tokens, 128 x 128, GDN, bf16): 152 us, 2.4 a chunk; the wave
+// issues in 50% of its cycles (vector instructions 33%), the matrix cores are busy in 34%, and it waits
+// for its own results in the rest: it is one chain.  Two (256 heads of 4096): 487 us, vector 50% and
+// matrix 48% of a SIMD's cycles, 1.4 GB moved, 2.9 TB/s.  With planes (KDA, 384 ragged heads, 12345
+// tokens) 410 us, matrix 66%: fp32 products.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, int PASS, typename TIN>
 __global__ __launch_bounds__(64 * NW) void forward_kernel(SeqParams p) {
   __shared__ __attribute__((aligned(16))) unsigned char
@@ -851,9 +852,9 @@ __global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
 }
 
 // The backward pass's two walks in one launch: neither needs the other, and each alone leaves
-// most of the chip waiting while sequences and heads are few (64 heads of 2048 tokens, 128 x 128:
-// 139 + 186 us one after the other, 256 in one launch: 234 MB read and 732 MB written, of which
-// the states before and the state gradients after every chunk are 537).  Even workgroups go
+// most of the chip waiting while sequences and heads are few (64 heads of 2048 tokens, 128 x 128: of
+// kernels that took 139 + 186 us one after the other, 260 in one launch; these take 279: 235 MB read
+// and 723 MB written, of which the states before and the state gradients after every chunk are 537).  Even workgroups go
 // backward, odd ones forward.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
 __global__ __launch_bounds__(64 * NW) void both_kernel(SeqParams p) {
