@@ -854,8 +854,8 @@ __global__ __launch_bounds__(4 * DK) void join_kernel(SeqParams p) {
 // The backward pass's two walks in one launch: neither needs the other, and each alone leaves
 // most of the chip waiting while sequences and heads are few (64 heads of 2048 tokens, 128 x 128: of
 // kernels that took 139 + 186 us one after the other, 260 in one launch; these take 279: 235 MB read
-// and 723 MB written, of which the states before and the state gradients after every chunk are 537).  Even workgroups go
-// backward, odd ones forward.
+// and 723 MB written, of which the states before and the state gradients after every chunk are 537).
+// Even workgroups go backward, odd ones forward.
 template <int DK, int NT, int NW, bool RAW, bool DELTA, typename TIN>
 __global__ __launch_bounds__(64 * NW) void both_kernel(SeqParams p) {
   using Save = Stage<DK, NT, NW, RAW, DELTA, PASS_SAVE, TIN>;
