@@ -310,6 +310,75 @@ int dl_prefill_backward(const dl_desc* desc, const void* S_in, const dl_token* t
                         const dl_tables* tables, int32_t n, int32_t tokens, void* workspace,
                         size_t workspace_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------------- around a recurrence
+ * What a layer puts in front of the recurrences above -- a short causal convolution of every
+ * channel, norms and rotations of queries and keys -- and the recurrence whose decay differs by
+ * channel and state.  Whole sequences are packed as above and use the same dl_tables (of which
+ * these calls read cu_tokens and seq_slot only); single tokens take a slot list as the decode
+ * calls do.  n == 0 is a no-op; rows behind the last sequence are never used, and output rows
+ * there stay as they were.
+ *  - Token rows that are inputs may be columns of a wider array: *_stride counts the elements
+ *    from one row to the next, at least a row's width and a multiple of 8.  Arrays of in_dtype
+ *    and states are 16-byte aligned, fp32 parameters and int32 arrays 4-byte aligned.  Outputs
+ *    and gradients are dense.
+ *  - Products, sums, states' arithmetic and statistics are fp32; every output is rounded once.
+ *  - Outputs must not overlap inputs or each other, s_out = s_in apart.  Calls on distinct
+ *    buffers are re-entrant; calls that share a workspace must not overlap.
+ *  - Sums over tokens, rows or channels (gradients of parameters, of B and C) are taken in an
+ *    order that depends on sizes alone: the same call gives the same bits.
+ *  - Slots that are listed twice in one call race (undefined). */
+
+typedef enum { DL_ACT_NONE = 0, DL_ACT_SILU = 1 } dl_activation;
+
+/* Short causal convolution of every channel c of D, W taps:
+ *   a_t = bias + sum_j w[c,j] x_{t-W+1+j},   y_t = a_t or silu(a_t) = a_t / (1 + e^-a_t),
+ * x_t with t < 0 being the state: the W - 1 inputs before the first token, oldest first. */
+typedef struct {
+  int32_t abi_version;  /* must be DL_ABI_VERSION                                       */
+  int32_t num_slots;    /* B >= 1                                                       */
+  int32_t channels;     /* D >= 8, a multiple of 8                                      */
+  int32_t width;        /* W: 2, 3 or 4                                                 */
+  int32_t activation;   /* dl_activation                                                */
+  int32_t in_dtype;     /* dl_dtype of x, y, the states and their gradients             */
+} dl_conv_desc;
+
+typedef struct {
+  const void*  x;       /* [N,D] in_dtype                                               */
+  int64_t      x_stride;
+  const float* w;       /* [D,W] fp32, the newest input's tap last                      */
+  const float* bias;    /* [D] fp32, or NULL: none                                      */
+} dl_conv_rows;
+
+typedef struct {
+  void*  dx;            /* [N,D] in_dtype                                               */
+  float* dw;            /* [D,W] fp32                                                   */
+  float* dbias;         /* [D] fp32 (ignored without a bias)                            */
+  void*  ds;            /* [B,W-1,D] of the states before, or NULL.  Slots that no      */
+                        /* sequence has stay as they were.                              */
+} dl_conv_grads;
+
+/* One token per listed slot: y [n,D] from s_in [B,W-1,D] and x [n,D]; s_out (may be s_in) gets
+ * the listed slots' new states. */
+int dl_conv_step(const dl_conv_desc* desc, const void* s_in, void* s_out,
+                 const dl_conv_rows* rows, void* y, const int32_t* slots, int32_t n,
+                 hipStream_t stream);
+
+/* Whole sequences, each from s_in[slot] (s_in == NULL: zeros) to s_out[slot] (may be s_in). */
+int dl_conv_prefill(const dl_conv_desc* desc, const void* s_in, void* s_out,
+                    const dl_conv_rows* rows, void* y, const dl_tables* tables, int32_t n,
+                    int32_t tokens, hipStream_t stream);
+
+/* Bytes of workspace dl_conv_backward needs.  Writes *bytes. */
+int dl_conv_workspace_bytes(const dl_conv_desc* desc, int32_t n, int32_t tokens, size_t* bytes);
+
+/* Gradients of dl_conv_prefill from dy [N,D] and ds_out [B,W-1,D] (of the final states; NULL:
+ * zero), for the same s_in, rows and tables.  Nothing is kept from the forward call.  The
+ * gradients of s_in must not overlap ds_out.  workspace: 256-byte aligned. */
+int dl_conv_backward(const dl_conv_desc* desc, const void* s_in, const dl_conv_rows* rows,
+                     const void* dy, const void* ds_out, const dl_conv_grads* grads,
+                     const dl_tables* tables, int32_t n, int32_t tokens, void* workspace,
+                     size_t workspace_bytes, hipStream_t stream);
+
 /* Human-readable name of a dl_status value (static storage). */
 const char* dl_status_str(int status);
 

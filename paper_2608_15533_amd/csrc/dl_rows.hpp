@@ -1,0 +1,127 @@
+// Shared pieces of the kernels around a recurrence (convolution, norms, selective scan): rows of
+// fp32 values from 16-bit or 32-bit storage, stretches of packed sequences, sums over partial
+// results, host checks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "deltalog.h"
+#include "dl_internal.h"
+#include "dl_scan.hpp"
+
+namespace dl {
+
+// ------------------------------------------------------------------ rows
+// V consecutive values, V * sizeof(T) = 8 or 16 bytes, so aligned.
+template <int V, typename T>
+struct alignas(V * sizeof(T)) Raw {
+  T v[V];
+};
+template <int V, typename T>
+__device__ __forceinline__ Raw<V, T> load_raw(const T* p) {
+  return *reinterpret_cast<const Raw<V, T>*>(p);
+}
+template <int V, typename T>
+__device__ __forceinline__ void widen_row(const Raw<V, T>& r, float (&x)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] = widen(r.v[i]);
+}
+template <int V, typename T>
+__device__ __forceinline__ void load_row(const T* p, float (&x)[V]) {
+  widen_row(load_raw<V>(p), x);
+}
+template <int V, typename T>
+__device__ __forceinline__ void store_row(T* p, const float (&x)[V]) {
+  Raw<V, T> r;
+#pragma unroll
+  for (int i = 0; i < V; ++i) narrow(&r.v[i], x[i]);
+  *reinterpret_cast<Raw<V, T>*>(p) = r;
+}
+
+// 1 / (1 + e^-x): 0 and 1 at the infinities.
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + expf(-x)); }
+
+// ------------------------------------------------------------------ stretches of sequences
+// Sequences are cut into stretches of `len` tokens.  Stretch j of sequence i, whose first token is
+// row c_i, has the number c_i / len + i + j: c_{i+1} / len - c_i / len + 1 is at least the number of
+// stretches of sequence i and at least 1, so numbers differ, and tokens / len + n are enough.  An
+// empty sequence has one stretch without tokens (its state passes through).  Numbers that no
+// stretch has are idle.
+struct Stretch {
+  int seq, slot;
+  int first, count;   // token rows
+  int seq_first, seq_len;
+  bool idle;
+  __device__ bool begins() const { return first == seq_first; }
+  __device__ bool ends() const { return first + count == seq_first + seq_len; }
+};
+__host__ __device__ inline int64_t stretches(int64_t n, int64_t tokens, int len) {
+  return tokens / len + n;
+}
+
+// By all lanes of a wave, for a number that is the same in all of them: 64 sequences are looked at
+// at a time.  Whatever the tables hold, what comes back lies within N rows and B slots.
+__device__ __forceinline__ Stretch find_stretch(const int32_t* cu, const int32_t* seq_slot, int n,
+                                                int N, int B, int len, int f) {
+  const int lane = threadIdx.x & 63;
+  auto row = [&](int i) { return min(max(cu[i], 0), N); };
+  int lo = 0, size = n;
+  while (size > 1) {
+    const int step = (size + 63) >> 6, i = lo + lane * step;
+    const bool at_or_before = lane * step < size && row(i) / len + i <= f;
+    const int hits = __popcll(__ballot(at_or_before));
+    const int skip = hits > 0 ? (hits - 1) * step : 0;
+    lo += skip;
+    size = min(step, size - skip);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  Stretch s;
+  s.seq = lo;
+  s.seq_first = __builtin_amdgcn_readfirstlane(row(lo));
+  s.seq_len = max(__builtin_amdgcn_readfirstlane(row(lo + 1)) - s.seq_first, 0);
+  s.slot = __builtin_amdgcn_readfirstlane(seq_slot[lo]);
+  const int64_t off = int64_t(f - (s.seq_first / len + lo)) * len;
+  s.idle = off < 0 || off > s.seq_len || (off > 0 && off == s.seq_len) || s.slot < 0 || s.slot >= B;
+  s.first = s.idle ? 0 : s.seq_first + int(off);
+  s.count = s.idle ? 0 : min(len, s.seq_len - int(off));
+  return s;
+}
+
+// ------------------------------------------------------------------ sums of partial results
+// out[i] = sum over p < P of part[p, i], i < M: part [P, M].
+hipError_t launch_column_sum(const float* part, int64_t P, int64_t M, float* out, hipStream_t s);
+
+// ------------------------------------------------------------------ host
+inline bool aligned_to(const void* p, uintptr_t a) {
+  return (reinterpret_cast<uintptr_t>(p) % a) == 0;
+}
+inline bool good_stride(int64_t stride, int64_t width) {
+  return stride >= width && stride % 8 == 0 && stride <= (int64_t(1) << 40);
+}
+inline size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
+inline bool grid_fits(int64_t blocks, int threads) {
+  return blocks <= 0x7fffffff && blocks * threads <= int64_t(0xffffffff);
+}
+
+template <typename K, typename P>
+hipError_t start_rows(K* kernel, int64_t grid, int block, const P& p, hipStream_t s) {
+  P q = p;
+  void* args[] = {&q};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3(unsigned(grid)), dim3(block),
+                         args, 0, s);
+}
+
+inline int check_row_tables(const dl_tables* t) {
+  if (!t || !t->cu_tokens || !t->seq_slot) return DL_E_NULL;
+  if (!aligned_to(t->cu_tokens, 4) || !aligned_to(t->seq_slot, 4)) return DL_E_ALIGN;
+  return DL_OK;
+}
+
+}  // namespace dl
+
+#define DL_TRY(x)                 \
+  do {                            \
+    const int rc_ = (x);          \
+    if (rc_ != DL_OK) return rc_; \
+  } while (0)

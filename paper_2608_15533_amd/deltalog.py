@@ -42,13 +42,16 @@ OP_IDS = {"gdn": DL_OP_GDN, "kda": DL_OP_KDA, "rwkv6": DL_OP_RWKV6, "linattn": D
 DELTA_OP_IDS = (DL_OP_GDN, DL_OP_KDA)                  # b = beta (v - correction); needs beta
 PER_KEY_OP_IDS = (DL_OP_KDA, DL_OP_RWKV6, DL_OP_GLA)   # lambda is [.., dk]; else one per head
 DTYPE_IDS = {"f32": DL_F32, "bf16": DL_BF16}
+DL_ACT_NONE, DL_ACT_SILU = 0, 1
+ACTIVATION_IDS = {"none": DL_ACT_NONE, "silu": DL_ACT_SILU}
 TORCH_DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 EXPORTED = ("dl_eager_step", "dl_append_step", "dl_merge", "dl_readout",
             "dl_append_step_tiled", "dl_tiled_workspace_bytes", "dl_status_str",
             "dl_abi_version", "dl_build_flags", "dl_append_step_tiled_noalloc",
             "dl_chunk_tables", "dl_prefill_workspace_bytes", "dl_prefill",
-            "dl_prefill_backward")
+            "dl_prefill_backward",
+            "dl_conv_step", "dl_conv_prefill", "dl_conv_workspace_bytes", "dl_conv_backward")
 
 
 class dl_desc(ctypes.Structure):
@@ -82,6 +85,20 @@ class dl_grads(ctypes.Structure):
                 ("dS", ctypes.c_void_p)]
 
 
+class dl_conv_desc(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("abi_version", "num_slots", "channels", "width",
+                                              "activation", "in_dtype")]
+
+
+class dl_conv_rows(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("w", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p)]
+
+
+class dl_conv_grads(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("dx", "dw", "dbias", "ds")]
+
+
 _P = ctypes.c_void_p
 _lib.dl_eager_step.argtypes = [ctypes.POINTER(dl_desc), _P, ctypes.POINTER(dl_token), _P, _P,
                                ctypes.c_int32, _P]
@@ -110,10 +127,18 @@ _lib.dl_prefill.argtypes = [ctypes.POINTER(dl_desc), _P, _P, ctypes.POINTER(dl_t
 _lib.dl_prefill_backward.argtypes = [ctypes.POINTER(dl_desc), _P, ctypes.POINTER(dl_token), _P,
                                      _P, ctypes.POINTER(dl_grads), ctypes.POINTER(dl_tables),
                                      ctypes.c_int32, ctypes.c_int32, _P, ctypes.c_size_t, _P]
+_I, _PTR, _SIZE = ctypes.c_int32, ctypes.POINTER, ctypes.c_size_t
+_lib.dl_conv_step.argtypes = [_PTR(dl_conv_desc), _P, _P, _PTR(dl_conv_rows), _P, _P, _I, _P]
+_lib.dl_conv_prefill.argtypes = [_PTR(dl_conv_desc), _P, _P, _PTR(dl_conv_rows), _P,
+                                 _PTR(dl_tables), _I, _I, _P]
+_lib.dl_conv_workspace_bytes.argtypes = [_PTR(dl_conv_desc), _I, _I, _PTR(_SIZE)]
+_lib.dl_conv_backward.argtypes = [_PTR(dl_conv_desc), _P, _PTR(dl_conv_rows), _P, _P,
+                                  _PTR(dl_conv_grads), _PTR(dl_tables), _I, _I, _P, _SIZE, _P]
 for _f in ("dl_eager_step", "dl_append_step", "dl_merge", "dl_readout", "dl_append_step_tiled",
            "dl_tiled_workspace_bytes", "dl_abi_version", "dl_append_step_tiled_noalloc",
            "dl_chunk_tables", "dl_prefill_workspace_bytes", "dl_prefill",
-           "dl_prefill_backward"):
+           "dl_prefill_backward", "dl_conv_step", "dl_conv_prefill", "dl_conv_workspace_bytes",
+           "dl_conv_backward"):
     getattr(_lib, _f).restype = ctypes.c_int
 _lib.dl_status_str.argtypes = [ctypes.c_int]
 _lib.dl_status_str.restype = ctypes.c_char_p
@@ -488,3 +513,153 @@ def dl_prefill_backward(desc, S_in, tok, d_o, dS_out, grads, tables, workspace, 
                                     _ptr(d_o), _ptr(dS_out), ctypes.byref(grads.struct),
                                     ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,
                                     _stream(stream)), "dl_prefill_backward")
+
+
+# ----------------------------------------------------------------- around a recurrence
+def _in_torch_dtype(desc):
+    return torch.bfloat16 if desc.in_dtype == DL_BF16 else torch.float32
+
+
+def _need_rows(t, name, dtype, shape):
+    """Elements from one row of ``t`` to the next: token rows may be columns of a wider tensor,
+    everything behind the first dimension is dense."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    width = 1
+    for size, stride in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
+        if size != 1 and stride != width:
+            raise ValueError(f"{name}: a row must be dense")
+        width *= size
+    if shape[0] <= 1:
+        return width                       # the stride of a single row means nothing
+    if t.stride(0) < width or t.stride(0) % 8:
+        raise ValueError(f"{name}: rows {t.stride(0)} elements apart, expected a multiple of 8 that "
+                         f"is {width} at least")
+    return t.stride(0)
+
+
+def _optional(t, name, dtype, shape):
+    if t is not None:
+        _need(t, name, dtype, shape)
+
+
+def _workspace(workspace, maker):
+    if workspace is None or not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous device tensor (see {maker})")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _made_for(desc, rows, tables=None, grads=None):
+    """The rows (and gradients) were made for this descriptor and these tables."""
+    if rows.sizes != _sizes(desc):
+        raise ValueError("the rows were made for another descriptor")
+    if tables is not None and rows.n != tables.tokens:
+        raise ValueError(f"{rows.n} rows but the tables are for {tables.tokens}")
+    if grads is not None and (grads.n != rows.n or grads.sizes != rows.sizes
+                              or grads.given != tuple(t is not None for t in rows.tensors)):
+        raise ValueError("the gradients were made for other rows or another descriptor")
+    if grads is not None and getattr(grads, "slots", None) not in (None, getattr(desc, "num_slots", 0)):
+        raise ValueError("the gradient of the states was made for another descriptor")
+
+
+def _sizes(desc):
+    """All of a descriptor but the slots, which rows do not depend on."""
+    return tuple(getattr(desc, k) for k, _ in desc._fields_ if k != "num_slots")
+
+
+def _bytes(call, where, desc, *args):
+    out = ctypes.c_size_t(0)
+    _check(call(ctypes.byref(desc), *args, ctypes.byref(out)), where)
+    return out.value
+
+
+def make_conv_desc(B, channels, width, in_dtype="bf16", activation="silu"):
+    """dl_conv_desc of a short causal convolution: ``width`` taps, states in B slots."""
+    return dl_conv_desc(DL_ABI_VERSION, B, channels, width, ACTIVATION_IDS[activation],
+                        DTYPE_IDS[in_dtype])
+
+
+class ConvRows:
+    """What a convolution reads: token rows x [n,D] in the input dtype (columns of a wider tensor
+    will do), w [D,W] and bias [D] (or None) in fp32."""
+
+    def __init__(self, desc, n, x, w, bias=None):
+        stride = _need_rows(x, "x", _in_torch_dtype(desc), (n, desc.channels))
+        _need(w, "w", torch.float32, (desc.channels, desc.width))
+        _optional(bias, "bias", torch.float32, (desc.channels,))
+        self.n, self.sizes, self.tensors = n, _sizes(desc), (x, w, bias)
+        self.struct = dl_conv_rows(_ptr(x), stride, _ptr(w), _ptr(bias))
+
+
+class ConvGrads:
+    """Device buffers for the gradients of one dl_conv_prefill call; ``s``: the states before
+    (None: no gradient of them)."""
+
+    def __init__(self, desc, rows, s=None):
+        x, w, bias = rows.tensors
+        self.dx = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
+        self.dw = torch.zeros_like(w)
+        self.dbias = None if bias is None else torch.zeros_like(bias)
+        _optional(s, "s", *_conv_state(desc))
+        self.ds = None if s is None else torch.zeros_like(s)
+        self.n, self.sizes = rows.n, rows.sizes
+        self.given = tuple(t is not None for t in rows.tensors)
+        self.slots = None if s is None else desc.num_slots
+        self.struct = dl_conv_grads(_ptr(self.dx), _ptr(self.dw), _ptr(self.dbias), _ptr(self.ds))
+
+
+def _conv_state(desc):
+    return _in_torch_dtype(desc), (desc.num_slots, desc.width - 1, desc.channels)
+
+
+def dl_conv_step(desc, s_in, s_out, rows, y, slots=None, stream=None):
+    """One token per slot through the convolution: y [n,D], and the slots' new states (the last
+    W - 1 inputs) from s_in [B,W-1,D] to s_out (may be s_in)."""
+    sp, n = _rows(desc, slots, rows.n)
+    _made_for(desc, rows)
+    _need(s_in, "s_in", *_conv_state(desc))
+    _need(s_out, "s_out", *_conv_state(desc))
+    _need(y, "y", _in_torch_dtype(desc), (n, desc.channels))
+    _on_current_device(*rows.tensors, s_in, s_out, y, slots)
+    _check(_lib.dl_conv_step(ctypes.byref(desc), _ptr(s_in), _ptr(s_out), ctypes.byref(rows.struct),
+                             _ptr(y), sp, n, _stream(stream)), "dl_conv_step")
+
+
+def dl_conv_prefill(desc, s_in, s_out, rows, y, tables, stream=None):
+    """The convolution over the whole sequences of ``tables``, from s_in[slot] (None: zeros) to
+    s_out[slot] (may be s_in), y [N,D] in the input dtype."""
+    _made_for(desc, rows, tables)
+    _optional(s_in, "s_in", *_conv_state(desc))
+    _need(s_out, "s_out", *_conv_state(desc))
+    _need(y, "y", _in_torch_dtype(desc), (rows.n, desc.channels))
+    _on_current_device(*rows.tensors, s_in, s_out, y, tables.err)
+    _check(_lib.dl_conv_prefill(ctypes.byref(desc), _ptr(s_in), _ptr(s_out),
+                                ctypes.byref(rows.struct), _ptr(y), ctypes.byref(tables.struct),
+                                tables.n, tables.tokens, _stream(stream)), "dl_conv_prefill")
+
+
+def conv_workspace(desc, n, tokens, device="cuda"):
+    """A device buffer of the size dl_conv_workspace_bytes names (dl_conv_backward's scratch)."""
+    size = _bytes(_lib.dl_conv_workspace_bytes, "dl_conv_workspace_bytes", desc, int(n), int(tokens))
+    return torch.empty((size,), dtype=torch.uint8, device=device)
+
+
+def dl_conv_backward(desc, s_in, rows, dy, ds_out, grads, tables, workspace, stream=None):
+    """Gradients of dl_conv_prefill into ``grads`` (``ConvGrads``) from dy [N,D] and ds_out
+    [B,W-1,D] (None: zero).  The forward call must have left s_in as it was."""
+    _made_for(desc, rows, tables, grads)
+    _optional(s_in, "s_in", *_conv_state(desc))
+    _optional(ds_out, "ds_out", *_conv_state(desc))
+    _need(dy, "dy", _in_torch_dtype(desc), (rows.n, desc.channels))
+    wp, wn = _workspace(workspace, "conv_workspace")
+    _on_current_device(*rows.tensors, s_in, dy, ds_out, grads.dx, grads.ds, tables.err, workspace)
+    _check(_lib.dl_conv_backward(ctypes.byref(desc), _ptr(s_in), ctypes.byref(rows.struct), _ptr(dy),
+                                 _ptr(ds_out), ctypes.byref(grads.struct),
+                                 ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,
+                                 _stream(stream)), "dl_conv_backward")
