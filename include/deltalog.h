@@ -379,6 +379,61 @@ int dl_conv_backward(const dl_conv_desc* desc, const void* s_in, const dl_conv_r
                      const dl_tables* tables, int32_t n, int32_t tokens, void* workspace,
                      size_t workspace_bytes, hipStream_t stream);
 
+/* Norms of queries and keys, head by head, with the rotation by position in the same pass.  For
+ * a head x of d places: n = scale w . x / sqrt(c sum x^2 + eps), c = 1 (L2) or 1 / d (root mean
+ * square); no norm: n = scale w . x; scale is q_scale for queries, 1 for keys.  Then pair i of
+ * the first rot places -- (i, rot/2 + i) for halves, (2i, 2i + 1) for pairs -- turns by the angle
+ * pos freq[i] (the product in 64 bits): (a cos - b sin, a sin + b cos).  Every head is written rep
+ * times, output heads h rep .. h rep + rep - 1, for recurrences whose heads share keys.  Any rows:
+ * prompts, training, one token a slot. */
+typedef enum { DL_NORM_NONE = 0, DL_NORM_L2 = 1, DL_NORM_RMS = 2 } dl_norm;
+typedef enum { DL_TURN_NONE = 0, DL_TURN_HALVES = 1, DL_TURN_PAIRS = 2 } dl_turn;
+
+typedef struct {
+  int32_t abi_version;  /* must be DL_ABI_VERSION                                       */
+  int32_t heads;        /* H >= 1 of the inputs; H rep <= DL_MAX_HEADS                  */
+  int32_t head_dim;     /* d: 64 or 128                                                 */
+  int32_t rep;          /* >= 1                                                         */
+  int32_t norm;         /* dl_norm                                                      */
+  int32_t turn;         /* dl_turn                                                      */
+  int32_t rot;          /* places that turn: a multiple of 16 up to d; 0 without turn   */
+  int32_t in_dtype;     /* dl_dtype of q, k, outputs and their gradients                */
+  float eps;            /* above 0 with a norm                                          */
+  float q_scale;
+} dl_qk_desc;
+
+typedef struct {
+  const void*    q;     /* [n,H,d] in_dtype                                             */
+  const void*    k;     /* [n,H,d] in_dtype                                             */
+  int64_t        q_stride, k_stride;
+  const int32_t* pos;   /* [n] positions (may be NULL without turn)                     */
+  const float*   freq;  /* [rot/2] fp32, radians a position (may be NULL without turn)  */
+  const float*   wq;    /* [d] fp32 weights, both or (NULL) neither                     */
+  const float*   wk;
+  const int32_t* used;  /* [1] rows in use, as dl_tables' cu_tokens + n (device); rows  */
+                        /* behind them stay untouched.  NULL: all n                     */
+} dl_qk_rows;
+
+typedef struct {
+  void*  dq;            /* [n,H,d] in_dtype                                             */
+  void*  dk;
+  float* dwq;           /* [d] fp32 (ignored without weights)                           */
+  float* dwk;
+} dl_qk_grads;
+
+/* q_out, k_out [n,H rep,d]. */
+int dl_qk_norm(const dl_qk_desc* desc, const dl_qk_rows* rows, void* q_out, void* k_out,
+               int32_t n, hipStream_t stream);
+
+/* Bytes of workspace dl_qk_norm_backward needs (with weights; without them it may be NULL).
+ * Writes *bytes. */
+int dl_qk_workspace_bytes(const dl_qk_desc* desc, int32_t n, size_t* bytes);
+
+/* Gradients of dl_qk_norm from dq_out, dk_out [n,H rep,d], for the same rows. */
+int dl_qk_norm_backward(const dl_qk_desc* desc, const dl_qk_rows* rows, const void* dq_out,
+                        const void* dk_out, const dl_qk_grads* grads, int32_t n, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+
 /* Human-readable name of a dl_status value (static storage). */
 const char* dl_status_str(int status);
 

@@ -7,8 +7,6 @@
 //   dbias = sum_t g_t.
 // Bound by memory: every input is read once and every output written once, but for the K rows that
 // neighbouring stretches of a sequence share.
-#include <algorithm>
-
 #include "dl_rows.hpp"
 
 namespace dl {
@@ -408,8 +406,8 @@ int dl_conv_backward(const dl_conv_desc* desc, const void* s_in, const dl_conv_r
   p.dw = static_cast<float*>(workspace);
   p.dbias = p.dw + parts * D * desc->width;
   hipError_t e = launch(BACKWARD, desc, p, parts, stream);
-  if (e == hipSuccess) e = launch_column_sum(p.dw, parts, D * desc->width, g->dw, stream);
-  if (e == hipSuccess && p.bias) e = launch_column_sum(p.dbias, parts, D, g->dbias, stream);
+  if (e == hipSuccess) e = launch_column_sum(p.dw, parts, D * desc->width, D * desc->width, g->dw, stream);
+  if (e == hipSuccess && p.bias) e = launch_column_sum(p.dbias, parts, D, D, g->dbias, stream);
   return e == hipSuccess ? DL_OK : DL_E_HIP;
 }
 

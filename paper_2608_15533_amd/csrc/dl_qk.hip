@@ -1,0 +1,365 @@
+// Norms of queries and keys for each head, with the rotation by position: entry points and kernels.
+//
+// For a head x of a token at position p, with r = (c sum x^2 + eps)^(-1/2), c = 1 (L2) or 1 / d (root
+// mean square), r = 1 without a norm:  n = scale r (w . x);  of the first rot places those of a pair
+// (a, b) become (a cos - b sin, a sin + b cos) with the angle p freq_i.  Every head is written rep times.
+// Gradients, g the sum over the rep copies turned back and scaled:  dw = sum g r x,
+// dx = r (w . g) - x c r^3 <w . g, x>.
+// Bound by memory: every head is read once and written rep times.
+#include "dl_rows.hpp"
+
+namespace dl {
+namespace {
+
+struct QkParams {
+  const void *q, *k;
+  void *qo, *ko;               // outputs (backward: dq, dk)
+  const void *dqo, *dko;       // backward
+  const int32_t *pos, *used;
+  const float *freq, *wq, *wk;
+  float* part;                 // backward: [workgroups, 2, d] partial sums, or null
+  int64_t q_stride, k_stride;
+  float share, eps, q_scale;   // share: c above
+  int32_t N, H, rep, rot, per; // per: tokens of a workgroup
+};
+
+constexpr int NT = 256;        // threads of a workgroup
+constexpr int V = 8;           // values of a head that a lane holds
+
+// Sum over the 8 or 16 lanes of a head, in all of them: lane i and its neighbours in a quad, then the
+// mirror images among 8 and among 16 lanes.
+template <int D>
+__device__ __forceinline__ float head_sum(float x) {
+  auto add = [&](auto ctrl) {
+    constexpr int C = decltype(ctrl)::value;
+    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), C, 0xf, 0xf, true));
+  };
+  add(std::integral_constant<int, 0xB1>{});    // quad_perm [1,0,3,2]
+  add(std::integral_constant<int, 0x4E>{});    // quad_perm [2,3,0,1]
+  add(std::integral_constant<int, 0x141>{});   // row_half_mirror
+  if (D == 128) add(std::integral_constant<int, 0x140>{});  // row_mirror
+  return x;
+}
+
+// cos and sin of position x frequency, the product in 64 bits: an angle of a million radians keeps
+// all of its fraction of a turn.
+__device__ __forceinline__ float2 turn_of(int pos, float freq) {
+  const double turns = double(pos) * double(freq) * 0.15915494309189533577;
+  const float part = float(turns - rint(turns));
+  float2 cs;
+  sincospif(2.0f * part, &cs.y, &cs.x);
+  return cs;
+}
+
+// The angles of this lane's values, from LDS: halves use 8 of them (the same in a pair's two lanes),
+// pairs 4.
+enum Turn { NONE = DL_TURN_NONE, HALVES = DL_TURN_HALVES, PAIRS = DL_TURN_PAIRS };
+template <int T>
+struct Angles {
+  static constexpr int M = T == HALVES ? V : T == PAIRS ? V / 2 : 1;
+  float c[M], s[M];
+  int partner;
+  bool turned, first;
+  __device__ __forceinline__ void load(const float2* lds, int li, int rot) {
+    if (T == NONE) return;
+    const int half = rot / 16;                 // lanes of one half
+    turned = li * V < rot;
+    first = li < half;
+    partner = (threadIdx.x & 63) + (!turned ? 0 : first ? half : -half);
+    const int at = !turned ? 0 : T == HALVES ? (first ? li : li - half) * V : li * M;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      c[i] = turned ? lds[at + i].x : 1.0f;
+      s[i] = turned ? lds[at + i].y : 0.0f;
+    }
+  }
+  // Turned by the angles, or back.  By all lanes of the head.
+  __device__ __forceinline__ void apply(float (&x)[V], bool back) const {
+    if (T == HALVES) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float other = __shfl(x[i], partner);
+        const float sn = first != back ? -s[i] : s[i];      // first place: a cos - b sin
+        if (turned) x[i] = fmaf(x[i], c[i], other * sn);
+      }
+    } else if (T == PAIRS) {
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) {
+        const float sn = back ? -s[i] : s[i], a = x[2 * i], b = x[2 * i + 1];
+        x[2 * i] = fmaf(a, c[i], -b * sn);
+        x[2 * i + 1] = fmaf(a, sn, b * c[i]);
+      }
+    }
+  }
+};
+
+template <int T>
+__device__ __forceinline__ void fill_angles(const QkParams& p, int token, float2* lds) {
+  if (T == NONE) return;
+  const int pos = p.pos[token];
+  for (int i = threadIdx.x; i < p.rot / 2; i += NT) lds[i] = turn_of(pos, p.freq[i]);
+}
+
+// A workgroup: `per` tokens, one after the other; D / 8 lanes a head.
+template <int D, int T, bool NORM, typename E>
+__global__ __launch_bounds__(NT) void qk_kernel(QkParams p) {
+  constexpr int LPH = D / V, HEADS = NT / LPH;
+  __shared__ float2 lds[2][D / 2];
+  const int li = threadIdx.x % LPH, group = threadIdx.x / LPH;
+  const int rows = p.used ? min(max(*p.used, 0), p.N) : p.N;
+  const int64_t first = int64_t(blockIdx.x) * p.per;
+  float w[2][V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    w[0][i] = (p.wq ? p.wq[li * V + i] : 1.0f) * p.q_scale;
+    w[1][i] = p.wk ? p.wk[li * V + i] : 1.0f;
+  }
+  for (int j = 0; j < p.per; ++j) {
+    const int64_t token = first + j;
+    if (token >= rows) return;
+    fill_angles<T>(p, int(token), lds[j & 1]);
+    if (T != NONE) __syncthreads();
+    Angles<T> turn;
+    turn.load(lds[j & 1], li, p.rot);
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+      const E* in = kind ? static_cast<const E*>(p.k) + token * p.k_stride
+                         : static_cast<const E*>(p.q) + token * p.q_stride;
+      E* out = static_cast<E*>(kind ? p.ko : p.qo) + token * p.H * p.rep * D;
+      for (int h = group; h < p.H; h += HEADS) {
+        float x[V];
+        load_row<V>(in + h * D + li * V, x);
+        float r = 1.0f;
+        if (NORM) {
+          float ss = 0.0f;
+#pragma unroll
+          for (int i = 0; i < V; ++i) ss = fmaf(x[i], x[i], ss);
+          r = __builtin_amdgcn_rsqf(fmaf(head_sum<D>(ss), p.share, p.eps));
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] *= r * w[kind][i];
+        turn.apply(x, false);
+        for (int c = 0; c < p.rep; ++c) store_row<V>(out + (int64_t(h) * p.rep + c) * D + li * V, x);
+      }
+    }
+  }
+}
+
+template <int D, int T, bool NORM, typename E>
+__global__ __launch_bounds__(NT) void qk_backward_kernel(QkParams p) {
+  constexpr int LPH = D / V, HEADS = NT / LPH;
+  __shared__ float2 lds[2][D / 2];
+  __shared__ float sums[HEADS][D];
+  const int li = threadIdx.x % LPH, group = threadIdx.x / LPH;
+  const int rows = p.used ? min(max(*p.used, 0), p.N) : p.N;
+  const int64_t first = int64_t(blockIdx.x) * p.per;
+  float w[2][V], dw[2][V] = {};
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    w[0][i] = p.wq ? p.wq[li * V + i] : 1.0f;
+    w[1][i] = p.wk ? p.wk[li * V + i] : 1.0f;
+  }
+  for (int j = 0; j < p.per; ++j) {
+    const int64_t token = first + j;
+    if (token >= rows) break;
+    fill_angles<T>(p, int(token), lds[j & 1]);
+    if (T != NONE) __syncthreads();
+    Angles<T> turn;
+    turn.load(lds[j & 1], li, p.rot);
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+      const E* in = kind ? static_cast<const E*>(p.k) + token * p.k_stride
+                         : static_cast<const E*>(p.q) + token * p.q_stride;
+      const E* up = static_cast<const E*>(kind ? p.dko : p.dqo) + token * p.H * p.rep * D;
+      E* out = static_cast<E*>(kind ? p.ko : p.qo) + token * p.H * D;
+      const float scale = kind ? 1.0f : p.q_scale;
+      for (int h = group; h < p.H; h += HEADS) {
+        float x[V], g[V];
+        load_row<V>(in + h * D + li * V, x);
+        load_row<V>(up + int64_t(h) * p.rep * D + li * V, g);
+        for (int c = 1; c < p.rep; ++c) {
+          float more[V];
+          load_row<V>(up + (int64_t(h) * p.rep + c) * D + li * V, more);
+#pragma unroll
+          for (int i = 0; i < V; ++i) g[i] += more[i];
+        }
+        turn.apply(g, true);
+        float ss = 0.0f, along = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) ss = fmaf(x[i], x[i], ss);
+        const float r = NORM ? __builtin_amdgcn_rsqf(fmaf(head_sum<D>(ss), p.share, p.eps)) : 1.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          g[i] *= scale * r;
+          dw[kind][i] = fmaf(g[i], x[i], dw[kind][i]);
+          g[i] *= w[kind][i];
+          along = fmaf(g[i], x[i], along);
+        }
+        if (NORM) {
+          const float back = head_sum<D>(along) * r * r * p.share;
+#pragma unroll
+          for (int i = 0; i < V; ++i) g[i] = fmaf(-back, x[i], g[i]);
+        }
+        store_row<V>(out + int64_t(h) * D + li * V, g);
+      }
+    }
+  }
+  if (!p.part) return;
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; ++i) sums[group][li * V + i] = dw[kind][i];
+    __syncthreads();
+    if (threadIdx.x < D) {
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < HEADS; ++i) s += sums[i][threadIdx.x];
+      p.part[(int64_t(blockIdx.x) * 2 + kind) * D + threadIdx.x] = s;
+    }
+  }
+}
+
+template <int D, int T, bool NORM, typename E>
+hipError_t launch_type(const QkParams& p, bool backward, int64_t grid, hipStream_t s) {
+  return backward ? start_rows(&qk_backward_kernel<D, T, NORM, E>, grid, NT, p, s)
+                  : start_rows(&qk_kernel<D, T, NORM, E>, grid, NT, p, s);
+}
+template <int D, int T>
+hipError_t launch_turn(const dl_qk_desc* d, const QkParams& p, bool backward, int64_t grid, hipStream_t s) {
+  const bool norm = d->norm != DL_NORM_NONE;
+  if (d->in_dtype == DL_BF16)
+    return norm ? launch_type<D, T, true, uint16_t>(p, backward, grid, s)
+                : launch_type<D, T, false, uint16_t>(p, backward, grid, s);
+  return norm ? launch_type<D, T, true, float>(p, backward, grid, s)
+              : launch_type<D, T, false, float>(p, backward, grid, s);
+}
+template <int D>
+hipError_t launch_dim(const dl_qk_desc* d, const QkParams& p, bool backward, int64_t grid, hipStream_t s) {
+  switch (d->turn) {
+    case DL_TURN_HALVES: return launch_turn<D, HALVES>(d, p, backward, grid, s);
+    case DL_TURN_PAIRS: return launch_turn<D, PAIRS>(d, p, backward, grid, s);
+    default: return launch_turn<D, NONE>(d, p, backward, grid, s);
+  }
+}
+
+// Tokens of a workgroup.
+int tokens_per(int32_t n, bool backward) { return backward ? std::max(1, std::min(8, n / 1024)) : 1; }
+
+int check_desc(const dl_qk_desc* d) {
+  if (!d) return DL_E_NULL;
+  if (d->abi_version != DL_ABI_VERSION) return DL_E_VERSION;
+  if (d->head_dim != 64 && d->head_dim != 128) return DL_E_UNSUPPORTED;
+  if (d->norm < DL_NORM_NONE || d->norm > DL_NORM_RMS) return DL_E_UNSUPPORTED;
+  if (d->turn < DL_TURN_NONE || d->turn > DL_TURN_PAIRS) return DL_E_UNSUPPORTED;
+  if (d->heads < 1 || d->rep < 1 || int64_t(d->heads) * d->rep > DL_MAX_HEADS) return DL_E_SHAPE;
+  if (d->turn == DL_TURN_NONE ? d->rot != 0 : d->rot < 16 || d->rot > d->head_dim || d->rot % 16 != 0)
+    return DL_E_SHAPE;
+  // Without an eps above 0 a head of zeros has no norm; what is not a number is neither.
+  if (d->norm != DL_NORM_NONE && !(d->eps > 0.0f)) return DL_E_UNSUPPORTED;
+  if (d->in_dtype != DL_F32 && d->in_dtype != DL_BF16) return DL_E_DTYPE;
+  return DL_OK;
+}
+
+int check_rows(const dl_qk_desc* d, const dl_qk_rows* r) {
+  if (!r || !r->q || !r->k) return DL_E_NULL;
+  if (d->turn != DL_TURN_NONE && (!r->pos || !r->freq)) return DL_E_NULL;
+  if ((r->wq == nullptr) != (r->wk == nullptr)) return DL_E_NULL;
+  if (!aligned_to(r->q, 16) || !aligned_to(r->k, 16) || !aligned_to(r->pos, 4) || !aligned_to(r->freq, 4) ||
+      !aligned_to(r->wq, 4) || !aligned_to(r->wk, 4) || !aligned_to(r->used, 4))
+    return DL_E_ALIGN;
+  const int64_t width = int64_t(d->heads) * d->head_dim;
+  if (!good_stride(r->q_stride, width) || !good_stride(r->k_stride, width)) return DL_E_SHAPE;
+  return DL_OK;
+}
+
+QkParams params(const dl_qk_desc* d, const dl_qk_rows* r, void* qo, void* ko, int32_t n, bool backward) {
+  QkParams p{};
+  p.q = r->q;
+  p.k = r->k;
+  p.qo = qo;
+  p.ko = ko;
+  p.pos = r->pos;
+  p.used = r->used;
+  p.freq = r->freq;
+  p.wq = r->wq;
+  p.wk = r->wk;
+  p.q_stride = r->q_stride;
+  p.k_stride = r->k_stride;
+  p.share = d->norm == DL_NORM_RMS ? 1.0f / float(d->head_dim) : 1.0f;
+  p.eps = d->eps;
+  p.q_scale = d->q_scale;
+  p.N = n;
+  p.H = d->heads;
+  p.rep = d->rep;
+  p.rot = d->rot;
+  p.per = tokens_per(n, backward);
+  return p;
+}
+
+hipError_t launch(const dl_qk_desc* d, const QkParams& p, bool backward, hipStream_t s) {
+  const int64_t grid = (int64_t(p.N) + p.per - 1) / p.per;
+  return d->head_dim == 128 ? launch_dim<128>(d, p, backward, grid, s)
+                            : launch_dim<64>(d, p, backward, grid, s);
+}
+
+int check_count(int32_t n) { return n < 0 || !grid_fits(n, NT) ? DL_E_SHAPE : DL_OK; }
+
+}  // namespace
+}  // namespace dl
+
+using namespace dl;
+
+extern "C" {
+
+int dl_qk_norm(const dl_qk_desc* desc, const dl_qk_rows* rows, void* q_out, void* k_out, int32_t n,
+               hipStream_t stream) {
+  DL_TRY(check_desc(desc));
+  DL_TRY(check_count(n));
+  if (n == 0) return DL_OK;               // nothing to do, whatever the pointers are
+  DL_TRY(check_rows(desc, rows));
+  if (!q_out || !k_out) return DL_E_NULL;
+  if (!aligned_to(q_out, 16) || !aligned_to(k_out, 16)) return DL_E_ALIGN;
+  return launch(desc, params(desc, rows, q_out, k_out, n, false), false, stream) == hipSuccess ? DL_OK : DL_E_HIP;
+}
+
+int dl_qk_workspace_bytes(const dl_qk_desc* desc, int32_t n, size_t* bytes) {
+  DL_TRY(check_desc(desc));
+  DL_TRY(check_count(n));
+  if (!bytes) return DL_E_NULL;
+  const int64_t per = tokens_per(n, true);
+  *bytes = size_t((n + per - 1) / per) * 2 * size_t(desc->head_dim) * sizeof(float);
+  return DL_OK;
+}
+
+int dl_qk_norm_backward(const dl_qk_desc* desc, const dl_qk_rows* rows, const void* dq_out, const void* dk_out,
+                        const dl_qk_grads* g, int32_t n, void* workspace, size_t workspace_bytes,
+                        hipStream_t stream) {
+  DL_TRY(check_desc(desc));
+  DL_TRY(check_count(n));
+  if (n == 0) return DL_OK;               // nothing to do, whatever the pointers are
+  DL_TRY(check_rows(desc, rows));
+  if (!dq_out || !dk_out || !g || !g->dq || !g->dk) return DL_E_NULL;
+  if (!aligned_to(dq_out, 16) || !aligned_to(dk_out, 16) || !aligned_to(g->dq, 16) || !aligned_to(g->dk, 16) ||
+      !aligned_to(g->dwq, 4) || !aligned_to(g->dwk, 4))
+    return DL_E_ALIGN;
+  QkParams p = params(desc, rows, g->dq, g->dk, n, true);
+  p.dqo = dq_out;
+  p.dko = dk_out;
+  if (p.wq) {
+    if (!g->dwq || !g->dwk) return DL_E_NULL;
+    size_t need = 0;
+    DL_TRY(dl_qk_workspace_bytes(desc, n, &need));
+    if (!workspace) return DL_E_NULL;
+    if (!aligned_to(workspace, 256)) return DL_E_ALIGN;
+    if (workspace_bytes < need) return DL_E_SHAPE;
+    p.part = static_cast<float*>(workspace);
+  }
+  hipError_t e = launch(desc, p, true, stream);
+  const int64_t parts = (int64_t(n) + p.per - 1) / p.per, d = desc->head_dim;
+  if (e == hipSuccess && p.part) e = launch_column_sum(p.part, parts, d, 2 * d, g->dwq, stream);
+  if (e == hipSuccess && p.part) e = launch_column_sum(p.part + d, parts, d, 2 * d, g->dwk, stream);
+  return e == hipSuccess ? DL_OK : DL_E_HIP;
+}
+
+}  // extern "C"

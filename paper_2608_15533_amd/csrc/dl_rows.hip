@@ -7,7 +7,7 @@ namespace {
 struct SumParams {
   const float* part;
   float* out;
-  int64_t P, M;
+  int64_t P, M, stride;
 };
 
 // A workgroup for 64 columns; four waves take every fourth row each and are joined in order.
@@ -17,7 +17,7 @@ __global__ __launch_bounds__(256) void column_sum_kernel(SumParams p) {
   const int64_t col = int64_t(blockIdx.x) * 64 + lane;
   float acc = 0.0f;
   if (col < p.M)
-    for (int64_t r = wave; r < p.P; r += 4) acc += p.part[r * p.M + col];
+    for (int64_t r = wave; r < p.P; r += 4) acc += p.part[r * p.stride + col];
   lds[wave][lane] = acc;
   __syncthreads();
   if (wave == 0 && col < p.M)
@@ -26,9 +26,10 @@ __global__ __launch_bounds__(256) void column_sum_kernel(SumParams p) {
 
 }  // namespace
 
-hipError_t launch_column_sum(const float* part, int64_t P, int64_t M, float* out, hipStream_t s) {
+hipError_t launch_column_sum(const float* part, int64_t P, int64_t M, int64_t stride, float* out,
+                             hipStream_t s) {
   if (M <= 0) return hipSuccess;
-  const SumParams p{part, out, P, M};
+  const SumParams p{part, out, P, M, stride};
   return start_rows(&column_sum_kernel, (M + 63) / 64, 256, p, s);
 }
 

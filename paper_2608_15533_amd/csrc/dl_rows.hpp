@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "deltalog.h"
 #include "dl_internal.h"
 #include "dl_scan.hpp"
@@ -13,9 +15,9 @@
 namespace dl {
 
 // ------------------------------------------------------------------ rows
-// V consecutive values, V * sizeof(T) = 8 or 16 bytes, so aligned.
+// V consecutive values: 8, 16 or 32 bytes, aligned to 16 at most.
 template <int V, typename T>
-struct alignas(V * sizeof(T)) Raw {
+struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Raw {
   T v[V];
 };
 template <int V, typename T>
@@ -89,8 +91,9 @@ __device__ __forceinline__ Stretch find_stretch(const int32_t* cu, const int32_t
 }
 
 // ------------------------------------------------------------------ sums of partial results
-// out[i] = sum over p < P of part[p, i], i < M: part [P, M].
-hipError_t launch_column_sum(const float* part, int64_t P, int64_t M, float* out, hipStream_t s);
+// out[i] = sum over p < P of part[p * stride + i], i < M.
+hipError_t launch_column_sum(const float* part, int64_t P, int64_t M, int64_t stride, float* out,
+                             hipStream_t s);
 
 // ------------------------------------------------------------------ host
 inline bool aligned_to(const void* p, uintptr_t a) {

@@ -44,6 +44,8 @@ PER_KEY_OP_IDS = (DL_OP_KDA, DL_OP_RWKV6, DL_OP_GLA)   # lambda is [.., dk]; els
 DTYPE_IDS = {"f32": DL_F32, "bf16": DL_BF16}
 DL_ACT_NONE, DL_ACT_SILU = 0, 1
 ACTIVATION_IDS = {"none": DL_ACT_NONE, "silu": DL_ACT_SILU}
+NORM_IDS = {"none": 0, "l2": 1, "rms": 2}
+TURN_IDS = {"none": 0, "halves": 1, "pairs": 2}
 TORCH_DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 EXPORTED = ("dl_eager_step", "dl_append_step", "dl_merge", "dl_readout",
@@ -51,7 +53,8 @@ EXPORTED = ("dl_eager_step", "dl_append_step", "dl_merge", "dl_readout",
             "dl_abi_version", "dl_build_flags", "dl_append_step_tiled_noalloc",
             "dl_chunk_tables", "dl_prefill_workspace_bytes", "dl_prefill",
             "dl_prefill_backward",
-            "dl_conv_step", "dl_conv_prefill", "dl_conv_workspace_bytes", "dl_conv_backward")
+            "dl_conv_step", "dl_conv_prefill", "dl_conv_workspace_bytes", "dl_conv_backward",
+            "dl_qk_norm", "dl_qk_workspace_bytes", "dl_qk_norm_backward")
 
 
 class dl_desc(ctypes.Structure):
@@ -99,6 +102,22 @@ class dl_conv_grads(ctypes.Structure):
     _fields_ = [(k, ctypes.c_void_p) for k in ("dx", "dw", "dbias", "ds")]
 
 
+class dl_qk_desc(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("abi_version", "heads", "head_dim", "rep", "norm",
+                                              "turn", "rot", "in_dtype")]
+    _fields_ += [("eps", ctypes.c_float), ("q_scale", ctypes.c_float)]
+
+
+class dl_qk_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64)]
+    _fields_ += [(k, ctypes.c_void_p) for k in ("pos", "freq", "wq", "wk", "used")]
+
+
+class dl_qk_grads(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("dq", "dk", "dwq", "dwk")]
+
+
 _P = ctypes.c_void_p
 _lib.dl_eager_step.argtypes = [ctypes.POINTER(dl_desc), _P, ctypes.POINTER(dl_token), _P, _P,
                                ctypes.c_int32, _P]
@@ -134,11 +153,15 @@ _lib.dl_conv_prefill.argtypes = [_PTR(dl_conv_desc), _P, _P, _PTR(dl_conv_rows),
 _lib.dl_conv_workspace_bytes.argtypes = [_PTR(dl_conv_desc), _I, _I, _PTR(_SIZE)]
 _lib.dl_conv_backward.argtypes = [_PTR(dl_conv_desc), _P, _PTR(dl_conv_rows), _P, _P,
                                   _PTR(dl_conv_grads), _PTR(dl_tables), _I, _I, _P, _SIZE, _P]
+_lib.dl_qk_norm.argtypes = [_PTR(dl_qk_desc), _PTR(dl_qk_rows), _P, _P, _I, _P]
+_lib.dl_qk_workspace_bytes.argtypes = [_PTR(dl_qk_desc), _I, _PTR(_SIZE)]
+_lib.dl_qk_norm_backward.argtypes = [_PTR(dl_qk_desc), _PTR(dl_qk_rows), _P, _P, _PTR(dl_qk_grads),
+                                     _I, _P, _SIZE, _P]
 for _f in ("dl_eager_step", "dl_append_step", "dl_merge", "dl_readout", "dl_append_step_tiled",
            "dl_tiled_workspace_bytes", "dl_abi_version", "dl_append_step_tiled_noalloc",
            "dl_chunk_tables", "dl_prefill_workspace_bytes", "dl_prefill",
            "dl_prefill_backward", "dl_conv_step", "dl_conv_prefill", "dl_conv_workspace_bytes",
-           "dl_conv_backward"):
+           "dl_conv_backward", "dl_qk_norm", "dl_qk_workspace_bytes", "dl_qk_norm_backward"):
     getattr(_lib, _f).restype = ctypes.c_int
 _lib.dl_status_str.argtypes = [ctypes.c_int]
 _lib.dl_status_str.restype = ctypes.c_char_p
@@ -663,3 +686,80 @@ def dl_conv_backward(desc, s_in, rows, dy, ds_out, grads, tables, workspace, str
                                  _ptr(ds_out), ctypes.byref(grads.struct),
                                  ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,
                                  _stream(stream)), "dl_conv_backward")
+
+
+def make_qk_desc(H, d, norm="l2", turn="none", rot=None, rep=1, in_dtype="bf16", eps=1e-6,
+                 q_scale=1.0):
+    """dl_qk_desc: ``norm`` "l2", "rms" or "none"; ``turn`` "halves", "pairs" or "none" for the first
+    ``rot`` places (None: all of them); ``rep`` output heads for each of the H input heads."""
+    rot = (0 if turn == "none" else d) if rot is None else rot
+    return dl_qk_desc(DL_ABI_VERSION, H, d, rep, NORM_IDS[norm], TURN_IDS[turn], rot,
+                      DTYPE_IDS[in_dtype], eps, q_scale)
+
+
+class QkRows:
+    """What the norm of queries and keys reads: q, k [n,H,d] in the input dtype (columns of a wider
+    tensor will do), positions pos [n] int32 and frequencies freq [rot/2] fp32 where they turn,
+    weights wq, wk [d] fp32 (both or neither).  ``tables``: rows behind its sequences are left out."""
+
+    def __init__(self, desc, n, q, k, pos=None, freq=None, wq=None, wk=None, tables=None):
+        H, d, it = desc.heads, desc.head_dim, _in_torch_dtype(desc)
+        qs, ks = (_need_rows(t, name, it, (n, H, d)) for t, name in ((q, "q"), (k, "k")))
+        if desc.turn == TURN_IDS["none"]:
+            pos = freq = None
+        else:
+            _need(pos, "pos", torch.int32, (n,))
+            _need(freq, "freq", torch.float32, (desc.rot // 2,))
+        if (wq is None) != (wk is None):
+            raise ValueError("weights for both queries and keys, or for neither")
+        _optional(wq, "wq", torch.float32, (d,))
+        _optional(wk, "wk", torch.float32, (d,))
+        if tables is not None and tables.tokens != n:
+            raise ValueError(f"{n} rows but the tables are for {tables.tokens}")
+        used = None if tables is None else tables.cu_tokens[tables.n:]
+        self.n, self.sizes, self.tensors = n, _sizes(desc), (q, k, pos, freq, wq, wk, used)
+        self.struct = dl_qk_rows(_ptr(q), _ptr(k), qs, ks, _ptr(pos), _ptr(freq), _ptr(wq),
+                                 _ptr(wk), _ptr(used))
+
+
+class QkGrads:
+    """Device buffers for the gradients of one dl_qk_norm call."""
+
+    def __init__(self, desc, rows):
+        q, k, wq, wk = (rows.tensors[i] for i in (0, 1, 4, 5))
+        self.dq, self.dk = (torch.zeros(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        self.dwq, self.dwk = (None if t is None else torch.zeros_like(t) for t in (wq, wk))
+        self.n, self.sizes = rows.n, rows.sizes
+        self.given = tuple(t is not None for t in rows.tensors)
+        self.struct = dl_qk_grads(_ptr(self.dq), _ptr(self.dk), _ptr(self.dwq), _ptr(self.dwk))
+
+
+def dl_qk_norm(desc, rows, q_out, k_out, stream=None):
+    """Queries and keys normalised head by head and turned by position, into q_out and k_out
+    [n,H rep,d]."""
+    _made_for(desc, rows)
+    out = (_in_torch_dtype(desc), (rows.n, desc.heads * desc.rep, desc.head_dim))
+    _need(q_out, "q_out", *out)
+    _need(k_out, "k_out", *out)
+    _on_current_device(*rows.tensors, q_out, k_out)
+    _check(_lib.dl_qk_norm(ctypes.byref(desc), ctypes.byref(rows.struct), _ptr(q_out), _ptr(k_out),
+                           rows.n, _stream(stream)), "dl_qk_norm")
+
+
+def qk_workspace(desc, n, device="cuda"):
+    """A device buffer of the size dl_qk_workspace_bytes names (dl_qk_norm_backward's scratch)."""
+    size = _bytes(_lib.dl_qk_workspace_bytes, "dl_qk_workspace_bytes", desc, int(n))
+    return torch.empty((size,), dtype=torch.uint8, device=device)
+
+
+def dl_qk_norm_backward(desc, rows, dq_out, dk_out, grads, workspace, stream=None):
+    """Gradients of dl_qk_norm into ``grads`` (``QkGrads``) from dq_out and dk_out [n,H rep,d]."""
+    _made_for(desc, rows, grads=grads)
+    out = (_in_torch_dtype(desc), (rows.n, desc.heads * desc.rep, desc.head_dim))
+    _need(dq_out, "dq_out", *out)
+    _need(dk_out, "dk_out", *out)
+    wp, wn = _workspace(workspace, "qk_workspace")
+    _on_current_device(*rows.tensors, dq_out, dk_out, grads.dq, grads.dk, workspace)
+    _check(_lib.dl_qk_norm_backward(ctypes.byref(desc), ctypes.byref(rows.struct), _ptr(dq_out),
+                                    _ptr(dk_out), ctypes.byref(grads.struct), rows.n, wp, wn,
+                                    _stream(stream)), "dl_qk_norm_backward")
