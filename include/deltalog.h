@@ -434,6 +434,69 @@ int dl_qk_norm_backward(const dl_qk_desc* desc, const dl_qk_rows* rows, const vo
                         const void* dk_out, const dl_qk_grads* grads, int32_t n, void* workspace,
                         size_t workspace_bytes, hipStream_t stream);
 
+/* Selective state space scan: channel c of D has S states, with its own decays.  With
+ * d_t = softplus(dt_t + dt_bias), softplus(r) = log(1 + e^r):
+ *   h_t = exp(d_t A) . h_{t-1} + d_t x_t B_t,   y_t = (<C_t, h_t> + skip x_t) silu(z_t),
+ * A and h_t [S] per channel (A <= 0 forgets; taken at its value), B_t and C_t [S] the same for
+ * all channels, skip and z left out where NULL.  Whole sequences are cut into stretches that run
+ * side by side: what a sequence's results round to depends on the call's n and tokens. */
+typedef struct {
+  int32_t abi_version;  /* must be DL_ABI_VERSION                                       */
+  int32_t num_slots;    /* >= 1                                                         */
+  int32_t channels;     /* D >= 8, a multiple of 8                                      */
+  int32_t states;       /* S: 16, 32 or 64                                              */
+  int32_t in_dtype;     /* dl_dtype of x, dt, z, B, C, y and their gradients            */
+} dl_ssm_desc;          /* states are fp32, [num_slots,D,S]                             */
+
+typedef struct {
+  const void*  x;       /* [N,D] in_dtype                                               */
+  const void*  dt;      /* [N,D] in_dtype                                               */
+  const void*  z;       /* [N,D] in_dtype, or NULL: no gate                             */
+  const void*  B;       /* [N,S] in_dtype                                               */
+  const void*  C;       /* [N,S] in_dtype                                               */
+  int64_t      x_stride, dt_stride, z_stride, b_stride, c_stride;
+  const float* A;       /* [D,S] fp32                                                   */
+  const float* skip;    /* [D] fp32, or NULL                                            */
+  const float* dt_bias; /* [D] fp32, or NULL                                            */
+} dl_ssm_rows;
+
+typedef struct {
+  void*  dx;            /* [N,D] in_dtype, and so on                                    */
+  void*  ddt;
+  void*  dz;            /* ignored without z                                            */
+  void*  dB;            /* [N,S]                                                        */
+  void*  dC;
+  float* dA;            /* [D,S]                                                        */
+  float* dskip;         /* [D]; ignored without skip                                    */
+  float* dbias;         /* [D]; ignored without dt_bias                                 */
+  float* ds;            /* [num_slots,D,S] of the states before, or NULL.  Slots that   */
+                        /* no sequence has stay as they were.                           */
+} dl_ssm_grads;
+
+/* One token per listed slot: y [n,D] from h_in and one row each; h_out (may be h_in) gets the
+ * listed slots' new states. */
+int dl_ssm_step(const dl_ssm_desc* desc, const float* h_in, float* h_out, const dl_ssm_rows* rows,
+                void* y, const int32_t* slots, int32_t n, hipStream_t stream);
+
+/* Bytes of workspace dl_ssm_prefill (backward == 0) or dl_ssm_prefill and dl_ssm_backward
+ * (backward != 0) need; may be 0, and the workspace NULL then.  Writes *bytes. */
+int dl_ssm_workspace_bytes(const dl_ssm_desc* desc, int32_t n, int32_t tokens, int32_t backward,
+                           size_t* bytes);
+
+/* Whole sequences, each from h_in[slot] (h_in == NULL: zeros) to h_out[slot] (may be h_in).
+ * workspace: 256-byte aligned. */
+int dl_ssm_prefill(const dl_ssm_desc* desc, const float* h_in, float* h_out,
+                   const dl_ssm_rows* rows, void* y, const dl_tables* tables, int32_t n,
+                   int32_t tokens, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Gradients of dl_ssm_prefill from dy [N,D] and dh_out (of the final states; NULL: zero), for the
+ * same h_in, rows and tables.  Nothing is kept from the forward call.  The gradients of h_in must
+ * not overlap dh_out. */
+int dl_ssm_backward(const dl_ssm_desc* desc, const float* h_in, const dl_ssm_rows* rows,
+                    const void* dy, const float* dh_out, const dl_ssm_grads* grads,
+                    const dl_tables* tables, int32_t n, int32_t tokens, void* workspace,
+                    size_t workspace_bytes, hipStream_t stream);
+
 /* Human-readable name of a dl_status value (static storage). */
 const char* dl_status_str(int status);
 

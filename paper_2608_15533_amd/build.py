@@ -24,7 +24,7 @@ ARCH = "gfx950"
 SOURCES = ["abi.cpp", "dl_gdn.hip", "dl_kda.hip", "dl_rwkv6.hip", "dl_linattn.hip",
            "dl_retnet.hip", "dl_gla.hip", "dl_noalloc.hip", "dl_tables.hip",
            "dl_prefill.hip", "dl_prefill_bwd.hip", "dl_rows.hip", "dl_conv.hip",
-           "dl_qk.hip"]
+           "dl_qk.hip", "dl_ssm.hip", "dl_ssm_bwd.hip"]
 
 # No packed-fp32 instructions; MFMA accumulators in ordinary VGPRs (the merge's MFMA
 # contraction accumulates into the state tile's own registers: AGPR accumulators would

@@ -26,21 +26,6 @@ struct QkParams {
 constexpr int NT = 256;        // threads of a workgroup
 constexpr int V = 8;           // values of a head that a lane holds
 
-// Sum over the 8 or 16 lanes of a head, in all of them: lane i and its neighbours in a quad, then the
-// mirror images among 8 and among 16 lanes.
-template <int D>
-__device__ __forceinline__ float head_sum(float x) {
-  auto add = [&](auto ctrl) {
-    constexpr int C = decltype(ctrl)::value;
-    x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), C, 0xf, 0xf, true));
-  };
-  add(std::integral_constant<int, 0xB1>{});    // quad_perm [1,0,3,2]
-  add(std::integral_constant<int, 0x4E>{});    // quad_perm [2,3,0,1]
-  add(std::integral_constant<int, 0x141>{});   // row_half_mirror
-  if (D == 128) add(std::integral_constant<int, 0x140>{});  // row_mirror
-  return x;
-}
-
 // cos and sin of position x frequency, the product in 64 bits: an angle of a million radians keeps
 // all of its fraction of a turn.
 __device__ __forceinline__ float2 turn_of(int pos, float freq) {
@@ -134,7 +119,7 @@ __global__ __launch_bounds__(NT) void qk_kernel(QkParams p) {
           float ss = 0.0f;
 #pragma unroll
           for (int i = 0; i < V; ++i) ss = fmaf(x[i], x[i], ss);
-          r = __builtin_amdgcn_rsqf(fmaf(head_sum<D>(ss), p.share, p.eps));
+          r = __builtin_amdgcn_rsqf(fmaf(lanes_sum<D / V>(ss), p.share, p.eps));
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) x[i] *= r * w[kind][i];
@@ -187,7 +172,7 @@ __global__ __launch_bounds__(NT) void qk_backward_kernel(QkParams p) {
         float ss = 0.0f, along = 0.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) ss = fmaf(x[i], x[i], ss);
-        const float r = NORM ? __builtin_amdgcn_rsqf(fmaf(head_sum<D>(ss), p.share, p.eps)) : 1.0f;
+        const float r = NORM ? __builtin_amdgcn_rsqf(fmaf(lanes_sum<D / V>(ss), p.share, p.eps)) : 1.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           g[i] *= scale * r;
@@ -196,7 +181,7 @@ __global__ __launch_bounds__(NT) void qk_backward_kernel(QkParams p) {
           along = fmaf(g[i], x[i], along);
         }
         if (NORM) {
-          const float back = head_sum<D>(along) * r * r * p.share;
+          const float back = lanes_sum<D / V>(along) * r * r * p.share;
 #pragma unroll
           for (int i = 0; i < V; ++i) g[i] = fmaf(-back, x[i], g[i]);
         }

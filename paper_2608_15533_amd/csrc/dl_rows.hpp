@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "deltalog.h"
 #include "dl_internal.h"
@@ -39,6 +40,38 @@ __device__ __forceinline__ void store_row(T* p, const float (&x)[V]) {
 #pragma unroll
   for (int i = 0; i < V; ++i) narrow(&r.v[i], x[i]);
   *reinterpret_cast<Raw<V, T>*>(p) = r;
+}
+
+// ------------------------------------------------------------------ lanes
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+// The sum over aligned groups of N lanes, in all of them: neighbours in a quad, then mirror images
+// among 8 and among 16 lanes.  Every lane of a group takes part.
+template <int N>
+__device__ __forceinline__ float lanes_sum(float x) {
+  static_assert(N == 4 || N == 8 || N == 16, "within rows of 16 lanes");
+  x += from_lane<0xB1>(x);                    // quad_perm [1,0,3,2]
+  x += from_lane<0x4E>(x);                    // quad_perm [2,3,0,1]
+  if constexpr (N >= 8) x += from_lane<0x141>(x);   // row_half_mirror
+  if constexpr (N >= 16) x += from_lane<0x140>(x);  // row_mirror
+  return x;
+}
+// Two sums over lane pairs, one for each half of the lanes: a(l) + a(l ^ 32) in lanes 0-31 and
+// b(l) + b(l ^ 32) in lanes 32-63; a(l) + a(l ^ 16) in even rows of 16 lanes and b's in odd ones;
+// a(l) + a(l ^ 8) in the first eight lanes of a row and b's in the last.
+__device__ __forceinline__ float halves_sum32(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halves_sum16(float a, float b) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halves_sum8(float a, float b) {
+  const bool last = threadIdx.x & 8;
+  return (last ? b : a) + from_lane<0x128>(last ? a : b);   // row_ror:8
 }
 
 // 1 / (1 + e^-x): 0 and 1 at the infinities.

@@ -1,0 +1,467 @@
+// Selective state space scan: entry points, forward pass, single tokens.
+#include "dl_ssm.hpp"
+#include "dl_ssm_bwd.hpp"
+
+namespace dl {
+namespace {
+
+constexpr int TILE = 16;       // tokens whose steps lie in LDS at a time
+
+// A workgroup: one stretch, 64 channels; wave w has states 4 w .. 4 w + 3.  OUT: outputs and final
+// states; else E and the sum of d, of stretches that others follow.
+template <int S, bool OUT, typename T>
+__global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
+  constexpr int NW = S / 4, NT = 64 * NW, EV = TILE * 64 / NT, CG = 64 / EV;
+  __shared__ __attribute__((aligned(16))) float step[TILE][64], input[TILE][64];
+  __shared__ __attribute__((aligned(16))) float partial[OUT ? NW : 1][OUT ? TILE : 1][64];
+  const int f = blockIdx.x / p.blocks, c0 = int(blockIdx.x % p.blocks) * 64;
+  const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, f);
+  if (s.idle || (!OUT && s.ends())) return;
+  const int lane = threadIdx.x & 63, w = wave_index(), c = c0 + lane;
+  const bool live = c < p.D;
+  // This thread's part of a tile: a token, EV channels.
+  const int te = threadIdx.x / CG, ce = (threadIdx.x % CG) * EV;
+  const bool le = c0 + ce < p.D;                     // D is a multiple of 8: all EV or none
+  const int64_t at = int64_t(f) * p.D * S + (int64_t(w) * p.D + c) * 4;   // of E
+
+  float a2[4], h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a2[i] = live ? p.A[int64_t(c) * S + 4 * w + i] * LOG2E : 0.0f;
+    h[i] = 0.0f;
+  }
+  const int64_t state = (int64_t(s.slot) * p.D + c) * S + 4 * w;
+  if (OUT && live && (p.E || p.h_in)) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(p.E ? p.E + at : p.h_in + state);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = v[i];
+  }
+  float bias[EV], skip[EV], total[EV];
+#pragma unroll
+  for (int e = 0; e < EV; ++e) {
+    bias[e] = p.bias && le ? p.bias[c0 + ce + e] : 0.0f;
+    skip[e] = OUT && p.skip && le ? p.skip[c0 + ce + e] : 0.0f;
+    total[e] = 0.0f;
+  }
+  const T* xp = static_cast<const T*>(p.x) + c0 + ce;
+  const T* dp = static_cast<const T*>(p.dt) + c0 + ce;
+  const T* zp = static_cast<const T*>(p.z) + c0 + ce;
+  const T* bp = static_cast<const T*>(p.Bm) + int64_t(s.first) * p.b_stride + 4 * w;
+  const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
+  Raw<EV, T> rx{}, rd{}, rz{};
+  auto fetch = [&](int t0) {
+    if (!le || t0 + te >= s.count) return;
+    const int64_t row = s.first + t0 + te;
+    rx = load_raw<EV>(xp + row * p.x_stride);
+    rd = load_raw<EV>(dp + row * p.dt_stride);
+    if (OUT && p.z) rz = load_raw<EV>(zp + row * p.z_stride);
+  };
+  fetch(0);
+  for (int t0 = 0; t0 < s.count; t0 += TILE) {
+    const int count = min(TILE, s.count - t0);
+    const bool mine = le && te < count;
+    float x[EV], z[EV];
+    widen_row(rx, x);
+    widen_row(rz, z);
+#pragma unroll
+    for (int e = 0; e < EV; ++e) {
+      const float d = mine ? softplus(widen(rd.v[e]) + bias[e]) : 0.0f;
+      step[te][ce + e] = d;
+      input[te][ce + e] = mine ? d * x[e] : 0.0f;
+      total[e] += d;
+    }
+    fetch(t0 + TILE);
+    __syncthreads();
+#pragma unroll 4
+    for (int t = 0; t < count; ++t) {
+      Four<T> B, C;
+      B.load(bp + int64_t(t0 + t) * p.b_stride);
+      if (OUT) C.load(cp + int64_t(t0 + t) * p.c_stride);
+      const float d = step[t][lane], u = input[t][lane];
+      float y = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[i] = fmaf(decay(d, a2[i]), h[i], u * B.at(i));
+        if (OUT) y = fmaf(C.at(i), h[i], y);
+      }
+      if (OUT) partial[w][t][lane] = y;
+    }
+    __syncthreads();
+    if (OUT && mine) {
+      float y[EV];
+#pragma unroll
+      for (int e = 0; e < EV; ++e) {
+        y[e] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) y[e] += partial[i][te][ce + e];
+        y[e] = fmaf(skip[e], x[e], y[e]);
+        if (p.z) y[e] *= z[e] * quick_sigmoid(z[e]);
+      }
+      store_row<EV>(static_cast<T*>(p.y) + (int64_t(s.first) + t0 + te) * p.D + c0 + ce, y);
+    }
+  }
+  if (OUT) {
+    if (s.ends() && live) *reinterpret_cast<f32x4*>(p.h_out + state) = f32x4{h[0], h[1], h[2], h[3]};
+    return;
+  }
+  if (live) *reinterpret_cast<f32x4*>(p.E + at) = f32x4{h[0], h[1], h[2], h[3]};
+  // The sum of d over the stretch: each thread's own tokens, then the tile's tokens in order.
+#pragma unroll
+  for (int e = 0; e < EV; ++e) step[te][ce + e] = total[e];
+  __syncthreads();
+  if (w == 0 && live) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < TILE; ++t) sum += step[t][lane];
+    p.sums[int64_t(f) * p.D + c] = sum;
+  }
+}
+
+// States before every stretch, in place of what each leaves from zero; a thread for one state of one
+// sequence.  BWD: likewise from the end, gradients behind every stretch.
+template <bool BWD>
+__global__ __launch_bounds__(256) void ssm_join_kernel(SsmParams p) {
+  const int64_t per = int64_t(p.D) * p.S, groups = (per + 255) / 256;
+  const int seq = int(blockIdx.x / groups);
+  const int64_t i = int64_t(blockIdx.x % groups) * 256 + threadIdx.x;
+  const int first = min(max(p.cu[seq], 0), p.N), end = min(max(p.cu[seq + 1], first), p.N);
+  const int slot = p.seq_slot[seq], base = first / p.len + seq;
+  const int parts = max(1, (end - first + p.len - 1) / p.len);
+  if (i >= per || slot < 0 || slot >= p.B) return;
+  const int c = int((i >> 2) % p.D), k = int(i / (4 * int64_t(p.D))) * 4 + int(i & 3);
+  const float a2 = p.A[int64_t(c) * p.S + k] * LOG2E;
+  const int64_t state = (int64_t(slot) * p.D + c) * p.S + k;
+  float* E = p.E + i;
+  float h = p.h_in ? p.h_in[state] : 0.0f;
+  constexpr int U = 8;
+  for (int j = 0; j < parts; j += U) {
+    float e[U], d[U];
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      const int64_t r = base + min(j + q, parts - 1);
+      const bool there = j + q + 1 < parts;          // the last stretch leaves nothing here
+      e[q] = there ? E[r * per] : 0.0f;
+      d[q] = there ? p.sums[r * p.D + c] : 0.0f;
+    }
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      if (j + q >= parts) break;
+      E[(base + j + q) * per] = h;
+      h = fmaf(decay(d[q], a2), h, e[q]);
+    }
+  }
+  if (!BWD) return;
+  float* F = p.F + i;
+  float g = p.dh_out ? p.dh_out[state] : 0.0f;
+  for (int j = parts - 1; j >= 0; j -= U) {
+    float e[U], d[U];
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      const int64_t r = base + max(j - q, 0);
+      const bool there = j - q > 0;                  // nothing is asked of the first
+      e[q] = there ? F[r * per] : 0.0f;
+      d[q] = there ? p.sums[r * p.D + c] : 0.0f;
+    }
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      if (j - q < 0) break;
+      F[(base + j - q) * per] = g;
+      g = fmaf(decay(d[q], a2), g, e[q]);
+    }
+  }
+}
+
+// One token a slot: four states a lane, S / 4 lanes a channel.
+template <int S, typename T>
+__global__ __launch_bounds__(256) void ssm_step_kernel(SsmParams p) {
+  constexpr int L = S / 4, CH = 256 / L;
+  const int i = blockIdx.x / p.blocks, c = int(blockIdx.x % p.blocks) * CH + int(threadIdx.x) / L;
+  const int k = (threadIdx.x % L) * 4;
+  const int slot = p.slots ? p.slots[i] : i;
+  if (c >= p.D || slot < 0 || slot >= p.B) return;
+  const int64_t state = (int64_t(slot) * p.D + c) * S + k;
+  const f32x4 old = *reinterpret_cast<const f32x4*>(p.h_in + state);
+  float B[4], C[4];
+  load_row<4>(static_cast<const T*>(p.Bm) + i * p.b_stride + k, B);
+  load_row<4>(static_cast<const T*>(p.Cm) + i * p.c_stride + k, C);
+  const float x = widen(static_cast<const T*>(p.x)[i * p.x_stride + c]);
+  const float raw = widen(static_cast<const T*>(p.dt)[i * p.dt_stride + c]) + (p.bias ? p.bias[c] : 0.0f);
+  const float d = softplus(raw), u = d * x;
+  f32x4 h;
+  float y = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    h[e] = fmaf(decay(d, p.A[int64_t(c) * S + k + e] * LOG2E), old[e], u * B[e]);
+    y = fmaf(C[e], h[e], y);
+  }
+  *reinterpret_cast<f32x4*>(p.h_out + state) = h;
+  y = lanes_sum<L>(y);
+  if (k) return;
+  if (p.skip) y = fmaf(p.skip[c], x, y);
+  if (p.z) {
+    const float z = widen(static_cast<const T*>(p.z)[i * p.z_stride + c]);
+    y *= z * quick_sigmoid(z);
+  }
+  narrow(static_cast<T*>(p.y) + int64_t(i) * p.D + c, y);
+}
+
+template <int S, typename T>
+hipError_t launch_prefill(const SsmParams& p, hipStream_t s) {
+  const int64_t grid = stretches(p.n, p.N, p.len) * p.blocks;
+  if (p.E) {
+    hipError_t e = start_rows(&ssm_kernel<S, false, T>, grid, S * 16, p, s);
+    const int64_t groups = (int64_t(p.D) * S + 255) / 256;
+    if (e == hipSuccess) e = start_rows(&ssm_join_kernel<false>, groups * p.n, 256, p, s);
+    if (e != hipSuccess) return e;
+  }
+  return start_rows(&ssm_kernel<S, true, T>, grid, S * 16, p, s);
+}
+
+template <int S, typename T>
+hipError_t launch_backward(const SsmParams& p, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (p.E) {
+    e = launch_ssm_ends(S, sizeof(T) == 2, p, s);
+    const int64_t groups = (int64_t(p.D) * S + 255) / 256;
+    if (e == hipSuccess) e = start_rows(&ssm_join_kernel<true>, groups * p.n, 256, p, s);
+  }
+  if (e == hipSuccess) e = launch_ssm_grad(S, sizeof(T) == 2, p, s);
+  return e;
+}
+
+template <int S, typename T>
+hipError_t launch_step(const SsmParams& q, hipStream_t s) {
+  SsmParams p = q;
+  p.blocks = (p.D + 1024 / S - 1) / (1024 / S);
+  return start_rows(&ssm_step_kernel<S, T>, int64_t(p.n) * p.blocks, 256, p, s);
+}
+
+enum Pass { STEP, FORWARD, BACKWARD };
+template <int S, typename T>
+hipError_t launch_pass(Pass pass, const SsmParams& p, hipStream_t s) {
+  return pass == STEP ? launch_step<S, T>(p, s) : pass == FORWARD ? launch_prefill<S, T>(p, s)
+                                                                 : launch_backward<S, T>(p, s);
+}
+template <typename T>
+hipError_t launch_states(Pass pass, const SsmParams& p, hipStream_t s) {
+  switch (p.S) {
+    case 16: return launch_pass<16, T>(pass, p, s);
+    case 32: return launch_pass<32, T>(pass, p, s);
+    default: return launch_pass<64, T>(pass, p, s);
+  }
+}
+hipError_t launch(Pass pass, const dl_ssm_desc* d, const SsmParams& p, hipStream_t s) {
+  return d->in_dtype == DL_BF16 ? launch_states<uint16_t>(pass, p, s) : launch_states<float>(pass, p, s);
+}
+
+int blocks_of(const dl_ssm_desc* d) { return (d->channels + 63) / 64; }
+
+// Tokens of a stretch: as long as enough waves are left to fill the chip.
+int stretch_len(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
+  if (backward) return ssm_grad_tokens(d->states);
+  const int64_t waves = int64_t(blocks_of(d)) * (d->states / 4);
+  int64_t len = 64;
+  while (len < tokens && stretches(n, tokens, int(2 * len)) * waves >= 4096) len *= 2;
+  return int(std::min<int64_t>(len, std::max(tokens, 1)));
+}
+// One stretch a sequence: nothing to join.
+bool whole(int32_t tokens, int len) { return tokens <= len; }
+
+int check_desc(const dl_ssm_desc* d) {
+  if (!d) return DL_E_NULL;
+  if (d->abi_version != DL_ABI_VERSION) return DL_E_VERSION;
+  if (d->states != 16 && d->states != 32 && d->states != 64) return DL_E_UNSUPPORTED;
+  if (d->channels < 8 || d->channels % 8 != 0 || d->channels > (1 << 20)) return DL_E_SHAPE;
+  if (d->num_slots < 1) return DL_E_SHAPE;
+  if (d->in_dtype != DL_F32 && d->in_dtype != DL_BF16) return DL_E_DTYPE;
+  return DL_OK;
+}
+
+int check_counts(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
+  if (n < 0 || tokens < 0 || n > d->num_slots) return DL_E_SHAPE;
+  const int64_t rows = stretches(n, tokens, stretch_len(d, n, tokens, backward));
+  if (!grid_fits(rows * blocks_of(d), d->states * 16)) return DL_E_SHAPE;
+  const int64_t groups = (int64_t(d->channels) * d->states + 255) / 256;
+  return grid_fits(groups * n, 256) ? DL_OK : DL_E_SHAPE;
+}
+
+int check_rows(const dl_ssm_desc* d, const dl_ssm_rows* r, bool any) {
+  if (!r || !r->A || (any && (!r->x || !r->dt || !r->B || !r->C))) return DL_E_NULL;
+  for (const void* v : {r->x, r->dt, r->z, r->B, r->C})
+    if (!aligned_to(v, 16)) return DL_E_ALIGN;
+  if (!aligned_to(r->A, 4) || !aligned_to(r->skip, 4) || !aligned_to(r->dt_bias, 4)) return DL_E_ALIGN;
+  if (!any) return DL_OK;
+  if (!good_stride(r->x_stride, d->channels) || !good_stride(r->dt_stride, d->channels) ||
+      (r->z && !good_stride(r->z_stride, d->channels)) || !good_stride(r->b_stride, d->states) ||
+      !good_stride(r->c_stride, d->states))
+    return DL_E_SHAPE;
+  return DL_OK;
+}
+
+SsmParams params(const dl_ssm_desc* d, const float* h_in, float* h_out, const dl_ssm_rows* r, int32_t n,
+                 int32_t tokens) {
+  SsmParams p{};
+  p.x = r->x;
+  p.dt = r->dt;
+  p.z = r->z;
+  p.Bm = r->B;
+  p.Cm = r->C;
+  p.x_stride = r->x_stride;
+  p.dt_stride = r->dt_stride;
+  p.z_stride = r->z_stride;
+  p.b_stride = r->b_stride;
+  p.c_stride = r->c_stride;
+  p.A = r->A;
+  p.skip = r->skip;
+  p.bias = r->dt_bias;
+  p.h_in = h_in;
+  p.h_out = h_out;
+  p.n = n;
+  p.N = tokens;
+  p.B = d->num_slots;
+  p.D = d->channels;
+  p.S = d->states;
+  p.blocks = blocks_of(d);
+  return p;
+}
+
+// Workspace, 256-byte aligned parts: E, sums (sequences in several stretches); backward F, then the
+// partial sums.
+struct Layout {
+  size_t E = 0, F = 0, sums = 0, part = 0, rows = 0, all = 0;
+};
+Layout layout(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
+  const int len = stretch_len(d, n, tokens, backward);
+  const size_t parts = size_t(stretches(n, tokens, len)), D = size_t(d->channels), S = size_t(d->states);
+  Layout l;
+  auto take = [&](size_t floats) {
+    const size_t at = l.all;
+    l.all += round256(floats * sizeof(float));
+    return at;
+  };
+  if (!whole(tokens, len)) {
+    l.E = take(parts * D * S);
+    l.sums = take(parts * D);
+    if (backward) l.F = take(parts * D * S);
+  }
+  if (backward) {
+    l.part = take(parts * D * (S + 2));
+    l.rows = take(size_t(blocks_of(d)) * size_t(tokens) * 2 * S);
+  }
+  return l;
+}
+
+void set_workspace(SsmParams& p, const dl_ssm_desc* d, const Layout& l, void* ws, bool backward) {
+  char* at = static_cast<char*>(ws);
+  p.len = stretch_len(d, p.n, p.N, backward);
+  if (!whole(p.N, p.len)) {
+    p.E = reinterpret_cast<float*>(at + l.E);
+    p.sums = reinterpret_cast<float*>(at + l.sums);
+    p.F = reinterpret_cast<float*>(at + l.F);
+  }
+  p.part = reinterpret_cast<float*>(at + l.part);
+  p.rows = reinterpret_cast<float*>(at + l.rows);
+}
+
+int check_workspace(const Layout& l, const void* ws, size_t bytes) {
+  if (l.all == 0) return DL_OK;
+  if (!ws) return DL_E_NULL;
+  if (!aligned_to(ws, 256)) return DL_E_ALIGN;
+  return bytes < l.all ? DL_E_SHAPE : DL_OK;
+}
+
+}  // namespace
+}  // namespace dl
+
+using namespace dl;
+
+extern "C" {
+
+int dl_ssm_step(const dl_ssm_desc* desc, const float* h_in, float* h_out, const dl_ssm_rows* rows, void* y,
+                const int32_t* slots, int32_t n, hipStream_t stream) {
+  DL_TRY(check_desc(desc));
+  if (n < 0 || n > desc->num_slots) return DL_E_SHAPE;
+  if (!grid_fits(int64_t(n) * ((int64_t(desc->channels) * desc->states + 1023) / 1024), 256)) return DL_E_SHAPE;
+  if (n == 0) return DL_OK;               // nothing to do, whatever the pointers are
+  if (!slots && n != desc->num_slots) return DL_E_SHAPE;
+  DL_TRY(check_rows(desc, rows, true));
+  if (!h_in || !h_out || !y) return DL_E_NULL;
+  if (!aligned_to(h_in, 16) || !aligned_to(h_out, 16) || !aligned_to(y, 16) || !aligned_to(slots, 4))
+    return DL_E_ALIGN;
+  SsmParams p = params(desc, h_in, h_out, rows, n, n);
+  p.y = y;
+  p.slots = slots;
+  return launch(STEP, desc, p, stream) == hipSuccess ? DL_OK : DL_E_HIP;
+}
+
+int dl_ssm_workspace_bytes(const dl_ssm_desc* desc, int32_t n, int32_t tokens, int32_t backward,
+                           size_t* bytes) {
+  DL_TRY(check_desc(desc));
+  DL_TRY(check_counts(desc, n, tokens, backward != 0));
+  DL_TRY(check_counts(desc, n, tokens, false));
+  if (!bytes) return DL_E_NULL;
+  *bytes = 0;
+  if (n == 0) return DL_OK;
+  *bytes = layout(desc, n, tokens, false).all;
+  if (backward) *bytes = std::max(*bytes, layout(desc, n, tokens, true).all);
+  return DL_OK;
+}
+
+int dl_ssm_prefill(const dl_ssm_desc* desc, const float* h_in, float* h_out, const dl_ssm_rows* rows, void* y,
+                   const dl_tables* tables, int32_t n, int32_t tokens, void* workspace,
+                   size_t workspace_bytes, hipStream_t stream) {
+  DL_TRY(check_desc(desc));
+  DL_TRY(check_counts(desc, n, tokens, false));
+  if (n == 0) return DL_OK;               // nothing to do, whatever the pointers are
+  DL_TRY(check_rows(desc, rows, tokens > 0));
+  DL_TRY(check_row_tables(tables));
+  const Layout l = layout(desc, n, tokens, false);
+  DL_TRY(check_workspace(l, workspace, workspace_bytes));
+  if (!h_out || (tokens > 0 && !y)) return DL_E_NULL;
+  if (!aligned_to(h_in, 16) || !aligned_to(h_out, 16) || !aligned_to(y, 16)) return DL_E_ALIGN;
+  SsmParams p = params(desc, h_in, h_out, rows, n, tokens);
+  p.y = y;
+  p.cu = tables->cu_tokens;
+  p.seq_slot = tables->seq_slot;
+  set_workspace(p, desc, l, workspace, false);
+  return launch(FORWARD, desc, p, stream) == hipSuccess ? DL_OK : DL_E_HIP;
+}
+
+int dl_ssm_backward(const dl_ssm_desc* desc, const float* h_in, const dl_ssm_rows* rows, const void* dy,
+                    const float* dh_out, const dl_ssm_grads* g, const dl_tables* tables, int32_t n,
+                    int32_t tokens, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  DL_TRY(check_desc(desc));
+  DL_TRY(check_counts(desc, n, tokens, true));
+  if (n == 0) return DL_OK;               // nothing to do, whatever the pointers are
+  DL_TRY(check_rows(desc, rows, tokens > 0));
+  DL_TRY(check_row_tables(tables));
+  if (!g || !g->dA || (rows->skip && !g->dskip) || (rows->dt_bias && !g->dbias)) return DL_E_NULL;
+  if (tokens > 0 && (!dy || !g->dx || !g->ddt || !g->dB || !g->dC || (rows->z && !g->dz))) return DL_E_NULL;
+  for (const void* v : {static_cast<const void*>(h_in), dy, static_cast<const void*>(dh_out),
+                        static_cast<const void*>(g->dx), static_cast<const void*>(g->ddt),
+                        static_cast<const void*>(g->dz), static_cast<const void*>(g->dB),
+                        static_cast<const void*>(g->dC), static_cast<const void*>(g->ds)})
+    if (!aligned_to(v, 16)) return DL_E_ALIGN;
+  if (!aligned_to(g->dA, 4) || !aligned_to(g->dskip, 4) || !aligned_to(g->dbias, 4)) return DL_E_ALIGN;
+  const Layout l = layout(desc, n, tokens, true);
+  DL_TRY(check_workspace(l, workspace, workspace_bytes));
+  SsmParams p = params(desc, h_in, g->ds, rows, n, tokens);
+  p.cu = tables->cu_tokens;
+  p.seq_slot = tables->seq_slot;
+  p.dy = dy;
+  p.dh_out = dh_out;
+  p.dx = g->dx;
+  p.ddt = g->ddt;
+  p.dz = g->dz;
+  p.dB = g->dB;
+  p.dC = g->dC;
+  set_workspace(p, desc, l, workspace, true);
+  hipError_t e = launch(BACKWARD, desc, p, stream);
+  const int64_t parts = stretches(n, tokens, p.len), D = p.D, S = p.S, row = D * (S + 2);
+  if (e == hipSuccess) e = launch_column_sum(p.part, parts, D * S, row, g->dA, stream);
+  if (e == hipSuccess && p.skip) e = launch_column_sum(p.part + D * S, parts, D, row, g->dskip, stream);
+  if (e == hipSuccess && p.bias) e = launch_column_sum(p.part + D * (S + 1), parts, D, row, g->dbias, stream);
+  return e == hipSuccess ? DL_OK : DL_E_HIP;
+}
+
+}  // extern "C"

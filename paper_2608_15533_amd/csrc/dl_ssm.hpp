@@ -1,0 +1,101 @@
+// Selective state space scan: formulas and pieces that its kernels share.
+//
+// A channel has S states.  With raw_t = dt_t + bias, d_t = softplus(raw_t), u_t = d_t x_t:
+//   h_t = a_t . h_{t-1} + u_t B_t,  a_t = e^{d_t A},   y_t = <C_t, h_t> + skip x_t,   out_t = y_t silu(z_t).
+// Over a stretch of tokens h = (e^{A sum d}) . h_before + E, E what the stretch leaves from zero states:
+// so all stretches of all sequences run at once for E, the states between them follow one by one
+// ("join"), and all run at once again for the outputs.
+// Backward, with w_t = d out_t silu(z_t) the gradient of y_t, G_t that of h_t:
+//   G_t = w_t C_t + a_{t+1} . G_{t+1};  with m_t = a_t . h_{t-1}:
+//   dB_t = sum over channels of G_t u_t,   dC_t = sum over channels of w_t h_t,
+//   dx_t = d_t <G_t, B_t> + skip w_t,      draw_t = sigmoid(raw_t) (<G_t, A m_t> + x_t <G_t, B_t>),
+//   dA = sum_t d_t G_t . m_t,  dskip = sum_t w_t x_t,  dbias = sum_t draw_t,  dz_t = dout_t y_t silu'(z_t).
+// The gradient before a stretch is e^{A sum d} . G_after + F, F = sum_t (a_first .. a_t) . C_t w_t.
+//
+// Work is split by channel over a wave's lanes and by state over a workgroup's waves, four states
+// each: B_t and C_t are the same for all lanes and come through scalar registers, sums over states
+// are in a lane but for the last step, and what a token needs of its channel (d, u) is formed once
+// and passed through LDS.  Bound by vector instructions: an exponential, two products and two
+// sums for every (token, channel, state).
+#pragma once
+
+#include "dl_rows.hpp"
+
+namespace dl {
+
+struct SsmParams {
+  const void *x, *dt, *z, *Bm, *Cm;
+  int64_t x_stride, dt_stride, z_stride, b_stride, c_stride;
+  const float *A, *skip, *bias;
+  const float* h_in;            // [B,D,S] or null
+  float* h_out;                 // [B,D,S] (backward: gradient of h_in, or null)
+  void* y;
+  const void* dy;               // backward
+  const float* dh_out;          // [B,D,S] or null
+  void *dx, *ddt, *dz;
+  void *dB, *dC;
+  const int32_t *cu, *seq_slot, *slots;
+  float *E, *F, *sums;          // [stretches][S/4][D][4] twice, [stretches][D]; null: sequences whole
+  float *part;                  // backward: [stretches][D*S + 2 D] partial sums of dA, dskip, dbias
+  float *rows;                  // backward: [blocks][N][2 S] partial sums of dB, dC
+  int32_t n, N, B, D, S, len, blocks;   // blocks: of 64 channels
+};
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+__device__ __forceinline__ float decay(float d, float a2) { return __builtin_amdgcn_exp2f(d * a2); }
+
+// log(1 + e^x) = max(x, 0) + log(1 + e), e = e^-|x|.  The power's exponent is -|x| log2 e with what its
+// rounding left out put back as a factor; log(1 + e) = 2 artanh(q), q = e / (2 + e) <= 1/3, by its
+// series through q^13 / 13 (the next term is 1.4e-8 of it): a few 2^-24 of the result, where 1 + e alone
+// would lose a small e.  Some 25 instructions; the library's two functions take 100.
+__device__ __forceinline__ float softplus(float x) {
+  const float hi = -fabsf(x) * LOG2E;
+  const float lo = fmaf(-fabsf(x), 1.92596303e-8f, fmaf(-fabsf(x), LOG2E, -hi));   // log2 e - LOG2E
+  float e = __builtin_amdgcn_exp2f(hi);
+  e = hi < -126.0f ? e : fmaf(e, lo * 0.69314718f, e);      // at -inf lo is none
+  const float q = e * __builtin_amdgcn_rcpf(2.0f + e), s = q * q;
+  float r = 1.0f / 13.0f;
+  r = fmaf(r, s, 1.0f / 11.0f);
+  r = fmaf(r, s, 1.0f / 9.0f);
+  r = fmaf(r, s, 1.0f / 7.0f);
+  r = fmaf(r, s, 1.0f / 5.0f);
+  r = fmaf(r, s, 1.0f / 3.0f);
+  r = fmaf(r * s, q, q);
+  return x > 20.0f ? x : fmaf(2.0f, r, fmaxf(x, 0.0f));
+}
+// 1 / (1 + e^-x), good to 2^-24 (|x| + 3) of itself.
+__device__ __forceinline__ float quick_sigmoid(float x) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -LOG2E));
+}
+
+// Four consecutive values of a row that is the same for all lanes, through scalar registers.
+template <typename T>
+struct Four;
+template <>
+struct Four<float> {
+  f32x4 v;
+  __device__ __forceinline__ void load(const float* p) {
+    typedef const __attribute__((address_space(4))) f32x4 scalar_t;
+    v = *(scalar_t*)(uintptr_t)p;
+  }
+  __device__ __forceinline__ float at(int i) const { return v[i]; }
+};
+template <>
+struct Four<uint16_t> {
+  typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+  u32x2 v;
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    typedef const __attribute__((address_space(4))) u32x2 scalar_t;
+    v = *(scalar_t*)(uintptr_t)p;
+  }
+  __device__ __forceinline__ float at(int i) const {
+    return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
+  }
+};
+
+__device__ __forceinline__ int wave_index() {
+  return __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+}
+
+}  // namespace dl

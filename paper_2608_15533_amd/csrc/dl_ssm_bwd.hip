@@ -1,0 +1,375 @@
+// Selective state space scan: the backward pass's kernels.
+#include "dl_ssm_bwd.hpp"
+
+namespace dl {
+namespace {
+
+// Tokens whose steps lie in LDS at a time, and whose decays and states a wave holds in registers: 8 (16
+// spill), or 4 where a workgroup of 16 waves leaves 128 registers a lane.
+template <int S>
+constexpr int tile_of = S == 64 ? 4 : 8;
+
+// A thread's part of a tile: one token, EV channels.
+template <int S, typename T>
+struct Part {
+  static constexpr int TB = tile_of<S>, NT = S * 16, EV = TB * 64 >= NT ? TB * 64 / NT : 1, CG = 64 / EV;
+  int te, ce, c;
+  bool live;                     // D is a multiple of 8: all EV channels or none
+  float bias[EV];
+  __device__ __forceinline__ Part(const SsmParams& p, int c0) {
+    te = threadIdx.x / CG;
+    ce = (threadIdx.x % CG) * EV;
+    c = c0 + ce;
+    live = c < p.D && te < TB;
+#pragma unroll
+    for (int e = 0; e < EV; ++e) bias[e] = p.bias && live ? p.bias[c + e] : 0.0f;
+  }
+  __device__ __forceinline__ Raw<EV, T> raw(const void* base, int64_t stride, int64_t row) const {
+    return load_raw<EV>(static_cast<const T*>(base) + row * stride + c);
+  }
+  __device__ __forceinline__ void load(const void* base, int64_t stride, int64_t row, float (&x)[EV]) const {
+    widen_row(raw(base, stride, row), x);
+  }
+};
+
+// E, F and the sum of d of a stretch, 64 channels; wave w has states 4 w .. 4 w + 3.
+template <int S, typename T>
+__global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
+  typedef Part<S, T> P;
+  constexpr int TB = P::TB, EV = P::EV;
+  __shared__ __attribute__((aligned(16))) float step[TB][64], input[TB][64], grad[TB][64];
+  const int f = blockIdx.x / p.blocks, c0 = int(blockIdx.x % p.blocks) * 64;
+  const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, f);
+  if (s.idle || (s.begins() && s.ends())) return;
+  const int lane = threadIdx.x & 63, w = wave_index(), c = c0 + lane;
+  const P part(p, c0);
+  float a2[4], h[4] = {}, g[4] = {}, decays[4], total[EV] = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a2[i] = c < p.D ? p.A[int64_t(c) * S + 4 * w + i] * LOG2E : 0.0f;
+    decays[i] = 1.0f;
+  }
+  const T* bp = static_cast<const T*>(p.Bm) + int64_t(s.first) * p.b_stride + 4 * w;
+  const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
+  for (int t0 = 0; t0 < s.count; t0 += TB) {
+    const int count = min(TB, s.count - t0);
+    if (part.te < TB) {
+      float x[EV] = {}, d[EV] = {}, up[EV] = {};
+      if (part.live && part.te < count) {
+        const int64_t row = int64_t(s.first) + t0 + part.te;
+        part.load(p.x, p.x_stride, row, x);
+        part.load(p.dt, p.dt_stride, row, d);
+        part.load(p.dy, p.D, row, up);
+#pragma unroll
+        for (int e = 0; e < EV; ++e) d[e] = softplus(d[e] + part.bias[e]);
+        if (p.z) {
+          float z[EV];
+          part.load(p.z, p.z_stride, row, z);
+#pragma unroll
+          for (int e = 0; e < EV; ++e) up[e] *= z[e] * quick_sigmoid(z[e]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < EV; ++e) {
+        step[part.te][part.ce + e] = d[e];
+        input[part.te][part.ce + e] = d[e] * x[e];
+        grad[part.te][part.ce + e] = up[e];
+        total[e] += d[e];
+      }
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int t = 0; t < count; ++t) {
+      Four<T> B, C;
+      B.load(bp + int64_t(t0 + t) * p.b_stride);
+      C.load(cp + int64_t(t0 + t) * p.c_stride);
+      const float d = step[t][lane], u = input[t][lane], up = grad[t][lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float a = decay(d, a2[i]);
+        h[i] = fmaf(a, h[i], u * B.at(i));
+        decays[i] *= a;
+        g[i] = fmaf(decays[i], up * C.at(i), g[i]);
+      }
+    }
+    __syncthreads();
+  }
+  if (c < p.D) {
+    const int64_t at = int64_t(f) * p.D * S + (int64_t(w) * p.D + c) * 4;
+    *reinterpret_cast<f32x4*>(p.E + at) = f32x4{h[0], h[1], h[2], h[3]};
+    *reinterpret_cast<f32x4*>(p.F + at) = f32x4{g[0], g[1], g[2], g[3]};
+  }
+  if (part.te < TB) {
+#pragma unroll
+    for (int e = 0; e < EV; ++e) step[part.te][part.ce + e] = total[e];
+  }
+  __syncthreads();
+  if (w == 0 && c < p.D) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < TB; ++t) sum += step[t][lane];
+    p.sums[int64_t(f) * p.D + c] = sum;
+  }
+}
+
+// Sums over the 64 lanes of eight values; lane l is left with number sum_number(l).
+__device__ __forceinline__ float eight_sums(const float (&v)[8]) {
+  float s[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[i] = halves_sum32(v[i], v[i + 4]);
+  return lanes_sum<8>(halves_sum8(halves_sum16(s[0], s[1]), halves_sum16(s[2], s[3])));
+}
+__device__ __forceinline__ int sum_number(int l) {
+  return 4 * (l >> 5) + 2 * ((l >> 3) & 1) + ((l >> 4) & 1);
+}
+
+// Every gradient of a stretch's tokens, 64 channels; wave w has states 4 w .. 4 w + 3.  The states
+// before every tile first (in LDS), then the tiles from the last to the first: a tile's decays a_t
+// and m_t = a_t . h_{t-1} in registers, then its tokens backwards.
+template <int S, typename T>
+__global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmParams p) {
+  typedef Part<S, T> P;
+  constexpr int TB = P::TB, EV = P::EV, NW = S / 4, TILES = ssm_grad_tokens(S) / TB;
+  __shared__ __attribute__((aligned(16))) float step[TB][64], input[TB][64], grad[TB][64];
+  __shared__ __attribute__((aligned(16))) float sum_gb[NW][TB][64], sum_gm[NW][TB][64], sum_ch[NW][TB][64];
+  __shared__ __attribute__((aligned(16))) f32x4 before[TILES][NW][64];
+  const int f = blockIdx.x / p.blocks, block = int(blockIdx.x % p.blocks), c0 = block * 64;
+  const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, f);
+  const int lane = threadIdx.x & 63, w = wave_index(), c = c0 + lane;
+  const bool live = c < p.D;
+  const P part(p, c0);
+  float dA[4] = {}, dskip[EV] = {}, dbias[EV] = {};
+  if (!s.idle) {
+    float a2[4], h[4] = {}, g[4] = {}, A[4], skip[EV];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      A[i] = live ? p.A[int64_t(c) * S + 4 * w + i] : 0.0f;
+      a2[i] = A[i] * LOG2E;
+    }
+#pragma unroll
+    for (int e = 0; e < EV; ++e) skip[e] = p.skip && part.live ? p.skip[part.c + e] : 0.0f;
+    const int64_t state = (int64_t(s.slot) * p.D + c) * S + 4 * w;
+    const int64_t at = int64_t(f) * p.D * S + (int64_t(w) * p.D + c) * 4;
+    const float* hp = p.E ? p.E + at : p.h_in ? p.h_in + state : nullptr;
+    const float* gp = p.E ? p.F + at : p.dh_out ? p.dh_out + state : nullptr;
+    if (live && hp) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(hp);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = v[i];
+    }
+    if (live && gp) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(gp);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = v[i];
+    }
+    const T* bp = static_cast<const T*>(p.Bm) + int64_t(s.first) * p.b_stride + 4 * w;
+    const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
+    const int tiles = (s.count + TB - 1) / TB;
+    for (int j = 0; j < tiles; ++j) {
+      before[j][w][lane] = f32x4{h[0], h[1], h[2], h[3]};
+      if (j + 1 == tiles) break;
+      if (part.te < TB) {
+        float x[EV] = {}, d[EV] = {};
+        if (part.live) {
+          const int64_t row = int64_t(s.first) + j * TB + part.te;
+          part.load(p.x, p.x_stride, row, x);
+          part.load(p.dt, p.dt_stride, row, d);
+#pragma unroll
+          for (int e = 0; e < EV; ++e) d[e] = softplus(d[e] + part.bias[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < EV; ++e) {
+          step[part.te][part.ce + e] = d[e];
+          input[part.te][part.ce + e] = d[e] * x[e];
+        }
+      }
+      __syncthreads();
+#pragma unroll 4
+      for (int t = 0; t < TB; ++t) {
+        Four<T> B;
+        B.load(bp + int64_t(j * TB + t) * p.b_stride);
+        const float d = step[t][lane], u = input[t][lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = fmaf(decay(d, a2[i]), h[i], u * B.at(i));
+      }
+      __syncthreads();
+    }
+    for (int j = tiles - 1; j >= 0; --j) {
+      const int t0 = j * TB, count = min(TB, s.count - t0);
+      const bool mine = part.live && part.te < count;
+      const int64_t row = int64_t(s.first) + t0 + part.te;
+      // Rows as they are stored stay in registers; what they stand for is formed again behind the tile.
+      Raw<EV, T> rx{}, rd{}, ro{}, rz{};
+      if (mine) {
+        rx = part.raw(p.x, p.x_stride, row);
+        rd = part.raw(p.dt, p.dt_stride, row);
+        ro = part.raw(p.dy, p.D, row);
+        if (p.z) rz = part.raw(p.z, p.z_stride, row);
+      }
+      if (part.te < TB) {
+#pragma unroll
+        for (int e = 0; e < EV; ++e) {
+          const float d = mine ? softplus(widen(rd.v[e]) + part.bias[e]) : 0.0f, z = widen(rz.v[e]);
+          step[part.te][part.ce + e] = d;
+          input[part.te][part.ce + e] = d * widen(rx.v[e]);
+          grad[part.te][part.ce + e] = widen(ro.v[e]) * (p.z ? z * quick_sigmoid(z) : 1.0f);
+        }
+      }
+      __syncthreads();
+      float a[TB][4], m[TB][4];
+      {
+        const f32x4 v = before[j][w][lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = v[i];
+      }
+#pragma unroll
+      for (int t = 0; t < TB; ++t) {
+        if (t < count) {
+          Four<T> B;
+          B.load(bp + int64_t(t0 + t) * p.b_stride);
+          const float dd = step[t][lane], u = input[t][lane];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            a[t][i] = decay(dd, a2[i]);
+            m[t][i] = a[t][i] * h[i];
+            h[i] = fmaf(u, B.at(i), m[t][i]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);     // one token's operands at a time: registers
+      }
+      float kept = 0.0f;
+#pragma unroll
+      for (int t = TB - 1; t >= 0; --t) {
+        if (t < count) {
+          Four<T> B, C;
+          B.load(bp + int64_t(t0 + t) * p.b_stride);
+          C.load(cp + int64_t(t0 + t) * p.c_stride);
+          const float dd = step[t][lane], u = input[t][lane], v = grad[t][lane];
+          float gb = 0.0f, gm = 0.0f, ch = 0.0f, over[8];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float b = B.at(i), cc = C.at(i);
+            g[i] = fmaf(v, cc, g[i]);
+            const float ht = fmaf(u, b, m[t][i]), x0 = g[i] * m[t][i];
+            gb = fmaf(g[i], b, gb);
+            gm = fmaf(x0, A[i], gm);
+            ch = fmaf(cc, ht, ch);
+            dA[i] = fmaf(x0, dd, dA[i]);
+            over[i] = g[i] * u;
+            over[4 + i] = ht * v;
+            g[i] *= a[t][i];
+          }
+          sum_gb[w][t][lane] = gb;
+          sum_gm[w][t][lane] = gm;
+          if (p.z) sum_ch[w][t][lane] = ch;
+          const float one = eight_sums(over);
+          if ((lane & 7) == (t & 7)) kept = one;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if ((t & 7) == 0) {
+          const int tt = t + (lane & 7), k = sum_number(lane);   // numbers 0-3: B's states, 4-7: C's
+          if (tt < count)
+            p.rows[(int64_t(block) * p.N + s.first + t0 + tt) * (2 * S) + (k >> 2) * S + 4 * w + (k & 3)] = kept;
+        }
+      }
+      __syncthreads();
+      if (mine) {
+        float dx[EV], ddt[EV], dz[EV];
+#pragma unroll
+        for (int e = 0; e < EV; ++e) {
+          float gb = 0.0f, gm = 0.0f, ch = 0.0f;
+          __builtin_amdgcn_sched_barrier(0);     // not all partial sums at once: registers
+#pragma unroll 4
+          for (int i = 0; i < NW; ++i) {
+            gb += sum_gb[i][part.te][part.ce + e];
+            gm += sum_gm[i][part.te][part.ce + e];
+            if (p.z) ch += sum_ch[i][part.te][part.ce + e];
+          }
+          const float x = widen(rx.v[e]), z = widen(rz.v[e]), sz = quick_sigmoid(z);
+          const float up = grad[part.te][part.ce + e];
+          dx[e] = fmaf(step[part.te][part.ce + e], gb, skip[e] * up);
+          ddt[e] = quick_sigmoid(widen(rd.v[e]) + part.bias[e]) * fmaf(x, gb, gm);
+          dskip[e] = fmaf(up, x, dskip[e]);
+          dbias[e] += ddt[e];
+          dz[e] = widen(ro.v[e]) * fmaf(skip[e], x, ch) * sz * (1.0f + z * (1.0f - sz));
+        }
+        store_row<EV>(static_cast<T*>(p.dx) + row * p.D + part.c, dx);
+        store_row<EV>(static_cast<T*>(p.ddt) + row * p.D + part.c, ddt);
+        if (p.z) store_row<EV>(static_cast<T*>(p.dz) + row * p.D + part.c, dz);
+      }
+      // What a thread reads of step and grad here, it alone writes in the next tile.
+    }
+    if (s.begins() && p.h_out && live)
+      *reinterpret_cast<f32x4*>(p.h_out + state) = f32x4{g[0], g[1], g[2], g[3]};
+  }
+  // Partial sums over the stretch; an idle one adds zeros.
+  float* sums = p.part + int64_t(f) * p.D * (S + 2);
+  if (live) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[int64_t(c) * S + 4 * w + i] = dA[i];
+  }
+  __syncthreads();
+  if (part.te < TB) {
+#pragma unroll
+    for (int e = 0; e < EV; ++e) {
+      step[part.te][part.ce + e] = dskip[e];
+      input[part.te][part.ce + e] = dbias[e];
+    }
+  }
+  __syncthreads();
+  if (w == 0 && live) {
+    float a = 0.0f, b = 0.0f;
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+      a += step[t][lane];
+      b += input[t][lane];
+    }
+    sums[int64_t(p.D) * S + c] = a;
+    sums[int64_t(p.D) * (S + 1) + c] = b;
+  }
+}
+
+// dB and dC of a stretch's tokens: the sums over blocks of channels, in their order.
+template <int S, typename T>
+__global__ __launch_bounds__(256) void ssm_rows_kernel(SsmParams p) {
+  const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, blockIdx.x);
+  if (s.idle) return;
+  for (int i = threadIdx.x; i < s.count * 2 * S; i += 256) {
+    const int64_t row = int64_t(s.first) + i / (2 * S);
+    const int k = i % (2 * S);
+    float sum = 0.0f;
+    for (int b = 0; b < p.blocks; ++b) sum += p.rows[(int64_t(b) * p.N + row) * (2 * S) + k];
+    narrow(static_cast<T*>(k < S ? p.dB : p.dC) + row * S + k % S, sum);
+  }
+}
+
+template <int S, typename T>
+hipError_t launch_grad(const SsmParams& p, hipStream_t s) {
+  const int64_t parts = stretches(p.n, p.N, p.len);
+  hipError_t e = start_rows(&ssm_grad_kernel<S, T>, parts * p.blocks, S * 16, p, s);
+  if (e == hipSuccess) e = start_rows(&ssm_rows_kernel<S, T>, parts, 256, p, s);
+  return e;
+}
+template <int S, typename T>
+hipError_t launch_ends(const SsmParams& p, hipStream_t s) {
+  return start_rows(&ssm_ends_kernel<S, T>, stretches(p.n, p.N, p.len) * p.blocks, S * 16, p, s);
+}
+
+}  // namespace
+
+hipError_t launch_ssm_ends(int states, bool bf16, const SsmParams& p, hipStream_t s) {
+  switch (states) {
+    case 16: return bf16 ? launch_ends<16, uint16_t>(p, s) : launch_ends<16, float>(p, s);
+    case 32: return bf16 ? launch_ends<32, uint16_t>(p, s) : launch_ends<32, float>(p, s);
+    default: return bf16 ? launch_ends<64, uint16_t>(p, s) : launch_ends<64, float>(p, s);
+  }
+}
+hipError_t launch_ssm_grad(int states, bool bf16, const SsmParams& p, hipStream_t s) {
+  switch (states) {
+    case 16: return bf16 ? launch_grad<16, uint16_t>(p, s) : launch_grad<16, float>(p, s);
+    case 32: return bf16 ? launch_grad<32, uint16_t>(p, s) : launch_grad<32, float>(p, s);
+    default: return bf16 ? launch_grad<64, uint16_t>(p, s) : launch_grad<64, float>(p, s);
+  }
+}
+
+}  // namespace dl

@@ -54,7 +54,8 @@ EXPORTED = ("dl_eager_step", "dl_append_step", "dl_merge", "dl_readout",
             "dl_chunk_tables", "dl_prefill_workspace_bytes", "dl_prefill",
             "dl_prefill_backward",
             "dl_conv_step", "dl_conv_prefill", "dl_conv_workspace_bytes", "dl_conv_backward",
-            "dl_qk_norm", "dl_qk_workspace_bytes", "dl_qk_norm_backward")
+            "dl_qk_norm", "dl_qk_workspace_bytes", "dl_qk_norm_backward",
+            "dl_ssm_step", "dl_ssm_prefill", "dl_ssm_workspace_bytes", "dl_ssm_backward")
 
 
 class dl_desc(ctypes.Structure):
@@ -118,6 +119,23 @@ class dl_qk_grads(ctypes.Structure):
     _fields_ = [(k, ctypes.c_void_p) for k in ("dq", "dk", "dwq", "dwk")]
 
 
+class dl_ssm_desc(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("abi_version", "num_slots", "channels", "states",
+                                              "in_dtype")]
+
+
+class dl_ssm_rows(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("x", "dt", "z", "B", "C")]
+    _fields_ += [(k, ctypes.c_int64) for k in ("x_stride", "dt_stride", "z_stride", "b_stride",
+                                               "c_stride")]
+    _fields_ += [(k, ctypes.c_void_p) for k in ("A", "skip", "dt_bias")]
+
+
+class dl_ssm_grads(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("dx", "ddt", "dz", "dB", "dC", "dA", "dskip",
+                                               "dbias", "ds")]
+
+
 _P = ctypes.c_void_p
 _lib.dl_eager_step.argtypes = [ctypes.POINTER(dl_desc), _P, ctypes.POINTER(dl_token), _P, _P,
                                ctypes.c_int32, _P]
@@ -157,11 +175,18 @@ _lib.dl_qk_norm.argtypes = [_PTR(dl_qk_desc), _PTR(dl_qk_rows), _P, _P, _I, _P]
 _lib.dl_qk_workspace_bytes.argtypes = [_PTR(dl_qk_desc), _I, _PTR(_SIZE)]
 _lib.dl_qk_norm_backward.argtypes = [_PTR(dl_qk_desc), _PTR(dl_qk_rows), _P, _P, _PTR(dl_qk_grads),
                                      _I, _P, _SIZE, _P]
+_lib.dl_ssm_step.argtypes = [_PTR(dl_ssm_desc), _P, _P, _PTR(dl_ssm_rows), _P, _P, _I, _P]
+_lib.dl_ssm_workspace_bytes.argtypes = [_PTR(dl_ssm_desc), _I, _I, _I, _PTR(_SIZE)]
+_lib.dl_ssm_prefill.argtypes = [_PTR(dl_ssm_desc), _P, _P, _PTR(dl_ssm_rows), _P, _PTR(dl_tables),
+                                _I, _I, _P, _SIZE, _P]
+_lib.dl_ssm_backward.argtypes = [_PTR(dl_ssm_desc), _P, _PTR(dl_ssm_rows), _P, _P,
+                                 _PTR(dl_ssm_grads), _PTR(dl_tables), _I, _I, _P, _SIZE, _P]
 for _f in ("dl_eager_step", "dl_append_step", "dl_merge", "dl_readout", "dl_append_step_tiled",
            "dl_tiled_workspace_bytes", "dl_abi_version", "dl_append_step_tiled_noalloc",
            "dl_chunk_tables", "dl_prefill_workspace_bytes", "dl_prefill",
            "dl_prefill_backward", "dl_conv_step", "dl_conv_prefill", "dl_conv_workspace_bytes",
-           "dl_conv_backward", "dl_qk_norm", "dl_qk_workspace_bytes", "dl_qk_norm_backward"):
+           "dl_conv_backward", "dl_qk_norm", "dl_qk_workspace_bytes", "dl_qk_norm_backward",
+           "dl_ssm_step", "dl_ssm_workspace_bytes", "dl_ssm_prefill", "dl_ssm_backward"):
     getattr(_lib, _f).restype = ctypes.c_int
 _lib.dl_status_str.argtypes = [ctypes.c_int]
 _lib.dl_status_str.restype = ctypes.c_char_p
@@ -763,3 +788,98 @@ def dl_qk_norm_backward(desc, rows, dq_out, dk_out, grads, workspace, stream=Non
     _check(_lib.dl_qk_norm_backward(ctypes.byref(desc), ctypes.byref(rows.struct), _ptr(dq_out),
                                     _ptr(dk_out), ctypes.byref(grads.struct), rows.n, wp, wn,
                                     _stream(stream)), "dl_qk_norm_backward")
+
+
+def make_ssm_desc(B, channels, states, in_dtype="bf16"):
+    """dl_ssm_desc of a selective scan: ``states`` (16, 32 or 64) states a channel, B slots."""
+    return dl_ssm_desc(DL_ABI_VERSION, B, channels, states, DTYPE_IDS[in_dtype])
+
+
+def _ssm_state(desc):
+    return torch.float32, (desc.num_slots, desc.channels, desc.states)
+
+
+class SsmRows:
+    """What a selective scan reads: token rows x, dt and z (or None: no gate) [n,D], Bm and Cm [n,S]
+    in the input dtype (columns of a wider tensor will do); A [D,S], skip [D] and dt_bias [D] (or
+    None) in fp32."""
+
+    def __init__(self, desc, n, x, dt, A, Bm, Cm, skip=None, dt_bias=None, z=None):
+        D, S, it = desc.channels, desc.states, _in_torch_dtype(desc)
+        strides = [_need_rows(x, "x", it, (n, D)), _need_rows(dt, "dt", it, (n, D)),
+                   0 if z is None else _need_rows(z, "z", it, (n, D)),
+                   _need_rows(Bm, "Bm", it, (n, S)), _need_rows(Cm, "Cm", it, (n, S))]
+        _need(A, "A", torch.float32, (D, S))
+        _optional(skip, "skip", torch.float32, (D,))
+        _optional(dt_bias, "dt_bias", torch.float32, (D,))
+        self.n, self.sizes = n, _sizes(desc)
+        self.tensors = (x, dt, z, Bm, Cm, A, skip, dt_bias)
+        self.struct = dl_ssm_rows(_ptr(x), _ptr(dt), _ptr(z), _ptr(Bm), _ptr(Cm), *strides, _ptr(A),
+                                  _ptr(skip), _ptr(dt_bias))
+
+
+class SsmGrads:
+    """Device buffers for the gradients of one dl_ssm_prefill call; ``h``: the states before (None:
+    no gradient of them)."""
+
+    def __init__(self, desc, rows, h=None):
+        like = lambda t: None if t is None else torch.zeros(t.shape, dtype=t.dtype,  # noqa: E731
+                                                            device=t.device)
+        (self.dx, self.ddt, self.dz, self.dB, self.dC, self.dA, self.dskip,
+         self.dbias) = map(like, rows.tensors)
+        _optional(h, "h", *_ssm_state(desc))
+        self.ds = like(h)
+        self.n, self.sizes = rows.n, rows.sizes
+        self.given = tuple(t is not None for t in rows.tensors)
+        self.slots = None if h is None else desc.num_slots
+        self.struct = dl_ssm_grads(*map(_ptr, (self.dx, self.ddt, self.dz, self.dB, self.dC, self.dA,
+                                               self.dskip, self.dbias, self.ds)))
+
+
+def dl_ssm_step(desc, h_in, h_out, rows, y, slots=None, stream=None):
+    """One token per slot through the scan: y [n,D], and the slots' new states from h_in [B,D,S] to
+    h_out (may be h_in)."""
+    sp, n = _rows(desc, slots, rows.n)
+    _made_for(desc, rows)
+    _need(h_in, "h_in", *_ssm_state(desc))
+    _need(h_out, "h_out", *_ssm_state(desc))
+    _need(y, "y", _in_torch_dtype(desc), (n, desc.channels))
+    _on_current_device(*rows.tensors, h_in, h_out, y, slots)
+    _check(_lib.dl_ssm_step(ctypes.byref(desc), _ptr(h_in), _ptr(h_out), ctypes.byref(rows.struct),
+                            _ptr(y), sp, n, _stream(stream)), "dl_ssm_step")
+
+
+def ssm_workspace(desc, n, tokens, backward=False, device="cuda"):
+    """A device buffer of the size dl_ssm_workspace_bytes names: for dl_ssm_prefill (with
+    ``backward``: and dl_ssm_backward)."""
+    size = _bytes(_lib.dl_ssm_workspace_bytes, "dl_ssm_workspace_bytes", desc, int(n), int(tokens),
+                  int(bool(backward)))
+    return torch.empty((size,), dtype=torch.uint8, device=device)
+
+
+def dl_ssm_prefill(desc, h_in, h_out, rows, y, tables, workspace, stream=None):
+    """The scan over the whole sequences of ``tables``, from h_in[slot] (None: zeros) to h_out[slot]
+    (may be h_in), y [N,D] in the input dtype."""
+    _made_for(desc, rows, tables)
+    _optional(h_in, "h_in", *_ssm_state(desc))
+    _need(h_out, "h_out", *_ssm_state(desc))
+    _need(y, "y", _in_torch_dtype(desc), (rows.n, desc.channels))
+    wp, wn = _workspace(workspace, "ssm_workspace")
+    _on_current_device(*rows.tensors, h_in, h_out, y, tables.err, workspace)
+    _check(_lib.dl_ssm_prefill(ctypes.byref(desc), _ptr(h_in), _ptr(h_out), ctypes.byref(rows.struct),
+                               _ptr(y), ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,
+                               _stream(stream)), "dl_ssm_prefill")
+
+
+def dl_ssm_backward(desc, h_in, rows, dy, dh_out, grads, tables, workspace, stream=None):
+    """Gradients of dl_ssm_prefill into ``grads`` (``SsmGrads``) from dy [N,D] and dh_out [B,D,S]
+    (None: zero).  The forward call must have left h_in as it was."""
+    _made_for(desc, rows, tables, grads)
+    _optional(h_in, "h_in", *_ssm_state(desc))
+    _optional(dh_out, "dh_out", *_ssm_state(desc))
+    _need(dy, "dy", _in_torch_dtype(desc), (rows.n, desc.channels))
+    wp, wn = _workspace(workspace, "ssm_workspace")
+    _on_current_device(*rows.tensors, h_in, dy, dh_out, grads.dx, grads.ds, tables.err, workspace)
+    _check(_lib.dl_ssm_backward(ctypes.byref(desc), _ptr(h_in), ctypes.byref(rows.struct), _ptr(dy),
+                                _ptr(dh_out), ctypes.byref(grads.struct), ctypes.byref(tables.struct),
+                                tables.n, tables.tokens, wp, wn, _stream(stream)), "dl_ssm_backward")

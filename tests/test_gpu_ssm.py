@@ -1,0 +1,150 @@
+"""The selective scan against 64 bits: prompts, training, single tokens, as it is used."""
+
+import pytest
+import torch
+
+import layer_harness as L
+import layer_reference as R
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+TYPES = pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+STATES = pytest.mark.parametrize("S", [16, 32, 64])
+
+
+@TYPES
+@STATES
+@pytest.mark.parametrize("lens,spare,D", [
+    ([1], 0, 8), ([2, 0, 1, 3], 0, 64), ([0, 0, 5], 3, 72), ([15, 16, 17, 63, 64, 65], 0, 136),
+    ([0], 4, 8), ([129, 3, 0, 200], 5, 200)], ids=str)
+def test_sequences(dtype, S, lens, spare, D):
+    x = R.ssm_inputs(lens, D, S, dtype, B=len(lens) + 1, seed=S, spare=spare)
+    L.check(L.run("ssm", x), R.ssm_expected(x))
+
+
+@TYPES
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("skip", [False, True])
+@pytest.mark.parametrize("bias", [False, True])
+def test_what_may_be_left_out(dtype, gate, skip, bias):
+    x = R.ssm_inputs([40, 0, 70], 72, 16, dtype, gate, skip, bias, seed=1, spare=2)
+    L.check(L.run("ssm", x), R.ssm_expected(x))
+
+
+@TYPES
+@pytest.mark.parametrize("step", [-6.0, 3.0, 30.0])
+def test_steps_that_keep_and_that_forget(dtype, step):
+    """Steps of 0.002 and of 3 and, past the softplus' straight part, of 30."""
+    x = R.ssm_inputs([150, 90], 64, 16, dtype, seed=2, step=step)
+    L.check(L.run("ssm", x), R.ssm_expected(x))
+
+
+@TYPES
+@STATES
+def test_rows_of_a_wider_tensor(dtype, S):
+    x = R.ssm_inputs([70, 7], 72, S, dtype, seed=3, spare=1)
+    L.check(L.run("ssm", x, strided=True), R.ssm_expected(x))
+
+
+@TYPES
+def test_no_initial_states_and_no_gradient_of_the_final_ones(dtype):
+    x = R.ssm_inputs([100, 0, 2], 64, 16, dtype, seed=4)
+    want = R.ssm_expected(x, zero_start=True, final_grad=False)
+    L.check(L.run("ssm", x, zero_start=True, final_grad=False), want)
+    c = L.Packed("ssm", x, zero_start=True)
+    c.grads = c.D.SsmGrads(c.desc, c.rows)                 # and none of the initial states wanted
+    c.build()
+    c.forward()
+    c.backward(False)
+    want["grads"].pop("s")
+    L.check(c, want)
+
+
+@pytest.mark.parametrize("lens,D", [([700], 64), ([1500, 3], 8), ([5] * 300, 16), ([300, 40], 1032)], ids=str)
+def test_long_and_many_and_wide(lens, D):
+    """Stretches joined over long sequences, many sequences, many blocks of channels."""
+    x = R.ssm_inputs(lens, D, 16, F32, seed=5, step=-3.0)
+    L.check(L.run("ssm", x), R.ssm_expected(x))
+
+
+@TYPES
+@STATES
+def test_single_tokens_follow_the_sequence(dtype, S):
+    from paper_2608_15533_amd import deltalog as D
+    lens = [9, 5, 0, 1]
+    x = R.ssm_inputs(lens, 136, S, dtype, B=6, seed=6)
+    c = L.run("ssm", x, backward=False)
+    want = R.ssm_expected(x, grads=False)
+    s, y, at = c.x["s"].clone(), torch.full_like(c.y, L.FILL), [0, 9, 14, 14]
+    for t in range(9):
+        live = [i for i in range(4) if t < lens[i]]
+        pick = [at[i] + t for i in live]
+        r = {k: c.x[k][pick].contiguous() for k in ("x", "dt", "B", "C", "z")}
+        slots = torch.tensor([x["slots"][i] for i in live], dtype=torch.int32, device="cuda")
+        rows = D.SsmRows(c.desc, len(live), L.wide(r["x"]), r["dt"], c.x["A"], L.wide(r["B"]), r["C"],
+                         c.x["skip"], c.x["bias"], r["z"])
+        out = torch.empty_like(r["x"])
+        D.dl_ssm_step(c.desc, s, s, rows, out, slots=slots)
+        y[pick] = out
+    assert R.rel(y, want["out"][0]) <= R.tol("ssm", dtype)
+    assert R.rel(s[x["slots"]], want["out"][1][x["slots"]]) <= R.TOL["ssm"]
+    rest = [i for i in range(6) if i not in x["slots"]]
+    assert torch.equal(s[rest], c.x["s"][rest])
+
+
+def test_step_leaves_slots_that_do_not_exist():
+    from paper_2608_15533_amd import deltalog as D
+    x = L.device(R.ssm_inputs([3], 64, 16, F32, B=3, seed=7))
+    desc = D.make_ssm_desc(3, 64, 16, "f32")
+    s, y = torch.full_like(x["s"], L.FILL), torch.full((3, 64), L.FILL, device="cuda")
+    rows = D.SsmRows(desc, 3, x["x"], x["dt"], x["A"], x["B"], x["C"])
+    D.dl_ssm_step(desc, x["s"], s, rows, y, slots=torch.tensor([2, -1, 3], dtype=torch.int32, device="cuda"))
+    assert torch.all(y[1:] == L.FILL) and torch.all(s[:2] == L.FILL)
+    assert not torch.any(y[0] == L.FILL) and not torch.any(s[2] == L.FILL)
+
+
+@pytest.mark.parametrize("lens", [[70, 1, 0, 33], [900, 20]], ids=str)
+def test_in_place_and_again(lens):
+    x = R.ssm_inputs(lens, 264, 16, BF16, seed=8)
+    c = L.run("ssm", x)
+    first = {k: v.clone() for k, v in c.results().items()}
+    c.ws.fill_(0xff)
+    c.forward()
+    c.backward()
+    assert all(torch.equal(v, first[k]) for k, v in c.results().items())
+    c.s_in = c.x["s"].clone()
+    c.forward(c.s_in)
+    assert torch.equal(c.s_in, first["s"]) and torch.equal(c.y, first["y"])
+
+
+def test_not_a_number_stays_in_its_sequence_and_channel():
+    """Of x, dt, z and the gradient; B and C are every channel's, of their sequence alone."""
+    x = R.ssm_inputs([150, 100, 80], 136, 16, F32, seed=9)
+    clean = L.run("ssm", x)
+    x["x"][160, 3], x["dt"][200, 70], x["z"][170, 5] = float("nan"), float("inf"), float("nan")
+    bad = L.run("ssm", x)
+    for k in ("y", "dx", "ddt", "dz"):
+        a, b = clean.results()[k].clone(), bad.results()[k].clone()
+        a[150:250, [3, 70, 5]] = b[150:250, [3, 70, 5]] = 0
+        assert torch.equal(a, b), k
+    x["B"][155, 2], x["C"][300, 1] = float("nan"), float("inf")
+    bad = L.run("ssm", x)
+    for k in ("y", "dx", "ddt", "dz", "dB", "dC"):
+        assert torch.equal(clean.results()[k][:150], bad.results()[k][:150]), k
+
+
+def test_bad_slots_are_skipped():
+    x = R.ssm_inputs([20, 130, 40], 64, 16, F32, seed=10)
+    x["slots"] = [2, 0, 1]
+    want = R.ssm_expected(x)
+    c = L.Packed("ssm", x)
+    c.slots[1] = 9
+    c.build()
+    c.forward()
+    c.backward()
+    assert c.tables.err.item() == 1
+    for got, ref in ((c.y, want["out"][0]), (c.grads.dx, want["grads"]["x"]), (c.grads.dB, want["grads"]["B"])):
+        assert R.rel(got[:20], ref[:20]) <= R.TOL["ssm"] and R.rel(got[150:], ref[150:]) <= R.TOL["ssm"]
+    assert torch.all(c.y[20:150] == L.FILL) and torch.all(c.s_out[0] == L.FILL)
+    assert torch.all(c.grads.dx[20:150] == 0) and torch.all(c.grads.dC[20:150] == 0)
