@@ -1,5 +1,6 @@
-"""Differentiable whole-sequence recurrence: ``dl_prefill`` and ``dl_prefill_backward`` as one
-torch.autograd function, for training a layer's projections through it."""
+"""Differentiable whole-sequence operators, for training a layer's projections through them:
+``delta_scan`` (``dl_prefill`` and ``dl_prefill_backward`` as one torch.autograd function),
+``short_conv``, ``selective_scan`` and ``qk_norm`` likewise."""
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -58,3 +59,132 @@ def delta_scan(op, q, k, v, lam=None, beta=None, u=None, S0=None, lens=None, sta
     return _Scan.apply(desc, tables, q, k, v, None if ids == D.DL_OP_LINATTN else lam,
                        beta if ids in D.DELTA_OP_IDS else None,
                        u if ids == D.DL_OP_RWKV6 else None, S0)
+
+def _batch(x, lens):
+    """(tables of the packed rows x, their sequences): ``lens`` [n] int32 on the device, None (one
+    sequence of all rows) or tables that the caller has built for these rows already."""
+    N = x.shape[0]
+    if isinstance(lens, D.ChunkTables):
+        return lens, lens.num_slots
+    if lens is None:
+        lens = torch.full((1,), N, dtype=torch.int32, device=x.device)
+    tables = D.ChunkTables(lens.numel(), N, device=x.device)
+    D.dl_chunk_tables(lens, tables)
+    return tables, lens.numel()
+
+
+def _type(x, name):
+    in_dtype = {torch.bfloat16: "bf16", torch.float32: "f32"}.get(x.dtype)
+    if in_dtype is None:
+        raise ValueError(f"{name}: dtype {x.dtype}, expected bf16 or fp32")
+    return in_dtype
+
+
+def _dense(t):
+    return None if t is None else t.contiguous()
+
+
+class _Conv(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, desc, tables, x, w, bias, s):
+        rows = D.ConvRows(desc, tables.tokens, x, w, bias)
+        y = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.zeros((desc.num_slots, desc.width - 1, desc.channels), dtype=x.dtype, device=x.device)
+        D.dl_conv_prefill(desc, s, out, rows, y, tables)
+        ctx.desc, ctx.tables = desc, tables
+        ctx.save_for_backward(x, w, bias, s)
+        return y, out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, ds):
+        x, w, bias, s = ctx.saved_tensors
+        desc, tables = ctx.desc, ctx.tables
+        rows = D.ConvRows(desc, tables.tokens, x, w, bias)
+        grads = D.ConvGrads(desc, rows, s)
+        ws = D.conv_workspace(desc, tables.n, tables.tokens, device=x.device)
+        D.dl_conv_backward(desc, s, rows, dy.contiguous(), _dense(ds), grads, tables, ws)
+        return None, None, grads.dx, grads.dw, grads.dbias, grads.ds
+
+
+def short_conv(x, w, bias=None, s0=None, lens=None, activation="silu"):
+    """The short causal convolution of every channel over packed sequences.
+
+    x [N,D] in bf16 or fp32 (columns of a wider tensor will do), w [D,W] and bias [D] in fp32; lens [n]
+    int32 on the device (None: one sequence), or ``ChunkTables`` of the batch; s0 [n,W-1,D] the inputs
+    before each sequence (None: zeros).  Returns (y [N,D], the last W - 1 inputs [n,W-1,D]); y and its
+    gradients are 0 in rows behind the last sequence.  Gradients once; a call keeps its inputs and
+    nothing else."""
+    tables, n = _batch(x, lens)
+    desc = D.make_conv_desc(n, x.shape[1], w.shape[1], _type(x, "x"), activation)
+    return _Conv.apply(desc, tables, x, w, bias, s0)
+
+
+class _Ssm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, desc, tables, x, dt, A, Bm, Cm, skip, dt_bias, z, h0):
+        rows = D.SsmRows(desc, tables.tokens, x, dt, A, Bm, Cm, skip, dt_bias, z)
+        y = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
+        h = torch.zeros((desc.num_slots, desc.channels, desc.states), device=x.device)
+        ws = D.ssm_workspace(desc, tables.n, tables.tokens, device=x.device)
+        D.dl_ssm_prefill(desc, h0, h, rows, y, tables, ws)
+        ctx.desc, ctx.tables = desc, tables
+        ctx.save_for_backward(x, dt, A, Bm, Cm, skip, dt_bias, z, h0)
+        return y, h
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh):
+        x, dt, A, Bm, Cm, skip, dt_bias, z, h0 = ctx.saved_tensors
+        desc, tables = ctx.desc, ctx.tables
+        rows = D.SsmRows(desc, tables.tokens, x, dt, A, Bm, Cm, skip, dt_bias, z)
+        g = D.SsmGrads(desc, rows, h0)
+        ws = D.ssm_workspace(desc, tables.n, tables.tokens, backward=True, device=x.device)
+        D.dl_ssm_backward(desc, h0, rows, dy.contiguous(), _dense(dh), g, tables, ws)
+        return (None, None, g.dx, g.ddt, g.dA, g.dB, g.dC, g.dskip, g.dbias, g.dz, g.ds)
+
+
+def selective_scan(x, dt, A, Bm, Cm, skip=None, dt_bias=None, z=None, h0=None, lens=None):
+    """The selective state space scan over packed sequences.
+
+    x, dt and z (the gate; None: none) [N,D], Bm and Cm [N,S] in bf16 or fp32 (columns of a wider tensor
+    will do); A [D,S], skip [D] and dt_bias [D] in fp32; lens as for ``short_conv``; h0 [n,D,S] fp32
+    initial states (None: zeros).  Returns (y [N,D], final states [n,D,S]); y and its gradients are 0 in
+    rows behind the last sequence.  Gradients once; a call keeps its inputs and nothing else."""
+    tables, n = _batch(x, lens)
+    desc = D.make_ssm_desc(n, x.shape[1], A.shape[1], _type(x, "x"))
+    return _Ssm.apply(desc, tables, x, dt, A, Bm, Cm, skip, dt_bias, z, h0)
+
+
+class _QkNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, desc, tables, q, k, pos, freq, wq, wk):
+        n = q.shape[0]
+        rows = D.QkRows(desc, n, q, k, pos, freq, wq, wk, tables)
+        shape = (n, desc.heads * desc.rep, desc.head_dim)
+        qo, ko = (torch.zeros(shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        D.dl_qk_norm(desc, rows, qo, ko)
+        ctx.desc, ctx.tables = desc, tables
+        ctx.save_for_backward(q, k, pos, freq, wq, wk)
+        return qo, ko
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dqo, dko):
+        q, k, pos, freq, wq, wk = ctx.saved_tensors
+        rows = D.QkRows(ctx.desc, q.shape[0], q, k, pos, freq, wq, wk, ctx.tables)
+        g = D.QkGrads(ctx.desc, rows)
+        ws = D.qk_workspace(ctx.desc, q.shape[0], device=q.device)
+        D.dl_qk_norm_backward(ctx.desc, rows, dqo.contiguous(), dko.contiguous(), g, ws)
+        return None, None, g.dq, g.dk, None, None, g.dwq, g.dwk
+
+
+def qk_norm(q, k, pos=None, freq=None, wq=None, wk=None, norm="l2", turn="none", rep=1, q_scale=1.0,
+            eps=1e-6, tables=None):
+    """Queries and keys [n,H,d] normalised head by head (``norm`` "l2", "rms" or "none"), weighted by wq
+    and wk [d] (fp32), queries scaled by ``q_scale``, the first 2 len(freq) places of every head turned by
+    the angles pos freq (``turn`` "halves" or "pairs"; pos [n] int32, freq fp32), every head written
+    ``rep`` times.  ``tables``: rows behind its sequences are left out (0).  Gradients once."""
+    rot = 0 if turn == "none" else 2 * freq.numel()
+    desc = D.make_qk_desc(q.shape[1], q.shape[2], norm, turn, rot, rep, _type(q, "q"), eps, q_scale)
+    return _QkNorm.apply(desc, tables, q, k, pos, freq, wq, wk)
