@@ -19,7 +19,7 @@ struct ConvParams {
   void* s_out;               // [B,K,D] (backward: gradient of s_in, or null)
   void* y;                   // (backward: dx)
   const void *dy, *ds_out;   // backward
-  float *dw, *dbias;         // backward: partial sums, one row per stretch
+  float* part;               // backward: [stretches][D W + D] partial sums of dw and dbias
   const int32_t *cu, *seq_slot, *slots;
   int64_t stride;
   int32_t n, N, B, D, len, blocks;   // blocks: workgroups across the channels
@@ -247,11 +247,12 @@ __global__ __launch_bounds__(64) void conv_backward_kernel(ConvParams p) {
       }
     }
   }
+  float* part = p.part + int64_t(f) * p.D * (W + 1);
 #pragma unroll
   for (int e = 0; e < V; ++e) {
 #pragma unroll
-    for (int j = 0; j < W; ++j) p.dw[(int64_t(f) * p.D + c + e) * W + j] = dw[j][e];
-    if (p.bias) p.dbias[int64_t(f) * p.D + c + e] = db[e];
+    for (int j = 0; j < W; ++j) part[int64_t(c + e) * W + j] = dw[j][e];
+    part[int64_t(p.D) * W + c + e] = db[e];
   }
 }
 
@@ -402,12 +403,12 @@ int dl_conv_backward(const dl_conv_desc* desc, const void* s_in, const dl_conv_r
   p.seq_slot = tables->seq_slot;
   p.dy = dy;
   p.ds_out = ds_out;
-  const int64_t parts = stretches(n, tokens, p.len), D = p.D;
-  p.dw = static_cast<float*>(workspace);
-  p.dbias = p.dw + parts * D * desc->width;
+  const int64_t parts = stretches(n, tokens, p.len), D = p.D, W = desc->width;
+  p.part = static_cast<float*>(workspace);
   hipError_t e = launch(BACKWARD, desc, p, parts, stream);
-  if (e == hipSuccess) e = launch_column_sum(p.dw, parts, D * desc->width, D * desc->width, g->dw, stream);
-  if (e == hipSuccess && p.bias) e = launch_column_sum(p.dbias, parts, D, D, g->dbias, stream);
+  if (e == hipSuccess)
+    e = launch_column_sums({p.part, parts, D * (W + 1), {g->dw, p.bias ? g->dbias : nullptr, nullptr}, {D * W, D, 0}},
+                           stream);
   return e == hipSuccess ? DL_OK : DL_E_HIP;
 }
 

@@ -342,8 +342,8 @@ int dl_qk_norm_backward(const dl_qk_desc* desc, const dl_qk_rows* rows, const vo
   }
   hipError_t e = launch(desc, p, true, stream);
   const int64_t parts = (int64_t(n) + p.per - 1) / p.per, d = desc->head_dim;
-  if (e == hipSuccess && p.part) e = launch_column_sum(p.part, parts, d, 2 * d, g->dwq, stream);
-  if (e == hipSuccess && p.part) e = launch_column_sum(p.part + d, parts, d, 2 * d, g->dwk, stream);
+  if (e == hipSuccess && p.part)
+    e = launch_column_sums({p.part, parts, 2 * d, {g->dwq, g->dwk, nullptr}, {d, d, 0}}, stream);
   return e == hipSuccess ? DL_OK : DL_E_HIP;
 }
 

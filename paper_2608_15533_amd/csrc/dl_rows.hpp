@@ -124,9 +124,15 @@ __device__ __forceinline__ Stretch find_stretch(const int32_t* cu, const int32_t
 }
 
 // ------------------------------------------------------------------ sums of partial results
-// out[i] = sum over p < P of part[p * stride + i], i < M.
-hipError_t launch_column_sum(const float* part, int64_t P, int64_t M, int64_t stride, float* out,
-                             hipStream_t s);
+// Sums over the rows of part (stride floats apart), whose columns are up to three outputs side by side;
+// an output that is null is left out.
+struct ColumnSums {
+  const float* part;
+  int64_t rows, stride;
+  float* out[3];
+  int64_t width[3];
+};
+hipError_t launch_column_sums(const ColumnSums& p, hipStream_t s);
 
 // ------------------------------------------------------------------ host
 inline bool aligned_to(const void* p, uintptr_t a) {

@@ -5,13 +5,16 @@
 namespace dl {
 namespace {
 
-constexpr int TILE = 16;       // tokens whose steps lie in LDS at a time
+// Tokens whose steps lie in LDS at a time, and whose B and C a wave holds in 64 scalar registers.
+template <typename T>
+constexpr int tile_tokens = 32 / int(sizeof(T));
 
 // A workgroup: one stretch, 64 channels; wave w has states 4 w .. 4 w + 3.  OUT: outputs and final
 // states; else E and the sum of d, of stretches that others follow.
 template <int S, bool OUT, typename T>
 __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
-  constexpr int NW = S / 4, NT = 64 * NW, EV = TILE * 64 / NT, CG = 64 / EV;
+  constexpr int TILE = tile_tokens<T>, NW = S / 4, NT = 64 * NW;
+  constexpr int EV = TILE * 64 >= NT ? TILE * 64 / NT : 1, CG = 64 / EV;
   __shared__ __attribute__((aligned(16))) float step[TILE][64], input[TILE][64];
   __shared__ __attribute__((aligned(16))) float partial[OUT ? NW : 1][OUT ? TILE : 1][64];
   const int f = blockIdx.x / p.blocks, c0 = int(blockIdx.x % p.blocks) * 64;
@@ -21,7 +24,7 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
   const bool live = c < p.D;
   // This thread's part of a tile: a token, EV channels.
   const int te = threadIdx.x / CG, ce = (threadIdx.x % CG) * EV;
-  const bool le = c0 + ce < p.D;                     // D is a multiple of 8: all EV or none
+  const bool le = c0 + ce < p.D && te < TILE;        // D is a multiple of 8: all EV or none
   const int64_t at = int64_t(f) * p.D * S + (int64_t(w) * p.D + c) * 4;   // of E
 
   float a2[4], h[4];
@@ -61,31 +64,45 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
     const int count = min(TILE, s.count - t0);
     const bool mine = le && te < count;
     float x[EV], z[EV];
+    TileRows<TILE, OUT, T> rows;
+    if (count == TILE) rows.load(bp, p.b_stride, cp, p.c_stride);
     widen_row(rx, x);
     widen_row(rz, z);
+    if (te < TILE) {
 #pragma unroll
-    for (int e = 0; e < EV; ++e) {
-      const float d = mine ? softplus(widen(rd.v[e]) + bias[e]) : 0.0f;
-      step[te][ce + e] = d;
-      input[te][ce + e] = mine ? d * x[e] : 0.0f;
-      total[e] += d;
+      for (int e = 0; e < EV; ++e) {
+        const float d = mine ? softplus(widen(rd.v[e]) + bias[e]) : 0.0f;
+        step[te][ce + e] = d;
+        input[te][ce + e] = mine ? d * x[e] : 0.0f;
+        total[e] += d;
+      }
     }
     fetch(t0 + TILE);
+    if (count == TILE) rows.settle();
     __syncthreads();
-#pragma unroll 4
-    for (int t = 0; t < count; ++t) {
-      Four<T> B, C;
-      B.load(bp + int64_t(t0 + t) * p.b_stride);
-      if (OUT) C.load(cp + int64_t(t0 + t) * p.c_stride);
+    auto token = [&](int t, const Four<T>& B, const Four<T>& C) {
       const float d = step[t][lane], u = input[t][lane];
       float y = 0.0f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         h[i] = fmaf(decay(d, a2[i]), h[i], u * B.at(i));
-        if (OUT) y = fmaf(C.at(i), h[i], y);
+        if (OUT) y = i ? fmaf(C.at(i), h[i], y) : C.at(0) * h[0];
       }
       if (OUT) partial[w][t][lane] = y;
+    };
+    if (count == TILE) {
+#pragma unroll
+      for (int t = 0; t < TILE; ++t) token(t, rows.B[t], rows.C[OUT ? t : 0]);
+    } else {
+      for (int t = 0; t < count; ++t) {
+        Four<T> B, C;
+        B.load(bp + t * p.b_stride);
+        C.load(cp + t * p.c_stride);
+        token(t, B, C);
+      }
     }
+    bp += TILE * p.b_stride;
+    cp += TILE * p.c_stride;
     __syncthreads();
     if (OUT && mine) {
       float y[EV];
@@ -106,8 +123,10 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
   }
   if (live) *reinterpret_cast<f32x4*>(p.E + at) = f32x4{h[0], h[1], h[2], h[3]};
   // The sum of d over the stretch: each thread's own tokens, then the tile's tokens in order.
+  if (te < TILE) {
 #pragma unroll
-  for (int e = 0; e < EV; ++e) step[te][ce + e] = total[e];
+    for (int e = 0; e < EV; ++e) step[te][ce + e] = total[e];
+  }
   __syncthreads();
   if (w == 0 && live) {
     float sum = 0.0f;
@@ -261,7 +280,7 @@ int stretch_len(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) 
   if (backward) return ssm_grad_tokens(d->states);
   const int64_t waves = int64_t(blocks_of(d)) * (d->states / 4);
   int64_t len = 64;
-  while (len < tokens && stretches(n, tokens, int(2 * len)) * waves >= 4096) len *= 2;
+  while (len < tokens && tokens / (2 * len) * waves >= 4096) len *= 2;
   return int(std::min<int64_t>(len, std::max(tokens, 1)));
 }
 // One stretch a sequence: nothing to join.
@@ -458,9 +477,9 @@ int dl_ssm_backward(const dl_ssm_desc* desc, const float* h_in, const dl_ssm_row
   set_workspace(p, desc, l, workspace, true);
   hipError_t e = launch(BACKWARD, desc, p, stream);
   const int64_t parts = stretches(n, tokens, p.len), D = p.D, S = p.S, row = D * (S + 2);
-  if (e == hipSuccess) e = launch_column_sum(p.part, parts, D * S, row, g->dA, stream);
-  if (e == hipSuccess && p.skip) e = launch_column_sum(p.part + D * S, parts, D, row, g->dskip, stream);
-  if (e == hipSuccess && p.bias) e = launch_column_sum(p.part + D * (S + 1), parts, D, row, g->dbias, stream);
+  if (e == hipSuccess)
+    e = launch_column_sums({p.part, parts, row, {g->dA, p.skip ? g->dskip : nullptr, p.bias ? g->dbias : nullptr},
+                            {D * S, D, D}}, stream);
   return e == hipSuccess ? DL_OK : DL_E_HIP;
 }
 

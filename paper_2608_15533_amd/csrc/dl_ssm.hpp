@@ -80,6 +80,7 @@ struct Four<float> {
     v = *(scalar_t*)(uintptr_t)p;
   }
   __device__ __forceinline__ float at(int i) const { return v[i]; }
+  __device__ __forceinline__ void settle() { asm volatile("" : "+s"(v)); }
 };
 template <>
 struct Four<uint16_t> {
@@ -91,6 +92,32 @@ struct Four<uint16_t> {
   }
   __device__ __forceinline__ float at(int i) const {
     return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16);
+  }
+  __device__ __forceinline__ void settle() { asm volatile("" : "+s"(v)); }
+};
+// B and C of TB tokens, a wave's four states each.  Scalar loads return in any order, so the first use
+// of one waits for all: they are asked for before a tile's steps are formed and settled behind that.
+template <int TB, bool WITH_C, typename T>
+struct TileRows {
+  Four<T> B[TB], C[WITH_C ? TB : 1];
+  // Rows past the count-th are that row again.
+  __device__ __forceinline__ void load(const T* b, int64_t b_stride, const T* c, int64_t c_stride, int count = TB) {
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+      B[t].load(b);
+      b += t + 1 < count ? b_stride : 0;
+      if constexpr (WITH_C) {
+        C[t].load(c);
+        c += t + 1 < count ? c_stride : 0;
+      }
+    }
+  }
+  __device__ __forceinline__ void settle() {
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+      B[t].settle();
+      if constexpr (WITH_C) C[t].settle();
+    }
   }
 };
 

@@ -53,6 +53,8 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
   const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
   for (int t0 = 0; t0 < s.count; t0 += TB) {
     const int count = min(TB, s.count - t0);
+    TileRows<TB, true, T> rows;
+    if (count == TB) rows.load(bp, p.b_stride, cp, p.c_stride);
     if (part.te < TB) {
       float x[EV] = {}, d[EV] = {}, up[EV] = {};
       if (part.live && part.te < count) {
@@ -77,12 +79,9 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
         total[e] += d[e];
       }
     }
+    if (count == TB) rows.settle();
     __syncthreads();
-#pragma unroll 4
-    for (int t = 0; t < count; ++t) {
-      Four<T> B, C;
-      B.load(bp + int64_t(t0 + t) * p.b_stride);
-      C.load(cp + int64_t(t0 + t) * p.c_stride);
+    auto token = [&](int t, const Four<T>& B, const Four<T>& C) {
       const float d = step[t][lane], u = input[t][lane], up = grad[t][lane];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -91,7 +90,20 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
         decays[i] *= a;
         g[i] = fmaf(decays[i], up * C.at(i), g[i]);
       }
+    };
+    if (count == TB) {
+#pragma unroll
+      for (int t = 0; t < TB; ++t) token(t, rows.B[t], rows.C[t]);
+    } else {
+      for (int t = 0; t < count; ++t) {
+        Four<T> B, C;
+        B.load(bp + t * p.b_stride);
+        C.load(cp + t * p.c_stride);
+        token(t, B, C);
+      }
     }
+    bp += TB * p.b_stride;
+    cp += TB * p.c_stride;
     __syncthreads();
   }
   if (c < p.D) {
@@ -168,6 +180,8 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
     for (int j = 0; j < tiles; ++j) {
       before[j][w][lane] = f32x4{h[0], h[1], h[2], h[3]};
       if (j + 1 == tiles) break;
+      TileRows<TB, false, T> rows;
+      rows.load(bp + int64_t(j * TB) * p.b_stride, p.b_stride, nullptr, 0);
       if (part.te < TB) {
         float x[EV] = {}, d[EV] = {};
         if (part.live) {
@@ -183,14 +197,13 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
           input[part.te][part.ce + e] = d[e] * x[e];
         }
       }
+      rows.settle();
       __syncthreads();
-#pragma unroll 4
+#pragma unroll
       for (int t = 0; t < TB; ++t) {
-        Four<T> B;
-        B.load(bp + int64_t(j * TB + t) * p.b_stride);
         const float d = step[t][lane], u = input[t][lane];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = fmaf(decay(d, a2[i]), h[i], u * B.at(i));
+        for (int i = 0; i < 4; ++i) h[i] = fmaf(decay(d, a2[i]), h[i], u * rows.B[t].at(i));
       }
       __syncthreads();
     }
@@ -198,6 +211,8 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
       const int t0 = j * TB, count = min(TB, s.count - t0);
       const bool mine = part.live && part.te < count;
       const int64_t row = int64_t(s.first) + t0 + part.te;
+      TileRows<TB, true, T> rows;
+      rows.load(bp + int64_t(t0) * p.b_stride, p.b_stride, cp + int64_t(t0) * p.c_stride, p.c_stride, count);
       // Rows as they are stored stay in registers; what they stand for is formed again behind the tile.
       Raw<EV, T> rx{}, rd{}, ro{}, rz{};
       if (mine) {
@@ -215,63 +230,61 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
           grad[part.te][part.ce + e] = widen(ro.v[e]) * (p.z ? z * quick_sigmoid(z) : 1.0f);
         }
       }
+      rows.settle();
       __syncthreads();
-      float a[TB][4], m[TB][4];
       {
         const f32x4 v = before[j][w][lane];
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = v[i];
       }
+      auto walk = [&](auto whole) {
+        constexpr bool ALL = decltype(whole)::value;
+        float a[TB][4], m[TB][4];
 #pragma unroll
-      for (int t = 0; t < TB; ++t) {
-        if (t < count) {
-          Four<T> B;
-          B.load(bp + int64_t(t0 + t) * p.b_stride);
+        for (int t = 0; t < TB; ++t) {
+          if (!ALL && t >= count) break;
           const float dd = step[t][lane], u = input[t][lane];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             a[t][i] = decay(dd, a2[i]);
             m[t][i] = a[t][i] * h[i];
-            h[i] = fmaf(u, B.at(i), m[t][i]);
+            h[i] = fmaf(u, rows.B[t].at(i), m[t][i]);
           }
         }
-        __builtin_amdgcn_sched_barrier(0);     // one token's operands at a time: registers
-      }
-      float kept = 0.0f;
+        float kept = 0.0f;
 #pragma unroll
-      for (int t = TB - 1; t >= 0; --t) {
-        if (t < count) {
-          Four<T> B, C;
-          B.load(bp + int64_t(t0 + t) * p.b_stride);
-          C.load(cp + int64_t(t0 + t) * p.c_stride);
-          const float dd = step[t][lane], u = input[t][lane], v = grad[t][lane];
-          float gb = 0.0f, gm = 0.0f, ch = 0.0f, over[8];
+        for (int t = TB - 1; t >= 0; --t) {
+          if (ALL || t < count) {
+            const float dd = step[t][lane], u = input[t][lane], v = grad[t][lane];
+            float gb = 0.0f, gm = 0.0f, ch = 0.0f, over[8];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float b = B.at(i), cc = C.at(i);
-            g[i] = fmaf(v, cc, g[i]);
-            const float ht = fmaf(u, b, m[t][i]), x0 = g[i] * m[t][i];
-            gb = fmaf(g[i], b, gb);
-            gm = fmaf(x0, A[i], gm);
-            ch = fmaf(cc, ht, ch);
-            dA[i] = fmaf(x0, dd, dA[i]);
-            over[i] = g[i] * u;
-            over[4 + i] = ht * v;
-            g[i] *= a[t][i];
+            for (int i = 0; i < 4; ++i) {
+              const float b = rows.B[t].at(i), cc = rows.C[t].at(i);
+              g[i] = fmaf(v, cc, g[i]);
+              const float ht = fmaf(u, b, m[t][i]), x0 = g[i] * m[t][i];
+              gb = fmaf(g[i], b, gb);
+              gm = fmaf(x0, A[i], gm);
+              ch = fmaf(cc, ht, ch);
+              dA[i] = fmaf(x0, dd, dA[i]);
+              over[i] = g[i] * u;
+              over[4 + i] = ht * v;
+              g[i] *= a[t][i];
+            }
+            sum_gb[w][t][lane] = gb;
+            sum_gm[w][t][lane] = gm;
+            if (p.z) sum_ch[w][t][lane] = ch;
+            const float one = eight_sums(over);
+            if ((lane & 7) == (t & 7)) kept = one;
           }
-          sum_gb[w][t][lane] = gb;
-          sum_gm[w][t][lane] = gm;
-          if (p.z) sum_ch[w][t][lane] = ch;
-          const float one = eight_sums(over);
-          if ((lane & 7) == (t & 7)) kept = one;
+          if ((t & 7) == 0) {
+            const int tt = t + (lane & 7), k = sum_number(lane);   // numbers 0-3: B's states, 4-7: C's
+            if (tt < count)
+              p.rows[(int64_t(block) * p.N + s.first + t0 + tt) * (2 * S) + (k >> 2) * S + 4 * w + (k & 3)] = kept;
+          }
         }
-        __builtin_amdgcn_sched_barrier(0);
-        if ((t & 7) == 0) {
-          const int tt = t + (lane & 7), k = sum_number(lane);   // numbers 0-3: B's states, 4-7: C's
-          if (tt < count)
-            p.rows[(int64_t(block) * p.N + s.first + t0 + tt) * (2 * S) + (k >> 2) * S + 4 * w + (k & 3)] = kept;
-        }
-      }
+      };
+      if (count == TB) walk(std::true_type{});
+      else walk(std::false_type{});
       __syncthreads();
       if (mine) {
         float dx[EV], ddt[EV], dz[EV];
@@ -329,25 +342,34 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
   }
 }
 
-// dB and dC of a stretch's tokens: the sums over blocks of channels, in their order.
+// dB and dC: the sums over blocks of channels, in their order, eight loads at a time.  A workgroup for 256
+// of a stretch's sums.
 template <int S, typename T>
 __global__ __launch_bounds__(256) void ssm_rows_kernel(SsmParams p) {
-  const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, blockIdx.x);
-  if (s.idle) return;
-  for (int i = threadIdx.x; i < s.count * 2 * S; i += 256) {
-    const int64_t row = int64_t(s.first) + i / (2 * S);
-    const int k = i % (2 * S);
-    float sum = 0.0f;
-    for (int b = 0; b < p.blocks; ++b) sum += p.rows[(int64_t(b) * p.N + row) * (2 * S) + k];
-    narrow(static_cast<T*>(k < S ? p.dB : p.dC) + row * S + k % S, sum);
+  constexpr int PIECES = ssm_grad_tokens(S) * 2 * S / 256, U = 8;
+  const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, blockIdx.x / PIECES);
+  const int i = int(blockIdx.x % PIECES) * 256 + int(threadIdx.x);
+  if (s.idle || i >= s.count * 2 * S) return;
+  const int64_t row = int64_t(s.first) + i / (2 * S), apart = int64_t(p.N) * (2 * S);
+  const int k = i % (2 * S);
+  const float* at = p.rows + row * (2 * S) + k;
+  float sum = 0.0f;
+  for (int b = 0; b < p.blocks; b += U) {
+    float v[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) v[j] = b + j < p.blocks ? at[(b + j) * apart] : 0.0f;
+#pragma unroll
+    for (int j = 0; j < U; ++j) sum += v[j];
   }
+  narrow(static_cast<T*>(k < S ? p.dB : p.dC) + row * S + k % S, sum);
 }
 
 template <int S, typename T>
 hipError_t launch_grad(const SsmParams& p, hipStream_t s) {
   const int64_t parts = stretches(p.n, p.N, p.len);
   hipError_t e = start_rows(&ssm_grad_kernel<S, T>, parts * p.blocks, S * 16, p, s);
-  if (e == hipSuccess) e = start_rows(&ssm_rows_kernel<S, T>, parts, 256, p, s);
+  if (e == hipSuccess)
+    e = start_rows(&ssm_rows_kernel<S, T>, parts * (ssm_grad_tokens(S) * 2 * S / 256), 256, p, s);
   return e;
 }
 template <int S, typename T>
