@@ -318,8 +318,8 @@ int dl_prefill_backward(const dl_desc* desc, const void* S_in, const dl_token* t
  * calls do.  n == 0 is a no-op; rows behind the last sequence are never used, and output rows
  * there stay as they were.
  *  - Token rows that are inputs may be columns of a wider array: *_stride counts the elements
- *    from one row to the next, at least a row's width and a multiple of 8.  Arrays of in_dtype
- *    and states are 16-byte aligned, fp32 parameters and int32 arrays 4-byte aligned.  Outputs
+ *    from one row to the next, at least a row's width, a multiple of 8 and up to
+ *    DL_MAX_STRIDE.  Arrays of in_dtype and states are 16-byte aligned, fp32 parameters and int32 arrays 4-byte aligned.  Outputs
  *    and gradients are dense.
  *  - Products, sums, states' arithmetic and statistics are fp32; every output is rounded once.
  *  - Outputs must not overlap inputs or each other, s_out = s_in apart.  Calls on distinct
@@ -327,6 +327,8 @@ int dl_prefill_backward(const dl_desc* desc, const void* S_in, const dl_token* t
  *  - Sums over tokens, rows or channels (gradients of parameters, of B and C) are taken in an
  *    order that depends on sizes alone: the same call gives the same bits.
  *  - Slots that are listed twice in one call race (undefined). */
+
+#define DL_MAX_STRIDE (1 << 24)
 
 typedef enum { DL_ACT_NONE = 0, DL_ACT_SILU = 1 } dl_activation;
 

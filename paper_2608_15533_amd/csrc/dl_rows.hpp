@@ -138,8 +138,9 @@ hipError_t launch_column_sums(const ColumnSums& p, hipStream_t s);
 inline bool aligned_to(const void* p, uintptr_t a) {
   return (reinterpret_cast<uintptr_t>(p) % a) == 0;
 }
+// Up to DL_MAX_STRIDE: offsets of 16 rows fit 32 bits.
 inline bool good_stride(int64_t stride, int64_t width) {
-  return stride >= width && stride % 8 == 0 && stride <= (int64_t(1) << 40);
+  return stride >= width && stride % 8 == 0 && stride <= DL_MAX_STRIDE;
 }
 inline size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
 inline bool grid_fits(int64_t blocks, int threads) {

@@ -5,15 +5,16 @@
 namespace dl {
 namespace {
 
-// Tokens whose steps lie in LDS at a time, and whose B and C a wave holds in 64 scalar registers.
-template <typename T>
-constexpr int tile_tokens = 32 / int(sizeof(T));
+// Tokens whose steps lie in LDS at a time, and whose B (and C) a wave holds in 32 scalar registers: 64
+// do not fit beside the pointers (8192 x 4096 outputs: 229 us instead of 199).
+template <bool OUT, typename T>
+constexpr int tile_tokens = (OUT ? 16 : 32) / int(sizeof(T));
 
 // A workgroup: one stretch, 64 channels; wave w has states 4 w .. 4 w + 3.  OUT: outputs and final
 // states; else E and the sum of d, of stretches that others follow.
 template <int S, bool OUT, typename T>
 __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
-  constexpr int TILE = tile_tokens<T>, NW = S / 4, NT = 64 * NW;
+  constexpr int TILE = tile_tokens<OUT, T>, NW = S / 4, NT = 64 * NW;
   constexpr int EV = TILE * 64 >= NT ? TILE * 64 / NT : 1, CG = 64 / EV;
   __shared__ __attribute__((aligned(16))) float step[TILE][64], input[TILE][64];
   __shared__ __attribute__((aligned(16))) float partial[OUT ? NW : 1][OUT ? TILE : 1][64];
@@ -46,22 +47,21 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
     skip[e] = OUT && p.skip && le ? p.skip[c0 + ce + e] : 0.0f;
     total[e] = 0.0f;
   }
-  const T* xp = static_cast<const T*>(p.x) + c0 + ce;
-  const T* dp = static_cast<const T*>(p.dt) + c0 + ce;
-  const T* zp = static_cast<const T*>(p.z) + c0 + ce;
+  typedef Cursor<EV, T> At;
+  const At xs(p.x, p.x_stride, s.first, c0, te, ce, TILE), ds(p.dt, p.dt_stride, s.first, c0, te, ce, TILE);
+  const At zs(p.z, p.z_stride, s.first, c0, te, ce, TILE), ys(p.y, p.D, s.first, c0, te, ce, TILE);
   const T* bp = static_cast<const T*>(p.Bm) + int64_t(s.first) * p.b_stride + 4 * w;
   const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
   Raw<EV, T> rx{}, rd{}, rz{};
-  auto fetch = [&](int t0) {
-    if (!le || t0 + te >= s.count) return;
-    const int64_t row = s.first + t0 + te;
-    rx = load_raw<EV>(xp + row * p.x_stride);
-    rd = load_raw<EV>(dp + row * p.dt_stride);
-    if (OUT && p.z) rz = load_raw<EV>(zp + row * p.z_stride);
+  auto fetch = [&](int j) {
+    if (!le || j * TILE + te >= s.count) return;
+    rx = xs.load(j);
+    rd = ds.load(j);
+    if (OUT && p.z) rz = zs.load(j);
   };
   fetch(0);
-  for (int t0 = 0; t0 < s.count; t0 += TILE) {
-    const int count = min(TILE, s.count - t0);
+  for (int j = 0; j * TILE < s.count; ++j) {
+    const int count = min(TILE, s.count - j * TILE);
     const bool mine = le && te < count;
     float x[EV], z[EV];
     TileRows<TILE, OUT, T> rows;
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
         total[e] += d;
       }
     }
-    fetch(t0 + TILE);
+    fetch(j + 1);
     if (count == TILE) rows.settle();
     __syncthreads();
     auto token = [&](int t, const Four<T>& B, const Four<T>& C) {
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
         y[e] = fmaf(skip[e], x[e], y[e]);
         if (p.z) y[e] *= z[e] * quick_sigmoid(z[e]);
       }
-      store_row<EV>(static_cast<T*>(p.y) + (int64_t(s.first) + t0 + te) * p.D + c0 + ce, y);
+      ys.store(j, y);
     }
   }
   if (OUT) {
@@ -275,12 +275,13 @@ hipError_t launch(Pass pass, const dl_ssm_desc* d, const SsmParams& p, hipStream
 
 int blocks_of(const dl_ssm_desc* d) { return (d->channels + 63) / 64; }
 
-// Tokens of a stretch: as long as enough waves are left to fill the chip.
+// Tokens of a stretch: as long as 16 waves a SIMD are left, so that ragged ends even out.  8192 tokens of 4096
+// channels with 2048, 4096, 8192, 16384 and 32768 waves: 476, 316, 294, 277 and 284 us.
 int stretch_len(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
   if (backward) return ssm_grad_tokens(d->states);
   const int64_t waves = int64_t(blocks_of(d)) * (d->states / 4);
-  int64_t len = 64;
-  while (len < tokens && tokens / (2 * len) * waves >= 4096) len *= 2;
+  int64_t len = 32;
+  while (len < tokens && tokens / (2 * len) * waves >= 16384) len *= 2;
   return int(std::min<int64_t>(len, std::max(tokens, 1)));
 }
 // One stretch a sequence: nothing to join.

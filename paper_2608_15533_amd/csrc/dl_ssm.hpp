@@ -121,6 +121,26 @@ struct TileRows {
   }
 };
 
+// A thread's values of a tile's rows, tile by tile: the tile's address is the same for all threads (scalar
+// registers), the thread's offset in it 32 bits.
+template <int EV, typename T>
+struct Cursor {
+  uint64_t at;
+  int64_t tile;          // bytes from a tile to the next
+  uint32_t off;
+  __device__ __forceinline__ Cursor(const void* base, int64_t stride, int64_t row, int c0, int te, int ce,
+                                    int tokens)
+      : at(reinterpret_cast<uint64_t>(base) + (row * stride + c0) * int64_t(sizeof(T))),
+        tile(tokens * stride * int64_t(sizeof(T))),
+        off(uint32_t(te) * uint32_t(stride) * uint32_t(sizeof(T)) + uint32_t(ce) * uint32_t(sizeof(T))) {}
+  __device__ __forceinline__ Raw<EV, T> load(int j) const {
+    return load_raw<EV>(reinterpret_cast<const T*>(at + j * tile + off));
+  }
+  __device__ __forceinline__ void store(int j, const float (&x)[EV]) const {
+    store_row<EV>(reinterpret_cast<T*>(at + j * tile + off), x);
+  }
+};
+
 __device__ __forceinline__ int wave_index() {
   return __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
 }

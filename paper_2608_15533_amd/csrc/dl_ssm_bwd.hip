@@ -24,11 +24,8 @@ struct Part {
 #pragma unroll
     for (int e = 0; e < EV; ++e) bias[e] = p.bias && live ? p.bias[c + e] : 0.0f;
   }
-  __device__ __forceinline__ Raw<EV, T> raw(const void* base, int64_t stride, int64_t row) const {
-    return load_raw<EV>(static_cast<const T*>(base) + row * stride + c);
-  }
-  __device__ __forceinline__ void load(const void* base, int64_t stride, int64_t row, float (&x)[EV]) const {
-    widen_row(raw(base, stride, row), x);
+  __device__ __forceinline__ Cursor<EV, T> rows(const void* base, int64_t stride, int first) const {
+    return Cursor<EV, T>(base, stride, first, c - ce, te, ce, TB);
   }
 };
 
@@ -51,34 +48,33 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
   }
   const T* bp = static_cast<const T*>(p.Bm) + int64_t(s.first) * p.b_stride + 4 * w;
   const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
-  for (int t0 = 0; t0 < s.count; t0 += TB) {
-    const int count = min(TB, s.count - t0);
+  const Cursor<EV, T> xs = part.rows(p.x, p.x_stride, s.first), ds = part.rows(p.dt, p.dt_stride, s.first);
+  const Cursor<EV, T> os = part.rows(p.dy, p.D, s.first), zs = part.rows(p.z, p.z_stride, s.first);
+  Raw<EV, T> rx{}, rd{}, ro{}, rz{};
+  auto fetch = [&](int j) {
+    if (!part.live || j * TB + part.te >= s.count) return;
+    rx = xs.load(j);
+    rd = ds.load(j);
+    ro = os.load(j);
+    if (p.z) rz = zs.load(j);
+  };
+  fetch(0);
+  for (int j = 0; j * TB < s.count; ++j) {
+    const int count = min(TB, s.count - j * TB);
+    const bool mine = part.live && part.te < count;
     TileRows<TB, true, T> rows;
     if (count == TB) rows.load(bp, p.b_stride, cp, p.c_stride);
     if (part.te < TB) {
-      float x[EV] = {}, d[EV] = {}, up[EV] = {};
-      if (part.live && part.te < count) {
-        const int64_t row = int64_t(s.first) + t0 + part.te;
-        part.load(p.x, p.x_stride, row, x);
-        part.load(p.dt, p.dt_stride, row, d);
-        part.load(p.dy, p.D, row, up);
-#pragma unroll
-        for (int e = 0; e < EV; ++e) d[e] = softplus(d[e] + part.bias[e]);
-        if (p.z) {
-          float z[EV];
-          part.load(p.z, p.z_stride, row, z);
-#pragma unroll
-          for (int e = 0; e < EV; ++e) up[e] *= z[e] * quick_sigmoid(z[e]);
-        }
-      }
 #pragma unroll
       for (int e = 0; e < EV; ++e) {
-        step[part.te][part.ce + e] = d[e];
-        input[part.te][part.ce + e] = d[e] * x[e];
-        grad[part.te][part.ce + e] = up[e];
-        total[e] += d[e];
+        const float d = mine ? softplus(widen(rd.v[e]) + part.bias[e]) : 0.0f, z = widen(rz.v[e]);
+        step[part.te][part.ce + e] = d;
+        input[part.te][part.ce + e] = mine ? d * widen(rx.v[e]) : 0.0f;
+        grad[part.te][part.ce + e] = mine ? widen(ro.v[e]) * (p.z ? z * quick_sigmoid(z) : 1.0f) : 0.0f;
+        total[e] += d;
       }
     }
+    fetch(j + 1);
     if (count == TB) rows.settle();
     __syncthreads();
     auto token = [&](int t, const Four<T>& B, const Four<T>& C) {
@@ -177,26 +173,34 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
     const T* bp = static_cast<const T*>(p.Bm) + int64_t(s.first) * p.b_stride + 4 * w;
     const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
     const int tiles = (s.count + TB - 1) / TB;
+    const Cursor<EV, T> xs = part.rows(p.x, p.x_stride, s.first), ds = part.rows(p.dt, p.dt_stride, s.first);
+    const Cursor<EV, T> os = part.rows(p.dy, p.D, s.first), zs = part.rows(p.z, p.z_stride, s.first);
+    const int64_t out = (int64_t(s.first) + part.te) * p.D + part.c;
+    // Rows as they are stored, a tile ahead in either direction.
+    Raw<EV, T> rx{}, rd{}, ro{}, rz{};
+    auto fetch = [&](int j, bool all) {
+      if (!part.live || j < 0 || j * TB + part.te >= s.count) return;
+      rx = xs.load(j);
+      rd = ds.load(j);
+      if (!all) return;
+      ro = os.load(j);
+      if (p.z) rz = zs.load(j);
+    };
+    fetch(0, tiles == 1);
     for (int j = 0; j < tiles; ++j) {
       before[j][w][lane] = f32x4{h[0], h[1], h[2], h[3]};
       if (j + 1 == tiles) break;
       TileRows<TB, false, T> rows;
       rows.load(bp + int64_t(j * TB) * p.b_stride, p.b_stride, nullptr, 0);
       if (part.te < TB) {
-        float x[EV] = {}, d[EV] = {};
-        if (part.live) {
-          const int64_t row = int64_t(s.first) + j * TB + part.te;
-          part.load(p.x, p.x_stride, row, x);
-          part.load(p.dt, p.dt_stride, row, d);
-#pragma unroll
-          for (int e = 0; e < EV; ++e) d[e] = softplus(d[e] + part.bias[e]);
-        }
 #pragma unroll
         for (int e = 0; e < EV; ++e) {
-          step[part.te][part.ce + e] = d[e];
-          input[part.te][part.ce + e] = d[e] * x[e];
+          const float d = part.live ? softplus(widen(rd.v[e]) + part.bias[e]) : 0.0f;
+          step[part.te][part.ce + e] = d;
+          input[part.te][part.ce + e] = d * widen(rx.v[e]);
         }
       }
+      fetch(j + 1, j + 2 == tiles);
       rows.settle();
       __syncthreads();
 #pragma unroll
@@ -210,26 +214,19 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
     for (int j = tiles - 1; j >= 0; --j) {
       const int t0 = j * TB, count = min(TB, s.count - t0);
       const bool mine = part.live && part.te < count;
-      const int64_t row = int64_t(s.first) + t0 + part.te;
       TileRows<TB, true, T> rows;
       rows.load(bp + int64_t(t0) * p.b_stride, p.b_stride, cp + int64_t(t0) * p.c_stride, p.c_stride, count);
-      // Rows as they are stored stay in registers; what they stand for is formed again behind the tile.
-      Raw<EV, T> rx{}, rd{}, ro{}, rz{};
-      if (mine) {
-        rx = part.raw(p.x, p.x_stride, row);
-        rd = part.raw(p.dt, p.dt_stride, row);
-        ro = part.raw(p.dy, p.D, row);
-        if (p.z) rz = part.raw(p.z, p.z_stride, row);
-      }
+      const Raw<EV, T> kx = rx, kd = rd, ko = ro, kz = rz;
       if (part.te < TB) {
 #pragma unroll
         for (int e = 0; e < EV; ++e) {
-          const float d = mine ? softplus(widen(rd.v[e]) + part.bias[e]) : 0.0f, z = widen(rz.v[e]);
+          const float d = mine ? softplus(widen(kd.v[e]) + part.bias[e]) : 0.0f, z = widen(kz.v[e]);
           step[part.te][part.ce + e] = d;
-          input[part.te][part.ce + e] = d * widen(rx.v[e]);
-          grad[part.te][part.ce + e] = widen(ro.v[e]) * (p.z ? z * quick_sigmoid(z) : 1.0f);
+          input[part.te][part.ce + e] = mine ? d * widen(kx.v[e]) : 0.0f;
+          grad[part.te][part.ce + e] = mine ? widen(ko.v[e]) * (p.z ? z * quick_sigmoid(z) : 1.0f) : 0.0f;
         }
       }
+      fetch(j - 1, true);
       rows.settle();
       __syncthreads();
       {
@@ -298,17 +295,18 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
             gm += sum_gm[i][part.te][part.ce + e];
             if (p.z) ch += sum_ch[i][part.te][part.ce + e];
           }
-          const float x = widen(rx.v[e]), z = widen(rz.v[e]), sz = quick_sigmoid(z);
+          const float x = widen(kx.v[e]), z = widen(kz.v[e]), sz = quick_sigmoid(z);
           const float up = grad[part.te][part.ce + e];
           dx[e] = fmaf(step[part.te][part.ce + e], gb, skip[e] * up);
-          ddt[e] = quick_sigmoid(widen(rd.v[e]) + part.bias[e]) * fmaf(x, gb, gm);
+          ddt[e] = quick_sigmoid(widen(kd.v[e]) + part.bias[e]) * fmaf(x, gb, gm);
           dskip[e] = fmaf(up, x, dskip[e]);
           dbias[e] += ddt[e];
-          dz[e] = widen(ro.v[e]) * fmaf(skip[e], x, ch) * sz * (1.0f + z * (1.0f - sz));
+          dz[e] = widen(ko.v[e]) * fmaf(skip[e], x, ch) * sz * (1.0f + z * (1.0f - sz));
         }
-        store_row<EV>(static_cast<T*>(p.dx) + row * p.D + part.c, dx);
-        store_row<EV>(static_cast<T*>(p.ddt) + row * p.D + part.c, ddt);
-        if (p.z) store_row<EV>(static_cast<T*>(p.dz) + row * p.D + part.c, dz);
+        const int64_t to = int64_t(t0) * p.D;
+        store_row<EV>(static_cast<T*>(p.dx) + to + out, dx);
+        store_row<EV>(static_cast<T*>(p.ddt) + to + out, ddt);
+        if (p.z) store_row<EV>(static_cast<T*>(p.dz) + to + out, dz);
       }
       // What a thread reads of step and grad here, it alone writes in the next tile.
     }

@@ -6,7 +6,7 @@
 namespace dl {
 
 // Tokens of a stretch of the backward pass: the states before its tiles fit LDS.
-__host__ __device__ constexpr int ssm_grad_tokens(int states) { return states == 64 ? 16 : 64; }
+__host__ __device__ constexpr int ssm_grad_tokens(int states) { return states == 32 ? 64 : states == 16 ? 32 : 16; }
 
 // E, F and the sum of d of every stretch.
 hipError_t launch_ssm_ends(int states, bool bf16, const SsmParams& p, hipStream_t s);

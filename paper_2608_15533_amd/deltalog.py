@@ -35,6 +35,7 @@ DL_OK, DL_E_NULL, DL_E_SHAPE, DL_E_DTYPE, DL_E_ALIGN, DL_E_UNSUPPORTED, DL_E_HIP
 DL_E_SCRATCH = -8
 DL_NOALLOC_SCRATCH_BYTES = 4 << 20
 DL_CHUNK, DL_MAX_HEADS = 32, 65536
+DL_MAX_STRIDE = 1 << 24
 DL_OP_GDN, DL_OP_KDA, DL_OP_RWKV6, DL_OP_LINATTN, DL_OP_RETNET, DL_OP_GLA = 0, 1, 2, 3, 4, 5
 DL_F32, DL_BF16 = 0, 1
 OP_IDS = {"gdn": DL_OP_GDN, "kda": DL_OP_KDA, "rwkv6": DL_OP_RWKV6, "linattn": DL_OP_LINATTN,
