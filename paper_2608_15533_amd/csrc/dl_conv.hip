@@ -70,7 +70,7 @@ __device__ __forceinline__ void push(float (&past)[R][V], const float (&x)[V]) {
 // state: the lane that reads a state's channels is the one that writes them (s_out may be s_in).
 template <int W, bool SILU, typename T>
 __global__ __launch_bounds__(64) void conv_kernel(ConvParams p) {
-  constexpr int V = 16 / sizeof(T), K = W - 1, U = 8;
+  constexpr int V = 4, K = W - 1, U = 8;
   const int c = (int(blockIdx.x % p.blocks) * 64 + int(threadIdx.x)) * V;
   const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, blockIdx.x / p.blocks);
   if (s.idle || c >= p.D) return;
@@ -110,10 +110,18 @@ __global__ __launch_bounds__(64) void conv_kernel(ConvParams p) {
   if (s.count == 0) return;
   Taps<W, V> taps;
   taps.load(p, c);
+  // U rows under way while the U before them are worked on; past the end the last row again.
+  Raw<V, T> next[U];
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) next[i] = load_raw<V>(x + int64_t(min(t + i, s.count - 1)) * p.stride);
+  };
+  fetch(0);
   for (int t = 0; t < s.count; t += U) {
     Raw<V, T> in[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i) in[i] = load_raw<V>(x + int64_t(min(t + i, s.count - 1)) * p.stride);
+    for (int i = 0; i < U; ++i) in[i] = next[i];
+    if (t + U < s.count) fetch(t + U);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       if (t + i >= s.count) break;
@@ -190,15 +198,24 @@ __global__ __launch_bounds__(64) void conv_backward_kernel(ConvParams p) {
     }
     // Rows of de that are this stretch's: its tokens, and the state's rows where it begins.
     const int steps = s.count + K;
+    Raw<V, T> next[U], above[U];
+    auto fetch = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int r = min(t + i, left - 1);
+        next[i] = load_raw<V>(x + int64_t(r) * p.stride);
+        above[i] = load_raw<V>(dy + int64_t(r) * p.D);
+      }
+    };
+    if (left > 0) fetch(0);                                      // else an empty sequence
     for (int t = 0; t < steps; t += U) {
       Raw<V, T> in[U], up[U];
 #pragma unroll
       for (int i = 0; i < U; ++i) {
-        const int r = min(t + i, left - 1);
-        if (r < 0) continue;                                     // an empty sequence
-        in[i] = load_raw<V>(x + int64_t(r) * p.stride);
-        up[i] = load_raw<V>(dy + int64_t(r) * p.D);
+        in[i] = next[i];
+        up[i] = above[i];
       }
+      if (left > 0 && t + U < steps) fetch(t + U);
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         const int u = t + i;
@@ -260,7 +277,7 @@ enum Pass { STEP, FORWARD, BACKWARD };
 template <int W, bool SILU, typename T>
 hipError_t launch_pass(Pass pass, const ConvParams& q, int64_t rows, hipStream_t s) {
   ConvParams p = q;
-  const int v = pass == BACKWARD ? 4 : int(16 / sizeof(T));
+  const int v = pass == STEP ? int(16 / sizeof(T)) : 4;
   p.blocks = (p.D + 64 * v - 1) / (64 * v);
   if (pass == STEP) return start_rows(&conv_step_kernel<W, SILU, T>, rows * p.blocks, 64, p, s);
   if (pass == FORWARD) return start_rows(&conv_kernel<W, SILU, T>, rows * p.blocks, 64, p, s);
@@ -283,8 +300,15 @@ hipError_t launch(Pass pass, const dl_conv_desc* d, const ConvParams& p, int64_t
               : launch_width<false, float>(pass, d, p, rows, s);
 }
 
-// Tokens of a stretch.
-int stretch_len(const dl_conv_desc*, int32_t, int32_t) { return 32; }
+// Tokens of a stretch: as long as enough waves are left (each reads W - 1 rows of its neighbours, backward twice,
+// and writes a row of partial sums).  4096 tokens of 12288 channels forward and backward: 126 us with half as
+// many waves, 120 with these, 128 with stretches of 32 for both; 12345 tokens of 4096 channels 49 and 47.
+int stretch_len(const dl_conv_desc* d, int32_t n, int32_t tokens, bool backward) {
+  const int64_t blocks = (int64_t(d->channels) + 255) / 256, waves = backward ? 2048 : 4096;
+  int len = 16;
+  while (len < 256 && stretches(n, tokens, 2 * len) * blocks >= waves) len *= 2;
+  return len;
+}
 
 int check_desc(const dl_conv_desc* d) {
   if (!d) return DL_E_NULL;
@@ -303,9 +327,9 @@ int check_grid(const dl_conv_desc* d, int64_t rows) {
   return grid_fits(rows * blocks, 64) ? DL_OK : DL_E_SHAPE;
 }
 
-int check_counts(const dl_conv_desc* d, int32_t n, int32_t tokens) {
+int check_counts(const dl_conv_desc* d, int32_t n, int32_t tokens, bool backward) {
   if (n < 0 || tokens < 0 || n > d->num_slots) return DL_E_SHAPE;
-  return check_grid(d, stretches(n, tokens, stretch_len(d, n, tokens)));
+  return check_grid(d, stretches(n, tokens, stretch_len(d, n, tokens, backward)));
 }
 
 int check_rows(const dl_conv_desc* d, const dl_conv_rows* r, bool any) {
@@ -316,7 +340,7 @@ int check_rows(const dl_conv_desc* d, const dl_conv_rows* r, bool any) {
 }
 
 ConvParams params(const dl_conv_desc* d, const void* s_in, void* s_out, const dl_conv_rows* r, void* y,
-                  int32_t n, int32_t tokens) {
+                  int32_t n, int32_t tokens, bool backward = false) {
   ConvParams p{};
   p.x = r->x;
   p.w = r->w;
@@ -329,7 +353,7 @@ ConvParams params(const dl_conv_desc* d, const void* s_in, void* s_out, const dl
   p.N = tokens;
   p.B = d->num_slots;
   p.D = d->channels;
-  p.len = stretch_len(d, n, tokens);
+  p.len = stretch_len(d, n, tokens, backward);
   return p;
 }
 
@@ -359,7 +383,7 @@ int dl_conv_step(const dl_conv_desc* desc, const void* s_in, void* s_out, const 
 int dl_conv_prefill(const dl_conv_desc* desc, const void* s_in, void* s_out, const dl_conv_rows* rows,
                     void* y, const dl_tables* tables, int32_t n, int32_t tokens, hipStream_t stream) {
   DL_TRY(check_desc(desc));
-  DL_TRY(check_counts(desc, n, tokens));
+  DL_TRY(check_counts(desc, n, tokens, false));
   if (n == 0) return DL_OK;               // nothing to do, whatever the pointers are
   DL_TRY(check_rows(desc, rows, tokens > 0));
   DL_TRY(check_row_tables(tables));
@@ -374,9 +398,9 @@ int dl_conv_prefill(const dl_conv_desc* desc, const void* s_in, void* s_out, con
 
 int dl_conv_workspace_bytes(const dl_conv_desc* desc, int32_t n, int32_t tokens, size_t* bytes) {
   DL_TRY(check_desc(desc));
-  DL_TRY(check_counts(desc, n, tokens));
+  DL_TRY(check_counts(desc, n, tokens, true));
   if (!bytes) return DL_E_NULL;
-  const size_t rows = size_t(stretches(n, tokens, stretch_len(desc, n, tokens)));
+  const size_t rows = size_t(stretches(n, tokens, stretch_len(desc, n, tokens, true)));
   *bytes = n == 0 ? 0 : rows * size_t(desc->channels) * size_t(desc->width + 1) * sizeof(float);
   return DL_OK;
 }
@@ -385,7 +409,7 @@ int dl_conv_backward(const dl_conv_desc* desc, const void* s_in, const dl_conv_r
                      const void* ds_out, const dl_conv_grads* g, const dl_tables* tables, int32_t n,
                      int32_t tokens, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   DL_TRY(check_desc(desc));
-  DL_TRY(check_counts(desc, n, tokens));
+  DL_TRY(check_counts(desc, n, tokens, true));
   if (n == 0) return DL_OK;               // nothing to do, whatever the pointers are
   DL_TRY(check_rows(desc, rows, tokens > 0));
   DL_TRY(check_row_tables(tables));
@@ -398,7 +422,7 @@ int dl_conv_backward(const dl_conv_desc* desc, const void* s_in, const dl_conv_r
   if (!workspace) return DL_E_NULL;
   if (!aligned_to(workspace, 256)) return DL_E_ALIGN;
   if (workspace_bytes < need) return DL_E_SHAPE;
-  ConvParams p = params(desc, s_in, g->ds, rows, g->dx, n, tokens);
+  ConvParams p = params(desc, s_in, g->ds, rows, g->dx, n, tokens, true);
   p.cu = tables->cu_tokens;
   p.seq_slot = tables->seq_slot;
   p.dy = dy;

@@ -24,7 +24,8 @@ struct QkParams {
 };
 
 constexpr int NT = 256;        // threads of a workgroup
-constexpr int V = 8;           // values of a head that a lane holds
+constexpr int V = 8;           // values of a head that a lane holds, in two fours
+constexpr int U = 2;           // heads of queries and of keys that a lane has under way
 
 // cos and sin of position x frequency, the product in 64 bits: an angle of a million radians keeps
 // all of its fraction of a turn.
@@ -36,96 +37,123 @@ __device__ __forceinline__ float2 turn_of(int pos, float freq) {
   return cs;
 }
 
-// The angles of this lane's values, from LDS: halves use 8 of them (the same in a pair's two lanes),
-// pairs 4.
+// A lane's places in a head: eight in a row, but with halves that turn both places of four pairs, so
+// that no lane needs another's.
 enum Turn { NONE = DL_TURN_NONE, HALVES = DL_TURN_HALVES, PAIRS = DL_TURN_PAIRS };
 template <int T>
-struct Angles {
-  static constexpr int M = T == HALVES ? V : T == PAIRS ? V / 2 : 1;
-  float c[M], s[M];
-  int partner;
-  bool turned, first;
-  __device__ __forceinline__ void load(const float2* lds, int li, int rot) {
-    if (T == NONE) return;
-    const int half = rot / 16;                 // lanes of one half
-    turned = li * V < rot;
-    first = li < half;
-    partner = (threadIdx.x & 63) + (!turned ? 0 : first ? half : -half);
-    const int at = !turned ? 0 : T == HALVES ? (first ? li : li - half) * V : li * M;
+struct Places {
+  int lo, hi;                  // first places of the two fours
+  bool turned;
+  __device__ __forceinline__ Places(int li, int rot) {
+    turned = T != NONE && li * V < rot;
+    lo = T == HALVES && turned ? li * 4 : li * V;
+    hi = T == HALVES && turned ? rot / 2 + li * 4 : li * V + 4;
+  }
+  template <typename E>
+  __device__ __forceinline__ void load(const E* row, Raw<4, E> (&r)[2]) const {
+    r[0] = load_raw<4>(row + lo);
+    r[1] = load_raw<4>(row + hi);
+  }
+  template <typename E>
+  __device__ __forceinline__ void store(E* row, const float (&x)[V]) const {
+    const float a[4] = {x[0], x[1], x[2], x[3]}, b[4] = {x[4], x[5], x[6], x[7]};
+    store_row<4>(row + lo, a);
+    store_row<4>(row + hi, b);
+  }
+  __device__ __forceinline__ int at(int i) const { return i < 4 ? lo + i : hi + i - 4; }
+};
+template <typename E>
+__device__ __forceinline__ void widen_fours(const Raw<4, E> (&r)[2], float (&x)[V]) {
 #pragma unroll
-    for (int i = 0; i < M; ++i) {
-      c[i] = turned ? lds[at + i].x : 1.0f;
-      s[i] = turned ? lds[at + i].y : 0.0f;
+  for (int i = 0; i < V; ++i) x[i] = widen(r[i >> 2].v[i & 3]);
+}
+
+// The angles of a lane's four pairs.
+template <int T>
+struct Angles {
+  float c[4], s[4];
+  __device__ __forceinline__ Angles(const float2* lds, int li, bool turned) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 cs = T != NONE && turned ? lds[4 * li + i] : make_float2(1.0f, 0.0f);
+      c[i] = cs.x;
+      s[i] = cs.y;
     }
   }
-  // Turned by the angles, or back.  By all lanes of the head.
+  // Turned by the angles, or back.
   __device__ __forceinline__ void apply(float (&x)[V], bool back) const {
-    if (T == HALVES) {
+    if (T == NONE) return;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float other = __shfl(x[i], partner);
-        const float sn = first != back ? -s[i] : s[i];      // first place: a cos - b sin
-        if (turned) x[i] = fmaf(x[i], c[i], other * sn);
-      }
-    } else if (T == PAIRS) {
-#pragma unroll
-      for (int i = 0; i < V / 2; ++i) {
-        const float sn = back ? -s[i] : s[i], a = x[2 * i], b = x[2 * i + 1];
-        x[2 * i] = fmaf(a, c[i], -b * sn);
-        x[2 * i + 1] = fmaf(a, sn, b * c[i]);
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int u = T == HALVES ? i : 2 * i, v = T == HALVES ? i + 4 : 2 * i + 1;
+      const float sn = back ? -s[i] : s[i], a = x[u], b = x[v];
+      x[u] = fmaf(a, c[i], -b * sn);
+      x[v] = fmaf(a, sn, b * c[i]);
     }
   }
 };
 
+// The angles of `count` tokens, a thread for each: 256 are one turn of the workgroup.
 template <int T>
-__device__ __forceinline__ void fill_angles(const QkParams& p, int token, float2* lds) {
+__device__ __forceinline__ void fill_angles(const QkParams& p, int64_t first, int count, float2* lds) {
   if (T == NONE) return;
-  const int pos = p.pos[token];
-  for (int i = threadIdx.x; i < p.rot / 2; i += NT) lds[i] = turn_of(pos, p.freq[i]);
+  const int half = p.rot / 2;
+  for (int i = threadIdx.x; i < count * half; i += NT) lds[i] = turn_of(p.pos[first + i / half], p.freq[i % half]);
+  __syncthreads();
 }
+
+constexpr int MOST = 8;        // tokens of a workgroup
 
 // A workgroup: `per` tokens, one after the other; D / 8 lanes a head.
 template <int D, int T, bool NORM, typename E>
 __global__ __launch_bounds__(NT) void qk_kernel(QkParams p) {
   constexpr int LPH = D / V, HEADS = NT / LPH;
-  __shared__ float2 lds[2][D / 2];
+  __shared__ float2 lds[T == NONE ? 1 : MOST * D / 2];
   const int li = threadIdx.x % LPH, group = threadIdx.x / LPH;
   const int rows = p.used ? min(max(*p.used, 0), p.N) : p.N;
   const int64_t first = int64_t(blockIdx.x) * p.per;
+  const int count = int(min(int64_t(p.per), rows - first));
+  if (count <= 0) return;
+  const Places<T> place(li, p.rot);
   float w[2][V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    w[0][i] = (p.wq ? p.wq[li * V + i] : 1.0f) * p.q_scale;
-    w[1][i] = p.wk ? p.wk[li * V + i] : 1.0f;
+    w[0][i] = (p.wq ? p.wq[place.at(i)] : 1.0f) * p.q_scale;
+    w[1][i] = p.wk ? p.wk[place.at(i)] : 1.0f;
   }
-  for (int j = 0; j < p.per; ++j) {
+  fill_angles<T>(p, first, count, lds);
+  for (int j = 0; j < count; ++j) {
     const int64_t token = first + j;
-    if (token >= rows) return;
-    fill_angles<T>(p, int(token), lds[j & 1]);
-    if (T != NONE) __syncthreads();
-    Angles<T> turn;
-    turn.load(lds[j & 1], li, p.rot);
+    const Angles<T> turn(lds + j * (p.rot / 2), li, place.turned);
+    const E* in[2] = {static_cast<const E*>(p.q) + token * p.q_stride, static_cast<const E*>(p.k) + token * p.k_stride};
+    E* out[2] = {static_cast<E*>(p.qo) + token * p.H * p.rep * D, static_cast<E*>(p.ko) + token * p.H * p.rep * D};
+    for (int h0 = group; h0 < p.H; h0 += HEADS * U) {
+      Raw<4, E> raw[2][U][2];
 #pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-      const E* in = kind ? static_cast<const E*>(p.k) + token * p.k_stride
-                         : static_cast<const E*>(p.q) + token * p.q_stride;
-      E* out = static_cast<E*>(kind ? p.ko : p.qo) + token * p.H * p.rep * D;
-      for (int h = group; h < p.H; h += HEADS) {
-        float x[V];
-        load_row<V>(in + h * D + li * V, x);
-        float r = 1.0f;
-        if (NORM) {
-          float ss = 0.0f;
+      for (int kind = 0; kind < 2; ++kind)
 #pragma unroll
-          for (int i = 0; i < V; ++i) ss = fmaf(x[i], x[i], ss);
-          r = __builtin_amdgcn_rsqf(fmaf(lanes_sum<D / V>(ss), p.share, p.eps));
+        for (int u = 0; u < U; ++u)
+          if (h0 + u * HEADS < p.H) place.load(in[kind] + (h0 + u * HEADS) * D, raw[kind][u]);
+#pragma unroll
+      for (int kind = 0; kind < 2; ++kind)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int h = h0 + u * HEADS;
+          if (h >= p.H) break;
+          float x[V];
+          widen_fours(raw[kind][u], x);
+          float r = 1.0f;
+          if (NORM) {
+            float ss = 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) ss = fmaf(x[i], x[i], ss);
+            r = __builtin_amdgcn_rsqf(fmaf(lanes_sum<LPH>(ss), p.share, p.eps));
+          }
+#pragma unroll
+          for (int i = 0; i < V; ++i) x[i] *= r * w[kind][i];
+          turn.apply(x, false);
+          for (int c = 0; c < p.rep; ++c) place.store(out[kind] + (int64_t(h) * p.rep + c) * D, x);
         }
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] *= r * w[kind][i];
-        turn.apply(x, false);
-        for (int c = 0; c < p.rep; ++c) store_row<V>(out + (int64_t(h) * p.rep + c) * D + li * V, x);
-      }
     }
   }
 }
@@ -133,38 +161,44 @@ __global__ __launch_bounds__(NT) void qk_kernel(QkParams p) {
 template <int D, int T, bool NORM, typename E>
 __global__ __launch_bounds__(NT) void qk_backward_kernel(QkParams p) {
   constexpr int LPH = D / V, HEADS = NT / LPH;
-  __shared__ float2 lds[2][D / 2];
+  __shared__ float2 lds[T == NONE ? 1 : MOST * D / 2];
   __shared__ float sums[HEADS][D];
   const int li = threadIdx.x % LPH, group = threadIdx.x / LPH;
   const int rows = p.used ? min(max(*p.used, 0), p.N) : p.N;
   const int64_t first = int64_t(blockIdx.x) * p.per;
+  const int count = int(max(min(int64_t(p.per), rows - first), int64_t(0)));
+  const Places<T> place(li, p.rot);
   float w[2][V], dw[2][V] = {};
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    w[0][i] = p.wq ? p.wq[li * V + i] : 1.0f;
-    w[1][i] = p.wk ? p.wk[li * V + i] : 1.0f;
+    w[0][i] = p.wq ? p.wq[place.at(i)] : 1.0f;
+    w[1][i] = p.wk ? p.wk[place.at(i)] : 1.0f;
   }
-  for (int j = 0; j < p.per; ++j) {
+  fill_angles<T>(p, first, count, lds);
+  for (int j = 0; j < count; ++j) {
     const int64_t token = first + j;
-    if (token >= rows) break;
-    fill_angles<T>(p, int(token), lds[j & 1]);
-    if (T != NONE) __syncthreads();
-    Angles<T> turn;
-    turn.load(lds[j & 1], li, p.rot);
+    const Angles<T> turn(lds + j * (p.rot / 2), li, place.turned);
+    const E* in[2] = {static_cast<const E*>(p.q) + token * p.q_stride, static_cast<const E*>(p.k) + token * p.k_stride};
+    const E* up[2] = {static_cast<const E*>(p.dqo) + token * p.H * p.rep * D,
+                      static_cast<const E*>(p.dko) + token * p.H * p.rep * D};
+    E* out[2] = {static_cast<E*>(p.qo) + token * p.H * D, static_cast<E*>(p.ko) + token * p.H * D};
+    for (int h = group; h < p.H; h += HEADS) {
+      Raw<4, E> raw[2][2], own[2][2];
 #pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-      const E* in = kind ? static_cast<const E*>(p.k) + token * p.k_stride
-                         : static_cast<const E*>(p.q) + token * p.q_stride;
-      const E* up = static_cast<const E*>(kind ? p.dko : p.dqo) + token * p.H * p.rep * D;
-      E* out = static_cast<E*>(kind ? p.ko : p.qo) + token * p.H * D;
-      const float scale = kind ? 1.0f : p.q_scale;
-      for (int h = group; h < p.H; h += HEADS) {
+      for (int kind = 0; kind < 2; ++kind) {
+        place.load(in[kind] + h * D, raw[kind]);
+        place.load(up[kind] + int64_t(h) * p.rep * D, own[kind]);
+      }
+#pragma unroll
+      for (int kind = 0; kind < 2; ++kind) {
         float x[V], g[V];
-        load_row<V>(in + h * D + li * V, x);
-        load_row<V>(up + int64_t(h) * p.rep * D + li * V, g);
+        widen_fours(raw[kind], x);
+        widen_fours(own[kind], g);
         for (int c = 1; c < p.rep; ++c) {
+          Raw<4, E> next[2];
           float more[V];
-          load_row<V>(up + (int64_t(h) * p.rep + c) * D + li * V, more);
+          place.load(up[kind] + (int64_t(h) * p.rep + c) * D, next);
+          widen_fours(next, more);
 #pragma unroll
           for (int i = 0; i < V; ++i) g[i] += more[i];
         }
@@ -172,20 +206,21 @@ __global__ __launch_bounds__(NT) void qk_backward_kernel(QkParams p) {
         float ss = 0.0f, along = 0.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) ss = fmaf(x[i], x[i], ss);
-        const float r = NORM ? __builtin_amdgcn_rsqf(fmaf(lanes_sum<D / V>(ss), p.share, p.eps)) : 1.0f;
+        const float r = NORM ? __builtin_amdgcn_rsqf(fmaf(lanes_sum<LPH>(ss), p.share, p.eps)) : 1.0f;
+        const float scale = (kind ? 1.0f : p.q_scale) * r;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          g[i] *= scale * r;
+          g[i] *= scale;
           dw[kind][i] = fmaf(g[i], x[i], dw[kind][i]);
           g[i] *= w[kind][i];
           along = fmaf(g[i], x[i], along);
         }
         if (NORM) {
-          const float back = lanes_sum<D / V>(along) * r * r * p.share;
+          const float back = lanes_sum<LPH>(along) * r * r * p.share;
 #pragma unroll
           for (int i = 0; i < V; ++i) g[i] = fmaf(-back, x[i], g[i]);
         }
-        store_row<V>(out + int64_t(h) * D + li * V, g);
+        place.store(out[kind] + int64_t(h) * D, g);
       }
     }
   }
@@ -194,7 +229,7 @@ __global__ __launch_bounds__(NT) void qk_backward_kernel(QkParams p) {
   for (int kind = 0; kind < 2; ++kind) {
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < V; ++i) sums[group][li * V + i] = dw[kind][i];
+    for (int i = 0; i < V; ++i) sums[group][place.at(i)] = dw[kind][i];
     __syncthreads();
     if (threadIdx.x < D) {
       float s = 0.0f;
@@ -228,8 +263,9 @@ hipError_t launch_dim(const dl_qk_desc* d, const QkParams& p, bool backward, int
   }
 }
 
-// Tokens of a workgroup.
-int tokens_per(int32_t n, bool backward) { return backward ? std::max(1, std::min(8, n / 1024)) : 1; }
+// Tokens of a workgroup: they share its angles' arithmetic (12345 rows of 32 heads: 132 us with a token a
+// workgroup, 79 with four), and backward the partial sums.
+int tokens_per(int32_t n, bool backward) { return std::max(1, std::min(backward ? MOST : 4, n / 512)); }
 
 int check_desc(const dl_qk_desc* d) {
   if (!d) return DL_E_NULL;

@@ -74,8 +74,13 @@ __device__ __forceinline__ float halves_sum8(float a, float b) {
   return (last ? b : a) + from_lane<0x128>(last ? a : b);   // row_ror:8
 }
 
-// 1 / (1 + e^-x): 0 and 1 at the infinities.
-__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + expf(-x)); }
+constexpr float LOG2E = 1.4426950408889634f;
+
+// 1 / (1 + e^-x): 0 and 1 at the infinities.  The exponential's argument is rounded once more than x is, so
+// where e^-x matters this is good to 2^-24 (|x| + 3) of itself; four instructions.
+__device__ __forceinline__ float sigmoid(float x) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -LOG2E));
+}
 
 // ------------------------------------------------------------------ stretches of sequences
 // Sequences are cut into stretches of `len` tokens.  Stretch j of sequence i, whose first token is

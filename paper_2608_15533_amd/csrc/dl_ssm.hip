@@ -112,7 +112,7 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
 #pragma unroll
         for (int i = 0; i < NW; ++i) y[e] += partial[i][te][ce + e];
         y[e] = fmaf(skip[e], x[e], y[e]);
-        if (p.z) y[e] *= z[e] * quick_sigmoid(z[e]);
+        if (p.z) y[e] *= z[e] * sigmoid(z[e]);
       }
       ys.store(j, y);
     }
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmParams p) {
   if (p.skip) y = fmaf(p.skip[c], x, y);
   if (p.z) {
     const float z = widen(static_cast<const T*>(p.z)[i * p.z_stride + c]);
-    y *= z * quick_sigmoid(z);
+    y *= z * sigmoid(z);
   }
   narrow(static_cast<T*>(p.y) + int64_t(i) * p.D + c, y);
 }

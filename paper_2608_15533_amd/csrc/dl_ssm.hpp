@@ -41,8 +41,6 @@ struct SsmParams {
   int32_t n, N, B, D, S, len, blocks;   // blocks: of 64 channels
 };
 
-constexpr float LOG2E = 1.4426950408889634f;
-
 __device__ __forceinline__ float decay(float d, float a2) { return __builtin_amdgcn_exp2f(d * a2); }
 
 // log(1 + e^x) = max(x, 0) + log(1 + e), e = e^-|x|.  The power's exponent is -|x| log2 e with what its
@@ -64,11 +62,6 @@ __device__ __forceinline__ float softplus(float x) {
   r = fmaf(r * s, q, q);
   return x > 20.0f ? x : fmaf(2.0f, r, fmaxf(x, 0.0f));
 }
-// 1 / (1 + e^-x), good to 2^-24 (|x| + 3) of itself.
-__device__ __forceinline__ float quick_sigmoid(float x) {
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -LOG2E));
-}
-
 // Four consecutive values of a row that is the same for all lanes, through scalar registers.
 template <typename T>
 struct Four;

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
         const float d = mine ? softplus(widen(rd.v[e]) + part.bias[e]) : 0.0f, z = widen(rz.v[e]);
         step[part.te][part.ce + e] = d;
         input[part.te][part.ce + e] = mine ? d * widen(rx.v[e]) : 0.0f;
-        grad[part.te][part.ce + e] = mine ? widen(ro.v[e]) * (p.z ? z * quick_sigmoid(z) : 1.0f) : 0.0f;
+        grad[part.te][part.ce + e] = mine ? widen(ro.v[e]) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
         total[e] += d;
       }
     }
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
           const float d = mine ? softplus(widen(kd.v[e]) + part.bias[e]) : 0.0f, z = widen(kz.v[e]);
           step[part.te][part.ce + e] = d;
           input[part.te][part.ce + e] = mine ? d * widen(kx.v[e]) : 0.0f;
-          grad[part.te][part.ce + e] = mine ? widen(ko.v[e]) * (p.z ? z * quick_sigmoid(z) : 1.0f) : 0.0f;
+          grad[part.te][part.ce + e] = mine ? widen(ko.v[e]) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
         }
       }
       fetch(j - 1, true);
@@ -295,10 +295,10 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
             gm += sum_gm[i][part.te][part.ce + e];
             if (p.z) ch += sum_ch[i][part.te][part.ce + e];
           }
-          const float x = widen(kx.v[e]), z = widen(kz.v[e]), sz = quick_sigmoid(z);
+          const float x = widen(kx.v[e]), z = widen(kz.v[e]), sz = sigmoid(z);
           const float up = grad[part.te][part.ce + e];
           dx[e] = fmaf(step[part.te][part.ce + e], gb, skip[e] * up);
-          ddt[e] = quick_sigmoid(widen(kd.v[e]) + part.bias[e]) * fmaf(x, gb, gm);
+          ddt[e] = sigmoid(widen(kd.v[e]) + part.bias[e]) * fmaf(x, gb, gm);
           dskip[e] = fmaf(up, x, dskip[e]);
           dbias[e] += ddt[e];
           dz[e] = widen(ko.v[e]) * fmaf(skip[e], x, ch) * sz * (1.0f + z * (1.0f - sz));

@@ -250,7 +250,7 @@ def _need(t, name, dtype, shape, device=None):
         raise ValueError(f"{name} must be a device tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != tuple(shape):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -604,9 +604,21 @@ def _workspace(workspace, maker):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
+class _Rows:
+    """What a call reads besides states: its tensors, the descriptor it was made for, the struct."""
+
+    def _keep(self, desc, n, tensors, struct):
+        self.n, self.tensors, self.struct = n, tensors, struct
+        self.ref, self.raw, self.sizes = ctypes.byref(struct), bytes(desc), _sizes(desc)
+        self.device = tensors[0].get_device()
+        for t in tensors:
+            if t is not None and t.get_device() != self.device:
+                raise ValueError(f"tensors on cuda:{self.device} and {t.device}")
+
+
 def _made_for(desc, rows, tables=None, grads=None):
     """The rows (and gradients) were made for this descriptor and these tables."""
-    if rows.sizes != _sizes(desc):
+    if rows.raw != bytes(desc) and rows.sizes != _sizes(desc):
         raise ValueError("the rows were made for another descriptor")
     if tables is not None and rows.n != tables.tokens:
         raise ValueError(f"{rows.n} rows but the tables are for {tables.tokens}")
@@ -622,6 +634,17 @@ def _sizes(desc):
     return tuple(getattr(desc, k) for k, _ in desc._fields_ if k != "num_slots")
 
 
+def _stream_of(stream, rows, *tensors):
+    """The stream to launch on; every tensor has to be on the current device, whose stream it is."""
+    cur = torch.cuda.current_device()
+    if rows.device != cur:
+        raise ValueError(f"tensors are on cuda:{rows.device}, the current device is cuda:{cur}")
+    for t in tensors:
+        if t is not None and t.get_device() != cur:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{cur}")
+    return _raw_stream(cur) if stream is None and _raw_stream is not None else _stream(stream)
+
+
 def _bytes(call, where, desc, *args):
     out = ctypes.c_size_t(0)
     _check(call(ctypes.byref(desc), *args, ctypes.byref(out)), where)
@@ -634,7 +657,7 @@ def make_conv_desc(B, channels, width, in_dtype="bf16", activation="silu"):
                         DTYPE_IDS[in_dtype])
 
 
-class ConvRows:
+class ConvRows(_Rows):
     """What a convolution reads: token rows x [n,D] in the input dtype (columns of a wider tensor
     will do), w [D,W] and bias [D] (or None) in fp32."""
 
@@ -642,8 +665,7 @@ class ConvRows:
         stride = _need_rows(x, "x", _in_torch_dtype(desc), (n, desc.channels))
         _need(w, "w", torch.float32, (desc.channels, desc.width))
         _optional(bias, "bias", torch.float32, (desc.channels,))
-        self.n, self.sizes, self.tensors = n, _sizes(desc), (x, w, bias)
-        self.struct = dl_conv_rows(_ptr(x), stride, _ptr(w), _ptr(bias))
+        self._keep(desc, n, (x, w, bias), dl_conv_rows(_ptr(x), stride, _ptr(w), _ptr(bias)))
 
 
 class ConvGrads:
@@ -672,12 +694,13 @@ def dl_conv_step(desc, s_in, s_out, rows, y, slots=None, stream=None):
     W - 1 inputs) from s_in [B,W-1,D] to s_out (may be s_in)."""
     sp, n = _rows(desc, slots, rows.n)
     _made_for(desc, rows)
-    _need(s_in, "s_in", *_conv_state(desc))
-    _need(s_out, "s_out", *_conv_state(desc))
-    _need(y, "y", _in_torch_dtype(desc), (n, desc.channels))
-    _on_current_device(*rows.tensors, s_in, s_out, y, slots)
-    _check(_lib.dl_conv_step(ctypes.byref(desc), _ptr(s_in), _ptr(s_out), ctypes.byref(rows.struct),
-                             _ptr(y), sp, n, _stream(stream)), "dl_conv_step")
+    state = _conv_state(desc)
+    _need(s_in, "s_in", *state)
+    _need(s_out, "s_out", *state)
+    _need(y, "y", state[0], (n, desc.channels))
+    st = _stream_of(stream, rows, s_in, s_out, y, slots)
+    _check(_lib.dl_conv_step(ctypes.byref(desc), _ptr(s_in), _ptr(s_out), rows.ref,
+                             _ptr(y), sp, n, st), "dl_conv_step")
 
 
 def dl_conv_prefill(desc, s_in, s_out, rows, y, tables, stream=None):
@@ -687,10 +710,10 @@ def dl_conv_prefill(desc, s_in, s_out, rows, y, tables, stream=None):
     _optional(s_in, "s_in", *_conv_state(desc))
     _need(s_out, "s_out", *_conv_state(desc))
     _need(y, "y", _in_torch_dtype(desc), (rows.n, desc.channels))
-    _on_current_device(*rows.tensors, s_in, s_out, y, tables.err)
+    st = _stream_of(stream, rows, s_in, s_out, y, tables.err)
     _check(_lib.dl_conv_prefill(ctypes.byref(desc), _ptr(s_in), _ptr(s_out),
-                                ctypes.byref(rows.struct), _ptr(y), ctypes.byref(tables.struct),
-                                tables.n, tables.tokens, _stream(stream)), "dl_conv_prefill")
+                                rows.ref, _ptr(y), ctypes.byref(tables.struct),
+                                tables.n, tables.tokens, st), "dl_conv_prefill")
 
 
 def conv_workspace(desc, n, tokens, device="cuda"):
@@ -707,11 +730,11 @@ def dl_conv_backward(desc, s_in, rows, dy, ds_out, grads, tables, workspace, str
     _optional(ds_out, "ds_out", *_conv_state(desc))
     _need(dy, "dy", _in_torch_dtype(desc), (rows.n, desc.channels))
     wp, wn = _workspace(workspace, "conv_workspace")
-    _on_current_device(*rows.tensors, s_in, dy, ds_out, grads.dx, grads.ds, tables.err, workspace)
-    _check(_lib.dl_conv_backward(ctypes.byref(desc), _ptr(s_in), ctypes.byref(rows.struct), _ptr(dy),
+    st = _stream_of(stream, rows, s_in, dy, ds_out, grads.dx, grads.ds, tables.err, workspace)
+    _check(_lib.dl_conv_backward(ctypes.byref(desc), _ptr(s_in), rows.ref, _ptr(dy),
                                  _ptr(ds_out), ctypes.byref(grads.struct),
                                  ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,
-                                 _stream(stream)), "dl_conv_backward")
+                                 st), "dl_conv_backward")
 
 
 def make_qk_desc(H, d, norm="l2", turn="none", rot=None, rep=1, in_dtype="bf16", eps=1e-6,
@@ -723,7 +746,7 @@ def make_qk_desc(H, d, norm="l2", turn="none", rot=None, rep=1, in_dtype="bf16",
                       DTYPE_IDS[in_dtype], eps, q_scale)
 
 
-class QkRows:
+class QkRows(_Rows):
     """What the norm of queries and keys reads: q, k [n,H,d] in the input dtype (columns of a wider
     tensor will do), positions pos [n] int32 and frequencies freq [rot/2] fp32 where they turn,
     weights wq, wk [d] fp32 (both or neither).  ``tables``: rows behind its sequences are left out."""
@@ -743,9 +766,9 @@ class QkRows:
         if tables is not None and tables.tokens != n:
             raise ValueError(f"{n} rows but the tables are for {tables.tokens}")
         used = None if tables is None else tables.cu_tokens[tables.n:]
-        self.n, self.sizes, self.tensors = n, _sizes(desc), (q, k, pos, freq, wq, wk, used)
-        self.struct = dl_qk_rows(_ptr(q), _ptr(k), qs, ks, _ptr(pos), _ptr(freq), _ptr(wq),
-                                 _ptr(wk), _ptr(used))
+        self._keep(desc, n, (q, k, pos, freq, wq, wk, used),
+                   dl_qk_rows(_ptr(q), _ptr(k), qs, ks, _ptr(pos), _ptr(freq), _ptr(wq), _ptr(wk),
+                              _ptr(used)))
 
 
 class QkGrads:
@@ -767,9 +790,9 @@ def dl_qk_norm(desc, rows, q_out, k_out, stream=None):
     out = (_in_torch_dtype(desc), (rows.n, desc.heads * desc.rep, desc.head_dim))
     _need(q_out, "q_out", *out)
     _need(k_out, "k_out", *out)
-    _on_current_device(*rows.tensors, q_out, k_out)
-    _check(_lib.dl_qk_norm(ctypes.byref(desc), ctypes.byref(rows.struct), _ptr(q_out), _ptr(k_out),
-                           rows.n, _stream(stream)), "dl_qk_norm")
+    st = _stream_of(stream, rows, q_out, k_out)
+    _check(_lib.dl_qk_norm(ctypes.byref(desc), rows.ref, _ptr(q_out), _ptr(k_out),
+                           rows.n, st), "dl_qk_norm")
 
 
 def qk_workspace(desc, n, device="cuda"):
@@ -785,10 +808,10 @@ def dl_qk_norm_backward(desc, rows, dq_out, dk_out, grads, workspace, stream=Non
     _need(dq_out, "dq_out", *out)
     _need(dk_out, "dk_out", *out)
     wp, wn = _workspace(workspace, "qk_workspace")
-    _on_current_device(*rows.tensors, dq_out, dk_out, grads.dq, grads.dk, workspace)
-    _check(_lib.dl_qk_norm_backward(ctypes.byref(desc), ctypes.byref(rows.struct), _ptr(dq_out),
+    st = _stream_of(stream, rows, dq_out, dk_out, grads.dq, grads.dk, workspace)
+    _check(_lib.dl_qk_norm_backward(ctypes.byref(desc), rows.ref, _ptr(dq_out),
                                     _ptr(dk_out), ctypes.byref(grads.struct), rows.n, wp, wn,
-                                    _stream(stream)), "dl_qk_norm_backward")
+                                    st), "dl_qk_norm_backward")
 
 
 def make_ssm_desc(B, channels, states, in_dtype="bf16"):
@@ -800,7 +823,7 @@ def _ssm_state(desc):
     return torch.float32, (desc.num_slots, desc.channels, desc.states)
 
 
-class SsmRows:
+class SsmRows(_Rows):
     """What a selective scan reads: token rows x, dt and z (or None: no gate) [n,D], Bm and Cm [n,S]
     in the input dtype (columns of a wider tensor will do); A [D,S], skip [D] and dt_bias [D] (or
     None) in fp32."""
@@ -813,10 +836,9 @@ class SsmRows:
         _need(A, "A", torch.float32, (D, S))
         _optional(skip, "skip", torch.float32, (D,))
         _optional(dt_bias, "dt_bias", torch.float32, (D,))
-        self.n, self.sizes = n, _sizes(desc)
-        self.tensors = (x, dt, z, Bm, Cm, A, skip, dt_bias)
-        self.struct = dl_ssm_rows(_ptr(x), _ptr(dt), _ptr(z), _ptr(Bm), _ptr(Cm), *strides, _ptr(A),
-                                  _ptr(skip), _ptr(dt_bias))
+        self._keep(desc, n, (x, dt, z, Bm, Cm, A, skip, dt_bias),
+                   dl_ssm_rows(_ptr(x), _ptr(dt), _ptr(z), _ptr(Bm), _ptr(Cm), *strides, _ptr(A),
+                               _ptr(skip), _ptr(dt_bias)))
 
 
 class SsmGrads:
@@ -842,12 +864,13 @@ def dl_ssm_step(desc, h_in, h_out, rows, y, slots=None, stream=None):
     h_out (may be h_in)."""
     sp, n = _rows(desc, slots, rows.n)
     _made_for(desc, rows)
-    _need(h_in, "h_in", *_ssm_state(desc))
-    _need(h_out, "h_out", *_ssm_state(desc))
+    state = _ssm_state(desc)
+    _need(h_in, "h_in", *state)
+    _need(h_out, "h_out", *state)
     _need(y, "y", _in_torch_dtype(desc), (n, desc.channels))
-    _on_current_device(*rows.tensors, h_in, h_out, y, slots)
-    _check(_lib.dl_ssm_step(ctypes.byref(desc), _ptr(h_in), _ptr(h_out), ctypes.byref(rows.struct),
-                            _ptr(y), sp, n, _stream(stream)), "dl_ssm_step")
+    st = _stream_of(stream, rows, h_in, h_out, y, slots)
+    _check(_lib.dl_ssm_step(ctypes.byref(desc), _ptr(h_in), _ptr(h_out), rows.ref,
+                            _ptr(y), sp, n, st), "dl_ssm_step")
 
 
 def ssm_workspace(desc, n, tokens, backward=False, device="cuda"):
@@ -866,10 +889,10 @@ def dl_ssm_prefill(desc, h_in, h_out, rows, y, tables, workspace, stream=None):
     _need(h_out, "h_out", *_ssm_state(desc))
     _need(y, "y", _in_torch_dtype(desc), (rows.n, desc.channels))
     wp, wn = _workspace(workspace, "ssm_workspace")
-    _on_current_device(*rows.tensors, h_in, h_out, y, tables.err, workspace)
-    _check(_lib.dl_ssm_prefill(ctypes.byref(desc), _ptr(h_in), _ptr(h_out), ctypes.byref(rows.struct),
+    st = _stream_of(stream, rows, h_in, h_out, y, tables.err, workspace)
+    _check(_lib.dl_ssm_prefill(ctypes.byref(desc), _ptr(h_in), _ptr(h_out), rows.ref,
                                _ptr(y), ctypes.byref(tables.struct), tables.n, tables.tokens, wp, wn,
-                               _stream(stream)), "dl_ssm_prefill")
+                               st), "dl_ssm_prefill")
 
 
 def dl_ssm_backward(desc, h_in, rows, dy, dh_out, grads, tables, workspace, stream=None):
@@ -880,7 +903,7 @@ def dl_ssm_backward(desc, h_in, rows, dy, dh_out, grads, tables, workspace, stre
     _optional(dh_out, "dh_out", *_ssm_state(desc))
     _need(dy, "dy", _in_torch_dtype(desc), (rows.n, desc.channels))
     wp, wn = _workspace(workspace, "ssm_workspace")
-    _on_current_device(*rows.tensors, h_in, dy, dh_out, grads.dx, grads.ds, tables.err, workspace)
-    _check(_lib.dl_ssm_backward(ctypes.byref(desc), _ptr(h_in), ctypes.byref(rows.struct), _ptr(dy),
+    st = _stream_of(stream, rows, h_in, dy, dh_out, grads.dx, grads.ds, tables.err, workspace)
+    _check(_lib.dl_ssm_backward(ctypes.byref(desc), _ptr(h_in), rows.ref, _ptr(dy),
                                 _ptr(dh_out), ctypes.byref(grads.struct), ctypes.byref(tables.struct),
-                                tables.n, tables.tokens, wp, wn, _stream(stream)), "dl_ssm_backward")
+                                tables.n, tables.tokens, wp, wn, st), "dl_ssm_backward")
