@@ -138,9 +138,9 @@ template <int S, typename T>
 __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmParams p) {
   typedef Part<S, T> P;
   constexpr int TB = P::TB, EV = P::EV, NW = S / 4, TILES = ssm_grad_tokens(S) / TB;
-  __shared__ __attribute__((aligned(16))) float step[TB][64], input[TB][64], grad[TB][64];
+  __shared__ __attribute__((aligned(16))) float steps[TILES * TB][64], inputs[TILES * TB][64], grad[TB][64];
   __shared__ __attribute__((aligned(16))) float sum_gb[NW][TB][64], sum_gm[NW][TB][64], sum_ch[NW][TB][64];
-  __shared__ __attribute__((aligned(16))) f32x4 before[TILES][NW][64];
+  __shared__ __attribute__((aligned(16))) f32x4 before[TILES - 2][NW][64];   // of the first and last: not here
   const int f = blockIdx.x / p.blocks, block = int(blockIdx.x % p.blocks), c0 = block * 64;
   const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, f);
   const int lane = threadIdx.x & 63, w = wave_index(), c = c0 + lane;
@@ -187,29 +187,38 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
       if (p.z) rz = zs.load(j);
     };
     fetch(0, tiles == 1);
-    for (int j = 0; j < tiles; ++j) {
-      before[j][w][lane] = f32x4{h[0], h[1], h[2], h[3]};
-      if (j + 1 == tiles) break;
-      TileRows<TB, false, T> rows;
-      rows.load(bp + int64_t(j * TB) * p.b_stride, p.b_stride, nullptr, 0);
-      if (part.te < TB) {
+    // Steps and inputs of a tile, and what its tokens' gradients are made of.
+    auto stage = [&](int j, int count, bool own_steps, bool gradients) {
+      if (part.te >= TB) return;
+      const bool mine = part.live && part.te < count;
+      const int t = j * TB + part.te;
 #pragma unroll
-        for (int e = 0; e < EV; ++e) {
-          const float d = part.live ? softplus(widen(rd.v[e]) + part.bias[e]) : 0.0f;
-          step[part.te][part.ce + e] = d;
-          input[part.te][part.ce + e] = d * widen(rx.v[e]);
+      for (int e = 0; e < EV; ++e) {
+        if (own_steps) {
+          const float d = mine ? softplus(widen(rd.v[e]) + part.bias[e]) : 0.0f;
+          steps[t][part.ce + e] = d;
+          inputs[t][part.ce + e] = mine ? d * widen(rx.v[e]) : 0.0f;
+        }
+        if (gradients) {
+          const float z = widen(rz.v[e]);
+          grad[part.te][part.ce + e] = mine ? widen(ro.v[e]) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
         }
       }
+    };
+    for (int j = 0; j + 1 < tiles; ++j) {
+      if (j > 0) before[j - 1][w][lane] = f32x4{h[0], h[1], h[2], h[3]};
+      TileRows<TB, false, T> rows;
+      rows.load(bp + int64_t(j * TB) * p.b_stride, p.b_stride, nullptr, 0);
+      stage(j, TB, true, false);
       fetch(j + 1, j + 2 == tiles);
       rows.settle();
       __syncthreads();
 #pragma unroll
       for (int t = 0; t < TB; ++t) {
-        const float d = step[t][lane], u = input[t][lane];
+        const float d = steps[j * TB + t][lane], u = inputs[j * TB + t][lane];
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = fmaf(decay(d, a2[i]), h[i], u * rows.B[t].at(i));
       }
-      __syncthreads();
     }
     for (int j = tiles - 1; j >= 0; --j) {
       const int t0 = j * TB, count = min(TB, s.count - t0);
@@ -217,23 +226,18 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
       TileRows<TB, true, T> rows;
       rows.load(bp + int64_t(t0) * p.b_stride, p.b_stride, cp + int64_t(t0) * p.c_stride, p.c_stride, count);
       const Raw<EV, T> kx = rx, kd = rd, ko = ro, kz = rz;
-      if (part.te < TB) {
-#pragma unroll
-        for (int e = 0; e < EV; ++e) {
-          const float d = mine ? softplus(widen(kd.v[e]) + part.bias[e]) : 0.0f, z = widen(kz.v[e]);
-          step[part.te][part.ce + e] = d;
-          input[part.te][part.ce + e] = mine ? d * widen(kx.v[e]) : 0.0f;
-          grad[part.te][part.ce + e] = mine ? widen(ko.v[e]) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
-        }
-      }
+      stage(j, count, j + 1 == tiles, true);
       fetch(j - 1, true);
       rows.settle();
       __syncthreads();
-      {
-        const f32x4 v = before[j][w][lane];
+      if (j + 1 < tiles) {                       // the last tile's are in hand
+        f32x4 v{};
+        if (j > 0) v = before[j - 1][w][lane];
+        else if (live && hp) v = *reinterpret_cast<const f32x4*>(hp);
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = v[i];
       }
+      const float(*step)[64] = steps + t0, (*input)[64] = inputs + t0;
       auto walk = [&](auto whole) {
         constexpr bool ALL = decltype(whole)::value;
         float a[TB][4], m[TB][4];
@@ -297,7 +301,7 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
           }
           const float x = widen(kx.v[e]), z = widen(kz.v[e]), sz = sigmoid(z);
           const float up = grad[part.te][part.ce + e];
-          dx[e] = fmaf(step[part.te][part.ce + e], gb, skip[e] * up);
+          dx[e] = fmaf(steps[t0 + part.te][part.ce + e], gb, skip[e] * up);
           ddt[e] = sigmoid(widen(kd.v[e]) + part.bias[e]) * fmaf(x, gb, gm);
           dskip[e] = fmaf(up, x, dskip[e]);
           dbias[e] += ddt[e];
@@ -308,7 +312,7 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
         store_row<EV>(static_cast<T*>(p.ddt) + to + out, ddt);
         if (p.z) store_row<EV>(static_cast<T*>(p.dz) + to + out, dz);
       }
-      // What a thread reads of step and grad here, it alone writes in the next tile.
+      // What a thread reads of grad here, it alone writes in the next tile.
     }
     if (s.begins() && p.h_out && live)
       *reinterpret_cast<f32x4*>(p.h_out + state) = f32x4{g[0], g[1], g[2], g[3]};
@@ -323,8 +327,8 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
   if (part.te < TB) {
 #pragma unroll
     for (int e = 0; e < EV; ++e) {
-      step[part.te][part.ce + e] = dskip[e];
-      input[part.te][part.ce + e] = dbias[e];
+      steps[part.te][part.ce + e] = dskip[e];
+      inputs[part.te][part.ce + e] = dbias[e];
     }
   }
   __syncthreads();
@@ -332,8 +336,8 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
     float a = 0.0f, b = 0.0f;
 #pragma unroll
     for (int t = 0; t < TB; ++t) {
-      a += step[t][lane];
-      b += input[t][lane];
+      a += steps[t][lane];
+      b += inputs[t][lane];
     }
     sums[int64_t(p.D) * S + c] = a;
     sums[int64_t(p.D) * (S + 1) + c] = b;
