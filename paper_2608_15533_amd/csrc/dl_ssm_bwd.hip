@@ -4,10 +4,10 @@
 namespace dl {
 namespace {
 
-// Tokens whose steps lie in LDS at a time, and whose decays and states a wave holds in registers: 8 (16
-// spill), or 4 where a workgroup of 16 waves leaves 128 registers a lane.
+// Tokens whose steps lie in LDS at a time, and whose decays and states a wave holds in registers: with 16 a
+// wave needs 255 of them, two to a SIMD.
 template <int S>
-constexpr int tile_of = S == 64 ? 4 : 8;
+constexpr int tile_of = S == 16 ? 8 : 4;
 
 // A thread's part of a tile: one token, EV channels.
 template <int S, typename T>
