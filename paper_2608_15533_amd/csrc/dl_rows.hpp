@@ -100,28 +100,45 @@ __host__ __device__ inline int64_t stretches(int64_t n, int64_t tokens, int len)
   return tokens / len + n;
 }
 
-// By all lanes of a wave, for a number that is the same in all of them: 64 sequences are looked at
-// at a time.  Whatever the tables hold, what comes back lies within N rows and B slots.
+// By all lanes of a wave, for a number that is the same in all of them.  Up to 63 sequences are looked at
+// at once, in one trip to memory; more 64 at a time.  Whatever the tables hold, what comes back lies
+// within N rows and B slots.
 __device__ __forceinline__ Stretch find_stretch(const int32_t* cu, const int32_t* seq_slot, int n,
                                                 int N, int B, int len, int f) {
   const int lane = threadIdx.x & 63;
   auto row = [&](int i) { return min(max(cu[i], 0), N); };
-  int lo = 0, size = n;
-  while (size > 1) {
-    const int step = (size + 63) >> 6, i = lo + lane * step;
-    const bool at_or_before = lane * step < size && row(i) / len + i <= f;
-    const int hits = __popcll(__ballot(at_or_before));
-    const int skip = hits > 0 ? (hits - 1) * step : 0;
-    lo += skip;
-    size = min(step, size - skip);
+  int seq, begin, end, slot;
+  if (n < 64) {
+    const int c = row(min(lane, n)), at = seq_slot[min(lane, n - 1)];
+    const int hits = __popcll(__ballot(lane < n && c / len + lane <= f));
+    seq = __builtin_amdgcn_readfirstlane(max(hits - 1, 0));
+    begin = __builtin_amdgcn_readlane(c, seq);
+    end = __builtin_amdgcn_readlane(c, seq + 1);
+    slot = __builtin_amdgcn_readlane(at, seq);
+  } else {
+    int lo = 0, size = n;
+    while (size > 1) {
+      const int step = (size + 63) >> 6, i = lo + lane * step;
+      const bool at_or_before = lane * step < size && row(i) / len + i <= f;
+      const int hits = __popcll(__ballot(at_or_before));
+      const int skip = hits > 0 ? (hits - 1) * step : 0;
+      lo += skip;
+      size = min(step, size - skip);
+    }
+    seq = lo;
+    begin = row(lo);
+    end = row(lo + 1);
+    slot = seq_slot[lo];
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
   Stretch s;
-  s.seq = lo;
-  s.seq_first = __builtin_amdgcn_readfirstlane(row(lo));
-  s.seq_len = max(__builtin_amdgcn_readfirstlane(row(lo + 1)) - s.seq_first, 0);
-  s.slot = __builtin_amdgcn_readfirstlane(seq_slot[lo]);
-  const int64_t off = int64_t(f - (s.seq_first / len + lo)) * len;
+  s.seq = __builtin_amdgcn_readfirstlane(seq);
+  s.slot = __builtin_amdgcn_readfirstlane(slot);
+  s.seq_first = __builtin_amdgcn_readfirstlane(begin);
+  s.seq_len = max(__builtin_amdgcn_readfirstlane(end) - s.seq_first, 0);
+  // The division is the vector unit's: its result is told to be the same in all lanes, or all that follows
+  // from it is taken for a lane's own.
+  const int before = __builtin_amdgcn_readfirstlane(s.seq_first / len);
+  const int64_t off = int64_t(f - (before + s.seq)) * len;
   s.idle = off < 0 || off > s.seq_len || (off > 0 && off == s.seq_len) || s.slot < 0 || s.slot >= B;
   s.first = s.idle ? 0 : s.seq_first + int(off);
   s.count = s.idle ? 0 : min(len, s.seq_len - int(off));
