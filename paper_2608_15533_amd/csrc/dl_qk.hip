@@ -65,7 +65,7 @@ struct Places {
 template <typename E>
 __device__ __forceinline__ void widen_fours(const Raw<4, E> (&r)[2], float (&x)[V]) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) x[i] = widen(r[i >> 2].v[i & 3]);
+  for (int i = 0; i < V; ++i) x[i] = r[i >> 2].get(i & 3);
 }
 
 // The angles of a lane's four pairs.

@@ -16,10 +16,30 @@
 namespace dl {
 
 // ------------------------------------------------------------------ rows
-// V consecutive values: 8, 16 or 32 bytes, aligned to 16 at most.
+// V consecutive values as they are stored: 2 to 32 bytes, aligned to 16 at most.  Kept as whole words, so
+// that a row loaded ahead is not waited for until its values are asked for.
 template <int V, typename T>
 struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Raw {
-  T v[V];
+  uint32_t w[V * sizeof(T) / 4];
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+  }
+  __device__ __forceinline__ void set(const float (&x)[V]) {
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+#pragma unroll
+    for (int i = 0; i < int(V * sizeof(T) / 4); ++i) {
+      if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(x[i]);
+      else w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2 * i], x[2 * i + 1]}), bf16x2));
+    }
+  }
+};
+template <>
+struct Raw<1, uint16_t> {
+  uint16_t w;
+  __device__ __forceinline__ float get(int) const { return widen(w); }
+  __device__ __forceinline__ void set(const float (&x)[1]) { narrow(&w, x[0]); }
 };
 template <int V, typename T>
 __device__ __forceinline__ Raw<V, T> load_raw(const T* p) {
@@ -28,7 +48,7 @@ __device__ __forceinline__ Raw<V, T> load_raw(const T* p) {
 template <int V, typename T>
 __device__ __forceinline__ void widen_row(const Raw<V, T>& r, float (&x)[V]) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) x[i] = widen(r.v[i]);
+  for (int i = 0; i < V; ++i) x[i] = r.get(i);
 }
 template <int V, typename T>
 __device__ __forceinline__ void load_row(const T* p, float (&x)[V]) {
@@ -37,8 +57,7 @@ __device__ __forceinline__ void load_row(const T* p, float (&x)[V]) {
 template <int V, typename T>
 __device__ __forceinline__ void store_row(T* p, const float (&x)[V]) {
   Raw<V, T> r;
-#pragma unroll
-  for (int i = 0; i < V; ++i) narrow(&r.v[i], x[i]);
+  r.set(x);
   *reinterpret_cast<Raw<V, T>*>(p) = r;
 }
 

@@ -48,16 +48,20 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
     total[e] = 0.0f;
   }
   typedef Cursor<EV, T> At;
-  const At xs(p.x, p.x_stride, s.first, c0, te, ce, TILE), ds(p.dt, p.dt_stride, s.first, c0, te, ce, TILE);
-  const At zs(p.z, p.z_stride, s.first, c0, te, ce, TILE), ys(p.y, p.D, s.first, c0, te, ce, TILE);
+  At xs(p.x, p.x_stride, s.first, c0, te, ce, TILE), ds(p.dt, p.dt_stride, s.first, c0, te, ce, TILE);
+  At zs(p.z, p.z_stride, s.first, c0, te, ce, TILE), ys(p.y, p.D, s.first, c0, te, ce, TILE);
   const T* bp = static_cast<const T*>(p.Bm) + int64_t(s.first) * p.b_stride + 4 * w;
   const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
   Raw<EV, T> rx{}, rd{}, rz{};
   auto fetch = [&](int j) {
-    if (!le || j * TILE + te >= s.count) return;
-    rx = xs.load(j);
-    rd = ds.load(j);
-    if (OUT && p.z) rz = zs.load(j);
+    if (le && j * TILE + te < s.count) {
+      rx = xs.load();
+      rd = ds.load();
+      if (OUT && p.z) rz = zs.load();
+    }
+    xs.move(1);
+    ds.move(1);
+    zs.move(1);
   };
   fetch(0);
   for (int j = 0; j * TILE < s.count; ++j) {
@@ -71,7 +75,7 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
     if (te < TILE) {
 #pragma unroll
       for (int e = 0; e < EV; ++e) {
-        const float d = mine ? softplus(widen(rd.v[e]) + bias[e]) : 0.0f;
+        const float d = mine ? softplus(rd.get(e) + bias[e]) : 0.0f;
         step[te][ce + e] = d;
         input[te][ce + e] = mine ? d * x[e] : 0.0f;
         total[e] += d;
@@ -114,8 +118,9 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
         y[e] = fmaf(skip[e], x[e], y[e]);
         if (p.z) y[e] *= z[e] * sigmoid(z[e]);
       }
-      ys.store(j, y);
+      ys.store(y);
     }
+    ys.move(1);
   }
   if (OUT) {
     if (s.ends() && live) *reinterpret_cast<f32x4*>(p.h_out + state) = f32x4{h[0], h[1], h[2], h[3]};
@@ -152,7 +157,7 @@ __global__ __launch_bounds__(256) void ssm_join_kernel(SsmParams p) {
   const int64_t state = (int64_t(slot) * p.D + c) * p.S + k;
   float* E = p.E + i;
   float h = p.h_in ? p.h_in[state] : 0.0f;
-  constexpr int U = 8;
+  constexpr int U = 16;          // loads in flight: they do not wait for the states
   for (int j = 0; j < parts; j += U) {
     float e[U], d[U];
 #pragma unroll
@@ -302,7 +307,8 @@ int check_counts(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward)
   const int64_t rows = stretches(n, tokens, stretch_len(d, n, tokens, backward));
   if (!grid_fits(rows * blocks_of(d), d->states * 16)) return DL_E_SHAPE;
   const int64_t groups = (int64_t(d->channels) * d->states + 255) / 256;
-  return grid_fits(groups * n, 256) ? DL_OK : DL_E_SHAPE;
+  if (!grid_fits(groups * n, 256)) return DL_E_SHAPE;
+  return !backward || grid_fits(rows * ssm_rows_pieces(d->states), 256) ? DL_OK : DL_E_SHAPE;
 }
 
 int check_rows(const dl_ssm_desc* d, const dl_ssm_rows* r, bool any) {

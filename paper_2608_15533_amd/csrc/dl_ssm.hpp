@@ -113,20 +113,21 @@ struct TileRows {
 // registers), the thread's offset in it 32 bits.
 template <int EV, typename T>
 struct Cursor {
-  uint64_t at;
+  char* at;
   int64_t tile;          // bytes from a tile to the next
   uint32_t off;
   __device__ __forceinline__ Cursor(const void* base, int64_t stride, int64_t row, int c0, int te, int ce,
                                     int tokens)
-      : at(reinterpret_cast<uint64_t>(base) + (row * stride + c0) * int64_t(sizeof(T))),
+      : at(const_cast<char*>(static_cast<const char*>(base)) + (row * stride + c0) * int64_t(sizeof(T))),
         tile(tokens * stride * int64_t(sizeof(T))),
         off(uint32_t(te) * uint32_t(stride) * uint32_t(sizeof(T)) + uint32_t(ce) * uint32_t(sizeof(T))) {}
-  __device__ __forceinline__ Raw<EV, T> load(int j) const {
-    return load_raw<EV>(reinterpret_cast<const T*>(at + j * tile + off));
+  __device__ __forceinline__ Raw<EV, T> load() const {
+    return *reinterpret_cast<const Raw<EV, T>*>(at + off);
   }
-  __device__ __forceinline__ void store(int j, const float (&x)[EV]) const {
-    store_row<EV>(reinterpret_cast<T*>(at + j * tile + off), x);
+  __device__ __forceinline__ void store(const float (&x)[EV]) const {
+    store_row<EV>(reinterpret_cast<T*>(at + off), x);
   }
+  __device__ __forceinline__ void move(int tiles) { at += tiles * tile; }
 };
 
 __device__ __forceinline__ int wave_index() {

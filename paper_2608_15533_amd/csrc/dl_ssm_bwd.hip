@@ -48,15 +48,20 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
   }
   const T* bp = static_cast<const T*>(p.Bm) + int64_t(s.first) * p.b_stride + 4 * w;
   const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
-  const Cursor<EV, T> xs = part.rows(p.x, p.x_stride, s.first), ds = part.rows(p.dt, p.dt_stride, s.first);
-  const Cursor<EV, T> os = part.rows(p.dy, p.D, s.first), zs = part.rows(p.z, p.z_stride, s.first);
+  Cursor<EV, T> xs = part.rows(p.x, p.x_stride, s.first), ds = part.rows(p.dt, p.dt_stride, s.first);
+  Cursor<EV, T> os = part.rows(p.dy, p.D, s.first), zs = part.rows(p.z, p.z_stride, s.first);
   Raw<EV, T> rx{}, rd{}, ro{}, rz{};
   auto fetch = [&](int j) {
-    if (!part.live || j * TB + part.te >= s.count) return;
-    rx = xs.load(j);
-    rd = ds.load(j);
-    ro = os.load(j);
-    if (p.z) rz = zs.load(j);
+    if (part.live && j * TB + part.te < s.count) {
+      rx = xs.load();
+      rd = ds.load();
+      ro = os.load();
+      if (p.z) rz = zs.load();
+    }
+    xs.move(1);
+    ds.move(1);
+    os.move(1);
+    zs.move(1);
   };
   fetch(0);
   for (int j = 0; j * TB < s.count; ++j) {
@@ -67,10 +72,10 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
     if (part.te < TB) {
 #pragma unroll
       for (int e = 0; e < EV; ++e) {
-        const float d = mine ? softplus(widen(rd.v[e]) + part.bias[e]) : 0.0f, z = widen(rz.v[e]);
+        const float d = mine ? softplus(rd.get(e) + part.bias[e]) : 0.0f, z = rz.get(e);
         step[part.te][part.ce + e] = d;
-        input[part.te][part.ce + e] = mine ? d * widen(rx.v[e]) : 0.0f;
-        grad[part.te][part.ce + e] = mine ? widen(ro.v[e]) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
+        input[part.te][part.ce + e] = mine ? d * rx.get(e) : 0.0f;
+        grad[part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
         total[e] += d;
       }
     }
@@ -173,20 +178,28 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
     const T* bp = static_cast<const T*>(p.Bm) + int64_t(s.first) * p.b_stride + 4 * w;
     const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
     const int tiles = (s.count + TB - 1) / TB;
-    const Cursor<EV, T> xs = part.rows(p.x, p.x_stride, s.first), ds = part.rows(p.dt, p.dt_stride, s.first);
-    const Cursor<EV, T> os = part.rows(p.dy, p.D, s.first), zs = part.rows(p.z, p.z_stride, s.first);
-    const int64_t out = (int64_t(s.first) + part.te) * p.D + part.c;
-    // Rows as they are stored, a tile ahead in either direction.
+    // Rows as they are stored, a tile ahead in either direction; dy and z from the last tile on alone.
+    const int last = s.first + max(tiles - 1, 0) * TB;
+    Cursor<EV, T> xs = part.rows(p.x, p.x_stride, s.first), ds = part.rows(p.dt, p.dt_stride, s.first);
+    Cursor<EV, T> os = part.rows(p.dy, p.D, last), zs = part.rows(p.z, p.z_stride, last);
+    Cursor<EV, T> dxs = part.rows(p.dx, p.D, last), dds = part.rows(p.ddt, p.D, last);
+    Cursor<EV, T> dzs = part.rows(p.dz, p.D, last);
     Raw<EV, T> rx{}, rd{}, ro{}, rz{};
-    auto fetch = [&](int j, bool all) {
-      if (!part.live || j < 0 || j * TB + part.te >= s.count) return;
-      rx = xs.load(j);
-      rd = ds.load(j);
+    auto fetch = [&](int j, int step, bool all) {
+      xs.move(step);
+      ds.move(step);
+      if (step < 0) {
+        os.move(step);
+        zs.move(step);
+      }
+      if (!part.live || j * TB + part.te >= s.count) return;
+      rx = xs.load();
+      rd = ds.load();
       if (!all) return;
-      ro = os.load(j);
-      if (p.z) rz = zs.load(j);
+      ro = os.load();
+      if (p.z) rz = zs.load();
     };
-    fetch(0, tiles == 1);
+    fetch(0, 0, tiles == 1);
     // Steps and inputs of a tile, and what its tokens' gradients are made of.
     auto stage = [&](int j, int count, bool own_steps, bool gradients) {
       if (part.te >= TB) return;
@@ -195,13 +208,13 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
 #pragma unroll
       for (int e = 0; e < EV; ++e) {
         if (own_steps) {
-          const float d = mine ? softplus(widen(rd.v[e]) + part.bias[e]) : 0.0f;
+          const float d = mine ? softplus(rd.get(e) + part.bias[e]) : 0.0f;
           steps[t][part.ce + e] = d;
-          inputs[t][part.ce + e] = mine ? d * widen(rx.v[e]) : 0.0f;
+          inputs[t][part.ce + e] = mine ? d * rx.get(e) : 0.0f;
         }
         if (gradients) {
-          const float z = widen(rz.v[e]);
-          grad[part.te][part.ce + e] = mine ? widen(ro.v[e]) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
+          const float z = rz.get(e);
+          grad[part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
         }
       }
     };
@@ -210,7 +223,7 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
       TileRows<TB, false, T> rows;
       rows.load(bp + int64_t(j * TB) * p.b_stride, p.b_stride, nullptr, 0);
       stage(j, TB, true, false);
-      fetch(j + 1, j + 2 == tiles);
+      fetch(j + 1, 1, j + 2 == tiles);
       rows.settle();
       __syncthreads();
 #pragma unroll
@@ -227,7 +240,7 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
       rows.load(bp + int64_t(t0) * p.b_stride, p.b_stride, cp + int64_t(t0) * p.c_stride, p.c_stride, count);
       const Raw<EV, T> kx = rx, kd = rd, ko = ro, kz = rz;
       stage(j, count, j + 1 == tiles, true);
-      fetch(j - 1, true);
+      if (j > 0) fetch(j - 1, -1, true);
       rows.settle();
       __syncthreads();
       if (j + 1 < tiles) {                       // the last tile's are in hand
@@ -299,19 +312,21 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
             gm += sum_gm[i][part.te][part.ce + e];
             if (p.z) ch += sum_ch[i][part.te][part.ce + e];
           }
-          const float x = widen(kx.v[e]), z = widen(kz.v[e]), sz = sigmoid(z);
+          const float x = kx.get(e), z = kz.get(e), sz = sigmoid(z);
           const float up = grad[part.te][part.ce + e];
           dx[e] = fmaf(steps[t0 + part.te][part.ce + e], gb, skip[e] * up);
-          ddt[e] = sigmoid(widen(kd.v[e]) + part.bias[e]) * fmaf(x, gb, gm);
+          ddt[e] = sigmoid(kd.get(e) + part.bias[e]) * fmaf(x, gb, gm);
           dskip[e] = fmaf(up, x, dskip[e]);
           dbias[e] += ddt[e];
-          dz[e] = widen(ko.v[e]) * fmaf(skip[e], x, ch) * sz * (1.0f + z * (1.0f - sz));
+          dz[e] = ko.get(e) * fmaf(skip[e], x, ch) * sz * (1.0f + z * (1.0f - sz));
         }
-        const int64_t to = int64_t(t0) * p.D;
-        store_row<EV>(static_cast<T*>(p.dx) + to + out, dx);
-        store_row<EV>(static_cast<T*>(p.ddt) + to + out, ddt);
-        if (p.z) store_row<EV>(static_cast<T*>(p.dz) + to + out, dz);
+        dxs.store(dx);
+        dds.store(ddt);
+        if (p.z) dzs.store(dz);
       }
+      dxs.move(-1);
+      dds.move(-1);
+      dzs.move(-1);
       // What a thread reads of grad here, it alone writes in the next tile.
     }
     if (s.begins() && p.h_out && live)
@@ -348,7 +363,7 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
 // of a stretch's sums.
 template <int S, typename T>
 __global__ __launch_bounds__(256) void ssm_rows_kernel(SsmParams p) {
-  constexpr int PIECES = ssm_grad_tokens(S) * 2 * S / 256, U = 8;
+  constexpr int PIECES = ssm_rows_pieces(S), U = 8;
   const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, blockIdx.x / PIECES);
   const int i = int(blockIdx.x % PIECES) * 256 + int(threadIdx.x);
   if (s.idle || i >= s.count * 2 * S) return;
@@ -371,7 +386,7 @@ hipError_t launch_grad(const SsmParams& p, hipStream_t s) {
   const int64_t parts = stretches(p.n, p.N, p.len);
   hipError_t e = start_rows(&ssm_grad_kernel<S, T>, parts * p.blocks, S * 16, p, s);
   if (e == hipSuccess)
-    e = start_rows(&ssm_rows_kernel<S, T>, parts * (ssm_grad_tokens(S) * 2 * S / 256), 256, p, s);
+    e = start_rows(&ssm_rows_kernel<S, T>, parts * ssm_rows_pieces(S), 256, p, s);
   return e;
 }
 template <int S, typename T>

@@ -11,6 +11,9 @@ namespace dl {
 // (in tiles of 4), 20 600, 553, 563; 64 states with 28, 24, 20, 16 677, 664, 675, 696.
 __host__ __device__ constexpr int ssm_grad_tokens(int states) { return states == 16 ? 32 : 24; }
 
+// Workgroups of 256 that sum dB and dC of a stretch.
+__host__ __device__ constexpr int ssm_rows_pieces(int states) { return ssm_grad_tokens(states) * 2 * states / 256; }
+
 // E, F and the sum of d of every stretch.
 hipError_t launch_ssm_ends(int states, bool bf16, const SsmParams& p, hipStream_t s);
 // Every gradient, from the states before and the gradients behind every stretch; dA, dskip and dbias

@@ -260,6 +260,31 @@ def test_gradients_against_differences(op):
         assert abs((up - down) / (2 * h.item()) - want) <= 2e-2 * want, n
 
 
+@pytest.mark.parametrize("tokens", [0, 1, 10, 32, 33])
+def test_short_batches_through_autograd(tokens):
+    """Few tokens need no workspace; without any, states pass through and parameters get nothing."""
+    from paper_2608_15533_amd import sequence as M
+    lens = [tokens, 0]
+    x = R.ssm_inputs(lens, 72, 16, seed=11)
+    x["slots"] = [0, 1]
+    want = R.ssm_expected(x)
+    t = leaves({k: x[k] for k in ("x", "dt", "A", "B", "C", "skip", "bias", "z", "s")})
+    y, h = M.selective_scan(t["x"], t["dt"], t["A"], t["B"], t["C"], t["skip"], t["bias"], t["z"], t["s"], i32(lens))
+    got = torch.autograd.grad([y, h], list(t.values()), [x["dy"].cuda(), x["ds"].cuda()])
+    assert R.rel(y, want["out"][0]) <= R.TOL["ssm"] and R.rel(h, want["out"][1]) <= R.TOL["ssm"]
+    for k, g in zip(t, got):
+        assert R.rel(g, want["grads"][k]) <= R.TOL["ssm"], k
+    c = R.conv_inputs(lens, 72, 4, seed=12)
+    c["slots"] = [0, 1]
+    want = R.conv_expected(c)
+    t = leaves({k: c[k] for k in ("x", "w", "bias", "s")})
+    y, s = M.short_conv(t["x"], t["w"], t["bias"], t["s"], i32(lens))
+    got = torch.autograd.grad([y, s], list(t.values()), [c["dy"].cuda(), c["ds"].cuda()])
+    assert R.rel(y, want["out"][0]) <= R.TOL["conv"] and torch.equal(s.double().cpu(), want["out"][1])
+    for k, g in zip(t, got):
+        assert R.rel(g, want["grads"][k]) <= R.TOL["conv"], k
+
+
 # ------------------------------------------------------------------ ways of calling
 @pytest.mark.parametrize("op", ["conv", "ssm"])
 def test_capture_and_replay(op):

@@ -190,6 +190,14 @@ def test_counts(call):
         assert call(n=2 ** 31 - 1) == D.DL_E_SHAPE
 
 
+def test_grids_of_the_sums_over_channels():
+    """Few channels, many tokens: more workgroups for the sums of dB and dC than for the gradients."""
+    d, r = Ssm.desc(channels=8, states=64), Ssm.rows(b_stride=64, c_stride=64)
+    assert Ssm.backward(d=d, r=r, tokens=30_000_000) == D.DL_E_ALIGN
+    assert Ssm.backward(d=d, r=r, tokens=60_000_000) == D.DL_E_SHAPE
+    assert Ssm.prefill(d=d, r=r, tokens=60_000_000) == D.DL_E_ALIGN
+
+
 @every
 def test_rows(call):
     op = owner(call)
