@@ -266,6 +266,8 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
           }
         }
         float kept = 0.0f;
+        int place = lane & 7;
+        asm volatile("" : "+v"(place));          // compared where it is used: eight masks kept spill registers
 #pragma unroll
         for (int t = TB - 1; t >= 0; --t) {
           if (ALL || t < count) {
@@ -288,10 +290,10 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
             sum_gm[w][t][lane] = gm;
             if (p.z) sum_ch[w][t][lane] = ch;
             const float one = eight_sums(over);
-            if ((lane & 7) == (t & 7)) kept = one;
+            if (place == (t & 7)) kept = one;
           }
           if ((t & 7) == 0) {
-            const int tt = t + (lane & 7), k = sum_number(lane);   // numbers 0-3: B's states, 4-7: C's
+            const int tt = t + place, k = sum_number(lane);   // numbers 0-3: B's states, 4-7: C's
             if (tt < count)
               p.rows[(int64_t(block) * p.N + s.first + t0 + tt) * (2 * S) + (k >> 2) * S + 4 * w + (k & 3)] = kept;
           }
