@@ -441,7 +441,10 @@ int dl_qk_norm_backward(const dl_qk_desc* desc, const dl_qk_rows* rows, const vo
  *   h_t = exp(d_t A) . h_{t-1} + d_t x_t B_t,   y_t = (<C_t, h_t> + skip x_t) silu(z_t),
  * A and h_t [S] per channel (A <= 0 forgets; taken at its value), B_t and C_t [S] the same for
  * all channels, skip and z left out where NULL.  Whole sequences are cut into stretches that run
- * side by side: what a sequence's results round to depends on the call's n and tokens. */
+ * side by side: what a sequence's results round to depends on the call's n and tokens.
+ * A value that is infinite or NaN stays in its sequence, and in its channel unless it is one of
+ * B or C; an infinite one may come out as NaN.  Steps are at most as large as fp32 holds; the
+ * hardware's exponential takes decays below 2^-126 for 0. */
 typedef struct {
   int32_t abi_version;  /* must be DL_ABI_VERSION                                       */
   int32_t num_slots;    /* >= 1                                                         */

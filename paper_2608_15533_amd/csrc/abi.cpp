@@ -202,10 +202,10 @@ const char* dl_status_str(int status) {
   switch (status) {
     case DL_OK: return "DL_OK";
     case DL_E_NULL: return "DL_E_NULL: a required pointer is NULL";
-    case DL_E_SHAPE: return "DL_E_SHAPE: inconsistent batch, head or slot-list shape";
+    case DL_E_SHAPE: return "DL_E_SHAPE: inconsistent batch, head, row or slot-list shape";
     case DL_E_DTYPE: return "DL_E_DTYPE: dtype combination not allowed";
     case DL_E_ALIGN: return "DL_E_ALIGN: pointer not aligned as required";
-    case DL_E_UNSUPPORTED: return "DL_E_UNSUPPORTED: dk, dv, merge interval or operator not supported";
+    case DL_E_UNSUPPORTED: return "DL_E_UNSUPPORTED: dk, dv, merge interval, operator or another size or kind not supported";
     case DL_E_HIP: return "DL_E_HIP: kernel launch failed";
     case DL_E_VERSION: return "DL_E_VERSION: descriptor ABI version mismatch";
     case DL_E_SCRATCH: return "DL_E_SCRATCH: the call needs more than the allocation-free entry point's fixed scratch";

@@ -2,7 +2,8 @@
 
 The entry points keep the C names (``dl_eager_step``, ``dl_append_step``, ``dl_merge``,
 ``dl_readout``; for whole sequences ``dl_chunk_tables``, ``dl_prefill``,
-``dl_prefill_backward``) and take torch CUDA tensors; each call checks layouts, builds the C
+``dl_prefill_backward``; around a recurrence ``dl_conv_*``, ``dl_ssm_*``,
+``dl_qk_norm``, ``dl_qk_norm_backward``) and take torch CUDA tensors; each call checks layouts, builds the C
 structs and calls the library, which launches the HIP kernels on the current (or the
 given) stream.  No arithmetic of the method happens here.  PyTorch is used only to
 own device memory and to name the stream.

@@ -111,9 +111,9 @@ def short_conv(x, w, bias=None, s0=None, lens=None, activation="silu"):
     """The short causal convolution of every channel over packed sequences.
 
     x [N,D] in bf16 or fp32 (columns of a wider tensor will do), w [D,W] and bias [D] in fp32; lens [n]
-    int32 on the device (None: one sequence), or ``ChunkTables`` of the batch; s0 [n,W-1,D] the inputs
-    before each sequence (None: zeros).  Returns (y [N,D], the last W - 1 inputs [n,W-1,D]); y and its
-    gradients are 0 in rows behind the last sequence.  Gradients once; a call keeps its inputs and
+    int32 on the device (None: one sequence), or ``ChunkTables`` of the batch (states are then by slot);
+    s0 [n,W-1,D] the inputs before each sequence (None: zeros).  Returns (y [N,D], the last W - 1 inputs
+    [n,W-1,D]); y and its gradients are 0 in rows behind the last sequence.  Gradients once; a call keeps its inputs and
     nothing else."""
     tables, n = _batch(x, lens)
     desc = D.make_conv_desc(n, x.shape[1], w.shape[1], _type(x, "x"), activation)
