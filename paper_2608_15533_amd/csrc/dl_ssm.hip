@@ -243,9 +243,8 @@ hipError_t launch_prefill(const SsmParams& p, hipStream_t s) {
 
 template <int S, typename T>
 hipError_t launch_backward(const SsmParams& p, hipStream_t s) {
-  hipError_t e = hipSuccess;
+  hipError_t e = launch_ssm_ends(S, sizeof(T) == 2, p, s);
   if (p.E) {
-    e = launch_ssm_ends(S, sizeof(T) == 2, p, s);
     const int64_t groups = (int64_t(p.D) * S + 255) / 256;
     if (e == hipSuccess) e = start_rows(&ssm_join_kernel<true>, groups * p.n, 256, p, s);
   }
@@ -280,14 +279,16 @@ hipError_t launch(Pass pass, const dl_ssm_desc* d, const SsmParams& p, hipStream
 
 int blocks_of(const dl_ssm_desc* d) { return (d->channels + 63) / 64; }
 
-// Tokens of a stretch: as long as 16 waves a SIMD are left, so that ragged ends even out.  8192 tokens of 4096
-// channels with 2048, 4096, 8192, 16384 and 32768 waves: 476, 316, 294, 277 and 284 us.
+// Tokens of a stretch: as long as enough waves are left to fill the chip and to even out ragged ends.  Forward, 8192
+// tokens of 4096 channels with 2048, 4096, 8192, 16384 and 32768 waves: 476, 316, 294, 277 and 284 us (an earlier
+// form).  Backward longer ones leave fewer states to join and rows of partial sums: 4096 tokens of 4096 x 16, 2048 x
+// 32 and 1024 x 64 channels x states, whole step, with 32, 64 and 128 tokens 513, 485, 481; 545, 513, 508; 649, 602,
+// 572 us; but 777 tokens of 200 channels 58, 79, 98 us.
 int stretch_len(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
-  if (backward) return ssm_grad_tokens(d->states);
-  const int64_t waves = int64_t(blocks_of(d)) * (d->states / 4);
+  const int64_t waves = int64_t(blocks_of(d)) * (d->states / 4), least = backward ? 8192 : 16384;
   int64_t len = 32;
-  while (len < tokens && tokens / (2 * len) * waves >= 16384) len *= 2;
-  return int(std::min<int64_t>(len, std::max(tokens, 1)));
+  while (len < (backward ? 256 : tokens) && tokens / (2 * len) * waves >= least) len *= 2;
+  return int(backward ? len : std::min<int64_t>(len, std::max(tokens, 1)));
 }
 // One stretch a sequence: nothing to join.
 bool whole(int32_t tokens, int len) { return tokens <= len; }
@@ -308,7 +309,8 @@ int check_counts(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward)
   if (!grid_fits(rows * blocks_of(d), d->states * 16)) return DL_E_SHAPE;
   const int64_t groups = (int64_t(d->channels) * d->states + 255) / 256;
   if (!grid_fits(groups * n, 256)) return DL_E_SHAPE;
-  return !backward || grid_fits(rows * ssm_rows_pieces(d->states), 256) ? DL_OK : DL_E_SHAPE;
+  const int64_t pieces = int64_t(stretch_len(d, n, tokens, true)) * 2 * d->states / 256;   // of dB's and dC's sums
+  return !backward || grid_fits(rows * pieces, 256) ? DL_OK : DL_E_SHAPE;
 }
 
 int check_rows(const dl_ssm_desc* d, const dl_ssm_rows* r, bool any) {
@@ -352,9 +354,9 @@ SsmParams params(const dl_ssm_desc* d, const float* h_in, float* h_out, const dl
 }
 
 // Workspace, 256-byte aligned parts: E, sums (sequences in several stretches); backward F, then the
-// partial sums.
+// tiles' starts and the partial sums.
 struct Layout {
-  size_t E = 0, F = 0, sums = 0, part = 0, rows = 0, all = 0;
+  size_t E = 0, F = 0, sums = 0, tiles = 0, tile_sums = 0, part = 0, rows = 0, all = 0;
 };
 Layout layout(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
   const int len = stretch_len(d, n, tokens, backward);
@@ -371,6 +373,9 @@ Layout layout(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
     if (backward) l.F = take(parts * D * S);
   }
   if (backward) {
+    const size_t inner = parts * size_t(len / ssm_grad_tile(d->states) - 1);
+    l.tiles = take(inner * D * S);
+    l.tile_sums = take(inner * D);
     l.part = take(parts * D * (S + 2));
     l.rows = take(size_t(blocks_of(d)) * size_t(tokens) * 2 * S);
   }
@@ -380,11 +385,14 @@ Layout layout(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
 void set_workspace(SsmParams& p, const dl_ssm_desc* d, const Layout& l, void* ws, bool backward) {
   char* at = static_cast<char*>(ws);
   p.len = stretch_len(d, p.n, p.N, backward);
+  p.inner = p.len / ssm_grad_tile(d->states) - 1;
   if (!whole(p.N, p.len)) {
     p.E = reinterpret_cast<float*>(at + l.E);
     p.sums = reinterpret_cast<float*>(at + l.sums);
     p.F = reinterpret_cast<float*>(at + l.F);
   }
+  p.tiles = reinterpret_cast<float*>(at + l.tiles);
+  p.tile_sums = reinterpret_cast<float*>(at + l.tile_sums);
   p.part = reinterpret_cast<float*>(at + l.part);
   p.rows = reinterpret_cast<float*>(at + l.rows);
 }

@@ -36,9 +36,11 @@ struct SsmParams {
   void *dB, *dC;
   const int32_t *cu, *seq_slot, *slots;
   float *E, *F, *sums;          // [stretches][S/4][D][4] twice, [stretches][D]; null: sequences whole
+  float *tiles, *tile_sums;     // backward: what a stretch has left before every tile but the first,
+                                // [stretches][inner][S/4][D][4], and the sums of d there, [stretches][inner][D]
   float *part;                  // backward: [stretches][D*S + 2 D] partial sums of dA, dskip, dbias
   float *rows;                  // backward: [blocks][N][2 S] partial sums of dB, dC
-  int32_t n, N, B, D, S, len, blocks;   // blocks: of 64 channels
+  int32_t n, N, B, D, S, len, blocks, inner;   // blocks: of 64 channels; inner: tiles of a stretch less one
 };
 
 __device__ __forceinline__ float decay(float d, float a2) { return __builtin_amdgcn_exp2f(d * a2); }

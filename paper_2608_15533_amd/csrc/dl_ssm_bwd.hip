@@ -4,15 +4,10 @@
 namespace dl {
 namespace {
 
-// Tokens whose steps lie in LDS at a time, and whose decays and states a wave holds in registers: with 16 a
-// wave needs 255 of them, two to a SIMD.
-template <int S>
-constexpr int tile_of = S == 16 ? 8 : 4;
-
 // A thread's part of a tile: one token, EV channels.
 template <int S, typename T>
 struct Part {
-  static constexpr int TB = tile_of<S>, NT = S * 16, EV = TB * 64 >= NT ? TB * 64 / NT : 1, CG = 64 / EV;
+  static constexpr int TB = ssm_grad_tile(S), NT = S * 16, EV = TB * 64 >= NT ? TB * 64 / NT : 1, CG = 64 / EV;
   int te, ce, c;
   bool live;                     // D is a multiple of 8: all EV channels or none
   float bias[EV];
@@ -29,7 +24,8 @@ struct Part {
   }
 };
 
-// E, F and the sum of d of a stretch, 64 channels; wave w has states 4 w .. 4 w + 3.
+// E, F and the sum of d of a stretch, 64 channels; wave w has states 4 w .. 4 w + 3.  On the way, before
+// every tile but the first, what the stretch has left so far and the sum of d: the gradients start there.
 template <int S, typename T>
 __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
   typedef Part<S, T> P;
@@ -37,10 +33,10 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
   __shared__ __attribute__((aligned(16))) float step[TB][64], input[TB][64], grad[TB][64];
   const int f = blockIdx.x / p.blocks, c0 = int(blockIdx.x % p.blocks) * 64;
   const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, f);
-  if (s.idle || (s.begins() && s.ends())) return;
+  if (s.idle) return;
   const int lane = threadIdx.x & 63, w = wave_index(), c = c0 + lane;
   const P part(p, c0);
-  float a2[4], h[4] = {}, g[4] = {}, decays[4], total[EV] = {};
+  float a2[4], h[4] = {}, g[4] = {}, decays[4], sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     a2[i] = c < p.D ? p.A[int64_t(c) * S + 4 * w + i] * LOG2E : 0.0f;
@@ -69,6 +65,11 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
     const bool mine = part.live && part.te < count;
     TileRows<TB, true, T> rows;
     if (count == TB) rows.load(bp, p.b_stride, cp, p.c_stride);
+    if (j > 0 && c < p.D) {
+      const int64_t tile = int64_t(f) * p.inner + j - 1;
+      *reinterpret_cast<f32x4*>(p.tiles + tile * p.D * S + (int64_t(w) * p.D + c) * 4) = f32x4{h[0], h[1], h[2], h[3]};
+      if (w == 0) p.tile_sums[tile * p.D + c] = sum;
+    }
     if (part.te < TB) {
 #pragma unroll
       for (int e = 0; e < EV; ++e) {
@@ -76,7 +77,6 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
         step[part.te][part.ce + e] = d;
         input[part.te][part.ce + e] = mine ? d * rx.get(e) : 0.0f;
         grad[part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
-        total[e] += d;
       }
     }
     fetch(j + 1);
@@ -84,6 +84,7 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
     __syncthreads();
     auto token = [&](int t, const Four<T>& B, const Four<T>& C) {
       const float d = step[t][lane], u = input[t][lane], up = grad[t][lane];
+      sum += d;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float a = decay(d, a2[i]);
@@ -107,21 +108,11 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
     cp += TB * p.c_stride;
     __syncthreads();
   }
-  if (c < p.D) {
+  if (p.E && c < p.D) {
     const int64_t at = int64_t(f) * p.D * S + (int64_t(w) * p.D + c) * 4;
     *reinterpret_cast<f32x4*>(p.E + at) = f32x4{h[0], h[1], h[2], h[3]};
     *reinterpret_cast<f32x4*>(p.F + at) = f32x4{g[0], g[1], g[2], g[3]};
-  }
-  if (part.te < TB) {
-#pragma unroll
-    for (int e = 0; e < EV; ++e) step[part.te][part.ce + e] = total[e];
-  }
-  __syncthreads();
-  if (w == 0 && c < p.D) {
-    float sum = 0.0f;
-#pragma unroll
-    for (int t = 0; t < TB; ++t) sum += step[t][lane];
-    p.sums[int64_t(f) * p.D + c] = sum;
+    if (w == 0) p.sums[int64_t(f) * p.D + c] = sum;
   }
 }
 
@@ -136,16 +127,15 @@ __device__ __forceinline__ int sum_number(int l) {
   return 4 * (l >> 5) + 2 * ((l >> 3) & 1) + ((l >> 4) & 1);
 }
 
-// Every gradient of a stretch's tokens, 64 channels; wave w has states 4 w .. 4 w + 3.  The states
-// before every tile first (in LDS), then the tiles from the last to the first: a tile's decays a_t
-// and m_t = a_t . h_{t-1} in registers, then its tokens backwards.
+// Every gradient of a stretch's tokens, 64 channels; wave w has states 4 w .. 4 w + 3.  Tiles from the last
+// to the first: a tile starts from what the stretch had left there and its decayed first state; its decays a_t
+// and m_t = a_t . h_{t-1} are held in registers, then come its tokens backwards.
 template <int S, typename T>
-__global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmParams p) {
+__global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmParams p) {
   typedef Part<S, T> P;
-  constexpr int TB = P::TB, EV = P::EV, NW = S / 4, TILES = ssm_grad_tokens(S) / TB;
-  __shared__ __attribute__((aligned(16))) float steps[TILES * TB][64], inputs[TILES * TB][64], grad[TB][64];
+  constexpr int TB = P::TB, EV = P::EV, NW = S / 4;
+  __shared__ __attribute__((aligned(16))) float step[TB][64], input[TB][64], grad[TB][64];
   __shared__ __attribute__((aligned(16))) float sum_gb[NW][TB][64], sum_gm[NW][TB][64], sum_ch[NW][TB][64];
-  __shared__ __attribute__((aligned(16))) f32x4 before[TILES - 2][NW][64];   // of the first and last: not here
   const int f = blockIdx.x / p.blocks, block = int(blockIdx.x % p.blocks), c0 = block * 64;
   const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, f);
   const int lane = threadIdx.x & 63, w = wave_index(), c = c0 + lane;
@@ -153,23 +143,17 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
   const P part(p, c0);
   float dA[4] = {}, dskip[EV] = {}, dbias[EV] = {};
   if (!s.idle) {
-    float a2[4], h[4] = {}, g[4] = {}, A[4], skip[EV];
+    float a2[4], g[4] = {}, skip[EV];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      A[i] = live ? p.A[int64_t(c) * S + 4 * w + i] : 0.0f;
-      a2[i] = A[i] * LOG2E;
-    }
+    for (int i = 0; i < 4; ++i) a2[i] = live ? p.A[int64_t(c) * S + 4 * w + i] * LOG2E : 0.0f;
 #pragma unroll
     for (int e = 0; e < EV; ++e) skip[e] = p.skip && part.live ? p.skip[part.c + e] : 0.0f;
     const int64_t state = (int64_t(s.slot) * p.D + c) * S + 4 * w;
-    const int64_t at = int64_t(f) * p.D * S + (int64_t(w) * p.D + c) * 4;
+    const int64_t quad = (int64_t(w) * p.D + c) * 4, at = int64_t(f) * p.D * S + quad;
     const float* hp = p.E ? p.E + at : p.h_in ? p.h_in + state : nullptr;
     const float* gp = p.E ? p.F + at : p.dh_out ? p.dh_out + state : nullptr;
-    if (live && hp) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(hp);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = v[i];
-    }
+    f32x4 first{};
+    if (live && hp) first = *reinterpret_cast<const f32x4*>(hp);
     if (live && gp) {
       const f32x4 v = *reinterpret_cast<const f32x4*>(gp);
 #pragma unroll
@@ -177,80 +161,54 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
     }
     const T* bp = static_cast<const T*>(p.Bm) + int64_t(s.first) * p.b_stride + 4 * w;
     const T* cp = static_cast<const T*>(p.Cm) + int64_t(s.first) * p.c_stride + 4 * w;
-    const int tiles = (s.count + TB - 1) / TB;
-    // Rows as they are stored, a tile ahead in either direction; dy and z from the last tile on alone.
-    const int last = s.first + max(tiles - 1, 0) * TB;
-    Cursor<EV, T> xs = part.rows(p.x, p.x_stride, s.first), ds = part.rows(p.dt, p.dt_stride, s.first);
+    const int tiles = (s.count + TB - 1) / TB, last = s.first + max(tiles - 1, 0) * TB;
+    Cursor<EV, T> xs = part.rows(p.x, p.x_stride, last), ds = part.rows(p.dt, p.dt_stride, last);
     Cursor<EV, T> os = part.rows(p.dy, p.D, last), zs = part.rows(p.z, p.z_stride, last);
     Cursor<EV, T> dxs = part.rows(p.dx, p.D, last), dds = part.rows(p.ddt, p.D, last);
     Cursor<EV, T> dzs = part.rows(p.dz, p.D, last);
+    // Rows as they are stored and the tile's start, a tile ahead.
     Raw<EV, T> rx{}, rd{}, ro{}, rz{};
-    auto fetch = [&](int j, int step, bool all) {
-      xs.move(step);
-      ds.move(step);
-      if (step < 0) {
-        os.move(step);
-        zs.move(step);
+    f32x4 left{};
+    float since = 0.0f;
+    auto fetch = [&](int j) {
+      if (part.live && j * TB + part.te < s.count) {
+        rx = xs.load();
+        rd = ds.load();
+        ro = os.load();
+        if (p.z) rz = zs.load();
       }
-      if (!part.live || j * TB + part.te >= s.count) return;
-      rx = xs.load();
-      rd = ds.load();
-      if (!all) return;
-      ro = os.load();
-      if (p.z) rz = zs.load();
-    };
-    fetch(0, 0, tiles == 1);
-    // Steps and inputs of a tile, and what its tokens' gradients are made of.
-    auto stage = [&](int j, int count, bool own_steps, bool gradients) {
-      if (part.te >= TB) return;
-      const bool mine = part.live && part.te < count;
-      const int t = j * TB + part.te;
-#pragma unroll
-      for (int e = 0; e < EV; ++e) {
-        if (own_steps) {
-          const float d = mine ? softplus(rd.get(e) + part.bias[e]) : 0.0f;
-          steps[t][part.ce + e] = d;
-          inputs[t][part.ce + e] = mine ? d * rx.get(e) : 0.0f;
-        }
-        if (gradients) {
-          const float z = rz.get(e);
-          grad[part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
-        }
+      xs.move(-1);
+      ds.move(-1);
+      os.move(-1);
+      zs.move(-1);
+      if (j > 0 && live) {
+        const int64_t tile = int64_t(f) * p.inner + j - 1;
+        left = *reinterpret_cast<const f32x4*>(p.tiles + tile * p.D * S + quad);
+        since = p.tile_sums[tile * p.D + c];
       }
     };
-    for (int j = 0; j + 1 < tiles; ++j) {
-      if (j > 0) before[j - 1][w][lane] = f32x4{h[0], h[1], h[2], h[3]};
-      TileRows<TB, false, T> rows;
-      rows.load(bp + int64_t(j * TB) * p.b_stride, p.b_stride, nullptr, 0);
-      stage(j, TB, true, false);
-      fetch(j + 1, 1, j + 2 == tiles);
-      rows.settle();
-      __syncthreads();
-#pragma unroll
-      for (int t = 0; t < TB; ++t) {
-        const float d = steps[j * TB + t][lane], u = inputs[j * TB + t][lane];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = fmaf(decay(d, a2[i]), h[i], u * rows.B[t].at(i));
-      }
-    }
+    if (tiles > 0) fetch(tiles - 1);
     for (int j = tiles - 1; j >= 0; --j) {
       const int t0 = j * TB, count = min(TB, s.count - t0);
       const bool mine = part.live && part.te < count;
       TileRows<TB, true, T> rows;
       rows.load(bp + int64_t(t0) * p.b_stride, p.b_stride, cp + int64_t(t0) * p.c_stride, p.c_stride, count);
       const Raw<EV, T> kx = rx, kd = rd, ko = ro, kz = rz;
-      stage(j, count, j + 1 == tiles, true);
-      if (j > 0) fetch(j - 1, -1, true);
+      float h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = j > 0 ? fmaf(decay(since, a2[i]), first[i], left[i]) : first[i];
+      if (part.te < TB) {
+#pragma unroll
+        for (int e = 0; e < EV; ++e) {
+          const float d = mine ? softplus(kd.get(e) + part.bias[e]) : 0.0f, z = kz.get(e);
+          step[part.te][part.ce + e] = d;
+          input[part.te][part.ce + e] = mine ? d * kx.get(e) : 0.0f;
+          grad[part.te][part.ce + e] = mine ? ko.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
+        }
+      }
+      if (j > 0) fetch(j - 1);
       rows.settle();
       __syncthreads();
-      if (j + 1 < tiles) {                       // the last tile's are in hand
-        f32x4 v{};
-        if (j > 0) v = before[j - 1][w][lane];
-        else if (live && hp) v = *reinterpret_cast<const f32x4*>(hp);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = v[i];
-      }
-      const float(*step)[64] = steps + t0, (*input)[64] = inputs + t0;
       auto walk = [&](auto whole) {
         constexpr bool ALL = decltype(whole)::value;
         float a[TB][4], m[TB][4];
@@ -279,7 +237,7 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
               g[i] = fmaf(v, cc, g[i]);
               const float ht = fmaf(u, b, m[t][i]), x0 = g[i] * m[t][i];
               gb = fmaf(g[i], b, gb);
-              gm = fmaf(x0, A[i], gm);
+              gm = fmaf(x0, a2[i], gm);
               ch = fmaf(cc, ht, ch);
               dA[i] = fmaf(x0, dd, dA[i]);
               over[i] = g[i] * u;
@@ -316,8 +274,8 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
           }
           const float x = kx.get(e), z = kz.get(e), sz = sigmoid(z);
           const float up = grad[part.te][part.ce + e];
-          dx[e] = fmaf(steps[t0 + part.te][part.ce + e], gb, skip[e] * up);
-          ddt[e] = sigmoid(kd.get(e) + part.bias[e]) * fmaf(x, gb, gm);
+          dx[e] = fmaf(step[part.te][part.ce + e], gb, skip[e] * up);
+          ddt[e] = sigmoid(kd.get(e) + part.bias[e]) * fmaf(x, gb, gm * 0.69314718f);   // A = a2 / log2 e
           dskip[e] = fmaf(up, x, dskip[e]);
           dbias[e] += ddt[e];
           dz[e] = ko.get(e) * fmaf(skip[e], x, ch) * sz * (1.0f + z * (1.0f - sz));
@@ -329,7 +287,7 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
       dxs.move(-1);
       dds.move(-1);
       dzs.move(-1);
-      // What a thread reads of grad here, it alone writes in the next tile.
+      // What a thread reads of step and grad here, it alone writes in the next tile.
     }
     if (s.begins() && p.h_out && live)
       *reinterpret_cast<f32x4*>(p.h_out + state) = f32x4{g[0], g[1], g[2], g[3]};
@@ -344,8 +302,8 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
   if (part.te < TB) {
 #pragma unroll
     for (int e = 0; e < EV; ++e) {
-      steps[part.te][part.ce + e] = dskip[e];
-      inputs[part.te][part.ce + e] = dbias[e];
+      step[part.te][part.ce + e] = dskip[e];
+      input[part.te][part.ce + e] = dbias[e];
     }
   }
   __syncthreads();
@@ -353,8 +311,8 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
     float a = 0.0f, b = 0.0f;
 #pragma unroll
     for (int t = 0; t < TB; ++t) {
-      a += steps[t][lane];
-      b += inputs[t][lane];
+      a += step[t][lane];
+      b += input[t][lane];
     }
     sums[int64_t(p.D) * S + c] = a;
     sums[int64_t(p.D) * (S + 1) + c] = b;
@@ -365,9 +323,10 @@ __global__ __launch_bounds__(S * 16, S == 64 ? 4 : 2) void ssm_grad_kernel(SsmPa
 // of a stretch's sums.
 template <int S, typename T>
 __global__ __launch_bounds__(256) void ssm_rows_kernel(SsmParams p) {
-  constexpr int PIECES = ssm_rows_pieces(S), U = 8;
-  const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, blockIdx.x / PIECES);
-  const int i = int(blockIdx.x % PIECES) * 256 + int(threadIdx.x);
+  constexpr int U = 8;
+  const int pieces = p.len * 2 * S / 256;
+  const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, blockIdx.x / pieces);
+  const int i = int(blockIdx.x % pieces) * 256 + int(threadIdx.x);
   if (s.idle || i >= s.count * 2 * S) return;
   const int64_t row = int64_t(s.first) + i / (2 * S), apart = int64_t(p.N) * (2 * S);
   const int k = i % (2 * S);
@@ -388,7 +347,7 @@ hipError_t launch_grad(const SsmParams& p, hipStream_t s) {
   const int64_t parts = stretches(p.n, p.N, p.len);
   hipError_t e = start_rows(&ssm_grad_kernel<S, T>, parts * p.blocks, S * 16, p, s);
   if (e == hipSuccess)
-    e = start_rows(&ssm_rows_kernel<S, T>, parts * ssm_rows_pieces(S), 256, p, s);
+    e = start_rows(&ssm_rows_kernel<S, T>, parts * (p.len * 2 * S / 256), 256, p, s);
   return e;
 }
 template <int S, typename T>

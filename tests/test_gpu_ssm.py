@@ -68,6 +68,44 @@ def test_long_and_many_and_wide(lens, D):
     L.check(L.run("ssm", x), R.ssm_expected(x))
 
 
+@pytest.mark.parametrize("S,D,lens", [(16, 4096, [5000, 3200]), (32, 2048, [4100, 20]), (64, 1024, [2100])], ids=str)
+def test_stretches_of_any_length_agree(S, D, lens):
+    """A large batch is cut into longer stretches than its sequences alone, or than the same channels in
+    parts of 64: each within the tolerance, so the two within twice that."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    z = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
+    N, n = sum(lens), len(lens)
+    x = {"x": z(N, D), "dt": z(N, D) - 4, "A": -(1 + 5 * torch.rand(D, S, generator=g, device="cuda")),
+         "B": z(N, S), "C": z(N, S), "skip": z(D), "bias": z(D), "z": z(N, D), "s": z(n, D, S), "dy": z(N, D),
+         "ds": z(n, D, S), "lens": lens, "slots": list(range(n))}
+
+    def run(x):
+        c = L.Packed("ssm", x)
+        c.build()
+        c.forward()
+        c.backward()
+        return c.results()
+
+    whole = run(x)
+    at = 0
+    for i, count in enumerate(lens):
+        r = slice(at, at + count)
+        alone = run({k: v[r] if k in ("x", "dt", "B", "C", "z", "dy") else v[i:i + 1] if k in ("s", "ds") else v
+                     for k, v in {**x, "lens": [count], "slots": [0]}.items()})
+        for k in ("y", "dx", "ddt", "dz", "dB", "dC"):
+            assert R.rel(whole[k][r], alone[k]) <= 2 * R.TOL["ssm"], k
+        for k in ("s", "ds"):
+            assert R.rel(whole[k][i], alone[k][0]) <= 2 * R.TOL["ssm"], k
+        at += count
+    few = slice(64, 128)
+    part = run({k: v[:, few].contiguous() if k in ("x", "dt", "z", "dy", "s", "ds") else
+                v[few] if k in ("A", "skip", "bias") else v for k, v in x.items()})
+    for k in ("y", "dx", "ddt", "dz", "s", "ds"):
+        assert R.rel(whole[k][:, few], part[k]) <= 2 * R.TOL["ssm"], k
+    for k in ("dA", "dskip", "dbias"):
+        assert R.rel(whole[k][few], part[k]) <= 2 * R.TOL["ssm"], k
+
+
 @TYPES
 @STATES
 def test_single_tokens_follow_the_sequence(dtype, S):
