@@ -1,6 +1,10 @@
 """Differentiable whole-sequence operators, for training a layer's projections through them:
 ``delta_scan`` (``dl_prefill`` and ``dl_prefill_backward`` as one torch.autograd function),
-``short_conv``, ``selective_scan`` and ``qk_norm`` likewise."""
+``short_conv``, ``selective_scan`` and ``qk_norm`` likewise.
+
+A training step may be captured into a graph, its forward and backward together.  No graph of an
+earlier eager step may still hold the same leaves then: autograd would join the captured stream with
+the stream of that step, which ends the capture and may end the process."""
 
 import torch
 from torch.autograd.function import once_differentiable

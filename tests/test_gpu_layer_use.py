@@ -340,6 +340,53 @@ def test_norm_in_a_graph():
         assert all(torch.equal(v, want[k]) for k, v in c.results().items())
 
 
+@pytest.mark.parametrize("op", ["conv", "ssm", "qk"])
+def test_a_training_step_in_a_graph(op):
+    """Forward and backward through autograd captured together, leaves that no eager graph holds; every
+    replay equals the eager step bit for bit, with eager work of other leaves in between."""
+    from paper_2608_15533_amd import sequence as M
+    lens = [70, 0, 1, 40]
+    make = {"conv": lambda s: R.conv_inputs(lens, 136, 4, BF16, seed=s),
+            "ssm": lambda s: R.ssm_inputs(lens, 136, 16, BF16, seed=s),
+            "qk": lambda s: R.qk_inputs(sum(lens), 2, 64, 64, 2, BF16, seed=s)}[op]
+    names = {"conv": ("x", "w", "bias"), "ssm": ("x", "dt", "A", "B", "C", "skip", "bias", "z"),
+             "qk": ("q", "k", "wq", "wk")}[op]
+
+    def step(t, n):
+        if op == "conv":
+            out = (M.short_conv(t["x"], t["w"], t["bias"], lens=n)[0],)
+        elif op == "ssm":
+            out = (M.selective_scan(t["x"], t["dt"], t["A"], t["B"], t["C"], t["skip"],
+                                    t["bias"], t["z"], lens=n)[0],)
+        else:
+            out = M.qk_norm(t["q"], t["k"], t["pos"], t["freq"], t["wq"], t["wk"], "rms", "halves",
+                            rep=2)
+        ones = [torch.full_like(o, 0.5) for o in out]
+        return [o.detach() for o in out] + list(torch.autograd.grad(out, [t[k] for k in names], ones))
+
+    n = i32(lens)
+    step(leaves(make(0)), n)
+    held = leaves(make(1))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step(held, n)
+    for seed in (1, 2, 3):
+        x = make(seed)
+        want = step(leaves(x), n)
+        with torch.no_grad():
+            for k in names:
+                held[k].copy_(x[k])
+            if op == "qk":
+                held["pos"].copy_(x["pos"])
+        for o in got:
+            o.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        for o, w in zip(got, want):
+            assert torch.equal(o, w)
+
+
 def test_other_streams_and_two_at_once():
     """Calls on two streams with workspaces of their own, one given by handle."""
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
