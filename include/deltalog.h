@@ -443,7 +443,8 @@ int dl_qk_norm_backward(const dl_qk_desc* desc, const dl_qk_rows* rows, const vo
  * all channels, skip and z left out where NULL.  Whole sequences are cut into stretches that run
  * side by side: what a sequence's results round to depends on the call's n and tokens.
  * A value that is infinite or NaN stays in its sequence, and in its channel unless it is one of
- * B or C; an infinite one may come out as NaN.  Steps are at most as large as fp32 holds; the
+ * B or C; an infinite one may come out as NaN, and so may what follows decays above 1 whose product
+ * over a sequence's tokens is beyond fp32.  Steps are at most as large as fp32 holds; the
  * hardware's exponential takes decays below 2^-126 for 0. */
 typedef struct {
   int32_t abi_version;  /* must be DL_ABI_VERSION                                       */

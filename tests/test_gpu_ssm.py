@@ -68,7 +68,8 @@ def test_long_and_many_and_wide(lens, D):
     L.check(L.run("ssm", x), R.ssm_expected(x))
 
 
-@pytest.mark.parametrize("S,D,lens", [(16, 4096, [5000, 3200]), (32, 2048, [4100, 20]), (64, 1024, [2100])], ids=str)
+@pytest.mark.parametrize("S,D,lens", [(16, 4096, [5000, 3200]), (32, 2048, [4100, 20]), (64, 1024, [2100]),
+                                      (64, 512, [500, 30])], ids=str)
 def test_stretches_of_any_length_agree(S, D, lens):
     """A large batch is cut into longer stretches than its sequences alone, or than the same channels in
     parts of 64: each within the tolerance, so the two within twice that."""
