@@ -130,12 +130,18 @@ __device__ __forceinline__ int sum_number(int l) {
 // Every gradient of a stretch's tokens, 64 channels; wave w has states 4 w .. 4 w + 3.  Tiles from the last
 // to the first: a tile starts from what the stretch had left there and its decayed first state; its decays a_t
 // and m_t = a_t . h_{t-1} are held in registers, then come its tokens backwards.
+// With 32 or 64 states LDS is there twice, and the next tile's steps are formed before the barrier that ends a tile's
+// walk: one barrier a tile, and its last part runs beside other waves' next walk (4096 tokens of 2048 x 32 and 1024
+// x 64 channels x states, whole step: 511 -> 493 and 576 -> 540 us).  With 16 a compute unit has three workgroups
+// for that, and it would cost one of them.
 template <int S, typename T>
 __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmParams p) {
   typedef Part<S, T> P;
   constexpr int TB = P::TB, EV = P::EV, NW = S / 4;
-  __shared__ __attribute__((aligned(16))) float step[TB][64], input[TB][64], grad[TB][64];
-  __shared__ __attribute__((aligned(16))) float sum_gb[NW][TB][64], sum_gm[NW][TB][64], sum_ch[NW][TB][64];
+  constexpr bool AHEAD = S > 16;
+  constexpr int NB = AHEAD ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) float step[NB][TB][64], input[NB][TB][64], grad[NB][TB][64];
+  __shared__ __attribute__((aligned(16))) float sum_gb[NB][NW][TB][64], sum_gm[NB][NW][TB][64], sum_ch[NB][NW][TB][64];
   const int f = blockIdx.x / p.blocks, block = int(blockIdx.x % p.blocks), c0 = block * 64;
   const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, f);
   const int lane = threadIdx.x & 63, w = wave_index(), c = c0 + lane;
@@ -187,35 +193,57 @@ __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmPa
         since = p.tile_sums[tile * p.D + c];
       }
     };
-    if (tiles > 0) fetch(tiles - 1);
-    for (int j = tiles - 1; j >= 0; --j) {
+    // A tile's steps, rows and start; its raw rows are kept for its own gradients.
+    TileRows<TB, true, T> rows;
+    float h[4];
+    auto prepare = [&](int j, int buf) {
       const int t0 = j * TB, count = min(TB, s.count - t0);
       const bool mine = part.live && part.te < count;
-      TileRows<TB, true, T> rows;
       rows.load(bp + int64_t(t0) * p.b_stride, p.b_stride, cp + int64_t(t0) * p.c_stride, p.c_stride, count);
-      const Raw<EV, T> kx = rx, kd = rd, ko = ro, kz = rz;
-      float h[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) h[i] = j > 0 ? fmaf(decay(since, a2[i]), first[i], left[i]) : first[i];
       if (part.te < TB) {
 #pragma unroll
         for (int e = 0; e < EV; ++e) {
-          const float d = mine ? softplus(kd.get(e) + part.bias[e]) : 0.0f, z = kz.get(e);
-          step[part.te][part.ce + e] = d;
-          input[part.te][part.ce + e] = mine ? d * kx.get(e) : 0.0f;
-          grad[part.te][part.ce + e] = mine ? ko.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
+          const float d = mine ? softplus(rd.get(e) + part.bias[e]) : 0.0f, z = rz.get(e);
+          step[buf][part.te][part.ce + e] = d;
+          input[buf][part.te][part.ce + e] = mine ? d * rx.get(e) : 0.0f;
+          grad[buf][part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
         }
       }
-      if (j > 0) fetch(j - 1);
+    };
+    Raw<EV, T> kx{}, kd{}, ko{}, kz{};
+    auto keep = [&] {
+      kx = rx;
+      kd = rd;
+      ko = ro;
+      kz = rz;
+    };
+    if (tiles > 0) fetch(tiles - 1);
+    if (AHEAD && tiles > 0) {
+      prepare(tiles - 1, 0);
+      keep();
+      if (tiles > 1) fetch(tiles - 2);
       rows.settle();
       __syncthreads();
+    }
+    for (int j = tiles - 1, buf = 0; j >= 0; --j) {
+      const int t0 = j * TB, count = min(TB, s.count - t0);
+      const bool mine = part.live && part.te < count;
+      if (!AHEAD) {
+        prepare(j, 0);
+        keep();
+        if (j > 0) fetch(j - 1);
+        rows.settle();
+        __syncthreads();
+      }
       auto walk = [&](auto whole) {
         constexpr bool ALL = decltype(whole)::value;
         float a[TB][4], m[TB][4];
 #pragma unroll
         for (int t = 0; t < TB; ++t) {
           if (!ALL && t >= count) break;
-          const float dd = step[t][lane], u = input[t][lane];
+          const float dd = step[buf][t][lane], u = input[buf][t][lane];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             a[t][i] = decay(dd, a2[i]);
@@ -229,7 +257,7 @@ __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmPa
 #pragma unroll
         for (int t = TB - 1; t >= 0; --t) {
           if (ALL || t < count) {
-            const float dd = step[t][lane], u = input[t][lane], v = grad[t][lane];
+            const float dd = step[buf][t][lane], u = input[buf][t][lane], v = grad[buf][t][lane];
             float gb = 0.0f, gm = 0.0f, ch = 0.0f, over[8];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -244,9 +272,9 @@ __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmPa
               over[4 + i] = ht * v;
               g[i] *= a[t][i];
             }
-            sum_gb[w][t][lane] = gb;
-            sum_gm[w][t][lane] = gm;
-            if (p.z) sum_ch[w][t][lane] = ch;
+            sum_gb[buf][w][t][lane] = gb;
+            sum_gm[buf][w][t][lane] = gm;
+            if (p.z) sum_ch[buf][w][t][lane] = ch;
             const float one = eight_sums(over);
             if (place == (t & 7)) kept = one;
           }
@@ -259,6 +287,10 @@ __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmPa
       };
       if (count == TB) walk(std::true_type{});
       else walk(std::false_type{});
+      if (AHEAD && j > 0) {
+        prepare(j - 1, buf ^ 1);
+        rows.settle();
+      }
       __syncthreads();
       if (mine) {
         float dx[EV], ddt[EV], dz[EV];
@@ -268,13 +300,13 @@ __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmPa
           __builtin_amdgcn_sched_barrier(0);     // not all partial sums at once: registers
 #pragma unroll 4
           for (int i = 0; i < NW; ++i) {
-            gb += sum_gb[i][part.te][part.ce + e];
-            gm += sum_gm[i][part.te][part.ce + e];
-            if (p.z) ch += sum_ch[i][part.te][part.ce + e];
+            gb += sum_gb[buf][i][part.te][part.ce + e];
+            gm += sum_gm[buf][i][part.te][part.ce + e];
+            if (p.z) ch += sum_ch[buf][i][part.te][part.ce + e];
           }
           const float x = kx.get(e), z = kz.get(e), sz = sigmoid(z);
-          const float up = grad[part.te][part.ce + e];
-          dx[e] = fmaf(step[part.te][part.ce + e], gb, skip[e] * up);
+          const float up = grad[buf][part.te][part.ce + e];
+          dx[e] = fmaf(step[buf][part.te][part.ce + e], gb, skip[e] * up);
           ddt[e] = sigmoid(kd.get(e) + part.bias[e]) * fmaf(x, gb, gm * 0.69314718f);   // A = a2 / log2 e
           dskip[e] = fmaf(up, x, dskip[e]);
           dbias[e] += ddt[e];
@@ -287,7 +319,12 @@ __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmPa
       dxs.move(-1);
       dds.move(-1);
       dzs.move(-1);
-      // What a thread reads of step and grad here, it alone writes in the next tile.
+      // What a thread reads of step and grad here, it alone writes in a later tile.
+      if (AHEAD) {
+        keep();
+        if (j > 1) fetch(j - 2);
+        buf ^= 1;
+      }
     }
     if (s.begins() && p.h_out && live)
       *reinterpret_cast<f32x4*>(p.h_out + state) = f32x4{g[0], g[1], g[2], g[3]};
@@ -302,8 +339,8 @@ __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmPa
   if (part.te < TB) {
 #pragma unroll
     for (int e = 0; e < EV; ++e) {
-      step[part.te][part.ce + e] = dskip[e];
-      input[part.te][part.ce + e] = dbias[e];
+      step[0][part.te][part.ce + e] = dskip[e];
+      input[0][part.te][part.ce + e] = dbias[e];
     }
   }
   __syncthreads();
@@ -311,8 +348,8 @@ __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmPa
     float a = 0.0f, b = 0.0f;
 #pragma unroll
     for (int t = 0; t < TB; ++t) {
-      a += step[t][lane];
-      b += input[t][lane];
+      a += step[0][t][lane];
+      b += input[0][t][lane];
     }
     sums[int64_t(p.D) * S + c] = a;
     sums[int64_t(p.D) * (S + 1) + c] = b;
