@@ -30,7 +30,9 @@ template <int S, typename T>
 __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
   typedef Part<S, T> P;
   constexpr int TB = P::TB, EV = P::EV;
-  __shared__ __attribute__((aligned(16))) float step[TB][64], input[TB][64], grad[TB][64];
+  constexpr bool AHEAD = S > 16;
+  constexpr int NB = AHEAD ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) float step[NB][TB][64], input[NB][TB][64], grad[NB][TB][64];
   const int f = blockIdx.x / p.blocks, c0 = int(blockIdx.x % p.blocks) * 64;
   const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, f);
   if (s.idle) return;
@@ -59,31 +61,41 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
     os.move(1);
     zs.move(1);
   };
-  fetch(0);
-  for (int j = 0; j * TB < s.count; ++j) {
+  TileRows<TB, true, T> rows;
+  auto prepare = [&](int j, int buf) {
     const int count = min(TB, s.count - j * TB);
     const bool mine = part.live && part.te < count;
-    TileRows<TB, true, T> rows;
     if (count == TB) rows.load(bp, p.b_stride, cp, p.c_stride);
+    if (part.te < TB) {
+#pragma unroll
+      for (int e = 0; e < EV; ++e) {
+        const float d = mine ? softplus(rd.get(e) + part.bias[e]) : 0.0f, z = rz.get(e);
+        step[buf][part.te][part.ce + e] = d;
+        input[buf][part.te][part.ce + e] = mine ? d * rx.get(e) : 0.0f;
+        grad[buf][part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
+      }
+    }
+    fetch(j + 1);
+    if (count == TB) rows.settle();
+  };
+  if (s.count > 0) fetch(0);
+  if (AHEAD && s.count > 0) {
+    prepare(0, 0);
+    __syncthreads();
+  }
+  for (int j = 0, buf = 0; j * TB < s.count; ++j) {
+    const int count = min(TB, s.count - j * TB);
+    if (!AHEAD) {
+      prepare(j, 0);
+      __syncthreads();
+    }
     if (j > 0 && c < p.D) {
       const int64_t tile = int64_t(f) * p.inner + j - 1;
       *reinterpret_cast<f32x4*>(p.tiles + tile * p.D * S + (int64_t(w) * p.D + c) * 4) = f32x4{h[0], h[1], h[2], h[3]};
       if (w == 0) p.tile_sums[tile * p.D + c] = sum;
     }
-    if (part.te < TB) {
-#pragma unroll
-      for (int e = 0; e < EV; ++e) {
-        const float d = mine ? softplus(rd.get(e) + part.bias[e]) : 0.0f, z = rz.get(e);
-        step[part.te][part.ce + e] = d;
-        input[part.te][part.ce + e] = mine ? d * rx.get(e) : 0.0f;
-        grad[part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
-      }
-    }
-    fetch(j + 1);
-    if (count == TB) rows.settle();
-    __syncthreads();
     auto token = [&](int t, const Four<T>& B, const Four<T>& C) {
-      const float d = step[t][lane], u = input[t][lane], up = grad[t][lane];
+      const float d = step[buf][t][lane], u = input[buf][t][lane], up = grad[buf][t][lane];
       sum += d;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -106,6 +118,10 @@ __global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
     }
     bp += TB * p.b_stride;
     cp += TB * p.c_stride;
+    if (AHEAD) {
+      if ((j + 1) * TB < s.count) prepare(j + 1, buf ^ 1);
+      buf ^= 1;
+    }
     __syncthreads();
   }
   if (p.E && c < p.D) {
@@ -132,8 +148,8 @@ __device__ __forceinline__ int sum_number(int l) {
 // and m_t = a_t . h_{t-1} are held in registers, then come its tokens backwards.
 // With 32 or 64 states LDS is there twice, and the next tile's steps are formed before the barrier that ends a tile's
 // walk: one barrier a tile, and its last part runs beside other waves' next walk (4096 tokens of 2048 x 32 and 1024
-// x 64 channels x states, whole step: 511 -> 493 and 576 -> 540 us).  With 16 a compute unit has three workgroups
-// for that, and it would cost one of them.
+// x 64 channels x states, whole step: 511 -> 493 and 576 -> 540 us; ssm_ends_kernel likewise, 484 and 530).  With 16 a
+// compute unit has three workgroups for that, and it would cost one of them.
 template <int S, typename T>
 __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmParams p) {
   typedef Part<S, T> P;
