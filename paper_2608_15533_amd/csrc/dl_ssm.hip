@@ -6,18 +6,23 @@ namespace dl {
 namespace {
 
 // Tokens whose steps lie in LDS at a time, and whose B (and C) a wave holds in 32 scalar registers: 64
-// do not fit beside the pointers (8192 x 4096 outputs: 229 us instead of 199).
-template <bool OUT, typename T>
-constexpr int tile_tokens = (OUT ? 16 : 32) / int(sizeof(T));
+// do not fit beside the pointers (8192 x 4096 outputs: 229 us instead of 199).  With 64 states a workgroup is 16 waves,
+// and two of them on a compute unit need the registers of eight waves to a SIMD: half as many tokens then (8192 x 1024,
+// both passes: 265 us -> 227; fp32 364 -> 279).  With 32 and 16 that costs more than it gives (236 -> 239, 250 -> 283).
+template <int S, bool OUT, typename T>
+constexpr int tile_tokens = OUT && S > 32 ? 4 : (OUT ? 16 : 32) / int(sizeof(T));
 
 // A workgroup: one stretch, 64 channels; wave w has states 4 w .. 4 w + 3.  OUT: outputs and final
-// states; else E and the sum of d, of stretches that others follow.
+// states; else E and the sum of d, of stretches that others follow.  AHEAD: LDS is there twice, and the next tile's
+// steps are formed before the barrier that ends a tile: one barrier instead of two (with 32 states 250 us, not 237).
 template <int S, bool OUT, typename T>
-__global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
-  constexpr int TILE = tile_tokens<OUT, T>, NW = S / 4, NT = 64 * NW;
+__global__ __launch_bounds__(S * 16, S > 32 ? 8 : 1) void ssm_kernel(SsmParams p) {
+  constexpr int TILE = tile_tokens<S, OUT, T>, NW = S / 4, NT = 64 * NW;
   constexpr int EV = TILE * 64 >= NT ? TILE * 64 / NT : 1, CG = 64 / EV;
-  __shared__ __attribute__((aligned(16))) float step[TILE][64], input[TILE][64];
-  __shared__ __attribute__((aligned(16))) float partial[OUT ? NW : 1][OUT ? TILE : 1][64];
+  constexpr bool AHEAD = OUT && S > 32;
+  constexpr int NB = AHEAD ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) float step[NB][TILE][64], input[NB][TILE][64];
+  __shared__ __attribute__((aligned(16))) float partial[NB][OUT ? NW : 1][OUT ? TILE : 1][64];
   const int f = blockIdx.x / p.blocks, c0 = int(blockIdx.x % p.blocks) * 64;
   const Stretch s = find_stretch(p.cu, p.seq_slot, p.n, p.N, p.B, p.len, f);
   if (s.idle || (!OUT && s.ends())) return;
@@ -63,36 +68,52 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
     ds.move(1);
     zs.move(1);
   };
-  fetch(0);
-  for (int j = 0; j * TILE < s.count; ++j) {
+  TileRows<TILE, OUT, T> rows;
+  Raw<EV, T> kx{}, kz{};                   // this thread's rows of the tile before
+  auto prepare = [&](int j, int buf) {
     const int count = min(TILE, s.count - j * TILE);
     const bool mine = le && te < count;
-    float x[EV], z[EV];
-    TileRows<TILE, OUT, T> rows;
     if (count == TILE) rows.load(bp, p.b_stride, cp, p.c_stride);
-    widen_row(rx, x);
-    widen_row(rz, z);
     if (te < TILE) {
 #pragma unroll
       for (int e = 0; e < EV; ++e) {
         const float d = mine ? softplus(rd.get(e) + bias[e]) : 0.0f;
-        step[te][ce + e] = d;
-        input[te][ce + e] = mine ? d * x[e] : 0.0f;
+        step[buf][te][ce + e] = d;
+        input[buf][te][ce + e] = mine ? d * rx.get(e) : 0.0f;
         total[e] += d;
       }
     }
+  };
+  auto keep = [&](int j) {
+    kx = rx;
+    kz = rz;
     fetch(j + 1);
-    if (count == TILE) rows.settle();
+  };
+  if (s.count > 0) fetch(0);
+  if (AHEAD && s.count > 0) {
+    prepare(0, 0);
+    keep(0);
+    if (s.count >= TILE) rows.settle();
     __syncthreads();
+  }
+  for (int j = 0, buf = 0; j * TILE < s.count; ++j) {
+    const int count = min(TILE, s.count - j * TILE);
+    const bool mine = le && te < count;
+    if (!AHEAD) {
+      prepare(j, 0);
+      keep(j);
+      if (count == TILE) rows.settle();
+      __syncthreads();
+    }
     auto token = [&](int t, const Four<T>& B, const Four<T>& C) {
-      const float d = step[t][lane], u = input[t][lane];
+      const float d = step[buf][t][lane], u = input[buf][t][lane];
       float y = 0.0f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         h[i] = fmaf(decay(d, a2[i]), h[i], u * B.at(i));
         if (OUT) y = i ? fmaf(C.at(i), h[i], y) : C.at(0) * h[0];
       }
-      if (OUT) partial[w][t][lane] = y;
+      if (OUT) partial[buf][w][t][lane] = y;
     };
     if (count == TILE) {
 #pragma unroll
@@ -107,6 +128,11 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
     }
     bp += TILE * p.b_stride;
     cp += TILE * p.c_stride;
+    const bool more = (j + 1) * TILE < s.count;
+    if (AHEAD && more) {
+      prepare(j + 1, buf ^ 1);
+      if (s.count - (j + 1) * TILE >= TILE) rows.settle();
+    }
     __syncthreads();
     if (OUT && mine) {
       float y[EV];
@@ -114,13 +140,18 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
       for (int e = 0; e < EV; ++e) {
         y[e] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) y[e] += partial[i][te][ce + e];
-        y[e] = fmaf(skip[e], x[e], y[e]);
-        if (p.z) y[e] *= z[e] * sigmoid(z[e]);
+        for (int i = 0; i < NW; ++i) y[e] += partial[buf][i][te][ce + e];
+        const float z = kz.get(e);
+        y[e] = fmaf(skip[e], kx.get(e), y[e]);
+        if (p.z) y[e] *= z * sigmoid(z);
       }
       ys.store(y);
     }
     ys.move(1);
+    if (AHEAD) {
+      keep(j + 1);
+      buf ^= 1;
+    }
   }
   if (OUT) {
     if (s.ends() && live) *reinterpret_cast<f32x4*>(p.h_out + state) = f32x4{h[0], h[1], h[2], h[3]};
@@ -130,13 +161,13 @@ __global__ __launch_bounds__(S * 16) void ssm_kernel(SsmParams p) {
   // The sum of d over the stretch: each thread's own tokens, then the tile's tokens in order.
   if (te < TILE) {
 #pragma unroll
-    for (int e = 0; e < EV; ++e) step[te][ce + e] = total[e];
+    for (int e = 0; e < EV; ++e) step[0][te][ce + e] = total[e];
   }
   __syncthreads();
   if (w == 0 && live) {
     float sum = 0.0f;
 #pragma unroll
-    for (int t = 0; t < TILE; ++t) sum += step[t][lane];
+    for (int t = 0; t < TILE; ++t) sum += step[0][t][lane];
     p.sums[int64_t(f) * p.D + c] = sum;
   }
 }
@@ -279,9 +310,9 @@ hipError_t launch(Pass pass, const dl_ssm_desc* d, const SsmParams& p, hipStream
 
 int blocks_of(const dl_ssm_desc* d) { return (d->channels + 63) / 64; }
 
-// Tokens of a stretch: as long as enough waves are left to fill the chip and to even out ragged ends.  Forward, 8192
-// tokens of 4096 channels with 2048, 4096, 8192, 16384 and 32768 waves: 476, 316, 294, 277 and 284 us (an earlier
-// form).  Backward longer ones leave fewer states to join and rows of partial sums: 4096 tokens of 4096 x 16, 2048 x
+// Tokens of a stretch: as long as enough waves are left to fill the chip and to even out ragged ends (the long ones'
+// figures are an earlier form's).  Forward, 8192
+// tokens of 4096 channels with 2048, 4096, 8192, 16384 and 32768 waves: 476, 316, 294, 277 and 284 us.  Backward longer ones leave fewer states to join and rows of partial sums: 4096 tokens of 4096 x 16, 2048 x
 // 32 and 1024 x 64 channels x states, whole step, with 32, 64 and 128 tokens 513, 485, 481; 545, 513, 508; 649, 602,
 // 572 us; but 777 tokens of 200 channels 58, 79, 98 us.  16 where 32 tokens leave fewer than 2048 waves: those 777
 // tokens 47 us, 64 of 4096 channels forward 14 us instead of 18; where 32 leave 4000, 500 tokens of 1024 x 64 would

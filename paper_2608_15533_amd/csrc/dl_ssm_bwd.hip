@@ -25,9 +25,11 @@ struct Part {
 };
 
 // E, F and the sum of d of a stretch, 64 channels; wave w has states 4 w .. 4 w + 3.  On the way, before
-// every tile but the first, what the stretch has left so far and the sum of d: the gradients start there.
+// every tile but the first, what the stretch has left so far and the sum of d: the gradients start there.  Registers
+// for eight waves to a SIMD let two workgroups of 16 waves share a compute unit (a step of 1024 x 64 channels x
+// states 502 -> 483 us).
 template <int S, typename T>
-__global__ __launch_bounds__(S * 16) void ssm_ends_kernel(SsmParams p) {
+__global__ __launch_bounds__(S * 16, S > 16 ? 8 : 1) void ssm_ends_kernel(SsmParams p) {
   typedef Part<S, T> P;
   constexpr int TB = P::TB, EV = P::EV;
   constexpr bool AHEAD = S > 16;
@@ -148,7 +150,7 @@ __device__ __forceinline__ int sum_number(int l) {
 // and m_t = a_t . h_{t-1} are held in registers, then come its tokens backwards.
 // With 32 or 64 states LDS is there twice, and the next tile's steps are formed before the barrier that ends a tile's
 // walk: one barrier a tile, and its last part runs beside other waves' next walk (4096 tokens of 2048 x 32 and 1024
-// x 64 channels x states, whole step: 511 -> 493 and 576 -> 540 us; ssm_ends_kernel likewise, 484 and 530).  With 16 a
+// x 64 channels x states, whole step: 511 -> 493 and 576 -> 540 us; ssm_ends_kernel likewise, 485 and 530).  With 16 a
 // compute unit has three workgroups for that, and it would cost one of them.
 template <int S, typename T>
 __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmParams p) {
