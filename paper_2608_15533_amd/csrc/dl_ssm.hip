@@ -311,12 +311,12 @@ hipError_t launch(Pass pass, const dl_ssm_desc* d, const SsmParams& p, hipStream
 int blocks_of(const dl_ssm_desc* d) { return (d->channels + 63) / 64; }
 
 // Tokens of a stretch: as long as enough waves are left to fill the chip and to even out ragged ends (the long ones'
-// figures are an earlier form's).  Forward, 8192
-// tokens of 4096 channels with 2048, 4096, 8192, 16384 and 32768 waves: 476, 316, 294, 277 and 284 us.  Backward longer ones leave fewer states to join and rows of partial sums: 4096 tokens of 4096 x 16, 2048 x
-// 32 and 1024 x 64 channels x states, whole step, with 32, 64 and 128 tokens 513, 485, 481; 545, 513, 508; 649, 602,
-// 572 us; but 777 tokens of 200 channels 58, 79, 98 us.  16 where 32 tokens leave fewer than 2048 waves: those 777
-// tokens 47 us, 64 of 4096 channels forward 14 us instead of 18; where 32 leave 4000, 500 tokens of 1024 x 64 would
-// take 35 instead of 29.  Up to 32 tokens stay whole, forward in one kernel: 9 us, 14 in two parts.
+// figures are an earlier form's).  Forward, 8192 tokens of 4096 channels with 2048, 4096, 8192, 16384 and 32768 waves:
+// 476, 316, 294, 277 and 284 us.  Backward longer ones leave fewer states to join and rows of partial sums: 4096
+// tokens of 4096 x 16, 2048 x 32 and 1024 x 64 channels x states, whole step, with 32, 64 and 128 tokens 513, 485, 481;
+// 545, 513, 508; 649, 602, 572 us; but 777 tokens of 200 channels 58, 79, 98 us.  16 where 32 tokens leave fewer than
+// 2048 waves: those 777 tokens 47 us, 64 of 4096 channels forward 14 us instead of 18; where 32 leave 4000, 500 tokens
+// of 1024 x 64 would take 35 instead of 29.  Up to 32 tokens stay whole, forward in one kernel: 9 us, 14 in two parts.
 int stretch_len(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
   const int64_t waves = int64_t(blocks_of(d)) * (d->states / 4), least = backward ? 8192 : 16384;
   int64_t len = tokens > 32 ? 16 : 32;
