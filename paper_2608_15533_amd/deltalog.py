@@ -456,15 +456,29 @@ class ChunkTables:
         i32 = dict(dtype=torch.int32, device=device)
         self.n, self.tokens = int(n), int(tokens)
         self.num_slots = max(self.n, 1) if num_slots is None else int(num_slots)
-        self.cu_tokens = torch.zeros((self.n + 1,), **i32)
+        self._words = torch.zeros((2 * self.n + 1,), **i32)
+        self.cu_tokens, self.seq_slot = self._words[:self.n + 1], self._words[self.n + 1:]
         self.cu_chunks = torch.zeros((self.n + 1,), **i32)
         self.chunks = torch.zeros((self.tokens // DL_CHUNK + self.n, 4), **i32)
         self.row_slot = torch.zeros((self.tokens,), **i32)
-        self.seq_slot = torch.zeros((self.n,), **i32)
         self.order = torch.zeros((self.n,), **i32)
         self.err = torch.zeros((1,), **i32)
         self.struct = dl_tables(_ptr(self.cu_tokens), _ptr(self.cu_chunks), _ptr(self.chunks),
                                 _ptr(self.row_slot), _ptr(self.seq_slot), _ptr(self.order))
+
+    def kept(self):
+        """What the operators around a recurrence read of these tables, copied on the current
+        stream: filling the tables again leaves it as it is."""
+        return _KeptTables(self)
+
+
+class _KeptTables:
+    def __init__(self, tables):
+        self.n, self.tokens, self.num_slots = tables.n, tables.tokens, tables.num_slots
+        self.err = tables.err
+        words = tables._words + 0            # a kernel, in a captured graph too
+        self.cu_tokens, self.seq_slot = words[:self.n + 1], words[self.n + 1:]
+        self.struct = dl_tables(_ptr(self.cu_tokens), None, None, None, _ptr(self.seq_slot), None)
 
 
 class Grads:

@@ -2,6 +2,9 @@
 ``delta_scan`` (``dl_prefill`` and ``dl_prefill_backward`` as one torch.autograd function),
 ``short_conv``, ``selective_scan`` and ``qk_norm`` likewise.
 
+Tables that are passed in may be filled again once a call has been made, for the next batch: a call's
+gradients go by the sequences that it had.
+
 A training step may be captured into a graph, its forward and backward together.  No graph of an
 earlier eager step may still hold the same leaves then: autograd would join the captured stream with
 the stream of that step, which ends the capture and may end the process."""
@@ -65,16 +68,22 @@ def delta_scan(op, q, k, v, lam=None, beta=None, u=None, S0=None, lens=None, sta
                        u if ids == D.DL_OP_RWKV6 else None, S0)
 
 def _batch(x, lens):
-    """(tables of the packed rows x, their sequences): ``lens`` [n] int32 on the device, None (one
-    sequence of all rows) or tables that the caller has built for these rows already."""
+    """(tables of the packed rows x, their slots, whether the caller built them): ``lens`` [n] int32 on
+    the device, None (one sequence of all rows) or tables that the caller has built for these rows already."""
     N = x.shape[0]
     if isinstance(lens, D.ChunkTables):
-        return lens, lens.num_slots
+        return lens, lens.num_slots, True
     if lens is None:
         lens = torch.full((1,), N, dtype=torch.int32, device=x.device)
     tables = D.ChunkTables(lens.numel(), N, device=x.device)
     D.dl_chunk_tables(lens, tables)
-    return tables, lens.numel()
+    return tables, lens.numel(), False
+
+
+def _for_backward(ctx, tables, given):
+    """The tables a call's gradients go by.  Those that the caller has built (``given``) may be filled
+    again, for the next batch, before the gradients are asked for."""
+    return tables.kept() if given and any(ctx.needs_input_grad) else tables
 
 
 def _type(x, name):
@@ -90,12 +99,12 @@ def _dense(t):
 
 class _Conv(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, desc, tables, x, w, bias, s):
+    def forward(ctx, desc, tables, given, x, w, bias, s):
         rows = D.ConvRows(desc, tables.tokens, x, w, bias)
         y = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
         out = torch.zeros((desc.num_slots, desc.width - 1, desc.channels), dtype=x.dtype, device=x.device)
         D.dl_conv_prefill(desc, s, out, rows, y, tables)
-        ctx.desc, ctx.tables = desc, tables
+        ctx.desc, ctx.tables = desc, _for_backward(ctx, tables, given)
         ctx.save_for_backward(x, w, bias, s)
         return y, out
 
@@ -108,7 +117,7 @@ class _Conv(torch.autograd.Function):
         grads = D.ConvGrads(desc, rows, s)
         ws = D.conv_workspace(desc, tables.n, tables.tokens, device=x.device)
         D.dl_conv_backward(desc, s, rows, dy.contiguous(), _dense(ds), grads, tables, ws)
-        return None, None, grads.dx, grads.dw, grads.dbias, grads.ds
+        return None, None, None, grads.dx, grads.dw, grads.dbias, grads.ds
 
 
 def short_conv(x, w, bias=None, s0=None, lens=None, activation="silu"):
@@ -119,20 +128,20 @@ def short_conv(x, w, bias=None, s0=None, lens=None, activation="silu"):
     s0 [n,W-1,D] the inputs before each sequence (None: zeros).  Returns (y [N,D], the last W - 1 inputs
     [n,W-1,D]); y and its gradients are 0 in rows behind the last sequence.  Gradients once; a call keeps its inputs and
     nothing else."""
-    tables, n = _batch(x, lens)
+    tables, n, given = _batch(x, lens)
     desc = D.make_conv_desc(n, x.shape[1], w.shape[1], _type(x, "x"), activation)
-    return _Conv.apply(desc, tables, x, w, bias, s0)
+    return _Conv.apply(desc, tables, given, x, w, bias, s0)
 
 
 class _Ssm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, desc, tables, x, dt, A, Bm, Cm, skip, dt_bias, z, h0):
+    def forward(ctx, desc, tables, given, x, dt, A, Bm, Cm, skip, dt_bias, z, h0):
         rows = D.SsmRows(desc, tables.tokens, x, dt, A, Bm, Cm, skip, dt_bias, z)
         y = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
         h = torch.zeros((desc.num_slots, desc.channels, desc.states), device=x.device)
         ws = D.ssm_workspace(desc, tables.n, tables.tokens, device=x.device)
         D.dl_ssm_prefill(desc, h0, h, rows, y, tables, ws)
-        ctx.desc, ctx.tables = desc, tables
+        ctx.desc, ctx.tables = desc, _for_backward(ctx, tables, given)
         ctx.save_for_backward(x, dt, A, Bm, Cm, skip, dt_bias, z, h0)
         return y, h
 
@@ -145,7 +154,7 @@ class _Ssm(torch.autograd.Function):
         g = D.SsmGrads(desc, rows, h0)
         ws = D.ssm_workspace(desc, tables.n, tables.tokens, backward=True, device=x.device)
         D.dl_ssm_backward(desc, h0, rows, dy.contiguous(), _dense(dh), g, tables, ws)
-        return (None, None, g.dx, g.ddt, g.dA, g.dB, g.dC, g.dskip, g.dbias, g.dz, g.ds)
+        return (None, None, None, g.dx, g.ddt, g.dA, g.dB, g.dC, g.dskip, g.dbias, g.dz, g.ds)
 
 
 def selective_scan(x, dt, A, Bm, Cm, skip=None, dt_bias=None, z=None, h0=None, lens=None):
@@ -155,9 +164,9 @@ def selective_scan(x, dt, A, Bm, Cm, skip=None, dt_bias=None, z=None, h0=None, l
     will do); A [D,S], skip [D] and dt_bias [D] in fp32; lens as for ``short_conv``; h0 [n,D,S] fp32
     initial states (None: zeros).  Returns (y [N,D], final states [n,D,S]); y and its gradients are 0 in
     rows behind the last sequence.  Gradients once; a call keeps its inputs and nothing else."""
-    tables, n = _batch(x, lens)
+    tables, n, given = _batch(x, lens)
     desc = D.make_ssm_desc(n, x.shape[1], A.shape[1], _type(x, "x"))
-    return _Ssm.apply(desc, tables, x, dt, A, Bm, Cm, skip, dt_bias, z, h0)
+    return _Ssm.apply(desc, tables, given, x, dt, A, Bm, Cm, skip, dt_bias, z, h0)
 
 
 class _QkNorm(torch.autograd.Function):
@@ -168,7 +177,7 @@ class _QkNorm(torch.autograd.Function):
         shape = (n, desc.heads * desc.rep, desc.head_dim)
         qo, ko = (torch.zeros(shape, dtype=t.dtype, device=t.device) for t in (q, k))
         D.dl_qk_norm(desc, rows, qo, ko)
-        ctx.desc, ctx.tables = desc, tables
+        ctx.desc, ctx.tables = desc, None if tables is None else _for_backward(ctx, tables, True)
         ctx.save_for_backward(q, k, pos, freq, wq, wk)
         return qo, ko
 
