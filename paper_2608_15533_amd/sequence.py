@@ -138,7 +138,7 @@ class _Ssm(torch.autograd.Function):
     def forward(ctx, desc, tables, given, x, dt, A, Bm, Cm, skip, dt_bias, z, h0):
         rows = D.SsmRows(desc, tables.tokens, x, dt, A, Bm, Cm, skip, dt_bias, z)
         y = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
-        h = torch.zeros((desc.num_slots, desc.channels, desc.states), device=x.device)
+        h = torch.zeros((desc.num_slots, desc.channels, desc.states), dtype=torch.float32, device=x.device)
         ws = D.ssm_workspace(desc, tables.n, tables.tokens, device=x.device)
         D.dl_ssm_prefill(desc, h0, h, rows, y, tables, ws)
         ctx.desc, ctx.tables = desc, _for_backward(ctx, tables, given)

@@ -1,5 +1,5 @@
 """The torch functions of the operators around a recurrence in a training program: tables filled again while
-earlier calls wait for their gradients."""
+earlier calls wait for their gradients, other default dtypes."""
 
 import pytest
 import torch
@@ -117,3 +117,26 @@ def test_tables_filled_in_a_graph(op):
         torch.cuda.synchronize()
         for k, o, w in zip(held, got, want):
             assert torch.equal(o, w), k
+
+
+# ------------------------------------------------------------------ default dtypes
+@pytest.mark.parametrize("default", [BF16, torch.float64], ids=["bf16", "f64"])
+@pytest.mark.parametrize("op", ["conv", "ssm", "qk"])
+def test_another_default_dtype(op, default):
+    """torch's default dtype is no input: outputs and gradients are bit for bit those under fp32."""
+    x = make(op, 1)
+    x["lens"] = i32([60, 0, 53, 0])
+
+    def step():
+        t = leaves(x, LEAVES[op])
+        out = call(op, t, x, None if op == "qk" else x["lens"])
+        return out + torch.autograd.grad(out, list(t.values()), [torch.ones_like(o) for o in out])
+
+    want = step()
+    torch.set_default_dtype(default)
+    try:
+        got = step()
+    finally:
+        torch.set_default_dtype(F32)
+    for g, w in zip(got, want):
+        assert g.dtype == w.dtype and torch.equal(g, w)
