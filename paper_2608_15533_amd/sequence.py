@@ -86,6 +86,18 @@ def _for_backward(ctx, tables, given):
     return tables.kept() if given and any(ctx.needs_input_grad) else tables
 
 
+def _states(s, given, shape, dtype, device):
+    """The buffer of a call's final states.  Tables of the caller's may have slots that no sequence has:
+    their states pass through."""
+    return s.clone() if given and s is not None else torch.zeros(shape, dtype=dtype, device=device)
+
+
+def _state_grads(grads, ds, given):
+    """The gradients of the initial states before the call: of slots that pass through, those behind them."""
+    if given and grads.ds is not None and ds is not None:
+        grads.ds.copy_(ds)
+
+
 def _type(x, name):
     in_dtype = {torch.bfloat16: "bf16", torch.float32: "f32"}.get(x.dtype)
     if in_dtype is None:
@@ -102,9 +114,9 @@ class _Conv(torch.autograd.Function):
     def forward(ctx, desc, tables, given, x, w, bias, s):
         rows = D.ConvRows(desc, tables.tokens, x, w, bias)
         y = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
-        out = torch.zeros((desc.num_slots, desc.width - 1, desc.channels), dtype=x.dtype, device=x.device)
+        out = _states(s, given, (desc.num_slots, desc.width - 1, desc.channels), x.dtype, x.device)
         D.dl_conv_prefill(desc, s, out, rows, y, tables)
-        ctx.desc, ctx.tables = desc, _for_backward(ctx, tables, given)
+        ctx.desc, ctx.tables, ctx.given = desc, _for_backward(ctx, tables, given), given
         ctx.save_for_backward(x, w, bias, s)
         return y, out
 
@@ -116,6 +128,7 @@ class _Conv(torch.autograd.Function):
         rows = D.ConvRows(desc, tables.tokens, x, w, bias)
         grads = D.ConvGrads(desc, rows, s)
         ws = D.conv_workspace(desc, tables.n, tables.tokens, device=x.device)
+        _state_grads(grads, ds, ctx.given)
         D.dl_conv_backward(desc, s, rows, dy.contiguous(), _dense(ds), grads, tables, ws)
         return None, None, None, grads.dx, grads.dw, grads.dbias, grads.ds
 
@@ -124,10 +137,10 @@ def short_conv(x, w, bias=None, s0=None, lens=None, activation="silu"):
     """The short causal convolution of every channel over packed sequences.
 
     x [N,D] in bf16 or fp32 (columns of a wider tensor will do), w [D,W] and bias [D] in fp32; lens [n]
-    int32 on the device (None: one sequence), or ``ChunkTables`` of the batch (states are then by slot);
-    s0 [n,W-1,D] the inputs before each sequence (None: zeros).  Returns (y [N,D], the last W - 1 inputs
-    [n,W-1,D]); y and its gradients are 0 in rows behind the last sequence.  Gradients once; a call keeps its inputs and
-    nothing else."""
+    int32 on the device (None: one sequence), or ``ChunkTables`` of the batch (states are then by slot, those of
+    slots without a sequence pass through); s0 [n,W-1,D] the inputs before each sequence (None: zeros).
+    Returns (y [N,D], the last W - 1 inputs [n,W-1,D]); y and its gradients are 0 in rows behind the last
+    sequence.  Gradients once; a call keeps its inputs and its tables and nothing else."""
     tables, n, given = _batch(x, lens)
     desc = D.make_conv_desc(n, x.shape[1], w.shape[1], _type(x, "x"), activation)
     return _Conv.apply(desc, tables, given, x, w, bias, s0)
@@ -138,10 +151,10 @@ class _Ssm(torch.autograd.Function):
     def forward(ctx, desc, tables, given, x, dt, A, Bm, Cm, skip, dt_bias, z, h0):
         rows = D.SsmRows(desc, tables.tokens, x, dt, A, Bm, Cm, skip, dt_bias, z)
         y = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
-        h = torch.zeros((desc.num_slots, desc.channels, desc.states), dtype=torch.float32, device=x.device)
+        h = _states(h0, given, (desc.num_slots, desc.channels, desc.states), torch.float32, x.device)
         ws = D.ssm_workspace(desc, tables.n, tables.tokens, device=x.device)
         D.dl_ssm_prefill(desc, h0, h, rows, y, tables, ws)
-        ctx.desc, ctx.tables = desc, _for_backward(ctx, tables, given)
+        ctx.desc, ctx.tables, ctx.given = desc, _for_backward(ctx, tables, given), given
         ctx.save_for_backward(x, dt, A, Bm, Cm, skip, dt_bias, z, h0)
         return y, h
 
@@ -153,6 +166,7 @@ class _Ssm(torch.autograd.Function):
         rows = D.SsmRows(desc, tables.tokens, x, dt, A, Bm, Cm, skip, dt_bias, z)
         g = D.SsmGrads(desc, rows, h0)
         ws = D.ssm_workspace(desc, tables.n, tables.tokens, backward=True, device=x.device)
+        _state_grads(g, dh, ctx.given)
         D.dl_ssm_backward(desc, h0, rows, dy.contiguous(), _dense(dh), g, tables, ws)
         return (None, None, None, g.dx, g.ddt, g.dA, g.dB, g.dC, g.dskip, g.dbias, g.dz, g.ds)
 
@@ -163,7 +177,7 @@ def selective_scan(x, dt, A, Bm, Cm, skip=None, dt_bias=None, z=None, h0=None, l
     x, dt and z (the gate; None: none) [N,D], Bm and Cm [N,S] in bf16 or fp32 (columns of a wider tensor
     will do); A [D,S], skip [D] and dt_bias [D] in fp32; lens as for ``short_conv``; h0 [n,D,S] fp32
     initial states (None: zeros).  Returns (y [N,D], final states [n,D,S]); y and its gradients are 0 in
-    rows behind the last sequence.  Gradients once; a call keeps its inputs and nothing else."""
+    rows behind the last sequence.  Gradients once; a call keeps its inputs and its tables and nothing else."""
     tables, n, given = _batch(x, lens)
     desc = D.make_ssm_desc(n, x.shape[1], A.shape[1], _type(x, "x"))
     return _Ssm.apply(desc, tables, given, x, dt, A, Bm, Cm, skip, dt_bias, z, h0)

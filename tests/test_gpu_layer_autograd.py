@@ -1,5 +1,5 @@
 """The torch functions of the operators around a recurrence in a training program: tables filled again while
-earlier calls wait for their gradients, other default dtypes."""
+earlier calls wait for their gradients, other default dtypes, slots without a sequence."""
 
 import pytest
 import torch
@@ -140,3 +140,84 @@ def test_another_default_dtype(op, default):
         torch.set_default_dtype(F32)
     for g, w in zip(got, want):
         assert g.dtype == w.dtype and torch.equal(g, w)
+
+
+# ------------------------------------------------------------------ slots without a sequence
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("op", ["conv", "ssm"])
+@pytest.mark.parametrize("lens,slots", [([70, 0, 43], [4, 0, 2]), ([113], [1]), ([0], [3]), ([], [])], ids=str)
+def test_slots_without_a_sequence_pass_through(op, lens, slots, dtype):
+    """Tables of more slots than sequences: the other slots' states come back as they were, and so does their
+    gradient; without initial states they are zero."""
+    from paper_2608_15533_amd import deltalog as D
+    x = dict(make(op, 3, dtype, B=5), lens=lens, slots=slots)
+    rest = [s for s in range(5) if s not in slots]
+    tables = D.ChunkTables(len(lens), 113, num_slots=5)
+    fill(tables, (lens, slots))
+    t = leaves(x, LEAVES[op])
+    y, s = call(op, t, x, tables)
+    got = dict(zip(t, torch.autograd.grad([y, s], list(t.values()), [x["dy"].cuda(), x["ds"].cuda()])))
+    assert torch.equal(s[rest].cpu(), x["s"][rest])
+    assert torch.equal(got["s"][rest].cpu(), x["ds"][rest])
+    if lens:
+        want = (R.conv_expected if op == "conv" else R.ssm_expected)(x)
+        bar = lambda v: R.tol(op, v.dtype)  # noqa: E731
+        N = sum(lens)
+        assert R.rel(y[:N], want["out"][0]) <= bar(y) and torch.all(y[N:] == 0)
+        assert R.rel(s[slots], want["out"][1][slots]) <= bar(s)
+        assert R.rel(got["s"][slots], want["grads"]["s"][slots]) <= bar(s)
+        for k in t:
+            g = got[k][:N] if got[k].shape[0] == 113 else got[k]
+            assert k == "s" or R.rel(g, want["grads"][k]) <= bar(g), k
+    else:
+        assert torch.all(y == 0) and all(torch.all(g == 0) for k, g in got.items() if k != "s")
+    _, s = call(op, dict(t, s=None), x, tables)
+    assert torch.all(s[rest] == 0)
+
+
+@pytest.mark.parametrize("op", ["conv", "ssm"])
+def test_a_sequence_that_is_left_out_leaves_its_slot(op):
+    """A slot that does not exist: its sequence is skipped, every slot that no sequence has passes through."""
+    from paper_2608_15533_amd import deltalog as D
+    x = make(op, 4, B=3)
+    tables = D.ChunkTables(3, 113)
+    fill(tables, ([50, 3, 60], [2, 9, 0]))
+    t = leaves(x, LEAVES[op])
+    y, s = call(op, t, x, tables)
+    (g,) = torch.autograd.grad([y, s], [t["s"]], [x["dy"].cuda(), x["ds"].cuda()])
+    assert tables.err.item() == 1 and torch.all(y[50:53] == 0)
+    assert torch.equal(s[1].cpu(), x["s"][1]) and torch.equal(g[1].cpu(), x["ds"][1])
+    assert not torch.equal(s[0].cpu(), x["s"][0]) and not torch.equal(g[0].cpu(), x["ds"][0])
+
+
+@pytest.mark.parametrize("op", ["conv", "ssm"])
+def test_slots_without_a_sequence_in_a_graph(op):
+    """Captured forward and backward: replays on other slots equal the eager step bit for bit."""
+    from paper_2608_15533_amd import deltalog as D
+    tables, lens, slots = D.ChunkTables(2, 113, num_slots=5), i32([70, 43]), i32([3, 1])
+
+    def step(t):
+        D.dl_chunk_tables(lens, tables, slots=slots)
+        out = call(op, t, None, tables)
+        grads = torch.autograd.grad(out, list(t.values()), [torch.full_like(o, 0.5) for o in out])
+        return [o.detach() for o in out] + list(grads)
+
+    step(leaves(make(op, 0, BF16, B=5), LEAVES[op]))
+    held = leaves(make(op, 1, BF16, B=5), LEAVES[op])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = step(held)
+    for seed, where in enumerate(([3, 1], [0, 4], [2, 3])):
+        slots.copy_(torch.tensor(where))
+        t = leaves(make(op, seed, BF16, B=5), LEAVES[op])
+        want = step(t)
+        with torch.no_grad():
+            for k in held:
+                held[k].copy_(t[k])
+        for o in got:
+            o.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        for o, w in zip(got, want):
+            assert torch.equal(o, w)
