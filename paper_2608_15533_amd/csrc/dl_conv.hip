@@ -26,9 +26,13 @@ struct ConvParams {
 };
 
 // silu(a) and its derivative from s = sigmoid(a).
-__device__ __forceinline__ float silu(float a) { return a * sigmoid(a); }
+template <typename T>
+__device__ __forceinline__ float silu(float a) {
+  return a * sigmoid<T>(a);
+}
+template <typename T>
 __device__ __forceinline__ float silu_slope(float a) {
-  const float s = sigmoid(a);
+  const float s = sigmoid<T>(a);
   return s * (1.0f + a * (1.0f - s));
 }
 
@@ -131,7 +135,7 @@ __global__ __launch_bounds__(64) void conv_kernel(ConvParams p) {
       push(past, row);
       if (SILU) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) a[e] = silu(a[e]);
+        for (int e = 0; e < V; ++e) a[e] = silu<T>(a[e]);
       }
       store_row<V>(y + int64_t(t + i) * p.D, a);
     }
@@ -159,7 +163,7 @@ __global__ __launch_bounds__(64) void conv_step_kernel(ConvParams p) {
   taps.apply(past, row, a);
   if (SILU) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) a[e] = silu(a[e]);
+    for (int e = 0; e < V; ++e) a[e] = silu<T>(a[e]);
   }
   store_row<V>(static_cast<T*>(p.y) + int64_t(i) * p.D + c, a);
 #pragma unroll
@@ -228,7 +232,7 @@ __global__ __launch_bounds__(64) void conv_backward_kernel(ConvParams p) {
           if (SILU) {
             taps.apply(past, row, a);
 #pragma unroll
-            for (int e = 0; e < V; ++e) now[e] *= silu_slope(a[e]);
+            for (int e = 0; e < V; ++e) now[e] *= silu_slope<T>(a[e]);
           }
           if (u < s.count) {
 #pragma unroll

@@ -95,10 +95,20 @@ __device__ __forceinline__ float halves_sum8(float a, float b) {
 
 constexpr float LOG2E = 1.4426950408889634f;
 
-// 1 / (1 + e^-x): 0 and 1 at the infinities.  The exponential's argument is rounded once more than x is, so
-// where e^-x matters this is good to 2^-24 (|x| + 3) of itself; four instructions.
+// What t = x log2 e, as it is rounded, leaves of x: x - t ln 2, to 0.05 2^-24 |x|.  Where that is not a number or
+// large (x beyond all exponents) some number up to 1, which finds a factor of 0.
+__device__ __forceinline__ float left_of(float x, float t) {
+  return __builtin_amdgcn_fmed3f(fmaf(t, -0.69314718f, x), -1.0f, 1.0f);
+}
+
+// 1 / (1 + e^-x): 0 and 1 at the infinities.  The exponential's argument is rounded: alone, that is 1.2 2^-24 |x| of
+// e^-x, less than a bf16 output's rounding by far, so TO = uint16_t leaves it there (four instructions).  TO =
+// float: the derivative s (1 - s) times what the rounding left, and the result is good to (6 + |x| / 16) 2^-24.
+template <typename TO>
 __device__ __forceinline__ float sigmoid(float x) {
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -LOG2E));
+  const float t = x * -LOG2E, s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
+  if constexpr (sizeof(TO) == 2) return s;
+  return fmaf(-fmaf(-s, s, s), left_of(-x, t), s);
 }
 
 // ------------------------------------------------------------------ stretches of sequences

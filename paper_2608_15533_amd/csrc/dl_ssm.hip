@@ -143,7 +143,7 @@ __global__ __launch_bounds__(S * 16, S > 32 ? 8 : 1) void ssm_kernel(SsmParams p
         for (int i = 0; i < NW; ++i) y[e] += partial[buf][i][te][ce + e];
         const float z = kz.get(e);
         y[e] = fmaf(skip[e], kx.get(e), y[e]);
-        if (p.z) y[e] *= z * sigmoid(z);
+        if (p.z) y[e] *= z * sigmoid<T>(z);
       }
       ys.store(y);
     }
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmParams p) {
   if (p.skip) y = fmaf(p.skip[c], x, y);
   if (p.z) {
     const float z = widen(static_cast<const T*>(p.z)[i * p.z_stride + c]);
-    y *= z * sigmoid(z);
+    y *= z * sigmoid<T>(z);
   }
   narrow(static_cast<T*>(p.y) + int64_t(i) * p.D + c, y);
 }

@@ -74,7 +74,7 @@ __global__ __launch_bounds__(S * 16, S > 16 ? 8 : 1) void ssm_ends_kernel(SsmPar
         const float d = mine ? softplus(rd.get(e) + part.bias[e]) : 0.0f, z = rz.get(e);
         step[buf][part.te][part.ce + e] = d;
         input[buf][part.te][part.ce + e] = mine ? d * rx.get(e) : 0.0f;
-        grad[buf][part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
+        grad[buf][part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid<T>(z) : 1.0f) : 0.0f;
       }
     }
     fetch(j + 1);
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmPa
           const float d = mine ? softplus(rd.get(e) + part.bias[e]) : 0.0f, z = rz.get(e);
           step[buf][part.te][part.ce + e] = d;
           input[buf][part.te][part.ce + e] = mine ? d * rx.get(e) : 0.0f;
-          grad[buf][part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid(z) : 1.0f) : 0.0f;
+          grad[buf][part.te][part.ce + e] = mine ? ro.get(e) * (p.z ? z * sigmoid<T>(z) : 1.0f) : 0.0f;
         }
       }
     };
@@ -322,10 +322,10 @@ __global__ __launch_bounds__(S * 16, S == 16 ? 3 : 4) void ssm_grad_kernel(SsmPa
             gm += sum_gm[buf][i][part.te][part.ce + e];
             if (p.z) ch += sum_ch[buf][i][part.te][part.ce + e];
           }
-          const float x = kx.get(e), z = kz.get(e), sz = sigmoid(z);
+          const float x = kx.get(e), z = kz.get(e), sz = sigmoid<T>(z);
           const float up = grad[buf][part.te][part.ce + e];
           dx[e] = fmaf(step[buf][part.te][part.ce + e], gb, skip[e] * up);
-          ddt[e] = sigmoid(kd.get(e) + part.bias[e]) * fmaf(x, gb, gm * 0.69314718f);   // A = a2 / log2 e
+          ddt[e] = sigmoid<T>(kd.get(e) + part.bias[e]) * fmaf(x, gb, gm * 0.69314718f);   // A = a2 / log2 e
           dskip[e] = fmaf(up, x, dskip[e]);
           dbias[e] += ddt[e];
           dz[e] = ko.get(e) * fmaf(skip[e], x, ch) * sz * (1.0f + z * (1.0f - sz));
