@@ -400,7 +400,7 @@ typedef struct {
   int32_t turn;         /* dl_turn                                                      */
   int32_t rot;          /* places that turn: a multiple of 16 up to d; 0 without turn   */
   int32_t in_dtype;     /* dl_dtype of q, k, outputs and their gradients                */
-  float eps;            /* above 0 with a norm                                          */
+  float eps;            /* 2^-126 (the smallest normal fp32 number) or above with a norm */
   float q_scale;
 } dl_qk_desc;
 

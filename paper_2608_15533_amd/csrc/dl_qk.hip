@@ -6,6 +6,8 @@
 // Gradients, g the sum over the rep copies turned back and scaled:  dw = sum g r x,
 // dx = r (w . g) - x c r^3 <w . g, x>.
 // Bound by memory: every head is read once and written rep times.
+#include <float.h>
+
 #include "dl_rows.hpp"
 
 namespace dl {
@@ -276,8 +278,9 @@ int check_desc(const dl_qk_desc* d) {
   if (d->heads < 1 || d->rep < 1 || int64_t(d->heads) * d->rep > DL_MAX_HEADS) return DL_E_SHAPE;
   if (d->turn == DL_TURN_NONE ? d->rot != 0 : d->rot < 16 || d->rot > d->head_dim || d->rot % 16 != 0)
     return DL_E_SHAPE;
-  // Without an eps above 0 a head of zeros has no norm; what is not a number is neither.
-  if (d->norm != DL_NORM_NONE && !(d->eps > 0.0f)) return DL_E_UNSUPPORTED;
+  // Without an eps above 0 a head of zeros has no norm, and the reciprocal root takes one below the normal numbers
+  // for 0; what is not a number is neither.
+  if (d->norm != DL_NORM_NONE && !(d->eps >= FLT_MIN)) return DL_E_UNSUPPORTED;
   if (d->in_dtype != DL_F32 && d->in_dtype != DL_BF16) return DL_E_DTYPE;
   return DL_OK;
 }

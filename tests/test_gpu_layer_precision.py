@@ -143,3 +143,20 @@ def test_ends_of_the_range():
     for y in (c.step().clone(), c.prefill().clone()):
         y = y.cpu()
         assert y[0] == 0 and y[1] == 400 and y[2] == inf and torch.isnan(y[3]) and y[4] == 0
+
+
+@pytest.mark.parametrize("norm", ["l2", "rms"])
+def test_zero_heads_under_the_smallest_eps(norm):
+    """eps = 2^-126: heads of zeros are zero, their gradient is the upper one times eps^-1/2."""
+    from paper_2608_15533_amd import deltalog as D
+    eps = 2.0 ** -126
+    desc = D.make_qk_desc(3, 64, norm, in_dtype="f32", eps=eps)
+    q = torch.zeros(5, 3, 64, device="cuda")
+    rows = D.QkRows(desc, 5, q, q)
+    out = [torch.full_like(q, 7.0) for _ in range(2)]
+    D.dl_qk_norm(desc, rows, *out)
+    assert not any(torch.any(o) for o in out)
+    g, up = D.QkGrads(desc, rows), torch.full_like(q, 2.0 ** -70)
+    D.dl_qk_norm_backward(desc, rows, up, up, g, D.qk_workspace(desc, 5))
+    for d in (g.dq, g.dk):
+        assert torch.all((d * 2.0 ** 7 - 1).abs() <= 4 * EPS)     # 2^63 to a unit in the last place
