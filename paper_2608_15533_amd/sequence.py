@@ -211,7 +211,8 @@ def qk_norm(q, k, pos=None, freq=None, wq=None, wk=None, norm="l2", turn="none",
     """Queries and keys [n,H,d] normalised head by head (``norm`` "l2", "rms" or "none"), weighted by wq
     and wk [d] (fp32), queries scaled by ``q_scale``, the first 2 len(freq) places of every head turned by
     the angles pos freq (``turn`` "halves" or "pairs"; pos [n] int32, freq fp32), every head written
-    ``rep`` times.  ``tables``: rows behind its sequences are left out (0).  Gradients once."""
+    ``rep`` times.  ``tables``: rows behind its sequences are left out (0).  Gradients once, of q, k, wq and wk;
+    freq is a constant, which gets none whatever it requires."""
     rot = 0 if turn == "none" else 2 * freq.numel()
     desc = D.make_qk_desc(q.shape[1], q.shape[2], norm, turn, rot, rep, _type(q, "q"), eps, q_scale)
     return _QkNorm.apply(desc, tables, q, k, pos, freq, wq, wk)

@@ -1,5 +1,5 @@
 """The torch functions of the operators around a recurrence in a training program: tables filled again while
-earlier calls wait for their gradients, other default dtypes, slots without a sequence."""
+earlier calls wait for their gradients, other default dtypes, slots without a sequence, frequencies."""
 
 import pytest
 import torch
@@ -221,3 +221,17 @@ def test_slots_without_a_sequence_in_a_graph(op):
         torch.cuda.synchronize()
         for o, w in zip(got, want):
             assert torch.equal(o, w)
+
+
+# ------------------------------------------------------------------ frequencies
+def test_frequencies_are_constants():
+    """The rotation's frequencies get no gradient, whatever they require; the others' is the same."""
+    x = make("qk", 5)
+    t = leaves(x, LEAVES["qk"] + ("freq",))
+    plain = leaves(x, LEAVES["qk"])
+    from paper_2608_15533_amd import sequence as M
+    out = M.qk_norm(t["q"], t["k"], x["pos"].cuda(), t["freq"], t["wq"], t["wk"], "rms", "halves", rep=2, q_scale=0.3)
+    got = torch.autograd.grad(out, list(t.values()), [torch.ones_like(o) for o in out], allow_unused=True)
+    out = call("qk", plain, x, None)
+    want = torch.autograd.grad(out, list(plain.values()), [torch.ones_like(o) for o in out])
+    assert got[-1] is None and all(torch.equal(g, w) for g, w in zip(got, want))
