@@ -387,7 +387,8 @@ int dl_conv_backward(const dl_conv_desc* desc, const void* s_in, const dl_conv_r
  * the first rot places -- (i, rot/2 + i) for halves, (2i, 2i + 1) for pairs -- turns by the angle
  * pos freq[i] (the product in 64 bits): (a cos - b sin, a sin + b cos).  Every head is written rep
  * times, output heads h rep .. h rep + rep - 1, for recurrences whose heads share keys.  Any rows:
- * prompts, training, one token a slot. */
+ * prompts, training, one token a slot.  What is infinite or NaN stays in its head; a head whose sum of
+ * squares is beyond fp32 has the norm infinity, and comes out 0. */
 typedef enum { DL_NORM_NONE = 0, DL_NORM_L2 = 1, DL_NORM_RMS = 2 } dl_norm;
 typedef enum { DL_TURN_NONE = 0, DL_TURN_HALVES = 1, DL_TURN_PAIRS = 2 } dl_turn;
 
@@ -441,7 +442,8 @@ int dl_qk_norm_backward(const dl_qk_desc* desc, const dl_qk_rows* rows, const vo
  *   h_t = exp(d_t A) . h_{t-1} + d_t x_t B_t,   y_t = (<C_t, h_t> + skip x_t) silu(z_t),
  * A and h_t [S] per channel (A <= 0 forgets; taken at its value), B_t and C_t [S] the same for
  * all channels, skip and z left out where NULL.  Whole sequences are cut into stretches that run
- * side by side: what a sequence's results round to depends on the call's n and tokens.
+ * side by side, of a length that goes by the call's tokens: what a sequence's results round to
+ * depends on how many rows the call has.
  * A value that is infinite or NaN stays in its sequence, and in its channel unless it is one of
  * B or C; an infinite one may come out as NaN, and so may what follows decays above 1 whose product
  * over a sequence's tokens is beyond fp32.  Steps are at most as large as fp32 holds; the
@@ -485,7 +487,10 @@ int dl_ssm_step(const dl_ssm_desc* desc, const float* h_in, float* h_out, const 
                 void* y, const int32_t* slots, int32_t n, hipStream_t stream);
 
 /* Bytes of workspace dl_ssm_prefill (backward == 0) or dl_ssm_prefill and dl_ssm_backward
- * (backward != 0) need; may be 0, and the workspace NULL then.  Writes *bytes. */
+ * (backward != 0) need for this n and these tokens (other ones can need more); may be 0, and the
+ * workspace NULL then.  Large calls: forward some 17 MiB, backward about 0.75 tokens x channels x
+ * states bytes with 16 states and 1.3 with 32 or 64 (4096 tokens of 4096 x 16: 195 MiB; 16384 of
+ * 1024 x 64: 1268 MiB), most of it the states before every tile of 8 (4) tokens.  Writes *bytes. */
 int dl_ssm_workspace_bytes(const dl_ssm_desc* desc, int32_t n, int32_t tokens, int32_t backward,
                            size_t* bytes);
 

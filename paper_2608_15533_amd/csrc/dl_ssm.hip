@@ -6,9 +6,10 @@ namespace dl {
 namespace {
 
 // Tokens whose steps lie in LDS at a time, and whose B (and C) a wave holds in 32 scalar registers: 64
-// do not fit beside the pointers (8192 x 4096 outputs: 229 us instead of 199).  With 64 states a workgroup is 16 waves,
-// and two of them on a compute unit need the registers of eight waves to a SIMD: half as many tokens then (8192 x 1024,
-// both passes: 265 us -> 227; fp32 364 -> 279).  With 32 and 16 that costs more than it gives (236 -> 239, 250 -> 283).
+// do not fit beside the pointers (8192 x 4096 outputs: 229 us instead of 199).  With 64 states a workgroup is 16 waves, and
+// two of them on a compute unit need the registers of eight waves to a SIMD: at most four tokens then, half as many in
+// bf16 and as many as ever in fp32.  With that limit and LDS twice (AHEAD below) 8192 x 1024, both passes, took 227 us
+// instead of 265, fp32 279 instead of 364.  With 32 and 16 states the limit costs more than it gives (236 -> 239, 250 -> 283).
 template <int S, bool OUT, typename T>
 constexpr int tile_tokens = OUT && S > 32 ? 4 : (OUT ? 16 : 32) / int(sizeof(T));
 
@@ -310,14 +311,17 @@ hipError_t launch(Pass pass, const dl_ssm_desc* d, const SsmParams& p, hipStream
 
 int blocks_of(const dl_ssm_desc* d) { return (d->channels + 63) / 64; }
 
-// Tokens of a stretch: as long as enough waves are left to fill the chip and to even out ragged ends (the long ones'
-// figures are an earlier form's).  Forward, 8192 tokens of 4096 channels with 2048, 4096, 8192, 16384 and 32768 waves:
-// 476, 316, 294, 277 and 284 us.  Backward longer ones leave fewer states to join and rows of partial sums: 4096
-// tokens of 4096 x 16, 2048 x 32 and 1024 x 64 channels x states, whole step, with 32, 64 and 128 tokens 513, 485, 481;
-// 545, 513, 508; 649, 602, 572 us; but 777 tokens of 200 channels 58, 79, 98 us.  16 where 32 tokens leave fewer than
-// 2048 waves: those 777 tokens 47 us, 64 of 4096 channels forward 14 us instead of 18; where 32 leave 4000, 500 tokens
-// of 1024 x 64 would take 35 instead of 29.  Up to 32 tokens stay whole, forward in one kernel: 9 us, 14 in two parts.
-int stretch_len(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
+// Tokens of a stretch: as long as the call's tokens leave enough waves to fill the chip and to even out ragged ends,
+// however many sequences they are.  Forward with 2048, 4096, 8192, 16384 and 32768 waves: 8192 tokens of one sequence, 4096
+// channels x 16 states, 394, 283, 254, 247, 254 us; 1024 x 64 588, 260, 224, 227, 250; 12 ragged ones, 6000 tokens of 2048 x 32,
+// 298, 209, 193, 193, 214; 8 of 1024 tokens, 4096 x 16, 337, 250, 240, 229, 240.  Not so where the sequences are waves
+// enough by themselves and a longer stretch leaves nothing to walk twice: 32 of 512 tokens 316, 317, 329, 393, 422; the
+// rule does not look at them.  Backward longer ones leave fewer states to join and rows of partial sums: 4096 tokens
+// in two sequences, 4096 x 16, 2048 x 32 and 1024 x 64, whole step, with 32, 64, 128 and 256 tokens 513, 483, 479, 513;
+// 526, 490, 478, 492; 558, 511, 484, 539 us.  16 where 32 tokens leave fewer than 2048 waves: 777 tokens of 200 channels
+// 47 us, 58 with 32, 64 of 4096 channels forward 14 us instead of 18; where 32 leave 4000, 500 tokens of 1024 x 64 would
+// take 35 instead of 29.  Up to 32 tokens stay whole, forward in one kernel: 9 us, 14 in two parts.
+int stretch_len(const dl_ssm_desc* d, int32_t tokens, bool backward) {
   const int64_t waves = int64_t(blocks_of(d)) * (d->states / 4), least = backward ? 8192 : 16384;
   int64_t len = tokens > 32 ? 16 : 32;
   while (len < (backward ? 256 : tokens) && tokens / (2 * len) * waves >= (len < 32 ? 2048 : least)) len *= 2;
@@ -338,11 +342,11 @@ int check_desc(const dl_ssm_desc* d) {
 
 int check_counts(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
   if (n < 0 || tokens < 0 || n > d->num_slots) return DL_E_SHAPE;
-  const int64_t rows = stretches(n, tokens, stretch_len(d, n, tokens, backward));
+  const int64_t rows = stretches(n, tokens, stretch_len(d, tokens, backward));
   if (!grid_fits(rows * blocks_of(d), d->states * 16)) return DL_E_SHAPE;
   const int64_t groups = (int64_t(d->channels) * d->states + 255) / 256;
   if (!grid_fits(groups * n, 256)) return DL_E_SHAPE;
-  const int64_t pieces = int64_t(stretch_len(d, n, tokens, true)) * 2 * d->states / 256;   // of dB's and dC's sums
+  const int64_t pieces = int64_t(stretch_len(d, tokens, true)) * 2 * d->states / 256;   // of dB's and dC's sums
   return !backward || grid_fits(rows * pieces, 256) ? DL_OK : DL_E_SHAPE;
 }
 
@@ -392,7 +396,7 @@ struct Layout {
   size_t E = 0, F = 0, sums = 0, tiles = 0, tile_sums = 0, part = 0, rows = 0, all = 0;
 };
 Layout layout(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
-  const int len = stretch_len(d, n, tokens, backward);
+  const int len = stretch_len(d, tokens, backward);
   const size_t parts = size_t(stretches(n, tokens, len)), D = size_t(d->channels), S = size_t(d->states);
   Layout l;
   auto take = [&](size_t floats) {
@@ -417,7 +421,7 @@ Layout layout(const dl_ssm_desc* d, int32_t n, int32_t tokens, bool backward) {
 
 void set_workspace(SsmParams& p, const dl_ssm_desc* d, const Layout& l, void* ws, bool backward) {
   char* at = static_cast<char*>(ws);
-  p.len = stretch_len(d, p.n, p.N, backward);
+  p.len = stretch_len(d, p.N, backward);
   p.inner = p.len / ssm_grad_tile(d->states) - 1;
   if (!whole(p.N, p.len)) {
     p.E = reinterpret_cast<float*>(at + l.E);

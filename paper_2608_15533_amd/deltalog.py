@@ -889,7 +889,7 @@ def dl_ssm_step(desc, h_in, h_out, rows, y, slots=None, stream=None):
 
 
 def ssm_workspace(desc, n, tokens, backward=False, device="cuda"):
-    """A device buffer of the size dl_ssm_workspace_bytes names: for dl_ssm_prefill (with
+    """A device buffer of the size dl_ssm_workspace_bytes names for n and tokens (fewer can need more): for dl_ssm_prefill (with
     ``backward``: and dl_ssm_backward)."""
     size = _bytes(_lib.dl_ssm_workspace_bytes, "dl_ssm_workspace_bytes", desc, int(n), int(tokens),
                   int(bool(backward)))

@@ -160,3 +160,20 @@ def test_zero_heads_under_the_smallest_eps(norm):
     D.dl_qk_norm_backward(desc, rows, up, up, g, D.qk_workspace(desc, 5))
     for d in (g.dq, g.dk):
         assert torch.all((d * 2.0 ** 7 - 1).abs() <= 4 * EPS)     # 2^63 to a unit in the last place
+
+
+def test_heads_beyond_fp32_come_out_0():
+    """Values whose squares overflow have the norm infinity; the other heads are as without them."""
+    from paper_2608_15533_amd import deltalog as D
+    desc = D.make_qk_desc(2, 64, "rms", in_dtype="f32")
+    q = torch.ones(3, 2, 64, device="cuda")
+    q[1, 0] = 1e25
+    rows = D.QkRows(desc, 3, q, q)
+    out = [torch.full_like(q, 7.0) for _ in range(2)]
+    D.dl_qk_norm(desc, rows, *out)
+    g, up = D.QkGrads(desc, rows), torch.ones_like(q)
+    D.dl_qk_norm_backward(desc, rows, up, up, g, D.qk_workspace(desc, 3))
+    for o, d in zip(out, (g.dq, g.dk)):
+        assert not torch.any(o[1, 0]) and not torch.any(d[1, 0])
+        o[1, 0] = 1
+        assert torch.all((o - 1).abs() <= 16 * EPS + 1e-6)          # (1 + eps)^-1/2
