@@ -685,15 +685,16 @@ class ConvRows(_Rows):
 
 class ConvGrads:
     """Device buffers for the gradients of one dl_conv_prefill call; ``s``: the states before
-    (None: no gradient of them)."""
+    (None: no gradient of them).  Slots without a sequence hold what ``ds`` holds there (None: 0)."""
 
-    def __init__(self, desc, rows, s=None):
+    def __init__(self, desc, rows, s=None, ds=None):
         x, w, bias = rows.tensors
         self.dx = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
         self.dw = torch.zeros_like(w)
         self.dbias = None if bias is None else torch.zeros_like(bias)
         _optional(s, "s", *_conv_state(desc))
-        self.ds = None if s is None else torch.zeros_like(s)
+        _optional(ds, "ds", *_conv_state(desc))
+        self.ds = None if s is None else torch.zeros_like(s) if ds is None else ds.clone()
         self.n, self.sizes = rows.n, rows.sizes
         self.given = tuple(t is not None for t in rows.tensors)
         self.slots = None if s is None else desc.num_slots
@@ -858,15 +859,16 @@ class SsmRows(_Rows):
 
 class SsmGrads:
     """Device buffers for the gradients of one dl_ssm_prefill call; ``h``: the states before (None:
-    no gradient of them)."""
+    no gradient of them).  Slots without a sequence hold what ``dh`` holds there (None: 0)."""
 
-    def __init__(self, desc, rows, h=None):
+    def __init__(self, desc, rows, h=None, dh=None):
         like = lambda t: None if t is None else torch.zeros(t.shape, dtype=t.dtype,  # noqa: E731
                                                             device=t.device)
         (self.dx, self.ddt, self.dz, self.dB, self.dC, self.dA, self.dskip,
          self.dbias) = map(like, rows.tensors)
         _optional(h, "h", *_ssm_state(desc))
-        self.ds = like(h)
+        _optional(dh, "dh", *_ssm_state(desc))
+        self.ds = like(h) if h is None or dh is None else dh.clone()
         self.n, self.sizes = rows.n, rows.sizes
         self.given = tuple(t is not None for t in rows.tensors)
         self.slots = None if h is None else desc.num_slots
@@ -889,8 +891,8 @@ def dl_ssm_step(desc, h_in, h_out, rows, y, slots=None, stream=None):
 
 
 def ssm_workspace(desc, n, tokens, backward=False, device="cuda"):
-    """A device buffer of the size dl_ssm_workspace_bytes names for n and tokens (fewer can need more): for dl_ssm_prefill (with
-    ``backward``: and dl_ssm_backward)."""
+    """A device buffer of the size dl_ssm_workspace_bytes names for n and tokens (fewer can need more):
+    for dl_ssm_prefill (with ``backward``: and dl_ssm_backward)."""
     size = _bytes(_lib.dl_ssm_workspace_bytes, "dl_ssm_workspace_bytes", desc, int(n), int(tokens),
                   int(bool(backward)))
     return torch.empty((size,), dtype=torch.uint8, device=device)

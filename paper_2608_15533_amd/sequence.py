@@ -88,14 +88,8 @@ def _for_backward(ctx, tables, given):
 
 def _states(s, given, shape, dtype, device):
     """The buffer of a call's final states.  Tables of the caller's may have slots that no sequence has:
-    their states pass through."""
+    their states pass through, and so do their gradients."""
     return s.clone() if given and s is not None else torch.zeros(shape, dtype=dtype, device=device)
-
-
-def _state_grads(grads, ds, given):
-    """The gradients of the initial states before the call: of slots that pass through, those behind them."""
-    if given and grads.ds is not None and ds is not None:
-        grads.ds.copy_(ds)
 
 
 def _type(x, name):
@@ -126,10 +120,10 @@ class _Conv(torch.autograd.Function):
         x, w, bias, s = ctx.saved_tensors
         desc, tables = ctx.desc, ctx.tables
         rows = D.ConvRows(desc, tables.tokens, x, w, bias)
-        grads = D.ConvGrads(desc, rows, s)
+        ds = _dense(ds)
+        grads = D.ConvGrads(desc, rows, s, ds if ctx.given else None)
         ws = D.conv_workspace(desc, tables.n, tables.tokens, device=x.device)
-        _state_grads(grads, ds, ctx.given)
-        D.dl_conv_backward(desc, s, rows, dy.contiguous(), _dense(ds), grads, tables, ws)
+        D.dl_conv_backward(desc, s, rows, dy.contiguous(), ds, grads, tables, ws)
         return None, None, None, grads.dx, grads.dw, grads.dbias, grads.ds
 
 
@@ -164,10 +158,10 @@ class _Ssm(torch.autograd.Function):
         x, dt, A, Bm, Cm, skip, dt_bias, z, h0 = ctx.saved_tensors
         desc, tables = ctx.desc, ctx.tables
         rows = D.SsmRows(desc, tables.tokens, x, dt, A, Bm, Cm, skip, dt_bias, z)
-        g = D.SsmGrads(desc, rows, h0)
+        dh = _dense(dh)
+        g = D.SsmGrads(desc, rows, h0, dh if ctx.given else None)
         ws = D.ssm_workspace(desc, tables.n, tables.tokens, backward=True, device=x.device)
-        _state_grads(g, dh, ctx.given)
-        D.dl_ssm_backward(desc, h0, rows, dy.contiguous(), _dense(dh), g, tables, ws)
+        D.dl_ssm_backward(desc, h0, rows, dy.contiguous(), dh, g, tables, ws)
         return (None, None, None, g.dx, g.ddt, g.dA, g.dB, g.dC, g.dskip, g.dbias, g.dz, g.ds)
 
 

@@ -235,3 +235,24 @@ def test_frequencies_are_constants():
     out = call("qk", plain, x, None)
     want = torch.autograd.grad(out, list(plain.values()), [torch.ones_like(o) for o in out])
     assert got[-1] is None and all(torch.equal(g, w) for g, w in zip(got, want))
+
+
+def test_gradient_buffers_start_from_states_of_the_call():
+    """What slots without a sequence hold has the states' type and shape, or is refused."""
+    from paper_2608_15533_amd import deltalog as D
+    x = L.device(R.conv_inputs([5], 64, 4, BF16, B=3))
+    desc = D.make_conv_desc(3, 64, 4)
+    rows = D.ConvRows(desc, 5, x["x"], x["w"], x["bias"])
+    g = D.ConvGrads(desc, rows, x["s"], x["ds"])
+    assert torch.equal(g.ds, x["ds"]) and g.ds.data_ptr() != x["ds"].data_ptr()
+    for bad in (x["ds"].float(), x["ds"][:2], x["ds"].cpu()):
+        with pytest.raises(ValueError):
+            D.ConvGrads(desc, rows, x["s"], bad)
+    x = L.device(R.ssm_inputs([5], 64, 16, BF16, B=3))
+    desc = D.make_ssm_desc(3, 64, 16)
+    rows = D.SsmRows(desc, 5, x["x"], x["dt"], x["A"], x["B"], x["C"])
+    assert torch.equal(D.SsmGrads(desc, rows, x["s"], x["ds"]).ds, x["ds"])
+    assert D.SsmGrads(desc, rows, None, x["ds"]).ds is None
+    for bad in (x["ds"].to(BF16), x["ds"][:2], x["ds"].cpu()):
+        with pytest.raises(ValueError):
+            D.SsmGrads(desc, rows, x["s"], bad)
