@@ -466,7 +466,7 @@ class ChunkTables:
         self.struct = dl_tables(_ptr(self.cu_tokens), _ptr(self.cu_chunks), _ptr(self.chunks),
                                 _ptr(self.row_slot), _ptr(self.seq_slot), _ptr(self.order))
 
-    def kept(self):
+    def _kept(self):
         """What the operators around a recurrence read of these tables, copied on the current
         stream: filling the tables again leaves it as it is."""
         return _KeptTables(self)

@@ -3,7 +3,8 @@
 ``short_conv``, ``selective_scan`` and ``qk_norm`` likewise.
 
 Tables that are passed in may be filled again once a call has been made, for the next batch: a call's
-gradients go by the sequences that it had.
+gradients go by the sequences that it had.  (A call that is made again, as activation checkpointing does, reads
+its tables again.)
 
 A training step may be captured into a graph, its forward and backward together.  No graph of an
 earlier eager step may still hold the same leaves then: autograd would join the captured stream with
@@ -83,7 +84,7 @@ def _batch(x, lens):
 def _for_backward(ctx, tables, given):
     """The tables a call's gradients go by.  Those that the caller has built (``given``) may be filled
     again, for the next batch, before the gradients are asked for."""
-    return tables.kept() if given and any(ctx.needs_input_grad) else tables
+    return tables._kept() if given and any(ctx.needs_input_grad) else tables
 
 
 def _states(s, given, shape, dtype, device):
